@@ -375,6 +375,154 @@ int32_t dq_quantize_pack(const dq_format* fmt, const float* t_large, int64_t n_r
                          void* hip_stream);
 
 /*
+ * ---- Attention from the raw projections: head norm and rotation, and a paged cache in 8 bits ----
+ *
+ * What a serving loop does around the cache of this library, or instead of it where 8 bits a value are
+ * what it wants: queries and keys are normed and rotated, rows are appended to pages, and ragged batches
+ * of queries (a generated token, drafted ones, whole prompts) attend to them.  Rows are 16-bit values of
+ * the type that `dtype` names.
+ */
+#define DQ_F16 0   /* IEEE binary16 */
+#define DQ_BF16 1  /* bfloat16 */
+
+/* Heads of rows somewhere in memory: channel c of head h of token t of sequence b is
+ * data[b*batch_stride + t*token_stride + h*head_stride + c].  data is 16-byte aligned and the strides are
+ * multiples of 8 elements; batch_stride is ignored where the rows are packed (one batch entry). */
+typedef struct dq_heads {
+  uint16_t* data;
+  int64_t batch_stride, token_stride, head_stride;
+  int32_t heads;
+} dq_heads;
+
+/* RMS norm of a head: x_c * w_c / sqrt(mean(x^2) + eps).  A NULL weight: those heads are not normed. */
+typedef struct dq_head_norm {
+  const uint16_t* q_weight; /* [head_dim], of the rows' type */
+  const uint16_t* k_weight;
+  float eps;
+} dq_head_norm;
+
+/* Position rotation of the first rot_dim channels: pair i turns by positions[axis][token] * inv_freq[i].
+ * The angle is formed in fp64 (far positions keep their phase). */
+typedef struct dq_rotary {
+  const double* inv_freq;      /* f64 [rot_dim / 2], radians per position                             */
+  const int32_t* positions;    /* i32 [axes, position_stride]; a token's column is its place among all
+                                  rows of the call (sequence by sequence); any value.
+                                  NULL (dq_paged_append only, one axis): a token's place in its sequence */
+  const uint8_t* axis_of_pair; /* u8 [rot_dim / 2]: the axis whose position turns pair i (time, height,
+                                  width, ...); NULL with one axis; values >= axes count as the last    */
+  int64_t position_stride;     /* >= the rows of the call where axes > 1                              */
+  int32_t axes;                /* 1..8                                                                */
+  int32_t rot_dim;             /* a multiple of 16, <= head_dim; the channels behind it stay          */
+  int32_t interleaved;         /* 0: pair i is channels (i, i + rot_dim/2); 1: channels (2i, 2i + 1)  */
+} dq_rotary;
+
+/*
+ * Norm and rotation of query and key heads in one pass: out = rotate(norm(x)), computed in fp32 and
+ * rounded once.  head_dim is a multiple of 16 in [32, 256].  q and k each may be NULL (with their
+ * output); an output may be its input itself (same data and strides), otherwise they must not overlap.
+ * norm or rot may be NULL (not both).  The rows of dq_compress_kv and dq_cache_append are such outputs
+ * ([B, H, n, d] is token_stride d, head_stride n*d).
+ */
+int32_t dq_rotate_heads(const dq_heads* q, const dq_heads* q_out, const dq_heads* k, const dq_heads* k_out,
+                        int32_t batch, int32_t tokens, int32_t head_dim, int32_t dtype,
+                        const dq_head_norm* norm, const dq_rotary* rot, void* hip_stream);
+
+#define DQ_CODES_INT8 0 /* code c in [-127, 127] */
+#define DQ_CODES_E4M3 1 /* 8-bit floats, 1-4-3, largest 448 */
+
+/*
+ * A layer's cache in pages of page_tokens (64 or 128) tokens.  A page holds 8-bit codes; a block (page,
+ * kv head) has one step for its keys and one for its values: a code c stands for c * scale.  The tokens
+ * of a sequence's last page stay in 16 bits (its tail) until it is full: token t of a sequence of
+ * length n is code row t % P of page page_table[b][t / P] if t / P < n / P, else tail row t % P.
+ *   k_codes  u8  [pages, H, P, d]         k_scales f32 [pages, H]
+ *   v_codes  u8  [pages, H, P/64, d, 64]  v_scales f32 [pages, H]    (64 tokens, channel by channel)
+ *   k_tail   u16 [slots, H, P, d]
+ *   v_tail   u16 [slots, H, P/64, d, 64]
+ * Quantization of a block x: the inverse step r is Q / max|x| in fp32 (Q = 127 or 448) with the low 12
+ * bits of its significand cleared, scale = 1 / r, code = x * r rounded to nearest even (exact up to that
+ * rounding: x has at most 11 significant bits, r 12).  A block whose largest value is below 2^-100 has scale 1 and
+ * codes 0.  Pages are quantized when they fill, from the 16-bit rows: a page's bits do not depend on how
+ * its rows were cut into calls.
+ * A token whose key or value row holds a value that is not finite is kept as a row of NaN keys and zero
+ * values, and its block, when it fills, gets the key scale NaN and key codes of 0 for that row: every
+ * query that sees the token (the block, once quantized) yields NaN, the others are untouched.
+ */
+typedef struct dq_paged_cache {
+  uint8_t* k_codes;
+  float* k_scales;
+  uint8_t* v_codes;
+  float* v_scales;
+  uint16_t* k_tail;
+  uint16_t* v_tail;
+  int32_t pages, kv_heads, head_dim; /* head_dim 64 or 128; pages * kv_heads * P / 64 < 2^31 */
+  int32_t page_tokens, slots;        /* slots * kv_heads * P / 64 < 2^31 */
+  int32_t dtype, codes;
+} dq_paged_cache;
+
+/*
+ * A ragged batch.  Sequence b owns rows starts[b] .. starts[b+1] - 1 of the packed rows of a call; they are
+ * its LAST tokens: row i of n is token seq_lens[b] - n + i.  The caller counts the lengths (one addition
+ * for all layers of a step) and names the pages.  Entries the kernels cannot use are not followed out of
+ * bounds: rows past `rows`, tokens before 0 or past table_width pages are left out; tokens of a page or
+ * slot that does not exist are dropped by dq_paged_append and make attention yield NaN.
+ */
+typedef struct dq_paged_batch {
+  const int32_t* starts;     /* i32 [batch + 1], ascending; NULL: one row per sequence (rows == batch)  */
+  const int32_t* seq_lens;   /* i32 [batch], tokens with the call's rows included                       */
+  const int32_t* page_table; /* i32 [batch, table_stride], page of the j-th P tokens; only full pages
+                                are read: the entry of the page being filled may be set late            */
+  const int32_t* tail_slots; /* i32 [batch] or NULL (slot b); no two sequences of a call share one      */
+  int32_t batch, rows;
+  int32_t table_width, table_stride;
+} dq_paged_batch;
+
+/*
+ * Append the batch's rows: k and v heads [rows, kv_heads, d] (token_stride, head_stride as they lie in a
+ * fused projection).  Keys are normed and rotated (norm, rot: NULL for rows that are ready), rounded to
+ * 16 bits and buffered or, with the whole of their page, quantized; values go as they are.  q (NULL:
+ * none), [rows, q_heads, d], takes the same norm and rotation in the same launch, into q_out.  One
+ * launch; page_table must name the pages that fill in this call.
+ */
+int32_t dq_paged_append(const dq_paged_cache* cache, const dq_paged_batch* batch, const dq_heads* k,
+                        const dq_heads* v, const dq_heads* q, const dq_heads* q_out,
+                        const dq_head_norm* norm, const dq_rotary* rot, void* hip_stream);
+
+/*
+ * What the cache stands for: tokens first[b] <= t < seq_lens[b] of every sequence as 16-bit rows,
+ * token t of sequence b in row out_starts[b] + t - first[b] of k_out and v_out ([rows, kv_heads, d],
+ * batch->rows of them; batch->starts is not used).  first NULL: from 0.  Codes come as c * scale rounded
+ * once.  The way from 8-bit pages to a DecoQuant cache (dq_compress_kv_blocks) or to another machine.
+ */
+int32_t dq_paged_read(const dq_paged_cache* cache, const dq_paged_batch* batch, const int32_t* first,
+                      const int32_t* out_starts, const dq_heads* k_out, const dq_heads* v_out,
+                      void* hip_stream);
+
+/* Bytes of workspace dq_paged_attention needs (0 on invalid arguments); zero it once before its first
+ * use (dq_workspace_init).  Calls that share it, graphs among them, must be ordered. */
+size_t dq_paged_workspace_bytes(const dq_paged_cache* cache, int32_t batch, int32_t rows, int32_t q_heads,
+                                int32_t max_rows, int32_t max_seq_len);
+
+#define DQ_PAGED_CAUSAL 1u /* row i sees tokens up to its own place (it is among the last n of its sequence) */
+
+/*
+ * out[row, h] = softmax_t(q[row, h] . K[t] * scale) V over the cached tokens of the row's sequence, kv
+ * head h / (q_heads / kv_heads): the batch's rows are the queries (append first, then attend).  Keys
+ * and values are what the cache stands for; fp32 accumulation, one rounding of the result, probabilities
+ * in 16 bits for their product with the values.
+ *   q, out         [rows, q_heads, d]; out may be q
+ *   max_rows       host bound on the rows of any sequence; max_seq_len on seq_lens (longer sequences
+ *                  are cut there); both choose kernel and launch
+ *   window         > 0: a row sees the last `window` tokens up to its own place only (needs causal)
+ *   softmax_scale  <= 0 selects 1/sqrt(d)
+ * A row that sees no token yields zeros.  Rows behind the last sequence's are not written.
+ */
+int32_t dq_paged_attention(const dq_paged_cache* cache, const dq_paged_batch* batch, const dq_heads* q,
+                           const dq_heads* out, int32_t max_rows, int32_t max_seq_len, float softmax_scale,
+                           int32_t window, void* workspace, size_t workspace_bytes, uint32_t flags,
+                           void* hip_stream);
+
+/*
  * Measurement helper: read `bytes` (multiple of 16) from src with 128-bit loads and fold them
  * into sink[0..3] (u32) so the reads cannot be elided.  Gives the achievable read bandwidth
  * that the decode kernel's rate is compared with.

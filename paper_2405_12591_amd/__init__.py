@@ -35,3 +35,14 @@ from .binding import (  # noqa: F401
     stream_read,
     decode_mfma_supported,
 )
+from .paged import (  # noqa: F401
+    Rotary,
+    rotary,
+    rotate_heads,
+    PagedCache,
+    alloc_paged_cache,
+    paged_append,
+    paged_read,
+    paged_workspace,
+    paged_attention,
+)

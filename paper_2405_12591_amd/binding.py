@@ -35,6 +35,7 @@ EXPORTED_SYMBOLS = [
     "dq_compress_workspace_bytes", "dq_compress_kv", "dq_compress_blocks_workspace_bytes", "dq_compress_kv_blocks",
     "dq_compress_kv_ex", "dq_cache_append_workspace_bytes", "dq_cache_append",
     "dq_quantize_pack", "dq_stream_read",
+    "dq_rotate_heads", "dq_paged_append", "dq_paged_read", "dq_paged_workspace_bytes", "dq_paged_attention",
 ]
 
 

@@ -1,0 +1,268 @@
+// Shared pieces of the paged 8-bit cache's kernels: types, argument checks, norm and rotation of a row's
+// piece, codes to and from 32-bit values.
+#pragma once
+#include "dq_common.h"
+
+namespace dq {
+
+typedef uint32_t u32x2 __attribute__((ext_vector_type(2)));
+typedef uint32_t u32x4 __attribute__((ext_vector_type(4)));
+typedef float f32x2 __attribute__((ext_vector_type(2)));
+typedef float f32x4 __attribute__((ext_vector_type(4)));
+typedef float f32x16 __attribute__((ext_vector_type(16)));
+typedef _Float16 f16x2 __attribute__((ext_vector_type(2)));
+typedef _Float16 f16x8 __attribute__((ext_vector_type(8)));
+typedef __bf16 bf16x2 __attribute__((ext_vector_type(2)));
+typedef __bf16 bf16x8 __attribute__((ext_vector_type(8)));
+
+constexpr int kPagedTile = 64;        // tokens of a work tile and of a run of the value layout
+constexpr int kPagedThreads = 256;
+constexpr int kMaxAxes = 8;
+constexpr float kSmallestAmax = 0x1p-100f;   // a block below it is held as zeros (its inverse step would leave fp32)
+
+// ---- argument checks (host) ----
+inline bool heads_ok(const dq_heads* x, bool batched) {
+  return x && x->data && !((uintptr_t)x->data & 15) && x->heads > 0 && x->token_stride >= 0 && x->head_stride >= 0 &&
+         !(x->token_stride & 7) && !(x->head_stride & 7) && (!batched || (x->batch_stride >= 0 && !(x->batch_stride & 7)));
+}
+
+inline bool norm_ok(const dq_head_norm* n) { return !n || (n->eps >= 0.f && !(((uintptr_t)n->q_weight | (uintptr_t)n->k_weight) & 15)); }
+
+inline bool rotary_ok(const dq_rotary* r, int head_dim, long rows, bool positions_needed) {
+  if (!r) return true;
+  if (!r->inv_freq || r->rot_dim <= 0 || r->rot_dim % 16 || r->rot_dim > head_dim) return false;
+  if (r->axes < 1 || r->axes > kMaxAxes || (r->interleaved != 0 && r->interleaved != 1)) return false;
+  if (r->axes > 1 && (!r->axis_of_pair || !r->positions || r->position_stride < rows)) return false;
+  if (positions_needed && !r->positions) return false;
+  return true;
+}
+
+inline bool paged_cache_ok(const dq_paged_cache* c) {
+  if (!c || !c->k_codes || !c->k_scales || !c->v_codes || !c->v_scales || !c->k_tail || !c->v_tail) return false;
+  if (((uintptr_t)c->k_codes | (uintptr_t)c->v_codes | (uintptr_t)c->k_tail | (uintptr_t)c->v_tail) & 15) return false;
+  if (((uintptr_t)c->k_scales | (uintptr_t)c->v_scales) & 3) return false;
+  if (c->head_dim != 64 && c->head_dim != 128) return false;
+  if (c->page_tokens != 64 && c->page_tokens != 128) return false;
+  if (c->dtype != DQ_F16 && c->dtype != DQ_BF16) return false;
+  if (c->codes != DQ_CODES_INT8 && c->codes != DQ_CODES_E4M3) return false;
+  if (c->pages <= 0 || c->kv_heads <= 0 || c->slots <= 0) return false;
+  const long runs = (long)c->kv_heads * (c->page_tokens / kPagedTile);
+  return c->pages * runs < (1l << 31) && c->slots * runs < (1l << 31);
+}
+
+inline bool paged_batch_ok(const dq_paged_batch* b, const dq_paged_cache* c, bool uses_starts) {
+  if (!b || !b->seq_lens || !b->page_table || b->batch <= 0 || b->rows < 0) return false;
+  if (b->table_width <= 0 || b->table_stride < b->table_width) return false;
+  if ((long)b->table_width * c->page_tokens >= (1l << 31) - 256) return false;   // token indexes stay in 32 bits
+  if (uses_starts && !b->starts && b->rows != b->batch) return false;
+  if (!b->tail_slots && b->batch > c->slots) return false;
+  return true;
+}
+
+// ---- the batch (device) ----
+// A sequence's rows and lengths, brought into the bounds of the call.
+struct Sequence {
+  int row0, n;      // its rows
+  int len;          // its tokens, the rows included
+};
+__device__ __forceinline__ Sequence sequence_of(const dq_paged_batch& bt, int page_tokens, int b) {
+  Sequence s;
+  const int lo = bt.starts ? bt.starts[b] : b, hi = bt.starts ? bt.starts[b + 1] : b + 1;
+  s.row0 = min(max(lo, 0), bt.rows);
+  s.n = min(max(hi, s.row0), bt.rows) - s.row0;
+  s.len = min(max(bt.seq_lens[b], 0), bt.table_width * page_tokens);
+  return s;
+}
+
+// Work items dealt to sequences without a scan: sequence b's items start at first(b) = starts[b] / unit + per_seq * b, which
+// leaves it at least rows / unit + per_seq - 1 of them.  The sequence an item belongs to, by bisection.
+__device__ __forceinline__ int item_first(const int32_t* starts, int rows, int b, int mul, int unit, int per_seq) {
+  const long at = starts ? min(max(starts[b], 0), rows) : b;
+  return (int)(at * mul / unit) + per_seq * b;
+}
+__device__ __forceinline__ int item_owner(const int32_t* starts, int rows, int batch, int item, int mul, int unit, int per_seq) {
+  int lo = 0, hi = batch - 1;
+  while (lo < hi) {
+    const int mid = (lo + hi + 1) >> 1;
+    if (item_first(starts, rows, mid, mul, unit, per_seq) <= item) lo = mid; else hi = mid - 1;
+  }
+  return lo;
+}
+
+// ---- 16-bit values ----
+template <typename T> struct Pair;
+template <> struct Pair<_Float16> { typedef f16x2 type; };
+template <> struct Pair<__bf16> { typedef bf16x2 type; };
+
+template <typename T>
+__device__ __forceinline__ void unpack2(uint32_t w, float& a, float& b) {
+  if constexpr (__is_same(T, __bf16)) {
+    a = __builtin_bit_cast(float, w << 16);
+    b = __builtin_bit_cast(float, w & 0xFFFF0000u);
+  } else {
+    const f16x2 h = __builtin_bit_cast(f16x2, w);
+    a = (float)h.x;
+    b = (float)h.y;
+  }
+}
+template <typename T>
+__device__ __forceinline__ uint32_t pack2(float a, float b) {   // to nearest even
+  typename Pair<T>::type h;
+  h.x = (T)a;
+  h.y = (T)b;
+  return __builtin_bit_cast(uint32_t, h);
+}
+template <typename T>
+__device__ __forceinline__ void unpack8(const u32x4& w, float* x) {
+#pragma unroll
+  for (int i = 0; i < 4; ++i) unpack2<T>(w[i], x[2 * i], x[2 * i + 1]);
+}
+template <typename T>
+__device__ __forceinline__ u32x4 pack8(const float* x) {
+  u32x4 w;
+#pragma unroll
+  for (int i = 0; i < 4; ++i) w[i] = pack2<T>(x[2 * i], x[2 * i + 1]);
+  return w;
+}
+
+// Sum / maximum over the 2, 4, 8 or 16 lanes that share a row (aligned groups of neighbours).
+template <int CTRL>
+__device__ __forceinline__ float lane_move(float x) {
+  return __builtin_bit_cast(float, __builtin_amdgcn_update_dpp(0, __builtin_bit_cast(int, x), CTRL, 0xF, 0xF, true));
+}
+template <int LANES, typename Op>
+__device__ __forceinline__ float row_reduce(float x, Op op) {
+  if constexpr (LANES >= 2) x = op(x, lane_move<0xB1>(x));    // neighbour
+  if constexpr (LANES >= 4) x = op(x, lane_move<0x4E>(x));    // other pair of four
+  if constexpr (LANES >= 8) x = op(x, lane_move<0x141>(x));   // other four of eight (mirrored)
+  if constexpr (LANES >= 16) x = op(x, lane_move<0x140>(x));  // other eight of sixteen (mirrored)
+  return x;
+}
+
+// ---- norm and rotation ----
+// A row of D channels is shared by D / 16 lanes ("units"), two pieces of 8 channels each, laid so that a lane
+// holds both channels of every pair it turns: the pieces at 8u and rot/2 + 8u of the rotated channels (pairs
+// 8u .. 8u+7), or 16 neighbours (neighbouring pairs, and the channels that are not rotated).
+struct RowLayout {
+  int at0, at1;     // first channels of the unit's two pieces
+  int pair0;        // first of its eight pairs, or -1
+};
+__device__ __forceinline__ RowLayout row_layout(int unit, int rot_dim, int interleaved) {
+  RowLayout l;
+  const bool turned = 16 * unit < rot_dim;
+  const bool halves = turned && !interleaved;
+  l.at0 = halves ? 8 * unit : 16 * unit;
+  l.at1 = halves ? rot_dim / 2 + 8 * unit : 16 * unit + 8;
+  l.pair0 = turned ? 8 * unit : -1;
+  return l;
+}
+
+// Cosines and sines of a unit's eight pairs for one token.  The angle in turns, p f / (2 pi), is formed in fp64 and
+// loses its whole turns there, so what is left of the largest position (2^31) is off by 2^-22 turns at most;
+// the hardware's sine and cosine take turns and are off by about 2^-20, both far below the 2^-12 of a 16-bit row.
+__device__ __forceinline__ void unit_turns(const dq_rotary& r, const RowLayout& l, long column, int own_place, float* cs, float* sn) {
+#pragma unroll
+  for (int i = 0; i < 8; ++i) {
+    cs[i] = 1.f;
+    sn[i] = 0.f;
+  }
+  if (l.pair0 < 0) return;
+  int p0 = own_place;
+  if (r.positions) p0 = r.positions[column];
+#pragma unroll
+  for (int i = 0; i < 8; ++i) {
+    int p = p0;
+    if (r.axes > 1) p = r.positions[min((int)r.axis_of_pair[l.pair0 + i], r.axes - 1) * r.position_stride + column];
+    const double turns = (double)p * (r.inv_freq[l.pair0 + i] * 0.15915494309189533577);
+    const float f = (float)(turns - __builtin_rint(turns));
+    cs[i] = __builtin_amdgcn_cosf(f);
+    sn[i] = __builtin_amdgcn_sinf(f);
+  }
+}
+
+// x: the unit's 16 channels in fp32, normed and rotated in place.  w: its weights.  LANES lanes share the row.
+template <int LANES>
+__device__ __forceinline__ void norm_unit(float* x, const float* w, float eps, float inv_dim) {
+  float s = 0.f;
+#pragma unroll
+  for (int i = 0; i < 16; ++i) s = __builtin_fmaf(x[i], x[i], s);
+  s = row_reduce<LANES>(s, [](float a, float b) { return a + b; });
+  const float r = 1.0f / sqrtf(s * inv_dim + eps);
+#pragma unroll
+  for (int i = 0; i < 16; ++i) x[i] *= r * w[i];
+}
+__device__ __forceinline__ void turn_unit(float* x, const float* cs, const float* sn, bool interleaved) {
+#pragma unroll
+  for (int i = 0; i < 8; ++i) {
+    const float a = interleaved ? x[2 * i] : x[i], b = interleaved ? x[2 * i + 1] : x[8 + i];
+    const float y = a * cs[i] - b * sn[i], z = a * sn[i] + b * cs[i];
+    if (interleaved) { x[2 * i] = y; x[2 * i + 1] = z; } else { x[i] = y; x[8 + i] = z; }
+  }
+}
+
+// Heads [h0, h1) of one token's row: the thread is the row's unit `unit` of LANES.
+template <typename T, int LANES>
+__device__ __forceinline__ void rotate_row(const uint16_t* in, uint16_t* out, long in_head, long out_head, int h0, int h1, bool live,
+                                           const RowLayout& l, const uint16_t* weight, float eps, float inv_dim, const float* cs,
+                                           const float* sn, bool interleaved) {
+  float w[16];
+  if (weight && live) {
+    unpack8<T>(*reinterpret_cast<const u32x4*>(weight + l.at0), w);
+    unpack8<T>(*reinterpret_cast<const u32x4*>(weight + l.at1), w + 8);
+  }
+  const bool turned = l.pair0 >= 0;
+  u32x4 a = {0, 0, 0, 0}, b = {0, 0, 0, 0};
+  if (live && h0 < h1) {
+    a = *reinterpret_cast<const u32x4*>(in + h0 * in_head + l.at0);
+    b = *reinterpret_cast<const u32x4*>(in + h0 * in_head + l.at1);
+  }
+  for (int h = h0; h < h1; ++h) {
+    float x[16];
+    unpack8<T>(a, x);
+    unpack8<T>(b, x + 8);
+    if (live && h + 1 < h1) {   // the next head's pieces are on their way meanwhile
+      a = *reinterpret_cast<const u32x4*>(in + (h + 1) * in_head + l.at0);
+      b = *reinterpret_cast<const u32x4*>(in + (h + 1) * in_head + l.at1);
+    }
+    if (weight) norm_unit<LANES>(x, w, eps, inv_dim);
+    if (turned) turn_unit(x, cs, sn, interleaved);
+    if (live) {
+      *reinterpret_cast<u32x4*>(out + h * out_head + l.at0) = pack8<T>(x);
+      *reinterpret_cast<u32x4*>(out + h * out_head + l.at1) = pack8<T>(x + 8);
+    }
+  }
+}
+
+// ---- codes ----
+template <bool FP8> constexpr float kQmax = FP8 ? 448.f : 127.f;
+
+// Inverse step of a block: 12 significant bits, so that the product with a 16-bit value is exact in fp32.
+template <bool FP8>
+__device__ __forceinline__ float inverse_step(float amax) {
+  return amax < kSmallestAmax ? 0.f : __builtin_bit_cast(float, __builtin_bit_cast(uint32_t, kQmax<FP8> / amax) & ~0xFFFu);
+}
+// Four codes of four exact products.
+template <bool FP8>
+__device__ __forceinline__ uint32_t codes4(float a, float b, float c, float d) {
+  if constexpr (FP8) {
+    int w = __builtin_amdgcn_cvt_pk_fp8_f32(a, b, 0, false);
+    return (uint32_t)__builtin_amdgcn_cvt_pk_fp8_f32(c, d, w, true);
+  } else {
+    const uint32_t x = (uint32_t)(int)__builtin_rintf(a) & 255u, y = (uint32_t)(int)__builtin_rintf(b) & 255u;
+    const uint32_t z = (uint32_t)(int)__builtin_rintf(c) & 255u, w = (uint32_t)(int)__builtin_rintf(d);
+    return x | y << 8 | z << 16 | w << 24;
+  }
+}
+// The values of four codes.
+template <bool FP8>
+__device__ __forceinline__ void values4(uint32_t w, float* x) {
+  if constexpr (FP8) {
+    const f32x2 lo = __builtin_amdgcn_cvt_pk_f32_fp8((int)w, false), hi = __builtin_amdgcn_cvt_pk_f32_fp8((int)w, true);
+    x[0] = lo.x; x[1] = lo.y; x[2] = hi.x; x[3] = hi.y;
+  } else {
+#pragma unroll
+    for (int i = 0; i < 4; ++i) x[i] = (float)(int8_t)(w >> (8 * i));
+  }
+}
+
+}  // namespace dq

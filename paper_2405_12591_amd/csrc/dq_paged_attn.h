@@ -1,0 +1,127 @@
+// What the two attention kernels over the paged cache share.
+#pragma once
+#include "dq_paged.h"
+
+namespace dq {
+
+struct PagedAttnArgs {
+  dq_paged_cache c;
+  dq_paged_batch bt;
+  dq_heads q, out;
+  int group;               // query heads per kv head
+  int max_rows;            // rows of any sequence at most
+  int max_seq_len;
+  int window;              // 0: none
+  int causal;
+  float scale_log2;        // softmax scale * log2(e)
+  int splits;
+  float* partials;         // [unit, split, column, D + 2]
+  int32_t* counters;       // [unit], zero between calls
+  int units;               // what the splits of are joined: (sequence, kv head), or a tile of query rows
+};
+
+constexpr float kLazy = 8.f;   // a running maximum may fall behind by so many powers of two before sums are rescaled
+
+// Eight codes as f16, exactly.  8-bit floats have an instruction for it; integers ride in the low bits of 1024 + 128 + c.
+template <bool FP8>
+__device__ __forceinline__ f16x8 codes_f16(uint32_t lo, uint32_t hi) {
+  f16x8 r;
+  if constexpr (FP8) {
+    const f16x2 a = __builtin_amdgcn_cvt_scalef32_pk_f16_fp8((int)lo, 1.0f, false), b = __builtin_amdgcn_cvt_scalef32_pk_f16_fp8((int)lo, 1.0f, true);
+    const f16x2 c = __builtin_amdgcn_cvt_scalef32_pk_f16_fp8((int)hi, 1.0f, false), d = __builtin_amdgcn_cvt_scalef32_pk_f16_fp8((int)hi, 1.0f, true);
+    r = f16x8{a.x, a.y, b.x, b.y, c.x, c.y, d.x, d.y};
+  } else {
+    const uint32_t base = 0x64646464u;
+    const f16x2 off = {(_Float16)1152.f, (_Float16)1152.f};
+    lo ^= 0x80808080u;
+    hi ^= 0x80808080u;
+    const f16x2 a = __builtin_bit_cast(f16x2, __builtin_amdgcn_perm(base, lo, 0x04010400u)) - off;
+    const f16x2 b = __builtin_bit_cast(f16x2, __builtin_amdgcn_perm(base, lo, 0x04030402u)) - off;
+    const f16x2 c = __builtin_bit_cast(f16x2, __builtin_amdgcn_perm(base, hi, 0x04010400u)) - off;
+    const f16x2 d = __builtin_bit_cast(f16x2, __builtin_amdgcn_perm(base, hi, 0x04030402u)) - off;
+    r = f16x8{a.x, a.y, b.x, b.y, c.x, c.y, d.x, d.y};
+  }
+  return r;
+}
+
+// A row's power of two that brings its largest value to [2^7, 2^8): bf16 queries then fit f16 exactly (what lies 2^22
+// below the row's largest loses bits below 2^-32 of it).
+__device__ __forceinline__ int fit_shift(float amax) {
+  const int e = (int)(__builtin_bit_cast(uint32_t, amax) >> 23 & 255);
+  return amax > 0.f ? min(max(134 - e, -120), 120) : 0;
+}
+
+__device__ __forceinline__ f32x4 mma16(f16x8 a, f16x8 b, f32x4 c) { return __builtin_amdgcn_mfma_f32_16x16x32_f16(a, b, c, 0, 0, 0); }
+__device__ __forceinline__ f32x4 mma16(bf16x8 a, bf16x8 b, f32x4 c) { return __builtin_amdgcn_mfma_f32_16x16x32_bf16(a, b, c, 0, 0, 0); }
+__device__ __forceinline__ f32x16 mma32(f16x8 a, f16x8 b, f32x16 c) { return __builtin_amdgcn_mfma_f32_32x32x16_f16(a, b, c, 0, 0, 0); }
+__device__ __forceinline__ f32x16 mma32(bf16x8 a, bf16x8 b, f32x16 c) { return __builtin_amdgcn_mfma_f32_32x32x16_bf16(a, b, c, 0, 0, 0); }
+
+template <typename T> struct Vec8;
+template <> struct Vec8<_Float16> { typedef f16x8 type; };
+template <> struct Vec8<__bf16> { typedef bf16x8 type; };
+
+template <typename V> struct Element;
+template <> struct Element<f16x8> { typedef _Float16 type; };
+template <> struct Element<bf16x8> { typedef __bf16 type; };
+template <typename V> __device__ __forceinline__ typename Element<V>::type to_element(float x) { return (typename Element<V>::type)x; }
+
+// Two 16-bit tokens of a value word, zero where the token lies behind the last one (`left` tokens count from the word's first).
+__device__ __forceinline__ uint32_t keep_tokens(uint32_t w, int left) { return left >= 2 ? w : left == 1 ? (w & 0xFFFFu) : 0u; }
+
+// Joins the partial results of a unit's splits in the workgroup that finishes last and writes the outputs.  The caller's
+// partials are device-scope stores; every wave waits for its own, then one thread takes a ticket at the memory side, so
+// the holder of the last ticket finds all of them performed and reads them with device-scope loads.
+// cols: valid columns of the unit; out_of(col): pointer to the column's output row.
+template <typename T, int D, typename Out>
+__device__ __forceinline__ void join_splits(const PagedAttnArgs& a, int unit, int stride_cols, int cols, int* s_last, Out out_of) {
+  asm volatile("s_waitcnt vmcnt(0)" ::: "memory");
+  __builtin_amdgcn_fence(__ATOMIC_RELEASE, "workgroup");
+  __syncthreads();
+  if (threadIdx.x == 0) {
+    const int ticket = __hip_atomic_fetch_add(a.counters + unit, 1, __ATOMIC_RELAXED, __HIP_MEMORY_SCOPE_AGENT);
+    *s_last = ticket == a.splits - 1;
+    if (*s_last) __hip_atomic_store(a.counters + unit, 0, __ATOMIC_RELAXED, __HIP_MEMORY_SCOPE_AGENT);   // clean for the next call
+  }
+  __syncthreads();
+  if (!*s_last) return;
+  const float* base = a.partials + (long)unit * a.splits * stride_cols * (D + 2);
+  const long step = (long)stride_cols * (D + 2);
+  for (int idx = threadIdx.x; idx < cols * D; idx += blockDim.x) {
+    const int col = idx / D, c = idx % D;
+    const float* at = base + (long)col * (D + 2);
+    float M = -INFINITY;
+    for (int s = 0; s < a.splits; s += 8) {
+      float m[8];
+#pragma unroll
+      for (int k = 0; k < 8; ++k) m[k] = s + k < a.splits ? __hip_atomic_load(at + (s + k) * step + D, __ATOMIC_RELAXED, __HIP_MEMORY_SCOPE_AGENT) : -INFINITY;
+#pragma unroll
+      for (int k = 0; k < 8; ++k) M = fmaxf(M, m[k]);
+    }
+    const float base_m = M == -INFINITY ? 0.f : M;
+    float o = 0.f, l = 0.f;
+    for (int s = 0; s < a.splits; s += 8) {
+      float m[8], ll[8], oo[8];
+#pragma unroll
+      for (int k = 0; k < 8; ++k) {
+        const bool in = s + k < a.splits;
+        const float* p = at + (in ? s + k : s) * step;
+        m[k] = in ? __hip_atomic_load(p + D, __ATOMIC_RELAXED, __HIP_MEMORY_SCOPE_AGENT) : -INFINITY;
+        ll[k] = in ? __hip_atomic_load(p + D + 1, __ATOMIC_RELAXED, __HIP_MEMORY_SCOPE_AGENT) : 0.f;
+        oo[k] = in ? __hip_atomic_load(p + c, __ATOMIC_RELAXED, __HIP_MEMORY_SCOPE_AGENT) : 0.f;
+      }
+#pragma unroll
+      for (int k = 0; k < 8; ++k) {
+        const float w = __builtin_amdgcn_exp2f(m[k] - base_m);
+        o = __builtin_fmaf(oo[k], w, o);
+        l = __builtin_fmaf(ll[k], w, l);
+      }
+    }
+    const T y = (T)(l == 0.f ? 0.f : o / l);
+    out_of(col)[c] = __builtin_bit_cast(uint16_t, y);
+  }
+}
+
+int32_t launch_paged_decode(const PagedAttnArgs& a, hipStream_t st);
+int32_t launch_paged_prompt(const PagedAttnArgs& a, hipStream_t st);
+
+}  // namespace dq

@@ -1,0 +1,273 @@
+// Attention of a few query rows per sequence (a generated token, drafted ones) over the paged 8-bit cache.
+#include "dq_paged_attn.h"
+
+namespace dq {
+
+constexpr int kCols = 16;   // (row, query head) columns of a workgroup: one matrix instruction's
+
+// One workgroup of four waves per (sequence, kv head, split); its columns are the (row, query head) pairs that read the
+// kv head.  Every wave works tiles of 64 tokens on its own, dealt round-robin over the waves of all splits, and keeps a
+// running maximum, sum and output; waves are joined through LDS, splits through memory.
+//
+// Scores are formed transposed, S^T = K Q^T, token rows against query columns.  Row r of the four 16-row products stands
+// for token 16 (r / 4) + 4 t4 + r % 4, so a lane ends up with the scores of 16 neighbouring tokens of its column:
+// exactly the right operand that O^T += V^T P^T wants, with the value codes of those tokens in one 16-byte load.
+// Nothing moves between lanes but the maximum, and that only when it grew.
+//
+// The values' scale rides in the exponent: u = s + log2(scale_v), p = 2^(u - m), O += p c, l += (sum p) / scale_v; the
+// products see codes and p only, and p is largest (2^8 at most) where the contribution to the output is.
+template <typename T, int D, bool FP8>
+__global__ __launch_bounds__(kPagedThreads) void paged_decode_kernel(PagedAttnArgs a) {
+  constexpr int NC = D / 64, NCT = D / 16;
+  typedef typename Vec8<T>::type tx8;
+  __shared__ float s_o[4][kCols][D + 1];
+  __shared__ float s_m[4][kCols], s_l[4][kCols];
+  __shared__ int s_last;
+  const int tid = threadIdx.x, lane = tid & 63, wave = tid >> 6, col = lane & 15, G = lane >> 4;
+  const int unit = (int)blockIdx.x / a.splits, split = (int)blockIdx.x % a.splits;
+  const int H = a.c.kv_heads, b = unit / H, h = unit % H, P = a.c.page_tokens;
+  Sequence s = sequence_of(a.bt, P, b);
+  s.len = min(s.len, a.max_seq_len);
+  const int n = min(s.n, a.max_rows), len = s.len;
+  if (n == 0) return;
+  const int cols = n * a.group;
+  const int qi = min(col / a.group, n - 1), hq = h * a.group + col % a.group;
+  const bool live = col < cols;
+  // tokens [see_lo, see_hi) of this column, and what every column sees
+  const int place = len - n + qi;
+  const int see_hi = a.causal ? min(place + 1, len) : len, see_lo = a.window ? max(place + 1 - a.window, 0) : 0;
+  const int all_hi = a.causal ? min(len - n + 1, len) : len, all_lo = a.window ? max(len - a.window, 0) : 0;
+  const int first_tile = a.window ? max(len - n + 1 - a.window, 0) / kPagedTile : 0;
+  const int runs = P / kPagedTile, code_tiles = len / P * runs, tiles = (len + kPagedTile - 1) / kPagedTile;
+
+  // ---- queries: 8 channels 64 c + 16 G + 8 half of the column, in f16 ----
+  const uint16_t* const q_row = a.q.data + (long)(s.row0 + qi) * a.q.token_stride + (long)(live ? hq : h * a.group) * a.q.head_stride;
+  f16x8 q[NC][2];
+  float sc = a.scale_log2;
+  {
+    float x[NC][2][8], amax = 0.f;
+#pragma unroll
+    for (int c = 0; c < NC; ++c)
+#pragma unroll
+      for (int hf = 0; hf < 2; ++hf) {
+        unpack8<T>(*reinterpret_cast<const u32x4*>(q_row + 64 * c + 16 * G + 8 * hf), x[c][hf]);
+#pragma unroll
+        for (int j = 0; j < 8; ++j) amax = fmaxf(amax, fabsf(x[c][hf][j]));
+      }
+    int shift = 0;
+    if constexpr (__is_same(T, __bf16)) {
+      amax = fmaxf(amax, __shfl_xor(amax, 16));
+      amax = fmaxf(amax, __shfl_xor(amax, 32));
+      shift = fit_shift(amax);
+      sc = __builtin_ldexpf(sc, -shift);
+    }
+#pragma unroll
+    for (int c = 0; c < NC; ++c)
+#pragma unroll
+      for (int hf = 0; hf < 2; ++hf)
+#pragma unroll
+        for (int j = 0; j < 8; ++j) q[c][hf][j] = (_Float16)(__is_same(T, __bf16) ? __builtin_ldexpf(x[c][hf][j], shift) : x[c][hf][j]);
+  }
+
+  f32x4 o[NCT];
+#pragma unroll
+  for (int ct = 0; ct < NCT; ++ct) o[ct] = f32x4{0.f, 0.f, 0.f, 0.f};
+  float m = -INFINITY, l = 0.f;
+
+  // Softmax of a tile's 16 scores of this lane (tokens 64 tile + 16 G + ..), in place: u -> p.
+  auto softmax = [&](float (&u)[16], int tile, float inv_sv) __attribute__((always_inline)) {
+    const int t0 = tile * kPagedTile;
+    if (t0 < all_lo || t0 + kPagedTile > all_hi) {
+#pragma unroll
+      for (int j = 0; j < 16; ++j) {
+        const int t = t0 + 16 * G + j;
+        if (t < see_lo || t >= see_hi) u[j] = -INFINITY;
+      }
+    }
+    float top = u[0];
+#pragma unroll
+    for (int j = 1; j < 16; ++j) top = fmaxf(top, u[j]);
+    if (__any(top > m + kLazy)) {
+      top = fmaxf(top, __shfl_xor(top, 16));
+      top = fmaxf(top, __shfl_xor(top, 32));
+      const float m_new = fmaxf(m, top);
+      const float alpha = m_new == -INFINITY ? 1.f : __builtin_amdgcn_exp2f(m - m_new);
+      m = m_new;
+      l *= alpha;
+#pragma unroll
+      for (int ct = 0; ct < NCT; ++ct) o[ct] *= alpha;
+    }
+    const float base = m == -INFINITY ? 0.f : m;
+    float sum = 0.f;
+#pragma unroll
+    for (int j = 0; j < 16; ++j) {
+      u[j] = __builtin_amdgcn_exp2f(u[j] - base);
+      sum += u[j];
+    }
+    l = __builtin_fmaf(sum, inv_sv, l);
+  };
+
+  // ---- full pages ----
+  const int stride = a.splits * 4, mine = first_tile + split * 4 + wave;
+  const int k_row = 16 * ((lane & 15) >> 2) + (lane & 3);   // + 4 t4: the token of this lane's row
+  for (int batch0 = mine; batch0 < code_tiles; batch0 += 64 * stride) {
+    // the next 64 tiles' blocks and scales, one per lane
+    const int t_l = batch0 + lane * stride;
+    int blk = 0;
+    float sk = 0.f, lsv = 0.f, isv = 0.f;
+    if (t_l < code_tiles) {
+      const int page = a.bt.page_table[(long)b * a.bt.table_stride + t_l / runs];
+      const bool ok = page >= 0 && page < a.c.pages;
+      const long block = (long)(ok ? page : 0) * H + h;
+      blk = (int)(block * runs) + t_l % runs;
+      sk = ok ? a.c.k_scales[block] : __builtin_nanf("");
+      const float sv = ok ? a.c.v_scales[block] : 1.f;
+      lsv = __builtin_amdgcn_logf(sv);
+      isv = 1.f / sv;
+    }
+    const int count = min(64, (code_tiles - batch0 + stride - 1) / stride);
+    u32x4 kb[4][NC], vb[NCT];
+    auto load_k = [&](int i) __attribute__((always_inline)) {
+      const uint8_t* p = a.c.k_codes + (long)__builtin_amdgcn_readlane(blk, i) * (kPagedTile * D) + k_row * D + 16 * G;
+#pragma unroll
+      for (int t4 = 0; t4 < 4; ++t4)
+#pragma unroll
+        for (int c = 0; c < NC; ++c) kb[t4][c] = __builtin_nontemporal_load(reinterpret_cast<const u32x4*>(p + 4 * t4 * D + 64 * c));
+    };
+    auto load_v = [&](int i) __attribute__((always_inline)) {
+      const uint8_t* p = a.c.v_codes + (long)__builtin_amdgcn_readlane(blk, i) * (kPagedTile * D) + (lane & 15) * kPagedTile + 16 * G;
+#pragma unroll
+      for (int ct = 0; ct < NCT; ++ct) vb[ct] = __builtin_nontemporal_load(reinterpret_cast<const u32x4*>(p + ct * 16 * kPagedTile));
+    };
+    load_k(0);
+    load_v(0);
+    for (int i = 0; i < count; ++i) {
+      const float f = __builtin_bit_cast(float, __builtin_amdgcn_readlane(__builtin_bit_cast(int, sk), i)) * sc;
+      const float add = __builtin_bit_cast(float, __builtin_amdgcn_readlane(__builtin_bit_cast(int, lsv), i));
+      const float inv_sv = __builtin_bit_cast(float, __builtin_amdgcn_readlane(__builtin_bit_cast(int, isv), i));
+      float u[16];
+#pragma unroll
+      for (int t4 = 0; t4 < 4; ++t4) {
+        f32x4 acc = {0.f, 0.f, 0.f, 0.f};
+#pragma unroll
+        for (int c = 0; c < NC; ++c) {
+          acc = mma16(codes_f16<FP8>(kb[t4][c].x, kb[t4][c].y), q[c][0], acc);
+          acc = mma16(codes_f16<FP8>(kb[t4][c].z, kb[t4][c].w), q[c][1], acc);
+        }
+#pragma unroll
+        for (int j = 0; j < 4; ++j) u[4 * t4 + j] = __builtin_fmaf(acc[j], f, add);
+      }
+      if (i + 1 < count) load_k(i + 1);
+      softmax(u, batch0 + i * stride, inv_sv);
+      f16x8 p0, p1;
+#pragma unroll
+      for (int j = 0; j < 8; ++j) { p0[j] = (_Float16)u[j]; p1[j] = (_Float16)u[8 + j]; }
+#pragma unroll
+      for (int ct = 0; ct < NCT; ++ct) {
+        o[ct] = mma16(codes_f16<FP8>(vb[ct].x, vb[ct].y), p0, o[ct]);
+        o[ct] = mma16(codes_f16<FP8>(vb[ct].z, vb[ct].w), p1, o[ct]);
+      }
+      if (i + 1 < count) load_v(i + 1);
+    }
+  }
+
+  // ---- the page being filled: 16-bit rows, products in their own type ----
+  const int tail_first = max(code_tiles, first_tile);
+  for (int tile = tail_first; tile < tiles; ++tile) {
+    if ((tile - first_tile) % stride != split * 4 + wave) continue;
+    const int slot = a.bt.tail_slots ? a.bt.tail_slots[b] : b;
+    const bool ok = slot >= 0 && slot < a.c.slots;
+    const int run = tile - code_tiles, left = len - tile * kPagedTile;   // tokens of the tile
+    const long at = (((long)(ok ? slot : 0) * H + h) * runs + run) * kPagedTile * D;
+    const uint16_t* const kt = a.c.k_tail + at + k_row * D + 16 * G;
+    const uint16_t* const vt = a.c.v_tail + at + (lane & 15) * kPagedTile + 16 * G;
+    const float f = ok ? a.scale_log2 : __builtin_nanf("");
+    float u[16];
+    tx8 qt[NC][2];
+#pragma unroll
+    for (int c = 0; c < NC; ++c)
+#pragma unroll
+      for (int hf = 0; hf < 2; ++hf) qt[c][hf] = __builtin_bit_cast(tx8, *reinterpret_cast<const u32x4*>(q_row + 64 * c + 16 * G + 8 * hf));
+#pragma unroll
+    for (int t4 = 0; t4 < 4; ++t4) {
+      f32x4 acc = {0.f, 0.f, 0.f, 0.f};
+#pragma unroll
+      for (int c = 0; c < NC; ++c)
+#pragma unroll
+        for (int hf = 0; hf < 2; ++hf)
+          acc = mma16(__builtin_bit_cast(tx8, *reinterpret_cast<const u32x4*>(kt + 4 * t4 * D + 64 * c + 8 * hf)), qt[c][hf], acc);
+#pragma unroll
+      for (int j = 0; j < 4; ++j) {
+        u[4 * t4 + j] = acc[j] * f;
+        if (16 * G + 4 * t4 + j >= left) u[4 * t4 + j] = -INFINITY;   // (a column that sees all tokens, and rows that hold anything)
+      }
+    }
+    softmax(u, tile, 1.f);
+    u32x4 p0, p1;
+#pragma unroll
+    for (int j = 0; j < 4; ++j) { p0[j] = pack2<T>(u[2 * j], u[2 * j + 1]); p1[j] = pack2<T>(u[8 + 2 * j], u[8 + 2 * j + 1]); }
+#pragma unroll
+    for (int ct = 0; ct < NCT; ++ct) {
+      u32x4 v0 = *reinterpret_cast<const u32x4*>(vt + ct * 16 * kPagedTile), v1 = *reinterpret_cast<const u32x4*>(vt + ct * 16 * kPagedTile + 8);
+#pragma unroll
+      for (int j = 0; j < 4; ++j) {   // rows behind the last token may hold anything: 0 * NaN is not 0
+        v0[j] = keep_tokens(v0[j], left - 16 * G - 2 * j);
+        v1[j] = keep_tokens(v1[j], left - 16 * G - 8 - 2 * j);
+      }
+      o[ct] = mma16(__builtin_bit_cast(tx8, v0), __builtin_bit_cast(tx8, p0), o[ct]);
+      o[ct] = mma16(__builtin_bit_cast(tx8, v1), __builtin_bit_cast(tx8, p1), o[ct]);
+    }
+  }
+
+  // ---- waves, then splits ----
+  l += __shfl_xor(l, 16);
+  l += __shfl_xor(l, 32);
+#pragma unroll
+  for (int ct = 0; ct < NCT; ++ct)
+#pragma unroll
+    for (int j = 0; j < 4; ++j) s_o[wave][col][16 * ct + 4 * G + j] = o[ct][j];
+  if (G == 0) { s_m[wave][col] = m; s_l[wave][col] = l; }
+  __syncthreads();
+  auto out_of = [&](int c) { return a.out.data + (long)(s.row0 + c / a.group) * a.out.token_stride + (long)(h * a.group + c % a.group) * a.out.head_stride; };
+  float* const part = a.partials + ((long)unit * a.splits + split) * kCols * (D + 2);
+  for (int idx = tid; idx < cols * D; idx += kPagedThreads) {
+    const int cc = idx / D, ch = idx % D;
+    const float M = fmaxf(fmaxf(s_m[0][cc], s_m[1][cc]), fmaxf(s_m[2][cc], s_m[3][cc]));
+    const float base = M == -INFINITY ? 0.f : M;
+    float oo = 0.f, ll = 0.f;
+#pragma unroll
+    for (int w = 0; w < 4; ++w) {
+      const float f = __builtin_amdgcn_exp2f(s_m[w][cc] - base);
+      oo = __builtin_fmaf(s_o[w][cc][ch], f, oo);
+      ll = __builtin_fmaf(s_l[w][cc], f, ll);
+    }
+    if (a.splits == 1) {
+      const T y = (T)(ll == 0.f ? 0.f : oo / ll);
+      out_of(cc)[ch] = __builtin_bit_cast(uint16_t, y);
+    } else {
+      float* const p = part + (long)cc * (D + 2);
+      __hip_atomic_store(p + ch, oo, __ATOMIC_RELAXED, __HIP_MEMORY_SCOPE_AGENT);
+      if (ch == 0) {
+        __hip_atomic_store(p + D, M, __ATOMIC_RELAXED, __HIP_MEMORY_SCOPE_AGENT);
+        __hip_atomic_store(p + D + 1, ll, __ATOMIC_RELAXED, __HIP_MEMORY_SCOPE_AGENT);
+      }
+    }
+  }
+  if (a.splits > 1) join_splits<T, D>(a, unit, kCols, cols, &s_last, out_of);
+}
+
+template <typename T, int D>
+static void launch_decode(const PagedAttnArgs& a, hipStream_t st) {
+  const dim3 grid((unsigned)((long)a.units * a.splits));
+  if (a.c.codes == DQ_CODES_E4M3) hipLaunchKernelGGL((paged_decode_kernel<T, D, true>), grid, dim3(kPagedThreads), 0, st, a);
+  else hipLaunchKernelGGL((paged_decode_kernel<T, D, false>), grid, dim3(kPagedThreads), 0, st, a);
+}
+
+int32_t launch_paged_decode(const PagedAttnArgs& a, hipStream_t st) {
+  if (a.c.dtype == DQ_BF16) { if (a.c.head_dim == 128) launch_decode<__bf16, 128>(a, st); else launch_decode<__bf16, 64>(a, st); }
+  else { if (a.c.head_dim == 128) launch_decode<_Float16, 128>(a, st); else launch_decode<_Float16, 64>(a, st); }
+  DQ_HIP_CHECK(hipGetLastError());
+  return DQ_OK;
+}
+
+}  // namespace dq
