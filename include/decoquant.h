@@ -498,12 +498,15 @@ int32_t dq_paged_read(const dq_paged_cache* cache, const dq_paged_batch* batch, 
                       const int32_t* out_starts, const dq_heads* k_out, const dq_heads* v_out,
                       void* hip_stream);
 
-/* Bytes of workspace dq_paged_attention needs (0 on invalid arguments); zero it once before its first
- * use (dq_workspace_init).  Calls that share it, graphs among them, must be ordered. */
+/* Bytes of workspace dq_paged_attention needs for these sizes and all smaller ones with the same heads (0
+ * on invalid arguments); zero it once before its first use (dq_workspace_init), it is left so.  Calls that
+ * share it, graphs among them, must be ordered. */
 size_t dq_paged_workspace_bytes(const dq_paged_cache* cache, int32_t batch, int32_t rows, int32_t q_heads,
                                 int32_t max_rows, int32_t max_seq_len);
 
 #define DQ_PAGED_CAUSAL 1u /* row i sees tokens up to its own place (it is among the last n of its sequence) */
+#define DQ_PAGED_SPLITS(n) (((uint32_t)(n) & 0x7Fu) << 8) /* workgroups that share a unit's tokens, 1..64 (32 for prompts); 0 leaves it to
+                              the library (for sweeps; the workspace must hold them or the call is DQ_ENOSPACE) */
 
 /*
  * out[row, h] = softmax_t(q[row, h] . K[t] * scale) V over the cached tokens of the row's sequence, kv

@@ -80,11 +80,16 @@ __device__ __forceinline__ int item_first(const int32_t* starts, int rows, int b
   const long at = starts ? min(max(starts[b], 0), rows) : b;
   return (int)(at * mul / unit) + per_seq * b;
 }
+// All 64 lanes look at once, so that a batch of up to 64 sequences takes one round trip (bisection took four or more,
+// 2 us of an appended token).
 __device__ __forceinline__ int item_owner(const int32_t* starts, int rows, int batch, int item, int mul, int unit, int per_seq) {
-  int lo = 0, hi = batch - 1;
-  while (lo < hi) {
-    const int mid = (lo + hi + 1) >> 1;
-    if (item_first(starts, rows, mid, mul, unit, per_seq) <= item) lo = mid; else hi = mid - 1;
+  int lo = 0, n = batch;                                  // the owner is in [lo, lo + n)
+  while (n > 1) {
+    const int step = (n + 63) / 64, b = lo + (int)(threadIdx.x & 63) * step;
+    const bool begun = b < lo + n && item_first(starts, rows, b, mul, unit, per_seq) <= item;
+    const int last = max(__popcll(__ballot(begun)) - 1, 0);
+    n = min(step, n - last * step);
+    lo += last * step;
   }
   return lo;
 }
@@ -157,26 +162,60 @@ __device__ __forceinline__ RowLayout row_layout(int unit, int rot_dim, int inter
   return l;
 }
 
-// Cosines and sines of a unit's eight pairs for one token.  The angle in turns, p f / (2 pi), is formed in fp64 and
-// loses its whole turns there, so what is left of the largest position (2^31) is off by 2^-22 turns at most;
-// the hardware's sine and cosine take turns and are off by about 2^-20, both far below the 2^-12 of a 16-bit row.
-__device__ __forceinline__ void unit_turns(const dq_rotary& r, const RowLayout& l, long column, int own_place, float* cs, float* sn) {
+// Cosine and sine of t turns.  What is left of t after its whole quarters, r in [-1/2, 1/2] quarters, is formed in fp64
+// (the largest position, 2^31, keeps 2^-24 turns) and rounded once; the Taylor polynomials of degree 9 and 10 on
+// |r pi / 2| <= pi / 4 are cut off at 2e-9 and 5e-10, below fp32's rounding.  (The hardware's sine and cosine are off by 2^-20 or so,
+// which turned ten times as many 16-bit roundings as fp32 does.)
+__device__ __forceinline__ void turn(double t, float* cs, float* sn) {
+  const double q = 4.0 * (t - __builtin_rint(t)), k = __builtin_rint(q);
+  const float x = (float)(q - k) * 1.57079632679489662f, z = x * x;
+  const int quarter = (int)k;
+  float s = __builtin_fmaf(z, 1.0f / 362880, -1.0f / 5040), c = __builtin_fmaf(z, -1.0f / 3628800, 1.0f / 40320);
+  s = __builtin_fmaf(z, s, 1.0f / 120);
+  c = __builtin_fmaf(z, c, -1.0f / 720);
+  s = __builtin_fmaf(z, s, -1.0f / 6);
+  c = __builtin_fmaf(z, c, 1.0f / 24);
+  s = __builtin_fmaf(z * x, s, x);
+  c = __builtin_fmaf(z, c, -0.5f);
+  c = __builtin_fmaf(z, c, 1.0f);
+  const float a = (quarter & 1) ? s : c, b = (quarter & 1) ? c : s;
+  *cs = ((quarter + 1) & 2) ? -a : a;
+  *sn = (quarter & 2) ? -b : b;
+}
+
+// What the angles of a unit's eight pairs are made of, asked for ahead of the rows' own loads.
+struct UnitTurns {
+  int p[8];
+  double f[8];
+};
+__device__ __forceinline__ void load_turns(const dq_rotary& r, const RowLayout& l, long column, int own_place, UnitTurns& t) {
+  if (l.pair0 < 0) return;
+#pragma unroll
+  for (int i = 0; i < 8; ++i) t.f[i] = r.inv_freq[l.pair0 + i];
+  if (r.axes > 1) {
+    const uint8_t* axis = r.axis_of_pair + l.pair0;
+    int at[8];
+#pragma unroll
+    for (int i = 0; i < 8; ++i) at[i] = min((int)axis[i], r.axes - 1);
+#pragma unroll
+    for (int i = 0; i < 8; ++i) t.p[i] = r.positions[at[i] * r.position_stride + column];
+  } else {
+    const int p = r.positions ? r.positions[column] : own_place;
+#pragma unroll
+    for (int i = 0; i < 8; ++i) t.p[i] = p;
+  }
+}
+__device__ __forceinline__ void make_turns(const RowLayout& l, const UnitTurns& t, float* cs, float* sn) {
 #pragma unroll
   for (int i = 0; i < 8; ++i) {
     cs[i] = 1.f;
     sn[i] = 0.f;
   }
   if (l.pair0 < 0) return;
-  int p0 = own_place;
-  if (r.positions) p0 = r.positions[column];
 #pragma unroll
   for (int i = 0; i < 8; ++i) {
-    int p = p0;
-    if (r.axes > 1) p = r.positions[min((int)r.axis_of_pair[l.pair0 + i], r.axes - 1) * r.position_stride + column];
-    const double turns = (double)p * (r.inv_freq[l.pair0 + i] * 0.15915494309189533577);
-    const float f = (float)(turns - __builtin_rint(turns));
-    cs[i] = __builtin_amdgcn_cosf(f);
-    sn[i] = __builtin_amdgcn_sinf(f);
+    turn((double)t.p[i] * (t.f[i] * 0.15915494309189533577), cs + i, sn + i);
+    if (i & 1) __builtin_amdgcn_sched_barrier(0);         // two pairs at a time: eight in a row hold 60 registers more
   }
 }
 
@@ -191,45 +230,56 @@ __device__ __forceinline__ void norm_unit(float* x, const float* w, float eps, f
 #pragma unroll
   for (int i = 0; i < 16; ++i) x[i] *= r * w[i];
 }
-__device__ __forceinline__ void turn_unit(float* x, const float* cs, const float* sn, bool interleaved) {
+template <bool INTERLEAVED>   // (a template: as a test at run time it became 28 selects a unit)
+__device__ __forceinline__ void turn_unit(float* x, const float* cs, const float* sn) {
 #pragma unroll
   for (int i = 0; i < 8; ++i) {
-    const float a = interleaved ? x[2 * i] : x[i], b = interleaved ? x[2 * i + 1] : x[8 + i];
-    const float y = a * cs[i] - b * sn[i], z = a * sn[i] + b * cs[i];
-    if (interleaved) { x[2 * i] = y; x[2 * i + 1] = z; } else { x[i] = y; x[8 + i] = z; }
+    const int f = INTERLEAVED ? 2 * i : i, g = INTERLEAVED ? 2 * i + 1 : 8 + i;
+    const float a = x[f], b = x[g];
+    x[f] = a * cs[i] - b * sn[i];
+    x[g] = a * sn[i] + b * cs[i];
   }
 }
 
-// Heads [h0, h1) of one token's row: the thread is the row's unit `unit` of LANES.
-template <typename T, int LANES>
-__device__ __forceinline__ void rotate_row(const uint16_t* in, uint16_t* out, long in_head, long out_head, int h0, int h1, bool live,
-                                           const RowLayout& l, const uint16_t* weight, float eps, float inv_dim, const float* cs,
-                                           const float* sn, bool interleaved) {
-  float w[16];
-  if (weight && live) {
-    unpack8<T>(*reinterpret_cast<const u32x4*>(weight + l.at0), w);
-    unpack8<T>(*reinterpret_cast<const u32x4*>(weight + l.at1), w + 8);
+// A unit's 16 channels: norm (w: the weights, packed; they stay so from head to head: 8 registers, not 16), rotation, one rounding.
+template <typename T, int LANES, bool INTERLEAVED>
+__device__ __forceinline__ void ready_unit(u32x4 (&v)[2], u32x4 (&w)[2], bool normed, bool turned, float eps, float inv_dim, const float* cs,
+                                           const float* sn) {
+  float x[16];
+  unpack8<T>(v[0], x);
+  unpack8<T>(v[1], x + 8);
+  if (normed) {                                           // (the lanes of a row are in this branch together)
+    float y[16];
+    asm volatile("" : "+v"(w[0]), "+v"(w[1]));
+    unpack8<T>(w[0], y);
+    unpack8<T>(w[1], y + 8);
+    norm_unit<LANES>(x, y, eps, inv_dim);
   }
-  const bool turned = l.pair0 >= 0;
-  u32x4 a = {0, 0, 0, 0}, b = {0, 0, 0, 0};
-  if (live && h0 < h1) {
-    a = *reinterpret_cast<const u32x4*>(in + h0 * in_head + l.at0);
-    b = *reinterpret_cast<const u32x4*>(in + h0 * in_head + l.at1);
-  }
+  if (turned) turn_unit<INTERLEAVED>(x, cs, sn);
+  v[0] = pack8<T>(x);
+  v[1] = pack8<T>(x + 8);
+}
+
+__device__ __forceinline__ void load_unit(u32x4 (&v)[2], const uint16_t* p, const RowLayout& l) {
+  v[0] = *reinterpret_cast<const u32x4*>(p + l.at0);
+  v[1] = *reinterpret_cast<const u32x4*>(p + l.at1);
+}
+__device__ __forceinline__ void store_unit(uint16_t* p, const RowLayout& l, const u32x4 (&v)[2]) {
+  *reinterpret_cast<u32x4*>(p + l.at0) = v[0];
+  *reinterpret_cast<u32x4*>(p + l.at1) = v[1];
+}
+
+// Heads [h0, h1) of one token's row: the thread is the row's unit of LANES.  v: the first head's pieces, asked for ahead.
+template <typename T, int LANES, bool INTERLEAVED>
+__device__ __forceinline__ void rotate_row(u32x4 (&v)[2], const uint16_t* in, uint16_t* out, long in_head, long out_head, int h0, int h1, bool live,
+                                           const RowLayout& l, const uint16_t* weight, float eps, float inv_dim, const float* cs, const float* sn) {
+  u32x4 w[2] = {};
+  if (weight && live) load_unit(w, weight, l);
   for (int h = h0; h < h1; ++h) {
-    float x[16];
-    unpack8<T>(a, x);
-    unpack8<T>(b, x + 8);
-    if (live && h + 1 < h1) {   // the next head's pieces are on their way meanwhile
-      a = *reinterpret_cast<const u32x4*>(in + (h + 1) * in_head + l.at0);
-      b = *reinterpret_cast<const u32x4*>(in + (h + 1) * in_head + l.at1);
-    }
-    if (weight) norm_unit<LANES>(x, w, eps, inv_dim);
-    if (turned) turn_unit(x, cs, sn, interleaved);
-    if (live) {
-      *reinterpret_cast<u32x4*>(out + h * out_head + l.at0) = pack8<T>(x);
-      *reinterpret_cast<u32x4*>(out + h * out_head + l.at1) = pack8<T>(x + 8);
-    }
+    u32x4 y[2] = {v[0], v[1]};
+    if (live && h + 1 < h1) load_unit(v, in + (h + 1) * in_head, l);   // the next head's pieces are on their way meanwhile
+    ready_unit<T, LANES, INTERLEAVED>(y, w, weight != nullptr, l.pair0 >= 0, eps, inv_dim, cs, sn);
+    if (live) store_unit(out + h * out_head, l, y);
   }
 }
 

@@ -16,55 +16,84 @@ struct AppendArgs {
   int q_heads_per_group, q_head_groups;
 };
 
-// One page of one sequence, PASSES rows of every thread: places and sources of the rows.
-// Keys of a page: thread (row r = pass * RP + tid / LPR, unit tid % LPR), the unit's channels laid for the rotation.
-// Values: rows PASSES * (tid / LPR) + pass, neighbours in the value layout, 16 neighbouring channels.
-template <typename T, int D, int P, bool FP8>
-struct PageWork {
-  static constexpr int LPR = D / 16, RP = kPagedThreads / LPR, PASSES = P / RP;
-  static_assert(PASSES == 1 || PASSES == 2 || PASSES == 4, "rows a thread");
-};
-
-__device__ __forceinline__ bool finite_pair(uint32_t w, uint32_t exponent) {   // both 16-bit values
-  return ((w & exponent) != exponent) & ((w & (exponent << 16)) != (exponent << 16));
+// Largest magnitudes as 16-bit patterns, which order as integers; those from `exponent` on are not finite.  Both values of
+// a word at a time.
+typedef uint16_t u16x2 __attribute__((ext_vector_type(2)));
+__device__ __forceinline__ uint32_t larger_pair(uint32_t a, uint32_t b) {
+  return __builtin_bit_cast(uint32_t, __builtin_elementwise_max(__builtin_bit_cast(u16x2, a), __builtin_bit_cast(u16x2, b)));
+}
+__device__ __forceinline__ uint32_t largest(const u32x4& v, uint32_t m) {
+#pragma unroll
+  for (int j = 0; j < 4; ++j) m = larger_pair(m, v[j] & 0x7FFF7FFFu);
+  return m;
+}
+__device__ __forceinline__ uint32_t higher_half(uint32_t m) { return max(m >> 16, m & 0xFFFFu); }
+template <int CTRL>
+__device__ __forceinline__ uint32_t larger_of_lanes(uint32_t x) {
+  return larger_pair(x, (uint32_t)__builtin_amdgcn_update_dpp(0, (int)x, CTRL, 0xF, 0xF, true));
 }
 
-// Pages are worked by one workgroup per (page, group of kv heads): the angles of a page's rows are formed once per group.
+// Pages are worked by one workgroup per (page, group of kv heads); a thread has 16 channels of one key row, laid for the
+// rotation, and 8 channels of two neighbouring value rows, as the value layout wants them.  The angles of a key row's
+// unit are formed once and kept for all heads of the group.
 // Reads 4 bytes and writes 2 per cached element pair (k, v); about 40 flops an element.  Bound by memory where
 // prompts are long, by latency for a generated token (its page is read only when it fills).
-template <typename T, int D, int P, bool FP8>
-__global__ __launch_bounds__(kPagedThreads) void paged_append_kernel(AppendArgs a) {
-  typedef PageWork<T, D, P, FP8> W;
-  constexpr int LPR = W::LPR, RP = W::RP, PASSES = W::PASSES;
+template <typename T, int D, int P, bool FP8, bool INTERLEAVED>
+__global__ __launch_bounds__(P * D / 16, 4) void paged_append_kernel(AppendArgs a) {
+  constexpr int THREADS = P * D / 16, LPR = D / 16, RP = P, WAVES = THREADS / 64;
   constexpr uint32_t kExponent = __is_same(T, __bf16) ? 0x7F80u : 0x7C00u;
   constexpr uint32_t kNanPair = __is_same(T, __bf16) ? 0x7FC07FC0u : 0x7E007E00u;
   constexpr int VS = 68;                                  // bytes of a channel's run in LDS: 64 and a word against bank conflicts
   __shared__ __align__(16) uint8_t s_v[(P / 64) * D * VS];
-  __shared__ float s_amax[2][4];
-  __shared__ int s_bad[4];
-  const int tid = threadIdx.x, lane = tid & 63, wave = tid >> 6, unit = tid % LPR;
-  const RowLayout l = row_layout(unit, a.rot.rot_dim, a.rot.interleaved);
-  const float inv_dim = 1.0f / D;
+  __shared__ f32x4 s_turn[4][THREADS];                    // the thread's eight cosines and sines, for all heads of its group (16 registers less)
+  __shared__ uint32_t s_amax[2][WAVES];
+  const int thread = threadIdx.x;
+  constexpr float inv_dim = 1.0f / D;
 
   if ((int)blockIdx.x >= a.page_blocks) {                 // query rows
+    const int tid = thread;
+    const RowLayout l = row_layout(tid % LPR, a.rot.rot_dim, INTERLEAVED);
     const int item = (int)blockIdx.x - a.page_blocks;
     const int group = item % a.q_head_groups;
     const long row = (long)(item / a.q_head_groups) * RP + tid / LPR;
     bool live = row < a.bt.rows;
-    int place = 0;
+    int place = 0, b = (int)row;
+    if (a.bt.starts) {                                    // the row's sequence: bisection in LDS, a row a thread
+      int32_t* const known = reinterpret_cast<int32_t*>(s_v);
+      constexpr int kKnown = sizeof(s_v) / 4;
+      const int stride = (a.bt.batch + kKnown - 1) / kKnown;   // more sequences than LDS holds: every stride-th, then in memory
+      for (int i = tid; i * stride < a.bt.batch; i += THREADS) known[i] = a.bt.starts[i * stride];
+      __syncthreads();
+      int lo = 0, hi = (a.bt.batch - 1) / stride;
+      while (lo < hi) {
+        const int mid = (lo + hi + 1) >> 1;
+        if (min(max(known[mid], 0), a.bt.rows) <= row) lo = mid; else hi = mid - 1;
+      }
+      lo *= stride;
+      hi = min(lo + stride, a.bt.batch) - 1;
+      while (lo < hi) {
+        const int mid = (lo + hi + 1) >> 1;
+        if (min(max(a.bt.starts[mid], 0), a.bt.rows) <= row) lo = mid; else hi = mid - 1;
+      }
+      b = lo;
+    }
     if (live) {
-      const int b = item_owner(a.bt.starts, a.bt.rows, a.bt.batch, (int)row, 1, 1, 0);
       const Sequence s = sequence_of(a.bt, P, b);
       live = row < s.row0 + s.n;                          // rows behind the last sequence's stay as they are
       place = s.len - s.n + (int)(row - s.row0);
     }
-    float cs[8], sn[8];
     RowLayout turned = l;
     if (!live) turned.pair0 = -1;
-    unit_turns(a.rot, turned, row, place, cs, sn);
+    UnitTurns ut;
+    load_turns(a.rot, turned, row, place, ut);
     const int h0 = group * a.q_heads_per_group;
-    rotate_row<T, LPR>(a.q.data + row * a.q.token_stride, a.q_out.data + row * a.q_out.token_stride, a.q.head_stride, a.q_out.head_stride, h0,
-                       min(h0 + a.q_heads_per_group, a.q.heads), live, l, a.norm.q_weight, a.norm.eps, inv_dim, cs, sn, a.rot.interleaved);
+    const uint16_t* const q = a.q.data + row * a.q.token_stride;
+    u32x4 v[2] = {};
+    if (live) load_unit(v, q + h0 * a.q.head_stride, l);
+    float cs[8], sn[8];
+    make_turns(turned, ut, cs, sn);
+    rotate_row<T, LPR, INTERLEAVED>(v, q, a.q_out.data + row * a.q_out.token_stride, a.q.head_stride, a.q_out.head_stride, h0,
+                                    min(h0 + a.q_heads_per_group, a.q.heads), live, l, a.norm.q_weight, a.norm.eps, inv_dim, cs, sn);
     return;
   }
 
@@ -86,211 +115,182 @@ __global__ __launch_bounds__(kPagedThreads) void paged_append_kernel(AppendArgs 
   if (page == last_page && page != first_page && partial_last && tail_read_first) return;
   const bool then_last = page == first_page && tail_read_first && partial_last;
 
-  float wk[16];
-  if (a.norm.k_weight) {
-    unpack8<T>(*reinterpret_cast<const u32x4*>(a.norm.k_weight + l.at0), wk);
-    unpack8<T>(*reinterpret_cast<const u32x4*>(a.norm.k_weight + l.at1), wk + 8);
-  }
-  for (int part = 0; part < (then_last ? 2 : 1); ++part) {
-    if (part) {
-      page = last_page;
-      __syncthreads();                                    // the old tail rows of all heads have been read
+  const int tid = thread, lane = tid & 63, wave = tid >> 6;
+  const RowLayout l = row_layout(tid % LPR, a.rot.rot_dim, INTERLEAVED);
+  const int r = tid / LPR, v8 = tid % (D / 8), rv = 2 * (tid / (D / 8));   // key row; value channels and first row
+  u32x4 wk[2] = {};
+  if (a.norm.k_weight) load_unit(wk, a.norm.k_weight, l);
+
+  // The thread's new rows of a page: where they come from, and the angles of the key row (to LDS).
+  struct NewRows {
+    const uint16_t *k, *v;                                // of kv head 0
+    bool k_new, v_new[2];
+  };
+  auto new_rows = [&](int base, int lo, int hi) __attribute__((always_inline)) {
+    NewRows n;
+    n.k_new = r >= lo && r < hi;
+    n.v_new[0] = rv >= lo && rv < hi;
+    n.v_new[1] = rv + 1 >= lo && rv + 1 < hi;
+    n.k = a.k.data + (s.row0 + (base + r - old)) * a.k.token_stride;
+    n.v = a.v.data + (s.row0 + (base + rv - old)) * a.v.token_stride + 8 * v8;
+    return n;
+  };
+  auto angles = [&](int base, const NewRows& n) __attribute__((always_inline)) {
+    RowLayout turned = l;
+    if (!n.k_new) turned.pair0 = -1;
+    UnitTurns ut;
+    float cs[8], sn[8];
+    load_turns(a.rot, turned, s.row0 + (base + r - old), base + r, ut);
+    make_turns(turned, ut, cs, sn);
+#pragma unroll
+    for (int i = 0; i < 2; ++i) {
+      s_turn[i][tid] = f32x4{cs[4 * i], cs[4 * i + 1], cs[4 * i + 2], cs[4 * i + 3]};
+      s_turn[2 + i][tid] = f32x4{sn[4 * i], sn[4 * i + 1], sn[4 * i + 2], sn[4 * i + 3]};
     }
-    const int base = page * P;                            // first token of the page
-    const bool full = base + P <= s.len;
-    const int page_id = full ? a.bt.page_table[(long)b * a.bt.table_stride + page] : 0;
-    if (full ? (page_id < 0 || page_id >= a.c.pages) : !slot_ok) continue;   // no such page: its rows are dropped
-    const int lo = max(old, base) - base, hi = min(s.len - base, P);         // new rows of the page: [lo, hi)
-    float cs[PASSES][8], sn[PASSES][8];
+  };
+  auto load_rows = [&](const NewRows& n, int h, u32x4 (&kn)[2], u32x4 (&vn)[2]) __attribute__((always_inline)) {
+    if (n.k_new) load_unit(kn, n.k + h * a.k.head_stride, l);
 #pragma unroll
-    for (int i = 0; i < PASSES; ++i) {
-      const int r = i * RP + tid / LPR;
-      RowLayout turned = l;
-      if (r < lo || r >= hi) turned.pair0 = -1;
-      unit_turns(a.rot, turned, s.row0 + (base + r - old), base + r, cs[i], sn[i]);
+    for (int i = 0; i < 2; ++i)
+      if (n.v_new[i]) vn[i] = *reinterpret_cast<const u32x4*>(n.v + i * a.v.token_stride + h * a.v.head_stride);
+  };
+  auto ready_key = [&](u32x4 (&kr)[2]) __attribute__((always_inline)) {   // norm, rotation, the rounding the tail keeps
+    float cs[8], sn[8];
+#pragma unroll
+    for (int i = 0; i < 8; ++i) {
+      cs[i] = s_turn[i / 4][tid][i % 4];
+      sn[i] = s_turn[2 + i / 4][tid][i % 4];
     }
-    for (int h = h_first; h < h_last; ++h) {
-      const long tail_block = ((long)slot * a.c.kv_heads + h) * P * D;
-      uint16_t* const k_tail = a.c.k_tail + tail_block;
-      uint16_t* const v_tail = a.c.v_tail + tail_block;
-      // ---- rows ----
-      u32x4 kr[PASSES][2], vr[PASSES][2];
+    ready_unit<T, LPR, INTERLEAVED>(kr, wk, a.norm.k_weight != nullptr, l.pair0 >= 0, a.norm.eps, inv_dim, cs, sn);
+  };
+  // Largest magnitudes of the workgroup's key and value pieces, as patterns in the high and low half.
+  auto amax_of = [&](const u32x4 (&kr)[2], const u32x4 (&vr)[2], int buf) __attribute__((always_inline)) {
+    uint32_t m = higher_half(largest(kr[1], largest(kr[0], 0))) << 16 | higher_half(largest(vr[1], largest(vr[0], 0)));
+    m = larger_of_lanes<0xB1>(m);
+    m = larger_of_lanes<0x4E>(m);
+    m = larger_of_lanes<0x141>(m);
+    m = larger_of_lanes<0x140>(m);
+    m = larger_pair(m, (uint32_t)__shfl_xor((int)m, 16));
+    m = larger_pair(m, (uint32_t)__shfl_xor((int)m, 32));
+    if (lane == 0) s_amax[buf][wave] = m;
+    __syncthreads();
 #pragma unroll
-      for (int i = 0; i < PASSES; ++i) {
-        const int r = i * RP + tid / LPR, rv = PASSES * (tid / LPR) + i;
-        kr[i][0] = kr[i][1] = vr[i][0] = vr[i][1] = u32x4{0, 0, 0, 0};
-        if (r >= lo && r < hi) {
-          const uint16_t* src = a.k.data + (s.row0 + (base + r - old)) * a.k.token_stride + h * a.k.head_stride;
-          kr[i][0] = *reinterpret_cast<const u32x4*>(src + l.at0);
-          kr[i][1] = *reinterpret_cast<const u32x4*>(src + l.at1);
-        } else if (r < lo && full && slot_ok) {
-          kr[i][0] = *reinterpret_cast<const u32x4*>(k_tail + (long)r * D + l.at0);
-          kr[i][1] = *reinterpret_cast<const u32x4*>(k_tail + (long)r * D + l.at1);
-        }
-        if (rv >= lo && rv < hi) {
-          const uint16_t* src = a.v.data + (s.row0 + (base + rv - old)) * a.v.token_stride + h * a.v.head_stride + 16 * unit;
-          vr[i][0] = *reinterpret_cast<const u32x4*>(src);
-          vr[i][1] = *reinterpret_cast<const u32x4*>(src + 8);
-        }
-      }
-      if (full && slot_ok) {                              // old value rows: from the channel runs of the tail
-#pragma unroll
-        for (int i = 0; i < PASSES; ++i) {
-          const int rv = PASSES * (tid / LPR) + i;
+    for (int w = 0; w < WAVES; ++w) m = larger_pair(m, s_amax[buf][w]);
+    return m;
+  };
+  // Rows that are not finite become NaN keys (`fill`) and zero values (no row of ordinary data comes here).  A row's key and
+  // value pieces lie in different threads.
+  auto drop_rows = [&](u32x4 (&kr)[2], u32x4 (&vr)[2], uint32_t fill) __attribute__((always_inline)) {
+    uint8_t* const flag = s_v;                            // one byte a row
+    if (tid < P) flag[tid] = 0;
+    __syncthreads();
+    if (higher_half(largest(kr[1], largest(kr[0], 0))) >= kExponent) flag[r] = 1;
+    if (higher_half(largest(vr[0], 0)) >= kExponent) flag[rv] = 1;
+    if (higher_half(largest(vr[1], 0)) >= kExponent) flag[rv + 1] = 1;
+    __syncthreads();
+    if (flag[r]) kr[0] = kr[1] = u32x4{fill, fill, fill, fill};
+    if (flag[rv]) vr[0] = u32x4{0, 0, 0, 0};
+    if (flag[rv + 1]) vr[1] = u32x4{0, 0, 0, 0};
+    __syncthreads();
+  };
+  const int v_at = (rv / 64) * 64 * D + 8 * v8 * 64 + rv % 64;   // the first row's place in a block of the value layout; + 64 j: channel 8 v8 + j
+
+  if ((page + 1) * P <= s.len) {
+    // ---- a full page ----
+    const int base = page * P, lo = max(old - base, 0);   // rows from lo on are new, the others in the tail
+    const int page_id = a.bt.page_table[(long)b * a.bt.table_stride + page];
+    if (page_id >= 0 && page_id < a.c.pages) {            // no such page: its rows are dropped
+      const NewRows rows = new_rows(base, lo, P);
+      angles(base, rows);
+      u32x4 kn[2] = {}, vn[2] = {};                       // the head to come
+      load_rows(rows, h_first, kn, vn);
+      for (int h = h_first; h < h_last; ++h) {
+        u32x4 kr[2] = {kn[0], kn[1]}, vr[2] = {vn[0], vn[1]};
+        if (h + 1 < h_last) load_rows(rows, h + 1, kn, vn);   // on their way while this head is worked
+        if (lo > 0 && slot_ok) {                          // old rows; the values' from the channel runs, both rows in a load
+          const long tail_block = ((long)slot * a.c.kv_heads + h) * P * D;
+          if (r < lo) load_unit(kr, a.c.k_tail + tail_block + (long)r * D, l);
           if (rv < lo) {
-            const uint16_t* src = v_tail + (long)(rv / 64) * 64 * D + 16 * unit * 64 + rv % 64;
+            const uint32_t keep0 = 0xFFFFu, keep1 = rv + 1 < lo ? 0xFFFF0000u : 0u;
 #pragma unroll
             for (int j = 0; j < 8; ++j) {
-              vr[i][0][j / 2] |= (uint32_t)src[j * 64] << (16 * (j & 1));
-              vr[i][1][j / 2] |= (uint32_t)src[(8 + j) * 64] << (16 * (j & 1));
+              const uint32_t w = *reinterpret_cast<const uint32_t*>(a.c.v_tail + tail_block + v_at + j * 64), x = w & keep0, y = w & keep1;
+              vr[0][j / 2] |= (j & 1) ? x << 16 : x;
+              vr[1][j / 2] |= (j & 1) ? y : y >> 16;
             }
           }
         }
-      }
-      // ---- keys: norm, rotation, the rounding the tail keeps ----
-#pragma unroll
-      for (int i = 0; i < PASSES; ++i) {
-        const int r = i * RP + tid / LPR;
-        float x[16];
-        unpack8<T>(kr[i][0], x);
-        unpack8<T>(kr[i][1], x + 8);
-        if (a.norm.k_weight) norm_unit<LPR>(x, wk, a.norm.eps, inv_dim);
-        if (l.pair0 >= 0) turn_unit(x, cs[i], sn[i], a.rot.interleaved);
-        const bool fresh = r >= lo && r < hi;             // the tail's rows are ready
-        const u32x4 y0 = pack8<T>(x), y1 = pack8<T>(x + 8);
-        if (fresh) { kr[i][0] = y0; kr[i][1] = y1; }
-      }
-      // ---- rows that are not finite: NaN keys, zero values.  Key and value pieces of a row lie in different threads ----
-      int bad = 0;
-#pragma unroll
-      for (int i = 0; i < PASSES; ++i) {
-        bool k_ok = true, v_ok = true;
-#pragma unroll
-        for (int j = 0; j < 4; ++j) {
-          k_ok &= finite_pair(kr[i][0][j], kExponent) & finite_pair(kr[i][1][j], kExponent);
-          v_ok &= finite_pair(vr[i][0][j], kExponent) & finite_pair(vr[i][1][j], kExponent);
+        if (rows.k_new) ready_key(kr);
+        // one step for the block's keys, one for its values
+        uint32_t top = amax_of(kr, vr, 0);
+        bool nan_block = lo > 0 && !slot_ok;              // (rows of no slot)
+        if (higher_half(top) >= kExponent) {
+          drop_rows(kr, vr, 0u);                          // (the scale says it)
+          top = amax_of(kr, vr, 1);
+          nan_block = true;
         }
-        bad |= (!k_ok | !v_ok);
-      }
-      if (__syncthreads_or(bad)) {                        // (no row of ordinary data comes here)
-        uint8_t* const flag = s_v;                        // one byte a row
-        for (int r = tid; r < P; r += kPagedThreads) flag[r] = 0;
-        __syncthreads();
-#pragma unroll
-        for (int i = 0; i < PASSES; ++i) {
-          bool k_ok = true, v_ok = true;
-#pragma unroll
-          for (int j = 0; j < 4; ++j) {
-            k_ok &= finite_pair(kr[i][0][j], kExponent) & finite_pair(kr[i][1][j], kExponent);
-            v_ok &= finite_pair(vr[i][0][j], kExponent) & finite_pair(vr[i][1][j], kExponent);
-          }
-          if (!k_ok) flag[i * RP + tid / LPR] = 1;
-          if (!v_ok) flag[PASSES * (tid / LPR) + i] = 1;
+        float k_amax, v_amax;
+        unpack2<T>(top, v_amax, k_amax);
+        const float k_step = inverse_step<FP8>(k_amax), v_step = inverse_step<FP8>(v_amax);
+        const long block = (long)page_id * a.c.kv_heads + h;
+        if (tid == 0) {
+          a.c.k_scales[block] = nan_block ? __builtin_nanf("") : k_step > 0.f ? 1.f / k_step : 1.f;
+          a.c.v_scales[block] = v_step > 0.f ? 1.f / v_step : 1.f;
         }
-        __syncthreads();
-        bad = 0;
+        uint8_t* const k_codes = a.c.k_codes + block * P * D + (long)r * D;
 #pragma unroll
-        for (int i = 0; i < PASSES; ++i) {
-          if (flag[i * RP + tid / LPR]) {
-            bad = 1;
-            const uint32_t fill = full ? 0u : kNanPair;   // in a full page the scale says it
-            kr[i][0] = kr[i][1] = u32x4{fill, fill, fill, fill};
+        for (int i = 0; i < 2; ++i) {
+          float x[8];
+          unpack8<T>(kr[i], x);
+          *reinterpret_cast<u32x2*>(k_codes + (i ? l.at1 : l.at0)) =
+              u32x2{codes4<FP8>(x[0] * k_step, x[1] * k_step, x[2] * k_step, x[3] * k_step),
+                    codes4<FP8>(x[4] * k_step, x[5] * k_step, x[6] * k_step, x[7] * k_step)};
+        }
+        // values channel by channel: the thread's two rows are neighbours of a channel's run
+#pragma unroll
+        for (int i = 0; i < 2; ++i) {                     // four channels at a time
+          float x[4], y[4];
+          unpack2<T>(vr[0][2 * i], x[0], x[1]);
+          unpack2<T>(vr[0][2 * i + 1], x[2], x[3]);
+          unpack2<T>(vr[1][2 * i], y[0], y[1]);
+          unpack2<T>(vr[1][2 * i + 1], y[2], y[3]);
+#pragma unroll
+          for (int j = 0; j < 4; j += 2) {                // codes of (row, row + 1) of two channels
+            const uint32_t w = codes4<FP8>(x[j] * v_step, y[j] * v_step, x[j + 1] * v_step, y[j + 1] * v_step);
+            uint8_t* dst = s_v + ((rv / 64) * D + 8 * v8 + 4 * i + j) * VS + rv % 64;
+            *reinterpret_cast<uint16_t*>(dst) = (uint16_t)w;
+            *reinterpret_cast<uint16_t*>(dst + VS) = (uint16_t)(w >> 16);
           }
-          if (flag[PASSES * (tid / LPR) + i]) vr[i][0] = vr[i][1] = u32x4{0, 0, 0, 0};
         }
         __syncthreads();
+        const uint32_t* src = reinterpret_cast<const uint32_t*>(s_v + (tid / 4) * VS + 16 * (tid % 4));   // 16 codes of a channel's run
+        *reinterpret_cast<u32x4*>(a.c.v_codes + block * P * D + 16l * tid) = u32x4{src[0], src[1], src[2], src[3]};
+        // (the next head's first barrier keeps s_v and s_amax until all have read them)
       }
-      if (!full) {
-        // ---- the page goes on: its new rows into the tail ----
+    }
+    if (!then_last) return;
+    page = last_page;
+    __syncthreads();                                      // the old tail rows of all heads have been read
+  }
+  // ---- a page that goes on: its new rows into the tail ----
+  if (!slot_ok) return;
+  const int base = page * P;
+  const NewRows rows = new_rows(base, max(old - base, 0), s.len - base);
+  angles(base, rows);
+  for (int h = h_first; h < h_last; ++h) {
+    u32x4 kr[2] = {}, vr[2] = {};
+    load_rows(rows, h, kr, vr);
+    if (rows.k_new) ready_key(kr);
+    if (__syncthreads_or(higher_half(largest(kr[1], largest(kr[0], largest(vr[1], largest(vr[0], 0))))) >= kExponent)) drop_rows(kr, vr, kNanPair);
+    const long tail_block = ((long)slot * a.c.kv_heads + h) * P * D;
+    if (rows.k_new) store_unit(a.c.k_tail + tail_block + (long)r * D, l, kr);
+    uint16_t* const v_tail = a.c.v_tail + tail_block + v_at;
 #pragma unroll
-        for (int i = 0; i < PASSES; ++i) {
-          const int r = i * RP + tid / LPR, rv = PASSES * (tid / LPR) + i;
-          if (r >= lo && r < hi) {
-            *reinterpret_cast<u32x4*>(k_tail + (long)r * D + l.at0) = kr[i][0];
-            *reinterpret_cast<u32x4*>(k_tail + (long)r * D + l.at1) = kr[i][1];
-          }
-          if (rv >= lo && rv < hi) {
-            uint16_t* dst = v_tail + (long)(rv / 64) * 64 * D + 16 * unit * 64 + rv % 64;
-#pragma unroll
-            for (int j = 0; j < 8; ++j) {
-              dst[j * 64] = (uint16_t)(vr[i][0][j / 2] >> (16 * (j & 1)));
-              dst[(8 + j) * 64] = (uint16_t)(vr[i][1][j / 2] >> (16 * (j & 1)));
-            }
-          }
-        }
-        continue;
-      }
-      // ---- the page is full: one step for the block's keys, one for its values ----
-      float k_amax = 0.f, v_amax = 0.f;
-#pragma unroll
-      for (int i = 0; i < PASSES; ++i) {
-        float x[16];
-        unpack8<T>(kr[i][0], x);
-        unpack8<T>(kr[i][1], x + 8);
-#pragma unroll
-        for (int j = 0; j < 16; ++j) k_amax = fmaxf(k_amax, fabsf(x[j]));
-        unpack8<T>(vr[i][0], x);
-        unpack8<T>(vr[i][1], x + 8);
-#pragma unroll
-        for (int j = 0; j < 16; ++j) v_amax = fmaxf(v_amax, fabsf(x[j]));
-      }
-      for (int o = 32; o; o >>= 1) {
-        k_amax = fmaxf(k_amax, __shfl_xor(k_amax, o));
-        v_amax = fmaxf(v_amax, __shfl_xor(v_amax, o));
-      }
-      const int any_bad = __any(bad);
-      if (lane == 0) { s_amax[0][wave] = k_amax; s_amax[1][wave] = v_amax; s_bad[wave] = any_bad; }
-      __syncthreads();
-      k_amax = fmaxf(fmaxf(s_amax[0][0], s_amax[0][1]), fmaxf(s_amax[0][2], s_amax[0][3]));
-      v_amax = fmaxf(fmaxf(s_amax[1][0], s_amax[1][1]), fmaxf(s_amax[1][2], s_amax[1][3]));
-      const bool nan_block = s_bad[0] | s_bad[1] | s_bad[2] | s_bad[3] | (lo > 0 && !slot_ok);   // (rows of no slot)
-      const float rk = inverse_step<FP8>(k_amax), rv_step = inverse_step<FP8>(v_amax);
-      const long block = (long)page_id * a.c.kv_heads + h;
-      if (tid == 0) {
-        a.c.k_scales[block] = nan_block ? __builtin_nanf("") : rk > 0.f ? 1.f / rk : 1.f;
-        a.c.v_scales[block] = rv_step > 0.f ? 1.f / rv_step : 1.f;
-      }
-      uint8_t* const k_codes = a.c.k_codes + block * P * D;
-      uint8_t* const v_codes = a.c.v_codes + block * P * D;
-      uint32_t vc[PASSES][4];
-#pragma unroll
-      for (int i = 0; i < PASSES; ++i) {
-        const int r = i * RP + tid / LPR;
-        float x[16];
-        unpack8<T>(kr[i][0], x);
-        unpack8<T>(kr[i][1], x + 8);
-#pragma unroll
-        for (int j = 0; j < 2; ++j) {
-          const u32x2 w = {codes4<FP8>(x[8 * j] * rk, x[8 * j + 1] * rk, x[8 * j + 2] * rk, x[8 * j + 3] * rk),
-                           codes4<FP8>(x[8 * j + 4] * rk, x[8 * j + 5] * rk, x[8 * j + 6] * rk, x[8 * j + 7] * rk)};
-          *reinterpret_cast<u32x2*>(k_codes + (long)r * D + (j ? l.at1 : l.at0)) = w;
-        }
-        unpack8<T>(vr[i][0], x);
-        unpack8<T>(vr[i][1], x + 8);
-#pragma unroll
-        for (int j = 0; j < 4; ++j)
-          vc[i][j] = codes4<FP8>(x[4 * j] * rv_step, x[4 * j + 1] * rv_step, x[4 * j + 2] * rv_step, x[4 * j + 3] * rv_step);
-      }
-      // values channel by channel: the thread's rows are neighbours of a channel's run
-      const int rv0 = PASSES * (tid / LPR);
-#pragma unroll
-      for (int j = 0; j < 16; ++j) {
-        uint8_t* dst = s_v + (rv0 / 64) * D * VS + (16 * unit + j) * VS + rv0 % 64;
-        uint32_t w = 0;
-#pragma unroll
-        for (int i = 0; i < PASSES; ++i) w |= (vc[i][j / 4] >> (8 * (j & 3)) & 255u) << (8 * i);
-        if constexpr (PASSES == 4) *reinterpret_cast<uint32_t*>(dst) = w;
-        else if constexpr (PASSES == 2) *reinterpret_cast<uint16_t*>(dst) = (uint16_t)w;
-        else *dst = (uint8_t)w;
-      }
-      __syncthreads();
-#pragma unroll
-      for (int i = 0; i < P * D / 16 / kPagedThreads; ++i) {
-        const int piece = i * kPagedThreads + tid;        // 16 codes of a channel's run
-        const uint32_t* src = reinterpret_cast<const uint32_t*>(s_v + (piece / 4) * VS + 16 * (piece % 4));
-        *reinterpret_cast<u32x4*>(v_codes + 16l * piece) = u32x4{src[0], src[1], src[2], src[3]};
-      }
-      // (the next head's first barrier, or the next page's, keeps s_v and s_amax until all have read them)
+    for (int j = 0; j < 8; ++j) {
+      const uint32_t x = vr[0][j / 2] >> (16 * (j & 1)) & 0xFFFFu, y = vr[1][j / 2] >> (16 * (j & 1)) & 0xFFFFu;
+      if (rows.v_new[0] && rows.v_new[1]) *reinterpret_cast<uint32_t*>(v_tail + j * 64) = x | y << 16;
+      else if (rows.v_new[0]) v_tail[j * 64] = (uint16_t)x;
+      else if (rows.v_new[1]) v_tail[j * 64 + 1] = (uint16_t)y;
     }
   }
 }
@@ -397,7 +397,8 @@ static void for_format(const dq_paged_cache* c, Args... args) {
 
 template <typename T, int D, int P, bool F> struct LaunchAppend {
   static void go(AppendArgs a, dim3 grid, hipStream_t st) {
-    hipLaunchKernelGGL((paged_append_kernel<T, D, P, F>), grid, dim3(kPagedThreads), 0, st, a);
+    if (a.rot.interleaved) hipLaunchKernelGGL((paged_append_kernel<T, D, P, F, true>), grid, dim3(P * D / 16), 0, st, a);
+    else hipLaunchKernelGGL((paged_append_kernel<T, D, P, F, false>), grid, dim3(P * D / 16), 0, st, a);
   }
 };
 template <typename T, int D, int P, bool F> struct LaunchRead {
@@ -423,7 +424,7 @@ extern "C" int32_t dq_paged_append(const dq_paged_cache* cache, const dq_paged_b
   if (q) { a.q = *q; a.q_out = *q_out; }
   if (norm) a.norm = *norm;
   if (rot) a.rot = *rot;
-  const int rows_per_block = kPagedThreads / (cache->head_dim / 16);
+  const int rows_per_block = cache->page_tokens;
   const long items = batch->rows / cache->page_tokens + 2l * batch->batch;
   const long q_items = q ? (batch->rows + rows_per_block - 1) / rows_per_block : 0;
   // Heads that share a page's angles: four where the pages alone fill the chip.

@@ -65,59 +65,91 @@ template <> struct Element<f16x8> { typedef _Float16 type; };
 template <> struct Element<bf16x8> { typedef __bf16 type; };
 template <typename V> __device__ __forceinline__ typename Element<V>::type to_element(float x) { return (typename Element<V>::type)x; }
 
+// Compile-time switch of a lambda: with the test inside one body the compiler makes the mask's 64 comparisons and
+// selects part of every tile (a third of the vector instructions of a prompt).
+struct Masked { static constexpr bool value = true; };
+struct Whole { static constexpr bool value = false; };
+
+// Scores are scaled inside the exponential's argument; a factor of 0 (an underflow) would make NaN of a masked -inf.
+__device__ __forceinline__ float keep_sign(float f) { return f < 1e-37f ? 1e-37f : f; }   // (NaN stays)
+
 // Two 16-bit tokens of a value word, zero where the token lies behind the last one (`left` tokens count from the word's first).
 __device__ __forceinline__ uint32_t keep_tokens(uint32_t w, int left) { return left >= 2 ? w : left == 1 ? (w & 0xFFFFu) : 0u; }
 
-// Joins the partial results of a unit's splits in the workgroup that finishes last and writes the outputs.  The caller's
-// partials are device-scope stores; every wave waits for its own, then one thread takes a ticket at the memory side, so
-// the holder of the last ticket finds all of them performed and reads them with device-scope loads.
-// cols: valid columns of the unit; out_of(col): pointer to the column's output row.
-template <typename T, int D, typename Out>
-__device__ __forceinline__ void join_splits(const PagedAttnArgs& a, int unit, int stride_cols, int cols, int* s_last, Out out_of) {
+// Whether this workgroup is the last of its unit's splits to hand in its partial results.  They are device-scope stores; every
+// wave waits for its own, then one thread takes a ticket at the memory side, so the holder of the last ticket finds all of
+// them performed; it reads them with device-scope loads.
+__device__ __forceinline__ bool last_of_splits(const PagedAttnArgs& a, int unit, int& s_last) {
   asm volatile("s_waitcnt vmcnt(0)" ::: "memory");
   __builtin_amdgcn_fence(__ATOMIC_RELEASE, "workgroup");
   __syncthreads();
   if (threadIdx.x == 0) {
     const int ticket = __hip_atomic_fetch_add(a.counters + unit, 1, __ATOMIC_RELAXED, __HIP_MEMORY_SCOPE_AGENT);
-    *s_last = ticket == a.splits - 1;
-    if (*s_last) __hip_atomic_store(a.counters + unit, 0, __ATOMIC_RELAXED, __HIP_MEMORY_SCOPE_AGENT);   // clean for the next call
+    s_last = ticket == a.splits - 1;
+    if (s_last) __hip_atomic_store(a.counters + unit, 0, __ATOMIC_RELAXED, __HIP_MEMORY_SCOPE_AGENT);   // clean for the next call
   }
   __syncthreads();
-  if (!*s_last) return;
+  return s_last;
+}
+
+struct JoinSpace {   // LDS
+  float m[16][kMaxSplits], l[16][kMaxSplits], inv[16];
+  int last;
+};
+
+// Joins the partial results of a unit's splits and writes the outputs.
+// cols: valid columns of the unit; out_of(col): pointer to the column's output row.
+template <typename T, int D, typename Out>
+__device__ __forceinline__ void join_splits(const PagedAttnArgs& a, int unit, int stride_cols, int cols, JoinSpace& js, Out out_of) {
+  if (!last_of_splits(a, unit, js.last)) return;
   const float* base = a.partials + (long)unit * a.splits * stride_cols * (D + 2);
   const long step = (long)stride_cols * (D + 2);
-  for (int idx = threadIdx.x; idx < cols * D; idx += blockDim.x) {
-    const int col = idx / D, c = idx % D;
-    const float* at = base + (long)col * (D + 2);
-    float M = -INFINITY;
-    for (int s = 0; s < a.splits; s += 8) {
-      float m[8];
-#pragma unroll
-      for (int k = 0; k < 8; ++k) m[k] = s + k < a.splits ? __hip_atomic_load(at + (s + k) * step + D, __ATOMIC_RELAXED, __HIP_MEMORY_SCOPE_AGENT) : -INFINITY;
-#pragma unroll
-      for (int k = 0; k < 8; ++k) M = fmaxf(M, m[k]);
+  // Sixteen columns at a time: every (column, split)'s maximum and sum in one round trip, weights to LDS, then the elements,
+  // eight splits of two of them on their way together.
+  const int ns = a.splits, tid = threadIdx.x, threads = blockDim.x;
+  auto load = [](const float* p) __attribute__((always_inline)) { return __hip_atomic_load(p, __ATOMIC_RELAXED, __HIP_MEMORY_SCOPE_AGENT); };
+  for (int c0 = 0; c0 < cols; c0 += 16) {
+    const int nc = min(16, cols - c0);
+    for (int i = tid; i < nc * ns; i += threads) {
+      const float* p = base + (i % ns) * step + (long)(c0 + i / ns) * (D + 2) + D;
+      js.m[i / ns][i % ns] = load(p);
+      js.l[i / ns][i % ns] = load(p + 1);
     }
-    const float base_m = M == -INFINITY ? 0.f : M;
-    float o = 0.f, l = 0.f;
-    for (int s = 0; s < a.splits; s += 8) {
-      float m[8], ll[8], oo[8];
-#pragma unroll
-      for (int k = 0; k < 8; ++k) {
-        const bool in = s + k < a.splits;
-        const float* p = at + (in ? s + k : s) * step;
-        m[k] = in ? __hip_atomic_load(p + D, __ATOMIC_RELAXED, __HIP_MEMORY_SCOPE_AGENT) : -INFINITY;
-        ll[k] = in ? __hip_atomic_load(p + D + 1, __ATOMIC_RELAXED, __HIP_MEMORY_SCOPE_AGENT) : 0.f;
-        oo[k] = in ? __hip_atomic_load(p + c, __ATOMIC_RELAXED, __HIP_MEMORY_SCOPE_AGENT) : 0.f;
+    __syncthreads();
+    for (int col = tid; col < nc; col += threads) {
+      float M = -INFINITY, l = 0.f;
+      for (int s = 0; s < ns; ++s) M = fmaxf(M, js.m[col][s]);
+      const float at = M == -INFINITY ? 0.f : M;
+      for (int s = 0; s < ns; ++s) {
+        const float w = __builtin_amdgcn_exp2f(js.m[col][s] - at);
+        js.m[col][s] = w;
+        l = __builtin_fmaf(js.l[col][s], w, l);
       }
-#pragma unroll
-      for (int k = 0; k < 8; ++k) {
-        const float w = __builtin_amdgcn_exp2f(m[k] - base_m);
-        o = __builtin_fmaf(oo[k], w, o);
-        l = __builtin_fmaf(ll[k], w, l);
-      }
+      js.inv[col] = l == 0.f ? 0.f : 1.f / l;
     }
-    const T y = (T)(l == 0.f ? 0.f : o / l);
-    out_of(col)[c] = __builtin_bit_cast(uint16_t, y);
+    __syncthreads();
+    for (int idx = 2 * tid; idx < nc * D; idx += 2 * threads) {
+      const int col = idx / D, c = idx % D;
+      const float* p = base + (long)(c0 + col) * (D + 2) + c;
+      float x = 0.f, y = 0.f;
+      for (int s = 0; s < ns; s += 8) {
+        float u[8], v[8];
+#pragma unroll
+        for (int k = 0; k < 8; ++k) {
+          const int at = min(s + k, ns - 1);
+          u[k] = load(p + at * step);
+          v[k] = load(p + at * step + 1);
+        }
+#pragma unroll
+        for (int k = 0; k < 8; ++k) {
+          if (s + k >= ns) break;
+          x = __builtin_fmaf(u[k], js.m[col][s + k], x);
+          y = __builtin_fmaf(v[k], js.m[col][s + k], y);
+        }
+      }
+      *reinterpret_cast<uint32_t*>(out_of(c0 + col) + c) = pack2<T>(x * js.inv[col], y * js.inv[col]);
+    }
+    __syncthreads();
   }
 }
 

@@ -22,7 +22,7 @@ __global__ __launch_bounds__(kPagedThreads) void paged_decode_kernel(PagedAttnAr
   typedef typename Vec8<T>::type tx8;
   __shared__ float s_o[4][kCols][D + 1];
   __shared__ float s_m[4][kCols], s_l[4][kCols];
-  __shared__ int s_last;
+  __shared__ JoinSpace s_join;
   const int tid = threadIdx.x, lane = tid & 63, wave = tid >> 6, col = lane & 15, G = lane >> 4;
   const int unit = (int)blockIdx.x / a.splits, split = (int)blockIdx.x % a.splits;
   const int H = a.c.kv_heads, b = unit / H, h = unit % H, P = a.c.page_tokens;
@@ -74,19 +74,21 @@ __global__ __launch_bounds__(kPagedThreads) void paged_decode_kernel(PagedAttnAr
   for (int ct = 0; ct < NCT; ++ct) o[ct] = f32x4{0.f, 0.f, 0.f, 0.f};
   float m = -INFINITY, l = 0.f;
 
-  // Softmax of a tile's 16 scores of this lane (tokens 64 tile + 16 G + ..), in place: u -> p.
-  auto softmax = [&](float (&u)[16], int tile, float inv_sv) __attribute__((always_inline)) {
-    const int t0 = tile * kPagedTile;
-    if (t0 < all_lo || t0 + kPagedTile > all_hi) {
+  // Softmax of a tile's 16 products of this lane (tokens 64 tile + 16 G + ..), in place: u -> p = 2^(u f + add - m).
+  auto softmax = [&](float (&u)[16], int tile, float f, float add, float inv_sv, auto mask) __attribute__((always_inline)) {
+    if constexpr (decltype(mask)::value) {
+      const float poison = f - f;                         // NaN where the block is: for those who see it, not through a masked -inf
+      f = f == f ? f : 1.f;
 #pragma unroll
       for (int j = 0; j < 16; ++j) {
-        const int t = t0 + 16 * G + j;
-        if (t < see_lo || t >= see_hi) u[j] = -INFINITY;
+        const int t = tile * kPagedTile + 16 * G + j;
+        u[j] = t < see_lo || t >= see_hi ? -INFINITY : u[j] + poison;
       }
     }
     float top = u[0];
 #pragma unroll
     for (int j = 1; j < 16; ++j) top = fmaxf(top, u[j]);
+    top = __builtin_fmaf(top, f, add);
     if (__any(top > m + kLazy)) {
       top = fmaxf(top, __shfl_xor(top, 16));
       top = fmaxf(top, __shfl_xor(top, 32));
@@ -97,11 +99,11 @@ __global__ __launch_bounds__(kPagedThreads) void paged_decode_kernel(PagedAttnAr
 #pragma unroll
       for (int ct = 0; ct < NCT; ++ct) o[ct] *= alpha;
     }
-    const float base = m == -INFINITY ? 0.f : m;
+    const float base = m == -INFINITY ? add : add - m;
     float sum = 0.f;
 #pragma unroll
     for (int j = 0; j < 16; ++j) {
-      u[j] = __builtin_amdgcn_exp2f(u[j] - base);
+      u[j] = __builtin_amdgcn_exp2f(__builtin_fmaf(u[j], f, base));
       sum += u[j];
     }
     l = __builtin_fmaf(sum, inv_sv, l);
@@ -142,7 +144,7 @@ __global__ __launch_bounds__(kPagedThreads) void paged_decode_kernel(PagedAttnAr
     load_k(0);
     load_v(0);
     for (int i = 0; i < count; ++i) {
-      const float f = __builtin_bit_cast(float, __builtin_amdgcn_readlane(__builtin_bit_cast(int, sk), i)) * sc;
+      const float f = __builtin_bit_cast(float, __builtin_amdgcn_readlane(__builtin_bit_cast(int, sk), i));
       const float add = __builtin_bit_cast(float, __builtin_amdgcn_readlane(__builtin_bit_cast(int, lsv), i));
       const float inv_sv = __builtin_bit_cast(float, __builtin_amdgcn_readlane(__builtin_bit_cast(int, isv), i));
       float u[16];
@@ -155,10 +157,12 @@ __global__ __launch_bounds__(kPagedThreads) void paged_decode_kernel(PagedAttnAr
           acc = mma16(codes_f16<FP8>(kb[t4][c].z, kb[t4][c].w), q[c][1], acc);
         }
 #pragma unroll
-        for (int j = 0; j < 4; ++j) u[4 * t4 + j] = __builtin_fmaf(acc[j], f, add);
+        for (int j = 0; j < 4; ++j) u[4 * t4 + j] = acc[j];
       }
       if (i + 1 < count) load_k(i + 1);
-      softmax(u, batch0 + i * stride, inv_sv);
+      const int tile = batch0 + i * stride;
+      if (tile * kPagedTile < all_lo || tile * kPagedTile + kPagedTile > all_hi) softmax(u, tile, keep_sign(f * sc), add, inv_sv, Masked{});
+      else softmax(u, tile, keep_sign(f * sc), add, inv_sv, Whole{});
       f16x8 p0, p1;
 #pragma unroll
       for (int j = 0; j < 8; ++j) { p0[j] = (_Float16)u[j]; p1[j] = (_Float16)u[8 + j]; }
@@ -181,7 +185,7 @@ __global__ __launch_bounds__(kPagedThreads) void paged_decode_kernel(PagedAttnAr
     const long at = (((long)(ok ? slot : 0) * H + h) * runs + run) * kPagedTile * D;
     const uint16_t* const kt = a.c.k_tail + at + k_row * D + 16 * G;
     const uint16_t* const vt = a.c.v_tail + at + (lane & 15) * kPagedTile + 16 * G;
-    const float f = ok ? a.scale_log2 : __builtin_nanf("");
+    const float f = ok ? keep_sign(a.scale_log2) : __builtin_nanf("");
     float u[16];
     tx8 qt[NC][2];
 #pragma unroll
@@ -197,12 +201,9 @@ __global__ __launch_bounds__(kPagedThreads) void paged_decode_kernel(PagedAttnAr
         for (int hf = 0; hf < 2; ++hf)
           acc = mma16(__builtin_bit_cast(tx8, *reinterpret_cast<const u32x4*>(kt + 4 * t4 * D + 64 * c + 8 * hf)), qt[c][hf], acc);
 #pragma unroll
-      for (int j = 0; j < 4; ++j) {
-        u[4 * t4 + j] = acc[j] * f;
-        if (16 * G + 4 * t4 + j >= left) u[4 * t4 + j] = -INFINITY;   // (a column that sees all tokens, and rows that hold anything)
-      }
+      for (int j = 0; j < 4; ++j) u[4 * t4 + j] = acc[j];
     }
-    softmax(u, tile, 1.f);
+    softmax(u, tile, f, 0.f, 1.f, Masked{});
     u32x4 p0, p1;
 #pragma unroll
     for (int j = 0; j < 4; ++j) { p0[j] = pack2<T>(u[2 * j], u[2 * j + 1]); p1[j] = pack2<T>(u[8 + 2 * j], u[8 + 2 * j + 1]); }
@@ -253,7 +254,7 @@ __global__ __launch_bounds__(kPagedThreads) void paged_decode_kernel(PagedAttnAr
       }
     }
   }
-  if (a.splits > 1) join_splits<T, D>(a, unit, kCols, cols, &s_last, out_of);
+  if (a.splits > 1) join_splits<T, D>(a, unit, kCols, cols, s_join, out_of);
 }
 
 template <typename T, int D>

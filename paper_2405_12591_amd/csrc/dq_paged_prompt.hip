@@ -5,6 +5,7 @@
 namespace dq {
 
 constexpr int kPromptWaves = 4;
+constexpr int kPromptSplits = 32;   // at most, of a tile of rows (their weights fit LDS)
 
 // Token of row r of a transposed 32-token score product: chosen so that a lane's 16 scores are tokens 8 h .. 8 h + 7 and
 // 16 + 8 h .. of the 32 (h = lane / 32), the right operand that the product with the values wants.
@@ -99,133 +100,163 @@ __global__ __launch_bounds__(64 * kPromptWaves, RB == 1 ? 2 : 1) void paged_prom
       for (int e = 0; e < 16; ++e) o[rb][ct][e] = 0.f;
   }
 
-  auto k_at = [&](int token, int piece) { return token * (D / 8) + (D == 128 ? piece ^ (token & 15) : piece ^ ((token >> 1) & 7)); };
-  auto v_at = [&](int ch, int piece) { return ch * 8 + (piece ^ ((ch >> 1) & 7)); };
+  // Places of 16-byte pieces in LDS.  Reads: 8 and 16 neighbouring lanes (tokens in score_token's order, or channels) hit different
+  // banks.  Writes: the two pieces of a thread's 16 codes lie half a row apart, so 8 neighbouring lanes do as well.
+  auto k_at = [&](int token, int piece) {
+    const int key = (token & 3) | (token >> 3 & 1) << 2 | (token >> 2 & 1) << 3;
+    return D == 128 ? token * 16 + ((piece >> 1 | (piece & 1) << 3) ^ key) : token * 8 + (piece ^ (key & 7) ^ (key >> 3));
+  };
+  auto v_at = [&](int ch, int piece) { return ch * 8 + (piece ^ (ch & 7) ^ (ch >> 3 & 1)); };
 
-  // Softmax of 32 tokens' scores from t0 on (lane: 8 hl .. and 16 + 8 hl ..), u -> p.
-  auto softmax = [&](f32x16& u, int rb, int t0, float inv_sv, bool masked) __attribute__((always_inline)) {
-    if (masked) {
-#pragma unroll
-      for (int e = 0; e < 16; ++e) {
-        const int t = t0 + 16 * (e >> 3) + 8 * hl + (e & 7);
-        if (t < see_lo[rb] || t >= see_hi[rb]) u[e] = -INFINITY;
-      }
+  // ---- a tile of 64 tokens ----
+  // Codes of the tile after it, on their way from memory to LDS; slice k of NK is turned to f16 between the matrix
+  // instructions of the scores, which leave the vector unit idle.
+  u32x4 kc[NB], vc[NB];
+  auto store_slice = [&](int buf, int k) __attribute__((always_inline)) {
+    const int i = k / 4, half = k & 1, piece = i * THREADS + tid;   // 16 codes: two pieces of keys, two of values
+    if ((k & 2) == 0) {
+      const int token = piece / (D / 16), kp = 2 * (piece % (D / 16)) + half;
+      s_k[buf][k_at(token, kp)] = __builtin_bit_cast(u32x4, half ? codes_f16<FP8>(kc[i].z, kc[i].w) : codes_f16<FP8>(kc[i].x, kc[i].y));
+    } else {
+      s_v[buf][v_at(piece / 4, 2 * (piece % 4) + half)] = __builtin_bit_cast(u32x4, half ? codes_f16<FP8>(vc[i].z, vc[i].w) : codes_f16<FP8>(vc[i].x, vc[i].y));
     }
-    float top = u[0];
-#pragma unroll
-    for (int e = 1; e < 16; ++e) top = fmaxf(top, u[e]);
-    if (__any(top > m[rb] + kLazy)) {
-      top = fmaxf(top, __shfl_xor(top, 32));
-      const float m_new = fmaxf(m[rb], top);
-      const float alpha = m_new == -INFINITY ? 1.f : __builtin_amdgcn_exp2f(m[rb] - m_new);
-      m[rb] = m_new;
-      l[rb] *= alpha;
-#pragma unroll
-      for (int ct = 0; ct < NCT; ++ct) o[rb][ct] *= alpha;
-    }
-    const float base = m[rb] == -INFINITY ? 0.f : m[rb];
-    float sum = 0.f;
-#pragma unroll
-    for (int e = 0; e < 16; ++e) {
-      u[e] = __builtin_amdgcn_exp2f(u[e] - base);
-      sum += u[e];
-    }
-    l[rb] = __builtin_fmaf(sum, inv_sv, l[rb]);
   };
 
-  // A tile of 64 tokens in buffer `buf`, elements of type E (f16 of codes, or the rows' own type).
-  auto work_tile = [&](int buf, int tile, auto zero, const auto& qf, auto scale_of, float add, float inv_sv) __attribute__((always_inline)) {
+  // Tile in buffer `buf`, elements of the type of `zero` (f16 of codes, or the rows' own type); `slice(k)` is done after the
+  // k-th pair of score products.  p = 2^(s f + add - m); lane: tokens 32 tt + 16 (e / 8) + 8 hl + e % 8.
+  auto work_tile = [&](int buf, int tile, auto zero, const auto& qf, auto scale_of, float add, float inv_sv, auto mask, auto slice) __attribute__((always_inline)) {
     typedef decltype(zero) ex8;
-    const bool masked = tile * kPagedTile < all_lo || tile * kPagedTile + kPagedTile > all_hi;
+    f32x16 u[RB][2];
 #pragma unroll
-    for (int tt = 0; tt < 2; ++tt) {
-      f32x16 u[RB];
+    for (int rb = 0; rb < RB; ++rb)
 #pragma unroll
-      for (int rb = 0; rb < RB; ++rb)
+      for (int e = 0; e < 32; ++e) u[rb][e >> 4][e & 15] = 0.f;
+    __builtin_amdgcn_s_setprio(1);   // matrix instructions go ahead of the other workgroup's softmax: 526 -> 507 us on 61 G products
 #pragma unroll
-        for (int e = 0; e < 16; ++e) u[rb][e] = 0.f;
-      const int token = 32 * tt + score_token(r32);
+    for (int k = 0; k < NK; ++k) {
 #pragma unroll
-      for (int k = 0; k < NK; ++k) {
-        const ex8 kf = __builtin_bit_cast(ex8, s_k[buf][k_at(token, 2 * k + hl)]);
+      for (int tt = 0; tt < 2; ++tt) {
+        const ex8 kf = __builtin_bit_cast(ex8, s_k[buf][k_at(32 * tt + score_token(r32), 2 * k + hl)]);
 #pragma unroll
-        for (int rb = 0; rb < RB; ++rb) u[rb] = mma32(kf, qf[rb][k], u[rb]);
+        for (int rb = 0; rb < RB; ++rb) u[rb][tt] = mma32(kf, qf[rb][k], u[rb][tt]);
       }
+      slice(k);
+    }
+    __builtin_amdgcn_s_setprio(0);
+    float base[RB], f[RB], sum[RB];
 #pragma unroll
-      for (int rb = 0; rb < RB; ++rb) {
-        const float f = scale_of(rb);
+    for (int rb = 0; rb < RB; ++rb) {
+      f[rb] = scale_of(rb);
+      if constexpr (decltype(mask)::value) {
+        const float poison = f[rb] - f[rb];               // NaN where the block is: for those who see it, not through a masked -inf
+        f[rb] = f[rb] == f[rb] ? f[rb] : 1.f;
 #pragma unroll
-        for (int e = 0; e < 16; ++e) u[rb][e] = __builtin_fmaf(u[rb][e], f, add);
-        softmax(u[rb], rb, tile * kPagedTile + 32 * tt, inv_sv, masked);
-      }
-#pragma unroll
-      for (int half = 0; half < 2; ++half) {
-        ex8 p[RB];
-#pragma unroll
-        for (int rb = 0; rb < RB; ++rb)
-#pragma unroll
-          for (int e = 0; e < 8; ++e) p[rb][e] = to_element<ex8>(u[rb][8 * half + e]);
-#pragma unroll
-        for (int ct = 0; ct < NCT; ++ct) {
-          const ex8 vf = __builtin_bit_cast(ex8, s_v[buf][v_at(32 * ct + r32, 4 * tt + 2 * half + hl)]);
-#pragma unroll
-          for (int rb = 0; rb < RB; ++rb) o[rb][ct] = mma32(vf, p[rb], o[rb][ct]);
+        for (int e = 0; e < 32; ++e) {
+          const int t = tile * kPagedTile + 32 * (e >> 4) + 16 * (e >> 3 & 1) + 8 * hl + (e & 7);
+          u[rb][e >> 4][e & 15] = t < see_lo[rb] || t >= see_hi[rb] ? -INFINITY : u[rb][e >> 4][e & 15] + poison;
         }
       }
-    }
-  };
-
-  // ---- full pages: a tile's codes in registers while the one before is worked ----
-  u32x4 kc[NB], vc[NB];
-  auto store_tile = [&](int buf) __attribute__((always_inline)) {
+      float top = u[rb][0][0];
 #pragma unroll
-    for (int i = 0; i < NB; ++i) {
-      const int piece = i * THREADS + tid;                // 16 codes
-      const int token = piece / (D / 16), kp = 2 * (piece % (D / 16)), ch = piece / 4, vp = 2 * (piece % 4);
-      s_k[buf][k_at(token, kp)] = __builtin_bit_cast(u32x4, codes_f16<FP8>(kc[i].x, kc[i].y));
-      s_k[buf][k_at(token, kp + 1)] = __builtin_bit_cast(u32x4, codes_f16<FP8>(kc[i].z, kc[i].w));
-      s_v[buf][v_at(ch, vp)] = __builtin_bit_cast(u32x4, codes_f16<FP8>(vc[i].x, vc[i].y));
-      s_v[buf][v_at(ch, vp + 1)] = __builtin_bit_cast(u32x4, codes_f16<FP8>(vc[i].z, vc[i].w));
-    }
-  };
-  const int code_end = min(t_last, code_tiles);
-  for (int batch0 = t_first; batch0 < code_end; batch0 += 64) {
-    const int t_l = batch0 + lane;
-    int blk = 0;
-    float sk = 0.f, lsv = 0.f, isv = 0.f;
-    if (t_l < code_end) {
-      const int page = a.bt.page_table[(long)b * a.bt.table_stride + t_l / runs];
-      const bool ok = page >= 0 && page < a.c.pages;
-      const long block = (long)(ok ? page : 0) * H + h;
-      blk = (int)(block * runs) + t_l % runs;
-      sk = ok ? a.c.k_scales[block] : __builtin_nanf("");
-      const float sv = ok ? a.c.v_scales[block] : 1.f;
-      lsv = __builtin_amdgcn_logf(sv);
-      isv = 1.f / sv;
-    }
-    const int count = min(64, code_end - batch0);
-    auto load_tile = [&](int i) __attribute__((always_inline)) {
-      const long at = (long)__builtin_amdgcn_readlane(blk, i) * (kPagedTile * D);
+      for (int e = 1; e < 32; ++e) top = fmaxf(top, u[rb][e >> 4][e & 15]);
+      top = __builtin_fmaf(top, f[rb], add);
+      if (__any(top > m[rb] + kLazy)) {
+        top = fmaxf(top, __shfl_xor(top, 32));
+        const float m_new = fmaxf(m[rb], top);
+        const float alpha = m_new == -INFINITY ? 1.f : __builtin_amdgcn_exp2f(m[rb] - m_new);
+        m[rb] = m_new;
+        l[rb] *= alpha;
 #pragma unroll
-      for (int k = 0; k < NB; ++k) {
-        kc[k] = *reinterpret_cast<const u32x4*>(a.c.k_codes + at + 16l * (k * THREADS + tid));
-        vc[k] = *reinterpret_cast<const u32x4*>(a.c.v_codes + at + 16l * (k * THREADS + tid));
+        for (int ct = 0; ct < NCT; ++ct) o[rb][ct] *= alpha;
+      }
+      base[rb] = m[rb] == -INFINITY ? add : add - m[rb];
+      sum[rb] = 0.f;
+    }
+    // Probabilities of 16 tokens (8 a lane) are made between the products of the 16 before them.
+    ex8 p[RB], p_next[RB];
+    auto probabilities = [&](int g, ex8 (&to)[RB]) __attribute__((always_inline)) {
+#pragma unroll
+      for (int rb = 0; rb < RB; ++rb) {
+        float x[8];
+#pragma unroll
+        for (int e = 0; e < 8; ++e) {
+          x[e] = __builtin_amdgcn_exp2f(__builtin_fmaf(u[rb][g >> 1][8 * (g & 1) + e], f[rb], base[rb]));
+          to[rb][e] = to_element<ex8>(x[e]);
+        }
+        sum[rb] += ((x[0] + x[1]) + (x[2] + x[3])) + ((x[4] + x[5]) + (x[6] + x[7]));
       }
     };
-    load_tile(0);
-    __syncthreads();                                      // buffer 0 has been read
-    store_tile(0);
-    __syncthreads();
-    for (int i = 0; i < count; ++i) {
-      if (i + 1 < count) load_tile(i + 1);
-      const float f = __builtin_bit_cast(float, __builtin_amdgcn_readlane(__builtin_bit_cast(int, sk), i));
-      const float add = __builtin_bit_cast(float, __builtin_amdgcn_readlane(__builtin_bit_cast(int, lsv), i));
-      const float inv_sv = __builtin_bit_cast(float, __builtin_amdgcn_readlane(__builtin_bit_cast(int, isv), i));
-      work_tile(i & 1, batch0 + i, f16x8{}, q, [&](int rb) { return f * sc[rb]; }, add, inv_sv);
-      if (i + 1 < count) store_tile((i + 1) & 1);
-      __syncthreads();
+    probabilities(0, p);
+    __builtin_amdgcn_s_setprio(1);   // matrix instructions go ahead of the other workgroup's softmax: 526 -> 507 us on 61 G products
+#pragma unroll
+    for (int g = 0; g < 4; ++g) {
+#pragma unroll
+      for (int ct = 0; ct < NCT; ++ct) {
+        const ex8 vf = __builtin_bit_cast(ex8, s_v[buf][v_at(32 * ct + r32, 2 * g + hl)]);
+#pragma unroll
+        for (int rb = 0; rb < RB; ++rb) o[rb][ct] = mma32(vf, p[rb], o[rb][ct]);
+      }
+      if (g < 3) {
+        probabilities(g + 1, p_next);
+#pragma unroll
+        for (int rb = 0; rb < RB; ++rb) p[rb] = p_next[rb];
+      }
     }
-  }
+#pragma unroll
+    for (int rb = 0; rb < RB; ++rb) l[rb] = __builtin_fmaf(sum[rb], inv_sv, l[rb]);
+    __builtin_amdgcn_s_setprio(0);
+  };
+
+  // `total` tiles of full pages, the i-th of them tile_of(i).
+  auto run = [&](int total, auto tile_of, auto mask) __attribute__((always_inline)) {
+    for (int batch0 = 0; batch0 < total; batch0 += 64) {
+      int blk = 0;
+      float sk = 0.f, lsv = 0.f, isv = 0.f;
+      if (batch0 + lane < total) {
+        const int t = tile_of(batch0 + lane), page = a.bt.page_table[(long)b * a.bt.table_stride + t / runs];
+        const bool ok = page >= 0 && page < a.c.pages;
+        const long block = (long)(ok ? page : 0) * H + h;
+        blk = (int)(block * runs) + t % runs;
+        sk = ok ? a.c.k_scales[block] : __builtin_nanf("");
+        const float sv = ok ? a.c.v_scales[block] : 1.f;
+        lsv = __builtin_amdgcn_logf(sv);
+        isv = 1.f / sv;
+      }
+      const int count = min(64, total - batch0);
+      auto load_tile = [&](int i) __attribute__((always_inline)) {   // (behind the last one: that one again, never used)
+        const long at = (long)__builtin_amdgcn_readlane(blk, min(i, count - 1)) * (kPagedTile * D);
+#pragma unroll
+        for (int k = 0; k < NB; ++k) {
+          kc[k] = *reinterpret_cast<const u32x4*>(a.c.k_codes + at + 16l * (k * THREADS + tid));
+          vc[k] = *reinterpret_cast<const u32x4*>(a.c.v_codes + at + 16l * (k * THREADS + tid));
+        }
+      };
+      load_tile(0);
+      __syncthreads();                                    // buffer 0 has been read
+#pragma unroll
+      for (int k = 0; k < NK; ++k) store_slice(0, k);
+      load_tile(1);
+      __syncthreads();
+      for (int i = 0; i < count; ++i) {
+        const float f = __builtin_bit_cast(float, __builtin_amdgcn_readlane(__builtin_bit_cast(int, sk), i));
+        const float add = __builtin_bit_cast(float, __builtin_amdgcn_readlane(__builtin_bit_cast(int, lsv), i));
+        const float inv_sv = __builtin_bit_cast(float, __builtin_amdgcn_readlane(__builtin_bit_cast(int, isv), i));
+        work_tile(i & 1, tile_of(batch0 + i), f16x8{}, q, [&](int rb) { return keep_sign(f * sc[rb]); }, add, inv_sv, mask,
+                  [&](int k) __attribute__((always_inline)) {
+                    store_slice((i + 1) & 1, k);
+                    if (k == NK - 1) load_tile(i + 2);
+                  });
+        __syncthreads();
+      }
+    }
+  };
+  // Tiles that every row sees whole, then those that need the mask (two loops: with both kinds in one, registers run out).
+  const int code_end = min(t_last, code_tiles);
+  const int whole_lo = min(max(t_first, (max(all_lo, 0) + kPagedTile - 1) / kPagedTile), max(code_end, t_first));
+  const int whole_hi = max(min(code_end, max(all_hi, 0) / kPagedTile), whole_lo);
+  run(whole_hi - whole_lo, [&](int i) { return whole_lo + i; }, Whole{});
+  const int before = whole_lo - t_first;
+  run(before + max(code_end - whole_hi, 0), [&](int i) { return i < before ? t_first + i : whole_hi + i - before; }, Masked{});
 
   // ---- the page being filled: 16-bit rows ----
   for (int tile = max(t_first, code_tiles); tile < t_last; ++tile) {
@@ -251,10 +282,9 @@ __global__ __launch_bounds__(64 * kPromptWaves, RB == 1 ? 2 : 1) void paged_prom
     for (int rb = 0; rb < RB; ++rb) {
 #pragma unroll
       for (int k = 0; k < NK; ++k) qt[rb][k] = __builtin_bit_cast(tx8, *reinterpret_cast<const u32x4*>(q_row[rb] + 16 * k));
-      see_hi[rb] = min(see_hi[rb], len);
     }
-    const float f = ok ? a.scale_log2 : __builtin_nanf("");
-    work_tile(0, tile, tx8{}, qt, [&](int) { return f; }, 0.f, 1.f);
+    const float f = ok ? keep_sign(a.scale_log2) : __builtin_nanf("");
+    work_tile(0, tile, tx8{}, qt, [&](int) { return f; }, 0.f, 1.f, Masked{}, [](int) {});
   }
 
   // ---- outputs, or partials for the workgroup that joins the splits ----
@@ -278,19 +308,57 @@ __global__ __launch_bounds__(64 * kPromptWaves, RB == 1 ? 2 : 1) void paged_prom
           *reinterpret_cast<u32x2*>(dst + 32 * ct + 8 * e + 4 * hl) = u32x2{pack2<T>(o[rb][ct][4 * e] * inv, o[rb][ct][4 * e + 1] * inv),
                                                                            pack2<T>(o[rb][ct][4 * e + 2] * inv, o[rb][ct][4 * e + 3] * inv)};
     } else {
-      float* const p = a.partials + (((long)unit * a.splits + split) * M + col) * (D + 2);
+      float* const p = a.partials + ((long)unit * a.splits + split) * (D + 2) * M + col;   // channel by channel: rows lie side by side
 #pragma unroll
       for (int ct = 0; ct < NCT; ++ct)
 #pragma unroll
         for (int e = 0; e < 16; ++e)
-          __hip_atomic_store(p + 32 * ct + 8 * (e >> 2) + 4 * hl + (e & 3), o[rb][ct][e], __ATOMIC_RELAXED, __HIP_MEMORY_SCOPE_AGENT);
+          __hip_atomic_store(p + (32 * ct + 8 * (e >> 2) + 4 * hl + (e & 3)) * M, o[rb][ct][e], __ATOMIC_RELAXED, __HIP_MEMORY_SCOPE_AGENT);
       if (hl == 0) {
-        __hip_atomic_store(p + D, m[rb], __ATOMIC_RELAXED, __HIP_MEMORY_SCOPE_AGENT);
-        __hip_atomic_store(p + D + 1, l[rb], __ATOMIC_RELAXED, __HIP_MEMORY_SCOPE_AGENT);
+        __hip_atomic_store(p + D * M, m[rb], __ATOMIC_RELAXED, __HIP_MEMORY_SCOPE_AGENT);
+        __hip_atomic_store(p + (D + 1) * M, l[rb], __ATOMIC_RELAXED, __HIP_MEMORY_SCOPE_AGENT);
       }
     }
   }
-  if (a.splits > 1) join_splits<T, D>(a, unit, M, min(M, pairs - first), &s_last, out_of);
+  if (a.splits == 1 || !last_of_splits(a, unit, s_last)) return;
+  // The splits' results: a thread takes a row and every (THREADS / M)-th run of eight channels of it.
+  static_assert(M <= THREADS && THREADS % M == 0 && sizeof(s_k) >= kPromptSplits * M * sizeof(float), "rows a thread, weights in LDS");
+  float* const weight = reinterpret_cast<float*>(s_k);    // [split][row]
+  const int col = tid % M, ns = a.splits;
+  const float* const part = a.partials + (long)unit * ns * (D + 2) * M + col;
+  auto load = [](const float* p) __attribute__((always_inline)) { return __hip_atomic_load(p, __ATOMIC_RELAXED, __HIP_MEMORY_SCOPE_AGENT); };
+  float top = -INFINITY, sum = 0.f;
+  if (tid < M) {
+    for (int i = 0; i < ns; ++i) {
+      const float x = load(part + ((long)i * (D + 2) + D) * M);
+      weight[i * M + col] = x;
+      top = fmaxf(top, x);
+    }
+    const float at = top == -INFINITY ? 0.f : top;
+    for (int i = 0; i < ns; ++i) {
+      const float w = __builtin_amdgcn_exp2f(weight[i * M + col] - at);
+      weight[i * M + col] = w;
+      sum = __builtin_fmaf(load(part + ((long)i * (D + 2) + D + 1) * M), w, sum);
+    }
+    reinterpret_cast<float*>(s_v)[col] = sum == 0.f ? 0.f : 1.f / sum;
+  }
+  __syncthreads();
+  if (first + col >= pairs) return;
+  const float inv = reinterpret_cast<float*>(s_v)[col];
+  for (int c = 8 * (tid / M); c < D; c += 8 * (THREADS / M)) {
+    float x[8] = {};
+    for (int i = 0; i < ns; ++i) {
+      const float w = weight[i * M + col];
+      float y[8];
+#pragma unroll
+      for (int e = 0; e < 8; ++e) y[e] = load(part + ((long)i * (D + 2) + c + e) * M);
+#pragma unroll
+      for (int e = 0; e < 8; ++e) x[e] = __builtin_fmaf(y[e], w, x[e]);
+    }
+#pragma unroll
+    for (int e = 0; e < 8; ++e) x[e] *= inv;
+    *reinterpret_cast<u32x4*>(out_of(col) + c) = pack8<T>(x);
+  }
 }
 
 constexpr int kPromptBlocks = 1;   // 32-row blocks of a wave
@@ -317,36 +385,60 @@ struct PagedShape {
   int splits, cols;
 };
 
-static int up_div(int a, int b) { return (a + b - 1) / b; }
+constexpr int kPagedCounters = 4096;      // units that may be split, with a ticket each at a fixed place: calls of all sizes may share a workspace
+constexpr int kMostSplitGroups = 1024;    // workgroups of a launch whose splits the library chose (below); tiles of rows: half of them may be empty
 
-// What the two queries below agree on: kernel, units and splits from the host's bounds.
-static bool paged_shape(const dq_paged_cache* c, int batch, long rows, int q_heads, int max_rows, int max_seq_len, PagedShape* s) {
+// Splits of a unit: as many as give `wanted` workgroups, or the next count that leaves few of them idle in the last round, at most
+// cap.  The smallest n within 4 % of the fullest rounds (so that a larger cap never means fewer splits).
+static int pick_splits(long units, int cap, int wanted) {
+  auto fill = [&](int n) { const long w = units * n; return (float)w / (float)(w <= wanted ? wanted : (w + wanted - 1) / wanted * wanted); };
+  float best = 0.f;
+  for (int n = 1; n <= cap && (n == 1 || units * n <= 2 * wanted); ++n) best = fmaxf(best, fill(n));
+  int n = 1;
+  while (fill(n) < 0.96f * best) ++n;
+  return n;
+}
+
+// Decode kernel: a workgroup per compute unit (two with 64 channels, whose waves have half the bytes on their way); at most 1.2 sqrt(tiles)
+// splits, where a split's ticket and merge (2 us) outweigh shorter shares; none below 12 tiles of 128 channels.  Measured over 1
+// to 1024 units of 2 to 2000 tiles, 13 split counts each: the picks are 1.3 % behind the best on average; 128 units of 512 tiles
+// 160 us in two splits, 165 in 6.
+static int decode_splits(long units, int tiles, int head_dim) {
+  if ((long)tiles * head_dim < 12 * 128) return 1;
+  const int cap = (int)(1.2f * sqrtf((float)tiles));
+  return pick_splits(units, cap < kMaxSplits ? cap : kMaxSplits, 256 * 128 / head_dim);
+}
+
+// Prompt kernel: two workgroups a compute unit; a split hands over 66 KB, so at most 0.75 sqrt(tiles).  8 units of 500 tiles 71 us in 16
+// splits, 521 in one, 85 in 32; 64 of 300 tiles 102 us in 8, 174 in 2, 128 in 12.
+static int prompt_cap(int tiles) {
+  const int cap = (int)(0.75f * sqrtf((float)tiles));
+  return cap < 1 ? 1 : cap < kPromptSplits ? cap : kPromptSplits;
+}
+
+// What the entry points agree on: kernel, units and splits from the host's bounds.
+static bool paged_shape(const dq_paged_cache* c, int batch, long rows, int q_heads, int max_rows, int max_seq_len, int window, uint32_t flags,
+                        PagedShape* s) {
   if (batch <= 0 || rows < 0 || q_heads <= 0 || q_heads % c->kv_heads || max_rows < 0 || max_seq_len < 0) return false;
   const int group = q_heads / c->kv_heads;
-  const int tiles = max_seq_len / kPagedTile + 1;
+  int tiles = max_seq_len / kPagedTile + 1;
+  if (window > 0 && ((long)window + max_rows) / kPagedTile + 2 < tiles) tiles = (int)(((long)window + max_rows) / kPagedTile + 2);
   s->decode = (long)max_rows * group <= 16;
-  if (s->decode) {
-    s->units = (long)batch * c->kv_heads;
-    s->cols = 16;
-  } else {
-    if (rows * group >= (1l << 31)) return false;
-    s->units = (rows * group / kPromptRows + batch) * c->kv_heads;
-    s->cols = kPromptRows;
-  }
+  if ((long)batch * max_rows < rows) rows = (long)batch * max_rows;   // (rows behind the last sequence's)
+  if (rows * group >= (1l << 31)) return false;
+  s->units = s->decode ? (long)batch * c->kv_heads : (rows * group / kPromptRows + batch) * c->kv_heads;
+  s->cols = s->decode ? 16 : kPromptRows;
   if (s->units >= (1l << 24)) return false;
-  // workgroups the chip holds at once: two per compute unit
-  const long want = s->decode ? 768 : 512;
-  int n = (int)((want + s->units - 1) / s->units);
-  const int most = s->decode ? up_div(tiles, 4) : up_div(tiles, 8);   // a tile a wave at least, or eight tiles a workgroup
-  if (n > most) n = most;
-  if (n > kMaxSplits) n = kMaxSplits;
-  s->splits = n < 1 ? 1 : n;
+  // (a sequence leaves part of its last tile of rows empty; no more tiles than the longest sequence would have)
+  const long filled = (long)batch * (((long)max_rows * group + kPromptRows - 1) / kPromptRows) * c->kv_heads;
+  s->splits = s->decode ? decode_splits(s->units, tiles, c->head_dim) : pick_splits(filled < s->units ? filled : s->units, prompt_cap(tiles), 512);
+  if (const int v = (int)(flags >> 8 & 0x7Fu)) s->splits = !s->decode && v > kPromptSplits ? kPromptSplits : v;   // the caller's override
+  if (s->units > kPagedCounters) s->splits = 1;
   return true;
 }
 
-static size_t paged_bytes(const PagedShape& s, int head_dim) {
-  if (s.splits == 1) return kWsHeaderBytes;
-  return kWsHeaderBytes + align_up((size_t)s.units * sizeof(int32_t), 256) + (size_t)s.units * s.splits * s.cols * (head_dim + 2) * sizeof(float);
+static size_t paged_bytes(long groups, int cols, int head_dim) {
+  return (size_t)kWsHeaderBytes + kPagedCounters * sizeof(int32_t) + (size_t)groups * cols * (head_dim + 2) * sizeof(float);
 }
 
 }  // namespace dq
@@ -356,8 +448,18 @@ using namespace dq;
 extern "C" size_t dq_paged_workspace_bytes(const dq_paged_cache* cache, int32_t batch, int32_t rows, int32_t q_heads, int32_t max_rows,
                                            int32_t max_seq_len) {
   PagedShape s;
-  if (!paged_cache_ok(cache) || !paged_shape(cache, batch, rows, q_heads, max_rows, max_seq_len, &s)) return 0;
-  return paged_bytes(s, cache->head_dim);
+  if (!paged_cache_ok(cache) || !paged_shape(cache, batch, rows, q_heads, max_rows, max_seq_len, 0, 0, &s)) return 0;
+  // smaller calls have fewer units and may have more splits: their product is what is bounded
+  const int tiles = max_seq_len / kPagedTile + 1;
+  const long decode_units = (long)batch * cache->kv_heads;
+  auto most = [](long units, int splits, long groups) { const long n = units * splits; return splits == 1 ? 0l : n < groups ? n : groups; };
+  const int cap = (long)tiles * cache->head_dim < 12 * 128 ? 1 : kMaxSplits;
+  size_t bytes = paged_bytes(most(decode_units, cap, kMostSplitGroups), 16, cache->head_dim);
+  if (!s.decode) {
+    const size_t p = paged_bytes(most(s.units, prompt_cap(tiles), 2 * kMostSplitGroups), kPromptRows, cache->head_dim);
+    if (p > bytes) bytes = p;
+  }
+  return bytes;
 }
 
 extern "C" int32_t dq_paged_attention(const dq_paged_cache* cache, const dq_paged_batch* batch, const dq_heads* q, const dq_heads* out,
@@ -365,11 +467,12 @@ extern "C" int32_t dq_paged_attention(const dq_paged_cache* cache, const dq_page
                                       size_t workspace_bytes, uint32_t flags, void* hip_stream) {
   if (!paged_cache_ok(cache) || !paged_batch_ok(batch, cache, true) || !heads_ok(q, false) || !heads_ok(out, false)) return DQ_EINVAL;
   if (q->heads != out->heads || q->heads % cache->kv_heads || !workspace || ((uintptr_t)workspace & 15)) return DQ_EINVAL;
-  if ((flags & ~DQ_PAGED_CAUSAL) || window < 0 || (window && !(flags & DQ_PAGED_CAUSAL))) return DQ_EINVAL;
+  if ((flags & ~(DQ_PAGED_CAUSAL | DQ_PAGED_SPLITS(0x7F))) || (flags >> 8 & 0x7Fu) > (uint32_t)kMaxSplits || window < 0 || (window && !(flags & DQ_PAGED_CAUSAL)))
+    return DQ_EINVAL;
   if (softmax_scale != softmax_scale) return DQ_EINVAL;
   PagedShape s;
-  if (!paged_shape(cache, batch->batch, batch->rows, q->heads, max_rows, max_seq_len, &s)) return DQ_EINVAL;
-  if (workspace_bytes < paged_bytes(s, cache->head_dim)) return DQ_ENOSPACE;
+  if (!paged_shape(cache, batch->batch, batch->rows, q->heads, max_rows, max_seq_len, window, flags, &s)) return DQ_EINVAL;
+  if (workspace_bytes < paged_bytes(s.splits == 1 ? 0 : s.units * s.splits, s.cols, cache->head_dim)) return DQ_ENOSPACE;
   if (batch->rows == 0 || max_rows == 0) return DQ_OK;
   PagedAttnArgs a = {};
   a.c = *cache; a.bt = *batch; a.q = *q; a.out = *out;
@@ -383,7 +486,7 @@ extern "C" int32_t dq_paged_attention(const dq_paged_cache* cache, const dq_page
   a.units = (int)s.units;
   char* ws = reinterpret_cast<char*>(workspace);
   a.counters = reinterpret_cast<int32_t*>(ws + kWsHeaderBytes);
-  a.partials = reinterpret_cast<float*>(ws + kWsHeaderBytes + align_up((size_t)s.units * sizeof(int32_t), 256));
+  a.partials = reinterpret_cast<float*>(ws + kWsHeaderBytes + kPagedCounters * sizeof(int32_t));
   hipStream_t st = (hipStream_t)hip_stream;
   return s.decode ? launch_paged_decode(a, st) : launch_paged_prompt(a, st);
 }

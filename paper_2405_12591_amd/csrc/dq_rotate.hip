@@ -13,37 +13,50 @@ struct RotateArgs {
 
 // A thread keeps one unit (16 channels) of one token for all heads of its group, so the eight angles of the unit are
 // formed once and turn every head.  Bound by memory: 2 bytes in and 2 out per element against about 7 flops.
-template <typename T, int LANES>
+template <typename T, int LANES, bool INTERLEAVED>
 __global__ __launch_bounds__(kPagedThreads) void rotate_heads_kernel(RotateArgs a) {
   const int unit = threadIdx.x % LANES;
   const long column = (long)blockIdx.x * (kPagedThreads / LANES) + threadIdx.x / LANES;
   const bool live = column < (long)a.batch * a.tokens && 16 * unit < a.head_dim;
-  const int b = live ? (int)(column / a.tokens) : 0;
-  const long t = live ? column % a.tokens : 0;
-  const RowLayout l = row_layout(unit, a.rot.rot_dim, a.rot.interleaved);
-  float cs[8], sn[8];
+  const int b = live && a.batch > 1 ? (int)(column / a.tokens) : 0;
+  const long t = live ? column - (long)b * a.tokens : 0;
+  const RowLayout l = row_layout(unit, a.rot.rot_dim, INTERLEAVED);
+  const int h0 = blockIdx.y * a.heads_per_group, h1 = min(h0 + a.heads_per_group, a.q.heads + a.k.heads);
+  const uint16_t* const q = a.q.data + b * a.q.batch_stride + t * a.q.token_stride;
+  const uint16_t* const k = a.k.data + b * a.k.batch_stride + t * a.k.token_stride;
+  const int k0 = max(h0 - a.q.heads, 0);
   RowLayout turned = l;
   if (!live) turned.pair0 = -1;
-  unit_turns(a.rot, turned, column, 0, cs, sn);
-  const int h0 = blockIdx.y * a.heads_per_group, h1 = min(h0 + a.heads_per_group, a.q.heads + a.k.heads);
+  UnitTurns ut;
+  load_turns(a.rot, turned, column, 0, ut);
+  u32x4 v[2] = {};
+  if (live) load_unit(v, h0 < a.q.heads ? q + h0 * a.q.head_stride : k + k0 * a.k.head_stride, l);
+  float cs[8], sn[8];
+  make_turns(turned, ut, cs, sn);
   const float inv_dim = 1.0f / (float)a.head_dim;
-  if (h0 < a.q.heads)
-    rotate_row<T, LANES>(a.q.data + b * a.q.batch_stride + t * a.q.token_stride, a.q_out.data + b * a.q_out.batch_stride + t * a.q_out.token_stride,
-                         a.q.head_stride, a.q_out.head_stride, h0, min(h1, a.q.heads), live, l, a.norm.q_weight, a.norm.eps, inv_dim, cs, sn,
-                         a.rot.interleaved);
+  if (h0 < a.q.heads) {
+    rotate_row<T, LANES, INTERLEAVED>(v, q, a.q_out.data + b * a.q_out.batch_stride + t * a.q_out.token_stride, a.q.head_stride, a.q_out.head_stride, h0,
+                                      min(h1, a.q.heads), live, l, a.norm.q_weight, a.norm.eps, inv_dim, cs, sn);
+    if (live && h1 > a.q.heads) load_unit(v, k, l);
+  }
   if (h1 > a.q.heads)
-    rotate_row<T, LANES>(a.k.data + b * a.k.batch_stride + t * a.k.token_stride, a.k_out.data + b * a.k_out.batch_stride + t * a.k_out.token_stride,
-                         a.k.head_stride, a.k_out.head_stride, max(h0 - a.q.heads, 0), h1 - a.q.heads, live, l, a.norm.k_weight, a.norm.eps, inv_dim,
-                         cs, sn, a.rot.interleaved);
+    rotate_row<T, LANES, INTERLEAVED>(v, k, a.k_out.data + b * a.k_out.batch_stride + t * a.k_out.token_stride, a.k.head_stride, a.k_out.head_stride, k0,
+                                      h1 - a.q.heads, live, l, a.norm.k_weight, a.norm.eps, inv_dim, cs, sn);
+}
+
+template <typename T, int LANES>
+static void launch_rotate2(const RotateArgs& a, dim3 grid, hipStream_t st) {
+  if (a.rot.interleaved) hipLaunchKernelGGL((rotate_heads_kernel<T, LANES, true>), grid, dim3(kPagedThreads), 0, st, a);
+  else hipLaunchKernelGGL((rotate_heads_kernel<T, LANES, false>), grid, dim3(kPagedThreads), 0, st, a);
 }
 
 template <typename T>
 static void launch_rotate(const RotateArgs& a, int lanes, dim3 grid, hipStream_t st) {
   switch (lanes) {
-    case 2: hipLaunchKernelGGL((rotate_heads_kernel<T, 2>), grid, dim3(kPagedThreads), 0, st, a); break;
-    case 4: hipLaunchKernelGGL((rotate_heads_kernel<T, 4>), grid, dim3(kPagedThreads), 0, st, a); break;
-    case 8: hipLaunchKernelGGL((rotate_heads_kernel<T, 8>), grid, dim3(kPagedThreads), 0, st, a); break;
-    default: hipLaunchKernelGGL((rotate_heads_kernel<T, 16>), grid, dim3(kPagedThreads), 0, st, a); break;
+    case 2: launch_rotate2<T, 2>(a, grid, st); break;
+    case 4: launch_rotate2<T, 4>(a, grid, st); break;
+    case 8: launch_rotate2<T, 8>(a, grid, st); break;
+    default: launch_rotate2<T, 16>(a, grid, st); break;
   }
 }
 

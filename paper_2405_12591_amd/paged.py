@@ -3,30 +3,25 @@ checks and marshalling only."""
 from __future__ import annotations
 
 import ctypes as C
+import struct
 from dataclasses import dataclass
-from typing import Dict, Optional, Sequence, Tuple
+from typing import Dict, Optional, Sequence
 
 import torch
 
-from .binding import DQError, KVCacheLayer, _check, _raw_stream, lib, workspace_init
+from .binding import DQError, _check, _raw_stream, lib, workspace_init
 
 PAGED_CAUSAL = 1
 _DTYPES = {torch.float16: 0, torch.bfloat16: 1}
 _CODES = {torch.int8: 0, torch.float8_e4m3fn: 1}
 
 
-class _CHeads(C.Structure):
-    _fields_ = [("data", C.c_void_p), ("batch_stride", C.c_int64), ("token_stride", C.c_int64), ("head_stride", C.c_int64),
-                ("heads", C.c_int32)]
-
-
-class _CNorm(C.Structure):
-    _fields_ = [("q_weight", C.c_void_p), ("k_weight", C.c_void_p), ("eps", C.c_float)]
-
-
-class _CRotary(C.Structure):
-    _fields_ = [("inv_freq", C.c_void_p), ("positions", C.c_void_p), ("axis_of_pair", C.c_void_p), ("position_stride", C.c_int64),
-                ("axes", C.c_int32), ("rot_dim", C.c_int32), ("interleaved", C.c_int32)]
+# The small structs of a call (dq_heads, dq_head_norm, dq_rotary, dq_paged_batch), packed: a ctypes structure takes three times
+# as long to fill, and a call of these operators on the GPU is over in a few microseconds.
+_pack_heads = struct.Struct("@Pqqqi4x").pack
+_pack_norm = struct.Struct("@PPf4x").pack
+_pack_rotary = struct.Struct("@PPPqiii4x").pack
+_pack_batch = struct.Struct("@PPPPiiii").pack
 
 
 class _CPaged(C.Structure):
@@ -35,14 +30,9 @@ class _CPaged(C.Structure):
                 ("page_tokens", C.c_int32), ("slots", C.c_int32), ("dtype", C.c_int32), ("codes", C.c_int32)]
 
 
-class _CBatch(C.Structure):
-    _fields_ = [("starts", C.c_void_p), ("seq_lens", C.c_void_p), ("page_table", C.c_void_p), ("tail_slots", C.c_void_p),
-                ("batch", C.c_int32), ("rows", C.c_int32), ("table_width", C.c_int32), ("table_stride", C.c_int32)]
-
-
 def _declare() -> None:
-    heads, norm, rot, cache, batch = (C.POINTER(t) for t in (_CHeads, _CNorm, _CRotary, _CPaged, _CBatch))
-    i32, ptr = C.c_int32, C.c_void_p
+    cache, i32, ptr = C.POINTER(_CPaged), C.c_int32, C.c_void_p
+    heads = norm = rot = batch = ptr
     lib.dq_rotate_heads.restype = i32
     lib.dq_rotate_heads.argtypes = [heads, heads, heads, heads, i32, i32, i32, i32, norm, rot, ptr]
     lib.dq_paged_append.restype = i32
@@ -58,54 +48,69 @@ def _declare() -> None:
 _declare()
 
 
-def _on(device, *tensors) -> None:
+_current_device = getattr(torch._C, "_cuda_getDevice", None) or torch.cuda.current_device
+
+
+def _on(index: int, *tensors) -> None:
     for t in tensors:
-        if t is not None and t.device != device:
-            raise DQError("all tensors of a call must be on one device (%s and %s given)" % (device, t.device))
+        if t is not None and t.get_device() != index:
+            raise DQError("all tensors of a call must be on one GPU (cuda:%d and %s given)" % (index, t.device))
 
 
-def _call(what: str, fn, device, *args) -> None:
-    """fn(*args, stream) on `device`'s current stream, with that device current."""
-    index = device.index
-    if index is None or index != torch.cuda.current_device():
-        with torch.cuda.device(device):
-            st = fn(*args, torch.cuda.current_stream(device).cuda_stream)
+def _call(what: str, fn, index: int, *args) -> None:
+    """fn(*args, stream) on device `index`'s current stream, with that device current."""
+    if index != _current_device():
+        with torch.cuda.device(index):
+            st = fn(*args, torch.cuda.current_stream(index).cuda_stream)
     else:
-        st = fn(*args, _raw_stream(index) if _raw_stream else torch.cuda.current_stream(device).cuda_stream)
+        st = fn(*args, _raw_stream(index) if _raw_stream else torch.cuda.current_stream(index).cuda_stream)
     if st:
         _check(st, what)
 
 
-def _heads(name: str, t: torch.Tensor, dtype, dim: int) -> Tuple[_CHeads, Tuple[int, ...]]:
-    """[rows, heads, dim] or [batch, rows, heads, dim] with channels side by side; (struct, shape without heads and dim)."""
-    if t.dtype != dtype or not t.is_cuda or t.dim() not in (3, 4) or t.shape[-1] != dim:
-        raise DQError("%s must be a %s device tensor [rows, heads, %d] or [batch, rows, heads, %d]" % (name, dtype, dim, dim))
-    s = t.stride()
-    if s[-1] != 1 or any(x % 8 or x < 0 for x in s[:-1]) or t.data_ptr() % 16:
+def _heads(name: str, t: torch.Tensor, dtype, dim: int, index: int, written: bool = False):
+    """[rows, heads, dim] or [batch, rows, heads, dim] with channels side by side: (packed dq_heads, (batch,) rows, heads)."""
+    shape, strides = t.shape, t.stride()
+    if len(shape) == 3:
+        rows, heads, d = shape
+        s1, s2, s3 = strides
+        batch, s0 = 1, 0
+    elif len(shape) == 4:
+        batch, rows, heads, d = shape
+        s0, s1, s2, s3 = strides
+        if batch == 1:
+            s0 = 0
+    else:
+        raise DQError("%s must be [rows, heads, %d] or [batch, rows, heads, %d]" % (name, dim, dim))
+    if rows == 1:                                    # a stride over one entry says nothing
+        s1 = 0
+    if heads == 1:
+        s2 = 0
+    ptr = t.data_ptr()
+    if t.dtype is not dtype or d != dim or t.get_device() != index:
+        raise DQError("%s must be a %s tensor on cuda:%d with %d channels a head" % (name, dtype, index, dim))
+    if s3 != 1 or (s0 | s1 | s2) & 7 or ptr & 15:
         raise DQError("%s: channels must be neighbours, the other strides multiples of 8 elements, the data 16-byte aligned" % name)
-    return _CHeads(t.data_ptr(), s[0] if t.dim() == 4 else 0, s[-3], s[-2], t.shape[-2]), tuple(t.shape[:-2])
-
-
-def _spread(name: str, t: torch.Tensor) -> None:
-    """Outputs may not lie on themselves (an expanded tensor)."""
-    if any(n > 1 and s == 0 for n, s in zip(t.shape, t.stride())):
+    if written and ((rows > 1 and s1 == 0) or (heads > 1 and s2 == 0) or (batch > 1 and s0 == 0)):
         raise DQError("%s must not be an expanded tensor" % name)
+    return _pack_heads(ptr, s0, s1, s2, heads), (batch, rows) if len(shape) == 4 else rows, heads
 
 
-def _weight(name: str, w: Optional[torch.Tensor], dtype, dim: int):
+def _weight(name: str, w: Optional[torch.Tensor], dtype, dim: int, index: int) -> int:
     if w is None:
-        return None
-    if w.dtype != dtype or w.numel() != dim or not w.is_contiguous() or w.data_ptr() % 16:
-        raise DQError("%s must be %d contiguous %s, 16-byte aligned" % (name, dim, dtype))
-    return w.data_ptr()
+        return 0
+    ptr = w.data_ptr()
+    if w.dtype is not dtype or w.numel() != dim or not w.is_contiguous() or ptr & 15 or w.get_device() != index:
+        raise DQError("%s must be %d contiguous %s on cuda:%d, 16-byte aligned" % (name, dim, dtype, index))
+    return ptr
 
 
-def _norm(q_weight, k_weight, eps: float, dtype, dim: int) -> Optional[_CNorm]:
+def _norm(q_weight, k_weight, eps: float, dtype, dim: int, index: int) -> Optional[bytes]:
     if q_weight is None and k_weight is None:
         return None
     if not eps >= 0.0:
         raise DQError("eps must not be negative")
-    return _CNorm(_weight("q_weight", q_weight, dtype, dim), _weight("k_weight", k_weight, dtype, dim), eps)
+    return _pack_norm(_weight("q_weight", q_weight, dtype, dim, index), _weight("k_weight", k_weight, dtype, dim, index), eps)
 
 
 @dataclass(frozen=True)
@@ -131,17 +136,26 @@ class Rotary:
     def rot_dim(self) -> int:
         return 2 * self.inv_freq.numel()
 
-    def _c(self, positions: Optional[torch.Tensor], rows: int, device) -> _CRotary:
-        _on(device, self.inv_freq, self.axis_of_pair, positions)
-        stride, at = rows, None
+    def _c(self, positions: Optional[torch.Tensor], rows: int, index: int) -> bytes:
+        fixed = self.__dict__.get("_fixed")
+        if fixed is None:                            # a Rotary never changes
+            a = self.axis_of_pair
+            if a is not None and a.device != self.inv_freq.device:
+                raise DQError("inv_freq and axis_of_pair must be on one device")
+            fixed = (self.inv_freq.get_device(), self.inv_freq.data_ptr(), 0 if a is None else a.data_ptr(), self.axes, self.rot_dim,
+                     int(self.interleaved))
+            object.__setattr__(self, "_fixed", fixed)   # (the dataclass is frozen)
+        if fixed[0] != index:
+            raise DQError("the rotation's frequencies must be on cuda:%d" % index)
+        at = 0
         if positions is not None:
-            if positions.dtype != torch.int32 or not positions.is_contiguous() or positions.numel() != self.axes * rows:
-                raise DQError("positions must be contiguous int32, one per row%s" % (" and axis [axes, rows]" if self.axes > 1 else ""))
+            if positions.dtype is not torch.int32 or positions.numel() != self.axes * rows or not positions.is_contiguous() \
+                    or positions.get_device() != index:
+                raise DQError("positions must be contiguous int32 on cuda:%d, one per row%s" % (index, " and axis [axes, rows]" if self.axes > 1 else ""))
             at = positions.data_ptr()
         elif self.axes > 1:
             raise DQError("several axes need positions")
-        return _CRotary(self.inv_freq.data_ptr(), at, None if self.axis_of_pair is None else self.axis_of_pair.data_ptr(), stride,
-                        self.axes, self.rot_dim, int(self.interleaved))
+        return _pack_rotary(fixed[1], at, fixed[2], rows, fixed[3], fixed[4], fixed[5])
 
 
 def rotary(rot_dim: int, base: float = 10000.0, sections: Optional[Sequence[int]] = None, interleaved: bool = False,
@@ -170,43 +184,43 @@ def rotate_heads(q: Optional[torch.Tensor], k: Optional[torch.Tensor], positions
     first = q if q is not None else k
     if first is None:
         raise DQError("rotate_heads needs q or k")
-    dtype, dim, device = first.dtype, first.shape[-1], first.device
-    if dtype not in _DTYPES:
-        raise DQError("heads must be float16 or bfloat16")
-    structs, lead = [], None
-    outs = []
-    for name, x, out in (("q", q, q_out), ("k", k, k_out)):
-        if x is None:
-            if out is not None:
-                raise DQError("%s_out without %s" % (name, name))
-            structs += [None, None]
-            outs.append(None)
-            continue
-        if out is None:
-            out = torch.empty(x.shape, dtype=dtype, device=device)
-        elif out.shape != x.shape:
-            raise DQError("%s_out must have %s's shape" % (name, name))
-        _on(device, x, out)
-        cx, shape = _heads(name, x, dtype, dim)
-        co, _ = _heads(name + "_out", out, dtype, dim)
-        _spread(name + "_out", out)
-        if lead is not None and shape != lead:
+    dtype, dim, index = first.dtype, first.shape[-1], first.get_device()
+    if dtype not in _DTYPES or index < 0:
+        raise DQError("heads must be float16 or bfloat16 on a GPU")
+    cq = cqo = ck = cko = lead = None
+    if q is not None:
+        if q_out is None:
+            q_out = torch.empty(q.shape, dtype=dtype, device=q.device)
+        cq, lead, heads = _heads("q", q, dtype, dim, index)
+        cqo, lead_o, heads_o = _heads("q_out", q_out, dtype, dim, index, True)
+        if lead_o != lead or heads_o != heads:
+            raise DQError("q_out must have q's shape")
+    elif q_out is not None:
+        raise DQError("q_out without q")
+    if k is not None:
+        if k_out is None:
+            k_out = torch.empty(k.shape, dtype=dtype, device=k.device)
+        ck, lead_k, heads = _heads("k", k, dtype, dim, index)
+        cko, lead_o, heads_o = _heads("k_out", k_out, dtype, dim, index, True)
+        if lead_o != lead_k or heads_o != heads:
+            raise DQError("k_out must have k's shape")
+        if lead is not None and lead_k != lead:
             raise DQError("q and k must have the same rows")
-        lead = shape
-        structs += [cx, co]
-        outs.append(out)
-    batch, tokens = lead if len(lead) == 2 else (1, lead[0])
-    _on(device, q_weight, k_weight)
-    norm = _norm(q_weight, k_weight, eps, dtype, dim)
-    if rotary is None and norm is None:
+        lead = lead_k
+    elif k_out is not None:
+        raise DQError("k_out without k")
+    batch, tokens = lead if type(lead) is tuple else (1, lead)
+    norm = _norm(q_weight, k_weight, eps, dtype, dim, index)
+    rot = None
+    if rotary is not None:
+        if positions is None:
+            raise DQError("rotate_heads needs positions")
+        rot = rotary._c(positions, batch * tokens, index)
+    elif norm is None:
         raise DQError("rotate_heads needs a rotation or a norm")
-    if rotary is not None and positions is None:
-        raise DQError("rotate_heads needs positions")
-    rot = None if rotary is None else rotary._c(positions, batch * tokens, device)
     if batch and tokens:
-        _call("dq_rotate_heads", lib.dq_rotate_heads, device, *(None if s is None else C.byref(s) for s in structs), batch, tokens, dim,
-              _DTYPES[dtype], None if norm is None else C.byref(norm), None if rot is None else C.byref(rot))
-    return outs[0], outs[1]
+        _call("dq_rotate_heads", lib.dq_rotate_heads, index, cq, cqo, ck, cko, batch, tokens, dim, _DTYPES[dtype], norm, rot)
+    return q_out, k_out
 
 
 class PagedCache:
@@ -230,7 +244,8 @@ class PagedCache:
             t = self.t[name]
             if not (t.is_cuda and t.is_contiguous()) or tuple(t.shape) != shape or t.dtype != dtype or t.data_ptr() % 16:
                 raise DQError("%s must be a contiguous, 16-byte aligned %s device tensor of shape %s" % (name, dtype, shape))
-        _on(self.device, *self.t.values())
+        self.index = kc.get_device()
+        _on(self.index, *self.t.values())
         self.c = _CPaged(*(self.t[n].data_ptr() for n in names), self.pages, self.kv_heads, self.head_dim, self.page_tokens, self.slots,
                          _DTYPES[self.dtype], _CODES[self.codes])
         self._ref = C.byref(self.c)
@@ -254,37 +269,41 @@ def alloc_paged_cache(pages: int, slots: int, kv_heads: int, head_dim: int, page
                        for n, (shape, t) in _paged_shapes(pages, slots, kv_heads, head_dim, page_tokens, dtype, codes).items()})
 
 
-def _batch(cache: PagedCache, starts, seq_lens, page_table, tail_slots, rows: int, uses_starts: bool = True) -> _CBatch:
+def _batch(cache: PagedCache, starts, seq_lens, page_table, tail_slots, rows: int, uses_starts: bool = True) -> bytes:
     """Sizes are checked here (the library sees pointers only)."""
-    _on(cache.device, starts, seq_lens, page_table, tail_slots)
-    for name, t in (("starts", starts), ("seq_lens", seq_lens), ("tail_slots", tail_slots)):
-        if t is not None and (t.dtype != torch.int32 or t.dim() != 1 or not t.is_contiguous()):
-            raise DQError("%s must be a contiguous int32 vector" % name)
+    index, i32 = cache.index, torch.int32
     n = seq_lens.numel()
-    if n < 1:
-        raise DQError("a batch has at least one sequence")
-    if starts is not None and starts.numel() != n + 1:
-        raise DQError("starts must have one entry more than the batch has sequences")
-    if uses_starts and starts is None and rows != n:
+    if n < 1 or seq_lens.dtype is not i32 or not seq_lens.is_contiguous() or seq_lens.get_device() != index:
+        raise DQError("seq_lens must hold one int32 per sequence, on the cache's GPU")
+    at = slots = 0
+    if starts is not None:
+        if starts.dtype is not i32 or starts.numel() != n + 1 or not starts.is_contiguous() or starts.get_device() != index:
+            raise DQError("starts must hold one int32 more than there are sequences, on the cache's GPU")
+        at = starts.data_ptr()
+    elif uses_starts and rows != n:
         raise DQError("without starts there is one row per sequence")
-    if tail_slots is not None and tail_slots.numel() != n:
-        raise DQError("tail_slots must have one slot per sequence")
-    if tail_slots is None and n > cache.slots:
+    if tail_slots is not None:
+        if tail_slots.dtype is not i32 or tail_slots.numel() != n or not tail_slots.is_contiguous() or tail_slots.get_device() != index:
+            raise DQError("tail_slots must hold one int32 per sequence, on the cache's GPU")
+        slots = tail_slots.data_ptr()
+    elif n > cache.slots:
         raise DQError("more sequences than the cache has slots")
-    if page_table.dtype != torch.int32 or page_table.dim() != 2 or page_table.shape[0] != n or page_table.shape[1] < 1 or page_table.stride(1) != 1 \
-            or (n > 1 and page_table.stride(0) < page_table.shape[1]):
-        raise DQError("page_table must be int32 [batch, pages], a sequence's pages side by side")
-    width = page_table.shape[1]
-    return _CBatch(None if starts is None else starts.data_ptr(), seq_lens.data_ptr(), page_table.data_ptr(),
-                   None if tail_slots is None else tail_slots.data_ptr(), n, rows, width, page_table.stride(0) if n > 1 else width)
+    shape = page_table.shape
+    if len(shape) != 2 or shape[0] != n or shape[1] < 1 or page_table.dtype is not i32 or page_table.get_device() != index:
+        raise DQError("page_table must be int32 [batch, pages], on the cache's GPU")
+    width, (stride, inner) = shape[1], page_table.stride()
+    if n == 1:
+        stride = width
+    if (inner != 1 and width > 1) or stride < width:
+        raise DQError("a sequence's pages must lie side by side in page_table")
+    return _pack_batch(at, seq_lens.data_ptr(), page_table.data_ptr(), slots, n, rows, width, stride)
 
 
-def _rows(cache: PagedCache, name: str, t: torch.Tensor, heads: Optional[int], rows: Optional[int]) -> _CHeads:
-    _on(cache.device, t)
-    c, lead = _heads(name, t, cache.dtype, cache.head_dim)
-    if len(lead) != 1 or (rows is not None and lead[0] != rows) or (heads is not None and t.shape[1] != heads):
+def _rows(cache: PagedCache, name: str, t: torch.Tensor, heads: Optional[int], rows: Optional[int], written: bool = False):
+    c, r, h = _heads(name, t, cache.dtype, cache.head_dim, cache.index, written)
+    if type(r) is tuple or (rows is not None and r != rows) or (heads is not None and h != heads):
         raise DQError("%s must be [rows%s, %sheads, head_dim]" % (name, "" if rows is None else " = %d" % rows, "" if heads is None else "%d " % heads))
-    return c
+    return c, r, h
 
 
 def paged_append(cache: PagedCache, k: torch.Tensor, v: torch.Tensor, starts: Optional[torch.Tensor], seq_lens: torch.Tensor,
@@ -295,28 +314,26 @@ def paged_append(cache: PagedCache, k: torch.Tensor, v: torch.Tensor, starts: Op
     and rotated on the way.  starts: int32 [batch + 1], rows starts[b] .. starts[b+1] - 1 are sequence b's last tokens
     (None: one row each); seq_lens: int32, the new rows included; page_table: int32 [batch, pages].  positions None: a
     token's place in its sequence.  Returns q_out (None without q)."""
-    ck = _rows(cache, "k", k, cache.kv_heads, None)
-    rows = k.shape[0]
-    cv = _rows(cache, "v", v, cache.kv_heads, rows)
+    index = cache.index
+    ck, rows, _ = _rows(cache, "k", k, cache.kv_heads, None)
+    cv, _, _ = _rows(cache, "v", v, cache.kv_heads, rows)
     cb = _batch(cache, starts, seq_lens, page_table, tail_slots, rows)
     cq = co = None
     if q is not None:
-        cq = _rows(cache, "q", q, None, rows)
+        cq, _, heads = _rows(cache, "q", q, None, rows)
         if q_out is None:
             q_out = torch.empty(q.shape, dtype=q.dtype, device=q.device)
-        co = _rows(cache, "q_out", q_out, q.shape[1], rows)
-        _spread("q_out", q_out)
+        co, _, _ = _rows(cache, "q_out", q_out, heads, rows, True)
     elif q_out is not None:
         raise DQError("q_out without q")
-    _on(cache.device, q_weight, k_weight)
-    norm = _norm(q_weight, k_weight, eps, cache.dtype, cache.head_dim)
-    if rotary is not None and rotary.rot_dim > cache.head_dim:
-        raise DQError("rot_dim is larger than head_dim")
-    rot = None if rotary is None else rotary._c(positions, rows, cache.device)
+    norm = _norm(q_weight, k_weight, eps, cache.dtype, cache.head_dim, index)
+    rot = None
+    if rotary is not None:
+        rot = rotary._c(positions, rows, index)
+        if rotary.rot_dim > cache.head_dim:
+            raise DQError("rot_dim is larger than head_dim")
     if rows:
-        _call("dq_paged_append", lib.dq_paged_append, cache.device, cache._ref, C.byref(cb), C.byref(ck), C.byref(cv),
-              None if cq is None else C.byref(cq), None if co is None else C.byref(co), None if norm is None else C.byref(norm),
-              None if rot is None else C.byref(rot))
+        _call("dq_paged_append", lib.dq_paged_append, index, cache._ref, cb, ck, cv, cq, co, norm, rot)
     return q_out
 
 
@@ -324,19 +341,18 @@ def paged_read(cache: PagedCache, first: Optional[torch.Tensor], seq_lens: torch
                k_out: torch.Tensor, v_out: torch.Tensor, tail_slots: Optional[torch.Tensor] = None):
     """The rows that tokens first[b] <= t < seq_lens[b] of the cache stand for, into k_out and v_out [rows, kv_heads, d]
     from row out_starts[b] on (dq_paged_read; first None: from 0).  Returns (k_out, v_out)."""
-    ck = _rows(cache, "k_out", k_out, cache.kv_heads, None)
-    cv = _rows(cache, "v_out", v_out, cache.kv_heads, k_out.shape[0])
-    _spread("k_out", k_out)
-    _spread("v_out", v_out)
-    cb = _batch(cache, out_starts, seq_lens, page_table, tail_slots, k_out.shape[0], uses_starts=False)
-    _on(cache.device, first)
-    if first is not None and (first.dtype != torch.int32 or first.numel() != seq_lens.numel() or not first.is_contiguous()):
-        raise DQError("first must hold one int32 per sequence")
+    ck, rows, _ = _rows(cache, "k_out", k_out, cache.kv_heads, None, True)
+    cv, _, _ = _rows(cache, "v_out", v_out, cache.kv_heads, rows, True)
     if out_starts is None:
         raise DQError("paged_read needs out_starts")
-    if k_out.shape[0]:
-        _call("dq_paged_read", lib.dq_paged_read, cache.device, cache._ref, C.byref(cb), None if first is None else first.data_ptr(),
-              out_starts.data_ptr(), C.byref(ck), C.byref(cv))
+    cb = _batch(cache, out_starts, seq_lens, page_table, tail_slots, rows, False)
+    at = 0
+    if first is not None:
+        if first.dtype is not torch.int32 or first.numel() != seq_lens.numel() or not first.is_contiguous() or first.get_device() != cache.index:
+            raise DQError("first must hold one int32 per sequence, on the cache's GPU")
+        at = first.data_ptr()
+    if rows:
+        _call("dq_paged_read", lib.dq_paged_read, cache.index, cache._ref, cb, at, out_starts.data_ptr(), ck, cv)
     return k_out, v_out
 
 
@@ -353,25 +369,23 @@ def paged_workspace(cache: PagedCache, batch: int, rows: int, q_heads: int, max_
 
 def paged_attention(cache: PagedCache, q: torch.Tensor, starts: Optional[torch.Tensor], seq_lens: torch.Tensor, page_table: torch.Tensor,
                     max_rows: int, max_seq_len: int, workspace: torch.Tensor, out: Optional[torch.Tensor] = None, softmax_scale: float = 0.0,
-                    causal: bool = True, window: int = 0, tail_slots: Optional[torch.Tensor] = None) -> torch.Tensor:
+                    causal: bool = True, window: int = 0, tail_slots: Optional[torch.Tensor] = None, splits: int = 0) -> torch.Tensor:
     """softmax(q . K * scale) V of the batch's rows q [rows, q_heads, d] over the cached tokens of their sequences
     (dq_paged_attention); rows are the last tokens of their sequence (append them first).  max_rows, max_seq_len: host
-    bounds on the rows and tokens of any sequence.  window > 0: the last `window` tokens only.  out may be q."""
-    cq = _rows(cache, "q", q, None, None)
-    rows, heads = q.shape[0], q.shape[1]
+    bounds on the rows and tokens of any sequence.  window > 0: the last `window` tokens only.  out may be q.
+    splits: launch override for sweeps (DQ_PAGED_SPLITS)."""
+    cq, rows, heads = _rows(cache, "q", q, None, None)
     if heads == 0 or heads % cache.kv_heads:
         raise DQError("q_heads must be a multiple of kv_heads")
     if out is None:
         out = torch.empty(q.shape, dtype=q.dtype, device=q.device)
-    co = _rows(cache, "out", out, heads, rows)
-    _spread("out", out)
+    co, _, _ = _rows(cache, "out", out, heads, rows, True)
     cb = _batch(cache, starts, seq_lens, page_table, tail_slots, rows)
-    _on(cache.device, workspace)
-    if workspace.dtype != torch.uint8 or not workspace.is_contiguous():
-        raise DQError("workspace must be contiguous uint8")
+    if workspace.dtype is not torch.uint8 or not workspace.is_contiguous() or workspace.get_device() != cache.index:
+        raise DQError("workspace must be contiguous uint8 on the cache's GPU")
     if max_rows < 0 or max_seq_len < 0 or window < 0 or (window and not causal):
         raise DQError("max_rows, max_seq_len and window must not be negative, and a window needs causal")
     if rows:
-        _call("dq_paged_attention", lib.dq_paged_attention, cache.device, cache._ref, C.byref(cb), C.byref(cq), C.byref(co), max_rows,
-              max_seq_len, softmax_scale, window, workspace.data_ptr(), workspace.numel(), PAGED_CAUSAL if causal else 0)
+        _call("dq_paged_attention", lib.dq_paged_attention, cache.index, cache._ref, cb, cq, co, max_rows, max_seq_len, softmax_scale, window,
+              workspace.data_ptr(), workspace.numel(), (PAGED_CAUSAL if causal else 0) | ((splits & 0x7F) << 8))
     return out
