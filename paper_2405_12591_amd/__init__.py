@@ -45,4 +45,5 @@ from .paged import (  # noqa: F401
     paged_read,
     paged_workspace,
     paged_attention,
+    PagedKVLayer,
 )

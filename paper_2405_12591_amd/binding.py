@@ -529,6 +529,19 @@ class KVCacheLayer:
             cache_append(self.cache, self.k_tail, self.v_tail, self.tail_lens, self.seq_lens, kr, vr, c, self.ws_append)
         self.rows_upper += n
 
+    def append_projected(self, q: torch.Tensor, k: torch.Tensor, v: torch.Tensor, positions: torch.Tensor, rotary,
+                         q_weight: Optional[torch.Tensor] = None, k_weight: Optional[torch.Tensor] = None, eps: float = 1e-6,
+                         counts=None, prompt: bool = False) -> torch.Tensor:
+        """The same from the projections' outputs q [B, n, q_heads, d], k and v [B, n, H_kv, d] (views of a fused one too):
+        keys and queries are normed (where a weight is given) and rotated (rotate_heads; positions int32 [B, n]) on the
+        way.  prompt: the rows are a prompt for empty sequences (prefill).  Returns the rotated queries [B, n, q_heads, d]."""
+        from .paged import rotate_heads
+        bsz, n = k.shape[:2]
+        rows = torch.empty((bsz, self.kv_heads, n, self.fmt.head_dim), dtype=k.dtype, device=k.device)
+        q, _ = rotate_heads(q, k, positions, rotary, q_weight=q_weight, k_weight=k_weight, eps=eps, k_out=rows.transpose(1, 2))
+        (self.prefill if prompt else self.append)(rows, v.transpose(1, 2).contiguous(), counts)
+        return q
+
     def prefill(self, k_new: torch.Tensor, v_new: torch.Tensor, counts=None) -> None:
         """Append the rows of a prompt, k_new, v_new [B, H_kv, n, d], to EMPTY sequences; sequence b
         takes the first counts[b] rows (default: all n).  The whole blocks of all sequences are

@@ -389,3 +389,64 @@ def paged_attention(cache: PagedCache, q: torch.Tensor, starts: Optional[torch.T
         _call("dq_paged_attention", lib.dq_paged_attention, cache.index, cache._ref, cb, cq, co, max_rows, max_seq_len, softmax_scale, window,
               workspace.data_ptr(), workspace.numel(), (PAGED_CAUSAL if causal else 0) | ((splits & 0x7F) << 8))
     return out
+
+
+class PagedKVLayer:
+    """One layer's keys and values in 8-bit pages, as KVCacheLayer is for the DecoQuant form: `batch` sequences of up to
+    max_tokens tokens, each with its own pages and tail, the lengths on the device.  Rows come packed, sequence by
+    sequence (`starts`, int32 [batch + 1]; None: one row each); the host tracks only bounds, which size the launches.
+    (Loops with a page allocator of their own call paged_append and paged_attention.)"""
+
+    def __init__(self, batch: int, q_heads: int, kv_heads: int, head_dim: int, max_tokens: int, page_tokens: int = 64,
+                 dtype=torch.float16, codes=torch.int8, device="cuda:0"):
+        if batch < 1 or max_tokens < 1 or q_heads < 1 or q_heads % kv_heads:
+            raise DQError("a layer has sequences, room for tokens and q_heads a multiple of kv_heads")
+        self.batch, self.q_heads, self.max_tokens = batch, q_heads, max_tokens
+        width = -(-max_tokens // page_tokens)
+        self.cache = alloc_paged_cache(batch * width, batch, kv_heads, head_dim, page_tokens, dtype, codes, device)
+        self.page_table = torch.arange(batch * width, dtype=torch.int32, device=device).view(batch, width)
+        self.seq_lens = torch.zeros(batch, dtype=torch.int32, device=device)
+        self.tokens_upper = 0               # no sequence holds more tokens than this (host-side bound)
+        self._ws = None
+
+    def append(self, k: torch.Tensor, v: torch.Tensor, starts: Optional[torch.Tensor] = None, max_rows: int = 1,
+               q: Optional[torch.Tensor] = None, rotary: Optional[Rotary] = None, positions: Optional[torch.Tensor] = None,
+               q_weight: Optional[torch.Tensor] = None, k_weight: Optional[torch.Tensor] = None, eps: float = 1e-6):
+        """Append rows k, v [rows, kv_heads, d], no sequence more than max_rows; norm and rotation as paged_append does
+        them; returns q normed and rotated (None without q)."""
+        if starts is None and max_rows != 1:
+            raise DQError("several rows per sequence need starts")
+        if self.tokens_upper + max_rows > self.max_tokens:
+            # the bound may be ahead of the lengths (ragged rows); only then is it worth a look at them
+            self.tokens_upper = int(self.seq_lens.max())
+            if self.tokens_upper + max_rows > self.max_tokens:
+                raise DQError("the rows exceed the layer's %d tokens per sequence" % self.max_tokens)
+        self.seq_lens += 1 if starts is None else starts.diff()
+        self.tokens_upper += max_rows
+        return paged_append(self.cache, k, v, starts, self.seq_lens, self.page_table, q=q, rotary=rotary, positions=positions,
+                            q_weight=q_weight, k_weight=k_weight, eps=eps)
+
+    def attend(self, q: torch.Tensor, starts: Optional[torch.Tensor] = None, max_rows: int = 1, out: Optional[torch.Tensor] = None,
+               softmax_scale: float = 0.0, causal: bool = True, window: int = 0) -> torch.Tensor:
+        """Attention of the rows just appended, q [rows, q_heads, d] (paged_attention)."""
+        rows, bound = q.shape[0], min(self.tokens_upper, self.max_tokens)
+        if self._ws is None or rows > self._ws[0] or max_rows > self._ws[1]:
+            sizes = (max(rows, self._ws[0]), max(max_rows, self._ws[1])) if self._ws else (rows, max_rows)
+            self._ws = (*sizes, paged_workspace(self.cache, self.batch, sizes[0], self.q_heads, sizes[1], self.max_tokens))
+        return paged_attention(self.cache, q, starts, self.seq_lens, self.page_table, max_rows, bound, self._ws[2], out=out,
+                               softmax_scale=softmax_scale, causal=causal, window=window)
+
+    def read(self, lengths: Sequence[int]):
+        """The rows the layer stands for, k and v [batch, kv_heads, max(lengths), d]; sequence b's first lengths[b] (host
+        integers, its tokens) are written, the rest is zero.  Goes into KVCacheLayer.prefill (fp16 layers)."""
+        c = self.cache
+        n = max(lengths)
+        k = torch.zeros((self.batch, c.kv_heads, n, c.head_dim), dtype=c.dtype, device=c.device)
+        v = torch.zeros_like(k)
+        lens = torch.tensor(list(lengths), dtype=torch.int32, device=c.device)
+        for b in range(self.batch):
+            if lengths[b] > 0:
+                one = torch.tensor([0, lengths[b]], dtype=torch.int32, device=c.device)
+                paged_read(c, None, lens[b:b + 1], one, self.page_table[b:b + 1], k[b].transpose(0, 1), v[b].transpose(0, 1),
+                           tail_slots=torch.tensor([b], dtype=torch.int32, device=c.device))
+        return k, v

@@ -433,3 +433,115 @@ def test_from_pages_to_the_decoquant_cache():
     assert torch.equal(k[0].transpose(0, 1).cpu(), read_back(cache, [n, n], table, slots)[0][:n])
     # 8-bit codes of the factored block: keys and values off by under 2 % of their norm, and attention to what the scores make of that
     assert float((a - p).norm() / p.norm()) < 0.2
+
+
+def test_a_workspace_of_the_largest_sizes_serves_all_smaller_ones_in_turn():
+    """Prompts, pieces, drafted and single tokens, long and short, one workspace after the other call's leavings."""
+    gen = torch.Generator().manual_seed(18)
+    lens = [9000, 300, 64, 4000]
+    seqs = Sequences(lens, 2, 64, F16, E4M3, 64, gen)
+    cache, table, slots = filled_cache(seqs, lens, gen)
+    ws = dq.paged_workspace(cache, 4, 1200, 4, 300, 9000)
+    want = {}
+    for turn in range(2):
+        for new, cut in (([300, 300, 60, 300], 9000), ([1, 1, 1, 1], 9000), ([40, 1, 2, 90], 9000), ([4, 4, 4, 4], 9000), ([1, 1, 1, 1], 320), ([64, 64, 64, 64], 256)):
+            now = [min(n, cut // 64 * 64) if n > cut else n for n in lens]
+            q = rows((sum(new), 4, 64), F16, torch.Generator().manual_seed(len(want) if turn == 0 else list(want).index((tuple(new), cut))), outliers=False)
+            out = dq.paged_attention(cache, q.to(DEV), ints(_sums(new)), ints(now), table, max(new), cut, ws, tail_slots=slots).cpu()
+            key = (tuple(new), cut)
+            if turn == 0:
+                own = dq.paged_workspace(cache, 4, sum(new), 4, max(new), cut)
+                want[key] = dq.paged_attention(cache, q.to(DEV), ints(_sums(new)), ints(now), table, max(new), cut, own, tail_slots=slots).cpu()
+            assert torch.equal(out, want[key]), key
+
+
+@pytest.mark.parametrize("dtype,codes", FORMATS[:2])
+def test_splits_of_every_kernel_agree(dtype, codes):
+    """The launch override changes how the work is dealt, not what is computed."""
+    gen = torch.Generator().manual_seed(19)
+    lens = [3000, 700, 65]
+    seqs = Sequences(lens, 2, 128, dtype, codes, 128, gen)
+    cache, table, slots = filled_cache(seqs, lens, gen)
+    for new in ([1, 1, 1], [100, 33, 64]):
+        q = rows((sum(new), 8, 128), dtype, gen, outliers=False).to(DEV)
+        ws = torch.zeros(1 << 28, dtype=torch.uint8, device=DEV)
+        outs = [dq.paged_attention(cache, q, ints(_sums(new)), ints(lens), table, max(new), 3000, ws, tail_slots=slots, splits=n).cpu().double()
+                for n in (1, 2, 5, 32, 64)]
+        at = 0
+        for b, n in enumerate(new):
+            k, v = seqs.stored(seqs.k[b]), seqs.stored(seqs.v[b])
+            want, size, ds = attend64(q[at:at + n].cpu(), k, v, torch.arange(lens[b] - n, lens[b]), True, 0, 128 ** -0.5)
+            tol = attend_tolerance(want, size, ds, float(v.abs().max()), lens[b], dtype, True)
+            for o in outs:
+                assert ((o[at:at + n] - want).abs() <= tol).all()
+            at += n
+
+
+def test_a_layer_from_projections_to_outputs():
+    """PagedKVLayer: prompts of mixed lengths, a step, drafted tokens, all from raw projections with norm and rotation,
+    against the 64-bit forms of every stage; then its rows move to a DecoQuant layer."""
+    from paged_util import heads64
+    gen = torch.Generator().manual_seed(20)
+    heads, hq, d, dtype = 2, 6, 128, F16
+    layer = dq.PagedKVLayer(3, hq, heads, d, 300, 64, dtype, INT8, DEV)
+    rot = dq.rotary(d, device=DEV)
+    wq, wk = (1 + 0.2 * torch.randn(2, d, generator=gen)).to(dtype)
+    seen = Sequences([0, 0, 0], heads, d, dtype, INT8, 64, gen)
+    for new in ([130, 63, 1], [1, 1, 1], [3, 0, 2], [64, 64, 64]):
+        total = sum(new)
+        fused = rows((total, hq + 2 * heads, d), dtype, gen).to(DEV)
+        starts = None if new == [1, 1, 1] else ints(_sums(new))
+        q = layer.append(fused[:, hq:hq + heads], fused[:, hq + heads:], starts, max(new), q=fused[:, :hq], rotary=rot, q_weight=wq.to(DEV), k_weight=wk.to(DEV))
+        out = layer.attend(q, starts, max(new))
+        host, at = fused.cpu(), 0
+        place = torch.cat([torch.arange(len(k), len(k) + n) for k, n in zip(seen.k, new)])
+        q64, _ = heads64(host[:, :hq], wq, 1e-6, rot.inv_freq.cpu(), None, place, d, False)
+        assert ((q.cpu().double() - q64).abs() <= q64.abs() * 2.0 ** -11 + 2.0 ** -17 * q64.abs().amax(-1, keepdim=True) + 2.0 ** -24).all()
+        # (the rows the cache took are the operator's own: their rounding is checked above and in the tests of the norm)
+        kk, _ = dq.rotate_heads(fused[:, hq:hq + heads], None, place.to(torch.int32).to(DEV), rot, q_weight=wk.to(DEV))
+        for b, n in enumerate(new):
+            seen.k[b] = torch.cat([seen.k[b], kk[at:at + n].cpu()])
+            seen.v[b] = torch.cat([seen.v[b], host[at:at + n, hq + heads:]])
+            if n:
+                k, v, ln = seen.stored(seen.k[b]), seen.stored(seen.v[b]), len(seen.k[b])
+                want, size, ds = attend64(q[at:at + n].cpu(), k, v, torch.arange(ln - n, ln), True, 0, d ** -0.5)
+                tol = attend_tolerance(want, size, ds, float(v.abs().max()), ln, dtype, True)
+                assert ((out[at:at + n].cpu().double() - want).abs() <= tol).all(), (b, new)
+            at += n
+    lens = [len(k) for k in seen.k]
+    assert layer.seq_lens.tolist() == lens
+    k, v = layer.read(lens)
+    for b, n in enumerate(lens):
+        for got, x in ((k, seen.k), (v, seen.v)):
+            want = seen.stored(x[b])
+            assert ((got[b, :, :n].transpose(0, 1).cpu().double() - want).abs() <= want.abs() * 2.0 ** -11 * (1 + 2.0 ** -12) + 2.0 ** -25).all()
+            assert (got[b, :, n:] == 0).all()
+    small = dq.KVCacheLayer(dq.Format(8, 128, d, 16, 8, 128), 3, hq, heads, 512, DEV)
+    small.prefill(k, v, counts=lens)
+    assert torch.isfinite(small.decode(torch.ones((3, hq, d), dtype=dtype, device=DEV))).all()
+    with pytest.raises(dq.DQError, match="exceed"):
+        layer.append(fused[:3, hq:hq + heads], fused[:3, hq + heads:], ints([0, 3, 3, 3]), 200)
+
+
+def test_the_decoquant_layer_takes_projections():
+    """KVCacheLayer.append_projected is rotate_heads and append (prefill) of its rows, bit for bit."""
+    gen = torch.Generator().manual_seed(21)
+    bsz, heads, hq, d = 2, 2, 4, 128
+    fmt = dq.Format(4, 128, d, 16, 8, 128)
+    a, b = (dq.KVCacheLayer(fmt, bsz, hq, heads, 512, DEV) for _ in range(2))
+    rot = dq.rotary(d, device=DEV)
+    w = (1 + 0.2 * torch.randn(2, d, generator=gen)).to(F16).to(DEV)
+    have = 0
+    for n in (150, 1, 130):
+        fused = rows((bsz, n, hq + 2 * heads, d), F16, gen).to(DEV)
+        q, k, v = fused[:, :, :hq], fused[:, :, hq:hq + heads], fused[:, :, hq + heads:]
+        pos = torch.arange(have, have + n, dtype=torch.int32, device=DEV).expand(bsz, n).contiguous()
+        have += n
+        qa = a.append_projected(q, k, v, pos, rot, q_weight=w[0], k_weight=w[1], prompt=n == 150)
+        qb, kb = dq.rotate_heads(q, k, pos, rot, q_weight=w[0], k_weight=w[1])
+        (b.prefill if n == 150 else b.append)(kb.transpose(1, 2).contiguous(), v.transpose(1, 2).contiguous())
+        assert torch.equal(qa, qb)
+        oa, ob = a.decode(qa[:, -1].contiguous()), b.decode(qb[:, -1].contiguous())
+        assert torch.equal(oa, ob)
+    for n in a.cache.t:
+        assert torch.equal(a.cache.t[n], b.cache.t[n]), n
