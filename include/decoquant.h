@@ -481,8 +481,8 @@ typedef struct dq_paged_batch {
  * Append the batch's rows: k and v heads [rows, kv_heads, d] (token_stride, head_stride as they lie in a
  * fused projection).  Keys are normed and rotated (norm, rot: NULL for rows that are ready), rounded to
  * 16 bits and buffered or, with the whole of their page, quantized; values go as they are.  q (NULL:
- * none), [rows, q_heads, d], takes the same norm and rotation in the same launch, into q_out.  One
- * launch; page_table must name the pages that fill in this call.
+ * none), [rows, q_heads, d], takes the same norm and rotation in the same launch, into q_out (q itself
+ * will do).  One launch; page_table must name the pages that fill in this call.
  */
 int32_t dq_paged_append(const dq_paged_cache* cache, const dq_paged_batch* batch, const dq_heads* k,
                         const dq_heads* v, const dq_heads* q, const dq_heads* q_out,
@@ -514,8 +514,9 @@ size_t dq_paged_workspace_bytes(const dq_paged_cache* cache, int32_t batch, int3
  * and values are what the cache stands for; fp32 accumulation, one rounding of the result, probabilities
  * in 16 bits for their product with the values.
  *   q, out         [rows, q_heads, d]; out may be q
- *   max_rows       host bound on the rows of any sequence; max_seq_len on seq_lens (longer sequences
- *                  are cut there); both choose kernel and launch
+ *   max_rows       host bound on the rows of any sequence; it chooses the kernel, and further rows of a
+ *                  sequence may be left out
+ *   max_seq_len    host bound on seq_lens (a guess does: it sizes the launch, results do not depend on it)
  *   window         > 0: a row sees the last `window` tokens up to its own place only (needs causal)
  *   softmax_scale  <= 0 selects 1/sqrt(d)
  * A row that sees no token yields zeros.  Rows behind the last sequence's are not written.

@@ -18,6 +18,7 @@ typedef __bf16 bf16x8 __attribute__((ext_vector_type(8)));
 constexpr int kPagedTile = 64;        // tokens of a work tile and of a run of the value layout
 constexpr int kPagedThreads = 256;
 constexpr int kMaxAxes = 8;
+constexpr long kMaxThreads = 1l << 32;   // a launch has fewer (along x)
 constexpr float kSmallestAmax = 0x1p-100f;   // a block below it is held as zeros (its inverse step would leave fp32)
 
 // ---- argument checks (host) ----

@@ -436,7 +436,7 @@ extern "C" int32_t dq_paged_append(const dq_paged_cache* cache, const dq_paged_b
   a.q_heads_per_group = q_per;
   a.q_head_groups = q ? (q->heads + q_per - 1) / q_per : 1;
   const long page_blocks = items * a.head_groups, blocks = page_blocks + q_items * a.q_head_groups;
-  if (blocks >= (1l << 31)) return DQ_EINVAL;
+  if (blocks * (cache->page_tokens * cache->head_dim / 16) >= kMaxThreads) return DQ_EINVAL;
   a.page_blocks = (int)page_blocks;
   for_format<LaunchAppend>(cache, a, dim3((unsigned)blocks), (hipStream_t)hip_stream);
   DQ_HIP_CHECK(hipGetLastError());
@@ -451,7 +451,7 @@ extern "C" int32_t dq_paged_read(const dq_paged_cache* cache, const dq_paged_bat
   if (batch->rows == 0) return DQ_OK;
   ReadArgs a = {*cache, *batch, first, out_starts, *k_out, *v_out};
   const long items = batch->rows / cache->page_tokens + 2l * batch->batch;
-  if (items >= (1l << 31)) return DQ_EINVAL;
+  if (items * kPagedThreads >= kMaxThreads) return DQ_EINVAL;
   for_format<LaunchRead>(cache, a, dim3((unsigned)items, (unsigned)cache->kv_heads), (hipStream_t)hip_stream);
   DQ_HIP_CHECK(hipGetLastError());
   return DQ_OK;

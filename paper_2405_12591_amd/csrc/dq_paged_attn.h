@@ -10,7 +10,6 @@ struct PagedAttnArgs {
   dq_heads q, out;
   int group;               // query heads per kv head
   int max_rows;            // rows of any sequence at most
-  int max_seq_len;
   int window;              // 0: none
   int causal;
   float scale_log2;        // softmax scale * log2(e)

@@ -26,18 +26,17 @@ __global__ __launch_bounds__(kPagedThreads) void paged_decode_kernel(PagedAttnAr
   const int tid = threadIdx.x, lane = tid & 63, wave = tid >> 6, col = lane & 15, G = lane >> 4;
   const int unit = (int)blockIdx.x / a.splits, split = (int)blockIdx.x % a.splits;
   const int H = a.c.kv_heads, b = unit / H, h = unit % H, P = a.c.page_tokens;
-  Sequence s = sequence_of(a.bt, P, b);
-  s.len = min(s.len, a.max_seq_len);
-  const int n = min(s.n, a.max_rows), len = s.len;
+  const Sequence s = sequence_of(a.bt, P, b);
+  const int n = min(s.n, a.max_rows), len = s.len, before = len - s.n;   // tokens before the sequence's first row
   if (n == 0) return;
   const int cols = n * a.group;
   const int qi = min(col / a.group, n - 1), hq = h * a.group + col % a.group;
   const bool live = col < cols;
   // tokens [see_lo, see_hi) of this column, and what every column sees
-  const int place = len - n + qi;
+  const int place = before + qi;
   const int see_hi = a.causal ? min(place + 1, len) : len, see_lo = a.window ? max(place + 1 - a.window, 0) : 0;
-  const int all_hi = a.causal ? min(len - n + 1, len) : len, all_lo = a.window ? max(len - a.window, 0) : 0;
-  const int first_tile = a.window ? max(len - n + 1 - a.window, 0) / kPagedTile : 0;
+  const int all_hi = a.causal ? min(before + 1, len) : len, all_lo = a.window ? max(before + n - a.window, 0) : 0;
+  const int first_tile = a.window ? max(before + 1 - a.window, 0) / kPagedTile : 0;
   const int runs = P / kPagedTile, code_tiles = len / P * runs, tiles = (len + kPagedTile - 1) / kPagedTile;
 
   // ---- queries: 8 channels 64 c + 16 G + 8 half of the column, in f16 ----

@@ -27,8 +27,7 @@ __global__ __launch_bounds__(64 * kPromptWaves, RB == 1 ? 2 : 1) void paged_prom
   const int H = a.c.kv_heads, P = a.c.page_tokens;
   const int h = (int)(blockIdx.x % H), split = (int)(blockIdx.x / H) % a.splits, item = (int)(blockIdx.x / H) / a.splits;
   const int b = item_owner(a.bt.starts, a.bt.rows, a.bt.batch, item, a.group, M, 1);
-  Sequence s = sequence_of(a.bt, P, b);
-  s.len = min(s.len, a.max_seq_len);
+  const Sequence s = sequence_of(a.bt, P, b);
   const int n = s.n, len = s.len;
   const int row_tiles = (int)(((long)n * a.group + M - 1) / M);
   const int j = item - item_first(a.bt.starts, a.bt.rows, b, a.group, M, 1);
@@ -478,7 +477,6 @@ extern "C" int32_t dq_paged_attention(const dq_paged_cache* cache, const dq_page
   a.c = *cache; a.bt = *batch; a.q = *q; a.out = *out;
   a.group = q->heads / cache->kv_heads;
   a.max_rows = max_rows;
-  a.max_seq_len = max_seq_len;
   a.window = window;
   a.causal = (flags & DQ_PAGED_CAUSAL) ? 1 : 0;
   a.scale_log2 = (softmax_scale > 0.f ? softmax_scale : 1.0f / sqrtf((float)cache->head_dim)) * 1.44269504088896340736f;

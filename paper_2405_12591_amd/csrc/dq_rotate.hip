@@ -85,7 +85,7 @@ extern "C" int32_t dq_rotate_heads(const dq_heads* q, const dq_heads* q_out, con
   while (16 * lanes < head_dim) lanes *= 2;
   const long groups = (rows + kPagedThreads / lanes - 1) / (kPagedThreads / lanes);
   const int heads = a.q.heads + a.k.heads;
-  if (heads > kMaxGridY) return DQ_EINVAL;
+  if (heads > kMaxGridY || groups * kPagedThreads >= kMaxThreads) return DQ_EINVAL;
   // Heads a workgroup takes: eight share the angles where the rows alone fill the chip, fewer where they do not.
   int per = 8;
   while (per > 1 && groups * ((heads + per - 1) / per) < 1024) per /= 2;

@@ -12,6 +12,7 @@ import torch
 from .binding import DQError, _check, _raw_stream, lib, workspace_init
 
 PAGED_CAUSAL = 1
+_I32 = torch.int32
 _DTYPES = {torch.float16: 0, torch.bfloat16: 1}
 _CODES = {torch.int8: 0, torch.float8_e4m3fn: 1}
 
@@ -269,37 +270,46 @@ def alloc_paged_cache(pages: int, slots: int, kv_heads: int, head_dim: int, page
                        for n, (shape, t) in _paged_shapes(pages, slots, kv_heads, head_dim, page_tokens, dtype, codes).items()})
 
 
+def _vector(name: str, t: torch.Tensor, n: int, index: int) -> int:
+    """Address of n int32 side by side on device `index`."""
+    if t.dtype is not _I32 or t.numel() != n or not t.is_contiguous() or t.get_device() != index:
+        raise DQError("%s must hold %d int32, side by side on cuda:%d" % (name, n, index))
+    return t.data_ptr()
+
+
 def _batch(cache: PagedCache, starts, seq_lens, page_table, tail_slots, rows: int, uses_starts: bool = True) -> bytes:
     """Sizes are checked here (the library sees pointers only)."""
-    index, i32 = cache.index, torch.int32
+    index = cache.index
     n = seq_lens.numel()
-    if n < 1 or seq_lens.dtype is not i32 or not seq_lens.is_contiguous() or seq_lens.get_device() != index:
-        raise DQError("seq_lens must hold one int32 per sequence, on the cache's GPU")
-    at = slots = 0
-    if starts is not None:
-        if starts.dtype is not i32 or starts.numel() != n + 1 or not starts.is_contiguous() or starts.get_device() != index:
-            raise DQError("starts must hold one int32 more than there are sequences, on the cache's GPU")
-        at = starts.data_ptr()
-    elif uses_starts and rows != n:
-        raise DQError("without starts there is one row per sequence")
-    if tail_slots is not None:
-        if tail_slots.dtype is not i32 or tail_slots.numel() != n or not tail_slots.is_contiguous() or tail_slots.get_device() != index:
-            raise DQError("tail_slots must hold one int32 per sequence, on the cache's GPU")
-        slots = tail_slots.data_ptr()
-    elif n > cache.slots:
-        raise DQError("more sequences than the cache has slots")
+    if n < 1:
+        raise DQError("a batch has at least one sequence")
     shape = page_table.shape
-    if len(shape) != 2 or shape[0] != n or shape[1] < 1 or page_table.dtype is not i32 or page_table.get_device() != index:
+    if len(shape) != 2 or shape[0] != n or shape[1] < 1 or page_table.dtype is not _I32 or page_table.get_device() != index:
         raise DQError("page_table must be int32 [batch, pages], on the cache's GPU")
-    width, (stride, inner) = shape[1], page_table.stride()
+    width = shape[1]
+    stride, inner = page_table.stride()
     if n == 1:
         stride = width
     if (inner != 1 and width > 1) or stride < width:
         raise DQError("a sequence's pages must lie side by side in page_table")
-    return _pack_batch(at, seq_lens.data_ptr(), page_table.data_ptr(), slots, n, rows, width, stride)
+    if starts is None and uses_starts and rows != n:
+        raise DQError("without starts there is one row per sequence")
+    if tail_slots is None and n > cache.slots:
+        raise DQError("more sequences than the cache has slots")
+    return _pack_batch(0 if starts is None else _vector("starts", starts, n + 1, index), _vector("seq_lens", seq_lens, n, index),
+                       page_table.data_ptr(), 0 if tail_slots is None else _vector("tail_slots", tail_slots, n, index), n, rows, width, stride)
 
 
 def _rows(cache: PagedCache, name: str, t: torch.Tensor, heads: Optional[int], rows: Optional[int], written: bool = False):
+    """(packed dq_heads, rows, heads) of rows [rows, heads, head_dim] of the cache's type."""
+    shape = t.shape
+    if len(shape) == 3:                                  # the usual case with as few looks at the tensor as can be
+        n, h, d = shape
+        s0, s1, s2 = t.stride()
+        ptr = t.data_ptr()
+        if d == cache.head_dim and s2 == 1 and s0 and s1 and not (s0 | s1) & 7 and not ptr & 15 and t.dtype is cache.dtype \
+                and t.get_device() == cache.index and (rows is None or n == rows) and (heads is None or h == heads):
+            return _pack_heads(ptr, 0, s0, s1, h), n, h
     c, r, h = _heads(name, t, cache.dtype, cache.head_dim, cache.index, written)
     if type(r) is tuple or (rows is not None and r != rows) or (heads is not None and h != heads):
         raise DQError("%s must be [rows%s, %sheads, head_dim]" % (name, "" if rows is None else " = %d" % rows, "" if heads is None else "%d " % heads))
@@ -348,9 +358,7 @@ def paged_read(cache: PagedCache, first: Optional[torch.Tensor], seq_lens: torch
     cb = _batch(cache, out_starts, seq_lens, page_table, tail_slots, rows, False)
     at = 0
     if first is not None:
-        if first.dtype is not torch.int32 or first.numel() != seq_lens.numel() or not first.is_contiguous() or first.get_device() != cache.index:
-            raise DQError("first must hold one int32 per sequence, on the cache's GPU")
-        at = first.data_ptr()
+        at = _vector("first", first, seq_lens.numel(), cache.index)
     if rows:
         _call("dq_paged_read", lib.dq_paged_read, cache.index, cache._ref, cb, at, out_starts.data_ptr(), ck, cv)
     return k_out, v_out
@@ -371,8 +379,8 @@ def paged_attention(cache: PagedCache, q: torch.Tensor, starts: Optional[torch.T
                     max_rows: int, max_seq_len: int, workspace: torch.Tensor, out: Optional[torch.Tensor] = None, softmax_scale: float = 0.0,
                     causal: bool = True, window: int = 0, tail_slots: Optional[torch.Tensor] = None, splits: int = 0) -> torch.Tensor:
     """softmax(q . K * scale) V of the batch's rows q [rows, q_heads, d] over the cached tokens of their sequences
-    (dq_paged_attention); rows are the last tokens of their sequence (append them first).  max_rows, max_seq_len: host
-    bounds on the rows and tokens of any sequence.  window > 0: the last `window` tokens only.  out may be q.
+    (dq_paged_attention); rows are the last tokens of their sequence (append them first).  max_rows: host bound on the
+    rows of any sequence; max_seq_len: on its tokens (a guess does).  window > 0: the last `window` tokens only.  out may be q.
     splits: launch override for sweeps (DQ_PAGED_SPLITS)."""
     cq, rows, heads = _rows(cache, "q", q, None, None)
     if heads == 0 or heads % cache.kv_heads:
