@@ -75,6 +75,16 @@ __device__ __forceinline__ Sequence sequence_of(const dq_paged_batch& bt, int pa
   return s;
 }
 
+// The same where the whole wave asks for one sequence: in scalar registers, so that loops over its tokens are scalar too (as
+// vector values they made every conditional load a divergent branch, and the wait behind it one for all loads).
+__device__ __forceinline__ Sequence sequence_of_wave(const dq_paged_batch& bt, int page_tokens, int b) {
+  Sequence s = sequence_of(bt, page_tokens, b);
+  s.row0 = __builtin_amdgcn_readfirstlane(s.row0);
+  s.n = __builtin_amdgcn_readfirstlane(s.n);
+  s.len = __builtin_amdgcn_readfirstlane(s.len);
+  return s;
+}
+
 // Work items dealt to sequences without a scan: sequence b's items start at first(b) = starts[b] / unit + per_seq * b, which
 // leaves it at least rows / unit + per_seq - 1 of them.  The sequence an item belongs to, by bisection.
 __device__ __forceinline__ int item_first(const int32_t* starts, int rows, int b, int mul, int unit, int per_seq) {

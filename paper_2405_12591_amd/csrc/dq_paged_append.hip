@@ -100,13 +100,13 @@ __global__ __launch_bounds__(P * D / 16, 4) void paged_append_kernel(AppendArgs 
   const int item = (int)blockIdx.x / a.head_groups, h_first = ((int)blockIdx.x % a.head_groups) * a.heads_per_group;
   const int h_last = min(h_first + a.heads_per_group, a.c.kv_heads);
   const int b = item_owner(a.bt.starts, a.bt.rows, a.bt.batch, item, 1, P, 2);
-  const Sequence s = sequence_of(a.bt, P, b);
+  const Sequence s = sequence_of_wave(a.bt, P, b);
   if (s.n == 0 || s.len == 0) return;
   const int old = s.len - s.n;                            // may be negative: those rows are left out
   const int first_page = max(old, 0) / P, last_page = (s.len - 1) / P;
   int page = first_page + item - item_first(a.bt.starts, a.bt.rows, b, 1, P, 2);
   if (page < first_page || page > last_page) return;
-  const int slot = a.bt.tail_slots ? a.bt.tail_slots[b] : b;
+  const int slot = a.bt.tail_slots ? __builtin_amdgcn_readfirstlane(a.bt.tail_slots[b]) : b;
   const bool slot_ok = slot >= 0 && slot < a.c.slots;
   // Where a page fills whose first rows lie in the tail and rows remain behind it, those go into the same tail: the
   // workgroup that reads the old rows also writes the new ones, afterwards.

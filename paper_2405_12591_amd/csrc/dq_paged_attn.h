@@ -13,11 +13,20 @@ struct PagedAttnArgs {
   int window;              // 0: none
   int causal;
   float scale_log2;        // softmax scale * log2(e)
-  int splits;
-  float* partials;         // [unit, split, column, D + 2]
+  int splits;              // prompt kernel: of every tile of rows
+  int shares;              // decode kernel: slots that are meant to have equal shares of all tiles (0: a slot per sequence)
+  float* partials;         // decode: [slot, kv head, column, D + 2]; prompt: [unit, split, D + 2, row]
   int32_t* counters;       // [unit], zero between calls
-  int units;               // what the splits of are joined: (sequence, kv head), or a tile of query rows
+  int units;               // what the splits of are joined: (sequence, kv head), or (tile of query rows, kv head)
 };
+
+// Most splits of a sequence in the decode kernel: 1.2 sqrt(tiles), where a split's ticket and merge (2 us with up to four
+// columns) outweigh shorter shares, 0.9 with more columns; none below 12 tiles, 24 with 64 channels or more columns.
+__host__ __device__ inline int decode_cap(int tiles, int head_dim, int cols) {
+  if (tiles < (head_dim == 64 || cols > 4 ? 24 : 12)) return 1;
+  const int cap = (int)((cols > 4 ? 0.9f : 1.2f) * sqrtf((float)tiles));
+  return cap < kMaxSplits ? cap : kMaxSplits;
+}
 
 constexpr float kLazy = 8.f;   // a running maximum may fall behind by so many powers of two before sums are rescaled
 
@@ -78,14 +87,14 @@ __device__ __forceinline__ uint32_t keep_tokens(uint32_t w, int left) { return l
 // Whether this workgroup is the last of its unit's splits to hand in its partial results.  They are device-scope stores; every
 // wave waits for its own, then one thread takes a ticket at the memory side, so the holder of the last ticket finds all of
 // them performed; it reads them with device-scope loads.
-__device__ __forceinline__ bool last_of_splits(const PagedAttnArgs& a, int unit, int& s_last) {
+__device__ __forceinline__ bool last_of_splits(int32_t* counter, int splits, int& s_last) {
   asm volatile("s_waitcnt vmcnt(0)" ::: "memory");
   __builtin_amdgcn_fence(__ATOMIC_RELEASE, "workgroup");
   __syncthreads();
   if (threadIdx.x == 0) {
-    const int ticket = __hip_atomic_fetch_add(a.counters + unit, 1, __ATOMIC_RELAXED, __HIP_MEMORY_SCOPE_AGENT);
-    s_last = ticket == a.splits - 1;
-    if (s_last) __hip_atomic_store(a.counters + unit, 0, __ATOMIC_RELAXED, __HIP_MEMORY_SCOPE_AGENT);   // clean for the next call
+    const int ticket = __hip_atomic_fetch_add(counter, 1, __ATOMIC_RELAXED, __HIP_MEMORY_SCOPE_AGENT);
+    s_last = ticket == splits - 1;
+    if (s_last) __hip_atomic_store(counter, 0, __ATOMIC_RELAXED, __HIP_MEMORY_SCOPE_AGENT);   // clean for the next call
   }
   __syncthreads();
   return s_last;
@@ -96,16 +105,14 @@ struct JoinSpace {   // LDS
   int last;
 };
 
-// Joins the partial results of a unit's splits and writes the outputs.
-// cols: valid columns of the unit; out_of(col): pointer to the column's output row.
+// Joins the partial results of `ns` splits, `step` floats apart from `base` on, and writes the outputs.
+// cols: valid columns; out_of(col): pointer to the column's output row.
 template <typename T, int D, typename Out>
-__device__ __forceinline__ void join_splits(const PagedAttnArgs& a, int unit, int stride_cols, int cols, JoinSpace& js, Out out_of) {
-  if (!last_of_splits(a, unit, js.last)) return;
-  const float* base = a.partials + (long)unit * a.splits * stride_cols * (D + 2);
-  const long step = (long)stride_cols * (D + 2);
+__device__ __forceinline__ void join_splits(int32_t* counter, int ns, const float* base, long step, int cols, JoinSpace& js, Out out_of) {
+  if (!last_of_splits(counter, ns, js.last)) return;
   // Sixteen columns at a time: every (column, split)'s maximum and sum in one round trip, weights to LDS, then the elements,
   // eight splits of two of them on their way together.
-  const int ns = a.splits, tid = threadIdx.x, threads = blockDim.x;
+  const int tid = threadIdx.x, threads = blockDim.x;
   auto load = [](const float* p) __attribute__((always_inline)) { return __hip_atomic_load(p, __ATOMIC_RELAXED, __HIP_MEMORY_SCOPE_AGENT); };
   for (int c0 = 0; c0 < cols; c0 += 16) {
     const int nc = min(16, cols - c0);

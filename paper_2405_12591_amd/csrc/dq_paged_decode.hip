@@ -5,9 +5,65 @@ namespace dq {
 
 constexpr int kCols = 16;   // (row, query head) columns of a workgroup: one matrix instruction's
 
-// One workgroup of four waves per (sequence, kv head, split); its columns are the (row, query head) pairs that read the
-// kv head.  Every wave works tiles of 64 tokens on its own, dealt round-robin over the waves of all splits, and keeps a
-// running maximum, sum and output; waves are joined through LDS, splits through memory.
+// The sequence and split a slot works on: a slot is a share of a sequence's tiles, the same for all kv heads.  `shares` slots are
+// meant to get as many tiles each, t = all tiles / shares; a sequence has tiles / t of them, rounded, at least one, at most
+// decode_cap().  With one length a sequence each that is an even split; in a batch of one long and many short sequences the long one
+// gets nearly all slots: 16 sequences of 8 heads, one of 32768 tokens and 15 of 500, 26 us, 220 with a slot each; 4 x 40 heads of 9384 to
+// 16384 tokens 93 us (98 split evenly).  Where there is one share a sequence, what is over a share gets another slot (32 x 8
+// heads of 64 to 8192 tokens 64 us, 77 rounded).  Up to 64 sequences, one a lane; more of them are split evenly.
+struct Share {
+  int b, split, splits;    // splits == 0: an empty slot
+  int first_slot;          // of the sequence
+  Sequence s;
+};
+__device__ __forceinline__ int first_tile_of(const Sequence& s, int window) { return window ? max(s.len - s.n + 1 - window, 0) / kPagedTile : 0; }
+
+__device__ __forceinline__ Share share_of(const PagedAttnArgs& a, int slot) {
+  Share r;
+  const int P = a.c.page_tokens, batch = a.bt.batch;
+  if (batch > 64 || a.shares == 0) {
+    r.splits = a.shares ? a.shares / batch : 1;
+    r.b = slot / r.splits;
+    r.split = slot % r.splits;
+    r.first_slot = slot - r.split;
+    r.s = sequence_of_wave(a.bt, P, r.b);
+    if (r.s.n == 0) r.splits = 0;
+    return r;
+  }
+  const int lane = threadIdx.x & 63;
+  Sequence s = {0, 0, 0};
+  if (lane < batch) s = sequence_of(a.bt, P, lane);
+  const int tiles = s.n ? (s.len + kPagedTile - 1) / kPagedTile - first_tile_of(s, a.window) : 0;
+  int total = tiles;
+#pragma unroll
+  for (int o = 1; o < 64; o *= 2) total += __shfl_xor(total, o);
+  const float per = fmaxf((float)total / (float)a.shares, 1.f), round = a.shares == batch ? 0.99f : 0.5f;
+  const int cap = decode_cap(tiles, a.c.head_dim, a.max_rows * a.group);
+  const int mine = s.n ? max(min((int)((float)tiles / per + round), min(cap, kMaxSplits)), 1) : 0;
+  int upto = mine;                                        // slots of the sequences up to this one
+#pragma unroll
+  for (int o = 1; o < 64; o *= 2) {
+    const int x = __shfl_up(upto, o);
+    if (lane >= o) upto += x;
+  }
+  const uint64_t owner = __ballot(slot < upto && slot >= upto - mine);
+  if (owner == 0) {
+    r.splits = 0;
+    return r;
+  }
+  r.b = __builtin_ctzll(owner);
+  r.splits = __builtin_amdgcn_readlane(mine, r.b);
+  r.first_slot = __builtin_amdgcn_readlane(upto, r.b) - r.splits;
+  r.split = slot - r.first_slot;
+  r.s.row0 = __builtin_amdgcn_readlane(s.row0, r.b);
+  r.s.n = __builtin_amdgcn_readlane(s.n, r.b);
+  r.s.len = __builtin_amdgcn_readlane(s.len, r.b);
+  return r;
+}
+
+// One workgroup of four waves per (slot, kv head); its columns are the (row, query head) pairs that read the kv head.  Every
+// wave works tiles of 64 tokens on its own, dealt round-robin over the waves of all splits, and keeps a running maximum, sum
+// and output; waves are joined through LDS, splits through memory.
 //
 // Scores are formed transposed, S^T = K Q^T, token rows against query columns.  Row r of the four 16-row products stands
 // for token 16 (r / 4) + 4 t4 + r % 4, so a lane ends up with the scores of 16 neighbouring tokens of its column:
@@ -17,18 +73,19 @@ constexpr int kCols = 16;   // (row, query head) columns of a workgroup: one mat
 // The values' scale rides in the exponent: u = s + log2(scale_v), p = 2^(u - m), O += p c, l += (sum p) / scale_v; the
 // products see codes and p only, and p is largest (2^8 at most) where the contribution to the output is.
 template <typename T, int D, bool FP8>
-__global__ __launch_bounds__(kPagedThreads) void paged_decode_kernel(PagedAttnArgs a) {
+__global__ __launch_bounds__(kPagedThreads, 2) void paged_decode_kernel(PagedAttnArgs a) {
   constexpr int NC = D / 64, NCT = D / 16;
   typedef typename Vec8<T>::type tx8;
   __shared__ float s_o[4][kCols][D + 1];
   __shared__ float s_m[4][kCols], s_l[4][kCols];
   __shared__ JoinSpace s_join;
-  const int tid = threadIdx.x, lane = tid & 63, wave = tid >> 6, col = lane & 15, G = lane >> 4;
-  const int unit = (int)blockIdx.x / a.splits, split = (int)blockIdx.x % a.splits;
-  const int H = a.c.kv_heads, b = unit / H, h = unit % H, P = a.c.page_tokens;
-  const Sequence s = sequence_of(a.bt, P, b);
+  const int tid = threadIdx.x, lane = tid & 63, wave = __builtin_amdgcn_readfirstlane(tid >> 6), col = lane & 15, G = lane >> 4;
+  const int H = a.c.kv_heads, P = a.c.page_tokens, slot = (int)blockIdx.x / H, h = (int)blockIdx.x % H;
+  const Share sh = share_of(a, slot);
+  if (sh.splits == 0) return;
+  const Sequence& s = sh.s;
+  const int b = sh.b, splits = sh.splits, unit = b * H + h;
   const int n = min(s.n, a.max_rows), len = s.len, before = len - s.n;   // tokens before the sequence's first row
-  if (n == 0) return;
   const int cols = n * a.group;
   const int qi = min(col / a.group, n - 1), hq = h * a.group + col % a.group;
   const bool live = col < cols;
@@ -36,7 +93,7 @@ __global__ __launch_bounds__(kPagedThreads) void paged_decode_kernel(PagedAttnAr
   const int place = before + qi;
   const int see_hi = a.causal ? min(place + 1, len) : len, see_lo = a.window ? max(place + 1 - a.window, 0) : 0;
   const int all_hi = a.causal ? min(before + 1, len) : len, all_lo = a.window ? max(before + n - a.window, 0) : 0;
-  const int first_tile = a.window ? max(before + 1 - a.window, 0) / kPagedTile : 0;
+  const int first_tile = first_tile_of(s, a.window);
   const int runs = P / kPagedTile, code_tiles = len / P * runs, tiles = (len + kPagedTile - 1) / kPagedTile;
 
   // ---- queries: 8 channels 64 c + 16 G + 8 half of the column, in f16 ----
@@ -109,7 +166,7 @@ __global__ __launch_bounds__(kPagedThreads) void paged_decode_kernel(PagedAttnAr
   };
 
   // ---- full pages ----
-  const int stride = a.splits * 4, mine = first_tile + split * 4 + wave;
+  const int stride = splits * 4, mine = first_tile + sh.split * 4 + wave;
   const int k_row = 16 * ((lane & 15) >> 2) + (lane & 3);   // + 4 t4: the token of this lane's row
   for (int batch0 = mine; batch0 < code_tiles; batch0 += 64 * stride) {
     // the next 64 tiles' blocks and scales, one per lane
@@ -177,11 +234,11 @@ __global__ __launch_bounds__(kPagedThreads) void paged_decode_kernel(PagedAttnAr
   // ---- the page being filled: 16-bit rows, products in their own type ----
   const int tail_first = max(code_tiles, first_tile);
   for (int tile = tail_first; tile < tiles; ++tile) {
-    if ((tile - first_tile) % stride != split * 4 + wave) continue;
-    const int slot = a.bt.tail_slots ? a.bt.tail_slots[b] : b;
-    const bool ok = slot >= 0 && slot < a.c.slots;
+    if ((tile - first_tile) % stride != sh.split * 4 + wave) continue;
+    const int at_slot = a.bt.tail_slots ? a.bt.tail_slots[b] : b;
+    const bool ok = at_slot >= 0 && at_slot < a.c.slots;
     const int run = tile - code_tiles, left = len - tile * kPagedTile;   // tokens of the tile
-    const long at = (((long)(ok ? slot : 0) * H + h) * runs + run) * kPagedTile * D;
+    const long at = (((long)(ok ? at_slot : 0) * H + h) * runs + run) * kPagedTile * D;
     const uint16_t* const kt = a.c.k_tail + at + k_row * D + 16 * G;
     const uint16_t* const vt = a.c.v_tail + at + (lane & 15) * kPagedTile + 16 * G;
     const float f = ok ? keep_sign(a.scale_log2) : __builtin_nanf("");
@@ -229,7 +286,9 @@ __global__ __launch_bounds__(kPagedThreads) void paged_decode_kernel(PagedAttnAr
   if (G == 0) { s_m[wave][col] = m; s_l[wave][col] = l; }
   __syncthreads();
   auto out_of = [&](int c) { return a.out.data + (long)(s.row0 + c / a.group) * a.out.token_stride + (long)(h * a.group + c % a.group) * a.out.head_stride; };
-  float* const part = a.partials + ((long)unit * a.splits + split) * kCols * (D + 2);
+  const long part_step = (long)H * kCols * (D + 2);        // from split to split
+  float* const parts = a.partials + ((long)sh.first_slot * H + h) * kCols * (D + 2);
+  float* const part = parts + sh.split * part_step;
   for (int idx = tid; idx < cols * D; idx += kPagedThreads) {
     const int cc = idx / D, ch = idx % D;
     const float M = fmaxf(fmaxf(s_m[0][cc], s_m[1][cc]), fmaxf(s_m[2][cc], s_m[3][cc]));
@@ -241,7 +300,7 @@ __global__ __launch_bounds__(kPagedThreads) void paged_decode_kernel(PagedAttnAr
       oo = __builtin_fmaf(s_o[w][cc][ch], f, oo);
       ll = __builtin_fmaf(s_l[w][cc], f, ll);
     }
-    if (a.splits == 1) {
+    if (splits == 1) {
       const T y = (T)(ll == 0.f ? 0.f : oo / ll);
       out_of(cc)[ch] = __builtin_bit_cast(uint16_t, y);
     } else {
@@ -253,12 +312,12 @@ __global__ __launch_bounds__(kPagedThreads) void paged_decode_kernel(PagedAttnAr
       }
     }
   }
-  if (a.splits > 1) join_splits<T, D>(a, unit, kCols, cols, s_join, out_of);
+  if (splits > 1) join_splits<T, D>(a.counters + unit, splits, parts, part_step, cols, s_join, out_of);
 }
 
 template <typename T, int D>
 static void launch_decode(const PagedAttnArgs& a, hipStream_t st) {
-  const dim3 grid((unsigned)((long)a.units * a.splits));
+  const dim3 grid((unsigned)((long)(a.shares ? a.bt.batch > 64 ? a.shares : a.shares + a.bt.batch : a.bt.batch) * a.c.kv_heads));
   if (a.c.codes == DQ_CODES_E4M3) hipLaunchKernelGGL((paged_decode_kernel<T, D, true>), grid, dim3(kPagedThreads), 0, st, a);
   else hipLaunchKernelGGL((paged_decode_kernel<T, D, false>), grid, dim3(kPagedThreads), 0, st, a);
 }

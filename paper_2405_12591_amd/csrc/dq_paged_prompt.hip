@@ -27,7 +27,7 @@ __global__ __launch_bounds__(64 * kPromptWaves, RB == 1 ? 2 : 1) void paged_prom
   const int H = a.c.kv_heads, P = a.c.page_tokens;
   const int h = (int)(blockIdx.x % H), split = (int)(blockIdx.x / H) % a.splits, item = (int)(blockIdx.x / H) / a.splits;
   const int b = item_owner(a.bt.starts, a.bt.rows, a.bt.batch, item, a.group, M, 1);
-  const Sequence s = sequence_of(a.bt, P, b);
+  const Sequence s = sequence_of_wave(a.bt, P, b);
   const int n = s.n, len = s.len;
   const int row_tiles = (int)(((long)n * a.group + M - 1) / M);
   const int j = item - item_first(a.bt.starts, a.bt.rows, b, a.group, M, 1);
@@ -319,7 +319,7 @@ __global__ __launch_bounds__(64 * kPromptWaves, RB == 1 ? 2 : 1) void paged_prom
       }
     }
   }
-  if (a.splits == 1 || !last_of_splits(a, unit, s_last)) return;
+  if (a.splits == 1 || !last_of_splits(a.counters + unit, a.splits, s_last)) return;
   // The splits' results: a thread takes a row and every (THREADS / M)-th run of eight channels of it.
   static_assert(M <= THREADS && THREADS % M == 0 && sizeof(s_k) >= kPromptSplits * M * sizeof(float), "rows a thread, weights in LDS");
   float* const weight = reinterpret_cast<float*>(s_k);    // [split][row]
@@ -381,7 +381,8 @@ int32_t launch_paged_prompt(const PagedAttnArgs& a, hipStream_t st) {
 struct PagedShape {
   bool decode;
   long units;
-  int splits, cols;
+  int splits, cols;        // splits: of every unit (prompt), of a sequence of the longest length if all were (decode)
+  long shares, groups;     // decode: PagedAttnArgs::shares; workgroups that may hand over partial results (0: none)
 };
 
 constexpr int kPagedCounters = 4096;      // units that may be split, with a ticket each at a fixed place: calls of all sizes may share a workspace
@@ -398,14 +399,11 @@ static int pick_splits(long units, int cap, int wanted) {
   return n;
 }
 
-// Decode kernel: a workgroup per compute unit (two with 64 channels, whose waves have half the bytes on their way); at most 1.2 sqrt(tiles)
-// splits, where a split's ticket and merge (2 us) outweigh shorter shares; none below 12 tiles of 128 channels.  Measured over 1
-// to 1024 units of 2 to 2000 tiles, 13 split counts each: the picks are 1.3 % behind the best on average; 128 units of 512 tiles
-// 160 us in two splits, 165 in 6.
-static int decode_splits(long units, int tiles, int head_dim) {
-  if ((long)tiles * head_dim < 12 * 128) return 1;
-  const int cap = (int)(1.2f * sqrtf((float)tiles));
-  return pick_splits(units, cap < kMaxSplits ? cap : kMaxSplits, 256 * 128 / head_dim);
+// Decode kernel: a workgroup per compute unit, two where 128 units or more of 64 channels (half the bytes on a wave's way) would
+// leave them with long shares.  Measured over 1 to 1024 units of 2 to 2000 tiles, 13 split counts each: the picks are 1.4 % behind the
+// best on average; 128 units of 512 tiles of 128 channels 160 us in two splits, 165 in 6; 128 of 47 tiles of 64 channels 11.6 us in 4, 14.5 in 2.
+static int decode_splits(long units, int tiles, int head_dim, int cols) {
+  return pick_splits(units, decode_cap(tiles, head_dim, cols), head_dim == 64 && units >= 128 ? 512 : 256);
 }
 
 // Prompt kernel: two workgroups a compute unit; a split hands over 66 KB, so at most 0.75 sqrt(tiles).  8 units of 500 tiles 71 us in 16
@@ -430,9 +428,17 @@ static bool paged_shape(const dq_paged_cache* c, int batch, long rows, int q_hea
   if (s->units >= (1l << 24)) return false;
   // (a sequence leaves part of its last tile of rows empty; no more tiles than the longest sequence would have)
   const long filled = (long)batch * (((long)max_rows * group + kPromptRows - 1) / kPromptRows) * c->kv_heads;
-  s->splits = s->decode ? decode_splits(s->units, tiles, c->head_dim) : pick_splits(filled < s->units ? filled : s->units, prompt_cap(tiles), 512);
+  s->splits = s->decode ? decode_splits(s->units, tiles, c->head_dim, max_rows * group) : pick_splits(filled < s->units ? filled : s->units, prompt_cap(tiles), 512);
   if (const int v = (int)(flags >> 8 & 0x7Fu)) s->splits = !s->decode && v > kPromptSplits ? kPromptSplits : v;   // the caller's override
   if (s->units > kPagedCounters) s->splits = 1;
+  s->shares = 0;
+  s->groups = s->splits == 1 ? 0 : s->units * s->splits;
+  if (s->decode) {
+    // also where every sequence gets one slot on average, long ones are split if their lengths differ
+    const bool some = s->splits > 1 || ((flags >> 8 & 0x7Fu) == 0 && batch > 1 && batch <= 64 && s->units <= kMostSplitGroups && decode_cap(tiles, c->head_dim, max_rows * group) > 1);
+    if (some) s->shares = (long)s->splits * batch;
+    s->groups = some ? (s->shares + (batch <= 64 ? batch : 0)) * c->kv_heads : 0;
+  }
   return true;
 }
 
@@ -452,8 +458,8 @@ extern "C" size_t dq_paged_workspace_bytes(const dq_paged_cache* cache, int32_t 
   const int tiles = max_seq_len / kPagedTile + 1;
   const long decode_units = (long)batch * cache->kv_heads;
   auto most = [](long units, int splits, long groups) { const long n = units * splits; return splits == 1 ? 0l : n < groups ? n : groups; };
-  const int cap = (long)tiles * cache->head_dim < 12 * 128 ? 1 : kMaxSplits;
-  size_t bytes = paged_bytes(most(decode_units, cap, kMostSplitGroups), 16, cache->head_dim);
+  const int cap = decode_cap(tiles, cache->head_dim, 1) == 1 ? 1 : kMaxSplits + 1;
+  size_t bytes = paged_bytes(most(decode_units, cap, 2 * kMostSplitGroups), 16, cache->head_dim);
   if (!s.decode) {
     const size_t p = paged_bytes(most(s.units, prompt_cap(tiles), 2 * kMostSplitGroups), kPromptRows, cache->head_dim);
     if (p > bytes) bytes = p;
@@ -471,7 +477,7 @@ extern "C" int32_t dq_paged_attention(const dq_paged_cache* cache, const dq_page
   if (softmax_scale != softmax_scale) return DQ_EINVAL;
   PagedShape s;
   if (!paged_shape(cache, batch->batch, batch->rows, q->heads, max_rows, max_seq_len, window, flags, &s)) return DQ_EINVAL;
-  if (workspace_bytes < paged_bytes(s.splits == 1 ? 0 : s.units * s.splits, s.cols, cache->head_dim)) return DQ_ENOSPACE;
+  if (workspace_bytes < paged_bytes(s.groups, s.cols, cache->head_dim)) return DQ_ENOSPACE;
   if (batch->rows == 0 || max_rows == 0) return DQ_OK;
   PagedAttnArgs a = {};
   a.c = *cache; a.bt = *batch; a.q = *q; a.out = *out;
@@ -481,6 +487,7 @@ extern "C" int32_t dq_paged_attention(const dq_paged_cache* cache, const dq_page
   a.causal = (flags & DQ_PAGED_CAUSAL) ? 1 : 0;
   a.scale_log2 = (softmax_scale > 0.f ? softmax_scale : 1.0f / sqrtf((float)cache->head_dim)) * 1.44269504088896340736f;
   a.splits = s.splits;
+  a.shares = (int)s.shares;
   a.units = (int)s.units;
   char* ws = reinterpret_cast<char*>(workspace);
   a.counters = reinterpret_cast<int32_t*>(ws + kWsHeaderBytes);

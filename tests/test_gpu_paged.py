@@ -555,3 +555,20 @@ def test_the_decoquant_layer_takes_projections():
         assert torch.equal(oa, ob)
     for n in a.cache.t:
         assert torch.equal(a.cache.t[n], b.cache.t[n]), n
+
+
+@pytest.mark.parametrize("dtype,codes", FORMATS[:2])
+def test_batches_of_very_different_lengths(dtype, codes):
+    """Slots are dealt by length: one long sequence among short and empty ones, rows without tokens before them, more
+    sequences than a wave has lanes, with and without a window."""
+    gen = torch.Generator().manual_seed(22)
+    lens = [3, 9000, 0, 64, 1, 700, 2500, 65]
+    new = [1, 1, 0, 1, 1, 1, 0, 1]
+    seqs = Sequences(lens, 1, 128, dtype, codes, 64, gen)
+    cache = filled_cache(seqs, lens, gen)
+    for window in (0, 300):
+        _run(seqs, lens, new, 4, torch.Generator().manual_seed(1), cache=cache, window=window)
+    lens = [int(x) for x in torch.randint(0, 400, (70,), generator=gen)]
+    lens[5], lens[66] = 4000, 1500
+    seqs = Sequences(lens, 1, 64, dtype, codes, 64, gen)
+    _run(seqs, lens, [min(n, 1 + i % 3) for i, n in enumerate(lens)], 4, gen)
