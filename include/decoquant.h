@@ -468,7 +468,8 @@ typedef struct dq_paged_cache {
  * slot that does not exist are dropped by dq_paged_append and make attention yield NaN.
  */
 typedef struct dq_paged_batch {
-  const int32_t* starts;     /* i32 [batch + 1], ascending; NULL: one row per sequence (rows == batch)  */
+  const int32_t* starts;     /* i32 [batch + 1], ascending, not always from 0; NULL: one row per sequence
+                                (rows == batch)                                                       */
   const int32_t* seq_lens;   /* i32 [batch], tokens with the call's rows included                       */
   const int32_t* page_table; /* i32 [batch, table_stride], page of the j-th P tokens; only full pages
                                 are read: the entry of the page being filled may be set late            */

@@ -85,14 +85,14 @@ __device__ __forceinline__ Sequence sequence_of_wave(const dq_paged_batch& bt, i
   return s;
 }
 
-// Work items dealt to sequences without a scan: sequence b's items start at first(b) = starts[b] / unit + per_seq * b, which
-// leaves it at least rows / unit + per_seq - 1 of them.  The sequence an item belongs to, by bisection.
+// Work items dealt to sequences without a scan: with `at` the rows before sequence b's, its items start at first(b) =
+// at * mul / unit + per_seq * b, which leaves it at least rows * mul / unit + per_seq - 1 of them.
 __device__ __forceinline__ int item_first(const int32_t* starts, int rows, int b, int mul, int unit, int per_seq) {
-  const long at = starts ? min(max(starts[b], 0), rows) : b;
+  const long at = starts ? min(max(starts[b], 0), rows) - min(max(starts[0], 0), rows) : b;
   return (int)(at * mul / unit) + per_seq * b;
 }
-// All 64 lanes look at once, so that a batch of up to 64 sequences takes one round trip (bisection took four or more,
-// 2 us of an appended token).
+// The sequence an item belongs to.  All 64 lanes look at once, so that a batch of up to 64 sequences takes one round trip
+// (bisection took four or more, 2 us of an appended token).
 __device__ __forceinline__ int item_owner(const int32_t* starts, int rows, int batch, int item, int mul, int unit, int per_seq) {
   int lo = 0, n = batch;                                  // the owner is in [lo, lo + n)
   while (n > 1) {

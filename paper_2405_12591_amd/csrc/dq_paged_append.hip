@@ -79,7 +79,7 @@ __global__ __launch_bounds__(P * D / 16, 4) void paged_append_kernel(AppendArgs 
     }
     if (live) {
       const Sequence s = sequence_of(a.bt, P, b);
-      live = row < s.row0 + s.n;                          // rows behind the last sequence's stay as they are
+      live = row >= s.row0 && row < s.row0 + s.n;         // rows before the first sequence's and behind the last's stay as they are
       place = s.len - s.n + (int)(row - s.row0);
     }
     RowLayout turned = l;
@@ -315,7 +315,7 @@ __global__ __launch_bounds__(kPagedThreads) void paged_read_kernel(ReadArgs a) {
   const int first = a.first ? max(a.first[b], 0) : 0;
   const int page = first / P + (int)blockIdx.x - item_first(a.out_starts, a.bt.rows, b, 1, P, 2);
   const int base = page * P;
-  if (first >= len || page < first / P || base >= len) return;
+  if (first >= len || page < first / P || page > (len - 1) / P) return;
   const long out0 = (long)a.out_starts[b] - first;        // row of token 0
   const long row_end = min((long)a.bt.rows, (long)a.out_starts[b + 1]);
   const bool full = base + P <= len;

@@ -572,3 +572,35 @@ def test_batches_of_very_different_lengths(dtype, codes):
     lens[5], lens[66] = 4000, 1500
     seqs = Sequences(lens, 1, 64, dtype, codes, 64, gen)
     _run(seqs, lens, [min(n, 1 + i % 3) for i, n in enumerate(lens)], 4, gen)
+
+
+@pytest.mark.parametrize("new", [1, 3, 300])
+def test_rows_that_belong_to_no_sequence_may_come_first(new):
+    """starts[0] > 0: the same bits as without the rows before it, which stay as they are, whatever bound on rows is given."""
+    gen = torch.Generator().manual_seed(23)
+    skip, have, hq = 700, 100, 4
+    lens = [have + new] * 2
+    seqs = Sequences(lens, 2, 64, F16, INT8, 64, gen)
+    cache, table, slots = filled_cache(seqs, lens, gen)
+    q = rows((skip + 2 * new, hq, 64), F16, gen, outliers=False).to(DEV)
+    ws = dq.paged_workspace(cache, 2, skip + 2 * new, hq, new, have + new)
+    out = torch.full_like(q, 5.0)
+    dq.paged_attention(cache, q, ints([skip, skip + new, skip + 2 * new]), ints(lens), table, new, have + new, ws, out=out, tail_slots=slots)
+    want = dq.paged_attention(cache, q[skip:], ints([0, new, 2 * new]), ints(lens), table, new, have + new, ws, tail_slots=slots)
+    assert torch.equal(out[skip:], want) and (out[:skip] == 5.0).all()
+    # append: keys, and queries beside them
+    rot = dq.rotary(64, device=DEV)
+    fused = rows((skip + 2 * new, hq + 4, 64), F16, gen).to(DEV)
+    both = []
+    for at, starts in ((0, [skip, skip + new, skip + 2 * new]), (skip, [0, new, 2 * new])):
+        c = dq.alloc_paged_cache(cache.pages, 2, 2, 64, 64, F16, INT8, DEV)
+        f = fused[at:]
+        qo = torch.full((len(f), hq, 64), 5.0, dtype=F16, device=DEV)
+        dq.paged_append(c, f[:, hq:hq + 2], f[:, hq + 2:], ints(starts), ints(lens), table, q=f[:, :hq], q_out=qo, rotary=rot)
+        assert (qo[:starts[0]] == 5.0).all()
+        back = torch.full((len(f), 2, 64), 5.0, dtype=F16, device=DEV), torch.full((len(f), 2, 64), 5.0, dtype=F16, device=DEV)
+        dq.paged_read(c, ints([have, have]), ints(lens), ints(starts), table, *back)
+        assert all((x[:starts[0]] == 5.0).all() for x in back)
+        both.append([qo[starts[0]:]] + [x[starts[0]:] for x in back] + list(c.t.values()))
+    for a, b in zip(*both):
+        assert torch.equal(a.view(torch.uint8), b.view(torch.uint8))
