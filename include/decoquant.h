@@ -517,7 +517,7 @@ size_t dq_paged_workspace_bytes(const dq_paged_cache* cache, int32_t batch, int3
  *   q, out         [rows, q_heads, d]; out may be q
  *   max_rows       host bound on the rows of any sequence; it chooses the kernel, and further rows of a
  *                  sequence may be left out
- *   max_seq_len    host bound on seq_lens (a guess does: it sizes the launch, results do not depend on it)
+ *   max_seq_len    host bound on seq_lens (a guess does: it sizes the launch only, which orders the sums)
  *   window         > 0: a row sees the last `window` tokens up to its own place only (needs causal)
  *   softmax_scale  <= 0 selects 1/sqrt(d)
  * A row that sees no token yields zeros.  Rows behind the last sequence's are not written.

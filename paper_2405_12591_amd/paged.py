@@ -415,7 +415,7 @@ class PagedKVLayer:
         self.page_table = torch.arange(batch * width, dtype=torch.int32, device=device).view(batch, width)
         self.seq_lens = torch.zeros(batch, dtype=torch.int32, device=device)
         self.tokens_upper = 0               # no sequence holds more tokens than this (host-side bound)
-        self._ws = None
+        self._ws, self._outgrown = None, []
 
     def append(self, k: torch.Tensor, v: torch.Tensor, starts: Optional[torch.Tensor] = None, max_rows: int = 1,
                q: Optional[torch.Tensor] = None, rotary: Optional[Rotary] = None, positions: Optional[torch.Tensor] = None,
@@ -429,17 +429,26 @@ class PagedKVLayer:
             self.tokens_upper = int(self.seq_lens.max())
             if self.tokens_upper + max_rows > self.max_tokens:
                 raise DQError("the rows exceed the layer's %d tokens per sequence" % self.max_tokens)
-        self.seq_lens += 1 if starts is None else starts.diff()
+        new = 1 if starts is None else starts.diff()
+        self.seq_lens += new
+        try:
+            q = paged_append(self.cache, k, v, starts, self.seq_lens, self.page_table, q=q, rotary=rotary, positions=positions,
+                             q_weight=q_weight, k_weight=k_weight, eps=eps)
+        except DQError:                     # nothing was launched
+            self.seq_lens -= new
+            raise
         self.tokens_upper += max_rows
-        return paged_append(self.cache, k, v, starts, self.seq_lens, self.page_table, q=q, rotary=rotary, positions=positions,
-                            q_weight=q_weight, k_weight=k_weight, eps=eps)
+        return q
 
     def attend(self, q: torch.Tensor, starts: Optional[torch.Tensor] = None, max_rows: int = 1, out: Optional[torch.Tensor] = None,
                softmax_scale: float = 0.0, causal: bool = True, window: int = 0) -> torch.Tensor:
         """Attention of the rows just appended, q [rows, q_heads, d] (paged_attention)."""
         rows, bound = q.shape[0], min(self.tokens_upper, self.max_tokens)
         if self._ws is None or rows > self._ws[0] or max_rows > self._ws[1]:
-            sizes = (max(rows, self._ws[0]), max(max_rows, self._ws[1])) if self._ws else (rows, max_rows)
+            sizes = (rows, max_rows)
+            if self._ws:
+                sizes = (max(rows, self._ws[0]), max(max_rows, self._ws[1]))
+                self._outgrown.append(self._ws[2])   # a captured graph may still work in it
             self._ws = (*sizes, paged_workspace(self.cache, self.batch, sizes[0], self.q_heads, sizes[1], self.max_tokens))
         return paged_attention(self.cache, q, starts, self.seq_lens, self.page_table, max_rows, bound, self._ws[2], out=out,
                                softmax_scale=softmax_scale, causal=causal, window=window)

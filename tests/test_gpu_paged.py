@@ -604,3 +604,43 @@ def test_rows_that_belong_to_no_sequence_may_come_first(new):
         both.append([qo[starts[0]:]] + [x[starts[0]:] for x in back] + list(c.t.values()))
     for a, b in zip(*both):
         assert torch.equal(a.view(torch.uint8), b.view(torch.uint8))
+
+
+def test_a_layer_after_a_refused_append_and_with_a_captured_step():
+    """A refused append leaves the lengths alone; a step captured before a larger call replays with it between the replays."""
+    gen = torch.Generator().manual_seed(24)
+    heads, hq, d = 2, 4, 64
+    layer, plain = (dq.PagedKVLayer(2, hq, heads, d, 4000, 64, F16, INT8, DEV) for _ in range(2))
+    k, v = (rows((2, heads, d), F16, gen).to(DEV) for _ in range(2))
+    q = rows((2, hq, d), F16, gen, outliers=False).to(DEV)
+    pk, pv = (rows((1400, heads, d), F16, gen).to(DEV) for _ in range(2))
+    pq = rows((1400, hq, d), F16, gen, outliers=False).to(DEV)
+    starts = ints([0, 700, 1400])
+
+    def step(x):
+        x.append(k, v)
+        return x.attend(q)
+
+    for x in (layer, plain):
+        x.append(pk, pv, starts, 700)
+    with pytest.raises(dq.DQError):
+        layer.append(k.bfloat16(), v)
+    with pytest.raises(dq.DQError):
+        layer.append(k, v, ints([0, 1]))
+    assert layer.seq_lens.tolist() == [700, 700] and layer.tokens_upper == 700
+    step(layer)                                          # (the workspace of one row each)
+    step(plain)
+    stream, graph = torch.cuda.Stream(), torch.cuda.CUDAGraph()
+    torch.cuda.synchronize()
+    with torch.cuda.graph(graph, stream=stream):
+        out = step(layer)
+    for i in range(3):
+        graph.replay()
+        assert torch.equal(out, step(plain))
+        if i:
+            continue
+        for x in (layer, plain):                         # needs a larger workspace
+            x.append(pk, pv, starts, 700)
+        hold = [layer.attend(pq, starts, 700)] + [torch.full((1 << 20,), 7, dtype=torch.uint8, device=DEV) for _ in range(64)]
+        assert torch.equal(hold[0], plain.attend(pq, starts, 700))
+    assert torch.equal(layer.seq_lens, plain.seq_lens)
