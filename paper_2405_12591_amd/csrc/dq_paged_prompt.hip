@@ -11,14 +11,14 @@ constexpr int kPromptSplits = 32;   // at most, of a tile of rows (their weights
 // 16 + 8 h .. of the 32 (h = lane / 32), the right operand that the product with the values wants.
 __device__ __forceinline__ int score_token(int r) { return 16 * (r >> 4) + 8 * ((r >> 2) & 1) + 4 * ((r >> 3) & 1) + (r & 3); }
 
-// One workgroup of four waves per (tile of rows, kv head, split): RB * 32 (row, query head) pairs a wave.  The tile's
+// One workgroup of four waves per (tile of rows, kv head, split): 32 (row, query head) pairs a wave.  The tile's
 // codes are turned to f16 once and shared through LDS (two buffers of 64 tokens, pieces of 16 bytes swizzled so that 16
 // neighbouring lanes touch all banks); keys as [token][channel], values as [channel][token], as they are stored.
 // Scores are formed transposed, as in the decode kernel: probabilities go from the first product's result registers to
 // the second's operand registers without leaving the lane.
-template <typename T, int D, bool FP8, int RB>
-__global__ __launch_bounds__(64 * kPromptWaves, RB == 1 ? 2 : 1) void paged_prompt_kernel(PagedAttnArgs a) {
-  constexpr int NK = D / 16, NCT = D / 32, NB = D / 64, M = 32 * RB * kPromptWaves;
+template <typename T, int D, bool FP8>
+__global__ __launch_bounds__(64 * kPromptWaves, 2) void paged_prompt_kernel(PagedAttnArgs a) {
+  constexpr int NK = D / 16, NCT = D / 32, NB = D / 64, M = 32 * kPromptWaves;
   constexpr int THREADS = 64 * kPromptWaves;
   typedef typename Vec8<T>::type tx8;
   __shared__ __align__(16) u32x4 s_k[2][64 * D / 8], s_v[2][64 * D / 8];
@@ -49,23 +49,18 @@ __global__ __launch_bounds__(64 * kPromptWaves, RB == 1 ? 2 : 1) void paged_prom
   }
 
   // ---- queries ----
-  int see_lo[RB], see_hi[RB];
-  float sc[RB], m[RB], l[RB];
-  f16x8 q[RB][NK];
-  f32x16 o[RB][NCT];
-  const uint16_t* q_row[RB];
-#pragma unroll
-  for (int rb = 0; rb < RB; ++rb) {
-    const int pair = min(first + (wave * RB + rb) * 32 + r32, pairs - 1);
-    const int i = pair / a.group, place = len - n + i;
-    see_hi[rb] = a.causal ? min(place + 1, len) : len;
-    see_lo[rb] = a.window ? place + 1 - a.window : 0;
-    q_row[rb] = a.q.data + (long)(s.row0 + i) * a.q.token_stride + (long)(h * a.group + pair % a.group) * a.q.head_stride + 8 * hl;
+  const int my_pair = min(first + wave * 32 + r32, pairs - 1), my_row = my_pair / a.group, place = len - n + my_row;
+  const int see_hi = a.causal ? min(place + 1, len) : len, see_lo = a.window ? place + 1 - a.window : 0;
+  const uint16_t* const q_row =
+      a.q.data + (long)(s.row0 + my_row) * a.q.token_stride + (long)(h * a.group + my_pair % a.group) * a.q.head_stride + 8 * hl;
+  float sc = a.scale_log2;
+  f16x8 q[NK];
+  {
     float amax = 0.f;
     u32x4 w[NK];
 #pragma unroll
     for (int k = 0; k < NK; ++k) {
-      w[k] = *reinterpret_cast<const u32x4*>(q_row[rb] + 16 * k);
+      w[k] = *reinterpret_cast<const u32x4*>(q_row + 16 * k);
       if constexpr (__is_same(T, __bf16)) {
         float x[8];
         unpack8<T>(w[k], x);
@@ -73,12 +68,11 @@ __global__ __launch_bounds__(64 * kPromptWaves, RB == 1 ? 2 : 1) void paged_prom
         for (int e = 0; e < 8; ++e) amax = fmaxf(amax, fabsf(x[e]));
       }
     }
-    sc[rb] = a.scale_log2;
     int shift = 0;
     if constexpr (__is_same(T, __bf16)) {
       amax = fmaxf(amax, __shfl_xor(amax, 32));
       shift = fit_shift(amax);
-      sc[rb] = __builtin_ldexpf(sc[rb], -shift);
+      sc = __builtin_ldexpf(sc, -shift);
     }
 #pragma unroll
     for (int k = 0; k < NK; ++k) {
@@ -86,18 +80,18 @@ __global__ __launch_bounds__(64 * kPromptWaves, RB == 1 ? 2 : 1) void paged_prom
         float x[8];
         unpack8<T>(w[k], x);
 #pragma unroll
-        for (int e = 0; e < 8; ++e) q[rb][k][e] = (_Float16)__builtin_ldexpf(x[e], shift);
+        for (int e = 0; e < 8; ++e) q[k][e] = (_Float16)__builtin_ldexpf(x[e], shift);
       } else {
-        q[rb][k] = __builtin_bit_cast(f16x8, w[k]);
+        q[k] = __builtin_bit_cast(f16x8, w[k]);
       }
     }
-    m[rb] = -INFINITY;
-    l[rb] = 0.f;
-#pragma unroll
-    for (int ct = 0; ct < NCT; ++ct)
-#pragma unroll
-      for (int e = 0; e < 16; ++e) o[rb][ct][e] = 0.f;
   }
+  float m = -INFINITY, l = 0.f;
+  f32x16 o[NCT];
+#pragma unroll
+  for (int ct = 0; ct < NCT; ++ct)
+#pragma unroll
+    for (int e = 0; e < 16; ++e) o[ct][e] = 0.f;
 
   // Places of 16-byte pieces in LDS.  Reads: 8 and 16 neighbouring lanes (tokens in score_token's order, or channels) hit different
   // banks.  Writes: the two pieces of a thread's 16 codes lie half a row apart, so 8 neighbouring lanes do as well.
@@ -123,67 +117,56 @@ __global__ __launch_bounds__(64 * kPromptWaves, RB == 1 ? 2 : 1) void paged_prom
 
   // Tile in buffer `buf`, elements of the type of `zero` (f16 of codes, or the rows' own type); `slice(k)` is done after the
   // k-th pair of score products.  p = 2^(s f + add - m); lane: tokens 32 tt + 16 (e / 8) + 8 hl + e % 8.
-  auto work_tile = [&](int buf, int tile, auto zero, const auto& qf, auto scale_of, float add, float inv_sv, auto mask, auto slice) __attribute__((always_inline)) {
+  auto work_tile = [&](int buf, int tile, auto zero, const auto& qf, float f, float add, float inv_sv, auto mask, auto slice) __attribute__((always_inline)) {
     typedef decltype(zero) ex8;
-    f32x16 u[RB][2];
+    f32x16 u[2];
 #pragma unroll
-    for (int rb = 0; rb < RB; ++rb)
-#pragma unroll
-      for (int e = 0; e < 32; ++e) u[rb][e >> 4][e & 15] = 0.f;
+    for (int e = 0; e < 32; ++e) u[e >> 4][e & 15] = 0.f;
     __builtin_amdgcn_s_setprio(1);   // matrix instructions go ahead of the other workgroup's softmax: 526 -> 507 us on 61 G products
 #pragma unroll
     for (int k = 0; k < NK; ++k) {
 #pragma unroll
       for (int tt = 0; tt < 2; ++tt) {
         const ex8 kf = __builtin_bit_cast(ex8, s_k[buf][k_at(32 * tt + score_token(r32), 2 * k + hl)]);
-#pragma unroll
-        for (int rb = 0; rb < RB; ++rb) u[rb][tt] = mma32(kf, qf[rb][k], u[rb][tt]);
+        u[tt] = mma32(kf, qf[k], u[tt]);
       }
       slice(k);
     }
     __builtin_amdgcn_s_setprio(0);
-    float base[RB], f[RB], sum[RB];
+    if constexpr (decltype(mask)::value) {
+      const float poison = f - f;                         // NaN where the block is: for those who see it, not through a masked -inf
+      f = f == f ? f : 1.f;
 #pragma unroll
-    for (int rb = 0; rb < RB; ++rb) {
-      f[rb] = scale_of(rb);
-      if constexpr (decltype(mask)::value) {
-        const float poison = f[rb] - f[rb];               // NaN where the block is: for those who see it, not through a masked -inf
-        f[rb] = f[rb] == f[rb] ? f[rb] : 1.f;
-#pragma unroll
-        for (int e = 0; e < 32; ++e) {
-          const int t = tile * kPagedTile + 32 * (e >> 4) + 16 * (e >> 3 & 1) + 8 * hl + (e & 7);
-          u[rb][e >> 4][e & 15] = t < see_lo[rb] || t >= see_hi[rb] ? -INFINITY : u[rb][e >> 4][e & 15] + poison;
-        }
+      for (int e = 0; e < 32; ++e) {
+        const int t = tile * kPagedTile + 32 * (e >> 4) + 16 * (e >> 3 & 1) + 8 * hl + (e & 7);
+        u[e >> 4][e & 15] = t < see_lo || t >= see_hi ? -INFINITY : u[e >> 4][e & 15] + poison;
       }
-      float top = u[rb][0][0];
-#pragma unroll
-      for (int e = 1; e < 32; ++e) top = fmaxf(top, u[rb][e >> 4][e & 15]);
-      top = __builtin_fmaf(top, f[rb], add);
-      if (__any(top > m[rb] + kLazy)) {
-        top = fmaxf(top, __shfl_xor(top, 32));
-        const float m_new = fmaxf(m[rb], top);
-        const float alpha = m_new == -INFINITY ? 1.f : __builtin_amdgcn_exp2f(m[rb] - m_new);
-        m[rb] = m_new;
-        l[rb] *= alpha;
-#pragma unroll
-        for (int ct = 0; ct < NCT; ++ct) o[rb][ct] *= alpha;
-      }
-      base[rb] = m[rb] == -INFINITY ? add : add - m[rb];
-      sum[rb] = 0.f;
     }
+    float top = u[0][0];
+#pragma unroll
+    for (int e = 1; e < 32; ++e) top = fmaxf(top, u[e >> 4][e & 15]);
+    top = __builtin_fmaf(top, f, add);
+    if (__any(top > m + kLazy)) {
+      top = fmaxf(top, __shfl_xor(top, 32));
+      const float m_new = fmaxf(m, top);
+      const float alpha = m_new == -INFINITY ? 1.f : __builtin_amdgcn_exp2f(m - m_new);
+      m = m_new;
+      l *= alpha;
+#pragma unroll
+      for (int ct = 0; ct < NCT; ++ct) o[ct] *= alpha;
+    }
+    const float base = m == -INFINITY ? add : add - m;
+    float sum = 0.f;
     // Probabilities of 16 tokens (8 a lane) are made between the products of the 16 before them.
-    ex8 p[RB], p_next[RB];
-    auto probabilities = [&](int g, ex8 (&to)[RB]) __attribute__((always_inline)) {
+    ex8 p, p_next;
+    auto probabilities = [&](int g, ex8& to) __attribute__((always_inline)) {
+      float x[8];
 #pragma unroll
-      for (int rb = 0; rb < RB; ++rb) {
-        float x[8];
-#pragma unroll
-        for (int e = 0; e < 8; ++e) {
-          x[e] = __builtin_amdgcn_exp2f(__builtin_fmaf(u[rb][g >> 1][8 * (g & 1) + e], f[rb], base[rb]));
-          to[rb][e] = to_element<ex8>(x[e]);
-        }
-        sum[rb] += ((x[0] + x[1]) + (x[2] + x[3])) + ((x[4] + x[5]) + (x[6] + x[7]));
+      for (int e = 0; e < 8; ++e) {
+        x[e] = __builtin_amdgcn_exp2f(__builtin_fmaf(u[g >> 1][8 * (g & 1) + e], f, base));
+        to[e] = to_element<ex8>(x[e]);
       }
+      sum += ((x[0] + x[1]) + (x[2] + x[3])) + ((x[4] + x[5]) + (x[6] + x[7]));
     };
     probabilities(0, p);
     __builtin_amdgcn_s_setprio(1);   // matrix instructions go ahead of the other workgroup's softmax: 526 -> 507 us on 61 G products
@@ -192,17 +175,14 @@ __global__ __launch_bounds__(64 * kPromptWaves, RB == 1 ? 2 : 1) void paged_prom
 #pragma unroll
       for (int ct = 0; ct < NCT; ++ct) {
         const ex8 vf = __builtin_bit_cast(ex8, s_v[buf][v_at(32 * ct + r32, 2 * g + hl)]);
-#pragma unroll
-        for (int rb = 0; rb < RB; ++rb) o[rb][ct] = mma32(vf, p[rb], o[rb][ct]);
+        o[ct] = mma32(vf, p, o[ct]);
       }
       if (g < 3) {
         probabilities(g + 1, p_next);
-#pragma unroll
-        for (int rb = 0; rb < RB; ++rb) p[rb] = p_next[rb];
+        p = p_next;
       }
     }
-#pragma unroll
-    for (int rb = 0; rb < RB; ++rb) l[rb] = __builtin_fmaf(sum[rb], inv_sv, l[rb]);
+    l = __builtin_fmaf(sum, inv_sv, l);
     __builtin_amdgcn_s_setprio(0);
   };
 
@@ -240,7 +220,7 @@ __global__ __launch_bounds__(64 * kPromptWaves, RB == 1 ? 2 : 1) void paged_prom
         const float f = __builtin_bit_cast(float, __builtin_amdgcn_readlane(__builtin_bit_cast(int, sk), i));
         const float add = __builtin_bit_cast(float, __builtin_amdgcn_readlane(__builtin_bit_cast(int, lsv), i));
         const float inv_sv = __builtin_bit_cast(float, __builtin_amdgcn_readlane(__builtin_bit_cast(int, isv), i));
-        work_tile(i & 1, tile_of(batch0 + i), f16x8{}, q, [&](int rb) { return keep_sign(f * sc[rb]); }, add, inv_sv, mask,
+        work_tile(i & 1, tile_of(batch0 + i), f16x8{}, q, keep_sign(f * sc), add, inv_sv, mask,
                   [&](int k) __attribute__((always_inline)) {
                     store_slice((i + 1) & 1, k);
                     if (k == NK - 1) load_tile(i + 2);
@@ -276,14 +256,11 @@ __global__ __launch_bounds__(64 * kPromptWaves, RB == 1 ? 2 : 1) void paged_prom
       s_v[0][v_at(piece / 8, piece % 8)] = vw;
     }
     __syncthreads();
-    tx8 qt[RB][NK];
+    tx8 qt[NK];
 #pragma unroll
-    for (int rb = 0; rb < RB; ++rb) {
-#pragma unroll
-      for (int k = 0; k < NK; ++k) qt[rb][k] = __builtin_bit_cast(tx8, *reinterpret_cast<const u32x4*>(q_row[rb] + 16 * k));
-    }
+    for (int k = 0; k < NK; ++k) qt[k] = __builtin_bit_cast(tx8, *reinterpret_cast<const u32x4*>(q_row + 16 * k));
     const float f = ok ? keep_sign(a.scale_log2) : __builtin_nanf("");
-    work_tile(0, tile, tx8{}, qt, [&](int) { return f; }, 0.f, 1.f, Masked{}, [](int) {});
+    work_tile(0, tile, tx8{}, qt, f, 0.f, 1.f, Masked{}, [](int) {});
   }
 
   // ---- outputs, or partials for the workgroup that joins the splits ----
@@ -292,31 +269,28 @@ __global__ __launch_bounds__(64 * kPromptWaves, RB == 1 ? 2 : 1) void paged_prom
     return a.out.data + (long)(s.row0 + pair / a.group) * a.out.token_stride + (long)(h * a.group + pair % a.group) * a.out.head_stride;
   };
   const int unit = item * H + h;
+  l += __shfl_xor(l, 32);
+  if (const int col = wave * 32 + r32; first + col >= pairs) {
+    // a row of another tile, or none
+  } else if (a.splits == 1) {
+    const float inv = l == 0.f ? 0.f : 1.f / l;
+    uint16_t* const dst = out_of(col);
 #pragma unroll
-  for (int rb = 0; rb < RB; ++rb) {
-    l[rb] += __shfl_xor(l[rb], 32);
-    const int col = (wave * RB + rb) * 32 + r32;
-    if (first + col >= pairs) continue;
-    if (a.splits == 1) {
-      const float inv = l[rb] == 0.f ? 0.f : 1.f / l[rb];
-      uint16_t* const dst = out_of(col);
+    for (int ct = 0; ct < NCT; ++ct)
 #pragma unroll
-      for (int ct = 0; ct < NCT; ++ct)
+      for (int e = 0; e < 4; ++e)
+        *reinterpret_cast<u32x2*>(dst + 32 * ct + 8 * e + 4 * hl) = u32x2{pack2<T>(o[ct][4 * e] * inv, o[ct][4 * e + 1] * inv),
+                                                                         pack2<T>(o[ct][4 * e + 2] * inv, o[ct][4 * e + 3] * inv)};
+  } else {
+    float* const p = a.partials + ((long)unit * a.splits + split) * (D + 2) * M + col;   // channel by channel: rows lie side by side
 #pragma unroll
-        for (int e = 0; e < 4; ++e)
-          *reinterpret_cast<u32x2*>(dst + 32 * ct + 8 * e + 4 * hl) = u32x2{pack2<T>(o[rb][ct][4 * e] * inv, o[rb][ct][4 * e + 1] * inv),
-                                                                           pack2<T>(o[rb][ct][4 * e + 2] * inv, o[rb][ct][4 * e + 3] * inv)};
-    } else {
-      float* const p = a.partials + ((long)unit * a.splits + split) * (D + 2) * M + col;   // channel by channel: rows lie side by side
+    for (int ct = 0; ct < NCT; ++ct)
 #pragma unroll
-      for (int ct = 0; ct < NCT; ++ct)
-#pragma unroll
-        for (int e = 0; e < 16; ++e)
-          __hip_atomic_store(p + (32 * ct + 8 * (e >> 2) + 4 * hl + (e & 3)) * M, o[rb][ct][e], __ATOMIC_RELAXED, __HIP_MEMORY_SCOPE_AGENT);
-      if (hl == 0) {
-        __hip_atomic_store(p + D * M, m[rb], __ATOMIC_RELAXED, __HIP_MEMORY_SCOPE_AGENT);
-        __hip_atomic_store(p + (D + 1) * M, l[rb], __ATOMIC_RELAXED, __HIP_MEMORY_SCOPE_AGENT);
-      }
+      for (int e = 0; e < 16; ++e)
+        __hip_atomic_store(p + (32 * ct + 8 * (e >> 2) + 4 * hl + (e & 3)) * M, o[ct][e], __ATOMIC_RELAXED, __HIP_MEMORY_SCOPE_AGENT);
+    if (hl == 0) {
+      __hip_atomic_store(p + D * M, m, __ATOMIC_RELAXED, __HIP_MEMORY_SCOPE_AGENT);
+      __hip_atomic_store(p + (D + 1) * M, l, __ATOMIC_RELAXED, __HIP_MEMORY_SCOPE_AGENT);
     }
   }
   if (a.splits == 1 || !last_of_splits(a.counters + unit, a.splits, s_last)) return;
@@ -360,14 +334,13 @@ __global__ __launch_bounds__(64 * kPromptWaves, RB == 1 ? 2 : 1) void paged_prom
   }
 }
 
-constexpr int kPromptBlocks = 1;   // 32-row blocks of a wave
-constexpr int kPromptRows = 32 * kPromptBlocks * kPromptWaves;
+constexpr int kPromptRows = 32 * kPromptWaves;
 
 template <typename T, int D>
 static void launch_prompt(const PagedAttnArgs& a, hipStream_t st) {
   const dim3 grid((unsigned)((long)a.units * a.splits)), block(64 * kPromptWaves);
-  if (a.c.codes == DQ_CODES_E4M3) hipLaunchKernelGGL((paged_prompt_kernel<T, D, true, kPromptBlocks>), grid, block, 0, st, a);
-  else hipLaunchKernelGGL((paged_prompt_kernel<T, D, false, kPromptBlocks>), grid, block, 0, st, a);
+  if (a.c.codes == DQ_CODES_E4M3) hipLaunchKernelGGL((paged_prompt_kernel<T, D, true>), grid, block, 0, st, a);
+  else hipLaunchKernelGGL((paged_prompt_kernel<T, D, false>), grid, block, 0, st, a);
 }
 
 int32_t launch_paged_prompt(const PagedAttnArgs& a, hipStream_t st) {
