@@ -100,6 +100,14 @@ __device__ __forceinline__ bool last_of_splits(int32_t* counter, int splits, int
   return s_last;
 }
 
+// Two neighbouring floats of partial results, at device scope.
+__device__ __forceinline__ void store_pair(float* p, float a, float b) {
+  __hip_atomic_store(reinterpret_cast<uint64_t*>(p), __builtin_bit_cast(uint64_t, f32x2{a, b}), __ATOMIC_RELAXED, __HIP_MEMORY_SCOPE_AGENT);
+}
+__device__ __forceinline__ f32x2 load_pair(const float* p) {
+  return __builtin_bit_cast(f32x2, __hip_atomic_load(reinterpret_cast<const uint64_t*>(p), __ATOMIC_RELAXED, __HIP_MEMORY_SCOPE_AGENT));
+}
+
 struct JoinSpace {   // LDS
   float m[16][kMaxSplits], l[16][kMaxSplits], inv[16];
   int last;
@@ -110,16 +118,22 @@ struct JoinSpace {   // LDS
 template <typename T, int D, typename Out>
 __device__ __forceinline__ void join_splits(int32_t* counter, int ns, const float* base, long step, int cols, JoinSpace& js, Out out_of) {
   if (!last_of_splits(counter, ns, js.last)) return;
-  // Sixteen columns at a time: every (column, split)'s maximum and sum in one round trip, weights to LDS, then the elements,
-  // eight splits of two of them on their way together.
+  // Sixteen columns at a time: every (column, split)'s maximum and sum and a thread's first two elements of eight splits in one
+  // round trip, weights to LDS, then what is left of the elements.
   const int tid = threadIdx.x, threads = blockDim.x;
-  auto load = [](const float* p) __attribute__((always_inline)) { return __hip_atomic_load(p, __ATOMIC_RELAXED, __HIP_MEMORY_SCOPE_AGENT); };
   for (int c0 = 0; c0 < cols; c0 += 16) {
     const int nc = min(16, cols - c0);
+    const float* const from = base + (long)c0 * (D + 2);
+    auto elements = [&](int idx, int s, f32x2 (&u)[8]) __attribute__((always_inline)) {   // (the last split's again behind it)
+#pragma unroll
+      for (int k = 0; k < 8; ++k) u[k] = load_pair(from + min(s + k, ns - 1) * step + idx / D * (D + 2) + idx % D);
+    };
+    f32x2 u[8];
+    if (2 * tid < nc * D) elements(2 * tid, 0, u);
     for (int i = tid; i < nc * ns; i += threads) {
-      const float* p = base + (i % ns) * step + (long)(c0 + i / ns) * (D + 2) + D;
-      js.m[i / ns][i % ns] = load(p);
-      js.l[i / ns][i % ns] = load(p + 1);
+      const f32x2 ml = load_pair(from + (i % ns) * step + (i / ns) * (D + 2) + D);
+      js.m[i / ns][i % ns] = ml.x;
+      js.l[i / ns][i % ns] = ml.y;
     }
     __syncthreads();
     for (int col = tid; col < nc; col += threads) {
@@ -135,25 +149,18 @@ __device__ __forceinline__ void join_splits(int32_t* counter, int ns, const floa
     }
     __syncthreads();
     for (int idx = 2 * tid; idx < nc * D; idx += 2 * threads) {
-      const int col = idx / D, c = idx % D;
-      const float* p = base + (long)(c0 + col) * (D + 2) + c;
+      const int col = idx / D;
       float x = 0.f, y = 0.f;
       for (int s = 0; s < ns; s += 8) {
-        float u[8], v[8];
-#pragma unroll
-        for (int k = 0; k < 8; ++k) {
-          const int at = min(s + k, ns - 1);
-          u[k] = load(p + at * step);
-          v[k] = load(p + at * step + 1);
-        }
+        if (s > 0 || idx >= 2 * threads) elements(idx, s, u);
 #pragma unroll
         for (int k = 0; k < 8; ++k) {
           if (s + k >= ns) break;
-          x = __builtin_fmaf(u[k], js.m[col][s + k], x);
-          y = __builtin_fmaf(v[k], js.m[col][s + k], y);
+          x = __builtin_fmaf(u[k].x, js.m[col][s + k], x);
+          y = __builtin_fmaf(u[k].y, js.m[col][s + k], y);
         }
       }
-      *reinterpret_cast<uint32_t*>(out_of(c0 + col) + c) = pack2<T>(x * js.inv[col], y * js.inv[col]);
+      *reinterpret_cast<uint32_t*>(out_of(c0 + col) + idx % D) = pack2<T>(x * js.inv[col], y * js.inv[col]);
     }
     __syncthreads();
   }

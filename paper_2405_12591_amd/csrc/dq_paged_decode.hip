@@ -289,27 +289,25 @@ __global__ __launch_bounds__(kPagedThreads, 2) void paged_decode_kernel(PagedAtt
   const long part_step = (long)H * kCols * (D + 2);        // from split to split
   float* const parts = a.partials + ((long)sh.first_slot * H + h) * kCols * (D + 2);
   float* const part = parts + sh.split * part_step;
-  for (int idx = tid; idx < cols * D; idx += kPagedThreads) {
+  for (int idx = 2 * tid; idx < cols * D; idx += 2 * kPagedThreads) {
     const int cc = idx / D, ch = idx % D;
     const float M = fmaxf(fmaxf(s_m[0][cc], s_m[1][cc]), fmaxf(s_m[2][cc], s_m[3][cc]));
     const float base = M == -INFINITY ? 0.f : M;
-    float oo = 0.f, ll = 0.f;
+    float x = 0.f, y = 0.f, ll = 0.f;
 #pragma unroll
     for (int w = 0; w < 4; ++w) {
       const float f = __builtin_amdgcn_exp2f(s_m[w][cc] - base);
-      oo = __builtin_fmaf(s_o[w][cc][ch], f, oo);
+      x = __builtin_fmaf(s_o[w][cc][ch], f, x);
+      y = __builtin_fmaf(s_o[w][cc][ch + 1], f, y);
       ll = __builtin_fmaf(s_l[w][cc], f, ll);
     }
     if (splits == 1) {
-      const T y = (T)(ll == 0.f ? 0.f : oo / ll);
-      out_of(cc)[ch] = __builtin_bit_cast(uint16_t, y);
+      const float inv = ll == 0.f ? 0.f : 1.f / ll;
+      *reinterpret_cast<uint32_t*>(out_of(cc) + ch) = pack2<T>(x * inv, y * inv);
     } else {
       float* const p = part + (long)cc * (D + 2);
-      __hip_atomic_store(p + ch, oo, __ATOMIC_RELAXED, __HIP_MEMORY_SCOPE_AGENT);
-      if (ch == 0) {
-        __hip_atomic_store(p + D, M, __ATOMIC_RELAXED, __HIP_MEMORY_SCOPE_AGENT);
-        __hip_atomic_store(p + D + 1, ll, __ATOMIC_RELAXED, __HIP_MEMORY_SCOPE_AGENT);
-      }
+      store_pair(p + ch, x, y);
+      if (ch == 0) store_pair(p + D, M, ll);
     }
   }
   if (splits > 1) join_splits<T, D>(a.counters + unit, splits, parts, part_step, cols, s_join, out_of);
