@@ -275,9 +275,9 @@ __device__ __forceinline__ void load_unit(u32x4 (&v)[2], const uint16_t* p, cons
   v[0] = *reinterpret_cast<const u32x4*>(p + l.at0);
   v[1] = *reinterpret_cast<const u32x4*>(p + l.at1);
 }
-__device__ __forceinline__ void store_unit(uint16_t* p, const RowLayout& l, const u32x4 (&v)[2]) {
-  *reinterpret_cast<u32x4*>(p + l.at0) = v[0];
-  *reinterpret_cast<u32x4*>(p + l.at1) = v[1];
+__device__ __forceinline__ void store_unit(uint16_t* p, const RowLayout& l, const u32x4 (&v)[2]) {   // rows that this kernel does not read again
+  __builtin_nontemporal_store(v[0], reinterpret_cast<u32x4*>(p + l.at0));
+  __builtin_nontemporal_store(v[1], reinterpret_cast<u32x4*>(p + l.at1));
 }
 
 // Heads [h0, h1) of one token's row: the thread is the row's unit of LANES.  v: the first head's pieces, asked for ahead.

@@ -37,7 +37,10 @@ __device__ __forceinline__ uint32_t larger_of_lanes(uint32_t x) {
 // rotation, and 8 channels of two neighbouring value rows, as the value layout wants them.  The angles of a key row's
 // unit are formed once and kept for all heads of the group.
 // Reads 4 bytes and writes 2 per cached element pair (k, v); about 40 flops an element.  Bound by memory where
-// prompts are long, by latency for a generated token (its page is read only when it fills).
+// prompts are long: 28.6 thousand tokens of 32 heads of 128 channels, pages of 128, 190 us, 3.7 TB/s (its workgroups of 16 waves
+// wait at two barriers a head, one a compute unit), and 272 us with 32 query heads, 4.3 TB/s.  By latency for a generated token
+// (its page is read only when it fills): 7 us for 16 sequences.  By both in between: of the 24 us for 7 thousand rows
+// of 8 heads 10 are vector instructions, most of them angles, which few rows share with few heads.
 template <typename T, int D, int P, bool FP8, bool INTERLEAVED>
 __global__ __launch_bounds__(P * D / 16, 4) void paged_append_kernel(AppendArgs a) {
   constexpr int THREADS = P * D / 16, LPR = D / 16, RP = P, WAVES = THREADS / 64;
@@ -303,17 +306,20 @@ struct ReadArgs {
   dq_heads k, v;
 };
 
-// One workgroup per (page, kv head).  Reads one byte and writes two per element.
+// One workgroup per (page, kv head), a page's heads neighbours in the grid: its rows are written by workgroups that run together.
+// Reads one byte and writes two per element, 16 neighbouring bytes a lane, past the caches' own order.  Bound by memory: 28.6
+// thousand tokens of 32 heads of 128 channels, 710 MB, 145 us, 4.9 TB/s (150 with the heads far apart, 190 with 32 bytes a lane in two stores).
 template <typename T, int D, int P, bool FP8>
 __global__ __launch_bounds__(kPagedThreads) void paged_read_kernel(ReadArgs a) {
-  constexpr int LPR = D / 16, RP = kPagedThreads / LPR, PASSES = P / RP;
+  constexpr int LPR = D / 8, RP = kPagedThreads / LPR, PASSES = P / RP;
   constexpr int RS = D / 2 + 1;                           // words of a token's row in LDS, an odd number
   __shared__ uint32_t s_v[64 * RS];
-  const int tid = threadIdx.x, h = blockIdx.y;
-  const int b = item_owner(a.out_starts, a.bt.rows, a.bt.batch, (int)blockIdx.x, 1, P, 2);
+  const int tid = threadIdx.x;
+  const int h = (int)(blockIdx.x % (unsigned)a.c.kv_heads), item = (int)(blockIdx.x / (unsigned)a.c.kv_heads);
+  const int b = item_owner(a.out_starts, a.bt.rows, a.bt.batch, item, 1, P, 2);
   const int len = min(max(a.bt.seq_lens[b], 0), a.bt.table_width * P);
   const int first = a.first ? max(a.first[b], 0) : 0;
-  const int page = first / P + (int)blockIdx.x - item_first(a.out_starts, a.bt.rows, b, 1, P, 2);
+  const int page = first / P + item - item_first(a.out_starts, a.bt.rows, b, 1, P, 2);
   const int base = page * P;
   if (first >= len || page < first / P || page > (len - 1) / P) return;
   const long out0 = (long)a.out_starts[b] - first;        // row of token 0
@@ -332,21 +338,19 @@ __global__ __launch_bounds__(kPagedThreads) void paged_read_kernel(ReadArgs a) {
   for (int i = 0; i < PASSES; ++i) {
     const int r = i * RP + tid / LPR;
     if (!live(r)) continue;
-    float x[16];
+    float x[8];
+    const long at = block * P * D + (long)r * D + 8 * unit;
     if (full) {
-      const u32x4 w = *reinterpret_cast<const u32x4*>(a.c.k_codes + block * P * D + (long)r * D + 16 * unit);
-#pragma unroll
-      for (int j = 0; j < 4; ++j) values4<FP8>(w[j], x + 4 * j);
+      const u32x2 w = *reinterpret_cast<const u32x2*>(a.c.k_codes + at);
+      values4<FP8>(w.x, x);
+      values4<FP8>(w.y, x + 4);
     } else {
-      const uint16_t* src = a.c.k_tail + block * P * D + (long)r * D + 16 * unit;
-      unpack8<T>(*reinterpret_cast<const u32x4*>(src), x);
-      unpack8<T>(*reinterpret_cast<const u32x4*>(src + 8), x + 8);
+      unpack8<T>(*reinterpret_cast<const u32x4*>(a.c.k_tail + at), x);
     }
 #pragma unroll
-    for (int j = 0; j < 16; ++j) x[j] *= ks;
-    uint16_t* dst = a.k.data + (out0 + base + r) * a.k.token_stride + h * a.k.head_stride + 16 * unit;
-    *reinterpret_cast<u32x4*>(dst) = pack8<T>(x);
-    *reinterpret_cast<u32x4*>(dst + 8) = pack8<T>(x + 8);
+    for (int j = 0; j < 8; ++j) x[j] *= ks;
+    u32x4* const dst = reinterpret_cast<u32x4*>(a.k.data + (out0 + base + r) * a.k.token_stride + h * a.k.head_stride + 8 * unit);
+    __builtin_nontemporal_store(pack8<T>(x), dst);
   }
   // values: a thread takes two channels of four tokens and leaves a word (both channels) per token
   for (int run = 0; run < P / 64; ++run) {
@@ -375,8 +379,8 @@ __global__ __launch_bounds__(kPagedThreads) void paged_read_kernel(ReadArgs a) {
       const int piece = i * kPagedThreads + tid, r = piece / (D / 8), c8 = piece % (D / 8);
       if (!live(run * 64 + r)) continue;
       const uint32_t* src = s_v + r * RS + 4 * c8;
-      *reinterpret_cast<u32x4*>(a.v.data + (out0 + base + run * 64 + r) * a.v.token_stride + h * a.v.head_stride + 8 * c8) =
-          u32x4{src[0], src[1], src[2], src[3]};
+      uint16_t* const dst = a.v.data + (out0 + base + run * 64 + r) * a.v.token_stride + h * a.v.head_stride + 8 * c8;
+      __builtin_nontemporal_store(u32x4{src[0], src[1], src[2], src[3]}, reinterpret_cast<u32x4*>(dst));
     }
   }
 }
@@ -447,12 +451,11 @@ extern "C" int32_t dq_paged_read(const dq_paged_cache* cache, const dq_paged_bat
                                  const dq_heads* k_out, const dq_heads* v_out, void* hip_stream) {
   if (!paged_cache_ok(cache) || !paged_batch_ok(batch, cache, false) || !out_starts) return DQ_EINVAL;
   if (!heads_ok(k_out, false) || !heads_ok(v_out, false) || k_out->heads != cache->kv_heads || v_out->heads != cache->kv_heads) return DQ_EINVAL;
-  if (cache->kv_heads > kMaxGridY) return DQ_EINVAL;
   if (batch->rows == 0) return DQ_OK;
   ReadArgs a = {*cache, *batch, first, out_starts, *k_out, *v_out};
   const long items = batch->rows / cache->page_tokens + 2l * batch->batch;
-  if (items * kPagedThreads >= kMaxThreads) return DQ_EINVAL;
-  for_format<LaunchRead>(cache, a, dim3((unsigned)items, (unsigned)cache->kv_heads), (hipStream_t)hip_stream);
+  if (items * cache->kv_heads >= kMaxThreads / kPagedThreads) return DQ_EINVAL;
+  for_format<LaunchRead>(cache, a, dim3((unsigned)(items * cache->kv_heads)), (hipStream_t)hip_stream);
   DQ_HIP_CHECK(hipGetLastError());
   return DQ_OK;
 }

@@ -9,19 +9,24 @@ struct RotateArgs {
   dq_head_norm norm;
   dq_rotary rot;                 // rot_dim == 0: none
   int heads_per_group;           // heads one workgroup takes of its rows, queries and keys counted through
+  int head_groups;
 };
 
 // A thread keeps one unit (16 channels) of one token for all heads of its group, so the eight angles of the unit are
-// formed once and turn every head.  Bound by memory: 2 bytes in and 2 out per element against about 7 flops.
+// formed once and turn every head.  Bound by memory: 2 bytes in and 2 out per element against about 7 flops.  A token's
+// groups of heads are neighbours in the grid, so that its row is read and written by workgroups that run together, and the
+// results are stored past the caches' own order (`store_unit`): 16384 tokens of 40 heads of 128 channels with norm and three axes,
+// 336 MB, 66 us (5.1 TB/s, as a copy of that size); 71 with the groups far apart, 69 with plain stores, 75 with both.
 template <typename T, int LANES, bool INTERLEAVED>
 __global__ __launch_bounds__(kPagedThreads) void rotate_heads_kernel(RotateArgs a) {
   const int unit = threadIdx.x % LANES;
-  const long column = (long)blockIdx.x * (kPagedThreads / LANES) + threadIdx.x / LANES;
+  const int group = (int)(blockIdx.x % (unsigned)a.head_groups);
+  const long column = (long)(blockIdx.x / (unsigned)a.head_groups) * (kPagedThreads / LANES) + threadIdx.x / LANES;
   const bool live = column < (long)a.batch * a.tokens && 16 * unit < a.head_dim;
   const int b = live && a.batch > 1 ? (int)(column / a.tokens) : 0;
   const long t = live ? column - (long)b * a.tokens : 0;
   const RowLayout l = row_layout(unit, a.rot.rot_dim, INTERLEAVED);
-  const int h0 = blockIdx.y * a.heads_per_group, h1 = min(h0 + a.heads_per_group, a.q.heads + a.k.heads);
+  const int h0 = group * a.heads_per_group, h1 = min(h0 + a.heads_per_group, a.q.heads + a.k.heads);
   const uint16_t* const q = a.q.data + b * a.q.batch_stride + t * a.q.token_stride;
   const uint16_t* const k = a.k.data + b * a.k.batch_stride + t * a.k.token_stride;
   const int k0 = max(h0 - a.q.heads, 0);
@@ -85,12 +90,13 @@ extern "C" int32_t dq_rotate_heads(const dq_heads* q, const dq_heads* q_out, con
   while (16 * lanes < head_dim) lanes *= 2;
   const long groups = (rows + kPagedThreads / lanes - 1) / (kPagedThreads / lanes);
   const int heads = a.q.heads + a.k.heads;
-  if (heads > kMaxGridY || groups * kPagedThreads >= kMaxThreads) return DQ_EINVAL;
   // Heads a workgroup takes: eight share the angles where the rows alone fill the chip, fewer where they do not.
   int per = 8;
   while (per > 1 && groups * ((heads + per - 1) / per) < 1024) per /= 2;
   a.heads_per_group = per;
-  const dim3 grid((unsigned)groups, (unsigned)((heads + per - 1) / per));
+  a.head_groups = (heads + per - 1) / per;
+  if (groups * a.head_groups >= kMaxThreads / kPagedThreads) return DQ_EINVAL;
+  const dim3 grid((unsigned)(groups * a.head_groups));
   if (dtype == DQ_BF16) launch_rotate<__bf16>(a, lanes, grid, (hipStream_t)hip_stream);
   else launch_rotate<_Float16>(a, lanes, grid, (hipStream_t)hip_stream);
   DQ_HIP_CHECK(hipGetLastError());
