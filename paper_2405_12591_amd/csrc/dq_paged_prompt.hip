@@ -7,13 +7,11 @@ namespace dq {
 constexpr int kPromptWaves = 4;
 constexpr int kPromptSplits = 32;   // at most, of a tile of rows (their weights fit LDS)
 
-// Token of row r of a transposed 32-token score product: chosen so that a lane's 16 scores are tokens 8 h .. 8 h + 7 and
-// 16 + 8 h .. of the 32 (h = lane / 32), the right operand that the product with the values wants.
-__device__ __forceinline__ int score_token(int r) { return 16 * (r >> 4) + 8 * ((r >> 2) & 1) + 4 * ((r >> 3) & 1) + (r & 3); }
-
+// Rows of a transposed 32-token score product stand for tokens with bits 2 and 3 of their place exchanged: a lane's 16 scores are
+// then tokens 8 h .. 8 h + 7 and 16 + 8 h .. of the 32 (h = lane / 32), the right operand that the product with the values wants.
 // One workgroup of four waves per (tile of rows, kv head, split): 32 (row, query head) pairs a wave.  The tile's
-// codes are turned to f16 once and shared through LDS (two buffers of 64 tokens, pieces of 16 bytes swizzled so that 16
-// neighbouring lanes touch all banks); keys as [token][channel], values as [channel][token], as they are stored.
+// codes are turned to f16 once and shared through LDS (two buffers of 64 tokens); keys as [token][channel], values as
+// [channel][token], as they are stored.
 // Scores are formed transposed, as in the decode kernel: probabilities go from the first product's result registers to
 // the second's operand registers without leaving the lane.
 //
@@ -25,8 +23,9 @@ template <typename T, int D, bool FP8>
 __global__ __launch_bounds__(64 * kPromptWaves, 2) void paged_prompt_kernel(PagedAttnArgs a) {
   constexpr int NK = D / 16, NCT = D / 32, NB = D / 64, M = 32 * kPromptWaves;
   constexpr int THREADS = 64 * kPromptWaves;
+  constexpr int KP = D / 8 + 1, VP = 9;                   // 16-byte pieces of a key row and of a channel's run in LDS
   typedef typename Vec8<T>::type tx8;
-  __shared__ __align__(16) u32x4 s_k[2][64 * D / 8], s_v[2][64 * D / 8];
+  __shared__ __align__(16) u32x4 s_k[2][64 * KP], s_v[2][D * VP];
   __shared__ int s_last;
   const int tid = threadIdx.x, lane = tid & 63, wave = tid >> 6, r32 = lane & 31, hl = lane >> 5;
   const int H = a.c.kv_heads, P = a.c.page_tokens;
@@ -98,13 +97,11 @@ __global__ __launch_bounds__(64 * kPromptWaves, 2) void paged_prompt_kernel(Page
 #pragma unroll
     for (int e = 0; e < 16; ++e) o[ct][e] = 0.f;
 
-  // Places of 16-byte pieces in LDS.  Reads: 8 and 16 neighbouring lanes (tokens in score_token's order, or channels) hit different
-  // banks.  Writes: the two pieces of a thread's 16 codes lie half a row apart, so 8 neighbouring lanes do as well.
-  auto k_at = [&](int token, int piece) {
-    const int key = (token & 3) | (token >> 3 & 1) << 2 | (token >> 2 & 1) << 3;
-    return D == 128 ? token * 16 + ((piece >> 1 | (piece & 1) << 3) ^ key) : token * 8 + (piece ^ (key & 7) ^ (key >> 3));
-  };
-  auto v_at = [&](int ch, int piece) { return ch * 8 + (piece ^ (ch & 7) ^ (ch >> 3 & 1)); };
+  // Places of 16-byte pieces in LDS: rows an odd number of pieces apart, so that neighbouring lanes, which read the same piece of
+  // neighbouring rows, touch all banks, and what a lane reads lies at fixed offsets from one address.  Keys lie in the order of the
+  // score product's rows (above).
+  auto k_at = [&](int token, int piece) { return ((token & ~12) | (token & 4) << 1 | (token & 8) >> 1) * KP + piece; };
+  auto v_at = [&](int ch, int piece) { return ch * VP + piece; };
 
   // ---- a tile of 64 tokens ----
   // Codes of the tile after it, on their way from memory to LDS; slice k of NK is turned to f16 between the matrix
@@ -124,6 +121,8 @@ __global__ __launch_bounds__(64 * kPromptWaves, 2) void paged_prompt_kernel(Page
   // k-th pair of score products.  p = 2^(s f + add - m); lane: tokens 32 tt + 16 (e / 8) + 8 hl + e % 8.
   auto work_tile = [&](int buf, int tile, auto zero, const auto& qf, float f, float add, float inv_sv, auto mask, auto slice) __attribute__((always_inline)) {
     typedef decltype(zero) ex8;
+    const u32x4* const k_from = s_k[buf] + r32 * KP + hl;   // row r32 of the first 32
+    const u32x4* const v_from = s_v[buf] + r32 * VP + hl;
     f32x16 u[2];
 #pragma unroll
     for (int e = 0; e < 32; ++e) u[e >> 4][e & 15] = 0.f;
@@ -132,7 +131,7 @@ __global__ __launch_bounds__(64 * kPromptWaves, 2) void paged_prompt_kernel(Page
     for (int k = 0; k < NK; ++k) {
 #pragma unroll
       for (int tt = 0; tt < 2; ++tt) {
-        const ex8 kf = __builtin_bit_cast(ex8, s_k[buf][k_at(32 * tt + score_token(r32), 2 * k + hl)]);
+        const ex8 kf = __builtin_bit_cast(ex8, k_from[32 * tt * KP + 2 * k]);
         u[tt] = mma32(kf, qf[k], u[tt]);
       }
       slice(k);
@@ -179,7 +178,7 @@ __global__ __launch_bounds__(64 * kPromptWaves, 2) void paged_prompt_kernel(Page
     for (int g = 0; g < 4; ++g) {
 #pragma unroll
       for (int ct = 0; ct < NCT; ++ct) {
-        const ex8 vf = __builtin_bit_cast(ex8, s_v[buf][v_at(32 * ct + r32, 2 * g + hl)]);
+        const ex8 vf = __builtin_bit_cast(ex8, v_from[32 * ct * VP + 2 * g]);
         o[ct] = mma32(vf, p, o[ct]);
       }
       if (g < 3) {
