@@ -16,9 +16,11 @@ constexpr int kPromptSplits = 32;   // at most, of a tile of rows (their weights
 // the second's operand registers without leaving the lane.
 //
 // Bound by the matrix instructions and what shares their waves: 4 x 32 query heads, prompts of 3500 to 4096 tokens of 128 channels,
-// 485 GFLOP within the mask, 515 us, 940 TFLOP/s, against 1100 of a large f16 matrix product; two pieces of 400 to
-// 512 rows behind 15 thousand tokens, 246 GFLOP, 255 us.  64 rows a wave (one workgroup a compute unit) took 693 us for 526, three
-// workgroups a compute unit with one buffer spilled (660), codes stored to LDS after the second product 535.
+// 485 GFLOP within the mask, 515 us, 940 TFLOP/s, against 1100 of a large f16 matrix product (1200 to 1350 of nothing but matrix
+// instructions with as many vector instructions as here between them, in registers); matrix units are busy 44 % of the cycles, LDS 40 %.
+// Two pieces of 400 to 512 rows behind 15 thousand tokens, 246 GFLOP, 255 us.  64 rows a wave (one workgroup a compute unit) took
+// 693 us for 526, three workgroups a compute unit with one buffer spilled (660), codes stored to LDS after the second product 535;
+// scores a tile ahead, between the exponentials of the tile before, made prompts no faster (515) and pieces slower (275).
 template <typename T, int D, bool FP8>
 __global__ __launch_bounds__(64 * kPromptWaves, 2) void paged_prompt_kernel(PagedAttnArgs a) {
   constexpr int NK = D / 16, NCT = D / 32, NB = D / 64, M = 32 * kPromptWaves;
