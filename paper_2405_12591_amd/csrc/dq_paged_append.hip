@@ -431,9 +431,12 @@ extern "C" int32_t dq_paged_append(const dq_paged_cache* cache, const dq_paged_b
   const int rows_per_block = cache->page_tokens;
   const long items = batch->rows / cache->page_tokens + 2l * batch->batch;
   const long q_items = q ? (batch->rows + rows_per_block - 1) / rows_per_block : 0;
-  // Heads that share a page's angles: four where the pages alone fill the chip.
+  // Heads that share a page's angles: four where pages alone take the place of every resident workgroup (16 waves a compute
+  // unit), fewer where they do not.  Pages of 128, 128 channels: 4096 tokens of 32 heads 26 us (34 with two heads a workgroup), 28
+  // thousand of 8 heads 53 (63 with one).  Eight: 3 % faster with query rows beside large pages, up to 10 % slower on pages of 64.
+  const int resident = (1 << 18) / (cache->page_tokens * cache->head_dim / 16);
   int per = 4, q_per = 8;
-  while (per > 1 && items * ((cache->kv_heads + per - 1) / per) < 1024) per /= 2;
+  while (per > 1 && items * ((cache->kv_heads + per - 1) / per) < resident) per /= 2;
   while (q && q_per > 1 && q_items * ((q->heads + q_per - 1) / q_per) < 1024) q_per /= 2;
   a.heads_per_group = per;
   a.head_groups = (cache->kv_heads + per - 1) / per;
