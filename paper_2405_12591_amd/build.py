@@ -1,4 +1,4 @@
-"""Build libdecoquant.so in-tree with hipcc for gfx950."""
+"""Build libdecoquant.so in-tree with hipcc for gfx950, and the compiled part of the binding (_paged.so) with g++."""
 from __future__ import annotations
 
 import glob
@@ -10,6 +10,7 @@ import subprocess
 PKG_DIR = os.path.dirname(os.path.abspath(__file__))
 ROOT = os.path.dirname(PKG_DIR)
 LIB_PATH = os.path.join(PKG_DIR, "libdecoquant.so")
+BIND_PATH = os.path.join(PKG_DIR, "_paged.so")
 # registers, scratch and LDS of every kernel of the last build, as the compiler reported them
 RESOURCES_PATH = os.path.join(PKG_DIR, "_build", "kernel_resources.json")
 
@@ -99,6 +100,25 @@ def build_library(verbose: bool = False, timeline: bool = False) -> str:
     return out_path
 
 
+def build_binding() -> str:
+    """Compile csrc/paged_bind.cpp, the tensor checks of paged.py, as the Python module _paged."""
+    import importlib.util
+    import sysconfig
+    torch_dir = importlib.util.find_spec("torch").submodule_search_locations[0]
+    inc, libs = os.path.join(torch_dir, "include"), os.path.join(torch_dir, "lib")
+    rc, log = _run([os.environ.get("CXX", "g++"), "-O2", "-std=c++17", "-fPIC", "-shared", "-fvisibility=hidden",
+                    *("-I" + p for p in (os.path.join(ROOT, "include"), inc, os.path.join(inc, "torch", "csrc", "api", "include"),
+                                         sysconfig.get_paths()["include"])),
+                    os.path.join(PKG_DIR, "csrc", "paged_bind.cpp"), "-L" + libs, "-ltorch_python", "-ltorch_cpu", "-ltorch", "-lc10",
+                    "-o", BIND_PATH + ".tmp"])
+    if rc != 0:
+        raise RuntimeError("the binding's compiled part does not build:\n" + log)
+    os.replace(BIND_PATH + ".tmp", BIND_PATH)
+    return BIND_PATH
+
+
 if __name__ == "__main__":
     import sys
     print(build_library(verbose=True, timeline="--timeline" in sys.argv))
+    if "--timeline" not in sys.argv:
+        print(build_binding())

@@ -1,11 +1,17 @@
 """What the entry points of the head rotation and the paged cache refuse before anything is launched: the C ABI
 with pointers that are never followed, and the binding's checks.  No GPU needed."""
 import ctypes as C
+import struct
 
 import pytest
 import torch
 
 PTR = 0x1000      # never dereferenced: the checks come first
+# the header's small structs
+_pack_heads = struct.Struct("@Pqqqi4x").pack
+_pack_norm = struct.Struct("@PPf4x").pack
+_pack_rotary = struct.Struct("@PPPqiii4x").pack
+_pack_batch = struct.Struct("@PPPPiiii").pack
 
 
 def _lib():
@@ -15,7 +21,7 @@ def _lib():
 
 
 def _heads(paged, data=PTR, heads=8, strides=(0, 1024, 128)):
-    return paged._pack_heads(data, *strides, heads)
+    return _pack_heads(data, *strides, heads)
 
 
 def _cache(paged, **change):
@@ -26,12 +32,12 @@ def _cache(paged, **change):
 
 
 def _batch(paged, starts=PTR, lens=PTR, table=PTR, slots=0, batch=4, rows=4, width=5, stride=5):
-    return paged._pack_batch(starts, lens, table, slots, batch, rows, width, stride)
+    return _pack_batch(starts, lens, table, slots, batch, rows, width, stride)
 
 
 def test_rotate_heads_refuses():
     dq, paged = _lib()
-    norm, rot = paged._pack_norm(PTR, PTR, 1e-6), paged._pack_rotary(PTR, PTR, 0, 4, 1, 128, 0)
+    norm, rot = _pack_norm(PTR, PTR, 1e-6), _pack_rotary(PTR, PTR, 0, 4, 1, 128, 0)
 
     def call(q=None, q_out=None, k=None, k_out=None, batch=1, tokens=0, d=128, dtype=0, norm=norm, rot=rot):
         return dq.lib.dq_rotate_heads(q, q_out, k, k_out, batch, tokens, d, dtype, norm, rot, None)
@@ -49,10 +55,10 @@ def test_rotate_heads_refuses():
         assert call(h, h, **bad) == -1, bad
     for r in ((0, PTR, 0, 4, 1, 128, 0), (PTR, 0, 0, 4, 1, 128, 0), (PTR, PTR, 0, 4, 1, 120, 0), (PTR, PTR, 0, 4, 1, 144, 0), (PTR, PTR, 0, 4, 1, 0, 0),
               (PTR, PTR, 0, 4, 0, 128, 0), (PTR, PTR, PTR, 4, 9, 128, 0), (PTR, PTR, 0, 4, 2, 128, 0), (PTR, PTR, 0, 4, 1, 128, 2)):
-        assert call(h, h, rot=paged._pack_rotary(*r)) == -1, r
-    assert call(h, h, tokens=5, rot=paged._pack_rotary(PTR, PTR, PTR, 4, 2, 128, 0)) == -1        # fewer positions than rows
+        assert call(h, h, rot=_pack_rotary(*r)) == -1, r
+    assert call(h, h, tokens=5, rot=_pack_rotary(PTR, PTR, PTR, 4, 2, 128, 0)) == -1        # fewer positions than rows
     for n in ((PTR + 2, 0, 1e-6), (0, PTR + 8, 1e-6), (PTR, 0, -1.0), (PTR, 0, float("nan"))):
-        assert call(h, h, norm=paged._pack_norm(*n)) == -1, n
+        assert call(h, h, norm=_pack_norm(*n)) == -1, n
 
 
 BAD_CACHES = [dict(k_codes=0), dict(v_scales=0), dict(k_tail=0), dict(v_tail=PTR + 8), dict(k_codes=PTR + 4), dict(k_scales=PTR + 2), dict(pages=0),
@@ -79,9 +85,9 @@ def test_paged_append_and_read_refuse():
     assert append(k=None) == -1 and append(v=None) == -1 and append(k=_heads(paged, heads=4)) == -1 and append(v=q) == -1
     assert append(q=q) == -1 and append(q_out=q) == -1 and append(q=q, q_out=h) == -1
     assert append(k=_heads(paged, data=PTR + 2)) == -1 and append(v=_heads(paged, strides=(0, 1, 128))) == -1
-    assert append(rot=paged._pack_rotary(PTR, 0, 0, 4, 1, 144, 0)) == -1 and append(norm=paged._pack_norm(PTR + 1, 0, 1e-6)) == -1
-    assert append(rot=paged._pack_rotary(PTR, 0, PTR, 4, 3, 128, 0)) == -1                 # several axes need positions
-    assert append(rot=paged._pack_rotary(PTR, 0, 0, 4, 1, 128, 0)) == 0                    # one may do without
+    assert append(rot=_pack_rotary(PTR, 0, 0, 4, 1, 144, 0)) == -1 and append(norm=_pack_norm(PTR + 1, 0, 1e-6)) == -1
+    assert append(rot=_pack_rotary(PTR, 0, PTR, 4, 3, 128, 0)) == -1                 # several axes need positions
+    assert append(rot=_pack_rotary(PTR, 0, 0, 4, 1, 128, 0)) == 0                    # one may do without
     assert lib.dq_paged_append(None, _batch(paged), h, h, None, None, None, None, None) == -1
     assert lib.dq_paged_append(_cache(paged), None, h, h, None, None, None, None, None) == -1
 
