@@ -308,10 +308,11 @@ struct ReadArgs {
 
 // One workgroup per (page, kv head), a page's heads neighbours in the grid: its rows are written by workgroups that run together.
 // Reads one byte and writes two per element, 16 neighbouring bytes a lane, past the caches' own order.  Bound by memory: 28.6
-// thousand tokens of 32 heads of 128 channels, 710 MB, 145 us, 4.9 TB/s (150 with the heads far apart, 190 with 32 bytes a lane in two stores).
+// thousand tokens of 32 heads of 128 channels, 710 MB, 139 us, 5.1 TB/s (145 with the values asked for behind the keys, 150 with the heads
+// far apart as well, 190 with 32 bytes a lane in two stores).
 template <typename T, int D, int P, bool FP8>
 __global__ __launch_bounds__(kPagedThreads) void paged_read_kernel(ReadArgs a) {
-  constexpr int LPR = D / 8, RP = kPagedThreads / LPR, PASSES = P / RP;
+  constexpr int LPR = D / 8, RP = kPagedThreads / LPR, PASSES = P / RP, VP = D / 2 * 16 / kPagedThreads;
   constexpr int RS = D / 2 + 1;                           // words of a token's row in LDS, an odd number
   __shared__ uint32_t s_v[64 * RS];
   const int tid = threadIdx.x;
@@ -334,41 +335,68 @@ __global__ __launch_bounds__(kPagedThreads) void paged_read_kernel(ReadArgs a) {
   const int lo = max(first - base, 0), hi = min(len - base, P);
   const int unit = tid % LPR;
   auto live = [&](int r) { const long at = out0 + base + r; return r >= lo && r < hi && at >= 0 && at < row_end; };
+  // keys and the first run of values are asked for together
+  u32x4 kw[PASSES] = {};
+  u32x2 vw[VP][2];
+  auto load_v = [&](int run) __attribute__((always_inline)) {
+#pragma unroll
+    for (int i = 0; i < VP; ++i) {
+      const int piece = i * kPagedThreads + tid;
+      const long at = block * P * D + (long)run * 64 * D + 2 * (piece / 16) * 64 + 4 * (piece % 16);
+#pragma unroll
+      for (int j = 0; j < 2; ++j) {
+        if (full) vw[i][j].x = *reinterpret_cast<const uint32_t*>(a.c.v_codes + at + 64 * j);
+        else vw[i][j] = *reinterpret_cast<const u32x2*>(a.c.v_tail + at + 64 * j);
+      }
+    }
+  };
+#pragma unroll
+  for (int i = 0; i < PASSES; ++i) {
+    const int r = i * RP + tid / LPR;
+    const long at = block * P * D + (long)r * D + 8 * unit;
+    if (!live(r)) continue;
+    if (full) {
+      const u32x2 w = *reinterpret_cast<const u32x2*>(a.c.k_codes + at);
+      kw[i].x = w.x;
+      kw[i].y = w.y;
+    } else {
+      kw[i] = *reinterpret_cast<const u32x4*>(a.c.k_tail + at);
+    }
+  }
+  load_v(0);
 #pragma unroll
   for (int i = 0; i < PASSES; ++i) {
     const int r = i * RP + tid / LPR;
     if (!live(r)) continue;
     float x[8];
-    const long at = block * P * D + (long)r * D + 8 * unit;
     if (full) {
-      const u32x2 w = *reinterpret_cast<const u32x2*>(a.c.k_codes + at);
-      values4<FP8>(w.x, x);
-      values4<FP8>(w.y, x + 4);
+      values4<FP8>(kw[i].x, x);
+      values4<FP8>(kw[i].y, x + 4);
     } else {
-      unpack8<T>(*reinterpret_cast<const u32x4*>(a.c.k_tail + at), x);
+      unpack8<T>(kw[i], x);
     }
 #pragma unroll
     for (int j = 0; j < 8; ++j) x[j] *= ks;
-    u32x4* const dst = reinterpret_cast<u32x4*>(a.k.data + (out0 + base + r) * a.k.token_stride + h * a.k.head_stride + 8 * unit);
-    __builtin_nontemporal_store(pack8<T>(x), dst);
+    __builtin_nontemporal_store(pack8<T>(x), reinterpret_cast<u32x4*>(a.k.data + (out0 + base + r) * a.k.token_stride + h * a.k.head_stride + 8 * unit));
   }
   // values: a thread takes two channels of four tokens and leaves a word (both channels) per token
   for (int run = 0; run < P / 64; ++run) {
-    if (run) __syncthreads();
+    if (run) {
+      __syncthreads();
+      load_v(run);
+    }
 #pragma unroll
-    for (int i = 0; i < D / 2 * 16 / kPagedThreads; ++i) {
+    for (int i = 0; i < VP; ++i) {
       const int piece = i * kPagedThreads + tid, pair = piece / 16, t4 = 4 * (piece % 16);
       float x[4], y[4];
-      const long at = block * P * D + (long)run * 64 * D + 2 * pair * 64 + t4;
       if (full) {
-        values4<FP8>(*reinterpret_cast<const uint32_t*>(a.c.v_codes + at), x);
-        values4<FP8>(*reinterpret_cast<const uint32_t*>(a.c.v_codes + at + 64), y);
+        values4<FP8>(vw[i][0].x, x);
+        values4<FP8>(vw[i][1].x, y);
       } else {
-        const u32x2 u = *reinterpret_cast<const u32x2*>(a.c.v_tail + at), w = *reinterpret_cast<const u32x2*>(a.c.v_tail + at + 64);
-        unpack2<T>(u.x, x[0], x[1]);
-        unpack2<T>(u.y, x[2], x[3]);
-        unpack2<T>(w.x, y[0], y[1]);
-        unpack2<T>(w.y, y[2], y[3]);
+        unpack2<T>(vw[i][0].x, x[0], x[1]);
+        unpack2<T>(vw[i][0].y, x[2], x[3]);
+        unpack2<T>(vw[i][1].x, y[0], y[1]);
+        unpack2<T>(vw[i][1].y, y[2], y[3]);
       }
 #pragma unroll
       for (int j = 0; j < 4; ++j) s_v[(t4 + j) * RS + pair] = pack2<T>(x[j] * vs, y[j] * vs);
