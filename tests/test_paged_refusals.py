@@ -217,3 +217,48 @@ def test_the_binding_refuses_tensors_that_do_not_fit():
     with pytest.raises(dq.DQError, match="exceed"):
         layer.append(k, k, starts, max_rows=101)
     torch.cuda.synchronize()
+
+
+def test_the_compiled_checks_refuse_what_is_no_tensor():
+    """Before any address is looked at; no GPU needed."""
+    dq, paged = _lib()
+    m = paged._module
+    with pytest.raises(TypeError):
+        m.rotate_heads()
+    cache = paged._CPaged(*[PTR] * 6, 10, 8, 128, 64, 4, 0, 0)
+    at = C.addressof(cache)
+    x = torch.zeros((4, 8, 128), dtype=torch.float16)
+    for bad in (None, [1, 2], 3.5, "k"):
+        with pytest.raises(dq.DQError, match="tensor"):
+            m.paged_append(at, 0, bad, x, None, x, x, None, None, None, None, None, None, None, 0.0, 0)
+        with pytest.raises(dq.DQError, match="tensor"):
+            m.paged_attention(at, 0, bad, x, None, x, x, None, 1, 100, 0.0, True, 0, 0, x, 0)
+        with pytest.raises(dq.DQError, match="tensor"):
+            m.paged_read(at, 0, None, x, x, x, None, bad, x, 0)
+        with pytest.raises(dq.DQError):
+            m.rotate_heads(bad, x, None, None, None, None, None, None, 0.0, 0, 0)
+    for wrong in (x, x.bfloat16(), x[0], x[..., :64], x[None, None]):            # on the host, of another type, shape
+        with pytest.raises(dq.DQError):
+            m.paged_append(at, 0, wrong, x, None, x, x, None, None, None, None, None, None, None, 0.0, 0)
+    with pytest.raises(TypeError):
+        m.paged_append("cache", 0, x, x, None, x, x, None, None, None, None, None, None, None, 0.0, 0)
+
+
+@pytest.mark.gpu
+def test_the_compiled_checks_refuse_numbers_that_do_not_fit():
+    dq, paged = _lib()
+    dev, i32, f16 = "cuda:0", torch.int32, torch.float16
+    c = dq.alloc_paged_cache(6, 3, 2, 64, 64, f16, torch.int8, dev)
+    lens, table = torch.ones(2, dtype=i32, device=dev), torch.zeros((2, 3), dtype=i32, device=dev)
+    q = torch.zeros((2, 4, 64), dtype=f16, device=dev)
+    ws = dq.paged_workspace(c, 2, 2, 4, 1, 192)
+    good = dict(cache=c, q=q, starts=None, seq_lens=lens, page_table=table, max_rows=1, max_seq_len=192, workspace=ws)
+    for bad in (dict(max_rows=1 << 31), dict(max_seq_len=1 << 40), dict(window=-(1 << 33)), dict(splits=-1), dict(splits=128), dict(q=q[None]),
+                dict(starts=[0, 1, 2]), dict(workspace=None)):
+        with pytest.raises(dq.DQError):
+            dq.paged_attention(**dict(good, **bad))
+    for bad in (dict(max_rows=1.5), dict(max_seq_len="long"), dict(softmax_scale="s")):
+        with pytest.raises(TypeError):
+            dq.paged_attention(**dict(good, **bad))
+    assert torch.equal(dq.paged_attention(**good), torch.zeros_like(q))
+    torch.cuda.synchronize()
