@@ -61,7 +61,7 @@ __device__ __forceinline__ Share share_of(const PagedAttnArgs& a, int slot) {
   return r;
 }
 
-// One workgroup of four waves per (slot, kv head); its columns are the (row, query head) pairs that read the kv head.  Every
+// One workgroup of four or eight waves per (slot, kv head); its columns are the (row, query head) pairs that read the kv head.  Every
 // wave works tiles of 64 tokens on its own, dealt round-robin over the waves of all splits, and keeps a running maximum, sum
 // and output; waves are joined through LDS, splits through memory.
 //
@@ -75,14 +75,14 @@ __device__ __forceinline__ Share share_of(const PagedAttnArgs& a, int slot) {
 //
 // Bound by memory where caches are long: two bytes a token and channel, 16 x 8 heads of 32768 tokens of 128 channels 1074 MB, 169 us,
 // 6.4 TB/s as a plain read of that size; four sequences of 9384 to 16384 tokens, 40 heads, 530 MB, 95 us, 5.6 TB/s.  By latency where
-// they are short: one tile a wave 5.6 us, launch, lengths, page, codes and two joins after one another; 64 units of 64 tiles of 64
-// channels (33 MB) 15 us.  Tiles requested two or three ahead made no launch faster and short ones slower.
-template <typename T, int D, bool FP8>
-__global__ __launch_bounds__(kPagedThreads, 2) void paged_decode_kernel(PagedAttnArgs a) {
-  constexpr int NC = D / 64, NCT = D / 16;
+// they are short: one tile a wave 5.0 us, launch, lengths, page, codes and joins after one another; 64 units of 64 tiles of 64
+// channels (33 MB) 13.4 us.  Tiles requested two or three ahead made no launch faster and short ones slower.
+template <typename T, int D, bool FP8, int WAVES>
+__global__ __launch_bounds__(64 * WAVES, 2) void paged_decode_kernel(PagedAttnArgs a) {
+  constexpr int NC = D / 64, NCT = D / 16, THREADS = 64 * WAVES;
   typedef typename Vec8<T>::type tx8;
-  __shared__ float s_o[4][kCols][D + 1];
-  __shared__ float s_m[4][kCols], s_l[4][kCols];
+  __shared__ float s_o[WAVES][kCols][D + 1];
+  __shared__ float s_m[WAVES][kCols], s_l[WAVES][kCols];
   __shared__ JoinSpace s_join;
   const int tid = threadIdx.x, lane = tid & 63, wave = __builtin_amdgcn_readfirstlane(tid >> 6), col = lane & 15, G = lane >> 4;
   const int H = a.c.kv_heads, P = a.c.page_tokens, slot = (int)blockIdx.x / H, h = (int)blockIdx.x % H;
@@ -171,7 +171,7 @@ __global__ __launch_bounds__(kPagedThreads, 2) void paged_decode_kernel(PagedAtt
   };
 
   // ---- full pages ----
-  const int stride = splits * 4, mine = first_tile + sh.split * 4 + wave;
+  const int stride = splits * WAVES, mine = first_tile + sh.split * WAVES + wave;
   const int k_row = 16 * ((lane & 15) >> 2) + (lane & 3);   // + 4 t4: the token of this lane's row
   for (int batch0 = mine; batch0 < code_tiles; batch0 += 64 * stride) {
     // the next 64 tiles' blocks and scales, one per lane
@@ -239,7 +239,7 @@ __global__ __launch_bounds__(kPagedThreads, 2) void paged_decode_kernel(PagedAtt
   // ---- the page being filled: 16-bit rows, products in their own type ----
   const int tail_first = max(code_tiles, first_tile);
   for (int tile = tail_first; tile < tiles; ++tile) {
-    if ((tile - first_tile) % stride != sh.split * 4 + wave) continue;
+    if ((tile - first_tile) % stride != sh.split * WAVES + wave) continue;
     const int at_slot = a.bt.tail_slots ? a.bt.tail_slots[b] : b;
     const bool ok = at_slot >= 0 && at_slot < a.c.slots;
     const int run = tile - code_tiles, left = len - tile * kPagedTile;   // tokens of the tile
@@ -294,13 +294,15 @@ __global__ __launch_bounds__(kPagedThreads, 2) void paged_decode_kernel(PagedAtt
   const long part_step = (long)H * kCols * (D + 2);        // from split to split
   float* const parts = a.partials + ((long)sh.first_slot * H + h) * kCols * (D + 2);
   float* const part = parts + sh.split * part_step;
-  for (int idx = 2 * tid; idx < cols * D; idx += 2 * kPagedThreads) {
+  for (int idx = 2 * tid; idx < cols * D; idx += 2 * THREADS) {
     const int cc = idx / D, ch = idx % D;
-    const float M = fmaxf(fmaxf(s_m[0][cc], s_m[1][cc]), fmaxf(s_m[2][cc], s_m[3][cc]));
+    float M = s_m[0][cc];
+#pragma unroll
+    for (int w = 1; w < WAVES; ++w) M = fmaxf(M, s_m[w][cc]);
     const float base = M == -INFINITY ? 0.f : M;
     float x = 0.f, y = 0.f, ll = 0.f;
 #pragma unroll
-    for (int w = 0; w < 4; ++w) {
+    for (int w = 0; w < WAVES; ++w) {
       const float f = __builtin_amdgcn_exp2f(s_m[w][cc] - base);
       x = __builtin_fmaf(s_o[w][cc][ch], f, x);
       y = __builtin_fmaf(s_o[w][cc][ch + 1], f, y);
@@ -318,11 +320,21 @@ __global__ __launch_bounds__(kPagedThreads, 2) void paged_decode_kernel(PagedAtt
   if (splits > 1) join_splits<T, D>(a.counters + unit, splits, parts, part_step, cols, s_join, out_of);
 }
 
+template <typename T, int D, int WAVES>
+static void launch_decode_waves(const PagedAttnArgs& a, hipStream_t st) {
+  const dim3 grid((unsigned)((long)(a.shares ? a.bt.batch > 64 ? a.shares : a.shares + a.bt.batch : a.bt.batch) * a.c.kv_heads));
+  if (a.c.codes == DQ_CODES_E4M3) hipLaunchKernelGGL((paged_decode_kernel<T, D, true, WAVES>), grid, dim3(64 * WAVES), 0, st, a);
+  else hipLaunchKernelGGL((paged_decode_kernel<T, D, false, WAVES>), grid, dim3(64 * WAVES), 0, st, a);
+}
+
+// Eight waves a workgroup where tiles are small (64 channels) and units few: waves are joined through LDS for less than splits through
+// memory.  5 tiles of one unit 5.0 us (5.6 with four waves), 64 units of 64 tiles of 16 columns 13.4 (15.0), 32 of 512 tiles 25.4 (27.6);
+// but 512 units of 8 tiles 10.4 (7.8), and 128 channels, which leave room for one such workgroup a compute unit, 2 to 15 % more.
 template <typename T, int D>
 static void launch_decode(const PagedAttnArgs& a, hipStream_t st) {
-  const dim3 grid((unsigned)((long)(a.shares ? a.bt.batch > 64 ? a.shares : a.shares + a.bt.batch : a.bt.batch) * a.c.kv_heads));
-  if (a.c.codes == DQ_CODES_E4M3) hipLaunchKernelGGL((paged_decode_kernel<T, D, true>), grid, dim3(kPagedThreads), 0, st, a);
-  else hipLaunchKernelGGL((paged_decode_kernel<T, D, false>), grid, dim3(kPagedThreads), 0, st, a);
+  if constexpr (D == 64)
+    if (a.units < 128) return launch_decode_waves<T, D, 8>(a, st);
+  launch_decode_waves<T, D, 4>(a, st);
 }
 
 int32_t launch_paged_decode(const PagedAttnArgs& a, hipStream_t st) {
