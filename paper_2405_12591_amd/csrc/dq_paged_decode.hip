@@ -34,15 +34,13 @@ __device__ __forceinline__ Share share_of(const PagedAttnArgs& a, int slot) {
   Sequence s = {0, 0, 0};
   if (lane < batch) s = sequence_of(a.bt, P, lane);
   const int tiles = s.n ? (s.len + kPagedTile - 1) / kPagedTile - first_tile_of(s, a.window) : 0;
-  int total = tiles;
-#pragma unroll
-  for (int o = 1; o < 64; o *= 2) total += __shfl_xor(total, o);
+  int total = tiles;                                      // (lanes of no sequence need not know it)
+  for (int o = 1; o < batch; o *= 2) total += __shfl_xor(total, o);
   const float per = fmaxf((float)total / (float)a.shares, 1.f), round = a.shares == batch ? 0.99f : 0.5f;
   const int cap = decode_cap(tiles, a.c.head_dim, a.max_rows * a.group);
   const int mine = s.n ? max(min((int)((float)tiles / per + round), min(cap, kMaxSplits)), 1) : 0;
   int upto = mine;                                        // slots of the sequences up to this one
-#pragma unroll
-  for (int o = 1; o < 64; o *= 2) {
+  for (int o = 1; o < batch; o *= 2) {
     const int x = __shfl_up(upto, o);
     if (lane >= o) upto += x;
   }
