@@ -263,6 +263,9 @@ __global__ __launch_bounds__(64 * WAVES, 2) void paged_decode_kernel(PagedAttnAr
       for (int j = 0; j < 4; ++j) u[4 * t4 + j] = acc[j];
     }
     softmax(u, tile, f, 0.f, 1.f, Masked{});
+    uint32_t keep[8];                                     // rows behind the last token may hold anything: 0 * NaN is not 0
+#pragma unroll
+    for (int j = 0; j < 8; ++j) keep[j] = keep_tokens(~0u, left - 16 * G - 2 * j);
     u32x4 p0, p1;
 #pragma unroll
     for (int j = 0; j < 4; ++j) { p0[j] = pack2<T>(u[2 * j], u[2 * j + 1]); p1[j] = pack2<T>(u[8 + 2 * j], u[8 + 2 * j + 1]); }
@@ -270,9 +273,9 @@ __global__ __launch_bounds__(64 * WAVES, 2) void paged_decode_kernel(PagedAttnAr
     for (int ct = 0; ct < NCT; ++ct) {
       u32x4 v0 = *reinterpret_cast<const u32x4*>(vt + ct * 16 * kPagedTile), v1 = *reinterpret_cast<const u32x4*>(vt + ct * 16 * kPagedTile + 8);
 #pragma unroll
-      for (int j = 0; j < 4; ++j) {   // rows behind the last token may hold anything: 0 * NaN is not 0
-        v0[j] = keep_tokens(v0[j], left - 16 * G - 2 * j);
-        v1[j] = keep_tokens(v1[j], left - 16 * G - 8 - 2 * j);
+      for (int j = 0; j < 4; ++j) {
+        v0[j] &= keep[j];
+        v1[j] &= keep[4 + j];
       }
       o[ct] = mma16(__builtin_bit_cast(tx8, v0), __builtin_bit_cast(tx8, p0), o[ct]);
       o[ct] = mma16(__builtin_bit_cast(tx8, v1), __builtin_bit_cast(tx8, p1), o[ct]);
