@@ -464,8 +464,9 @@ typedef struct dq_paged_cache {
  * A ragged batch.  Sequence b owns rows starts[b] .. starts[b+1] - 1 of the packed rows of a call; they are
  * its LAST tokens: row i of n is token seq_lens[b] - n + i.  The caller counts the lengths (one addition
  * for all layers of a step) and names the pages.  Entries the kernels cannot use are not followed out of
- * bounds: rows past `rows`, tokens before 0 or past table_width pages are left out; tokens of a page or
- * slot that does not exist are dropped by dq_paged_append and make attention yield NaN.
+ * bounds: rows past `rows`, tokens before 0 or past table_width pages are left out (the others keep their
+ * places, and rows of such tokens theirs as queries); tokens of a page or slot that does not exist are
+ * dropped by dq_paged_append and make attention yield NaN.
  */
 typedef struct dq_paged_batch {
   const int32_t* starts;     /* i32 [batch + 1], ascending, not always from 0; NULL: one row per sequence

@@ -18,6 +18,7 @@ typedef __bf16 bf16x8 __attribute__((ext_vector_type(8)));
 constexpr int kPagedTile = 64;        // tokens of a work tile and of a run of the value layout
 constexpr int kPagedThreads = 256;
 constexpr int kMaxAxes = 8;
+constexpr long kMostTokens = (1l << 31) - 256;   // of a sequence: token indexes, and a tile's behind them, stay in 32 bits
 constexpr long kMaxThreads = 1l << 32;   // a launch has fewer (along x)
 constexpr float kSmallestAmax = 0x1p-100f;   // a block below it is held as zeros (its inverse step would leave fp32)
 
@@ -54,7 +55,7 @@ inline bool paged_cache_ok(const dq_paged_cache* c) {
 inline bool paged_batch_ok(const dq_paged_batch* b, const dq_paged_cache* c, bool uses_starts) {
   if (!b || !b->seq_lens || !b->page_table || b->batch <= 0 || b->rows < 0) return false;
   if (b->table_width <= 0 || b->table_stride < b->table_width) return false;
-  if ((long)b->table_width * c->page_tokens >= (1l << 31) - 256) return false;   // token indexes stay in 32 bits
+  if ((long)b->table_width * c->page_tokens >= kMostTokens) return false;
   if (uses_starts && !b->starts && b->rows != b->batch) return false;
   if (!b->tail_slots && b->batch > c->slots) return false;
   return true;
@@ -64,14 +65,17 @@ inline bool paged_batch_ok(const dq_paged_batch* b, const dq_paged_cache* c, boo
 // A sequence's rows and lengths, brought into the bounds of the call.
 struct Sequence {
   int row0, n;      // its rows
-  int len;          // its tokens, the rows included
+  int old;          // tokens before them: row i is token old + i, which may lie before 0 or past `len`
+  int len;          // tokens it can have here: seq_lens, or what the page table holds if that is less
 };
 __device__ __forceinline__ Sequence sequence_of(const dq_paged_batch& bt, int page_tokens, int b) {
   Sequence s;
   const int lo = bt.starts ? bt.starts[b] : b, hi = bt.starts ? bt.starts[b + 1] : b + 1;
   s.row0 = min(max(lo, 0), bt.rows);
   s.n = min(max(hi, s.row0), bt.rows) - s.row0;
-  s.len = min(max(bt.seq_lens[b], 0), bt.table_width * page_tokens);
+  const int len = min(max(bt.seq_lens[b], 0), (int)kMostTokens);
+  s.old = len - s.n;
+  s.len = min(len, bt.table_width * page_tokens);
   return s;
 }
 
@@ -81,6 +85,7 @@ __device__ __forceinline__ Sequence sequence_of_wave(const dq_paged_batch& bt, i
   Sequence s = sequence_of(bt, page_tokens, b);
   s.row0 = __builtin_amdgcn_readfirstlane(s.row0);
   s.n = __builtin_amdgcn_readfirstlane(s.n);
+  s.old = __builtin_amdgcn_readfirstlane(s.old);
   s.len = __builtin_amdgcn_readfirstlane(s.len);
   return s;
 }

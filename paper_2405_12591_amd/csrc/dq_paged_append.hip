@@ -83,7 +83,7 @@ __global__ __launch_bounds__(P * D / 16, 4) void paged_append_kernel(AppendArgs 
     if (live) {
       const Sequence s = sequence_of(a.bt, P, b);
       live = row >= s.row0 && row < s.row0 + s.n;         // rows before the first sequence's and behind the last's stay as they are
-      place = s.len - s.n + (int)(row - s.row0);
+      place = s.old + (int)(row - s.row0);
     }
     RowLayout turned = l;
     if (!live) turned.pair0 = -1;
@@ -105,7 +105,7 @@ __global__ __launch_bounds__(P * D / 16, 4) void paged_append_kernel(AppendArgs 
   const int b = item_owner(a.bt.starts, a.bt.rows, a.bt.batch, item, 1, P, 2);
   const Sequence s = sequence_of_wave(a.bt, P, b);
   if (s.n == 0 || s.len == 0) return;
-  const int old = s.len - s.n;                            // may be negative: those rows are left out
+  const int old = s.old;                                  // rows of tokens before 0 or past the table are left out
   const int first_page = max(old, 0) / P, last_page = (s.len - 1) / P;
   int page = first_page + item - item_first(a.bt.starts, a.bt.rows, b, 1, P, 2);
   if (page < first_page || page > last_page) return;

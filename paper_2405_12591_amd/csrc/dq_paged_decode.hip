@@ -16,7 +16,7 @@ struct Share {
   int first_slot;          // of the sequence
   Sequence s;
 };
-__device__ __forceinline__ int first_tile_of(const Sequence& s, int window) { return window ? max(s.len - s.n + 1 - window, 0) / kPagedTile : 0; }
+__device__ __forceinline__ int first_tile_of(const Sequence& s, int window) { return window ? max(s.old + 1 - window, 0) / kPagedTile : 0; }
 
 __device__ __forceinline__ Share share_of(const PagedAttnArgs& a, int slot) {
   Share r;
@@ -31,9 +31,9 @@ __device__ __forceinline__ Share share_of(const PagedAttnArgs& a, int slot) {
     return r;
   }
   const int lane = threadIdx.x & 63;
-  Sequence s = {0, 0, 0};
+  Sequence s = {0, 0, 0, 0};
   if (lane < batch) s = sequence_of(a.bt, P, lane);
-  const int tiles = s.n ? (s.len + kPagedTile - 1) / kPagedTile - first_tile_of(s, a.window) : 0;
+  const int tiles = s.n ? max((s.len + kPagedTile - 1) / kPagedTile - first_tile_of(s, a.window), 0) : 0;
   int total = tiles;                                      // (lanes of no sequence need not know it)
   for (int o = 1; o < batch; o *= 2) total += __shfl_xor(total, o);
   const float per = fmaxf((float)total / (float)a.shares, 1.f), round = a.shares == batch ? 0.99f : 0.5f;
@@ -55,6 +55,7 @@ __device__ __forceinline__ Share share_of(const PagedAttnArgs& a, int slot) {
   r.split = slot - r.first_slot;
   r.s.row0 = __builtin_amdgcn_readlane(s.row0, r.b);
   r.s.n = __builtin_amdgcn_readlane(s.n, r.b);
+  r.s.old = __builtin_amdgcn_readlane(s.old, r.b);
   r.s.len = __builtin_amdgcn_readlane(s.len, r.b);
   return r;
 }
@@ -88,7 +89,7 @@ __global__ __launch_bounds__(64 * WAVES, 2) void paged_decode_kernel(PagedAttnAr
   if (sh.splits == 0) return;
   const Sequence& s = sh.s;
   const int b = sh.b, splits = sh.splits, unit = b * H + h;
-  const int n = min(s.n, a.max_rows), len = s.len, before = len - s.n;   // tokens before the sequence's first row
+  const int n = min(s.n, a.max_rows), len = s.len, before = s.old;
   const int cols = n * a.group;
   const int qi = min(col / a.group, n - 1), hq = h * a.group + col % a.group;
   const bool live = col < cols;

@@ -34,7 +34,7 @@ __global__ __launch_bounds__(64 * kPromptWaves, 2) void paged_prompt_kernel(Page
   const int h = (int)(blockIdx.x % H), split = (int)(blockIdx.x / H) % a.splits, item = (int)(blockIdx.x / H) / a.splits;
   const int b = item_owner(a.bt.starts, a.bt.rows, a.bt.batch, item, a.group, M, 1);
   const Sequence s = sequence_of_wave(a.bt, P, b);
-  const int n = s.n, len = s.len;
+  const int n = s.n, len = s.len, before = s.old;
   const int row_tiles = (int)(((long)n * a.group + M - 1) / M);
   const int j = item - item_first(a.bt.starts, a.bt.rows, b, a.group, M, 1);
   if (j < 0 || j >= row_tiles) return;
@@ -42,9 +42,9 @@ __global__ __launch_bounds__(64 * kPromptWaves, 2) void paged_prompt_kernel(Page
   const int pairs = n * a.group, first = row_tile * M;
   const int rows_lo = first / a.group, rows_hi = min(first + M - 1, pairs - 1) / a.group;
   // tokens that any / every row of the tile sees
-  const int any_hi = a.causal ? min(max(len - n + rows_hi + 1, 0), len) : len;
-  const int any_lo = a.window ? max(len - n + rows_lo + 1 - a.window, 0) : 0;
-  const int all_hi = a.causal ? len - n + rows_lo + 1 : len, all_lo = a.window ? len - n + rows_hi + 1 - a.window : 0;
+  const int any_hi = a.causal ? min(max(before + rows_hi + 1, 0), len) : len;
+  const int any_lo = a.window ? max(before + rows_lo + 1 - a.window, 0) : 0;
+  const int all_hi = a.causal ? before + rows_lo + 1 : len, all_lo = a.window ? before + rows_hi + 1 - a.window : 0;
   const int runs = P / kPagedTile, code_tiles = len / P * runs;
   int t_first = any_lo / kPagedTile, t_last = (any_hi + kPagedTile - 1) / kPagedTile;
   if (t_last < t_first) t_last = t_first;
@@ -55,7 +55,7 @@ __global__ __launch_bounds__(64 * kPromptWaves, 2) void paged_prompt_kernel(Page
   }
 
   // ---- queries ----
-  const int my_pair = min(first + wave * 32 + r32, pairs - 1), my_row = my_pair / a.group, place = len - n + my_row;
+  const int my_pair = min(first + wave * 32 + r32, pairs - 1), my_row = my_pair / a.group, place = before + my_row;
   const int see_hi = a.causal ? min(place + 1, len) : len, see_lo = a.window ? place + 1 - a.window : 0;
   const uint16_t* const q_row =
       a.q.data + (long)(s.row0 + my_row) * a.q.token_stride + (long)(h * a.group + my_pair % a.group) * a.q.head_stride + 8 * hl;
@@ -240,8 +240,8 @@ __global__ __launch_bounds__(64 * kPromptWaves, 2) void paged_prompt_kernel(Page
   const int whole_lo = min(max(t_first, (max(all_lo, 0) + kPagedTile - 1) / kPagedTile), max(code_end, t_first));
   const int whole_hi = max(min(code_end, max(all_hi, 0) / kPagedTile), whole_lo);
   run(whole_hi - whole_lo, [&](int i) { return whole_lo + i; }, Whole{});
-  const int before = whole_lo - t_first;
-  run(before + max(code_end - whole_hi, 0), [&](int i) { return i < before ? t_first + i : whole_hi + i - before; }, Masked{});
+  const int ahead = whole_lo - t_first;
+  run(ahead + max(code_end - whole_hi, 0), [&](int i) { return i < ahead ? t_first + i : whole_hi + i - ahead; }, Masked{});
 
   // ---- the page being filled: 16-bit rows ----
   for (int tile = max(t_first, code_tiles); tile < t_last; ++tile) {

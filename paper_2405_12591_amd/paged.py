@@ -240,6 +240,8 @@ class PagedKVLayer:
     """One layer's keys and values in 8-bit pages, as KVCacheLayer is for the DecoQuant form: `batch` sequences of up to
     max_tokens tokens, each with its own pages and tail, the lengths on the device.  Rows come packed, sequence by
     sequence (`starts`, int32 [batch + 1]; None: one row each); the host tracks only bounds, which size the launches.
+    Replays of a captured step count on the device only: add their rows to tokens_upper (which refuses what is too much;
+    rows of replays past max_tokens' pages are left out).
     (Loops with a page allocator of their own call paged_append and paged_attention.)"""
 
     def __init__(self, batch: int, q_heads: int, kv_heads: int, head_dim: int, max_tokens: int, page_tokens: int = 64,

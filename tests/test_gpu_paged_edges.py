@@ -1,0 +1,122 @@
+"""The paged 8-bit cache at the ends of what a call may ask: rows past the page table, blocks and pages that hold nothing
+of use, bounds that are too small.  Against the 64-bit forms and against calls that stay within."""
+import math
+
+import pytest
+import torch
+
+import paper_2405_12591_amd as dq
+from paged_util import DEV, Sequences, attend64, attend_tolerance, filled_cache, fill_tails, ints, quantize64, read_back, rows
+
+pytestmark = pytest.mark.gpu
+E4M3, INT8, F16, BF16 = torch.float8_e4m3fn, torch.int8, torch.float16, torch.bfloat16
+PAIRS = [(F16, INT8), (BF16, E4M3)]
+
+
+def _sums(v):
+    out = [0]
+    for x in v:
+        out.append(out[-1] + x)
+    return out
+
+
+def _bits(cache):
+    return {n: t.clone().view(torch.uint8) for n, t in cache.t.items()}
+
+
+# ---------------------------------------------------------------------------------------- lengths past the page table
+@pytest.mark.parametrize("dtype,codes", PAIRS)
+@pytest.mark.parametrize("page,width", [(64, 1), (64, 3), (128, 2)])
+def test_rows_past_the_table_are_left_out_and_the_others_keep_their_places(dtype, codes, page, width):
+    """Rows that straddle the table's end: those within it are stored where they belong, with their own rotation, and the
+    page they fill is quantized from them; rows wholly past it change nothing."""
+    gen = torch.Generator().manual_seed(page + width)
+    heads, hq, d, have, new = 2, 4, 64, width * page - 14, 20
+    end = width * page
+    rot = dq.rotary(d, device=DEV)
+    seqs = Sequences([have, have], heads, d, dtype, codes, page, gen)
+    cache, table, slots = filled_cache(seqs, [have, have], gen)
+    fused = rows((2 * new, hq + 2 * heads, d), dtype, gen).to(DEV)
+    q, k, v = fused[:, :hq], fused[:, hq:hq + heads], fused[:, hq + heads:]
+    q_out = torch.full((2 * new, hq, d), 5.0, dtype=dtype, device=DEV)
+    dq.paged_append(cache, k, v, ints([0, new, 2 * new]), ints([have + new] * 2), table, q=q, q_out=q_out, rotary=rot, tail_slots=slots)
+    place = torch.cat([torch.arange(have, have + new)] * 2).to(torch.int32).to(DEV)
+    q_want, k_turned = dq.rotate_heads(q, k, place, rot)
+    assert torch.equal(q_out, q_want)
+    for b in range(2):
+        kept = slice(b * new, b * new + end - have)
+        kk = torch.cat([seqs.k[b], k_turned[kept].cpu()])[-page:].double()
+        vv = torch.cat([seqs.v[b], v[kept].cpu()])[-page:].double()
+        at = int(table[b, width - 1])
+        for h in range(heads):
+            for x, name in ((kk, "k"), (vv, "v")):
+                got = cache.t[name + "_codes"][at, h].cpu().double()
+                got = got if name == "k" else got.transpose(-1, -2).reshape(page, d)
+                want, scale = quantize64(x[:, h], codes)
+                assert torch.equal(got, want) and float(cache.t[name + "_scales"][at, h]) == scale, (b, h, name)
+    before = _bits(cache)
+    for length in (end + new, end + new + 1, end + 10 * page, 2 ** 31 - 1):
+        dq.paged_append(cache, k, v, ints([0, new, 2 * new]), ints([length] * 2), table, rotary=rot, tail_slots=slots)
+    torch.cuda.synchronize()
+    for n, t in _bits(cache).items():
+        assert torch.equal(t, before[n]), n
+
+
+@pytest.mark.parametrize("dtype,codes", PAIRS)
+@pytest.mark.parametrize("new", [1, 4, 100])
+@pytest.mark.parametrize("window", [0, 6, 90])
+def test_queries_past_the_table_see_what_it_holds_from_their_own_place(dtype, codes, new, window):
+    gen = torch.Generator().manual_seed(new + window)
+    heads, hq, d, page, width = 2, 4, 64, 64, 3
+    end = width * page
+    seqs = Sequences([end] * 5, heads, d, dtype, codes, page, gen)
+    cache, table, slots = filled_cache(seqs, [end] * 5, gen)
+    lens = [end, end + 1, end + new // 2, end + new, end + 3 * page]
+    q = rows((5 * new, hq, d), dtype, gen, outliers=False)
+    ws = dq.paged_workspace(cache, 5, 5 * new, hq, new, end)
+    out = dq.paged_attention(cache, q.to(DEV), ints(_sums([new] * 5)), ints(lens), table, new, end, ws, window=window, tail_slots=slots).cpu()
+    for b, n in enumerate(lens):
+        at = slice(b * new, (b + 1) * new)
+        k, v = seqs.stored(seqs.k[b]), seqs.stored(seqs.v[b])
+        want, size, ds = attend64(q[at], k, v, torch.arange(n - new, n), True, window, 1 / math.sqrt(d))
+        tol = attend_tolerance(want, size, ds, float(v.abs().max()), end, dtype, False)
+        assert ((out[at].double() - want).abs() <= tol).all(), (b, float(((out[at].double() - want).abs() / tol).max()))
+        if window and n - new >= end + window:
+            assert (out[at] == 0).all()
+
+
+def test_a_layer_whose_captured_step_runs_past_its_end():
+    """Replays advance the lengths on the device alone: steps past the last page leave the cache as it is, and the bound
+    refuses further rows once it is told."""
+    gen = torch.Generator().manual_seed(31)
+    heads, hq, d = 2, 4, 64
+    layer = dq.PagedKVLayer(2, hq, heads, d, 64, 64, F16, INT8, DEV)
+    pk, pv = (rows((2 * 60, heads, d), F16, gen).to(DEV) for _ in range(2))
+    layer.append(pk, pv, ints([0, 60, 120]), 60)
+    k, v = (torch.empty((2, heads, d), dtype=F16, device=DEV) for _ in range(2))
+    q = rows((2, hq, d), F16, gen, outliers=False).to(DEV)
+    fresh = [[rows((2, heads, d), F16, gen).to(DEV) for _ in range(2)] for _ in range(9)]
+    k.copy_(fresh[0][0])
+    v.copy_(fresh[0][1])
+    layer.append(k, v)
+    layer.attend(q)
+    st, graph = torch.cuda.Stream(), torch.cuda.CUDAGraph()
+    torch.cuda.synchronize()
+    with torch.cuda.graph(graph, stream=st):
+        layer.append(k, v)
+        out = layer.attend(q)
+    full = None
+    for i, (kk, vv) in enumerate(fresh[1:]):             # tokens 61 to 68: the page ends behind token 63
+        k.copy_(kk)
+        v.copy_(vv)
+        graph.replay()
+        torch.cuda.synchronize()
+        if i == 2:
+            full = _bits(layer.cache), out.clone()
+    assert layer.seq_lens.tolist() == [69, 69]
+    for n, t in _bits(layer.cache).items():
+        assert torch.equal(t, full[0][n]), n
+    assert torch.equal(out, full[1])                     # the same 64 tokens
+    layer.tokens_upper += 7
+    with pytest.raises(dq.DQError, match="exceed"):
+        layer.append(k, v)
