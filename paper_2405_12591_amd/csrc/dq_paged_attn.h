@@ -28,6 +28,9 @@ __host__ __device__ inline int decode_cap(int tiles, int head_dim, int cols) {
   return cap < kMaxSplits ? cap : kMaxSplits;
 }
 
+// First token that a row in this place sees (a place before 0, which sees none, must not wrap round with a large window).
+__device__ __forceinline__ int window_start(int place, int window) { return window ? max(max(place + 1, 0) - window, 0) : 0; }
+
 constexpr float kLazy = 8.f;   // a running maximum may fall behind by so many powers of two before sums are rescaled
 
 // Eight codes as f16, exactly.  8-bit floats have an instruction for it; integers ride in the low bits of 1024 + 128 + c.

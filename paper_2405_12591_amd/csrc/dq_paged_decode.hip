@@ -16,7 +16,7 @@ struct Share {
   int first_slot;          // of the sequence
   Sequence s;
 };
-__device__ __forceinline__ int first_tile_of(const Sequence& s, int window) { return window ? max(s.old + 1 - window, 0) / kPagedTile : 0; }
+__device__ __forceinline__ int first_tile_of(const Sequence& s, int window) { return window_start(s.old, window) / kPagedTile; }
 
 __device__ __forceinline__ Share share_of(const PagedAttnArgs& a, int slot) {
   Share r;
@@ -95,8 +95,8 @@ __global__ __launch_bounds__(64 * WAVES, 2) void paged_decode_kernel(PagedAttnAr
   const bool live = col < cols;
   // tokens [see_lo, see_hi) of this column, and what every column sees
   const int place = before + qi;
-  const int see_hi = a.causal ? min(place + 1, len) : len, see_lo = a.window ? max(place + 1 - a.window, 0) : 0;
-  const int all_hi = a.causal ? min(before + 1, len) : len, all_lo = a.window ? max(before + n - a.window, 0) : 0;
+  const int see_hi = a.causal ? min(place + 1, len) : len, see_lo = window_start(place, a.window);
+  const int all_hi = a.causal ? min(before + 1, len) : len, all_lo = window_start(before + n - 1, a.window);
   const int first_tile = first_tile_of(s, a.window);
   const int runs = P / kPagedTile, code_tiles = len / P * runs, tiles = (len + kPagedTile - 1) / kPagedTile;
 

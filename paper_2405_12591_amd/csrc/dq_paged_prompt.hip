@@ -43,8 +43,8 @@ __global__ __launch_bounds__(64 * kPromptWaves, 2) void paged_prompt_kernel(Page
   const int rows_lo = first / a.group, rows_hi = min(first + M - 1, pairs - 1) / a.group;
   // tokens that any / every row of the tile sees
   const int any_hi = a.causal ? min(max(before + rows_hi + 1, 0), len) : len;
-  const int any_lo = a.window ? max(before + rows_lo + 1 - a.window, 0) : 0;
-  const int all_hi = a.causal ? before + rows_lo + 1 : len, all_lo = a.window ? before + rows_hi + 1 - a.window : 0;
+  const int any_lo = window_start(before + rows_lo, a.window);
+  const int all_hi = a.causal ? before + rows_lo + 1 : len, all_lo = window_start(before + rows_hi, a.window);
   const int runs = P / kPagedTile, code_tiles = len / P * runs;
   int t_first = any_lo / kPagedTile, t_last = (any_hi + kPagedTile - 1) / kPagedTile;
   if (t_last < t_first) t_last = t_first;
@@ -56,7 +56,7 @@ __global__ __launch_bounds__(64 * kPromptWaves, 2) void paged_prompt_kernel(Page
 
   // ---- queries ----
   const int my_pair = min(first + wave * 32 + r32, pairs - 1), my_row = my_pair / a.group, place = before + my_row;
-  const int see_hi = a.causal ? min(place + 1, len) : len, see_lo = a.window ? place + 1 - a.window : 0;
+  const int see_hi = a.causal ? min(place + 1, len) : len, see_lo = window_start(place, a.window);
   const uint16_t* const q_row =
       a.q.data + (long)(s.row0 + my_row) * a.q.token_stride + (long)(h * a.group + my_pair % a.group) * a.q.head_stride + 8 * hl;
   float sc = a.scale_log2;
@@ -237,7 +237,7 @@ __global__ __launch_bounds__(64 * kPromptWaves, 2) void paged_prompt_kernel(Page
   };
   // Tiles that every row sees whole, then those that need the mask (two loops: with both kinds in one, registers run out).
   const int code_end = min(t_last, code_tiles);
-  const int whole_lo = min(max(t_first, (max(all_lo, 0) + kPagedTile - 1) / kPagedTile), max(code_end, t_first));
+  const int whole_lo = min(max(t_first, (all_lo + kPagedTile - 1) / kPagedTile), max(code_end, t_first));
   const int whole_hi = max(min(code_end, max(all_hi, 0) / kPagedTile), whole_lo);
   run(whole_hi - whole_lo, [&](int i) { return whole_lo + i; }, Whole{});
   const int ahead = whole_lo - t_first;

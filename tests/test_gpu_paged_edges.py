@@ -120,3 +120,19 @@ def test_a_layer_whose_captured_step_runs_past_its_end():
     layer.tokens_upper += 7
     with pytest.raises(dq.DQError, match="exceed"):
         layer.append(k, v)
+
+
+@pytest.mark.parametrize("new", [8, 400])
+def test_the_largest_window_is_none(new):
+    """Also for sequences of more rows than tokens, whose first rows lie before token 0."""
+    gen = torch.Generator().manual_seed(new)
+    lens = [3, 200, 64]
+    seqs = Sequences(lens, 2, 64, F16, INT8, 64, gen)
+    cache, table, slots = filled_cache(seqs, lens, gen)
+    q = rows((3 * new, 2, 64), F16, gen, outliers=False).to(DEV)
+    ws = dq.paged_workspace(cache, 3, 3 * new, 2, new, 200)
+    want = dq.paged_attention(cache, q, ints(_sums([new] * 3)), ints(lens), table, new, 200, ws, tail_slots=slots)
+    assert (want[new - 3:new] != 0).any() and (want[:new - 3] == 0).all()
+    for window in (2 ** 31 - 1, 2 ** 31 - 256, 2 ** 31 - 257, 201):
+        got = dq.paged_attention(cache, q, ints(_sums([new] * 3)), ints(lens), table, new, 200, ws, window=window, tail_slots=slots)
+        assert torch.equal(got, want), window
