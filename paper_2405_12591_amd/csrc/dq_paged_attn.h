@@ -84,6 +84,16 @@ struct Whole { static constexpr bool value = false; };
 // Scores are scaled inside the exponential's argument; a factor of 0 (an underflow) would make NaN of a masked -inf.
 __device__ __forceinline__ float keep_sign(float f) { return f < 1e-37f ? 1e-37f : f; }   // (NaN stays)
 
+// Codes that a page which does not exist has: its tokens are NaN by the factor of their scores, for those who see them, and must
+// not reach the others as 0 * NaN of whatever another page holds.
+__device__ const u32x4 g_no_codes[kPagedTile * 128 / 16] = {};
+// A tile's codes (its number, or -1).  The address space is named: a choice between two plain pointers became flat loads, which LDS waits count too.
+typedef const uint8_t __attribute__((address_space(1))) * GlobalBytes;
+typedef const u32x4 __attribute__((address_space(1))) * GlobalPieces;
+__device__ __forceinline__ GlobalBytes codes_of(const uint8_t* codes, int tile, int bytes) {
+  return tile < 0 ? (GlobalBytes)g_no_codes : (GlobalBytes)codes + (long)tile * bytes;
+}
+
 // Two 16-bit tokens of a value word, zero where the token lies behind the last one (`left` tokens count from the word's first).
 __device__ __forceinline__ uint32_t keep_tokens(uint32_t w, int left) { return left >= 2 ? w : left == 1 ? (w & 0xFFFFu) : 0u; }
 

@@ -175,13 +175,13 @@ __global__ __launch_bounds__(64 * WAVES, 2) void paged_decode_kernel(PagedAttnAr
   for (int batch0 = mine; batch0 < code_tiles; batch0 += 64 * stride) {
     // the next 64 tiles' blocks and scales, one per lane
     const int t_l = batch0 + lane * stride;
-    int blk = 0;
+    int blk = -1;
     float sk = 0.f, lsv = 0.f, isv = 0.f;
     if (t_l < code_tiles) {
       const int page = a.bt.page_table[(long)b * a.bt.table_stride + t_l / runs];
       const bool ok = page >= 0 && page < a.c.pages;
       const long block = (long)(ok ? page : 0) * H + h;
-      blk = (int)(block * runs) + t_l % runs;
+      blk = ok ? (int)(block * runs) + t_l % runs : -1;
       sk = ok ? a.c.k_scales[block] : __builtin_nanf("");
       const float sv = ok ? a.c.v_scales[block] : 1.f;
       lsv = __builtin_amdgcn_logf(sv);
@@ -190,16 +190,16 @@ __global__ __launch_bounds__(64 * WAVES, 2) void paged_decode_kernel(PagedAttnAr
     const int count = min(64, (code_tiles - batch0 + stride - 1) / stride);
     u32x4 kb[4][NC], vb[NCT];
     auto load_k = [&](int i) __attribute__((always_inline)) {
-      const uint8_t* p = a.c.k_codes + (long)__builtin_amdgcn_readlane(blk, i) * (kPagedTile * D) + k_row * D + 16 * G;
+      const GlobalBytes p = codes_of(a.c.k_codes, __builtin_amdgcn_readlane(blk, i), kPagedTile * D) + k_row * D + 16 * G;
 #pragma unroll
       for (int t4 = 0; t4 < 4; ++t4)
 #pragma unroll
-        for (int c = 0; c < NC; ++c) kb[t4][c] = __builtin_nontemporal_load(reinterpret_cast<const u32x4*>(p + 4 * t4 * D + 64 * c));
+        for (int c = 0; c < NC; ++c) kb[t4][c] = __builtin_nontemporal_load((GlobalPieces)(p + 4 * t4 * D + 64 * c));
     };
     auto load_v = [&](int i) __attribute__((always_inline)) {
-      const uint8_t* p = a.c.v_codes + (long)__builtin_amdgcn_readlane(blk, i) * (kPagedTile * D) + (lane & 15) * kPagedTile + 16 * G;
+      const GlobalBytes p = codes_of(a.c.v_codes, __builtin_amdgcn_readlane(blk, i), kPagedTile * D) + (lane & 15) * kPagedTile + 16 * G;
 #pragma unroll
-      for (int ct = 0; ct < NCT; ++ct) vb[ct] = __builtin_nontemporal_load(reinterpret_cast<const u32x4*>(p + ct * 16 * kPagedTile));
+      for (int ct = 0; ct < NCT; ++ct) vb[ct] = __builtin_nontemporal_load((GlobalPieces)(p + ct * 16 * kPagedTile));
     };
     load_k(0);
     load_v(0);
@@ -241,7 +241,7 @@ __global__ __launch_bounds__(64 * WAVES, 2) void paged_decode_kernel(PagedAttnAr
     if ((tile - first_tile) % stride != sh.split * WAVES + wave) continue;
     const int at_slot = a.bt.tail_slots ? a.bt.tail_slots[b] : b;
     const bool ok = at_slot >= 0 && at_slot < a.c.slots;
-    const int run = tile - code_tiles, left = len - tile * kPagedTile;   // tokens of the tile
+    const int run = tile - code_tiles, left = ok ? len - tile * kPagedTile : 0;   // tokens of the tile
     const long at = (((long)(ok ? at_slot : 0) * H + h) * runs + run) * kPagedTile * D;
     const uint16_t* const kt = a.c.k_tail + at + k_row * D + 16 * G;
     const uint16_t* const vt = a.c.v_tail + at + (lane & 15) * kPagedTile + 16 * G;

@@ -195,13 +195,13 @@ __global__ __launch_bounds__(64 * kPromptWaves, 2) void paged_prompt_kernel(Page
   // `total` tiles of full pages, the i-th of them tile_of(i).
   auto run = [&](int total, auto tile_of, auto mask) __attribute__((always_inline)) {
     for (int batch0 = 0; batch0 < total; batch0 += 64) {
-      int blk = 0;
+      int blk = -1;
       float sk = 0.f, lsv = 0.f, isv = 0.f;
       if (batch0 + lane < total) {
         const int t = tile_of(batch0 + lane), page = a.bt.page_table[(long)b * a.bt.table_stride + t / runs];
         const bool ok = page >= 0 && page < a.c.pages;
         const long block = (long)(ok ? page : 0) * H + h;
-        blk = (int)(block * runs) + t % runs;
+        blk = ok ? (int)(block * runs) + t % runs : -1;
         sk = ok ? a.c.k_scales[block] : __builtin_nanf("");
         const float sv = ok ? a.c.v_scales[block] : 1.f;
         lsv = __builtin_amdgcn_logf(sv);
@@ -209,11 +209,12 @@ __global__ __launch_bounds__(64 * kPromptWaves, 2) void paged_prompt_kernel(Page
       }
       const int count = min(64, total - batch0);
       auto load_tile = [&](int i) __attribute__((always_inline)) {   // (behind the last one: that one again, never used)
-        const long at = (long)__builtin_amdgcn_readlane(blk, min(i, count - 1)) * (kPagedTile * D);
+        const int at = __builtin_amdgcn_readlane(blk, min(i, count - 1));
+        const GlobalBytes ks = codes_of(a.c.k_codes, at, kPagedTile * D), vs = codes_of(a.c.v_codes, at, kPagedTile * D);
 #pragma unroll
         for (int k = 0; k < NB; ++k) {
-          kc[k] = *reinterpret_cast<const u32x4*>(a.c.k_codes + at + 16l * (k * THREADS + tid));
-          vc[k] = *reinterpret_cast<const u32x4*>(a.c.v_codes + at + 16l * (k * THREADS + tid));
+          kc[k] = *(GlobalPieces)(ks + 16l * (k * THREADS + tid));
+          vc[k] = *(GlobalPieces)(vs + 16l * (k * THREADS + tid));
         }
       };
       load_tile(0);
@@ -247,7 +248,7 @@ __global__ __launch_bounds__(64 * kPromptWaves, 2) void paged_prompt_kernel(Page
   for (int tile = max(t_first, code_tiles); tile < t_last; ++tile) {
     const int slot = a.bt.tail_slots ? a.bt.tail_slots[b] : b;
     const bool ok = slot >= 0 && slot < a.c.slots;
-    const int left = len - tile * kPagedTile;
+    const int left = ok ? len - tile * kPagedTile : 0;
     const long at = (((long)(ok ? slot : 0) * H + h) * runs + (tile - code_tiles)) * kPagedTile * D;
     __syncthreads();
 #pragma unroll

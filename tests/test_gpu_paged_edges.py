@@ -136,3 +136,39 @@ def test_the_largest_window_is_none(new):
     for window in (2 ** 31 - 1, 2 ** 31 - 256, 2 ** 31 - 257, 201):
         got = dq.paged_attention(cache, q, ints(_sums([new] * 3)), ints(lens), table, new, 200, ws, window=window, tail_slots=slots)
         assert torch.equal(got, want), window
+
+
+@pytest.mark.parametrize("dtype,codes", [(F16, E4M3), (BF16, E4M3), (F16, INT8)])
+@pytest.mark.parametrize("new,window,bad", [(8, 188, "page 0"), (70, 0, "page 3"), (70, 160, "page 0"), (12, 0, "slot"), (140, 0, "slot")])
+def test_rows_that_do_not_see_a_missing_page_are_untouched(dtype, codes, new, window, bad):
+    """Whatever the first page and slot of the pool hold: the others' rows come out as they should, those that see it as NaN."""
+    gen = torch.Generator().manual_seed(new + window)
+    heads, hq, d, page = 2, 2, 64, 64
+    n = 200 if bad == "slot" else 256
+    seqs = Sequences([n, n], heads, d, dtype, codes, page, gen)
+    cache = dq.alloc_paged_cache(9, 3, heads, d, page, dtype, codes, DEV)
+    fill_tails(cache)                                     # slot 0 belongs to nobody and stays so
+    for x in ("k", "v"):
+        cache.t[x + "_codes"][0].view(torch.uint8).fill_(0x7F)      # NaN as e4m3
+        cache.t[x + "_scales"][0] = float("nan")
+    table, slots = ints([[3, 1, 7, 5], [2, 8, 4, 6]]), ints([2, 1])
+    dq.paged_append(cache, torch.cat(seqs.k).to(DEV), torch.cat(seqs.v).to(DEV), ints([0, n, 2 * n]), ints([n, n]), table, tail_slots=slots)
+    lo, hi = (192, 256) if bad in ("slot", "page 3") else (0, 64)
+    if bad == "slot":
+        slots[1] = 99
+    else:
+        table[1, int(bad[-1])] = -1
+    q = rows((2 * new, hq, d), dtype, gen, outliers=False)
+    ws = dq.paged_workspace(cache, 2, 2 * new, hq, new, n)
+    out = dq.paged_attention(cache, q.to(DEV), ints([0, new, 2 * new]), ints([n, n]), table, new, n, ws, window=window, tail_slots=slots).cpu()
+    place = torch.arange(n - new, n)
+    sees = (place >= lo) & ((place + 1 - window if window else torch.zeros_like(place)) < hi)
+    assert sees.any() and not sees.all()
+    for b in range(2):
+        k, v = seqs.stored(seqs.k[b]), seqs.stored(seqs.v[b])
+        want, size, ds = attend64(q[b * new:(b + 1) * new], k, v, place, True, window, 1 / math.sqrt(d))
+        tol = attend_tolerance(want, size, ds, float(v.abs().max()), n, dtype, True)
+        got = out[b * new:(b + 1) * new]
+        fine = ~sees if b == 1 else torch.ones_like(sees)
+        assert torch.isnan(got[~fine]).all()
+        assert ((got[fine].double() - want[fine]).abs() <= tol[fine]).all(), b
