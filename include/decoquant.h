@@ -516,8 +516,8 @@ size_t dq_paged_workspace_bytes(const dq_paged_cache* cache, int32_t batch, int3
  * and values are what the cache stands for; fp32 accumulation, one rounding of the result, probabilities
  * in 16 bits for their product with the values.
  *   q, out         [rows, q_heads, d]; out may be q
- *   max_rows       host bound on the rows of any sequence; it chooses the kernel, and further rows of a
- *                  sequence may be left out
+ *   max_rows       host bound on the rows of any sequence; it chooses the kernel, and further rows of that
+ *                  sequence may be left out (not written)
  *   max_seq_len    host bound on seq_lens (a guess does: it sizes the launch only, which orders the sums)
  *   window         > 0: a row sees the last `window` tokens up to its own place only (needs causal)
  *   softmax_scale  <= 0 selects 1/sqrt(d)

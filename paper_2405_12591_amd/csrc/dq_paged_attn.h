@@ -14,6 +14,7 @@ struct PagedAttnArgs {
   int causal;
   float scale_log2;        // softmax scale * log2(e)
   int splits;              // prompt kernel: of every tile of rows
+  int seq_tiles;           // prompt kernel: tiles of rows that every sequence gets, whatever it has (0: dealt by starts)
   int shares;              // decode kernel: slots that are meant to have equal shares of all tiles (0: a slot per sequence)
   float* partials;         // decode: [slot, kv head, column, D + 2]; prompt: [unit, split, D + 2, row]
   int32_t* counters;       // [unit], zero between calls

@@ -32,11 +32,11 @@ __global__ __launch_bounds__(64 * kPromptWaves, 2) void paged_prompt_kernel(Page
   const int tid = threadIdx.x, lane = tid & 63, wave = tid >> 6, r32 = lane & 31, hl = lane >> 5;
   const int H = a.c.kv_heads, P = a.c.page_tokens;
   const int h = (int)(blockIdx.x % H), split = (int)(blockIdx.x / H) % a.splits, item = (int)(blockIdx.x / H) / a.splits;
-  const int b = item_owner(a.bt.starts, a.bt.rows, a.bt.batch, item, a.group, M, 1);
+  const int b = a.seq_tiles ? item / a.seq_tiles : item_owner(a.bt.starts, a.bt.rows, a.bt.batch, item, a.group, M, 1);
   const Sequence s = sequence_of_wave(a.bt, P, b);
-  const int n = s.n, len = s.len, before = s.old;
+  const int n = a.seq_tiles ? min(s.n, a.max_rows) : s.n, len = s.len, before = s.old;
   const int row_tiles = (int)(((long)n * a.group + M - 1) / M);
-  const int j = item - item_first(a.bt.starts, a.bt.rows, b, a.group, M, 1);
+  const int j = a.seq_tiles ? item % a.seq_tiles : item - item_first(a.bt.starts, a.bt.rows, b, a.group, M, 1);
   if (j < 0 || j >= row_tiles) return;
   const int row_tile = row_tiles - 1 - j;                 // the longest first
   const int pairs = n * a.group, first = row_tile * M;
@@ -361,6 +361,7 @@ int32_t launch_paged_prompt(const PagedAttnArgs& a, hipStream_t st) {
 struct PagedShape {
   bool decode;
   long units;
+  int seq_tiles;           // prompt: PagedAttnArgs::seq_tiles
   int splits, cols;        // splits: of every unit (prompt), of a sequence of the longest length if all were (decode)
   long shares, groups;     // decode: PagedAttnArgs::shares; workgroups that may hand over partial results (0: none)
 };
@@ -401,14 +402,19 @@ static bool paged_shape(const dq_paged_cache* c, int batch, long rows, int q_hea
   int tiles = max_seq_len / kPagedTile + 1;
   if (window > 0 && ((long)window + max_rows) / kPagedTile + 2 < tiles) tiles = (int)(((long)window + max_rows) / kPagedTile + 2);
   s->decode = (long)max_rows * group <= 16;
-  if ((long)batch * max_rows < rows) rows = (long)batch * max_rows;   // (rows behind the last sequence's)
-  if (rows * group >= (1l << 31)) return false;
-  s->units = s->decode ? (long)batch * c->kv_heads : (rows * group / kPromptRows + batch) * c->kv_heads;
+  const long most = (long)batch * max_rows;
+  if ((most < rows ? most : rows) * group >= (1l << 31)) return false;
+  // Tiles of rows: dealt by starts there are `rows` rows of them and one a sequence that may stay empty.  Where the bound on rows gives
+  // every sequence tiles of its own with no more in all (one sequence, equal ones, rows behind the last sequence's), it does: a sequence
+  // with more rows than the bound then takes nothing from the others.
+  const long seq_tiles = ((long)max_rows * group + kPromptRows - 1) / kPromptRows, dealt = rows * group / kPromptRows + batch;
+  s->seq_tiles = !s->decode && seq_tiles <= dealt / batch ? (int)seq_tiles : 0;
+  const long items = s->decode ? batch : s->seq_tiles ? batch * seq_tiles : dealt;
+  if (items >= (1l << 24)) return false;
+  s->units = items * c->kv_heads;
   s->cols = s->decode ? 16 : kPromptRows;
   if (s->units >= (1l << 24)) return false;
-  // (a sequence leaves part of its last tile of rows empty; no more tiles than the longest sequence would have)
-  const long filled = (long)batch * (((long)max_rows * group + kPromptRows - 1) / kPromptRows) * c->kv_heads;
-  s->splits = s->decode ? decode_splits(s->units, tiles, c->head_dim, max_rows * group) : pick_splits(filled < s->units ? filled : s->units, prompt_cap(tiles), 512);
+  s->splits = s->decode ? decode_splits(s->units, tiles, c->head_dim, max_rows * group) : pick_splits(s->units, prompt_cap(tiles), 512);
   if (const int v = (int)(flags >> 8 & 0x7Fu)) s->splits = !s->decode && v > kPromptSplits ? kPromptSplits : v;   // the caller's override
   if (s->units > kPagedCounters) s->splits = 1;
   s->shares = 0;
@@ -467,6 +473,7 @@ extern "C" int32_t dq_paged_attention(const dq_paged_cache* cache, const dq_page
   a.causal = (flags & DQ_PAGED_CAUSAL) ? 1 : 0;
   a.scale_log2 = (softmax_scale > 0.f ? softmax_scale : 1.0f / sqrtf((float)cache->head_dim)) * 1.44269504088896340736f;
   a.splits = s.splits;
+  a.seq_tiles = s.seq_tiles;
   a.shares = (int)s.shares;
   a.units = (int)s.units;
   char* ws = reinterpret_cast<char*>(workspace);

@@ -172,3 +172,43 @@ def test_rows_that_do_not_see_a_missing_page_are_untouched(dtype, codes, new, wi
         fine = ~sees if b == 1 else torch.ones_like(sees)
         assert torch.isnan(got[~fine]).all()
         assert ((got[fine].double() - want[fine]).abs() <= tol[fine]).all(), b
+
+
+# ---------------------------------------------------------------------------------------- the bound on rows
+@pytest.mark.parametrize("dtype,codes", PAIRS)
+@pytest.mark.parametrize("new,most,group", [([500, 17], 17, 1), ([17, 500, 30], 30, 2), ([300, 300], 100, 1), ([40, 1, 900], 20, 4), ([200, 5, 150], 4, 4),
+                                            ([90, 0, 90], 89, 1)])
+def test_a_sequence_with_more_rows_than_the_bound_takes_nothing_from_the_others(dtype, codes, new, most, group):
+    """Its rows up to the bound and all rows of the others come out; further ones may be left out, none is wrong."""
+    gen = torch.Generator().manual_seed(sum(new) + most)
+    heads, d = 2, 64
+    lens = [n + 100 + 7 * i for i, n in enumerate(new)]
+    seqs = Sequences(lens, heads, d, dtype, codes, 64, gen)
+    cache, table, slots = filled_cache(seqs, lens, gen)
+    q = rows((sum(new), heads * group, d), dtype, gen, outliers=False)
+    ws = dq.paged_workspace(cache, len(new), sum(new), heads * group, most, max(lens))
+    out = torch.full((sum(new), heads * group, d), 5.0, dtype=dtype, device=DEV)
+    dq.paged_attention(cache, q.to(DEV), ints(_sums(new)), ints(lens), table, most, max(lens), ws, out=out, tail_slots=slots)
+    out, at = out.cpu(), 0
+    for b, n in enumerate(new):
+        k, v = seqs.stored(seqs.k[b]), seqs.stored(seqs.v[b])
+        want, size, ds = attend64(q[at:at + n], k, v, torch.arange(lens[b] - n, lens[b]), True, 0, 1 / math.sqrt(d))
+        right = ((out[at:at + n].double() - want).abs() <= attend_tolerance(want, size, ds, float(v.abs().max()), lens[b], dtype, True)).flatten(1).all(1)
+        assert right[:most].all(), (b, right.nonzero().flatten().tolist())
+        assert (right[most:] | (out[at:at + n][most:] == 5.0).flatten(1).all(1)).all(), b
+        at += n
+
+
+def test_a_padded_buffer_of_rows():
+    """Many more rows than the sequences have, before and behind theirs: the bits of a call without them."""
+    gen = torch.Generator().manual_seed(41)
+    lens, new, skip, behind = [300, 77, 200], [60, 60, 41], 900, 3000
+    seqs = Sequences(lens, 2, 64, BF16, E4M3, 64, gen)
+    cache, table, slots = filled_cache(seqs, lens, gen)
+    total = sum(new)
+    q = rows((skip + total + behind, 6, 64), BF16, gen, outliers=False).to(DEV)
+    ws = dq.paged_workspace(cache, 3, len(q), 6, 60, 300)
+    out = torch.full_like(q, 5.0)
+    dq.paged_attention(cache, q, ints([skip + x for x in _sums(new)]), ints(lens), table, 60, 300, ws, out=out, tail_slots=slots)
+    want = dq.paged_attention(cache, q[skip:skip + total], ints(_sums(new)), ints(lens), table, 60, 300, ws, tail_slots=slots)
+    assert torch.equal(out[skip:skip + total], want) and (out[:skip] == 5.0).all() and (out[skip + total:] == 5.0).all()
