@@ -195,13 +195,15 @@ __global__ __launch_bounds__(64 * kPromptWaves, 2) void paged_prompt_kernel(Page
   // `total` tiles of full pages, the i-th of them tile_of(i).
   auto run = [&](int total, auto tile_of, auto mask) __attribute__((always_inline)) {
     for (int batch0 = 0; batch0 < total; batch0 += 64) {
-      int blk = -1;
+      int blk = 0;
+      uint64_t values = 0;                                // where the tile's codes are (the choice cost prompts 1 % in load_tile)
       float sk = 0.f, lsv = 0.f, isv = 0.f;
       if (batch0 + lane < total) {
         const int t = tile_of(batch0 + lane), page = a.bt.page_table[(long)b * a.bt.table_stride + t / runs];
         const bool ok = page >= 0 && page < a.c.pages;
         const long block = (long)(ok ? page : 0) * H + h;
-        blk = ok ? (int)(block * runs) + t % runs : -1;
+        blk = (int)(block * runs) + t % runs;
+        values = (uint64_t)(ok ? a.c.v_codes + (long)blk * (kPagedTile * D) : reinterpret_cast<const uint8_t*>(g_no_codes));
         sk = ok ? a.c.k_scales[block] : __builtin_nanf("");
         const float sv = ok ? a.c.v_scales[block] : 1.f;
         lsv = __builtin_amdgcn_logf(sv);
@@ -209,8 +211,10 @@ __global__ __launch_bounds__(64 * kPromptWaves, 2) void paged_prompt_kernel(Page
       }
       const int count = min(64, total - batch0);
       auto load_tile = [&](int i) __attribute__((always_inline)) {   // (behind the last one: that one again, never used)
-        const int at = __builtin_amdgcn_readlane(blk, min(i, count - 1));
-        const GlobalBytes ks = codes_of(a.c.k_codes, at, kPagedTile * D), vs = codes_of(a.c.v_codes, at, kPagedTile * D);
+        const int j = min(i, count - 1);
+        const GlobalBytes ks = (GlobalBytes)a.c.k_codes + (long)__builtin_amdgcn_readlane(blk, j) * (kPagedTile * D);
+        const GlobalBytes vs = (GlobalBytes)((uint64_t)(uint32_t)__builtin_amdgcn_readlane((int)(values >> 32), j) << 32 |
+                                             (uint32_t)__builtin_amdgcn_readlane((int)values, j));
 #pragma unroll
         for (int k = 0; k < NB; ++k) {
           kc[k] = *(GlobalPieces)(ks + 16l * (k * THREADS + tid));
