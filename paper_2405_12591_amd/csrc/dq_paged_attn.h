@@ -95,6 +95,35 @@ __device__ __forceinline__ GlobalBytes codes_of(const uint8_t* codes, int tile, 
   return tile < 0 ? (GlobalBytes)g_no_codes : (GlobalBytes)codes + (long)tile * bytes;
 }
 
+// A block of zero values has the scale 1, which says nothing of its size: as it is, it would hold the running maximum far above blocks
+// of small values, whose probabilities would lose bits in f16 or vanish.  Any scale 2^k serves it as well (codes of 0; k cancels in the
+// sum): 2^-40 of the least of the wave's other blocks, so that it stays out of their way also where its tokens weigh most, and no less
+// than 2^-95, which keeps the sum in fp32.  lsv, isv: log2 and inverse of the scale of the lane's block `tile` (where `ok`).  A wave
+// with no scale of exactly 1 passes by.
+template <int D, bool FP8>
+__device__ __forceinline__ void place_zero_blocks(const uint8_t* v_codes, int tile, bool ok, float& lsv, float& isv) {
+  const bool one = ok && isv == 1.f;
+  uint64_t asks = __ballot(one);
+  if (asks == 0) return;
+  float least = ok && !one ? lsv : INFINITY;
+  for (int o = 1; o < 64; o *= 2) least = fminf(least, __shfl_xor(least, o));
+  const float k = least == INFINITY ? -60.f : fmaxf(floorf(least) - 40.f, -95.f);
+  const int lane = threadIdx.x & 63;
+  for (; asks; asks &= asks - 1) {
+    const int i = __builtin_ctzll(asks);
+    const u32x4* const from = reinterpret_cast<const u32x4*>(v_codes + (long)__builtin_amdgcn_readlane(tile, i) * (kPagedTile * D));
+    uint32_t any = 0;
+#pragma unroll
+    for (int p = 0; p < D / 16; ++p) {
+      const u32x4 w = from[64 * p + lane];
+      any |= w.x | w.y | w.z | w.w;
+    }
+    if (__any((any & (FP8 ? 0x7F7F7F7Fu : ~0u)) != 0) || lane != i) continue;
+    lsv = k;
+    isv = __builtin_amdgcn_exp2f(-k);
+  }
+}
+
 // Two 16-bit tokens of a value word, zero where the token lies behind the last one (`left` tokens count from the word's first).
 __device__ __forceinline__ uint32_t keep_tokens(uint32_t w, int left) { return left >= 2 ? w : left == 1 ? (w & 0xFFFFu) : 0u; }
 

@@ -187,6 +187,7 @@ __global__ __launch_bounds__(64 * WAVES, 2) void paged_decode_kernel(PagedAttnAr
       lsv = __builtin_amdgcn_logf(sv);
       isv = 1.f / sv;
     }
+    place_zero_blocks<D, FP8>(a.c.v_codes, blk, blk >= 0, lsv, isv);
     const int count = min(64, (code_tiles - batch0 + stride - 1) / stride);
     u32x4 kb[4][NC], vb[NCT];
     auto load_k = [&](int i) __attribute__((always_inline)) {

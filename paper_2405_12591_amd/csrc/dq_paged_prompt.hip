@@ -196,6 +196,7 @@ __global__ __launch_bounds__(64 * kPromptWaves, 2) void paged_prompt_kernel(Page
   auto run = [&](int total, auto tile_of, auto mask) __attribute__((always_inline)) {
     for (int batch0 = 0; batch0 < total; batch0 += 64) {
       int blk = 0;
+      bool held = false;
       uint64_t values = 0;                                // where the tile's codes are (the choice cost prompts 1 % in load_tile)
       float sk = 0.f, lsv = 0.f, isv = 0.f;
       if (batch0 + lane < total) {
@@ -208,7 +209,9 @@ __global__ __launch_bounds__(64 * kPromptWaves, 2) void paged_prompt_kernel(Page
         const float sv = ok ? a.c.v_scales[block] : 1.f;
         lsv = __builtin_amdgcn_logf(sv);
         isv = 1.f / sv;
+        held = ok;
       }
+      place_zero_blocks<D, FP8>(a.c.v_codes, blk, held, lsv, isv);
       const int count = min(64, total - batch0);
       auto load_tile = [&](int i) __attribute__((always_inline)) {   // (behind the last one: that one again, never used)
         const int j = min(i, count - 1);

@@ -212,3 +212,37 @@ def test_a_padded_buffer_of_rows():
     dq.paged_attention(cache, q, ints([skip + x for x in _sums(new)]), ints(lens), table, 60, 300, ws, out=out, tail_slots=slots)
     want = dq.paged_attention(cache, q[skip:skip + total], ints(_sums(new)), ints(lens), table, 60, 300, ws, tail_slots=slots)
     assert torch.equal(out[skip:skip + total], want) and (out[:skip] == 5.0).all() and (out[skip + total:] == 5.0).all()
+
+
+# ---------------------------------------------------------------------------------------- blocks of zeros
+@pytest.mark.parametrize("dtype,codes", [(F16, INT8), (F16, E4M3), (BF16, E4M3), (BF16, INT8)])
+@pytest.mark.parametrize("page,new,small", [(64, 1, True), (128, 1, True), (64, 3, False), (64, 40, True), (128, 40, False)])
+def test_blocks_of_zero_values_beside_small_ones(dtype, codes, page, new, small):
+    """The scale 1 of a block of zeros takes no bits from blocks of small values, wherever it stands and however its tokens
+    weigh; sequences of nothing but zeros yield zeros."""
+    gen = torch.Generator().manual_seed(page + new)
+    heads, hq, d = 2, 4, 64
+    lens = [5 * page + 9, 300, 64 * 130 + 5, 4 * page]
+    seqs = Sequences(lens, heads, d, dtype, codes, page, gen)
+    power = (-11 if dtype == F16 else -60) if small else 4
+    for b in range(4):
+        seqs.v[b] = (seqs.v[b].double() * 2.0 ** power).to(dtype)
+    seqs.v[0][:page] = 0
+    seqs.k[0][:page] *= 3                                 # its tokens may weigh most
+    seqs.v[1][page:2 * page, 1] = -0.0
+    for p in range(0, lens[2] // page, 3):
+        seqs.v[2][p * page:(p + 1) * page, p % 2] = 0
+    seqs.v[3][:] = 0
+    cache, table, slots = filled_cache(seqs, lens, gen)
+    q = rows((4 * new, hq, d), dtype, gen, outliers=False)
+    ws = dq.paged_workspace(cache, 4, 4 * new, hq, new, max(lens))
+    out = dq.paged_attention(cache, q.to(DEV), ints(_sums([new] * 4)), ints(lens), table, new, max(lens), ws, tail_slots=slots).cpu()
+    for b, n in enumerate(lens):
+        at = slice(b * new, (b + 1) * new)
+        k, v = seqs.stored(seqs.k[b]), seqs.stored(seqs.v[b])
+        want, size, ds = attend64(q[at], k, v, torch.arange(n - new, n), True, 0, 1 / math.sqrt(d))
+        # values of the size that these have: bf16 has no smallest step here, fp16's results one of 2^-24
+        tol = attend_tolerance(want, size, ds, float(v.abs().max()), n, dtype, True) - (2.0 ** -24 if dtype == BF16 else 2.0 ** -25)
+        err = (out[at].double() - want).abs()
+        assert (err <= tol).all(), (b, float((err / tol).max()))
+    assert (out[3 * new:] == 0).all()
