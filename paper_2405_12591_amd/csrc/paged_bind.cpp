@@ -127,13 +127,21 @@ void turning(Turning& t, PyObject* q_weight, PyObject* k_weight, PyObject* eps, 
     t.n = &t.norm;
   }
   if (none(rotary)) return;
-  int device = 0, axes = 0, rot_dim = 0, interleaved = 0;   // a Rotary's own tensors, as it keeps them
-  unsigned long long freq = 0, axis = 0;
-  if (!PyArg_ParseTuple(rotary, "iKKiii", &device, &freq, &axis, &axes, &rot_dim, &interleaved)) throw Refused{};
-  if (device != index) refuse("the rotation's frequencies must be on cuda:%lld", (long long)index);
-  if (rot_dim > dim) refuse("rot_dim is larger than head_dim");
-  t.rot.inv_freq = reinterpret_cast<const double*>(freq);
-  t.rot.axis_of_pair = reinterpret_cast<const uint8_t*>(axis);
+  PyObject *freq = nullptr, *axis = nullptr;              // looked at in every call: a Rotary's tensors are the caller's
+  int axes = 0, interleaved = 0;
+  if (!PyArg_ParseTuple(rotary, "OOii", &freq, &axis, &axes, &interleaved)) throw Refused{};
+  const at::Tensor& f = tensor("inv_freq", freq);
+  if (f.scalar_type() != at::kDouble || !f.is_contiguous() || f.get_device() != index) refuse("inv_freq must be contiguous float64 on cuda:%lld", (long long)index);
+  if (2 * f.numel() > dim) refuse("rot_dim is larger than head_dim");
+  const int rot_dim = (int)(2 * f.numel());
+  t.rot.inv_freq = static_cast<const double*>(f.data_ptr());
+  if (none(axis) != (axes <= 1)) refuse("several axes need axis_of_pair");
+  if (!none(axis)) {
+    const at::Tensor& x = tensor("axis_of_pair", axis);
+    if (x.scalar_type() != at::kByte || x.numel() != f.numel() || !x.is_contiguous() || x.get_device() != index)
+      refuse("axis_of_pair must be one uint8 per pair on cuda:%lld", (long long)index);
+    t.rot.axis_of_pair = static_cast<const uint8_t*>(x.data_ptr());
+  }
   t.rot.position_stride = rows;
   t.rot.axes = axes;
   t.rot.rot_dim = rot_dim;

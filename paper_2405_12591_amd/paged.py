@@ -82,11 +82,12 @@ class Rotary:
             raise DQError("axes must be 1..8, with axis_of_pair where there are several")
         if a is not None and (a.dtype != torch.uint8 or a.shape != f.shape or not a.is_contiguous()):
             raise DQError("axis_of_pair must be one uint8 per pair")
-
         if a is not None and a.device != f.device:
             raise DQError("inv_freq and axis_of_pair must be on one device")
-        # what the compiled checks take (the dataclass is frozen, and so are its tensors' places)
-        object.__setattr__(self, "_c", (f.get_device(), f.data_ptr(), 0 if a is None else a.data_ptr(), self.axes, self.rot_dim, int(self.interleaved)))
+
+    @property
+    def _c(self):
+        return self.inv_freq, self.axis_of_pair, self.axes, bool(self.interleaved)   # what the compiled checks take
 
     @property
     def rot_dim(self) -> int:

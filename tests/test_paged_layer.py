@@ -1,0 +1,76 @@
+"""What a program keeps between calls: rotations, layers, the compiled part of the binding.  Most of it on the CPU."""
+import copy
+import io
+import pickle
+
+import pytest
+import torch
+
+DEV = "cuda:0"
+
+
+def _lib():
+    import paper_2405_12591_amd as dq
+    from paper_2405_12591_amd import paged
+    return dq, paged
+
+
+def _copies(r):
+    """Copies by every way a model takes."""
+    buf = io.BytesIO()
+    torch.save(r, buf)
+    buf.seek(0)
+    return {"copy": copy.copy(r), "deepcopy": copy.deepcopy(r), "pickle": pickle.loads(pickle.dumps(r)), "torch": torch.load(buf, weights_only=False),
+            "of a copy": copy.deepcopy(pickle.loads(pickle.dumps(r)))}
+
+
+@pytest.mark.parametrize("sections", [None, (8, 12, 12)])
+def test_a_copied_rotation_hands_over_its_own_tensors(sections):
+    dq, paged = _lib()
+    r = dq.rotary(64, sections=sections, interleaved=True, device="cpu")
+    for how, c in _copies(r).items():
+        assert c is not r and torch.equal(c.inv_freq, r.inv_freq) and c.axes == r.axes and c.interleaved and c.rot_dim == 64, how
+        freq, axis, axes, interleaved = c._c
+        assert freq is c.inv_freq and axis is c.axis_of_pair and axes == c.axes and interleaved is True, how
+
+
+@pytest.mark.gpu
+@pytest.mark.parametrize("sections", [None, (8, 12, 12)])
+def test_a_copied_rotation_turns_by_its_own_frequencies(sections):
+    """The copy's tensors, also after they changed in place or the original's memory holds something else."""
+    dq, _ = _lib()
+    gen = torch.Generator().manual_seed(1)
+    x = torch.randn((20, 3, 64), generator=gen).half().to(DEV)
+    pos = torch.randint(0, 5000, (1 if sections is None else 3, 20), generator=gen).to(torch.int32).to(DEV)
+    r = dq.rotary(64, sections=sections, device=DEV)
+    want, _ = dq.rotate_heads(x, None, pos, r)
+    copies = {n: c for n, c in _copies(r).items() if n != "copy"}
+    r.inv_freq.fill_(0.25)                               # (the original's)
+    if sections is not None:
+        r.axis_of_pair.zero_()
+    for how, c in copies.items():
+        got, _ = dq.rotate_heads(x, None, pos, c)
+        assert torch.equal(got, want), how
+        k = dq.alloc_paged_cache(2, 1, 3, 64, device=DEV)
+        got = dq.paged_append(k, x, x, torch.tensor([0, 20], dtype=torch.int32, device=DEV), torch.tensor([20], dtype=torch.int32, device=DEV),
+                              torch.zeros((1, 1), dtype=torch.int32, device=DEV), q=x, rotary=c, positions=pos)
+        assert torch.equal(got, want), how
+
+
+@pytest.mark.gpu
+def test_a_rotation_whose_tensors_were_exchanged_is_looked_at_again():
+    dq, _ = _lib()
+    x = torch.zeros((2, 1, 64), dtype=torch.float16, device=DEV)
+    pos = torch.zeros(2, dtype=torch.int32, device=DEV)
+    for bad in (torch.zeros(32, device=DEV), torch.zeros(32, dtype=torch.float64), torch.zeros(64, dtype=torch.float64, device=DEV),
+                torch.zeros(64, dtype=torch.float64, device=DEV)[::2], torch.zeros(4, dtype=torch.float64, device=DEV)):
+        r = dq.rotary(64, device=DEV)
+        r.inv_freq.data = bad if bad.is_cuda else r.inv_freq.data
+        if not bad.is_cuda:
+            object.__setattr__(r, "inv_freq", bad)
+        with pytest.raises(dq.DQError):
+            dq.rotate_heads(x, None, pos, r)
+    r = dq.rotary(64, sections=(16, 16), device=DEV)
+    object.__setattr__(r, "axis_of_pair", r.axis_of_pair[:8])
+    with pytest.raises(dq.DQError):
+        dq.rotate_heads(x, None, torch.zeros(4, dtype=torch.int32, device=DEV), r)
