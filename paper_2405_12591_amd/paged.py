@@ -270,11 +270,12 @@ class PagedKVLayer:
             if self.tokens_upper + max_rows > self.max_tokens:
                 raise DQError("the rows exceed the layer's %d tokens per sequence" % self.max_tokens)
         new = 1 if starts is None else starts.diff()
+        q_out = None if q is None else torch.empty(q.shape, dtype=q.dtype, device=q.device)
         self.seq_lens += new
         try:
-            q = paged_append(self.cache, k, v, starts, self.seq_lens, self.page_table, q=q, rotary=rotary, positions=positions,
+            q = paged_append(self.cache, k, v, starts, self.seq_lens, self.page_table, q=q, q_out=q_out, rotary=rotary, positions=positions,
                              q_weight=q_weight, k_weight=k_weight, eps=eps)
-        except DQError:                     # nothing was launched
+        except Exception:                   # whatever it was, nothing was launched
             self.seq_lens -= new
             raise
         self.tokens_upper += max_rows

@@ -74,3 +74,54 @@ def test_a_rotation_whose_tensors_were_exchanged_is_looked_at_again():
     object.__setattr__(r, "axis_of_pair", r.axis_of_pair[:8])
     with pytest.raises(dq.DQError):
         dq.rotate_heads(x, None, torch.zeros(4, dtype=torch.int32, device=DEV), r)
+
+
+class _CacheOnTheHost:
+    """A layer whose cache is never reached."""
+    kv_heads, head_dim, page_tokens, dtype, device, index = 2, 64, 64, torch.float16, torch.device("cpu"), 0
+
+
+def _host_layer(paged, max_tokens=100):
+    layer = object.__new__(paged.PagedKVLayer)
+    layer.batch, layer.q_heads, layer.max_tokens, layer.cache = 2, 4, max_tokens, _CacheOnTheHost()
+    layer.page_table = torch.arange(4, dtype=torch.int32).view(2, 2)
+    layer.seq_lens, layer.tokens_upper = torch.tensor([7, 3], dtype=torch.int32), 7
+    layer._ws, layer._outgrown = None, []
+    return layer
+
+
+@pytest.mark.parametrize("error", [TypeError("eps"), MemoryError(), torch.OutOfMemoryError("no memory"), OverflowError(), RuntimeError("x"), AttributeError("x")])
+def test_lengths_stay_where_they_were_after_any_error(monkeypatch, error):
+    dq, paged = _lib()
+    layer = _host_layer(paged)
+
+    def fails(*a, **k):
+        raise error
+
+    monkeypatch.setattr(paged, "paged_append", fails)
+    rows = torch.zeros((5, 2, 64), dtype=torch.float16)
+    for starts, n in ((None, 1), (torch.tensor([0, 4, 5], dtype=torch.int32), 4)):
+        with pytest.raises(type(error)):
+            layer.append(rows, rows, starts, n)
+        assert layer.seq_lens.tolist() == [7, 3] and layer.tokens_upper == 7
+    monkeypatch.setattr(paged.torch, "empty", fails)     # no room for the queries
+    with pytest.raises(type(error)):
+        layer.append(rows, rows, None, 1, q=rows)
+    assert layer.seq_lens.tolist() == [7, 3]
+
+
+@pytest.mark.gpu
+def test_a_layer_after_arguments_that_are_no_numbers_or_tensors():
+    dq, _ = _lib()
+    layer = dq.PagedKVLayer(2, 4, 2, 64, 100, device=DEV)
+    k = torch.ones((2, 2, 64), dtype=torch.float16, device=DEV)
+    q = torch.ones((2, 4, 64), dtype=torch.float16, device=DEV)
+    layer.append(k, k)
+    for bad in (dict(eps="small", k_weight=k[0, 0]), dict(eps=None, k_weight=k[0, 0]), dict(q="queries"), dict(rotary=3), dict(positions=3, rotary=dq.rotary(64, device=DEV)),
+                dict(q=q.float()), dict(k_weight=5)):
+        with pytest.raises((TypeError, AttributeError, dq.DQError)):
+            layer.append(k, k, **bad)
+        assert layer.seq_lens.tolist() == [1, 1] and layer.tokens_upper == 1, bad
+    layer.append(k, k)
+    assert layer.seq_lens.tolist() == [2, 2]
+    assert (layer.attend(q) == 1).all()
