@@ -493,8 +493,9 @@ int32_t dq_paged_append(const dq_paged_cache* cache, const dq_paged_batch* batch
 /*
  * What the cache stands for: tokens first[b] <= t < seq_lens[b] of every sequence as 16-bit rows,
  * token t of sequence b in row out_starts[b] + t - first[b] of k_out and v_out ([rows, kv_heads, d],
- * batch->rows of them; batch->starts is not used).  first NULL: from 0.  Codes come as c * scale rounded
- * once.  The way from 8-bit pages to a DecoQuant cache (dq_compress_kv_blocks) or to another machine.
+ * batch->rows of them; batch->starts is not used).  first NULL: from 0.  seq_lens are the sequences' own
+ * lengths (they say which page is still a tail); a read that ends earlier is one with fewer rows: tokens
+ * past row out_starts[b+1] - 1 are left out.  Codes come as c * scale rounded once.  The way from 8-bit pages to a DecoQuant cache (dq_compress_kv_blocks) or to another machine.
  */
 int32_t dq_paged_read(const dq_paged_cache* cache, const dq_paged_batch* batch, const int32_t* first,
                       const int32_t* out_starts, const dq_heads* k_out, const dq_heads* v_out,

@@ -205,7 +205,8 @@ def paged_append(cache: PagedCache, k: torch.Tensor, v: torch.Tensor, starts: Op
 def paged_read(cache: PagedCache, first: Optional[torch.Tensor], seq_lens: torch.Tensor, out_starts: torch.Tensor, page_table: torch.Tensor,
                k_out: torch.Tensor, v_out: torch.Tensor, tail_slots: Optional[torch.Tensor] = None):
     """The rows that tokens first[b] <= t < seq_lens[b] of the cache stand for, into k_out and v_out [rows, kv_heads, d]
-    from row out_starts[b] on (dq_paged_read; first None: from 0).  Returns (k_out, v_out)."""
+    from row out_starts[b] to out_starts[b+1] - 1 at most (dq_paged_read; first None: from 0).  seq_lens: the sequences' own lengths, also
+    for a read that ends earlier.  Returns (k_out, v_out)."""
     index = cache.index
     _call(_module.paged_read, index, cache._at, index, first, seq_lens, out_starts, page_table, tail_slots, k_out, v_out)
     return k_out, v_out
@@ -295,16 +296,17 @@ class PagedKVLayer:
                                softmax_scale=softmax_scale, causal=causal, window=window)
 
     def read(self, lengths: Sequence[int]):
-        """The rows the layer stands for, k and v [batch, kv_heads, max(lengths), d]; sequence b's first lengths[b] (host
-        integers, its tokens) are written, the rest is zero.  Goes into KVCacheLayer.prefill (fp16 layers)."""
+        """The rows the layer stands for, k and v [batch, kv_heads, max(lengths), d]; of sequence b the first lengths[b] (host
+        integers) are written, the rest, and what lies behind its tokens, is zero.  Goes into KVCacheLayer.prefill (fp16 layers)."""
         c = self.cache
-        n = max(lengths)
-        k = torch.zeros((self.batch, c.kv_heads, n, c.head_dim), dtype=c.dtype, device=c.device)
+        if len(lengths) != self.batch or min(lengths) < 0:
+            raise DQError("read needs a length for every sequence, none negative")
+        k = torch.zeros((self.batch, c.kv_heads, max(lengths), c.head_dim), dtype=c.dtype, device=c.device)
         v = torch.zeros_like(k)
-        lens = torch.tensor(list(lengths), dtype=torch.int32, device=c.device)
+        rows = torch.tensor([[0, n] for n in lengths], dtype=torch.int32, device=c.device)
+        slots = torch.arange(self.batch, dtype=torch.int32, device=c.device)
         for b in range(self.batch):
-            if lengths[b] > 0:
-                one = torch.tensor([0, lengths[b]], dtype=torch.int32, device=c.device)
-                paged_read(c, None, lens[b:b + 1], one, self.page_table[b:b + 1], k[b].transpose(0, 1), v[b].transpose(0, 1),
-                           tail_slots=torch.tensor([b], dtype=torch.int32, device=c.device))
+            if lengths[b]:                  # (the sequence's own length says which page is its tail, rows[b] where to stop)
+                paged_read(c, None, self.seq_lens[b:b + 1], rows[b], self.page_table[b:b + 1], k[b].transpose(0, 1), v[b].transpose(0, 1),
+                           tail_slots=slots[b:b + 1])
         return k, v

@@ -125,3 +125,33 @@ def test_a_layer_after_arguments_that_are_no_numbers_or_tensors():
     layer.append(k, k)
     assert layer.seq_lens.tolist() == [2, 2]
     assert (layer.attend(q) == 1).all()
+
+
+@pytest.mark.gpu
+@pytest.mark.parametrize("dtype,codes,page", [(torch.float16, torch.int8, 64), (torch.bfloat16, torch.float8_e4m3fn, 128)])
+def test_a_layer_reads_any_prefix(dtype, codes, page):
+    """Prefixes that end inside a quantized page, in the tail, at a page's end, at 0 and behind the tokens: the rows of the whole
+    read, zeros behind them."""
+    dq, _ = _lib()
+    gen = torch.Generator().manual_seed(page)
+    heads, d, lens = 2, 64, [3 * page + 8, page, 17]
+    layer = dq.PagedKVLayer(3, 4, heads, d, 4 * page, page, dtype, codes, DEV)
+    k, v = (torch.randn((sum(lens), heads, d), generator=gen).to(dtype).to(DEV) for _ in range(2))
+    layer.append(k, v, torch.tensor([0, lens[0], lens[0] + lens[1], sum(lens)], dtype=torch.int32, device=DEV), max(lens))
+    whole = layer.read(lens)
+    at = torch.tensor([0, lens[0], lens[0] + lens[1]])
+    for got, x in zip(whole, (k, v)):
+        for b, n in enumerate(lens):
+            # codes of a block are off by half a step of its largest value at most: 1 / 254, or 2^-4 of the value itself
+            err = (got[b, :, :n].transpose(0, 1).float() - x[at[b]:at[b] + n].float()).abs()
+            assert (err <= x.float().abs().max() / 250 + x[at[b]:at[b] + n].float().abs() * 2.0 ** -4 * 1.1).all()
+    for lengths in ([page + 36, page - 1, 3], [2 * page, 1, 17], [3 * page + 1, 0, 0], [1, page, 16], [0, 0, 0], [4 * page, 2 * page, page]):
+        for got, full in zip(layer.read(lengths), whole):
+            assert got.shape[2] == max(lengths)
+            for b, n in enumerate(lengths):
+                m = min(n, lens[b])
+                assert torch.equal(got[b, :, :m], full[b, :, :m]), (lengths, b)
+                assert (got[b, :, m:] == 0).all(), (lengths, b)
+    for bad in ([1, 2], [1, 2, -1], [1, 2, 3, 4]):
+        with pytest.raises(dq.DQError, match="length"):
+            layer.read(bad)
