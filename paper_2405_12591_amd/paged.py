@@ -212,15 +212,23 @@ def paged_read(cache: PagedCache, first: Optional[torch.Tensor], seq_lens: torch
     return k_out, v_out
 
 
-def paged_workspace(cache: PagedCache, batch: int, rows: int, q_heads: int, max_rows: int, max_seq_len: int) -> torch.Tensor:
-    """Workspace of paged_attention for these sizes."""
+def _workspace_bytes(cache: PagedCache, batch: int, rows: int, q_heads: int, max_rows: int, max_seq_len: int) -> int:
     n = lib.dq_paged_workspace_bytes(C.byref(cache.c), batch, rows, q_heads, max_rows, max_seq_len)
     if n == 0:
         raise DQError("dq_paged_workspace_bytes rejected the arguments")
-    ws = torch.empty((n + 15) // 16 * 16, dtype=torch.uint8, device=cache.device)
+    return (n + 15) // 16 * 16
+
+
+def _new_workspace(cache: PagedCache, n: int) -> torch.Tensor:
+    ws = torch.empty(n, dtype=torch.uint8, device=cache.device)
     with torch.cuda.device(cache.device):
         workspace_init(ws)
     return ws
+
+
+def paged_workspace(cache: PagedCache, batch: int, rows: int, q_heads: int, max_rows: int, max_seq_len: int) -> torch.Tensor:
+    """Workspace of paged_attention for these sizes."""
+    return _new_workspace(cache, _workspace_bytes(cache, batch, rows, q_heads, max_rows, max_seq_len))
 
 
 def paged_attention(cache: PagedCache, q: torch.Tensor, starts: Optional[torch.Tensor], seq_lens: torch.Tensor, page_table: torch.Tensor,
@@ -282,17 +290,24 @@ class PagedKVLayer:
         self.tokens_upper += max_rows
         return q
 
+    _fits = (0, 0)                          # rows of a call and of a sequence that the workspace is known to be enough for
+
+    def _make_room(self, rows: int, max_rows: int) -> None:
+        need = _workspace_bytes(self.cache, self.batch, rows, self.q_heads, max_rows, self.max_tokens)
+        if self._ws is None or need > self._ws.numel():
+            if self._ws is not None:
+                self._outgrown.append(self._ws)      # a captured graph may still work in it
+                need = max(need, 2 * self._ws.numel())   # (all that were outgrown together are smaller than the next one)
+            self._ws = _new_workspace(self.cache, need)
+        self._fits = (rows, max_rows)
+
     def attend(self, q: torch.Tensor, starts: Optional[torch.Tensor] = None, max_rows: int = 1, out: Optional[torch.Tensor] = None,
                softmax_scale: float = 0.0, causal: bool = True, window: int = 0) -> torch.Tensor:
         """Attention of the rows just appended, q [rows, q_heads, d] (paged_attention)."""
-        rows, bound = q.shape[0], min(self.tokens_upper, self.max_tokens)
-        if self._ws is None or rows > self._ws[0] or max_rows > self._ws[1]:
-            sizes = (rows, max_rows)
-            if self._ws:
-                sizes = (max(rows, self._ws[0]), max(max_rows, self._ws[1]))
-                self._outgrown.append(self._ws[2])   # a captured graph may still work in it
-            self._ws = (*sizes, paged_workspace(self.cache, self.batch, sizes[0], self.q_heads, sizes[1], self.max_tokens))
-        return paged_attention(self.cache, q, starts, self.seq_lens, self.page_table, max_rows, bound, self._ws[2], out=out,
+        bound = min(self.tokens_upper, self.max_tokens)
+        if q.shape[0] > self._fits[0] or max_rows > self._fits[1]:
+            self._make_room(max(q.shape[0], self._fits[0]), max(max_rows, self._fits[1]))
+        return paged_attention(self.cache, q, starts, self.seq_lens, self.page_table, max_rows, bound, self._ws, out=out,
                                softmax_scale=softmax_scale, causal=causal, window=window)
 
     def read(self, lengths: Sequence[int]):

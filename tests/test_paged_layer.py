@@ -155,3 +155,25 @@ def test_a_layer_reads_any_prefix(dtype, codes, page):
     for bad in ([1, 2], [1, 2, -1], [1, 2, 3, 4]):
         with pytest.raises(dq.DQError, match="length"):
             layer.read(bad)
+
+
+def test_the_workspaces_of_a_layer_stay_within_twice_the_largest(monkeypatch):
+    """Prompts that are each a little longer than the last: a new workspace only where its bytes grew, each at least twice the one before."""
+    dq, paged = _lib()
+    made, given = [], []
+    monkeypatch.setattr(paged, "_new_workspace", lambda cache, n: made.append(n) or torch.empty(n, dtype=torch.uint8))
+    monkeypatch.setattr(paged, "paged_attention", lambda cache, q, starts, lens, table, most, bound, ws, **k: given.append(ws) or q)
+    for kv_heads, d, batch, top in ((8, 128, 8, 4096), (1, 64, 1, 1200), (2, 64, 3, 300)):
+        layer = _host_layer(paged, 8192)
+        layer.batch, layer.q_heads = batch, 4 * kv_heads
+        layer.cache = type("Cache", (), {})()
+        layer.cache.c = paged._CPaged(*[0x1000] * 6, 10, kv_heads, d, 64, 8, 0, 0)
+        made.clear()
+        for rows in [1] + [5 + i * top // 100 for i in range(100)] + [1, 3]:
+            layer.attend(torch.empty((batch * rows, 4 * kv_heads, d), dtype=torch.float16, device="meta"), None, rows)
+            need = dq.lib.dq_paged_workspace_bytes(layer.cache.c, batch, batch * rows, 4 * kv_heads, rows, 8192)
+            assert given[-1].numel() >= need and given[-1] is layer._ws
+        assert sum(made) < 2 * made[-1] and len(made) <= 12, made
+        assert made == sorted(made) and all(b >= 2 * a for a, b in zip(made, made[1:]))
+        assert made[-1] <= 2 * dq.lib.dq_paged_workspace_bytes(layer.cache.c, batch, batch * top, 4 * kv_heads, top, 8192)
+        assert len(layer._outgrown) == len(made) - 1
