@@ -292,22 +292,28 @@ class PagedKVLayer:
 
     _fits = (0, 0)                          # rows of a call and of a sequence that the workspace is known to be enough for
 
-    def _make_room(self, rows: int, max_rows: int) -> None:
+    def _make_room(self, rows: int, max_rows: int) -> torch.Tensor:
         need = _workspace_bytes(self.cache, self.batch, rows, self.q_heads, max_rows, self.max_tokens)
         if self._ws is None or need > self._ws.numel():
+            if torch.cuda.is_current_stream_capturing():
+                # zeroed by the graph's replays only: this call's own, none for calls outside the graph
+                self._outgrown.append(_new_workspace(self.cache, need))
+                return self._outgrown[-1]
             if self._ws is not None:
                 self._outgrown.append(self._ws)      # a captured graph may still work in it
                 need = max(need, 2 * self._ws.numel())   # (all that were outgrown together are smaller than the next one)
             self._ws = _new_workspace(self.cache, need)
         self._fits = (rows, max_rows)
+        return self._ws
 
     def attend(self, q: torch.Tensor, starts: Optional[torch.Tensor] = None, max_rows: int = 1, out: Optional[torch.Tensor] = None,
                softmax_scale: float = 0.0, causal: bool = True, window: int = 0) -> torch.Tensor:
         """Attention of the rows just appended, q [rows, q_heads, d] (paged_attention)."""
         bound = min(self.tokens_upper, self.max_tokens)
+        ws = self._ws
         if q.shape[0] > self._fits[0] or max_rows > self._fits[1]:
-            self._make_room(max(q.shape[0], self._fits[0]), max(max_rows, self._fits[1]))
-        return paged_attention(self.cache, q, starts, self.seq_lens, self.page_table, max_rows, bound, self._ws, out=out,
+            ws = self._make_room(max(q.shape[0], self._fits[0]), max(max_rows, self._fits[1]))
+        return paged_attention(self.cache, q, starts, self.seq_lens, self.page_table, max_rows, bound, ws, out=out,
                                softmax_scale=softmax_scale, causal=causal, window=window)
 
     def read(self, lengths: Sequence[int]):

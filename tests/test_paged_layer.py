@@ -177,3 +177,49 @@ def test_the_workspaces_of_a_layer_stay_within_twice_the_largest(monkeypatch):
         assert made == sorted(made) and all(b >= 2 * a for a, b in zip(made, made[1:]))
         assert made[-1] <= 2 * dq.lib.dq_paged_workspace_bytes(layer.cache.c, batch, batch * top, 4 * kv_heads, top, 8192)
         assert len(layer._outgrown) == len(made) - 1
+
+
+def test_a_workspace_made_in_a_capture_is_for_that_call_alone(monkeypatch):
+    dq, paged = _lib()
+    given = []
+    monkeypatch.setattr(paged, "_new_workspace", lambda cache, n: torch.empty(n, dtype=torch.uint8))
+    monkeypatch.setattr(paged, "paged_attention", lambda cache, q, starts, lens, table, most, bound, ws, **k: given.append(ws) or q)
+    layer = _host_layer(paged, 8192)
+    layer.cache = type("Cache", (), {})()
+    layer.cache.c = paged._CPaged(*[0x1000] * 6, 10, 1, 64, 64, 8, 0, 0)
+    q = [torch.empty((2 * n, 4, 64), dtype=torch.float16, device="meta") for n in (1, 300)]
+    for capturing in (True, False, True, True, False):
+        monkeypatch.setattr(paged.torch.cuda, "is_current_stream_capturing", lambda: capturing)
+        layer.attend(q[0], None, 1)
+    layer.attend(q[1], None, 300)
+    assert given[0] is layer._outgrown[0] and given[0] is not given[1]           # the first call was captured
+    assert all(x is given[1] for x in given[1:5])                               # there was one from then on
+    monkeypatch.setattr(paged.torch.cuda, "is_current_stream_capturing", lambda: True)
+    kept = layer._ws
+    layer.attend(torch.empty((2000, 4, 64), dtype=torch.float16, device="meta"), None, 1000)
+    assert layer._ws is kept and given[-1] is layer._outgrown[-1] or given[-1] is kept
+
+
+@pytest.mark.gpu
+def test_a_layer_whose_first_attention_is_captured():
+    """Outside the graph and in its replays, in any order, the results of a layer that was never captured."""
+    dq, _ = _lib()
+    gen = torch.Generator().manual_seed(5)
+    heads, hq, d, n = 1, 4, 64, 3000
+    k, v = (torch.randn((2 * n, heads, d), generator=gen).half().to(DEV) for _ in range(2))
+    q = torch.randn((2, hq, d), generator=gen).half().to(DEV)
+    starts = torch.tensor([0, n, 2 * n], dtype=torch.int32, device=DEV)
+    layer, plain = (dq.PagedKVLayer(2, hq, heads, d, 4000, device=DEV) for _ in range(2))
+    for x in (layer, plain):
+        x.append(k, v, starts, n)
+    want = plain.attend(q)
+    stream, graph = torch.cuda.Stream(), torch.cuda.CUDAGraph()
+    torch.cuda.synchronize()
+    with torch.cuda.graph(graph, stream=stream):
+        out = layer.attend(q)
+    for _ in range(3):
+        assert torch.equal(layer.attend(q), want)        # before the first replay too
+        out.zero_()
+        graph.replay()
+        torch.cuda.synchronize()
+        assert torch.equal(out, want)
