@@ -161,6 +161,7 @@ def test_the_workspaces_of_a_layer_stay_within_twice_the_largest(monkeypatch):
     """Prompts that are each a little longer than the last: a new workspace only where its bytes grew, each at least twice the one before."""
     dq, paged = _lib()
     made, given = [], []
+    monkeypatch.setattr(paged.torch.cuda, "is_current_stream_capturing", lambda: False)      # (raises where there is no GPU)
     monkeypatch.setattr(paged, "_new_workspace", lambda cache, n: made.append(n) or torch.empty(n, dtype=torch.uint8))
     monkeypatch.setattr(paged, "paged_attention", lambda cache, q, starts, lens, table, most, bound, ws, **k: given.append(ws) or q)
     for kv_heads, d, batch, top in ((8, 128, 8, 4096), (1, 64, 1, 1200), (2, 64, 3, 300)):
