@@ -485,6 +485,11 @@ typedef struct dq_paged_batch {
  * 16 bits and buffered or, with the whole of their page, quantized; values go as they are.  q (NULL:
  * none), [rows, q_heads, d], takes the same norm and rotation in the same launch, into q_out (q itself
  * will do).  One launch; page_table must name the pages that fill in this call.
+ * Lengths may go back (drafted tokens that are refused): within the page being filled, and to the end of a
+ * page, by a smaller seq_lens alone.  A page that was quantized is no tail again by that: its rows were
+ * appended to its codes, and the tail holds other tokens.  To end inside such a page at length n, read its
+ * rows n / P * P .. n - 1 with dq_paged_read and the length they were appended with, then append them (no
+ * norm, no rotation) with seq_lens n.
  */
 int32_t dq_paged_append(const dq_paged_cache* cache, const dq_paged_batch* batch, const dq_heads* k,
                         const dq_heads* v, const dq_heads* q, const dq_heads* q_out,

@@ -190,7 +190,8 @@ def paged_append(cache: PagedCache, k: torch.Tensor, v: torch.Tensor, starts: Op
     """Append the rows k, v [rows, kv_heads, d] of a ragged batch (dq_paged_append); keys, and q beside them, are normed
     and rotated on the way.  starts: int32 [batch + 1], rows starts[b] .. starts[b+1] - 1 are sequence b's last tokens
     (None: one row each); seq_lens: int32, the new rows included; page_table: int32 [batch, pages].  positions None: a
-    token's place in its sequence.  Returns q_out (None without q)."""
+    token's place in its sequence.  Returns q_out (None without q).  seq_lens may go back later within the page being filled or to
+    a page's end; into a page that was quantized as PagedKVLayer.shorten does it."""
     if q is None:
         if q_out is not None:
             raise DQError("q_out without q")
@@ -315,6 +316,26 @@ class PagedKVLayer:
             ws = self._make_room(max(q.shape[0], self._fits[0]), max(max_rows, self._fits[1]))
         return paged_attention(self.cache, q, starts, self.seq_lens, self.page_table, max_rows, bound, ws, out=out,
                                softmax_scale=softmax_scale, causal=causal, window=window)
+
+    def shorten(self, lengths: Sequence[int]) -> None:
+        """Drop tokens from the ends: sequence b keeps its first lengths[b] (host integers; 0 empties it), after drafted tokens
+        were refused or a sequence ended.  In the page being filled nothing moves, and what is appended next gives the bits it
+        would have given without them; where a page that was quantized becomes the last one again, its rows go back to the
+        tail as what their codes stand for.  Looks at the device's lengths, so not for captures."""
+        c, page = self.cache, self.cache.page_tokens
+        have = [min(n, self.page_table.shape[1] * page) for n in self.seq_lens.tolist()]
+        if len(lengths) != self.batch or any(not 0 <= n <= h for n, h in zip(lengths, have)):
+            raise DQError("shorten needs a length for every sequence, at most its tokens")
+        back = [n % page if n // page < h // page else 0 for n, h in zip(lengths, have)]
+        lens = torch.tensor(list(lengths), dtype=torch.int32, device=c.device)
+        if any(back):
+            first = torch.tensor([n - b for n, b in zip(lengths, back)], dtype=torch.int32, device=c.device)
+            starts = torch.tensor([sum(back[:b]) for b in range(self.batch + 1)], dtype=torch.int32, device=c.device)
+            k, v = (torch.empty((sum(back), c.kv_heads, c.head_dim), dtype=c.dtype, device=c.device) for _ in range(2))
+            paged_read(c, first, self.seq_lens, starts, self.page_table, k, v)
+            paged_append(c, k, v, starts, lens, self.page_table)
+        self.seq_lens.copy_(lens)
+        self.tokens_upper = max(lengths)
 
     def read(self, lengths: Sequence[int]):
         """The rows the layer stands for, k and v [batch, kv_heads, max(lengths), d]; of sequence b the first lengths[b] (host
