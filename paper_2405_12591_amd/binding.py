@@ -70,6 +70,9 @@ def _load() -> C.CDLL:
     l.dq_version.restype = C.c_int32
     if int(l.dq_version()) != ABI_VERSION:   # the structs below would not match the library's
         raise DQError("%s is version %d, this binding needs %d: rebuild it" % (path, int(l.dq_version()), ABI_VERSION))
+    missing = [n for n in EXPORTED_SYMBOLS if not hasattr(l, n)]   # (functions are added within a version)
+    if missing:
+        raise DQError("%s lacks %s: rebuild it" % (path, ", ".join(missing)))
     l.dq_status_string.restype = C.c_char_p
     l.dq_status_string.argtypes = [C.c_int32]
     l.dq_last_hip_error.restype = C.c_int32

@@ -100,6 +100,19 @@ def build_library(verbose: bool = False, timeline: bool = False) -> str:
     return out_path
 
 
+BIND_SOURCES = [os.path.join(PKG_DIR, "csrc", "paged_bind.cpp"), os.path.join(ROOT, "include", "decoquant.h")]
+
+
+def bind_stamp() -> str:
+    """What the compiled part of the binding carries of its sources (the header's structs among them)."""
+    import hashlib
+    h = hashlib.sha256()
+    for path in BIND_SOURCES:
+        with open(path, "rb") as f:
+            h.update(f.read())
+    return h.hexdigest()[:32]
+
+
 def build_binding() -> str:
     """Compile csrc/paged_bind.cpp, the tensor checks of paged.py, as the Python module _paged."""
     import importlib.util
@@ -109,7 +122,7 @@ def build_binding() -> str:
     rc, log = _run([os.environ.get("CXX", "g++"), "-O2", "-std=c++17", "-fPIC", "-shared", "-fvisibility=hidden",
                     *("-I" + p for p in (os.path.join(ROOT, "include"), inc, os.path.join(inc, "torch", "csrc", "api", "include"),
                                          sysconfig.get_paths()["include"])),
-                    os.path.join(PKG_DIR, "csrc", "paged_bind.cpp"), "-L" + libs, "-ltorch_python", "-ltorch_cpu", "-ltorch", "-lc10",
+                    '-DDQ_BIND_STAMP="%s"' % bind_stamp(), BIND_SOURCES[0], "-L" + libs, "-ltorch_python", "-ltorch_cpu", "-ltorch", "-lc10",
                     "-o", BIND_PATH + ".tmp"])
     if rc != 0:
         raise RuntimeError("the binding's compiled part does not build:\n" + log)

@@ -329,4 +329,11 @@ PyModuleDef g_module = {PyModuleDef_HEAD_INIT, "_paged", nullptr, -1, g_methods}
 
 }  // namespace
 
-PyMODINIT_FUNC PyInit__paged(void) { return PyModule_Create(&g_module); }
+PyMODINIT_FUNC PyInit__paged(void) {
+  PyObject* const m = PyModule_Create(&g_module);
+  if (m && PyModule_AddStringConstant(m, "stamp", DQ_BIND_STAMP)) {   // of the sources it was built from
+    Py_DECREF(m);
+    return nullptr;
+  }
+  return m;
+}

@@ -44,12 +44,26 @@ def _load_module():
     if not os.path.exists(_build.BIND_PATH):
         _build.build_binding()
     from . import _paged
+    if getattr(_paged, "stamp", None) != _build.bind_stamp():   # its structs would not match the library's
+        raise DQError("%s was built from other sources: rebuild it" % _build.BIND_PATH)
     _paged.set_up(DQError, _check, *(C.cast(getattr(lib, n), C.c_void_p).value
                                      for n in ("dq_rotate_heads", "dq_paged_append", "dq_paged_read", "dq_paged_attention")))
     return _paged
 
 
-_module = _load_module()
+class _Module:
+    """The compiled checks, loaded (and built where they are missing) with their first use: callers of the rest need neither them nor g++."""
+
+    def __getattr__(self, name):
+        if name.startswith("_"):
+            raise AttributeError(name)
+        loaded = _load_module()
+        for n in ("rotate_heads", "paged_append", "paged_read", "paged_attention"):
+            setattr(self, n, getattr(loaded, n))
+        return getattr(loaded, name)
+
+
+_module = _Module()
 _current_device = getattr(torch._C, "_cuda_getDevice", None) or torch.cuda.current_device
 
 
