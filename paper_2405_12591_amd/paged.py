@@ -1,5 +1,6 @@
 """Binding of the head norm and rotation and of the paged 8-bit cache (include/decoquant.h): argument
-checks and marshalling only, the checks of tensors in csrc/paged_bind.cpp."""
+checks and marshalling only, the checks of tensors in csrc/paged_bind.cpp.  These operators serve: tensors that require gradients are
+taken as they are, outputs carry none, and what is written in place (an output that is its own input, a cache) is not recorded."""
 from __future__ import annotations
 
 import ctypes as C
@@ -130,7 +131,7 @@ def rotate_heads(q: Optional[torch.Tensor], k: Optional[torch.Tensor], positions
     """RMS norm (where a weight is given) and rotation of query and key heads, fp16 or bf16, in one pass
     (dq_rotate_heads); returns (q_out, k_out).  q, k: [rows, heads, d] or [batch, rows, heads, d], any strides with
     channels side by side (views of a fused projection, transposed layouts); either may be None.  positions:
-    int32, one per row ([axes, ...] with several axes).  An output may be its own input."""
+    int32, one per row ([axes, ...] with several axes).  An output may be its own input.  No gradients."""
     first = q if q is not None else k
     if first is None:
         raise DQError("rotate_heads needs q or k")
@@ -204,7 +205,7 @@ def paged_append(cache: PagedCache, k: torch.Tensor, v: torch.Tensor, starts: Op
     """Append the rows k, v [rows, kv_heads, d] of a ragged batch (dq_paged_append); keys, and q beside them, are normed
     and rotated on the way.  starts: int32 [batch + 1], rows starts[b] .. starts[b+1] - 1 are sequence b's last tokens
     (None: one row each); seq_lens: int32, the new rows included; page_table: int32 [batch, pages].  positions None: a
-    token's place in its sequence.  Returns q_out (None without q).  seq_lens may go back later within the page being filled or to
+    token's place in its sequence.  Returns q_out (None without q).  No gradients.  seq_lens may go back later within the page being filled or to
     a page's end; into a page that was quantized as PagedKVLayer.shorten does it."""
     if q is None:
         if q_out is not None:
@@ -251,7 +252,7 @@ def paged_attention(cache: PagedCache, q: torch.Tensor, starts: Optional[torch.T
                     causal: bool = True, window: int = 0, tail_slots: Optional[torch.Tensor] = None, splits: int = 0) -> torch.Tensor:
     """softmax(q . K * scale) V of the batch's rows q [rows, q_heads, d] over the cached tokens of their sequences
     (dq_paged_attention); rows are the last tokens of their sequence (append them first).  max_rows: host bound on the
-    rows of any sequence; max_seq_len: on its tokens (a guess does).  window > 0: the last `window` tokens only.  out may be q.
+    rows of any sequence; max_seq_len: on its tokens (a guess does).  window > 0: the last `window` tokens only.  out may be q.  No gradients.
     splits: launch override for sweeps (DQ_PAGED_SPLITS)."""
     if out is None:
         out = torch.empty(q.shape, dtype=q.dtype, device=q.device)

@@ -224,3 +224,18 @@ def test_a_layer_whose_first_attention_is_captured():
         graph.replay()
         torch.cuda.synchronize()
         assert torch.equal(out, want)
+
+
+@pytest.mark.gpu
+def test_tensors_that_require_gradients_are_taken_and_outputs_carry_none():
+    dq, paged = _lib()
+    x = torch.ones((2, 2, 64), dtype=torch.float16, device=DEV, requires_grad=True)
+    w = torch.ones(64, dtype=torch.float16, device=DEV, requires_grad=True)
+    q, _ = dq.rotate_heads(x, None, q_weight=w)
+    assert not q.requires_grad
+    layer = dq.PagedKVLayer(2, 2, 2, 64, 64, device=DEV)
+    q = layer.append(x, x, q=x, k_weight=w, q_weight=w)
+    out = layer.attend(q)
+    assert not q.requires_grad and not out.requires_grad and (out == 1).all()
+    for f in (dq.rotate_heads, dq.paged_append, dq.paged_attention):
+        assert "No gradients" in f.__doc__
