@@ -246,3 +246,60 @@ def test_blocks_of_zero_values_beside_small_ones(dtype, codes, page, new, small)
         err = (out[at].double() - want).abs()
         assert (err <= tol).all(), (b, float((err / tol).max()))
     assert (out[3 * new:] == 0).all()
+
+
+# ---------------------------------------------------------------------------------------- what stands in a tile beside a bad row
+@pytest.mark.parametrize("dtype,codes", PAIRS)
+def test_rows_of_a_decode_call_before_and_behind_a_row_that_is_not_finite(dtype, codes):
+    """Rows of one call of the kernel for few rows: those before the bad token of the tail, those whose window has left it or its
+    quantized block, and those that see it."""
+    gen = torch.Generator().manual_seed(51)
+    heads, group, d, page, n = 2, 2, 64, 64, 150
+    seqs = Sequences([n], heads, d, dtype, codes, page, gen)
+    seqs.k[0][145, 0, 3] = float("inf")                   # in the tail, seen by the second half of the rows
+    seqs.v[0][70, 1, 9] = float("nan")                    # in a page
+    cache, table, slots = filled_cache(seqs, [n], gen)
+    good = Sequences([n], heads, d, dtype, codes, page, torch.Generator().manual_seed(51))
+    good.k[0][145, 0, 3] = 0                              # (never compared: the rows that see it are NaN)
+    new = 8                                               # 16 columns
+    q = rows((new, heads * group, d), dtype, gen, outliers=False)
+    place = torch.arange(n - new, n)
+    ws = dq.paged_workspace(cache, 1, new, heads * group, new, n)
+    for window in (0, 19, 5, 3):
+        out = dq.paged_attention(cache, q.to(DEV), ints([0, new]), ints([n]), table, new, n, ws, window=window, tail_slots=slots).cpu()
+        from_ = place + 1 - window if window else torch.zeros_like(place)
+        bad = torch.zeros(new, heads * group, dtype=torch.bool)
+        bad[:, :group] = ((place >= 145) & (from_ <= 145))[:, None]
+        bad[:, group:] = (from_ < 128)[:, None]           # the block of tokens 64 to 127
+        assert torch.equal(torch.isnan(out).any(-1), bad) and torch.equal(torch.isnan(out).all(-1), bad), window
+        k, v = good.stored(good.k[0]), good.stored(good.v[0])
+        want, size, ds = attend64(q, k, v, place, True, window, 1 / math.sqrt(d))
+        tol = attend_tolerance(want, size, ds, float(v.abs().max()), n, dtype, True)
+        assert ((out.double() - want).abs() <= tol)[~bad].all(), window
+
+
+@pytest.mark.parametrize("dtype,codes", [(F16, INT8), (BF16, E4M3), (BF16, INT8)])
+@pytest.mark.parametrize("new", [4, 60])
+def test_probabilities_over_code_pages_have_eleven_bits(dtype, codes, new):
+    """Two tokens of opposite values nearly cancel, so the result shows what their probabilities were rounded to: half a step
+    of 16-bit floats, whatever the rows' type."""
+    heads, hq, d, page = 1, 4, 64, 64
+    gen = torch.Generator().manual_seed(52)
+    seqs = Sequences([page], heads, d, dtype, codes, page, gen)
+    k, v = torch.zeros(page, 1, d), torch.zeros(page, 1, d)
+    k[:, 0, 0] = -4
+    k[3, 0, 0], k[40, 0, 0] = 4, 4
+    k[40, 0, 1] = -1
+    v[3], v[40] = 1, -1                                   # the others add nothing to the result
+    seqs.k[0], seqs.v[0] = k.to(dtype), v.to(dtype)
+    cache, table, slots = filled_cache(seqs, [page], gen)
+    q = torch.zeros(new, hq, d)
+    q[..., 0] = 8
+    q[..., 1] = 0.32 * torch.rand(new, hq, generator=gen)   # p = 1 and about exp(-q1 / 8): in bf16 0.96 to 1 has eleven numbers
+    q = q.to(dtype)
+    ws = dq.paged_workspace(cache, 1, new, hq, new, page)
+    out = dq.paged_attention(cache, q.to(DEV), ints([0, new]), ints([page]), table, new, page, ws, causal=False, tail_slots=slots).cpu()
+    kk, vv = seqs.stored(seqs.k[0]), seqs.stored(seqs.v[0])
+    want, size, ds = attend64(q, kk, vv, torch.arange(new), False, 0, 1 / math.sqrt(d))
+    tol = attend_tolerance(want, size, ds, 1.0, page, dtype, False)
+    assert ((out.double() - want).abs() <= tol).all(), float(((out.double() - want).abs() / tol).max())
