@@ -456,7 +456,7 @@ extern "C" int32_t dq_paged_append(const dq_paged_cache* cache, const dq_paged_b
   if (q) { a.q = *q; a.q_out = *q_out; }
   if (norm) a.norm = *norm;
   if (rot) a.rot = *rot;
-  const int rows_per_block = cache->page_tokens;
+  const long rows_per_block = cache->page_tokens;
   const long items = batch->rows / cache->page_tokens + 2l * batch->batch;
   const long q_items = q ? (batch->rows + rows_per_block - 1) / rows_per_block : 0;
   // Heads that share a page's angles: four where pages alone take the place of every resident workgroup (16 waves a compute
@@ -464,12 +464,13 @@ extern "C" int32_t dq_paged_append(const dq_paged_cache* cache, const dq_paged_b
   // thousand of 8 heads 53 (63 with one).  Eight: 3 % faster with query rows beside large pages, up to 10 % slower on pages of 64.
   const int resident = (1 << 18) / (cache->page_tokens * cache->head_dim / 16);
   int per = 4, q_per = 8;
-  while (per > 1 && items * ((cache->kv_heads + per - 1) / per) < resident) per /= 2;
-  while (q && q_per > 1 && q_items * ((q->heads + q_per - 1) / q_per) < 1024) q_per /= 2;
+  auto groups = [](long heads, int each) { return (int)((heads + each - 1) / each); };
+  while (per > 1 && items * groups(cache->kv_heads, per) < resident) per /= 2;
+  while (q && q_per > 1 && q_items * groups(q->heads, q_per) < 1024) q_per /= 2;
   a.heads_per_group = per;
-  a.head_groups = (cache->kv_heads + per - 1) / per;
+  a.head_groups = groups(cache->kv_heads, per);
   a.q_heads_per_group = q_per;
-  a.q_head_groups = q ? (q->heads + q_per - 1) / q_per : 1;
+  a.q_head_groups = q ? groups(q->heads, q_per) : 1;
   const long page_blocks = items * a.head_groups, blocks = page_blocks + q_items * a.q_head_groups;
   if (blocks * (cache->page_tokens * cache->head_dim / 16) >= kMaxThreads) return DQ_EINVAL;
   a.page_blocks = (int)page_blocks;

@@ -89,13 +89,14 @@ extern "C" int32_t dq_rotate_heads(const dq_heads* q, const dq_heads* q_out, con
   int lanes = 2;
   while (16 * lanes < head_dim) lanes *= 2;
   const long groups = (rows + kPagedThreads / lanes - 1) / (kPagedThreads / lanes);
-  const int heads = a.q.heads + a.k.heads;
+  const long heads = (long)a.q.heads + a.k.heads;
   // Heads a workgroup takes: eight share the angles where the rows alone fill the chip, fewer where they do not.
   int per = 8;
   while (per > 1 && groups * ((heads + per - 1) / per) < 1024) per /= 2;
   a.heads_per_group = per;
-  a.head_groups = (heads + per - 1) / per;
-  if (groups * a.head_groups >= kMaxThreads / kPagedThreads) return DQ_EINVAL;
+  const long head_groups = (heads + per - 1) / per;
+  if (heads > INT32_MAX || groups * head_groups >= kMaxThreads / kPagedThreads) return DQ_EINVAL;
+  a.head_groups = (int)head_groups;
   const dim3 grid((unsigned)(groups * a.head_groups));
   if (dtype == DQ_BF16) launch_rotate<__bf16>(a, lanes, grid, (hipStream_t)hip_stream);
   else launch_rotate<_Float16>(a, lanes, grid, (hipStream_t)hip_stream);
