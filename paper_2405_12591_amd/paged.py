@@ -113,8 +113,8 @@ def rotary(rot_dim: int, base: float = 10000.0, sections: Optional[Sequence[int]
            device="cuda:0") -> Rotary:
     """The usual frequencies base^(-2i / rot_dim).  sections: pairs per axis, one run of pairs after the
     other (time, height, width, ...), summing to rot_dim / 2."""
-    if rot_dim <= 0 or rot_dim % 16:
-        raise DQError("rot_dim must be a multiple of 16")
+    if rot_dim <= 0 or rot_dim % 16 or not float(base) > 0:
+        raise DQError("rot_dim must be a multiple of 16, base positive")
     half = rot_dim // 2
     inv = float(base) ** (-torch.arange(half, dtype=torch.float64) / half)
     axis = None
@@ -272,8 +272,8 @@ class PagedKVLayer:
 
     def __init__(self, batch: int, q_heads: int, kv_heads: int, head_dim: int, max_tokens: int, page_tokens: int = 64,
                  dtype=torch.float16, codes=torch.int8, device="cuda:0"):
-        if batch < 1 or max_tokens < 1 or q_heads < 1 or q_heads % kv_heads:
-            raise DQError("a layer has sequences, room for tokens and q_heads a multiple of kv_heads")
+        if min(batch, max_tokens, q_heads, kv_heads) < 1 or q_heads % kv_heads or page_tokens not in (64, 128):
+            raise DQError("a layer has sequences, room for tokens, q_heads a multiple of kv_heads and pages of 64 or 128 tokens")
         self.batch, self.q_heads, self.max_tokens = batch, q_heads, max_tokens
         width = -(-max_tokens // page_tokens)
         self.cache = alloc_paged_cache(batch * width, batch, kv_heads, head_dim, page_tokens, dtype, codes, device)

@@ -239,3 +239,15 @@ def test_tensors_that_require_gradients_are_taken_and_outputs_carry_none():
     assert not q.requires_grad and not out.requires_grad and (out == 1).all()
     for f in (dq.rotate_heads, dq.paged_append, dq.paged_attention):
         assert "No gradients" in f.__doc__
+
+
+def test_a_layer_and_a_rotation_refuse_sizes_that_make_no_sense():
+    """Before anything is allocated, by the package's own error."""
+    dq, _ = _lib()
+    good = dict(batch=2, q_heads=4, kv_heads=2, head_dim=64, max_tokens=100, device="cpu")
+    for bad in (dict(batch=0), dict(q_heads=0), dict(kv_heads=0), dict(kv_heads=-2), dict(kv_heads=3), dict(max_tokens=0), dict(page_tokens=0), dict(page_tokens=96)):
+        with pytest.raises(dq.DQError, match="a layer has"):
+            dq.PagedKVLayer(**dict(good, **bad))
+    for base in (0, -10.0, float("nan")):
+        with pytest.raises(dq.DQError, match="base"):
+            dq.rotary(64, base=base, device="cpu")
