@@ -404,7 +404,7 @@ typedef struct dq_head_norm {
 /* Position rotation of the first rot_dim channels: pair i turns by positions[axis][token] * inv_freq[i].
  * The angle is formed in fp64 (far positions keep their phase). */
 typedef struct dq_rotary {
-  const double* inv_freq;      /* f64 [rot_dim / 2], radians per position                             */
+  const double* inv_freq;      /* f64 [rot_dim / 2], radians per position; angles stay below 2^50     */
   const int32_t* positions;    /* i32 [axes, position_stride]; a token's column is its place among all
                                   rows of the call (sequence by sequence); any value.
                                   NULL (dq_paged_append only, one axis): a token's place in its sequence */

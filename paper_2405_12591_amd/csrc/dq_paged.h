@@ -178,14 +178,15 @@ __device__ __forceinline__ RowLayout row_layout(int unit, int rot_dim, int inter
   return l;
 }
 
-// Cosine and sine of t turns.  What is left of t after its whole quarters, r in [-1/2, 1/2] quarters, is formed in fp64
-// (the largest position, 2^31, keeps 2^-24 turns) and rounded once; the Taylor polynomials of degree 9 and 10 on
-// |r pi / 2| <= pi / 4 are cut off at 2e-9 and 5e-10, below fp32's rounding.  (The hardware's sine and cosine are off by 2^-20 or so,
-// which turned ten times as many 16-bit roundings as fp32 does.)
+// Cosine and sine of t quarter turns (|t| < 2^51).  t + 1.5 2^52 has the quarters nearest to t in its last bits; what is left of t,
+// in [-1/2, 1/2], comes in fp64 (the largest position, 2^31, keeps 2^-24 turns) and is rounded once, as an angle x, |x| <= pi / 4.
+// The Taylor polynomials of degree 9 and 10 are cut off at 2e-9 and 5e-10, below fp32's rounding, and end in one rounding of
+// 1 - .. or x - ..: sine and cosine are off by about one unit of 2^-24.  (The hardware's are off by 2^-20 or so, which turned ten times as
+// many 16-bit roundings; an angle rounded three times a quarter more: 1.8e-4 of fp16 results instead of 1.5e-4.)
 __device__ __forceinline__ void turn(double t, float* cs, float* sn) {
-  const double q = 4.0 * (t - __builtin_rint(t)), k = __builtin_rint(q);
-  const float x = (float)(q - k) * 1.57079632679489662f, z = x * x;
-  const int quarter = (int)k;
+  const double whole = 6755399441055744.0, k = t + whole;
+  const int quarter = (int)(uint32_t)__builtin_bit_cast(uint64_t, k);
+  const float x = (float)((t - (k - whole)) * 1.57079632679489662), z = x * x;
   float s = __builtin_fmaf(z, 1.0f / 362880, -1.0f / 5040), c = __builtin_fmaf(z, -1.0f / 3628800, 1.0f / 40320);
   s = __builtin_fmaf(z, s, 1.0f / 120);
   c = __builtin_fmaf(z, c, -1.0f / 720);
@@ -230,7 +231,7 @@ __device__ __forceinline__ void make_turns(const RowLayout& l, const UnitTurns& 
   if (l.pair0 < 0) return;
 #pragma unroll
   for (int i = 0; i < 8; ++i) {
-    turn((double)t.p[i] * (t.f[i] * 0.15915494309189533577), cs + i, sn + i);
+    turn((double)t.p[i] * (t.f[i] * 0.63661977236758134308), cs + i, sn + i);
     if (i & 1) __builtin_amdgcn_sched_barrier(0);         // two pairs at a time: eight in a row hold 60 registers more
   }
 }
