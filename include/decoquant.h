@@ -484,7 +484,8 @@ typedef struct dq_paged_batch {
  * fused projection).  Keys are normed and rotated (norm, rot: NULL for rows that are ready), rounded to
  * 16 bits and buffered or, with the whole of their page, quantized; values go as they are.  q (NULL:
  * none), [rows, q_heads, d], takes the same norm and rotation in the same launch, into q_out (q itself
- * will do).  One launch; page_table must name the pages that fill in this call.
+ * will do).  One launch; page_table must name the pages that fill in this call (sequences may share full
+ * pages, but no page fills for two of them).
  * Lengths may go back (drafted tokens that are refused): within the page being filled, and to the end of a
  * page, by a smaller seq_lens alone.  A page that was quantized is no tail again by that: its rows were
  * appended to its codes, and the tail holds other tokens.  To end inside such a page at length n, read its

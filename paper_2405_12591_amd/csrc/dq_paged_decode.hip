@@ -224,6 +224,7 @@ __global__ __launch_bounds__(64 * WAVES, 2) void paged_decode_kernel(PagedAttnAr
       const int tile = batch0 + i * stride;
       if (tile * kPagedTile < all_lo || tile * kPagedTile + kPagedTile > all_hi) softmax(u, tile, keep_sign(f * sc), add, inv_sv, Masked{});
       else softmax(u, tile, keep_sign(f * sc), add, inv_sv, Whole{});
+      // 11 bits, as the codes' products want them (the sum keeps fp32): the error of one more fp16 rounding a token
       f16x8 p0, p1;
 #pragma unroll
       for (int j = 0; j < 8; ++j) { p0[j] = (_Float16)u[j]; p1[j] = (_Float16)u[8 + j]; }
@@ -268,6 +269,7 @@ __global__ __launch_bounds__(64 * WAVES, 2) void paged_decode_kernel(PagedAttnAr
     uint32_t keep[8];                                     // rows behind the last token may hold anything: 0 * NaN is not 0
 #pragma unroll
     for (int j = 0; j < 8; ++j) keep[j] = keep_tokens(~0u, left - 16 * G - 2 * j);
+    // in the rows' type, which their products need: 8 bits with bf16 rows, one more such rounding for each of the page's tokens
     u32x4 p0, p1;
 #pragma unroll
     for (int j = 0; j < 4; ++j) { p0[j] = pack2<T>(u[2 * j], u[2 * j + 1]); p1[j] = pack2<T>(u[8 + 2 * j], u[8 + 2 * j + 1]); }

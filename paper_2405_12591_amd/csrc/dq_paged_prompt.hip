@@ -163,7 +163,8 @@ __global__ __launch_bounds__(64 * kPromptWaves, 2) void paged_prompt_kernel(Page
     }
     const float base = m == -INFINITY ? add : add - m;
     float sum = 0.f;
-    // Probabilities of 16 tokens (8 a lane) are made between the products of the 16 before them.
+    // Probabilities of 16 tokens (8 a lane) are made between the products of the 16 before them; in the products' type (f16 over
+    // codes, the rows' own over the tail), the sum in fp32.
     ex8 p, p_next;
     auto probabilities = [&](int g, ex8& to) __attribute__((always_inline)) {
       float x[8];

@@ -303,3 +303,26 @@ def test_probabilities_over_code_pages_have_eleven_bits(dtype, codes, new):
     want, size, ds = attend64(q, kk, vv, torch.arange(new), False, 0, 1 / math.sqrt(d))
     tol = attend_tolerance(want, size, ds, 1.0, page, dtype, False)
     assert ((out.double() - want).abs() <= tol).all(), float(((out.double() - want).abs() / tol).max())
+
+
+@pytest.mark.parametrize("dtype,codes", PAIRS)
+@pytest.mark.parametrize("group,new", [(17, 1), (32, 1), (64, 1), (8, 3), (4, 5), (64, 3), (130, 2), (3, 6)])
+def test_more_columns_than_the_decode_kernel_takes(dtype, codes, group, new):
+    """Few rows of many query heads on a kv head, long and short and empty sequences, with a window."""
+    gen = torch.Generator().manual_seed(group + new)
+    heads, d, lens = 2, 64, [5000, new, 0, 64, 333]
+    have = [new, new, 0, new, 1]
+    seqs = Sequences(lens, heads, d, dtype, codes, 64, gen)
+    cache, table, slots = filled_cache(seqs, lens, gen)
+    q = rows((sum(have), heads * group, d), dtype, gen, outliers=False)
+    ws = dq.paged_workspace(cache, 5, sum(have), heads * group, new, max(lens))
+    for window in (0, 100):
+        out = dq.paged_attention(cache, q.to(DEV), ints(_sums(have)), ints(lens), table, new, max(lens), ws, window=window, tail_slots=slots).cpu()
+        at = 0
+        for b, n in enumerate(have):
+            k, v = seqs.stored(seqs.k[b]), seqs.stored(seqs.v[b])
+            if n:
+                want, size, ds = attend64(q[at:at + n], k, v, torch.arange(lens[b] - n, lens[b]), True, window, 1 / math.sqrt(d))
+                tol = attend_tolerance(want, size, ds, float(v.abs().max()), lens[b], dtype, True)
+                assert ((out[at:at + n].double() - want).abs() <= tol).all(), (b, window)
+            at += n
