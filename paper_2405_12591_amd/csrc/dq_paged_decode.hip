@@ -72,10 +72,10 @@ __device__ __forceinline__ Share share_of(const PagedAttnArgs& a, int slot) {
 // The values' scale rides in the exponent: u = s + log2(scale_v), p = 2^(u - m), O += p c, l += (sum p) / scale_v; the
 // products see codes and p only, and p is largest (2^8 at most) where the contribution to the output is.
 //
-// Bound by memory where caches are long: two bytes a token and channel, 16 x 8 heads of 32768 tokens of 128 channels 1074 MB, 169 us,
-// 6.4 TB/s as a plain read of that size; four sequences of 9384 to 16384 tokens, 40 heads, 530 MB, 95 us, 5.6 TB/s.  By latency where
+// Bound by memory where caches are long: two bytes a token and channel, 16 x 8 heads of 32768 tokens of 128 channels 1074 MB, 163 us,
+// 6.6 TB/s as a plain read of that size; four sequences of 9384 to 16384 tokens, 40 heads, 530 MB, 91 us, 5.8 TB/s.  By latency where
 // they are short: one tile a wave 5.0 us, launch, lengths, page, codes and joins after one another; 64 units of 64 tiles of 64
-// channels (33 MB) 13.4 us.  Tiles requested two or three ahead made no launch faster and short ones slower.
+// channels (33 MB) 13.1 us.  Tiles requested two or three ahead made no launch faster and short ones slower.
 template <typename T, int D, bool FP8, int WAVES>
 __global__ __launch_bounds__(64 * WAVES, 2) void paged_decode_kernel(PagedAttnArgs a) {
   constexpr int NC = D / 64, NCT = D / 16, THREADS = 64 * WAVES;
