@@ -253,7 +253,7 @@ def paged_attention(cache: PagedCache, q: torch.Tensor, starts: Optional[torch.T
     """softmax(q . K * scale) V of the batch's rows q [rows, q_heads, d] over the cached tokens of their sequences
     (dq_paged_attention); rows are the last tokens of their sequence (append them first).  max_rows: host bound on the
     rows of any sequence; max_seq_len: on its tokens (a guess does).  window > 0: the last `window` tokens only.  out may be q.  No gradients.
-    splits: launch override for sweeps (DQ_PAGED_SPLITS)."""
+    Rows of no sequence and a sequence's rows past max_rows are not written.  splits: launch override for sweeps (DQ_PAGED_SPLITS)."""
     if out is None:
         out = torch.empty(q.shape, dtype=q.dtype, device=q.device)
     index = cache.index
