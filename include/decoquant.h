@@ -490,7 +490,7 @@ typedef struct dq_paged_batch {
  * page, by a smaller seq_lens alone.  A page that was quantized is no tail again by that: its rows were
  * appended to its codes, and the tail holds other tokens.  To end inside such a page at length n, read its
  * rows n / P * P .. n - 1 with dq_paged_read and the length they were appended with, then append them (no
- * norm, no rotation) with seq_lens n.
+ * norm, no rotation) with seq_lens n; a page that other sequences share gets another in page_table first.
  */
 int32_t dq_paged_append(const dq_paged_cache* cache, const dq_paged_batch* batch, const dq_heads* k,
                         const dq_heads* v, const dq_heads* q, const dq_heads* q_out,
