@@ -536,6 +536,67 @@ int32_t dq_paged_attention(const dq_paged_cache* cache, const dq_paged_batch* ba
                            void* hip_stream);
 
 /*
+ * ---- Attention over one latent vector a token ----
+ *
+ * Layers whose heads' keys and values are products of one vector c a token (the latent) with the heads' weights,
+ * besides some key channels k_rot that all heads share and that alone are rotated.  The cache holds [c | k_rot]
+ * in 16 bits.  Attention over it has two forms: with the key weights taken into the query and the value weights
+ * into the output (absorbed: one key and one value for all heads, few rows), or with keys and values expanded
+ * from c by a matrix product (expanded: prompts).
+ *
+ * The cache: rows u16 [pages, P, latent_dim + rot_dim], token t of a sequence in row t % P of page
+ * page_table[b][t / P].  latent_dim and rot_dim are 512 and 64, or 256 and 32.
+ * Batches are dq_paged_batch without tail_slots; seq_lens count the call's rows.
+ */
+typedef struct dq_latent_cache {
+  uint16_t* rows;                   /* 16-byte aligned */
+  int32_t pages, page_tokens;       /* page_tokens 64 or 128 */
+  int32_t latent_dim, rot_dim;
+  int32_t dtype;
+} dq_latent_cache;
+
+/*
+ * Append the batch's rows: latent [rows, latent_dim] and k_rot [rows, rot_dim], rows `stride` elements apart (16-byte
+ * aligned, strides multiples of 8), as they lie in a fused projection.  c = latent * weight / sqrt(mean(latent^2) + eps)
+ * (weight NULL: latent as it is), k_rot turned by its position (rot NULL: as it is; rot->rot_dim is the cache's, positions NULL: a
+ * token's place in its sequence); both in fp32 and rounded once.  q (NULL: none), heads [rows, q_heads, rot_dim], the
+ * queries' channels that meet k_rot, takes the same rotation in the same launch, into q_out (q itself will do).
+ * A row with a value that is not finite after that is kept as zeros with k_rot of NaN: a query that sees the token yields
+ * NaN, the others are untouched.  Rows of a page that does not exist are dropped.  Lengths may go back at will.
+ */
+int32_t dq_latent_append(const dq_latent_cache* cache, const dq_paged_batch* batch, const uint16_t* latent,
+                         int64_t latent_stride, const uint16_t* k_rot, int64_t k_rot_stride, const uint16_t* weight,
+                         float eps, const dq_heads* q, const dq_heads* q_out, const dq_rotary* rot, void* hip_stream);
+
+/* Rows first[b] <= t < seq_lens[b] (first NULL: from 0) into out [batch->rows, latent_dim + rot_dim], row out_starts[b] + t -
+ * first[b]; tokens past row out_starts[b+1] - 1 are left out, rows of a page that does not exist are zeros with k_rot of NaN.
+ * batch->starts is not used. */
+int32_t dq_latent_read(const dq_latent_cache* cache, const dq_paged_batch* batch, const int32_t* first,
+                       const int32_t* out_starts, uint16_t* out, int64_t out_stride, void* hip_stream);
+
+/* Bytes dq_latent_attention needs for these sizes and all smaller ones with the same heads (0 on invalid arguments); no zeros needed,
+ * calls that share it must be ordered. */
+size_t dq_latent_workspace_bytes(const dq_latent_cache* cache, int32_t batch, int32_t rows, int32_t q_heads,
+                                 int32_t max_rows, int32_t max_seq_len);
+
+/*
+ * Absorbed form: out[row, h] = softmax_t(q[row, h] . [c_t | k_rot_t] * scale) c_t over the cached tokens of the
+ * row's sequence, the batch's rows being its last tokens (append first, then attend).
+ *   q         [rows, q_heads, latent_dim + rot_dim];  out [rows, q_heads, latent_dim], not overlapping q
+ *   seen      NULL, or u64 [rows] (with DQ_PAGED_CAUSAL, max_rows <= 64): of the sequence's own rows, row i sees
+ *             the j-th where bit j is set (a tree of drafted tokens), of the tokens before them all
+ *   softmax_scale  must be positive (1/sqrt of a head's expanded channels)
+ *   max_rows  host bound on the rows of any sequence; further rows of that sequence may be left out (not written)
+ *   max_seq_len    host bound on seq_lens (a guess does: it sizes the launch only, which orders the sums)
+ * fp32 accumulation, one rounding of the result, probabilities in the rows' type for their product with c.  A row that sees no
+ * token yields zeros; tokens of a page that does not exist yield NaN for those who see them.  flags: DQ_PAGED_CAUSAL.
+ */
+int32_t dq_latent_attention(const dq_latent_cache* cache, const dq_paged_batch* batch, const dq_heads* q,
+                            const dq_heads* out, const uint64_t* seen, int32_t max_rows, int32_t max_seq_len,
+                            float softmax_scale, void* workspace, size_t workspace_bytes, uint32_t flags,
+                            void* hip_stream);
+
+/*
  * Measurement helper: read `bytes` (multiple of 16) from src with 128-bit loads and fold them
  * into sink[0..3] (u32) so the reads cannot be elided.  Gives the achievable read bandwidth
  * that the decode kernel's rate is compared with.

@@ -47,3 +47,11 @@ from .paged import (  # noqa: F401
     paged_attention,
     PagedKVLayer,
 )
+from .latent import (  # noqa: F401
+    LatentCache,
+    alloc_latent_cache,
+    latent_append,
+    latent_read,
+    latent_workspace,
+    latent_attention,
+)

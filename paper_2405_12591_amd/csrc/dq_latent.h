@@ -1,0 +1,147 @@
+// Shared pieces of attention over latents and of drafted trees: argument checks, and how a launch's workgroups share the tiles
+// of a ragged batch.
+#pragma once
+#include "dq_paged_attn.h"
+
+namespace dq {
+
+inline bool latent_cache_ok(const dq_latent_cache* c) {
+  if (!c || !c->rows || ((uintptr_t)c->rows & 15) || c->pages <= 0) return false;
+  if (c->page_tokens != 64 && c->page_tokens != 128) return false;
+  if (!(c->latent_dim == 512 && c->rot_dim == 64) && !(c->latent_dim == 256 && c->rot_dim == 32)) return false;
+  return c->dtype == DQ_F16 || c->dtype == DQ_BF16;
+}
+inline bool latent_batch_ok(const dq_paged_batch* b, const dq_latent_cache* c, bool uses_starts) {
+  if (!b || !b->seq_lens || !b->page_table || b->batch <= 0 || b->rows < 0) return false;
+  if (b->table_width <= 0 || b->table_stride < b->table_width) return false;
+  if ((long)b->table_width * c->page_tokens >= kMostTokens) return false;
+  return !uses_starts || b->starts || b->rows == b->batch;
+}
+
+// A ragged batch's tiles in one line: sequence after sequence, in a sequence unit after unit (a tile of query columns, a kv head), in a
+// unit from its first token tile on.  Workgroup w takes tiles [w quota, (w + 1) quota) of the line, whatever units they belong
+// to, so that all end together however lengths differ.  A unit that one workgroup takes whole is written out; pieces of the others
+// are left in the workspace, two at most for a workgroup (slot 2 w: a piece that does not begin its unit; 2 w + 1: one that does
+// and does not end it), and joined by a second launch, over the columns, which finds them by the same counting.  (One
+// workgroup alone joining a unit of 128 columns of 512 channels in 16 pieces would read 4 MB.)
+struct Line {
+  int workgroups;
+  int min_quota;           // tiles that are worth a workgroup of their own
+};
+struct Weight {
+  int units, tiles;        // of a sequence
+};
+
+__device__ __forceinline__ long wave_sum(long x) {
+  for (int o = 1; o < 64; o *= 2) x += __shfl_xor(x, o);
+  return x;
+}
+__device__ __forceinline__ long wave_uniform(long x) {
+  return (long)((uint64_t)(uint32_t)__builtin_amdgcn_readfirstlane((int)(x >> 32)) << 32 | (uint32_t)__builtin_amdgcn_readfirstlane((int)x));
+}
+
+// weight_of(b): a sequence's Weight.  Every lane of a wave calls it with other sequences.
+template <typename F> __device__ __forceinline__ long line_total(int batch, F weight_of) {
+  long mine = 0;
+  for (int b = threadIdx.x & 63; b < batch; b += 64) {
+    const Weight w = weight_of(b);
+    mine += (long)w.units * w.tiles;
+  }
+  return wave_uniform(wave_sum(mine));
+}
+__device__ __forceinline__ long line_quota(const Line& l, long total) { return max((total + l.workgroups - 1) / l.workgroups, (long)l.min_quota); }
+
+// The sequence that holds place `at` of the line (at < total), and the place at which it begins.
+template <typename F> __device__ __forceinline__ int line_owner(int batch, long at, F weight_of, long& begin) {
+  const int lane = threadIdx.x & 63;
+  long before = 0;
+  for (int b0 = 0; b0 < batch; b0 += 64) {
+    long mine = 0;
+    if (b0 + lane < batch) {
+      const Weight w = weight_of(b0 + lane);
+      mine = (long)w.units * w.tiles;
+    }
+    long upto = mine;
+    for (int o = 1; o < 64; o *= 2) {
+      const long x = __shfl_up(upto, o);
+      if (lane >= o) upto += x;
+    }
+    const uint64_t owner = __ballot(at < before + upto && at >= before + upto - mine);
+    if (owner) {
+      const int l = __builtin_ctzll(owner);
+      begin = wave_uniform(before + __shfl(upto - mine, l));
+      return b0 + l;
+    }
+    before += wave_uniform(__shfl(upto, 63));
+  }
+  begin = before;
+  return batch;
+}
+
+// The places of the line before sequence b.
+template <typename F> __device__ __forceinline__ long line_before(int b, F weight_of) { return line_total(b, weight_of); }
+
+// Pieces of a unit whose tiles are places [begin, begin + tiles) of the line: the workgroups first .. last, one piece each.
+struct Pieces {
+  long first, last;
+};
+__device__ __forceinline__ Pieces pieces_of(long begin, int tiles, long quota) { return {begin / quota, (begin + tiles - 1) / quota}; }
+__device__ __forceinline__ long slot_of(const Pieces& p, long w) { return w == p.first ? 2 * w + 1 : 2 * w; }
+
+// Joins a column's pieces: a workgroup of four waves, which take every fourth of them.  o: [slot, column, D] floats, ml: [slot, column, 2].
+// Two pieces of a lane's channels are asked for at once, by all four waves.
+template <typename T, int D>
+__device__ __forceinline__ void join_column(const Pieces& p, const float* o, const float* ml, int columns, int column, uint16_t* out) {
+  constexpr int PER = D / 64, AHEAD = 8;
+  __shared__ float s_o[4][D], s_m[4], s_l[4];
+  const int tid = threadIdx.x, lane = tid & 63, wave = tid >> 6;
+  const int count = (int)(p.last - p.first) + 1;
+  float m = -INFINITY, l = 0.f, x[PER] = {};
+  for (int i0 = wave; i0 < count; i0 += 4 * AHEAD) {
+    float y[AHEAD][PER], pm[AHEAD], pl[AHEAD];
+#pragma unroll
+    for (int k = 0; k < AHEAD; ++k) {                     // (behind the last piece: that one again, with no weight)
+      const int i = min(i0 + 4 * k, count - 1);
+      const long at = slot_of(p, p.first + i) * columns + column;
+      const f32x2 v = *reinterpret_cast<const f32x2*>(ml + 2 * at);
+      pm[k] = i0 + 4 * k < count ? v.x : -INFINITY;
+      pl[k] = v.y;
+#pragma unroll
+      for (int e = 0; e < PER; ++e) y[k][e] = o[at * D + PER * lane + e];
+    }
+    float top = m;
+#pragma unroll
+    for (int k = 0; k < AHEAD; ++k) top = fmaxf(top, pm[k]);
+    const float at = top == -INFINITY ? 0.f : top, back = __builtin_amdgcn_exp2f(m - at);
+    m = top;
+    l *= back;
+#pragma unroll
+    for (int e = 0; e < PER; ++e) x[e] *= back;
+#pragma unroll
+    for (int k = 0; k < AHEAD; ++k) {
+      const float w = __builtin_amdgcn_exp2f(pm[k] - at);
+      if (i0 + 4 * k >= count) break;
+      l = __builtin_fmaf(pl[k], w, l);
+#pragma unroll
+      for (int e = 0; e < PER; ++e) x[e] = __builtin_fmaf(y[k][e], w, x[e]);
+    }
+  }
+#pragma unroll
+  for (int e = 0; e < PER; ++e) s_o[wave][PER * lane + e] = x[e];
+  if (lane == 0) { s_m[wave] = m; s_l[wave] = l; }
+  __syncthreads();
+  if (2 * tid >= D) return;
+  const float top = fmaxf(fmaxf(s_m[0], s_m[1]), fmaxf(s_m[2], s_m[3])), at = top == -INFINITY ? 0.f : top;
+  float a = 0.f, b = 0.f, sum = 0.f;
+#pragma unroll
+  for (int w = 0; w < 4; ++w) {
+    const float f = __builtin_amdgcn_exp2f(s_m[w] - at);
+    sum = __builtin_fmaf(s_l[w], f, sum);
+    a = __builtin_fmaf(s_o[w][2 * tid], f, a);
+    b = __builtin_fmaf(s_o[w][2 * tid + 1], f, b);
+  }
+  const float inv = sum == 0.f ? 0.f : 1.f / sum;
+  reinterpret_cast<uint32_t*>(out)[tid] = pack2<T>(a * inv, b * inv);
+}
+
+}  // namespace dq

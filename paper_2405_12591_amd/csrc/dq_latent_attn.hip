@@ -1,0 +1,348 @@
+// Attention over latents in the absorbed form: one key and one value for all heads, a paged cache of 16-bit rows.
+#include "dq_latent.h"
+
+namespace dq {
+
+struct LatentArgs {
+  dq_latent_cache c;
+  dq_paged_batch bt;
+  dq_heads q, out;
+  const uint64_t* seen;    // of the sequence's own rows, the ones a row sees; null: up to its place
+  int max_rows, causal;
+  float scale_log2;
+  Line line;
+  float *o, *ml;           // pieces: [slot, column, R], [slot, column, 2]
+};
+
+constexpr int kLatentTile = 32;   // tokens
+
+typedef __attribute__((address_space(3))) char* LdsBytes;
+typedef __attribute__((address_space(3))) const u32x4* LdsPieces;
+typedef short s16x4 __attribute__((ext_vector_type(4)));
+typedef __attribute__((address_space(3))) s16x4* LdsQuads;
+
+// What a token that is not there has (zeros: nothing sees it, and 0 * NaN of what lies there would not be 0), and the key channels of
+// a page that does not exist (NaN for those who see its tokens).
+__device__ const u32x4 g_blank[2] = {{0, 0, 0, 0}, {0x7FFF7FFFu, 0x7FFF7FFFu, 0x7FFF7FFFu, 0x7FFF7FFFu}};
+
+// 64 pieces of 16 bytes to LDS, one behind the other from `lds` on, past the registers: lane's piece is at base + offset, or at `from`.  As
+// instructions of their own: the compiler waits for all such copies ahead of every LDS read, the ones for later tiles too.  The
+// kernel counts them itself (no register is written; a wait that counts too many of them waits longer).
+__device__ __forceinline__ void copy_to_lds(const uint16_t* base, uint32_t offset, uint32_t lds) {
+  asm volatile("s_mov_b32 m0, %0\n\ts_nop 0\n\tglobal_load_lds_dwordx4 %1, %2" ::"s"(lds), "v"(offset), "s"(base) : "memory");
+}
+__device__ __forceinline__ void copy_to_lds(const uint16_t* from, uint32_t lds) {
+  asm volatile("s_mov_b32 m0, %0\n\ts_nop 0\n\tglobal_load_lds_dwordx4 %1, off" ::"s"(lds), "v"(from) : "memory");
+}
+__device__ __forceinline__ uint32_t lds_of(const void* p) { return (uint32_t)(uintptr_t)(LdsBytes)p; }
+
+template <int M>
+__device__ __forceinline__ Weight latent_weight(const LatentArgs& a, int b) {
+  const Sequence s = sequence_of(a.bt, a.c.page_tokens, b);
+  const int n = min(s.n, a.max_rows);
+  return {n ? (int)(((long)n * a.q.heads + M - 1) / M) : 0, max((s.len + kLatentTile - 1) / kLatentTile, 1)};
+}
+
+template <typename T, int R, int CB>
+struct LatentShape {
+  static constexpr int ROT = R == 512 ? 64 : 32, W = R + ROT;
+  static constexpr int CH = 4 / CB;                       // waves that share a block of 32 columns, each with a part of the channels
+  static constexpr int M = 32 * CB;
+  static constexpr int BUFFERS = 4;
+  static constexpr int PER_SIMD = R == 512 ? 1 : 2;       // waves
+};
+
+// A workgroup of four waves takes 32 CB (row, head) columns over its tiles of 32 tokens, which are copied to LDS past the registers and
+// are keys and values both.  Every wave forms the transposed scores of its 32 columns, S^T = [c | k_rot] q^T, with the key rows in
+// the order that leaves a lane the probabilities of 8 neighbouring tokens twice, the right operand of O^T += c^T P^T; the left
+// one comes from the same rows by transposing LDS reads.
+template <typename T, int R, int CB>
+__global__ __launch_bounds__(256, (LatentShape<T, R, CB>::PER_SIMD)) void latent_attn_kernel(LatentArgs a) {
+  typedef LatentShape<T, R, CB> Shape;
+  constexpr int ROT = Shape::ROT, W = Shape::W, CH = Shape::CH, M = Shape::M, NB = Shape::BUFFERS;
+  constexpr int TT = kLatentTile, NK = R / 16, NR = ROT / 16, NCT = R / 32 / CH;
+  constexpr int LOADS = 8 * R * 2 / 1024 + 1;             // of a wave and tile
+  typedef typename Vec8<T>::type tx8;
+  __shared__ __align__(1024) char s_c[NB][TT * R * 2], s_r[NB][TT * ROT * 2];
+  const int tid = threadIdx.x, lane = tid & 63, wave = __builtin_amdgcn_readfirstlane(tid >> 6), r32 = lane & 31, hl = lane >> 5;
+  const int cb = wave % CB, chs = wave / CB, H = a.q.heads, P = a.c.page_tokens;
+  const auto weight_of = [&](int b) { return latent_weight<M>(a, b); };
+  const long total = line_total(a.bt.batch, weight_of), quota = line_quota(a.line, total);
+  long at = (long)blockIdx.x * quota;
+  const long end = min(at + quota, total);
+  if (at >= end) return;
+  long begin;
+  int b = line_owner(a.bt.batch, at, weight_of, begin);
+
+  // ---- places in LDS ----
+  // A row's 16-byte pieces are exchanged within runs of 16 by bits of the token, so that the 16 lanes that read one piece of 16 tokens'
+  // rows (keys), and those that read four pieces of four (values), touch all banks.
+  auto swap_of = [](int token) { return (token & 3) << 2 | (token >> 2 & 3); };
+  auto rot_swap_of = [](int token) { return ROT == 64 ? token >> 1 & 7 : token >> 2 & 3; };
+  const int k_token = (r32 & ~12) | (r32 & 4) << 1 | (r32 & 8) >> 1;
+  const int k_at = k_token * R * 2 + ((hl ^ swap_of(k_token)) << 4);            // ^ 32 (k % 8), + 256 (k / 8)
+  const int rot_at = k_token * ROT * 2 + ((hl ^ rot_swap_of(k_token)) << 4);    // ^ 32 k
+  const int i16 = lane & 15, side = lane >> 4 & 1;
+  const int v_token = 8 * hl + (i16 >> 2);                                       // + 4 j + 16 s
+  auto v_at = [&](int j) { return (v_token + 4 * j) * R * 2 + ((2 * side + ((i16 & 3) >> 1) ^ swap_of(v_token + 4 * j)) << 4) + (i16 & 1) * 8; };   // ^ 64 (c % 4), + 256 (c / 4)
+  const int v_at0 = v_at(0), v_at1 = v_at(1);
+
+  for (; at < end;) {
+    const Sequence s = sequence_of_wave(a.bt, P, b);
+    const Weight wt = weight_of(b);
+    const int n = min(s.n, a.max_rows), len = s.len, before = s.old;
+    const int unit = __builtin_amdgcn_readfirstlane((int)((at - begin) / wt.tiles)), tiles = __builtin_amdgcn_readfirstlane(wt.tiles);
+    const int t0 = __builtin_amdgcn_readfirstlane((int)(at - begin - (long)unit * tiles)), t1 = (int)min((long)tiles, t0 + (end - at));
+    const int pairs = n * H, first = unit * M;
+    const int rows_lo = first / H, rows_hi = min(first + M - 1, pairs - 1) / H;
+
+    // ---- queries ----
+    const int my_pair = min(first + cb * 32 + r32, pairs - 1), my_row = my_pair / H;
+    const uint16_t* const q_row = a.q.data + (long)(s.row0 + my_row) * a.q.token_stride + (long)(my_pair % H) * a.q.head_stride + 8 * hl;
+    tx8 q[NK + NR];
+#pragma unroll
+    for (int k = 0; k < NK + NR; ++k) q[k] = __builtin_bit_cast(tx8, *reinterpret_cast<const u32x4*>(q_row + 16 * k));
+    const int place = before + my_row;
+    uint64_t bits = 0;                                    // of the sequence's own rows
+    int see_hi = a.causal ? min(place + 1, len) : len, all_hi = a.causal ? min(before + rows_lo + 1, len) : len;
+    int any_hi = a.causal ? min(before + rows_hi + 1, len) : len;
+    if (a.seen) {
+      bits = a.seen[s.row0 + my_row];
+      if (s.n < 64) bits &= (1ull << s.n) - 1;
+      see_hi = all_hi = min(before, len);
+      any_hi = len;
+    }
+    const int t_end = min(t1, (max(any_hi, 0) + TT - 1) / TT);
+
+    f32x16 o[NCT];
+#pragma unroll
+    for (int ct = 0; ct < NCT; ++ct)
+#pragma unroll
+      for (int e = 0; e < 16; ++e) o[ct][e] = 0.f;
+    float m = -INFINITY, l = 0.f;
+
+    int pages = 0, pages_from = t0;                       // of 64 tiles from pages_from on, one a lane
+    auto load_pages = [&](int from) __attribute__((always_inline)) {
+      pages_from = from;
+      const int t = from + lane;
+      const int page = t < tiles && (long)t * TT < len ? a.bt.page_table[(long)b * a.bt.table_stride + t * TT / P] : -1;
+      pages = page >= 0 && page < a.c.pages ? page : -1;
+    };
+    auto load_tile = [&](int t) __attribute__((always_inline)) {
+      if (t - pages_from >= 64) load_pages(t);
+      const int page = __builtin_amdgcn_readlane(pages, t - pages_from), left = len - t * TT;
+      const uint16_t* const from = a.c.rows + ((long)max(page, 0) * P + t * TT % P) * W + 8 * wave * W;
+      const uint32_t to = lds_of(s_c[t % NB]) + 8 * wave * R * 2, rot_to = lds_of(s_r[t % NB]) + 8 * wave * ROT * 2;
+      constexpr int STEP = 1024 / (R * 2);                // rows of one copy
+      const int slot = R == 512 ? lane : lane & 31, ahead = R == 512 ? 0 : lane >> 5;
+      const int rot_token = lane / (ROT / 8), rot_slot = lane % (ROT / 8);
+      if (page >= 0 && left >= TT) {
+#pragma unroll
+        for (int i = 0; i < LOADS - 1; ++i)
+          copy_to_lds(from + i * STEP * W, ahead * W * 2 + ((slot ^ swap_of(8 * wave + i * STEP + ahead)) << 4), to + 1024 * i);
+        if (ROT == 64 || lane < 32)
+          copy_to_lds(from + R, rot_token * W * 2 + ((rot_slot ^ rot_swap_of(8 * wave + rot_token)) << 4), rot_to);
+        return;
+      }
+      auto source = [&](int token, int piece, bool rot) __attribute__((always_inline)) {
+        const bool there = 8 * wave + token < left;
+        return there && page >= 0 ? from + token * W + (rot ? R : 0) + 8 * piece : reinterpret_cast<const uint16_t*>(&g_blank[rot && there ? 1 : 0]);
+      };
+#pragma unroll
+      for (int i = 0; i < LOADS - 1; ++i) {
+        const int token = i * STEP + ahead;
+        copy_to_lds(source(token, slot ^ swap_of(8 * wave + token), false), to + 1024 * i);
+      }
+      if (ROT == 64 || lane < 32) copy_to_lds(source(rot_token, rot_slot ^ rot_swap_of(8 * wave + rot_token), true), rot_to);
+    };
+
+    load_pages(t0);
+    __syncthreads();                                      // buffers have been read
+#pragma unroll
+    for (int i = 0; i < NB - 1; ++i)
+      if (t0 + i < t_end) load_tile(t0 + i);
+    for (int t = t0; t < t_end; ++t) {
+      if (t + NB - 2 < t_end) asm volatile("s_waitcnt vmcnt(%0)" ::"i"((NB - 2) * LOADS) : "memory");
+      else asm volatile("s_waitcnt vmcnt(0)" ::: "memory");
+      __builtin_amdgcn_s_barrier();
+      if (t + NB - 1 < t_end) load_tile(t + NB - 1);
+      const LdsBytes c_from = (LdsBytes)s_c[t % NB], r_from = (LdsBytes)s_r[t % NB];
+
+      f32x16 u;
+#pragma unroll
+      for (int e = 0; e < 16; ++e) u[e] = 0.f;
+#pragma unroll
+      for (int k = 0; k < NK; ++k) {
+        const tx8 kf = __builtin_bit_cast(tx8, *(LdsPieces)(c_from + (k_at ^ 32 * (k % 8)) + 256 * (k / 8)));
+        u = mma32(kf, q[k], u);
+        if (k % 8 == 7) __builtin_amdgcn_sched_barrier(0);   // (reads of all steps ahead of the first product would take 144 registers)
+      }
+#pragma unroll
+      for (int k = 0; k < NR; ++k) {
+        const tx8 kf = __builtin_bit_cast(tx8, *(LdsPieces)(r_from + (rot_at ^ 32 * k)));
+        u = mma32(kf, q[NK + k], u);
+      }
+      if (t * TT + TT > all_hi) {
+        asm volatile("" ::: "memory");                    // (a branch: as selects they would be part of every tile)
+#pragma unroll
+        for (int e = 0; e < 16; ++e) {
+          const int token = t * TT + 16 * (e >> 3) + 8 * hl + (e & 7), own = token - before;
+          const bool sees = token < see_hi || (token < len && own >= 0 && own < 64 && (bits >> (own & 63) & 1));
+          u[e] = sees ? u[e] : -INFINITY;
+        }
+      }
+      float top = u[0];
+#pragma unroll
+      for (int e = 1; e < 16; ++e) top = fmaxf(top, u[e]);
+      top *= a.scale_log2;
+      if (__any(top > m + kLazy)) {
+        top = fmaxf(top, __shfl_xor(top, 32));
+        const float m_new = fmaxf(m, top);
+        const float alpha = m_new == -INFINITY ? 1.f : __builtin_amdgcn_exp2f(m - m_new);
+        m = m_new;
+        l *= alpha;
+#pragma unroll
+        for (int ct = 0; ct < NCT; ++ct) o[ct] *= alpha;
+      }
+      const float base = m == -INFINITY ? 0.f : -m;
+      // probabilities in the rows' type, which their product with c needs (the sum keeps fp32)
+      tx8 p[2];
+      float sum = 0.f;
+#pragma unroll
+      for (int e = 0; e < 16; ++e) {
+        const float x = __builtin_amdgcn_exp2f(__builtin_fmaf(u[e], a.scale_log2, base));
+        sum += x;
+        p[e >> 3][e & 7] = to_element<tx8>(x);
+      }
+      l += sum;
+#pragma unroll
+      for (int ct = 0; ct < NCT; ++ct) {
+        const int c = chs * NCT + ct;                     // (NCT is a multiple of 4, or all of a wave's channel tiles share c / 4's)
+#pragma unroll
+        for (int ks = 0; ks < 2; ++ks) {
+          const LdsBytes from = c_from + 16 * ks * R * 2 + 256 * (c / 4);
+          const s16x4 lo = __builtin_amdgcn_ds_read_tr16_b64_v4i16((LdsQuads)(from + (v_at0 ^ 64 * (c % 4))));
+          const s16x4 hi = __builtin_amdgcn_ds_read_tr16_b64_v4i16((LdsQuads)(from + (v_at1 ^ 64 * (c % 4))));
+          struct { s16x4 a, b; } const both = {lo, hi};
+          o[ct] = mma32(__builtin_bit_cast(tx8, both), p[ks], o[ct]);
+        }
+      }
+    }
+
+    // ---- the result, or a piece of it ----
+    l += __shfl_xor(l, 32);
+    const int col = cb * 32 + r32;
+    const bool whole = t0 == 0 && t1 == tiles;
+    if (first + col < pairs) {
+      if (whole) {
+        const float inv = l == 0.f ? 0.f : 1.f / l;
+        uint16_t* const dst = a.out.data + (long)(s.row0 + my_row) * a.out.token_stride + (long)(my_pair % H) * a.out.head_stride + chs * NCT * 32;
+#pragma unroll
+        for (int ct = 0; ct < NCT; ++ct)
+#pragma unroll
+          for (int e = 0; e < 4; ++e)
+            *reinterpret_cast<u32x2*>(dst + 32 * ct + 8 * e + 4 * hl) = u32x2{pack2<T>(o[ct][4 * e] * inv, o[ct][4 * e + 1] * inv),
+                                                                             pack2<T>(o[ct][4 * e + 2] * inv, o[ct][4 * e + 3] * inv)};
+      } else {
+        const long slot = 2l * blockIdx.x + (t0 == 0);
+        float* const dst = a.o + (slot * M + col) * R + chs * NCT * 32;
+#pragma unroll
+        for (int ct = 0; ct < NCT; ++ct)
+#pragma unroll
+          for (int e = 0; e < 4; ++e)
+            *reinterpret_cast<f32x4*>(dst + 32 * ct + 8 * e + 4 * hl) = f32x4{o[ct][4 * e], o[ct][4 * e + 1], o[ct][4 * e + 2], o[ct][4 * e + 3]};
+        if (hl == 0 && chs == 0) *reinterpret_cast<f32x2*>(a.ml + 2 * (slot * M + col)) = f32x2{m, l};
+      }
+    }
+    at += t1 - t0;
+    if (t1 == tiles && unit == __builtin_amdgcn_readfirstlane(wt.units) - 1) {   // the next sequence that has rows
+      begin = at;
+      do ++b;
+      while (at < end && weight_of(b).units == 0);
+    }
+  }
+}
+
+template <typename T, int R, int CB>
+__global__ __launch_bounds__(256) void latent_join_kernel(LatentArgs a) {
+  constexpr int M = LatentShape<T, R, CB>::M;
+  const int H = a.q.heads, item = (int)(blockIdx.x / M), col = (int)(blockIdx.x % M);
+  const int b = item_owner(a.bt.starts, a.bt.rows, a.bt.batch, item, H, M, 1);
+  const Sequence s = sequence_of_wave(a.bt, a.c.page_tokens, b);
+  const int n = min(s.n, a.max_rows), pair = (item - item_first(a.bt.starts, a.bt.rows, b, H, M, 1)) * M + col;
+  if (pair < 0 || pair >= n * H) return;
+  const auto weight_of = [&](int i) { return latent_weight<M>(a, i); };
+  const Weight w = weight_of(b);
+  const long quota = line_quota(a.line, line_total(a.bt.batch, weight_of));
+  const Pieces p = pieces_of(line_before(b, weight_of) + (long)(pair / M) * w.tiles, w.tiles, quota);
+  if (p.first == p.last) return;
+  join_column<T, R>(p, a.o, a.ml, M, col, a.out.data + (long)(s.row0 + pair / H) * a.out.token_stride + (long)(pair % H) * a.out.head_stride);
+}
+
+struct LatentPlan {
+  int cb;
+  long items, workgroups;
+};
+
+static bool latent_plan(const dq_latent_cache* c, int batch, long rows, int heads, int max_rows, int max_seq_len, LatentPlan* p) {
+  if (batch <= 0 || rows < 0 || heads <= 0 || max_rows < 0 || max_seq_len < 0 || rows * heads >= (1l << 31) - 256) return false;
+  const long cols = (long)max_rows * heads;
+  p->cb = cols <= 32 ? 1 : 2;
+  p->items = rows * heads / (32 * p->cb) + batch;
+  if (p->items * 32 * p->cb >= kMaxThreads / 256) return false;
+  p->workgroups = c->latent_dim == 512 ? 256 : 512;
+  return true;
+}
+static size_t latent_bytes(const dq_latent_cache* c, const LatentPlan& p) {
+  return (size_t)(2 * p.workgroups * 32 * p.cb) * (c->latent_dim + 2) * sizeof(float);
+}
+
+template <typename T, int R, int CB>
+static void launch_latent(const LatentArgs& a, const LatentPlan& p, hipStream_t st) {
+  hipLaunchKernelGGL((latent_attn_kernel<T, R, CB>), dim3((unsigned)p.workgroups), dim3(256), 0, st, a);
+  hipLaunchKernelGGL((latent_join_kernel<T, R, CB>), dim3((unsigned)(p.items * 32 * CB)), dim3(256), 0, st, a);
+}
+template <typename T, int R>
+static void launch_latent_cols(const LatentArgs& a, const LatentPlan& p, hipStream_t st) {
+  if (p.cb == 1) launch_latent<T, R, 1>(a, p, st);
+  else launch_latent<T, R, 2>(a, p, st);
+}
+
+}  // namespace dq
+
+using namespace dq;
+
+extern "C" size_t dq_latent_workspace_bytes(const dq_latent_cache* cache, int32_t batch, int32_t rows, int32_t q_heads, int32_t max_rows,
+                                            int32_t max_seq_len) {
+  LatentPlan p;
+  if (!latent_cache_ok(cache) || !latent_plan(cache, batch, rows, q_heads, max_rows, max_seq_len, &p)) return 0;
+  p.cb = 2;                                               // (smaller calls with the same heads may take fewer columns, never more)
+  p.workgroups = 512;
+  return latent_bytes(cache, p);
+}
+
+extern "C" int32_t dq_latent_attention(const dq_latent_cache* cache, const dq_paged_batch* batch, const dq_heads* q, const dq_heads* out,
+                                       const uint64_t* seen, int32_t max_rows, int32_t max_seq_len, float softmax_scale, void* workspace,
+                                       size_t workspace_bytes, uint32_t flags, void* hip_stream) {
+  if (!latent_cache_ok(cache) || !latent_batch_ok(batch, cache, true) || !heads_ok(q, false) || !heads_ok(out, false)) return DQ_EINVAL;
+  if (q->heads != out->heads || !workspace || ((uintptr_t)workspace & 15) || (flags & ~DQ_PAGED_CAUSAL) || !(softmax_scale > 0.f)) return DQ_EINVAL;
+  if (seen && (((uintptr_t)seen & 7) || !(flags & DQ_PAGED_CAUSAL) || max_rows > 64)) return DQ_EINVAL;
+  LatentPlan p;
+  if (!latent_plan(cache, batch->batch, batch->rows, q->heads, max_rows, max_seq_len, &p)) return DQ_EINVAL;
+  if (workspace_bytes < latent_bytes(cache, p)) return DQ_ENOSPACE;
+  if (batch->rows == 0 || max_rows == 0) return DQ_OK;
+  LatentArgs a = {};
+  a.c = *cache; a.bt = *batch; a.q = *q; a.out = *out;
+  a.seen = seen;
+  a.max_rows = max_rows;
+  a.causal = (flags & DQ_PAGED_CAUSAL) ? 1 : 0;
+  a.scale_log2 = fmaxf(softmax_scale * 1.44269504088896340736f, 1e-37f);
+  a.line = {(int)p.workgroups, 4};
+  a.o = reinterpret_cast<float*>(workspace);
+  a.ml = a.o + 2 * p.workgroups * 32 * p.cb * cache->latent_dim;
+  hipStream_t st = (hipStream_t)hip_stream;
+  if (cache->dtype == DQ_BF16) { if (cache->latent_dim == 512) launch_latent_cols<__bf16, 512>(a, p, st); else launch_latent_cols<__bf16, 256>(a, p, st); }
+  else { if (cache->latent_dim == 512) launch_latent_cols<_Float16, 512>(a, p, st); else launch_latent_cols<_Float16, 256>(a, p, st); }
+  DQ_HIP_CHECK(hipGetLastError());
+  return DQ_OK;
+}

@@ -14,6 +14,9 @@ decltype(&dq_rotate_heads) g_rotate;
 decltype(&dq_paged_append) g_append;
 decltype(&dq_paged_read) g_read;
 decltype(&dq_paged_attention) g_attention;
+decltype(&dq_latent_append) g_latent_append;
+decltype(&dq_latent_read) g_latent_read;
+decltype(&dq_latent_attention) g_latent_attention;
 PyObject* g_error;   // DQError
 PyObject* g_check;   // raises for a status
 
@@ -94,6 +97,37 @@ Heads packed_rows(const dq_paged_cache* cache, int64_t index, const char* name, 
   return h;
 }
 
+// heads [rows, heads, dim]; heads and rows < 0: any.
+Heads plain_rows(const char* name, PyObject* o, int32_t dtype, int64_t dim, int64_t index, int64_t n_heads, int64_t rows, bool written) {
+  const Heads h = heads(name, o, dtype, dim, index, written);
+  if (h.dims != 3 || (rows >= 0 && h.rows != rows) || (n_heads >= 0 && h.c.heads != n_heads) || h.c.heads == 0)
+    refuse("%s must be [rows, heads, %lld], of as many rows and heads as the tensors beside it", name, (long long)dim);
+  return h;
+}
+
+// [rows, dim] with channels side by side; rows < 0: any.
+struct Rows {
+  uint16_t* data;
+  int64_t stride, rows;
+};
+Rows rows_of(const char* name, PyObject* o, int32_t dtype, int64_t dim, int64_t index, int64_t rows, bool written) {
+  const at::Tensor& t = tensor(name, o);
+  if (t.dim() != 2 || t.size(1) != dim || (rows >= 0 && t.size(0) != rows) || t.size(0) > INT32_MAX || t.scalar_type() != row_type(dtype) || t.get_device() != index)
+    refuse("%s must be a torch.%s tensor [rows, %lld] on cuda:%lld, of as many rows as the tensors beside it", name, type_name(dtype), (long long)dim, (long long)index);
+  Rows r = {static_cast<uint16_t*>(t.data_ptr()), t.size(0) == 1 ? 0 : t.stride(0), t.size(0)};
+  if (t.stride(1) != 1 || (r.stride & 7) || ((uintptr_t)r.data & 15) || (written && r.rows > 1 && r.stride < dim))
+    refuse("%s: channels must be neighbours, rows a multiple of 8 elements apart, the data 16-byte aligned", name);
+  return r;
+}
+
+// a mask of the rows it sees for each row
+const uint64_t* masks(const char* name, PyObject* o, int64_t rows, int64_t index) {
+  const at::Tensor& t = tensor(name, o);
+  if (t.scalar_type() != at::kLong || t.numel() != rows || !t.is_contiguous() || t.get_device() != index)
+    refuse("%s must hold an int64 for each of the %lld rows, side by side on cuda:%lld", name, (long long)rows, (long long)index);
+  return static_cast<const uint64_t*>(t.data_ptr());
+}
+
 // n int32 side by side.
 const int32_t* vector(const char* name, PyObject* o, int64_t n, int64_t index) {
   const at::Tensor& t = tensor(name, o);
@@ -153,7 +187,7 @@ void turning(Turning& t, PyObject* q_weight, PyObject* k_weight, PyObject* eps, 
 
 // Sizes are checked here (the library sees pointers only).
 dq_paged_batch batch_of(const dq_paged_cache* cache, int64_t index, PyObject* starts, PyObject* seq_lens, PyObject* page_table, PyObject* tail_slots,
-                        int64_t rows, bool uses_starts) {
+                        int64_t rows, bool uses_starts) {   // cache null: one without tails
   dq_paged_batch b = {};
   const int64_t n = tensor("seq_lens", seq_lens).numel();
   if (n < 1) refuse("a batch has at least one sequence");
@@ -164,7 +198,7 @@ dq_paged_batch batch_of(const dq_paged_cache* cache, int64_t index, PyObject* st
   const int64_t width = table.size(1), stride = n == 1 ? width : table.stride(0);
   if ((width > 1 && table.stride(1) != 1) || stride < width || stride > INT32_MAX) refuse("a sequence's pages must lie side by side in page_table");
   if (none(starts) && uses_starts && rows != n) refuse("without starts there is one row per sequence");
-  if (none(tail_slots) && n > cache->slots) refuse("more sequences than the cache has slots");
+  if (cache && none(tail_slots) && n > cache->slots) refuse("more sequences than the cache has slots");
   b.starts = none(starts) ? nullptr : vector("starts", starts, n + 1, index);
   b.seq_lens = vector("seq_lens", seq_lens, n, index);
   b.page_table = static_cast<const int32_t*>(table.data_ptr());
@@ -305,13 +339,92 @@ PyObject* paged_attention(PyObject*, PyObject* const* a, Py_ssize_t n) {
   });
 }
 
+PyObject* latent_append(PyObject*, PyObject* const* a, Py_ssize_t n) {
+  // cache, index, latent, k_rot, starts, seq_lens, page_table, q, q_out, rotary, positions, weight, eps, stream
+  return guarded(n, 14, [&]() -> PyObject* {
+    const dq_latent_cache* const cache = static_cast<const dq_latent_cache*>(address(a[0]));
+    const int64_t index = integer(a[1]);
+    const Rows latent = rows_of("latent", a[2], cache->dtype, cache->latent_dim, index, -1, false);
+    const Rows k_rot = rows_of("k_rot", a[3], cache->dtype, cache->rot_dim, index, latent.rows, false);
+    const dq_paged_batch b = batch_of(nullptr, index, a[4], a[5], a[6], Py_None, latent.rows, true);
+    Heads q = {}, out = {};
+    const bool with_q = !none(a[7]);
+    if (with_q) {
+      q = plain_rows("q", a[7], cache->dtype, cache->rot_dim, index, -1, latent.rows, false);
+      out = plain_rows("q_out", a[8], cache->dtype, cache->rot_dim, index, q.c.heads, latent.rows, true);
+    }
+    Turning t;
+    turning(t, Py_None, Py_None, a[12], a[9], a[10], cache->dtype, cache->rot_dim, latent.rows, index);
+    if (t.r && t.rot.rot_dim != cache->rot_dim) refuse("the rotation must be of the cache's %d shared key channels", cache->rot_dim);
+    if (with_q && !t.r) refuse("q without a rotation");
+    const uint16_t* const w = weight("weight", a[11], cache->dtype, cache->latent_dim, index);
+    const float eps = (float)real(a[12]);
+    if (w && !(eps >= 0.f)) refuse("eps must not be negative");
+    if (latent.rows == 0) Py_RETURN_NONE;
+    void* const stream = address(a[13]);
+    return launch("dq_latent_append", [&] {
+      return g_latent_append(cache, &b, latent.data, latent.stride, k_rot.data, k_rot.stride, w, eps, with_q ? &q.c : nullptr, with_q ? &out.c : nullptr,
+                             t.r, stream);
+    });
+  });
+}
+
+PyObject* latent_read(PyObject*, PyObject* const* a, Py_ssize_t n) {
+  // cache, index, first, seq_lens, out_starts, page_table, out, stream
+  return guarded(n, 8, [&]() -> PyObject* {
+    const dq_latent_cache* const cache = static_cast<const dq_latent_cache*>(address(a[0]));
+    const int64_t index = integer(a[1]);
+    const Rows out = rows_of("out", a[6], cache->dtype, cache->latent_dim + cache->rot_dim, index, -1, true);
+    if (none(a[4])) refuse("latent_read needs out_starts");
+    const dq_paged_batch b = batch_of(nullptr, index, a[4], a[3], a[5], Py_None, out.rows, false);
+    const int32_t* const first = none(a[2]) ? nullptr : vector("first", a[2], b.batch, index);
+    if (out.rows == 0) Py_RETURN_NONE;
+    void* const stream = address(a[7]);
+    return launch("dq_latent_read", [&] { return g_latent_read(cache, &b, first, b.starts, out.data, out.stride, stream); });
+  });
+}
+
+const at::Tensor& workspace_of(PyObject* o, int64_t index) {
+  const at::Tensor& ws = tensor("workspace", o);
+  if (ws.scalar_type() != at::kByte || !ws.is_contiguous() || ws.get_device() != index) refuse("workspace must be contiguous uint8 on cuda:%lld", (long long)index);
+  return ws;
+}
+
+PyObject* latent_attention(PyObject*, PyObject* const* a, Py_ssize_t n) {
+  // cache, index, q, out, starts, seq_lens, page_table, seen, max_rows, max_seq_len, softmax_scale, causal, workspace, stream
+  return guarded(n, 14, [&]() -> PyObject* {
+    const dq_latent_cache* const cache = static_cast<const dq_latent_cache*>(address(a[0]));
+    const int64_t index = integer(a[1]);
+    const Heads q = plain_rows("q", a[2], cache->dtype, cache->latent_dim + cache->rot_dim, index, -1, -1, false);
+    const Heads out = plain_rows("out", a[3], cache->dtype, cache->latent_dim, index, q.c.heads, q.rows, true);
+    const dq_paged_batch b = batch_of(nullptr, index, a[4], a[5], a[6], Py_None, q.rows, true);
+    const uint64_t* const seen = none(a[7]) ? nullptr : masks("seen", a[7], q.rows, index);
+    const int32_t max_rows = int32("max_rows", a[8]), max_len = int32("max_seq_len", a[9]);
+    const float scale = (float)real(a[10]);
+    const int causal = PyObject_IsTrue(a[11]);
+    if (causal < 0) throw Refused{};
+    if (max_rows < 0 || max_len < 0) refuse("max_rows and max_seq_len must not be negative");
+    if (!(scale > 0.f)) refuse("softmax_scale must be positive");
+    if (seen && (!causal || max_rows > 64)) refuse("seen needs causal and at most 64 rows per sequence");
+    const at::Tensor& ws = workspace_of(a[12], index);
+    if (q.rows == 0) Py_RETURN_NONE;
+    void *const work = ws.data_ptr(), *const stream = address(a[13]);
+    return launch("dq_latent_attention", [&] {
+      return g_latent_attention(cache, &b, &q.c, &out.c, seen, max_rows, max_len, scale, work, (size_t)ws.numel(), causal ? DQ_PAGED_CAUSAL : 0u, stream);
+    });
+  });
+}
+
 PyObject* set_up(PyObject*, PyObject* const* a, Py_ssize_t n) {
-  // DQError, check(status, what), addresses of dq_rotate_heads, dq_paged_append, dq_paged_read, dq_paged_attention
-  return guarded(n, 6, [&]() -> PyObject* {
+  // DQError, check(status, what), addresses of the library's functions in this order
+  return guarded(n, 9, [&]() -> PyObject* {
     g_rotate = reinterpret_cast<decltype(g_rotate)>(address(a[2]));
     g_append = reinterpret_cast<decltype(g_append)>(address(a[3]));
     g_read = reinterpret_cast<decltype(g_read)>(address(a[4]));
     g_attention = reinterpret_cast<decltype(g_attention)>(address(a[5]));
+    g_latent_append = reinterpret_cast<decltype(g_latent_append)>(address(a[6]));
+    g_latent_read = reinterpret_cast<decltype(g_latent_read)>(address(a[7]));
+    g_latent_attention = reinterpret_cast<decltype(g_latent_attention)>(address(a[8]));
     Py_INCREF(a[0]);
     Py_INCREF(a[1]);
     g_error = a[0];
@@ -323,8 +436,15 @@ PyObject* set_up(PyObject*, PyObject* const* a, Py_ssize_t n) {
 template <PyObject* (*F)(PyObject*, PyObject* const*, Py_ssize_t)> PyMethodDef method(const char* name) {
   return {name, reinterpret_cast<PyCFunction>(reinterpret_cast<void (*)(void)>(F)), METH_FASTCALL, nullptr};
 }
-PyMethodDef g_methods[] = {method<set_up>("set_up"),           method<rotate_heads>("rotate_heads"),       method<paged_append>("paged_append"),
-                           method<paged_read>("paged_read"), method<paged_attention>("paged_attention"), {nullptr, nullptr, 0, nullptr}};
+PyMethodDef g_methods[] = {method<set_up>("set_up"),
+                           method<rotate_heads>("rotate_heads"),
+                           method<paged_append>("paged_append"),
+                           method<paged_read>("paged_read"),
+                           method<paged_attention>("paged_attention"),
+                           method<latent_append>("latent_append"),
+                           method<latent_read>("latent_read"),
+                           method<latent_attention>("latent_attention"),
+                           {nullptr, nullptr, 0, nullptr}};
 PyModuleDef g_module = {PyModuleDef_HEAD_INIT, "_paged", nullptr, -1, g_methods};
 
 }  // namespace

@@ -1,0 +1,122 @@
+"""Binding of attention over one latent vector a token (include/decoquant.h): the paged cache of latents with its append, read-back and
+absorbed attention, and attention over expanded keys and values.  Argument checks and marshalling only, the checks of tensors
+in csrc/paged_bind.cpp.  These operators serve: tensors that require gradients are taken as they are, outputs carry none."""
+from __future__ import annotations
+
+import ctypes as C
+from typing import Optional
+
+import torch
+
+from .binding import DQError, lib
+from .paged import _DTYPES, Rotary, _call, _module
+
+
+class _CLatent(C.Structure):
+    _fields_ = [("rows", C.c_void_p), ("pages", C.c_int32), ("page_tokens", C.c_int32), ("latent_dim", C.c_int32), ("rot_dim", C.c_int32),
+                ("dtype", C.c_int32)]
+
+
+def _declare() -> None:
+    i32, i64, f32, u32, size, ptr = C.c_int32, C.c_int64, C.c_float, C.c_uint32, C.c_size_t, C.c_void_p
+    cache = C.POINTER(_CLatent)
+    batch = heads = rot = ptr
+    lib.dq_latent_append.restype = i32
+    lib.dq_latent_append.argtypes = [cache, batch, ptr, i64, ptr, i64, ptr, f32, heads, heads, rot, ptr]
+    lib.dq_latent_read.restype = i32
+    lib.dq_latent_read.argtypes = [cache, batch, ptr, ptr, ptr, i64, ptr]
+    lib.dq_latent_workspace_bytes.restype = size
+    lib.dq_latent_workspace_bytes.argtypes = [cache, i32, i32, i32, i32, i32]
+    lib.dq_latent_attention.restype = i32
+    lib.dq_latent_attention.argtypes = [cache, batch, heads, heads, ptr, i32, i32, f32, ptr, size, u32, ptr]
+
+
+_declare()
+
+LATENT_FORMS = ((512, 64), (256, 32))     # channels of the latent and of the shared, rotated key
+
+
+class LatentCache:
+    """Device tensor of a layer's paged cache of latents, rows [pages, P, latent_dim + rot_dim] (float16 or bfloat16, P 64 or 128),
+    plus the C struct that points at it (dq_latent_cache)."""
+
+    def __init__(self, rows: torch.Tensor, latent_dim: int):
+        if rows.dim() != 3 or (latent_dim, rows.shape[2] - latent_dim) not in LATENT_FORMS or rows.shape[1] not in (64, 128):
+            raise DQError("rows must be [pages, 64 or 128, latent_dim + rot_dim], of 512 + 64 or 256 + 32 channels")
+        if rows.dtype not in _DTYPES or not (rows.is_cuda and rows.is_contiguous()) or rows.data_ptr() % 16 or not rows.shape[0]:
+            raise DQError("rows must be a contiguous, 16-byte aligned float16 or bfloat16 device tensor of at least one page")
+        if rows.shape[0] >= 1 << 31:
+            raise DQError("too many pages")
+        self.rows, self.latent_dim, self.rot_dim = rows, latent_dim, rows.shape[2] - latent_dim
+        self.pages, self.page_tokens, self.dtype, self.device, self.index = rows.shape[0], rows.shape[1], rows.dtype, rows.device, rows.get_device()
+        self.c = _CLatent(rows.data_ptr(), self.pages, self.page_tokens, self.latent_dim, self.rot_dim, _DTYPES[self.dtype])
+        self._at = C.addressof(self.c)
+
+    def nbytes(self) -> int:
+        return self.rows.numel() * self.rows.element_size()
+
+
+def alloc_latent_cache(pages: int, latent_dim: int = 512, rot_dim: int = 64, page_tokens: int = 64, dtype=torch.bfloat16,
+                       device="cuda:0") -> LatentCache:
+    """A paged cache of latents."""
+    if pages < 1 or (latent_dim, rot_dim) not in LATENT_FORMS or page_tokens not in (64, 128):
+        raise DQError("a cache of latents has pages of 64 or 128 tokens and 512 + 64 or 256 + 32 channels")
+    return LatentCache(torch.zeros((pages, page_tokens, latent_dim + rot_dim), dtype=dtype, device=device), latent_dim)
+
+
+def latent_append(cache: LatentCache, latent: torch.Tensor, k_rot: torch.Tensor, starts: Optional[torch.Tensor], seq_lens: torch.Tensor,
+                  page_table: torch.Tensor, q: Optional[torch.Tensor] = None, q_out: Optional[torch.Tensor] = None,
+                  rotary: Optional[Rotary] = None, positions: Optional[torch.Tensor] = None, weight: Optional[torch.Tensor] = None,
+                  eps: float = 1e-6):
+    """Append the rows of a ragged batch (dq_latent_append): latent [rows, latent_dim], normed where a weight is given, and k_rot [rows,
+    rot_dim], rotated where a rotation is; q [rows, heads, rot_dim], the queries' channels that meet k_rot, takes the same rotation
+    on the way.  Rows are views of a fused projection as they lie there.  starts: int32 [batch + 1], rows starts[b] ..
+    starts[b+1] - 1 are sequence b's last tokens (None: one row each); seq_lens: int32, the new rows included; page_table: int32
+    [batch, pages].  positions None: a token's place in its sequence.  Returns q_out (None without q).  Rows of no sequence stay
+    as they are.  seq_lens may go back at will: rows behind a sequence's end are never read."""
+    if q is None:
+        if q_out is not None:
+            raise DQError("q_out without q")
+    elif q_out is None:
+        q_out = torch.empty(q.shape, dtype=q.dtype, device=q.device)
+    index = cache.index
+    _call(_module.latent_append, index, cache._at, index, latent, k_rot, starts, seq_lens, page_table, q, q_out,
+          None if rotary is None else rotary._c, positions, weight, eps)
+    return q_out
+
+
+def latent_read(cache: LatentCache, first: Optional[torch.Tensor], seq_lens: torch.Tensor, out_starts: torch.Tensor, page_table: torch.Tensor,
+                out: torch.Tensor) -> torch.Tensor:
+    """The rows of tokens first[b] <= t < seq_lens[b] into out [rows, latent_dim + rot_dim], from row out_starts[b] to out_starts[b+1] - 1
+    at most (dq_latent_read; first None: from 0): what expanded_attention's keys and values are expanded from."""
+    index = cache.index
+    _call(_module.latent_read, index, cache._at, index, first, seq_lens, out_starts, page_table, out)
+    return out
+
+
+def _workspace_bytes(cache: LatentCache, batch: int, rows: int, q_heads: int, max_rows: int, max_seq_len: int) -> int:
+    n = lib.dq_latent_workspace_bytes(C.byref(cache.c), batch, rows, q_heads, max_rows, max_seq_len)
+    if n == 0:
+        raise DQError("dq_latent_workspace_bytes rejected the arguments")
+    return n
+
+
+def latent_workspace(cache: LatentCache, batch: int, rows: int, q_heads: int, max_rows: int, max_seq_len: int) -> torch.Tensor:
+    """Workspace of latent_attention for these sizes."""
+    return torch.empty(_workspace_bytes(cache, batch, rows, q_heads, max_rows, max_seq_len), dtype=torch.uint8, device=cache.device)
+
+
+def latent_attention(cache: LatentCache, q: torch.Tensor, starts: Optional[torch.Tensor], seq_lens: torch.Tensor, page_table: torch.Tensor,
+                     max_rows: int, max_seq_len: int, softmax_scale: float, workspace: torch.Tensor, out: Optional[torch.Tensor] = None,
+                     causal: bool = True, seen: Optional[torch.Tensor] = None) -> torch.Tensor:
+    """softmax(q . [c | k_rot] * softmax_scale) c of the batch's rows q [rows, heads, latent_dim + rot_dim] over the cached tokens of their
+    sequences, [rows, heads, latent_dim] (dq_latent_attention); rows are the last tokens of their sequence (append them first).
+    max_rows: host bound on the rows of any sequence; max_seq_len: on its tokens (a guess does).  seen: int64, a mask for each row: bit j
+    names the j-th row of the sequence (a tree of drafted tokens; at most 64 rows); None: every row up to its own place.
+    Rows of no sequence and a sequence's rows past max_rows are not written.  No gradients."""
+    if out is None:
+        out = torch.empty(q.shape[:2] + (cache.latent_dim,), dtype=q.dtype, device=q.device)
+    index = cache.index
+    _call(_module.latent_attention, index, cache._at, index, q, out, starts, seq_lens, page_table, seen, max_rows, max_seq_len, softmax_scale,
+          causal, workspace)
+    return out

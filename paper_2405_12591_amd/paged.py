@@ -41,14 +41,16 @@ def _declare() -> None:
 _declare()
 
 
+_COMPILED = ("rotate_heads", "paged_append", "paged_read", "paged_attention", "latent_append", "latent_read", "latent_attention")
+
+
 def _load_module():
     if not os.path.exists(_build.BIND_PATH):
         _build.build_binding()
     from . import _paged
     if getattr(_paged, "stamp", None) != _build.bind_stamp():   # its structs would not match the library's
         raise DQError("%s was built from other sources: rebuild it" % _build.BIND_PATH)
-    _paged.set_up(DQError, _check, *(C.cast(getattr(lib, n), C.c_void_p).value
-                                     for n in ("dq_rotate_heads", "dq_paged_append", "dq_paged_read", "dq_paged_attention")))
+    _paged.set_up(DQError, _check, *(C.cast(getattr(lib, "dq_" + n), C.c_void_p).value for n in _COMPILED))
     return _paged
 
 
@@ -59,7 +61,7 @@ class _Module:
         if name.startswith("_"):
             raise AttributeError(name)
         loaded = _load_module()
-        for n in ("rotate_heads", "paged_append", "paged_read", "paged_attention"):
+        for n in _COMPILED:
             setattr(self, n, getattr(loaded, n))
         return getattr(loaded, name)
 
