@@ -597,6 +597,35 @@ int32_t dq_latent_attention(const dq_latent_cache* cache, const dq_paged_batch* 
                             void* hip_stream);
 
 /*
+ * Expanded form: softmax((q . [k | k_rot]) * scale) v for ragged prompts over keys and values that lie packed,
+ * nothing paged: sequence b has rows starts[b] .. starts[b+1] - 1 of q and out and tokens kv_starts[b] ..
+ * kv_starts[b+1] - 1 of k, k_rot and v, and its rows are its last tokens (earlier ones were read back and expanded).
+ *   q [rows, heads, head_dim + rot_dim], k and v [tokens, heads, head_dim], k_rot [tokens, rot_dim],
+ *   out [rows, heads, head_dim]; head_dim and rot_dim are 128 and 64, or 64 and 32
+ */
+typedef struct dq_expanded {
+  dq_heads q, k, v, out;
+  const uint16_t* k_rot;            /* 16-byte aligned */
+  int64_t k_rot_stride;             /* a multiple of 8 */
+  const int32_t* starts;            /* i32 [batch + 1], ascending */
+  const int32_t* kv_starts;         /* i32 [batch + 1], ascending */
+  int32_t batch, rows, tokens;      /* rows of q, tokens of k, k_rot and v: what lies past them is not touched */
+  int32_t head_dim, rot_dim, dtype;
+} dq_expanded;
+
+size_t dq_expanded_workspace_bytes(int32_t batch, int32_t rows, int32_t heads, int32_t head_dim, int32_t max_rows,
+                                   int32_t max_seq_len);
+/*
+ *   max_rows, max_seq_len   host bounds as above (max_seq_len on a sequence's tokens)
+ *   softmax_scale           <= 0 selects 1/sqrt(head_dim + rot_dim)
+ *   flags                   DQ_PAGED_CAUSAL: row i sees tokens up to its own place; without it all of its sequence
+ * A row that sees no token yields zeros.  A row that sees no key or value that is not finite is untouched by those; one that
+ * does has values that are not finite.
+ */
+int32_t dq_expanded_attention(const dq_expanded* x, int32_t max_rows, int32_t max_seq_len, float softmax_scale,
+                              void* workspace, size_t workspace_bytes, uint32_t flags, void* hip_stream);
+
+/*
  * Measurement helper: read `bytes` (multiple of 16) from src with 128-bit loads and fold them
  * into sink[0..3] (u32) so the reads cannot be elided.  Gives the achievable read bandwidth
  * that the decode kernel's rate is compared with.

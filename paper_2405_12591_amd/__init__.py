@@ -54,4 +54,6 @@ from .latent import (  # noqa: F401
     latent_read,
     latent_workspace,
     latent_attention,
+    expanded_workspace,
+    expanded_attention,
 )

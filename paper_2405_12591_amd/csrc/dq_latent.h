@@ -18,6 +18,34 @@ inline bool latent_batch_ok(const dq_paged_batch* b, const dq_latent_cache* c, b
   return !uses_starts || b->starts || b->rows == b->batch;
 }
 
+// ---- memory to LDS, past the registers ----
+typedef __attribute__((address_space(3))) char* LdsBytes;
+typedef __attribute__((address_space(3))) const u32x4* LdsPieces;
+typedef short s16x4 __attribute__((ext_vector_type(4)));
+typedef __attribute__((address_space(3))) s16x4* LdsQuads;
+
+// 64 pieces of 16 bytes, one behind the other from `lds` on: a lane's piece is at base + offset, or at `from`.  As instructions of
+// their own: the compiler waits for all such copies ahead of every LDS read, the ones for later tiles too.  Kernels count
+// them themselves (no register is written; a wait that counts too many of them waits longer).
+__device__ __forceinline__ void copy_to_lds(const uint16_t* base, uint32_t offset, uint32_t lds) {
+  asm volatile("s_mov_b32 m0, %0\n\ts_nop 0\n\tglobal_load_lds_dwordx4 %1, %2" ::"s"(__builtin_amdgcn_readfirstlane(lds)), "v"(offset), "s"(base) : "memory");
+}
+__device__ __forceinline__ void copy_to_lds(const uint16_t* from, uint32_t lds) {
+  asm volatile("s_mov_b32 m0, %0\n\ts_nop 0\n\tglobal_load_lds_dwordx4 %1, off" ::"s"(__builtin_amdgcn_readfirstlane(lds)), "v"(from) : "memory");
+}
+__device__ __forceinline__ uint32_t lds_of(const void* p) { return (uint32_t)(uintptr_t)(LdsBytes)p; }
+
+// Eight 16-bit values: the left operand of a product with rows as they lie (token by token) as channels.  Of each 16 lanes, four read
+// 8 bytes each of one token's 16 channels, and lane i gets channel i of four tokens; `a` and `b` are the first and last four tokens.
+template <typename V> __device__ __forceinline__ V turned_rows(LdsBytes a, LdsBytes b) {
+  struct { s16x4 a, b; } const both = {__builtin_amdgcn_ds_read_tr16_b64_v4i16((LdsQuads)a), __builtin_amdgcn_ds_read_tr16_b64_v4i16((LdsQuads)b)};
+  return __builtin_bit_cast(V, both);
+}
+
+// What a token that is not there has (zeros: nothing sees it, and 0 * NaN of what lies there would not be 0), and the key channels of
+// a page that does not exist (NaN for those who see its tokens).
+__device__ const u32x4 g_blank[2] = {{0, 0, 0, 0}, {0x7FFF7FFFu, 0x7FFF7FFFu, 0x7FFF7FFFu, 0x7FFF7FFFu}};
+
 // A ragged batch's tiles in one line: sequence after sequence, in a sequence unit after unit (a tile of query columns, a kv head), in a
 // unit from its first token tile on.  Workgroup w takes tiles [w quota, (w + 1) quota) of the line, whatever units they belong
 // to, so that all end together however lengths differ.  A unit that one workgroup takes whole is written out; pieces of the others
@@ -88,21 +116,20 @@ struct Pieces {
 __device__ __forceinline__ Pieces pieces_of(long begin, int tiles, long quota) { return {begin / quota, (begin + tiles - 1) / quota}; }
 __device__ __forceinline__ long slot_of(const Pieces& p, long w) { return w == p.first ? 2 * w + 1 : 2 * w; }
 
-// Joins a column's pieces: a workgroup of four waves, which take every fourth of them.  o: [slot, column, D] floats, ml: [slot, column, 2].
-// Two pieces of a lane's channels are asked for at once, by all four waves.
-template <typename T, int D>
-__device__ __forceinline__ void join_column(const Pieces& p, const float* o, const float* ml, int columns, int column, uint16_t* out) {
+// Joins a column's pieces: a workgroup of four waves, which take every fourth of them, eight asked for at once.  o: [slot, column, D]
+// floats, ml: [slot, column, 2].
+template <typename T, int D, typename Slot>
+__device__ __forceinline__ void join_column(int count, Slot slot_of_piece, const float* o, const float* ml, int columns, int column, uint16_t* out) {
   constexpr int PER = D / 64, AHEAD = 8;
   __shared__ float s_o[4][D], s_m[4], s_l[4];
   const int tid = threadIdx.x, lane = tid & 63, wave = tid >> 6;
-  const int count = (int)(p.last - p.first) + 1;
   float m = -INFINITY, l = 0.f, x[PER] = {};
   for (int i0 = wave; i0 < count; i0 += 4 * AHEAD) {
     float y[AHEAD][PER], pm[AHEAD], pl[AHEAD];
 #pragma unroll
     for (int k = 0; k < AHEAD; ++k) {                     // (behind the last piece: that one again, with no weight)
       const int i = min(i0 + 4 * k, count - 1);
-      const long at = slot_of(p, p.first + i) * columns + column;
+      const long at = slot_of_piece(i) * columns + column;
       const f32x2 v = *reinterpret_cast<const f32x2*>(ml + 2 * at);
       pm[k] = i0 + 4 * k < count ? v.x : -INFINITY;
       pl[k] = v.y;

@@ -16,26 +16,6 @@ struct LatentArgs {
 
 constexpr int kLatentTile = 32;   // tokens
 
-typedef __attribute__((address_space(3))) char* LdsBytes;
-typedef __attribute__((address_space(3))) const u32x4* LdsPieces;
-typedef short s16x4 __attribute__((ext_vector_type(4)));
-typedef __attribute__((address_space(3))) s16x4* LdsQuads;
-
-// What a token that is not there has (zeros: nothing sees it, and 0 * NaN of what lies there would not be 0), and the key channels of
-// a page that does not exist (NaN for those who see its tokens).
-__device__ const u32x4 g_blank[2] = {{0, 0, 0, 0}, {0x7FFF7FFFu, 0x7FFF7FFFu, 0x7FFF7FFFu, 0x7FFF7FFFu}};
-
-// 64 pieces of 16 bytes to LDS, one behind the other from `lds` on, past the registers: lane's piece is at base + offset, or at `from`.  As
-// instructions of their own: the compiler waits for all such copies ahead of every LDS read, the ones for later tiles too.  The
-// kernel counts them itself (no register is written; a wait that counts too many of them waits longer).
-__device__ __forceinline__ void copy_to_lds(const uint16_t* base, uint32_t offset, uint32_t lds) {
-  asm volatile("s_mov_b32 m0, %0\n\ts_nop 0\n\tglobal_load_lds_dwordx4 %1, %2" ::"s"(lds), "v"(offset), "s"(base) : "memory");
-}
-__device__ __forceinline__ void copy_to_lds(const uint16_t* from, uint32_t lds) {
-  asm volatile("s_mov_b32 m0, %0\n\ts_nop 0\n\tglobal_load_lds_dwordx4 %1, off" ::"s"(lds), "v"(from) : "memory");
-}
-__device__ __forceinline__ uint32_t lds_of(const void* p) { return (uint32_t)(uintptr_t)(LdsBytes)p; }
-
 template <int M>
 __device__ __forceinline__ Weight latent_weight(const LatentArgs& a, int b) {
   const Sequence s = sequence_of(a.bt, a.c.page_tokens, b);
@@ -221,10 +201,7 @@ __global__ __launch_bounds__(256, (LatentShape<T, R, CB>::PER_SIMD)) void latent
 #pragma unroll
         for (int ks = 0; ks < 2; ++ks) {
           const LdsBytes from = c_from + 16 * ks * R * 2 + 256 * (c / 4);
-          const s16x4 lo = __builtin_amdgcn_ds_read_tr16_b64_v4i16((LdsQuads)(from + (v_at0 ^ 64 * (c % 4))));
-          const s16x4 hi = __builtin_amdgcn_ds_read_tr16_b64_v4i16((LdsQuads)(from + (v_at1 ^ 64 * (c % 4))));
-          struct { s16x4 a, b; } const both = {lo, hi};
-          o[ct] = mma32(__builtin_bit_cast(tx8, both), p[ks], o[ct]);
+          o[ct] = mma32(turned_rows<tx8>(from + (v_at0 ^ 64 * (c % 4)), from + (v_at1 ^ 64 * (c % 4))), p[ks], o[ct]);
         }
       }
     }
@@ -276,7 +253,7 @@ __global__ __launch_bounds__(256) void latent_join_kernel(LatentArgs a) {
   const long quota = line_quota(a.line, line_total(a.bt.batch, weight_of));
   const Pieces p = pieces_of(line_before(b, weight_of) + (long)(pair / M) * w.tiles, w.tiles, quota);
   if (p.first == p.last) return;
-  join_column<T, R>(p, a.o, a.ml, M, col, a.out.data + (long)(s.row0 + pair / H) * a.out.token_stride + (long)(pair % H) * a.out.head_stride);
+  join_column<T, R>((int)(p.last - p.first) + 1, [&](int i) { return slot_of(p, p.first + i); }, a.o, a.ml, M, col, a.out.data + (long)(s.row0 + pair / H) * a.out.token_stride + (long)(pair % H) * a.out.head_stride);
 }
 
 struct LatentPlan {

@@ -17,6 +17,7 @@ decltype(&dq_paged_attention) g_attention;
 decltype(&dq_latent_append) g_latent_append;
 decltype(&dq_latent_read) g_latent_read;
 decltype(&dq_latent_attention) g_latent_attention;
+decltype(&dq_expanded_attention) g_expanded_attention;
 PyObject* g_error;   // DQError
 PyObject* g_check;   // raises for a status
 
@@ -415,9 +416,53 @@ PyObject* latent_attention(PyObject*, PyObject* const* a, Py_ssize_t n) {
   });
 }
 
+PyObject* expanded_attention(PyObject*, PyObject* const* a, Py_ssize_t n) {
+  // index, q, k, k_rot, v, out, starts, kv_starts, max_rows, max_seq_len, softmax_scale, causal, workspace, stream
+  return guarded(n, 14, [&]() -> PyObject* {
+    const int64_t index = integer(a[0]);
+    const at::Tensor& first = tensor("v", a[4]);
+    if ((first.scalar_type() != at::kHalf && first.scalar_type() != at::kBFloat16) || index < 0) refuse("heads must be float16 or bfloat16 on a GPU");
+    dq_expanded x = {};
+    x.dtype = first.scalar_type() == at::kBFloat16 ? DQ_BF16 : DQ_F16;
+    const int64_t dim = first.dim() == 3 ? first.size(2) : 0;
+    if (dim != 128 && dim != 64) refuse("v must be [tokens, heads, 128 or 64]");
+    x.head_dim = (int32_t)dim;
+    x.rot_dim = (int32_t)(dim / 2);
+    const Heads v = plain_rows("v", a[4], x.dtype, dim, index, -1, -1, false);
+    const Heads k = plain_rows("k", a[2], x.dtype, dim, index, v.c.heads, v.rows, false);
+    const Rows k_rot = rows_of("k_rot", a[3], x.dtype, x.rot_dim, index, v.rows, false);
+    const Heads q = plain_rows("q", a[1], x.dtype, dim + x.rot_dim, index, v.c.heads, -1, false);
+    const Heads out = plain_rows("out", a[5], x.dtype, dim, index, v.c.heads, q.rows, true);
+    const int64_t batch = tensor("starts", a[6]).numel() - 1;
+    if (batch < 1 || batch >= INT32_MAX) refuse("a batch has at least one sequence");
+    x.q = q.c;
+    x.k = k.c;
+    x.v = v.c;
+    x.out = out.c;
+    x.k_rot = k_rot.data;
+    x.k_rot_stride = k_rot.stride;
+    x.starts = vector("starts", a[6], batch + 1, index);
+    x.kv_starts = vector("kv_starts", a[7], batch + 1, index);
+    x.batch = (int32_t)batch;
+    x.rows = (int32_t)q.rows;
+    x.tokens = (int32_t)v.rows;
+    const int32_t max_rows = int32("max_rows", a[8]), max_len = int32("max_seq_len", a[9]);
+    const float scale = (float)real(a[10]);
+    const int causal = PyObject_IsTrue(a[11]);
+    if (causal < 0) throw Refused{};
+    if (max_rows < 0 || max_len < 0) refuse("max_rows and max_seq_len must not be negative");
+    const at::Tensor& ws = workspace_of(a[12], index);
+    if (q.rows == 0) Py_RETURN_NONE;
+    void *const work = ws.data_ptr(), *const stream = address(a[13]);
+    return launch("dq_expanded_attention", [&] {
+      return g_expanded_attention(&x, max_rows, max_len, scale, work, (size_t)ws.numel(), causal ? DQ_PAGED_CAUSAL : 0u, stream);
+    });
+  });
+}
+
 PyObject* set_up(PyObject*, PyObject* const* a, Py_ssize_t n) {
   // DQError, check(status, what), addresses of the library's functions in this order
-  return guarded(n, 9, [&]() -> PyObject* {
+  return guarded(n, 10, [&]() -> PyObject* {
     g_rotate = reinterpret_cast<decltype(g_rotate)>(address(a[2]));
     g_append = reinterpret_cast<decltype(g_append)>(address(a[3]));
     g_read = reinterpret_cast<decltype(g_read)>(address(a[4]));
@@ -425,6 +470,7 @@ PyObject* set_up(PyObject*, PyObject* const* a, Py_ssize_t n) {
     g_latent_append = reinterpret_cast<decltype(g_latent_append)>(address(a[6]));
     g_latent_read = reinterpret_cast<decltype(g_latent_read)>(address(a[7]));
     g_latent_attention = reinterpret_cast<decltype(g_latent_attention)>(address(a[8]));
+    g_expanded_attention = reinterpret_cast<decltype(g_expanded_attention)>(address(a[9]));
     Py_INCREF(a[0]);
     Py_INCREF(a[1]);
     g_error = a[0];
@@ -444,6 +490,7 @@ PyMethodDef g_methods[] = {method<set_up>("set_up"),
                            method<latent_append>("latent_append"),
                            method<latent_read>("latent_read"),
                            method<latent_attention>("latent_attention"),
+                           method<expanded_attention>("expanded_attention"),
                            {nullptr, nullptr, 0, nullptr}};
 PyModuleDef g_module = {PyModuleDef_HEAD_INIT, "_paged", nullptr, -1, g_methods};
 

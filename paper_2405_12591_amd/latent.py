@@ -29,6 +29,10 @@ def _declare() -> None:
     lib.dq_latent_workspace_bytes.argtypes = [cache, i32, i32, i32, i32, i32]
     lib.dq_latent_attention.restype = i32
     lib.dq_latent_attention.argtypes = [cache, batch, heads, heads, ptr, i32, i32, f32, ptr, size, u32, ptr]
+    lib.dq_expanded_workspace_bytes.restype = size
+    lib.dq_expanded_workspace_bytes.argtypes = [i32, i32, i32, i32, i32, i32]
+    lib.dq_expanded_attention.restype = i32
+    lib.dq_expanded_attention.argtypes = [ptr, i32, i32, f32, ptr, size, u32, ptr]
 
 
 _declare()
@@ -119,4 +123,27 @@ def latent_attention(cache: LatentCache, q: torch.Tensor, starts: Optional[torch
     index = cache.index
     _call(_module.latent_attention, index, cache._at, index, q, out, starts, seq_lens, page_table, seen, max_rows, max_seq_len, softmax_scale,
           causal, workspace)
+    return out
+
+
+def expanded_workspace(batch: int, rows: int, heads: int, head_dim: int, max_rows: int, max_seq_len: int, device="cuda:0") -> torch.Tensor:
+    """Workspace of expanded_attention for these sizes and all smaller ones with the same heads."""
+    n = lib.dq_expanded_workspace_bytes(batch, rows, heads, head_dim, max_rows, max_seq_len)
+    if n == 0:
+        raise DQError("dq_expanded_workspace_bytes rejected the arguments")
+    return torch.empty(n, dtype=torch.uint8, device=device)
+
+
+def expanded_attention(q: torch.Tensor, k: torch.Tensor, k_rot: torch.Tensor, v: torch.Tensor, starts: torch.Tensor, kv_starts: torch.Tensor,
+                       max_rows: int, max_seq_len: int, workspace: torch.Tensor, out: Optional[torch.Tensor] = None,
+                       softmax_scale: float = 0.0, causal: bool = True) -> torch.Tensor:
+    """softmax((q . [k | k_rot]) * scale) v of ragged prompts (dq_expanded_attention): q [rows, heads, d + d / 2], k and v [tokens, heads, d],
+    k_rot [tokens, d / 2] for all heads, d 128 or 64; views of one projection as they lie.  starts, kv_starts: int32 [batch + 1],
+    the rows and the tokens of each sequence; its rows are its last tokens.  max_rows: host bound on the rows of any sequence;
+    max_seq_len: on its tokens (a guess does).  softmax_scale <= 0: 1 / sqrt(d + d / 2).  Rows of no sequence and a sequence's rows past
+    max_rows are not written.  No gradients."""
+    if out is None:
+        out = torch.empty(q.shape[:2] + v.shape[2:], dtype=q.dtype, device=q.device)
+    index = q.get_device()
+    _call(_module.expanded_attention, index, index, q, k, k_rot, v, out, starts, kv_starts, max_rows, max_seq_len, softmax_scale, causal, workspace)
     return out

@@ -41,7 +41,8 @@ def _declare() -> None:
 _declare()
 
 
-_COMPILED = ("rotate_heads", "paged_append", "paged_read", "paged_attention", "latent_append", "latent_read", "latent_attention")
+_COMPILED = ("rotate_heads", "paged_append", "paged_read", "paged_attention", "latent_append", "latent_read", "latent_attention",
+             "expanded_attention")
 
 
 def _load_module():
