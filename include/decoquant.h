@@ -536,6 +536,32 @@ int32_t dq_paged_attention(const dq_paged_cache* cache, const dq_paged_batch* ba
                            void* hip_stream);
 
 /*
+ * ---- Trees of drafted tokens over the paged 8-bit cache ----
+ *
+ * Drafted rows that are NOT in the cache attend to the cached tokens of their sequence, all of them, and to those
+ * drafted rows of it that a mask names (a row's ancestors in the tree, itself among them):
+ *   out[row, h] = softmax over both (q . K * scale) V
+ * so that refused rows leave nothing behind: accepted ones are appended afterwards (dq_paged_append), and no
+ * page is quantized with a row that goes.  Sequence b owns rows starts[b] .. starts[b+1] - 1; seq_lens are the
+ * CACHED tokens.  A row's place is seq_lens[b] + the number of rows it sees - 1.
+ *   q, out    [rows, q_heads, d]; out may be q
+ *   k, v      [rows, kv_heads, d], keys ready (rotated by their places)
+ *   seen      u64 [rows]: bit j: the row sees the j-th row of its sequence; bits of rows that are not there
+ *             count neither here nor for the place
+ *   max_rows  host bound on the rows of any sequence, 1..64 (or 0); further rows of that sequence are not seen and not written
+ *   window    > 0 (64 at least): of the cached tokens a row sees the ones less than `window` before its place only
+ * The rest is as for dq_paged_attention, but the workspace: it needs no zeros (dq_paged_tree_workspace_bytes, for these sizes
+ * and all smaller ones with the same heads; calls that share it must be ordered).  A drafted key or value row with a value
+ * that is not finite yields NaN for the rows that see it and does nothing to the others.
+ */
+size_t dq_paged_tree_workspace_bytes(const dq_paged_cache* cache, int32_t batch, int32_t rows, int32_t q_heads,
+                                     int32_t max_rows, int32_t max_seq_len);
+int32_t dq_paged_tree_attention(const dq_paged_cache* cache, const dq_paged_batch* batch, const dq_heads* q,
+                                const dq_heads* k, const dq_heads* v, const dq_heads* out, const uint64_t* seen,
+                                int32_t max_rows, int32_t max_seq_len, float softmax_scale, int32_t window,
+                                void* workspace, size_t workspace_bytes, uint32_t flags, void* hip_stream);
+
+/*
  * ---- Attention over one latent vector a token ----
  *
  * Layers whose heads' keys and values are products of one vector c a token (the latent) with the heads' weights,

@@ -36,6 +36,7 @@ EXPORTED_SYMBOLS = [
     "dq_compress_kv_ex", "dq_cache_append_workspace_bytes", "dq_cache_append",
     "dq_quantize_pack", "dq_stream_read",
     "dq_rotate_heads", "dq_paged_append", "dq_paged_read", "dq_paged_workspace_bytes", "dq_paged_attention",
+    "dq_paged_tree_workspace_bytes", "dq_paged_tree_attention",
     "dq_latent_append", "dq_latent_read", "dq_latent_workspace_bytes", "dq_latent_attention",
     "dq_expanded_workspace_bytes", "dq_expanded_attention",
 ]

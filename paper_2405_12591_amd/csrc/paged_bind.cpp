@@ -18,6 +18,7 @@ decltype(&dq_latent_append) g_latent_append;
 decltype(&dq_latent_read) g_latent_read;
 decltype(&dq_latent_attention) g_latent_attention;
 decltype(&dq_expanded_attention) g_expanded_attention;
+decltype(&dq_paged_tree_attention) g_tree_attention;
 PyObject* g_error;   // DQError
 PyObject* g_check;   // raises for a status
 
@@ -300,7 +301,7 @@ PyObject* paged_append(PyObject*, PyObject* const* a, Py_ssize_t n) {
 
 PyObject* paged_read(PyObject*, PyObject* const* a, Py_ssize_t n) {
   // cache, index, first, seq_lens, out_starts, page_table, tail_slots, k_out, v_out, stream
-  return guarded(n, 10, [&]() -> PyObject* {
+  return guarded(n, 11, [&]() -> PyObject* {
     const dq_paged_cache* const cache = static_cast<const dq_paged_cache*>(address(a[0]));
     const int64_t index = integer(a[1]);
     const Heads k = packed_rows(cache, index, "k_out", a[7], cache->kv_heads, -1, true);
@@ -460,9 +461,34 @@ PyObject* expanded_attention(PyObject*, PyObject* const* a, Py_ssize_t n) {
   });
 }
 
+PyObject* tree_attention(PyObject*, PyObject* const* a, Py_ssize_t n) {
+  // cache, index, q, k, v, out, seen, starts, seq_lens, page_table, tail_slots, max_rows, max_seq_len, softmax_scale, window, workspace, stream
+  return guarded(n, 17, [&]() -> PyObject* {
+    const dq_paged_cache* const cache = static_cast<const dq_paged_cache*>(address(a[0]));
+    const int64_t index = integer(a[1]);
+    const Heads q = packed_rows(cache, index, "q", a[2], -1, -1, false);
+    if (q.c.heads == 0 || q.c.heads % cache->kv_heads) refuse("q_heads must be a multiple of kv_heads");
+    const Heads k = packed_rows(cache, index, "k", a[3], cache->kv_heads, q.rows, false);
+    const Heads v = packed_rows(cache, index, "v", a[4], cache->kv_heads, q.rows, false);
+    const Heads out = packed_rows(cache, index, "out", a[5], q.c.heads, q.rows, true);
+    const uint64_t* const seen = masks("seen", a[6], q.rows, index);
+    const dq_paged_batch b = batch_of(cache, index, a[7], a[8], a[9], a[10], q.rows, true);
+    const int32_t max_rows = int32("max_rows", a[11]), max_len = int32("max_seq_len", a[12]), window = int32("window", a[14]);
+    const float scale = (float)real(a[13]);
+    if (max_rows < 0 || max_rows > 64 || max_len < 0) refuse("max_rows must be 0 to 64, max_seq_len not negative");
+    if (window != 0 && window < 64) refuse("a window must hold 64 tokens at least");
+    const at::Tensor& ws = workspace_of(a[15], index);
+    if (q.rows == 0) Py_RETURN_NONE;
+    void *const work = ws.data_ptr(), *const stream = address(a[16]);
+    return launch("dq_paged_tree_attention", [&] {
+      return g_tree_attention(cache, &b, &q.c, &k.c, &v.c, &out.c, seen, max_rows, max_len, scale, window, work, (size_t)ws.numel(), 0u, stream);
+    });
+  });
+}
+
 PyObject* set_up(PyObject*, PyObject* const* a, Py_ssize_t n) {
   // DQError, check(status, what), addresses of the library's functions in this order
-  return guarded(n, 10, [&]() -> PyObject* {
+  return guarded(n, 11, [&]() -> PyObject* {
     g_rotate = reinterpret_cast<decltype(g_rotate)>(address(a[2]));
     g_append = reinterpret_cast<decltype(g_append)>(address(a[3]));
     g_read = reinterpret_cast<decltype(g_read)>(address(a[4]));
@@ -471,6 +497,7 @@ PyObject* set_up(PyObject*, PyObject* const* a, Py_ssize_t n) {
     g_latent_read = reinterpret_cast<decltype(g_latent_read)>(address(a[7]));
     g_latent_attention = reinterpret_cast<decltype(g_latent_attention)>(address(a[8]));
     g_expanded_attention = reinterpret_cast<decltype(g_expanded_attention)>(address(a[9]));
+    g_tree_attention = reinterpret_cast<decltype(g_tree_attention)>(address(a[10]));
     Py_INCREF(a[0]);
     Py_INCREF(a[1]);
     g_error = a[0];
@@ -491,6 +518,7 @@ PyMethodDef g_methods[] = {method<set_up>("set_up"),
                            method<latent_read>("latent_read"),
                            method<latent_attention>("latent_attention"),
                            method<expanded_attention>("expanded_attention"),
+                           method<tree_attention>("paged_tree_attention"),
                            {nullptr, nullptr, 0, nullptr}};
 PyModuleDef g_module = {PyModuleDef_HEAD_INIT, "_paged", nullptr, -1, g_methods};
 

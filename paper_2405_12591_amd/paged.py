@@ -34,6 +34,10 @@ def _declare() -> None:
     lib.dq_paged_read.argtypes = [cache, batch, ptr, ptr, heads, heads, ptr]
     lib.dq_paged_workspace_bytes.restype = C.c_size_t
     lib.dq_paged_workspace_bytes.argtypes = [cache, i32, i32, i32, i32, i32]
+    lib.dq_paged_tree_workspace_bytes.restype = C.c_size_t
+    lib.dq_paged_tree_workspace_bytes.argtypes = [cache, i32, i32, i32, i32, i32]
+    lib.dq_paged_tree_attention.restype = i32
+    lib.dq_paged_tree_attention.argtypes = [cache, batch, heads, heads, heads, heads, ptr, i32, i32, C.c_float, i32, ptr, C.c_size_t, C.c_uint32, ptr]
     lib.dq_paged_attention.restype = i32
     lib.dq_paged_attention.argtypes = [cache, batch, heads, heads, i32, i32, C.c_float, i32, ptr, C.c_size_t, C.c_uint32, ptr]
 
@@ -42,7 +46,7 @@ _declare()
 
 
 _COMPILED = ("rotate_heads", "paged_append", "paged_read", "paged_attention", "latent_append", "latent_read", "latent_attention",
-             "expanded_attention")
+             "expanded_attention", "paged_tree_attention")
 
 
 def _load_module():
@@ -262,6 +266,32 @@ def paged_attention(cache: PagedCache, q: torch.Tensor, starts: Optional[torch.T
     index = cache.index
     _call(_module.paged_attention, index, cache._at, index, q, out, starts, seq_lens, page_table, tail_slots, max_rows, max_seq_len,
           softmax_scale, causal, window, splits, workspace)
+    return out
+
+
+def paged_tree_workspace(cache: PagedCache, batch: int, rows: int, q_heads: int, max_rows: int, max_seq_len: int) -> torch.Tensor:
+    """Workspace of paged_tree_attention for these sizes and all smaller ones with the same heads."""
+    n = lib.dq_paged_tree_workspace_bytes(C.byref(cache.c), batch, rows, q_heads, max_rows, max_seq_len)
+    if n == 0:
+        raise DQError("dq_paged_tree_workspace_bytes rejected the arguments")
+    return torch.empty(n, dtype=torch.uint8, device=cache.device)
+
+
+def paged_tree_attention(cache: PagedCache, q: torch.Tensor, k: torch.Tensor, v: torch.Tensor, seen: torch.Tensor, starts: Optional[torch.Tensor],
+                         seq_lens: torch.Tensor, page_table: torch.Tensor, max_rows: int, max_seq_len: int, workspace: torch.Tensor,
+                         out: Optional[torch.Tensor] = None, softmax_scale: float = 0.0, window: int = 0,
+                         tail_slots: Optional[torch.Tensor] = None) -> torch.Tensor:
+    """Attention of drafted rows that are not in the cache (dq_paged_tree_attention): q [rows, q_heads, d] over the seq_lens cached tokens of
+    their sequences and over those drafted rows k, v [rows, kv_heads, d] (rotated by their places) that `seen` names: int64, a mask for
+    each row, bit j its sequence's j-th row (the row itself and its ancestors).  A sequence has at most 64 rows, max_rows at most;
+    further ones are not seen and not written.  window > 0 (64 at least): of the cached tokens only those less than `window` before a row's
+    place, which is seq_lens plus the rows it sees, less one.  Accepted rows are appended afterwards, refused ones leave nothing.  out
+    may be q.  No gradients."""
+    if out is None:
+        out = torch.empty(q.shape, dtype=q.dtype, device=q.device)
+    index = cache.index
+    _call(_module.paged_tree_attention, index, cache._at, index, q, k, v, out, seen, starts, seq_lens, page_table, tail_slots, max_rows, max_seq_len,
+          softmax_scale, window, workspace)
     return out
 
 

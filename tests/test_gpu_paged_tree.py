@@ -1,0 +1,199 @@
+"""Attention of drafted trees over the paged 8-bit cache against the definition in 64 bits."""
+import pytest
+import torch
+
+import paper_2405_12591_amd as dq
+from latent_util import attend64, check, normal, starts_of
+from paged_util import DEV, HALF, Sequences, filled_cache, ints, quantize64
+
+pytestmark = pytest.mark.gpu
+
+BF, F16, I8, E4 = torch.bfloat16, torch.float16, torch.int8, torch.float8_e4m3fn
+
+
+def masks(counts, gen):
+    """Random trees: a row's parent is one of the rows before it or none; some rows do not see themselves, some see nothing drafted, and
+    bits of rows that are not there are set."""
+    out = []
+    for c in counts:
+        seen = []
+        for i in range(c):
+            parent = int(torch.randint(-1, max(i, 1), (1,), generator=gen)) if i else -1
+            seen.append((seen[parent] if parent >= 0 else 0) | 1 << i)
+        out += [0 if i % 11 == 7 else m ^ (1 << i) if i % 13 == 5 else m for i, m in enumerate(m | ((1 << 64) - (1 << c)) if i % 2 else m for i, m in enumerate(seen))]
+    return torch.tensor([m - (1 << 64) if m >> 63 else m for m in out], dtype=torch.int64)
+
+
+class Trees:
+    def __init__(self, lens, counts, q_heads, kv_heads, d, dtype, codes, page, seed, gap=0):
+        gen = torch.Generator().manual_seed(seed)
+        self.lens, self.counts, self.gap, self.q_heads, self.kv_heads, self.d, self.dtype = lens, counts, gap, q_heads, kv_heads, d, dtype
+        self.seqs = Sequences(lens, kv_heads, d, dtype, codes, page, gen)
+        self.cache, self.table, self.slots = filled_cache(self.seqs, lens, gen)
+        total = sum(counts) + gap + 2
+        self.qkv = normal((total, q_heads + 2 * kv_heads, d), dtype, gen)
+        self.seen = torch.full((total,), -1, dtype=torch.int64)
+        self.seen[gap:gap + sum(counts)] = masks(counts, gen)
+        self.starts = starts_of(counts, gap)
+
+    def run(self, window=0, max_rows=None, max_len=None, out=None, ws=None, table=None, scale=0.0):
+        h, max_rows, max_len = self.kv_heads, max(self.counts) if max_rows is None else max_rows, max(self.lens) if max_len is None else max_len
+        if ws is None:
+            ws = dq.paged_tree_workspace(self.cache, len(self.lens), len(self.qkv), self.q_heads, max_rows, max_len)
+            ws.fill_(255)
+        x = self.qkv.to(DEV)
+        q, k, v = x[:, :self.q_heads], x[:, self.q_heads:self.q_heads + h], x[:, self.q_heads + h:]
+        out = torch.full((len(x), self.q_heads, self.d), 7.0, dtype=self.dtype, device=DEV) if out is None else out
+        dq.paged_tree_attention(self.cache, q, k, v, self.seen.to(DEV), ints(self.starts), ints(self.lens), self.table if table is None else table, max_rows,
+                                max_len, ws, out=out, window=window, tail_slots=self.slots, softmax_scale=scale)
+        return out
+
+    def want(self, window=0, scale=None):
+        hq, h, d, g = self.q_heads, self.kv_heads, self.d, self.q_heads // self.kv_heads
+        scale = d ** -0.5 if scale is None else scale
+        out = torch.full((len(self.qkv), hq, d), 7.0, dtype=torch.float64)
+        tol, own = torch.zeros_like(out), torch.zeros(len(out), dtype=torch.bool)
+        for b, (c, n) in enumerate(zip(self.counts, self.lens)):
+            r = slice(self.starts[b], self.starts[b + 1])
+            k = torch.cat([self.seqs.stored(self.seqs.k[b]), self.qkv[r, hq:hq + h].double()])
+            v = torch.cat([self.seqs.stored(self.seqs.v[b]), self.qkv[r, hq + h:].double()])
+            see = torch.zeros(c, n + c, dtype=torch.bool)
+            for i in range(c):
+                bits = [bool(int(self.seen[self.starts[b] + i]) >> j & 1) for j in range(c)]
+                see[i, n:] = torch.tensor(bits)
+                see[i, :n] = torch.arange(n) > n + sum(bits) - 1 - window if window else True
+            o, size, ds = attend64(self.qkv[r, :hq], k.repeat_interleave(g, 1), v.repeat_interleave(g, 1), see, scale)
+            # half a step of the result; probabilities in f16 over codes, in the rows' type over 16-bit rows (all here, for simplicity); f16's
+            # smallest step for each token; scores: 16 matrix instructions of 16 products at the most, four roundings each, 2^-18 of the sum of
+            # their sizes, queries of bf16 exact in f16, twice (numerator and sum); 2^-18 for exponentials, scales and the sums over tokens
+            v_max = float(v.abs().max()) if len(v) else 0.0
+            out[r], own[r] = o, True
+            tol[r] = o.abs() * HALF[self.dtype] + size * (HALF[self.dtype] + 2.0 ** -18 + 2 * 2.0 ** -18 * ds) + (n + c) * 2.0 ** -25 * v_max + 2.0 ** -24
+        return out, tol, own
+
+
+@pytest.mark.parametrize("dtype,codes,d,page", [(BF, E4, 128, 64), (F16, I8, 128, 128), (BF, I8, 64, 128), (F16, E4, 64, 64)])
+@pytest.mark.parametrize("lens,counts,q_heads,kv_heads,gap", [
+    ([1, 63, 64, 65, 300], [1, 5, 31, 32, 2], 4, 4, 2),             # lengths around pages and tiles, one block of columns
+    ([130, 0, 77], [9, 3, 0], 12, 2, 0),                            # groups of six: two blocks; no cached tokens; no rows
+    ([200, 129], [64, 33], 4, 2, 1),                                # full trees: four blocks of columns
+    ([90], [13], 24, 1, 0),                                         # three tiles of 128 columns
+])
+def test_attention(dtype, codes, d, page, lens, counts, q_heads, kv_heads, gap):
+    x = Trees(lens, counts, q_heads, kv_heads, d, dtype, codes, page, d + page, gap)
+    check(x.run(), *x.want())
+
+
+@pytest.mark.parametrize("window", [64, 65, 100, 1000, 2 ** 31 - 1])
+def test_windows(window):
+    x = Trees([300, 64, 10, 0], [20, 40, 5, 3], 4, 2, 64, BF, E4, 64, 3)
+    check(x.run(window=window), *x.want(window=window))
+
+
+def test_long_caches_and_many_sequences():
+    for lens, counts, heads, d in (([6000, 40, 2500], [17, 60, 3], (2, 1), 128), ([1 + 11 * i % 150 for i in range(140)], [1 + i % 5 for i in range(140)], (3, 3), 64)):
+        x = Trees(lens, counts, *heads, d, BF, I8, 64, 4)
+        want = x.want()
+        for max_len in (max(lens), 1, 100000):
+            check(x.run(max_len=max_len), *want, "bound %d" % max_len)
+
+
+def test_a_row_that_sees_nothing_is_zero_and_the_output_may_be_the_queries():
+    x = Trees([0, 70], [6, 2], 3, 3, 64, F16, I8, 64, 5)
+    x.seen[:6] = torch.tensor([1, 0, 5, 1 << 40, 0, 63])
+    want, tol, own = x.want()
+    got = x.run()
+    check(got, want, tol, own)
+    assert not got[[1, 3, 4]].any()
+    q = x.qkv.to(DEV)
+    dq.paged_tree_attention(x.cache, q[:, :3], q[:, 3:6], q[:, 6:], x.seen.to(DEV), ints(x.starts), ints(x.lens), x.table, 6, 70,
+                            dq.paged_tree_workspace(x.cache, 2, len(q), 3, 6, 70), out=q[:, :3], tail_slots=x.slots)
+    assert torch.equal(q[:8, :3], got[:8])
+
+
+def test_rows_past_the_bound_are_neither_seen_nor_written():
+    x = Trees([100, 40], [20, 9], 4, 4, 64, BF, E4, 64, 6)
+    x.seen[:] = -1
+    got = x.run(max_rows=9)
+    x.seen[:20] = 511                                               # of the first nine rows
+    want, tol, _ = x.want()
+    fine = (got.double().cpu() - want).abs() <= tol
+    assert bool(fine[:9].all()) and bool(fine[20:29].all()) and bool((got[9:20] == 7).all())
+
+
+def test_pages_and_slots_that_do_not_exist_and_rows_that_are_not_finite():
+    x = Trees([200, 100, 30], [10, 12, 7], 4, 2, 64, F16, I8, 64, 7)
+    want, tol, _ = x.want()
+    table = x.table.clone()
+    table[0, 1] = -3
+    got = x.run(table=table).double().cpu()
+    assert got[:10].isnan().all() and bool(((got - want).abs() <= tol)[10:29].all())
+    slots = x.slots.clone()
+    x.slots = slots.clone()
+    x.slots[1] = 99
+    got = x.run().double().cpu()
+    assert got[10:22].isnan().all() and bool(((got - want).abs() <= tol)[:10].all()) and bool(((got - want).abs() <= tol)[22:29].all())
+    x.slots = slots
+    # drafted rows: a key of the second sequence's third row, a value of the first's last
+    x.qkv[12, 4 + 1, 9], x.qkv[9, 4 + 2 + 0, 63] = float("inf"), float("nan")
+    x.seen[:10], x.seen[10:22], x.seen[22:29] = 7, 3, -1
+    x.seen[4], x.seen[15], x.seen[0] = 1 << 9 | 1, 4, 1 << 9
+    got = x.run().double().cpu()
+    x.qkv[12, 5, 9], x.qkv[9, 6, 63] = 0.0, 0.0
+    want, tol, _ = x.want()
+    fine = (got - want).abs() <= tol
+    hit = torch.zeros(len(want), 4, dtype=torch.bool)
+    hit[[4, 0], :2] = True                                          # heads 0, 1 read kv head 0
+    hit[15, 2:] = True
+    assert bool(fine[:29][~hit[:29]].all()) and bool(got[hit].isnan().all())
+
+
+def test_a_chain_is_what_appended_rows_see():
+    """A chain of drafted rows, unquantized, against the same rows appended: the same within the rounding of both."""
+    x = Trees([64, 128], [5, 8], 4, 4, 64, F16, I8, 64, 8)
+    x.seen[:13] = torch.tensor([(1 << i + 1) - 1 for c in x.counts for i in range(c)])
+    got = x.run()
+    q, k, v = (x.qkv[:13, i:i + 4].contiguous().to(DEV) for i in (0, 4, 8))
+    lens, width = [69, 136], 3
+    cache, table = x.cache, torch.cat([x.table, x.table[:, -1:] * 0 + torch.tensor([[x.cache.pages - 1], [x.cache.pages - 2]], device=DEV, dtype=torch.int32)], 1).contiguous()
+    dq.paged_append(cache, k, v, ints([0, 5, 13]), ints(lens), table, tail_slots=x.slots)
+    ws = dq.paged_workspace(cache, 2, 13, 4, 8, 136)
+    appended = dq.paged_attention(cache, q, ints([0, 5, 13]), ints(lens), table, 8, 136, ws, tail_slots=x.slots)
+    want, tol, _ = x.want()
+    assert bool(((appended.double().cpu() - want[:13]).abs() <= tol[:13]).all()) and bool(((got.double().cpu() - want).abs() <= tol)[:13].all())
+
+
+def test_one_workspace_and_a_captured_call():
+    x = Trees([500, 900], [16, 30], 8, 2, 128, BF, E4, 64, 9)
+    ws = dq.paged_tree_workspace(x.cache, 2, len(x.qkv), 8, 30, 900)
+    ws.fill_(255)
+    first = x.run(ws=ws)
+    q = x.qkv.to(DEV)
+    out, seen, starts, lens = torch.zeros_like(first), x.seen.to(DEV), ints(x.starts), ints(x.lens)
+
+    def call(out, ws):
+        dq.paged_tree_attention(x.cache, q[:, :8], q[:, 8:10], q[:, 10:], seen, starts, lens, x.table, 30, 900, ws, out=out, tail_slots=x.slots)
+
+    side = torch.cuda.Stream()
+    side.wait_stream(torch.cuda.current_stream())
+    with torch.cuda.stream(side):
+        call(out, ws)
+    torch.cuda.current_stream().wait_stream(side)
+    assert torch.equal(out[:46], first[:46])
+    graph = torch.cuda.CUDAGraph()
+    with torch.cuda.graph(graph):
+        call(out, ws)
+    other, other_ws = torch.zeros_like(out), torch.zeros_like(ws)
+    for i in range(5):
+        q.copy_(normal(x.qkv.shape, x.dtype, torch.Generator().manual_seed(i)))
+        lens -= 37                                                  # lengths are the device's (and inside pages whose tails hold NaN: bits)
+        out.zero_()
+        graph.replay()
+        call(other, other_ws)
+        torch.cuda.synchronize()
+        assert torch.equal(out[:46].view(torch.int16), other[:46].view(torch.int16))
+        lens.copy_(ints([448 - 64 * i, 896 - 64 * i]))               # to the ends of pages: tokens that are there
+        graph.replay()
+        call(other, other_ws)
+        torch.cuda.synchronize()
+        assert bool(out[:46].isfinite().all()) and torch.equal(out[:46], other[:46])
