@@ -216,17 +216,19 @@ template <typename T, int D>
 __global__ __launch_bounds__(256) void expanded_join_kernel(ExpandedArgs a) {
   constexpr int M = kExpandedRows;
   const dq_expanded& x = a.x;
-  const int H = x.q.heads, col = (int)(blockIdx.x % M);
-  const long unit = blockIdx.x / M;
+  constexpr unsigned GROUPS = M / kJoinColumns;
+  const int H = x.q.heads, col = (int)(blockIdx.x % GROUPS) * kJoinColumns;
+  const long unit = blockIdx.x / GROUPS;
   const int h = (int)(unit % H), item = (int)(unit / H);
   const int b = a.seq_tiles ? item / a.seq_tiles : item_owner(x.starts, x.rows, x.batch, item, 1, M, 1);
   const ExpandedSequence s = expanded_sequence(x, b);
   const int n = min(s.n, a.max_rows), row_tiles = (n + M - 1) / M;
   const int j = a.seq_tiles ? item % a.seq_tiles : item - item_first(x.starts, x.rows, b, 1, M, 1);
-  const int row = (row_tiles - 1 - j) * M + col;
-  if (j < 0 || j >= row_tiles || row >= n) return;
-  join_column<T, D>(a.splits, [&](int i) { return unit * a.splits + i; }, a.o, a.ml, M, col,
-                    x.out.data + (long)(s.row0 + row) * x.out.token_stride + (long)h * x.out.head_stride);
+  const int first = (row_tiles - 1 - j) * M;
+  if (j < 0 || j >= row_tiles || first + col >= n) return;
+  join_columns<T, D>(a.splits, [&](int i) { return unit * a.splits + i; }, a.o, a.ml, M, col, min(n - first, M), [&](int c) {
+    return x.out.data + (long)(s.row0 + first + c) * x.out.token_stride + (long)h * x.out.head_stride;
+  });
 }
 
 struct ExpandedPlan {
@@ -261,7 +263,7 @@ static bool expanded_dims_ok(int head_dim, int rot_dim) { return (head_dim == 12
 template <typename T, int D>
 static void launch_expanded(const ExpandedArgs& a, const ExpandedPlan& p, hipStream_t st) {
   hipLaunchKernelGGL((expanded_attn_kernel<T, D>), dim3((unsigned)(p.units * a.splits)), dim3(256), 0, st, a);
-  if (a.splits > 1) hipLaunchKernelGGL((expanded_join_kernel<T, D>), dim3((unsigned)(p.units * kExpandedRows)), dim3(256), 0, st, a);
+  if (a.splits > 1) hipLaunchKernelGGL((expanded_join_kernel<T, D>), dim3((unsigned)(p.units * (kExpandedRows / kJoinColumns))), dim3(256), 0, st, a);
 }
 
 }  // namespace dq

@@ -106,8 +106,20 @@ template <typename F> __device__ __forceinline__ int line_owner(int batch, long 
   return batch;
 }
 
-// The places of the line before sequence b.
-template <typename F> __device__ __forceinline__ long line_before(int b, F weight_of) { return line_total(b, weight_of); }
+// The line's length, and its places before sequence b.
+struct LineSums {
+  long total, before;
+};
+template <typename F> __device__ __forceinline__ LineSums line_sums(int batch, int b, F weight_of) {
+  long all = 0, lower = 0;
+  for (int i = threadIdx.x & 63; i < batch; i += 64) {
+    const Weight w = weight_of(i);
+    const long n = (long)w.units * w.tiles;
+    all += n;
+    if (i < b) lower += n;
+  }
+  return {wave_uniform(wave_sum(all)), wave_uniform(wave_sum(lower))};
+}
 
 // Pieces of a unit whose tiles are places [begin, begin + tiles) of the line: the workgroups first .. last, one piece each.
 struct Pieces {
@@ -116,59 +128,81 @@ struct Pieces {
 __device__ __forceinline__ Pieces pieces_of(long begin, int tiles, long quota) { return {begin / quota, (begin + tiles - 1) / quota}; }
 __device__ __forceinline__ long slot_of(const Pieces& p, long w) { return w == p.first ? 2 * w + 1 : 2 * w; }
 
-// Joins a column's pieces: a workgroup of four waves, which take every fourth of them, eight asked for at once.  o: [slot, column, D]
-// floats, ml: [slot, column, 2].
-template <typename T, int D, typename Slot>
-__device__ __forceinline__ void join_column(int count, Slot slot_of_piece, const float* o, const float* ml, int columns, int column, uint16_t* out) {
+// Joins the pieces of kJoinColumns columns (those below `valid`): a wave a column where there are few pieces, four waves a column, which take
+// every fourth piece, where there are many.  o: [slot, column, D] floats, ml: [slot, column, 2]; eight pieces are asked for at once.
+// (A workgroup a column spent most of its time on finding its unit: 39 us where this takes 8, 64 columns of 128 units in 4 or 5 pieces.)
+constexpr int kJoinColumns = 4;
+template <typename T, int D, typename Slot, typename Out>
+__device__ __forceinline__ void join_columns(int count, Slot slot_of_piece, const float* o, const float* ml, int columns, int column0, int valid, Out out_of) {
   constexpr int PER = D / 64, AHEAD = 8;
   __shared__ float s_o[4][D], s_m[4], s_l[4];
-  const int tid = threadIdx.x, lane = tid & 63, wave = tid >> 6;
-  float m = -INFINITY, l = 0.f, x[PER] = {};
-  for (int i0 = wave; i0 < count; i0 += 4 * AHEAD) {
-    float y[AHEAD][PER], pm[AHEAD], pl[AHEAD];
+  const int tid = threadIdx.x, lane = tid & 63, wave = __builtin_amdgcn_readfirstlane(tid >> 6);
+  struct Sum { float m, l, x[PER]; };
+  auto add = [&](int column, int from, int step) {
+    Sum r = {-INFINITY, 0.f, {}};
+    for (int i0 = from; i0 < count; i0 += step * AHEAD) {
+      float y[AHEAD][PER], pm[AHEAD], pl[AHEAD];
 #pragma unroll
-    for (int k = 0; k < AHEAD; ++k) {                     // (behind the last piece: that one again, with no weight)
-      const int i = min(i0 + 4 * k, count - 1);
-      const long at = slot_of_piece(i) * columns + column;
-      const f32x2 v = *reinterpret_cast<const f32x2*>(ml + 2 * at);
-      pm[k] = i0 + 4 * k < count ? v.x : -INFINITY;
-      pl[k] = v.y;
+      for (int k = 0; k < AHEAD; ++k) {                   // (behind the last piece: that one again, with no weight)
+        const long at = slot_of_piece(min(i0 + step * k, count - 1)) * columns + column;
+        const f32x2 v = *reinterpret_cast<const f32x2*>(ml + 2 * at);
+        pm[k] = i0 + step * k < count ? v.x : -INFINITY;
+        pl[k] = v.y;
 #pragma unroll
-      for (int e = 0; e < PER; ++e) y[k][e] = o[at * D + PER * lane + e];
+        for (int e = 0; e < PER; ++e) y[k][e] = o[at * D + PER * lane + e];
+      }
+      float top = r.m;
+#pragma unroll
+      for (int k = 0; k < AHEAD; ++k) top = fmaxf(top, pm[k]);
+      const float at = top == -INFINITY ? 0.f : top, back = __builtin_amdgcn_exp2f(r.m - at);
+      r.m = top;
+      r.l *= back;
+#pragma unroll
+      for (int e = 0; e < PER; ++e) r.x[e] *= back;
+#pragma unroll
+      for (int k = 0; k < AHEAD; ++k) {
+        const float w = __builtin_amdgcn_exp2f(pm[k] - at);
+        r.l = __builtin_fmaf(pl[k], w, r.l);
+#pragma unroll
+        for (int e = 0; e < PER; ++e) r.x[e] = __builtin_fmaf(y[k][e], w, r.x[e]);
+      }
     }
-    float top = m;
+    return r;
+  };
+  auto store = [&](uint16_t* out, const float* x, float l) {   // PER neighbouring channels a lane
+    const float inv = l == 0.f ? 0.f : 1.f / l;
+    if constexpr (PER == 1) {
+      out[lane] = (uint16_t)pack2<T>(x[0] * inv, 0.f);
+    } else {
 #pragma unroll
-    for (int k = 0; k < AHEAD; ++k) top = fmaxf(top, pm[k]);
-    const float at = top == -INFINITY ? 0.f : top, back = __builtin_amdgcn_exp2f(m - at);
-    m = top;
-    l *= back;
-#pragma unroll
-    for (int e = 0; e < PER; ++e) x[e] *= back;
-#pragma unroll
-    for (int k = 0; k < AHEAD; ++k) {
-      const float w = __builtin_amdgcn_exp2f(pm[k] - at);
-      if (i0 + 4 * k >= count) break;
-      l = __builtin_fmaf(pl[k], w, l);
-#pragma unroll
-      for (int e = 0; e < PER; ++e) x[e] = __builtin_fmaf(y[k][e], w, x[e]);
+      for (int e = 0; e < PER; e += 2) reinterpret_cast<uint32_t*>(out + PER * lane)[e / 2] = pack2<T>(x[e] * inv, x[e + 1] * inv);
     }
+  };
+  if (count <= 4 * AHEAD) {
+    if (column0 + wave >= valid) return;
+    const Sum r = add(column0 + wave, 0, 1);
+    store(out_of(column0 + wave), r.x, r.l);
+    return;
   }
+  for (int c = column0; c < min(column0 + kJoinColumns, valid); ++c) {
+    const Sum r = add(c, wave, 4);
+    __syncthreads();                                      // the last column's results have been read
 #pragma unroll
-  for (int e = 0; e < PER; ++e) s_o[wave][PER * lane + e] = x[e];
-  if (lane == 0) { s_m[wave] = m; s_l[wave] = l; }
-  __syncthreads();
-  if (2 * tid >= D) return;
-  const float top = fmaxf(fmaxf(s_m[0], s_m[1]), fmaxf(s_m[2], s_m[3])), at = top == -INFINITY ? 0.f : top;
-  float a = 0.f, b = 0.f, sum = 0.f;
+    for (int e = 0; e < PER; ++e) s_o[wave][PER * lane + e] = r.x[e];
+    if (lane == 0) { s_m[wave] = r.m; s_l[wave] = r.l; }
+    __syncthreads();
+    if (wave != (c & 3)) continue;
+    const float top = fmaxf(fmaxf(s_m[0], s_m[1]), fmaxf(s_m[2], s_m[3])), at = top == -INFINITY ? 0.f : top;
+    float x[PER] = {}, l = 0.f;
 #pragma unroll
-  for (int w = 0; w < 4; ++w) {
-    const float f = __builtin_amdgcn_exp2f(s_m[w] - at);
-    sum = __builtin_fmaf(s_l[w], f, sum);
-    a = __builtin_fmaf(s_o[w][2 * tid], f, a);
-    b = __builtin_fmaf(s_o[w][2 * tid + 1], f, b);
+    for (int w = 0; w < 4; ++w) {
+      const float f = __builtin_amdgcn_exp2f(s_m[w] - at);
+      l = __builtin_fmaf(s_l[w], f, l);
+#pragma unroll
+      for (int e = 0; e < PER; ++e) x[e] = __builtin_fmaf(s_o[w][PER * lane + e], f, x[e]);
+    }
+    store(out_of(c), x, l);
   }
-  const float inv = sum == 0.f ? 0.f : 1.f / sum;
-  reinterpret_cast<uint32_t*>(out)[tid] = pack2<T>(a * inv, b * inv);
 }
 
 }  // namespace dq

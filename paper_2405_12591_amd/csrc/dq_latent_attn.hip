@@ -243,17 +243,21 @@ __global__ __launch_bounds__(256, (LatentShape<T, R, CB>::PER_SIMD)) void latent
 template <typename T, int R, int CB>
 __global__ __launch_bounds__(256) void latent_join_kernel(LatentArgs a) {
   constexpr int M = LatentShape<T, R, CB>::M;
-  const int H = a.q.heads, item = (int)(blockIdx.x / M), col = (int)(blockIdx.x % M);
+  constexpr int GROUPS = M / kJoinColumns;
+  const int H = a.q.heads, item = (int)(blockIdx.x / GROUPS), col = (int)(blockIdx.x % GROUPS) * kJoinColumns;
   const int b = item_owner(a.bt.starts, a.bt.rows, a.bt.batch, item, H, M, 1);
   const Sequence s = sequence_of_wave(a.bt, a.c.page_tokens, b);
-  const int n = min(s.n, a.max_rows), pair = (item - item_first(a.bt.starts, a.bt.rows, b, H, M, 1)) * M + col;
-  if (pair < 0 || pair >= n * H) return;
+  const int pairs = min(s.n, a.max_rows) * H, first = (item - item_first(a.bt.starts, a.bt.rows, b, H, M, 1)) * M;
+  if (first < 0 || first + col >= pairs) return;
   const auto weight_of = [&](int i) { return latent_weight<M>(a, i); };
-  const Weight w = weight_of(b);
-  const long quota = line_quota(a.line, line_total(a.bt.batch, weight_of));
-  const Pieces p = pieces_of(line_before(b, weight_of) + (long)(pair / M) * w.tiles, w.tiles, quota);
+  const int tiles = weight_of(b).tiles;
+  const LineSums sums = line_sums(a.bt.batch, b, weight_of);
+  const Pieces p = pieces_of(sums.before + (long)(first / M) * tiles, tiles, line_quota(a.line, sums.total));
   if (p.first == p.last) return;
-  join_column<T, R>((int)(p.last - p.first) + 1, [&](int i) { return slot_of(p, p.first + i); }, a.o, a.ml, M, col, a.out.data + (long)(s.row0 + pair / H) * a.out.token_stride + (long)(pair % H) * a.out.head_stride);
+  join_columns<T, R>((int)(p.last - p.first) + 1, [&](int i) { return slot_of(p, p.first + i); }, a.o, a.ml, M, col, min(pairs - first, M), [&](int c) {
+    const int pair = first + c;
+    return a.out.data + (long)(s.row0 + pair / H) * a.out.token_stride + (long)(pair % H) * a.out.head_stride;
+  });
 }
 
 struct LatentPlan {
@@ -277,7 +281,7 @@ static size_t latent_bytes(const dq_latent_cache* c, const LatentPlan& p) {
 template <typename T, int R, int CB>
 static void launch_latent(const LatentArgs& a, const LatentPlan& p, hipStream_t st) {
   hipLaunchKernelGGL((latent_attn_kernel<T, R, CB>), dim3((unsigned)p.workgroups), dim3(256), 0, st, a);
-  hipLaunchKernelGGL((latent_join_kernel<T, R, CB>), dim3((unsigned)(p.items * 32 * CB)), dim3(256), 0, st, a);
+  hipLaunchKernelGGL((latent_join_kernel<T, R, CB>), dim3((unsigned)(p.items * (32 * CB / kJoinColumns))), dim3(256), 0, st, a);
 }
 template <typename T, int R>
 static void launch_latent_cols(const LatentArgs& a, const LatentPlan& p, hipStream_t st) {

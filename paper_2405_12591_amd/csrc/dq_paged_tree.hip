@@ -412,17 +412,21 @@ __global__ __launch_bounds__(256, 2) void tree_attn_kernel(TreeArgs a) {
 template <typename T, int D, int CB>
 __global__ __launch_bounds__(256) void tree_join_kernel(TreeArgs a) {
   constexpr int M = 32 * CB;
-  const int H = a.c.kv_heads, col = (int)(blockIdx.x % M), h = (int)(blockIdx.x / M % (unsigned)H), item = (int)(blockIdx.x / M / (unsigned)H);
+  constexpr unsigned GROUPS = M / kJoinColumns;
+  const int H = a.c.kv_heads, col = (int)(blockIdx.x % GROUPS) * kJoinColumns, h = (int)(blockIdx.x / GROUPS % (unsigned)H);
+  const int item = (int)(blockIdx.x / GROUPS / (unsigned)H);
   const int b = item_owner(a.bt.starts, a.bt.rows, a.bt.batch, item, a.group, M, 1);
   const TreeSequence s = tree_sequence<M>(a, b);
-  const int j = item - item_first(a.bt.starts, a.bt.rows, b, a.group, M, 1), col_tiles = s.w.units / H, pair = j * M + col;
-  if (j < 0 || j >= col_tiles || pair >= s.n * a.group) return;
+  const int j = item - item_first(a.bt.starts, a.bt.rows, b, a.group, M, 1), col_tiles = s.w.units / H, first = j * M, pairs = s.n * a.group;
+  if (j < 0 || first + col >= pairs) return;
   const auto weight_of = [&](int i) { return tree_sequence<M>(a, i).w; };
-  const long quota = line_quota(a.line, line_total(a.bt.batch, weight_of));
-  const Pieces p = pieces_of(line_before(b, weight_of) + ((long)h * col_tiles + j) * s.w.tiles, s.w.tiles, quota);
+  const LineSums sums = line_sums(a.bt.batch, b, weight_of);
+  const Pieces p = pieces_of(sums.before + ((long)h * col_tiles + j) * s.w.tiles, s.w.tiles, line_quota(a.line, sums.total));
   if (p.first == p.last) return;
-  join_column<T, D>((int)(p.last - p.first) + 1, [&](int i) { return slot_of(p, p.first + i); }, a.o, a.ml, M, col,
-                    a.out.data + (long)(s.row0 + pair / a.group) * a.out.token_stride + (long)(h * a.group + pair % a.group) * a.out.head_stride);
+  join_columns<T, D>((int)(p.last - p.first) + 1, [&](int i) { return slot_of(p, p.first + i); }, a.o, a.ml, M, col, min(pairs - first, M), [&](int c) {
+    const int pair = first + c;
+    return a.out.data + (long)(s.row0 + pair / a.group) * a.out.token_stride + (long)(h * a.group + pair % a.group) * a.out.head_stride;
+  });
 }
 
 struct TreePlan {
@@ -448,7 +452,7 @@ static void launch_tree(const TreeArgs& a, const TreePlan& p, hipStream_t st) {
   const dim3 grid((unsigned)p.workgroups);
   if (a.c.codes == DQ_CODES_E4M3) hipLaunchKernelGGL((tree_attn_kernel<T, D, true, CB>), grid, dim3(256), 0, st, a);
   else hipLaunchKernelGGL((tree_attn_kernel<T, D, false, CB>), grid, dim3(256), 0, st, a);
-  hipLaunchKernelGGL((tree_join_kernel<T, D, CB>), dim3((unsigned)(p.items * a.c.kv_heads * 32 * CB)), dim3(256), 0, st, a);
+  hipLaunchKernelGGL((tree_join_kernel<T, D, CB>), dim3((unsigned)(p.items * a.c.kv_heads * (32 * CB / kJoinColumns))), dim3(256), 0, st, a);
 }
 template <typename T, int D>
 static void launch_tree_cols(const TreeArgs& a, const TreePlan& p, hipStream_t st) {
