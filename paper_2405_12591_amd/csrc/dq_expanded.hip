@@ -130,7 +130,7 @@ __global__ __launch_bounds__(256, 2) void expanded_attn_kernel(ExpandedArgs a) {
       }
       asm volatile("s_waitcnt lgkmcnt(0)" ::: "memory");
     }
-    __builtin_amdgcn_s_barrier();
+    copies_done<0>();
     if (t + 1 < t_last) load_tile(t + 1);
     const LdsBytes k_from = (LdsBytes)s_k[t & 1], r_from = (LdsBytes)s_r[t & 1], v_from = (LdsBytes)s_v[t & 1];
     f32x16 u[2];

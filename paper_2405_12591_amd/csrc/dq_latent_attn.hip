@@ -32,6 +32,13 @@ struct LatentShape {
   static constexpr int PER_SIMD = R == 512 ? 1 : 2;       // waves
 };
 
+// The first n of 32 tokens, as bits; 32 tokens' bits from place `at` on (there are 64, from 0).
+__device__ __forceinline__ uint32_t low_bits(int n) { return n <= 0 ? 0u : n >= 32 ? ~0u : (1u << n) - 1; }
+__device__ __forceinline__ uint32_t bits_from(uint64_t bits, int at) {
+  const uint64_t w = at >= 0 ? bits >> (at & 63) : bits << (-at & 63);
+  return at > -32 && at < 64 ? (uint32_t)w : 0u;
+}
+
 // A workgroup of four waves takes 32 CB (row, head) columns over its tiles of 32 tokens, which are copied to LDS past the registers and
 // are keys and values both.  Every wave forms the transposed scores of its 32 columns, S^T = [c | k_rot] q^T, with the key rows in
 // the order that leaves a lane the probabilities of 8 neighbouring tokens twice, the right operand of O^T += c^T P^T; the left
@@ -136,74 +143,120 @@ __global__ __launch_bounds__(256, (LatentShape<T, R, CB>::PER_SIMD)) void latent
       if (ROT == 64 || lane < 32) copy_to_lds(source(rot_token, rot_slot ^ rot_swap_of(8 * wave + rot_token), true), rot_to);
     };
 
-    load_pages(t0);
-    __syncthreads();                                      // buffers have been read
+    // ---- tile by tile: the scores of the next one while this one's probabilities are formed ----
+    constexpr int KS = NK + NR, AHEAD = Shape::PER_SIMD == 1 ? 8 : 4, V_AHEAD = AHEAD / 2;     // LDS reads on their way ahead of the products that take them
+    tx8 kf[AHEAD];
+    auto key = [&](int t, int k) __attribute__((always_inline)) {
+      if (k < NK) return __builtin_bit_cast(tx8, *(LdsPieces)((LdsBytes)s_c[t % NB] + (k_at ^ 32 * (k % 8)) + 256 * (k / 8)));
+      return __builtin_bit_cast(tx8, *(LdsPieces)((LdsBytes)s_r[t % NB] + (rot_at ^ 32 * (k - NK))));
+    };
+    auto first_keys = [&](int t) __attribute__((always_inline)) {
 #pragma unroll
-    for (int i = 0; i < NB - 1; ++i)
-      if (t0 + i < t_end) load_tile(t0 + i);
-    for (int t = t0; t < t_end; ++t) {
-      if (t + NB - 2 < t_end) asm volatile("s_waitcnt vmcnt(%0)" ::"i"((NB - 2) * LOADS) : "memory");
-      else asm volatile("s_waitcnt vmcnt(0)" ::: "memory");
-      __builtin_amdgcn_s_barrier();
-      if (t + NB - 1 < t_end) load_tile(t + NB - 1);
-      const LdsBytes c_from = (LdsBytes)s_c[t % NB], r_from = (LdsBytes)s_r[t % NB];
-
-      f32x16 u;
+      for (int k = 0; k < AHEAD; ++k) kf[k] = key(t, k);
+    };
+    // between(k) is done after product k; values' reads begin behind the last key's.
+    auto scores = [&](int t, f32x16& u, auto between) __attribute__((always_inline)) {
 #pragma unroll
       for (int e = 0; e < 16; ++e) u[e] = 0.f;
 #pragma unroll
-      for (int k = 0; k < NK; ++k) {
-        const tx8 kf = __builtin_bit_cast(tx8, *(LdsPieces)(c_from + (k_at ^ 32 * (k % 8)) + 256 * (k / 8)));
-        u = mma32(kf, q[k], u);
-        if (k % 8 == 7) __builtin_amdgcn_sched_barrier(0);   // (reads of all steps ahead of the first product would take 144 registers)
+      for (int k = 0; k < KS; ++k) {
+        u = mma32(kf[k % AHEAD], q[k], u);
+        if (k + AHEAD < KS) kf[k % AHEAD] = key(t, k + AHEAD);
+        between(k);
+        __builtin_amdgcn_sched_barrier(0);
       }
-#pragma unroll
-      for (int k = 0; k < NR; ++k) {
-        const tx8 kf = __builtin_bit_cast(tx8, *(LdsPieces)(r_from + (rot_at ^ 32 * k)));
-        u = mma32(kf, q[NK + k], u);
+    };
+    tx8 vf[V_AHEAD];
+    auto value = [&](int t, int i) __attribute__((always_inline)) {   // (NCT is a multiple of 4, or all of a wave's channel tiles share c / 4's)
+      const int c = chs * NCT + i / 2;
+      const LdsBytes from = (LdsBytes)s_c[t % NB] + 16 * (i & 1) * R * 2 + 256 * (c / 4);
+      return turned_rows<tx8>(from + (v_at0 ^ 64 * (c % 4)), from + (v_at1 ^ 64 * (c % 4)));
+    };
+
+    load_pages(t0);
+    __syncthreads();                                      // buffers have been read
+    f32x16 u, next;
+    if (t0 < t_end) {
+      load_tile(t0);
+      if (t0 + 1 < t_end) load_tile(t0 + 1);
+      if (t0 + 2 < t_end) {
+        load_tile(t0 + 2);
+        copies_done<2 * LOADS>();
+      } else {
+        copies_done<0>();
       }
+      first_keys(t0);
+      scores(t0, u, [](int) {});
+    }
+    // Tile t's scores are in u: those that a column does not see hidden, the lane's largest.
+    auto largest = [&](int t) __attribute__((always_inline)) {
       if (t * TT + TT > all_hi) {
-        asm volatile("" ::: "memory");                    // (a branch: as selects they would be part of every tile)
+        int from = t * TT + 8 * hl;
+        asm volatile("" : "+v"(from)::"memory");          // (a branch, and nothing of it ahead of the loop)
+        const uint32_t seen = low_bits(see_hi - from) | (bits_from(bits, from - before) & low_bits(len - from));
 #pragma unroll
-        for (int e = 0; e < 16; ++e) {
-          const int token = t * TT + 16 * (e >> 3) + 8 * hl + (e & 7), own = token - before;
-          const bool sees = token < see_hi || (token < len && own >= 0 && own < 64 && (bits >> (own & 63) & 1));
-          u[e] = sees ? u[e] : -INFINITY;
-        }
+        for (int e = 0; e < 16; ++e) u[e] = seen >> (16 * (e >> 3) + (e & 7)) & 1 ? u[e] : -INFINITY;
       }
       float top = u[0];
 #pragma unroll
       for (int e = 1; e < 16; ++e) top = fmaxf(top, u[e]);
-      top *= a.scale_log2;
-      if (__any(top > m + kLazy)) {
-        top = fmaxf(top, __shfl_xor(top, 32));
-        const float m_new = fmaxf(m, top);
-        const float alpha = m_new == -INFINITY ? 1.f : __builtin_amdgcn_exp2f(m - m_new);
-        m = m_new;
-        l *= alpha;
+      return top * a.scale_log2;
+    };
+    // The next tile is there, and all are done with the last one.
+    auto advance = [&](int t) __attribute__((always_inline)) {
+      if (t + 1 >= t_end) return;
+      if (t + 2 < t_end) copies_done<LOADS>();
+      else copies_done<0>();
+      if (t + 3 < t_end) load_tile(t + 3);
+      first_keys(t + 1);
+    };
+    float top = -INFINITY;
+    if (t0 < t_end) {
+      advance(t0);
+      top = largest(t0);
+    }
+    for (int t = t0; t < t_end;) {
+      // The sums are rescaled outside the loop over tiles (inside it they moved between register files with every tile).
+      top = fmaxf(top, __shfl_xor(top, 32));
+      const float m_new = fmaxf(m, top), alpha = m_new == -INFINITY ? 1.f : __builtin_amdgcn_exp2f(m - m_new);
+      m = m_new;
+      l *= alpha;
 #pragma unroll
-        for (int ct = 0; ct < NCT; ++ct) o[ct] *= alpha;
-      }
-      const float base = m == -INFINITY ? 0.f : -m;
-      // probabilities in the rows' type, which their product with c needs (the sum keeps fp32)
-      tx8 p[2];
-      float sum = 0.f;
+      for (int ct = 0; ct < NCT; ++ct) o[ct] *= alpha;
+      do {
+        // probabilities in the rows' type, which their product with c needs (the sum keeps fp32)
+        float base = m == -INFINITY ? 0.f : -m;
+        tx8 p[2];
+        float sum = 0.f;
+        auto probability = [&](int e) __attribute__((always_inline)) {
+          const float x = __builtin_amdgcn_exp2f(__builtin_fmaf(u[e], a.scale_log2, base));
+          sum += x;
+          p[e >> 3][e & 7] = to_element<tx8>(x);
+        };
+        if (t + 1 < t_end) {
+          asm volatile("" : "+v"(base));                  // (else both branches' probabilities are formed ahead of the branch)
+          scores(t + 1, next, [&](int k) __attribute__((always_inline)) {
+            if (k < 16) probability(k);
+            if (k >= KS - V_AHEAD) vf[k - (KS - V_AHEAD)] = value(t, k - (KS - V_AHEAD));
+          });
+        } else {
 #pragma unroll
-      for (int e = 0; e < 16; ++e) {
-        const float x = __builtin_amdgcn_exp2f(__builtin_fmaf(u[e], a.scale_log2, base));
-        sum += x;
-        p[e >> 3][e & 7] = to_element<tx8>(x);
-      }
-      l += sum;
+          for (int i = 0; i < V_AHEAD; ++i) vf[i] = value(t, i);
 #pragma unroll
-      for (int ct = 0; ct < NCT; ++ct) {
-        const int c = chs * NCT + ct;                     // (NCT is a multiple of 4, or all of a wave's channel tiles share c / 4's)
-#pragma unroll
-        for (int ks = 0; ks < 2; ++ks) {
-          const LdsBytes from = c_from + 16 * ks * R * 2 + 256 * (c / 4);
-          o[ct] = mma32(turned_rows<tx8>(from + (v_at0 ^ 64 * (c % 4)), from + (v_at1 ^ 64 * (c % 4))), p[ks], o[ct]);
+          for (int e = 0; e < 16; ++e) probability(e);
         }
-      }
+        l += sum;
+#pragma unroll
+        for (int i = 0; i < 2 * NCT; ++i) {
+          o[i / 2] = mma32(vf[i % V_AHEAD], p[i & 1], o[i / 2]);
+          if (i + V_AHEAD < 2 * NCT) vf[i % V_AHEAD] = value(t, i + V_AHEAD);
+          __builtin_amdgcn_sched_barrier(0);
+        }
+        u = next;
+        if (++t >= t_end) break;
+        advance(t);
+        top = largest(t);
+      } while (!__any(top > m + kLazy));
     }
 
     // ---- the result, or a piece of it ----
