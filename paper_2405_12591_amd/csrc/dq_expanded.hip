@@ -110,7 +110,7 @@ __global__ __launch_bounds__(256, 2) void expanded_attn_kernel(ExpandedArgs a) {
   float m = -INFINITY, l = 0.f;
   if (t_first < t_last) load_tile(t_first);
   for (int t = t_first; t < t_last; ++t) {
-    asm volatile("s_waitcnt vmcnt(0)" ::: "memory");
+    wait_copies<0>();
     const bool masked = t * TT + TT > all_hi;
     if (masked) {
       // A value that is not finite must not reach rows that do not see it (0 * inf): in tiles with a mask its token becomes one of zero
@@ -130,7 +130,7 @@ __global__ __launch_bounds__(256, 2) void expanded_attn_kernel(ExpandedArgs a) {
       }
       asm volatile("s_waitcnt lgkmcnt(0)" ::: "memory");
     }
-    copies_done<0>();
+    barrier();
     if (t + 1 < t_last) load_tile(t + 1);
     const LdsBytes k_from = (LdsBytes)s_k[t & 1], r_from = (LdsBytes)s_r[t & 1], v_from = (LdsBytes)s_v[t & 1];
     f32x16 u[2];

@@ -33,9 +33,10 @@ __device__ __forceinline__ void copy_to_lds(const uint16_t* base, uint32_t offse
 __device__ __forceinline__ void copy_to_lds(const uint16_t* from, uint32_t lds) {
   asm volatile("s_mov_b32 m0, %0\n\ts_nop 0\n\tglobal_load_lds_dwordx4 %1, off" ::"s"(__builtin_amdgcn_readfirstlane(lds)), "v"(from) : "memory");
 }
-// Waits for all of the wave's copies but the newest N, then for the workgroup's other waves; as one instruction sequence that no LDS read
-// passes (the compiler moves reads across the barrier builtin).
-template <int N> __device__ __forceinline__ void copies_done() { asm volatile("s_waitcnt vmcnt(%0)\n\ts_barrier" ::"i"(N) : "memory"); }
+// Waits for all of the wave's copies but the newest N; for the workgroup's other waves.  As instructions that no LDS read passes (the
+// compiler moves reads across the barrier builtin).
+template <int N> __device__ __forceinline__ void wait_copies() { asm volatile("s_waitcnt vmcnt(%0)" ::"i"(N) : "memory"); }
+__device__ __forceinline__ void barrier() { asm volatile("s_barrier" ::: "memory"); }
 __device__ __forceinline__ uint32_t lds_of(const void* p) { return (uint32_t)(uintptr_t)(LdsBytes)p; }
 
 // Eight 16-bit values: the left operand of a product with rows as they lie (token by token) as channels.  Of each 16 lanes, four read

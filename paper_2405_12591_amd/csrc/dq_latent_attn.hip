@@ -26,10 +26,9 @@ __device__ __forceinline__ Weight latent_weight(const LatentArgs& a, int b) {
 template <typename T, int R, int CB>
 struct LatentShape {
   static constexpr int ROT = R == 512 ? 64 : 32, W = R + ROT;
-  static constexpr int CH = 4 / CB;                       // waves that share a block of 32 columns, each with a part of the channels
-  static constexpr int M = 32 * CB;
-  static constexpr int BUFFERS = 4;
-  static constexpr int PER_SIMD = R == 512 ? 1 : 2;       // waves
+  static constexpr int CH = CB == 4 ? 2 : 4;              // waves that share a block of 32 columns, each with a part of the channels
+  static constexpr int WAVES = CB * CH, M = 32 * CB;
+  static constexpr int BUFFERS = 3;
 };
 
 // The first n of 32 tokens, as bits; 32 tokens' bits from place `at` on (there are 64, from 0).
@@ -39,20 +38,23 @@ __device__ __forceinline__ uint32_t bits_from(uint64_t bits, int at) {
   return at > -32 && at < 64 ? (uint32_t)w : 0u;
 }
 
-// A workgroup of four waves takes 32 CB (row, head) columns over its tiles of 32 tokens, which are copied to LDS past the registers and
-// are keys and values both.  Every wave forms the transposed scores of its 32 columns, S^T = [c | k_rot] q^T, with the key rows in
-// the order that leaves a lane the probabilities of 8 neighbouring tokens twice, the right operand of O^T += c^T P^T; the left
-// one comes from the same rows by transposing LDS reads.
+// A workgroup takes 32 CB (row, head) columns over its tiles of 32 tokens, which are copied to LDS past the registers and are keys and values
+// both.  CH waves share a block of 32 columns: each multiplies its part of the channels, S^T = [c | k_rot] q^T, hands its sums to the
+// others through LDS, and then holds its part of O^T += c^T P^T, whose left operand comes from the same rows by transposing reads.  (So a
+// wave's queries and results fit 256 registers and two waves a SIMD hide each other's latencies: with all channels' queries in one wave,
+// alone on its SIMD, 16 sequences of 14 thousand tokens with 128 heads took 178 us.)  Key rows are taken in the order that leaves a lane
+// the probabilities of 8 neighbouring tokens twice, the right operand of the second product.
 template <typename T, int R, int CB>
-__global__ __launch_bounds__(256, (LatentShape<T, R, CB>::PER_SIMD)) void latent_attn_kernel(LatentArgs a) {
+__global__ __launch_bounds__((64 * LatentShape<T, R, CB>::WAVES), (LatentShape<T, R, CB>::WAVES / 4)) void latent_attn_kernel(LatentArgs a) {
   typedef LatentShape<T, R, CB> Shape;
-  constexpr int ROT = Shape::ROT, W = Shape::W, CH = Shape::CH, M = Shape::M, NB = Shape::BUFFERS;
-  constexpr int TT = kLatentTile, NK = R / 16, NR = ROT / 16, NCT = R / 32 / CH;
-  constexpr int LOADS = 8 * R * 2 / 1024 + 1;             // of a wave and tile
+  constexpr int ROT = Shape::ROT, W = Shape::W, CH = Shape::CH, M = Shape::M, NB = Shape::BUFFERS, WAVES = Shape::WAVES;
+  constexpr int TT = kLatentTile, NK = R / 16 / CH, NR = ROT / 16 >= CH ? ROT / 16 / CH : 1, NCT = R / 32 / CH;   // a wave's steps and channel tiles
+  constexpr int ROWS = TT / WAVES, LOADS = ROWS * R * 2 / 1024 + 1;   // rows that a wave copies of a tile, and its copies
   typedef typename Vec8<T>::type tx8;
   __shared__ __align__(1024) char s_c[NB][TT * R * 2], s_r[NB][TT * ROT * 2];
+  __shared__ __align__(16) f32x4 s_sums[WAVES][4][64];
   const int tid = threadIdx.x, lane = tid & 63, wave = __builtin_amdgcn_readfirstlane(tid >> 6), r32 = lane & 31, hl = lane >> 5;
-  const int cb = wave % CB, chs = wave / CB, H = a.q.heads, P = a.c.page_tokens;
+  const int cb = wave / CH, chs = wave % CH, H = a.q.heads, P = a.c.page_tokens;
   const auto weight_of = [&](int b) { return latent_weight<M>(a, b); };
   const long total = line_total(a.bt.batch, weight_of), quota = line_quota(a.line, total);
   long at = (long)blockIdx.x * quota;
@@ -88,7 +90,10 @@ __global__ __launch_bounds__(256, (LatentShape<T, R, CB>::PER_SIMD)) void latent
     const uint16_t* const q_row = a.q.data + (long)(s.row0 + my_row) * a.q.token_stride + (long)(my_pair % H) * a.q.head_stride + 8 * hl;
     tx8 q[NK + NR];
 #pragma unroll
-    for (int k = 0; k < NK + NR; ++k) q[k] = __builtin_bit_cast(tx8, *reinterpret_cast<const u32x4*>(q_row + 16 * k));
+    for (int k = 0; k < NK; ++k) q[k] = __builtin_bit_cast(tx8, *reinterpret_cast<const u32x4*>(q_row + 16 * (chs * NK + k)));
+    const bool turns = ROT / 16 >= CH || chs < ROT / 16;    // (four waves, two steps of shared channels)
+#pragma unroll
+    for (int k = 0; k < NR; ++k) q[NK + k] = __builtin_bit_cast(tx8, turns ? *reinterpret_cast<const u32x4*>(q_row + R + 16 * (chs * NR + k)) : u32x4{0, 0, 0, 0});
     const int place = before + my_row;
     uint64_t bits = 0;                                    // of the sequence's own rows
     int see_hi = a.causal ? min(place + 1, len) : len, all_hi = a.causal ? min(before + rows_lo + 1, len) : len;
@@ -115,81 +120,109 @@ __global__ __launch_bounds__(256, (LatentShape<T, R, CB>::PER_SIMD)) void latent
       const int page = t < tiles && (long)t * TT < len ? a.bt.page_table[(long)b * a.bt.table_stride + t * TT / P] : -1;
       pages = page >= 0 && page < a.c.pages ? page : -1;
     };
-    auto load_tile = [&](int t) __attribute__((always_inline)) {
+    // Tile t's copies: begin_tile(t), then copy(i) for every i < LOADS.  A tile lies in one page, whose rows are all there to be copied; what
+    // is not to be seen of it, or of a page that does not exist, is replaced in LDS (mend_tile).  Copy i has rows EACH (wave + WAVES i) and on.
+    constexpr int EACH = 1024 / (R * 2);
+    const uint16_t* copy_from = nullptr;
+    uint32_t copy_to = 0, copy_rot_to = 0, missing = 0;   // missing: bit t % NB
+    auto begin_tile = [&](int t) __attribute__((always_inline)) {
       if (t - pages_from >= 64) load_pages(t);
-      const int page = __builtin_amdgcn_readlane(pages, t - pages_from), left = len - t * TT;
-      const uint16_t* const from = a.c.rows + ((long)max(page, 0) * P + t * TT % P) * W + 8 * wave * W;
-      const uint32_t to = lds_of(s_c[t % NB]) + 8 * wave * R * 2, rot_to = lds_of(s_r[t % NB]) + 8 * wave * ROT * 2;
-      constexpr int STEP = 1024 / (R * 2);                // rows of one copy
-      const int slot = R == 512 ? lane : lane & 31, ahead = R == 512 ? 0 : lane >> 5;
-      const int rot_token = lane / (ROT / 8), rot_slot = lane % (ROT / 8);
-      if (page >= 0 && left >= TT) {
+      const int page = __builtin_amdgcn_readlane(pages, t - pages_from);
+      missing = (missing & ~(1u << t % NB)) | (page < 0 ? 1u << t % NB : 0u);
+      copy_from = a.c.rows + ((long)max(page, 0) * P + t * TT % P) * W;
+      copy_to = lds_of(s_c[t % NB]) + 1024 * wave;
+      copy_rot_to = lds_of(s_r[t % NB]) + ROWS * wave * ROT * 2;
+    };
+    const int copy_row = R == 512 ? 0 : lane >> 5, rot_row = lane / (ROT / 8);
+    const uint32_t copy_piece = ((R == 512 ? lane : lane & 31) ^ swap_of(EACH * wave + copy_row)) << 4;
+    const uint32_t rot_offset = rot_row * W * 2 + ((lane % (ROT / 8) ^ rot_swap_of(ROWS * wave + rot_row)) << 4);
+    auto copy = [&](int i) __attribute__((always_inline)) {
+      if (i < LOADS - 1) copy_to_lds(copy_from + EACH * (wave + WAVES * i) * W, copy_row * W * 2 + (copy_piece ^ swap_of(WAVES * EACH * i) << 4), copy_to + 1024 * WAVES * i);
+      else if (rot_row < ROWS) copy_to_lds(copy_from + ROWS * wave * W + R, rot_offset, copy_rot_to);
+    };
+    auto load_tile = [&](int t) __attribute__((always_inline)) {
+      begin_tile(t);
 #pragma unroll
-        for (int i = 0; i < LOADS - 1; ++i)
-          copy_to_lds(from + i * STEP * W, ahead * W * 2 + ((slot ^ swap_of(8 * wave + i * STEP + ahead)) << 4), to + 1024 * i);
-        if (ROT == 64 || lane < 32)
-          copy_to_lds(from + R, rot_token * W * 2 + ((rot_slot ^ rot_swap_of(8 * wave + rot_token)) << 4), rot_to);
-        return;
-      }
-      auto source = [&](int token, int piece, bool rot) __attribute__((always_inline)) {
-        const bool there = 8 * wave + token < left;
-        return there && page >= 0 ? from + token * W + (rot ? R : 0) + 8 * piece : reinterpret_cast<const uint16_t*>(&g_blank[rot && there ? 1 : 0]);
-      };
-#pragma unroll
-      for (int i = 0; i < LOADS - 1; ++i) {
-        const int token = i * STEP + ahead;
-        copy_to_lds(source(token, slot ^ swap_of(8 * wave + token), false), to + 1024 * i);
-      }
-      if (ROT == 64 || lane < 32) copy_to_lds(source(rot_token, rot_slot ^ rot_swap_of(8 * wave + rot_token), true), rot_to);
+      for (int i = 0; i < LOADS; ++i) copy(i);
+    };
+    // Behind the wave's copies of tile t, ahead of the barrier: values behind the last token become zeros (0 * NaN is not 0), a page that does not
+    // exist rows of zeros with keys of NaN.
+    auto mend_tile = [&](int t) __attribute__((always_inline)) {
+      const int left = missing >> t % NB & 1 ? 0 : len - t * TT;
+      if (left >= TT) return;
+#pragma unroll 1
+      for (int i = 0; i < LOADS - 1; ++i)
+        if (EACH * (wave + WAVES * i) + copy_row >= left) *reinterpret_cast<u32x4*>(s_c[t % NB] + 1024 * (wave + WAVES * i) + 16 * lane) = u32x4{0, 0, 0, 0};
+      if ((missing >> t % NB & 1) && rot_row < ROWS) *reinterpret_cast<u32x4*>(s_r[t % NB] + ROWS * wave * ROT * 2 + 16 * lane) = g_blank[1];
+      asm volatile("s_waitcnt lgkmcnt(0)" ::: "memory");
     };
 
-    // ---- tile by tile: the scores of the next one while this one's probabilities are formed ----
-    constexpr int KS = NK + NR, AHEAD = Shape::PER_SIMD == 1 ? 8 : 4, V_AHEAD = AHEAD / 2;     // LDS reads on their way ahead of the products that take them
-    tx8 kf[AHEAD];
+    // ---- tile by tile ----
+    constexpr int KS = NK + NR, AHEAD = 4, V_AHEAD = 2;     // LDS reads on their way ahead of the products that take them
+    int k_here = k_at, rot_here = rot_at, v0_here = v_at0, v1_here = v_at1;
     auto key = [&](int t, int k) __attribute__((always_inline)) {
-      if (k < NK) return __builtin_bit_cast(tx8, *(LdsPieces)((LdsBytes)s_c[t % NB] + (k_at ^ 32 * (k % 8)) + 256 * (k / 8)));
-      return __builtin_bit_cast(tx8, *(LdsPieces)((LdsBytes)s_r[t % NB] + (rot_at ^ 32 * (k - NK))));
+      if (k < NK) {
+        const int step = chs * NK + k;
+        return __builtin_bit_cast(tx8, *(LdsPieces)((LdsBytes)s_c[t % NB] + (k_here ^ 32 * (step % 8)) + 256 * (step / 8)));
+      }
+      return __builtin_bit_cast(tx8, *(LdsPieces)((LdsBytes)s_r[t % NB] + (rot_here ^ 32 * (turns ? chs * NR + k - NK : 0))));
     };
-    auto first_keys = [&](int t) __attribute__((always_inline)) {
-#pragma unroll
-      for (int k = 0; k < AHEAD; ++k) kf[k] = key(t, k);
+    auto value = [&](int t, int i) __attribute__((always_inline)) {
+      const int c = chs * NCT + i % NCT;
+      const LdsBytes from = (LdsBytes)s_c[t % NB] + 16 * (i / NCT) * R * 2 + 256 * (c / 4);
+      return turned_rows<tx8>(from + (v0_here ^ 64 * (c % 4)), from + (v1_here ^ 64 * (c % 4)));
     };
-    // between(k) is done after product k; values' reads begin behind the last key's.
-    auto scores = [&](int t, f32x16& u, auto between) __attribute__((always_inline)) {
+    load_pages(t0);
+    __syncthreads();                                      // buffers have been read
+    if (t0 < t_end) {
+      load_tile(t0);
+      if (t0 + 1 < t_end) {
+        load_tile(t0 + 1);
+        wait_copies<LOADS>();
+      } else {
+        wait_copies<0>();
+      }
+      mend_tile(t0);
+      barrier();
+    }
+    for (int t = t0; t < t_end; ++t) {
+      asm volatile("" : "+v"(k_here), "+v"(rot_here), "+v"(v0_here), "+v"(v1_here));   // (else 18 places formed from them are held)
+      f32x16 u;
 #pragma unroll
       for (int e = 0; e < 16; ++e) u[e] = 0.f;
+      tx8 kf[AHEAD];
+#pragma unroll
+      for (int k = 0; k < AHEAD; ++k) kf[k] = key(t, k);
 #pragma unroll
       for (int k = 0; k < KS; ++k) {
         u = mma32(kf[k % AHEAD], q[k], u);
         if (k + AHEAD < KS) kf[k % AHEAD] = key(t, k + AHEAD);
-        between(k);
         __builtin_amdgcn_sched_barrier(0);
       }
-    };
-    tx8 vf[V_AHEAD];
-    auto value = [&](int t, int i) __attribute__((always_inline)) {   // (NCT is a multiple of 4, or all of a wave's channel tiles share c / 4's)
-      const int c = chs * NCT + i / 2;
-      const LdsBytes from = (LdsBytes)s_c[t % NB] + 16 * (i & 1) * R * 2 + 256 * (c / 4);
-      return turned_rows<tx8>(from + (v_at0 ^ 64 * (c % 4)), from + (v_at1 ^ 64 * (c % 4)));
-    };
-
-    load_pages(t0);
-    __syncthreads();                                      // buffers have been read
-    f32x16 u, next;
-    if (t0 < t_end) {
-      load_tile(t0);
-      if (t0 + 1 < t_end) load_tile(t0 + 1);
-      if (t0 + 2 < t_end) {
-        load_tile(t0 + 2);
-        copies_done<2 * LOADS>();
-      } else {
-        copies_done<0>();
+      barrier();                                          // the last tile's sums have been read
+#pragma unroll
+      for (int i = 0; i < 4; ++i) s_sums[wave][i][lane] = f32x4{u[4 * i], u[4 * i + 1], u[4 * i + 2], u[4 * i + 3]};
+      wait_copies<0>();
+      if (t + 1 < t_end) mend_tile(t + 1);
+      asm volatile("s_waitcnt lgkmcnt(0)" ::: "memory");
+      barrier();                                          // sums and the next tile are there, and all are done with the last one
+      if (t + 2 < t_end) load_tile(t + 2);
+      // in an order that gives all of them the same bits: the waves must agree on maxima
+      auto others = [&](int w, f32x16& to, bool add) __attribute__((always_inline)) {
+#pragma unroll
+        for (int i = 0; i < 4; ++i) {
+          const f32x4 x = s_sums[cb * CH + (chs ^ w)][i][lane];
+#pragma unroll
+          for (int e = 0; e < 4; ++e) to[4 * i + e] = add ? to[4 * i + e] + x[e] : x[e];
+        }
+      };
+      others(1, u, true);
+      if constexpr (CH == 4) {
+        f32x16 pair;
+        others(2, pair, false);
+        others(3, pair, true);
+        u += pair;
       }
-      first_keys(t0);
-      scores(t0, u, [](int) {});
-    }
-    // Tile t's scores are in u: those that a column does not see hidden, the lane's largest.
-    auto largest = [&](int t) __attribute__((always_inline)) {
       if (t * TT + TT > all_hi) {
         int from = t * TT + 8 * hl;
         asm volatile("" : "+v"(from)::"memory");          // (a branch, and nothing of it ahead of the loop)
@@ -200,63 +233,35 @@ __global__ __launch_bounds__(256, (LatentShape<T, R, CB>::PER_SIMD)) void latent
       float top = u[0];
 #pragma unroll
       for (int e = 1; e < 16; ++e) top = fmaxf(top, u[e]);
-      return top * a.scale_log2;
-    };
-    // The next tile is there, and all are done with the last one.
-    auto advance = [&](int t) __attribute__((always_inline)) {
-      if (t + 1 >= t_end) return;
-      if (t + 2 < t_end) copies_done<LOADS>();
-      else copies_done<0>();
-      if (t + 3 < t_end) load_tile(t + 3);
-      first_keys(t + 1);
-    };
-    float top = -INFINITY;
-    if (t0 < t_end) {
-      advance(t0);
-      top = largest(t0);
-    }
-    for (int t = t0; t < t_end;) {
-      // The sums are rescaled outside the loop over tiles (inside it they moved between register files with every tile).
-      top = fmaxf(top, __shfl_xor(top, 32));
-      const float m_new = fmaxf(m, top), alpha = m_new == -INFINITY ? 1.f : __builtin_amdgcn_exp2f(m - m_new);
-      m = m_new;
-      l *= alpha;
+      top *= a.scale_log2;
+      if (__any(top > m + kLazy)) {
+        top = fmaxf(top, __shfl_xor(top, 32));
+        const float m_new = fmaxf(m, top), alpha = m_new == -INFINITY ? 1.f : __builtin_amdgcn_exp2f(m - m_new);
+        m = m_new;
+        l *= alpha;
 #pragma unroll
-      for (int ct = 0; ct < NCT; ++ct) o[ct] *= alpha;
-      do {
-        // probabilities in the rows' type, which their product with c needs (the sum keeps fp32)
-        float base = m == -INFINITY ? 0.f : -m;
-        tx8 p[2];
-        float sum = 0.f;
-        auto probability = [&](int e) __attribute__((always_inline)) {
-          const float x = __builtin_amdgcn_exp2f(__builtin_fmaf(u[e], a.scale_log2, base));
-          sum += x;
-          p[e >> 3][e & 7] = to_element<tx8>(x);
-        };
-        if (t + 1 < t_end) {
-          asm volatile("" : "+v"(base));                  // (else both branches' probabilities are formed ahead of the branch)
-          scores(t + 1, next, [&](int k) __attribute__((always_inline)) {
-            if (k < 16) probability(k);
-            if (k >= KS - V_AHEAD) vf[k - (KS - V_AHEAD)] = value(t, k - (KS - V_AHEAD));
-          });
-        } else {
+        for (int ct = 0; ct < NCT; ++ct) o[ct] *= alpha;
+      }
+      // probabilities in the rows' type, which their product with c needs (the sum keeps fp32)
+      const float base = m == -INFINITY ? 0.f : -m;
+      tx8 p[2];
+      float sum = 0.f;
 #pragma unroll
-          for (int i = 0; i < V_AHEAD; ++i) vf[i] = value(t, i);
+      for (int e = 0; e < 16; ++e) {
+        const float x = __builtin_amdgcn_exp2f(__builtin_fmaf(u[e], a.scale_log2, base));
+        sum += x;
+        p[e >> 3][e & 7] = to_element<tx8>(x);
+      }
+      l += sum;
+      tx8 vf[V_AHEAD];
 #pragma unroll
-          for (int e = 0; e < 16; ++e) probability(e);
-        }
-        l += sum;
+      for (int i = 0; i < V_AHEAD; ++i) vf[i] = value(t, i);
 #pragma unroll
-        for (int i = 0; i < 2 * NCT; ++i) {
-          o[i / 2] = mma32(vf[i % V_AHEAD], p[i & 1], o[i / 2]);
-          if (i + V_AHEAD < 2 * NCT) vf[i % V_AHEAD] = value(t, i + V_AHEAD);
-          __builtin_amdgcn_sched_barrier(0);
-        }
-        u = next;
-        if (++t >= t_end) break;
-        advance(t);
-        top = largest(t);
-      } while (!__any(top > m + kLazy));
+      for (int i = 0; i < 2 * NCT; ++i) {
+        o[i % NCT] = mma32(vf[i % V_AHEAD], p[i / NCT], o[i % NCT]);
+        if (i + V_AHEAD < 2 * NCT) vf[i % V_AHEAD] = value(t, i + V_AHEAD);
+        __builtin_amdgcn_sched_barrier(0);
+      }
     }
 
     // ---- the result, or a piece of it ----
@@ -321,10 +326,10 @@ struct LatentPlan {
 static bool latent_plan(const dq_latent_cache* c, int batch, long rows, int heads, int max_rows, int max_seq_len, LatentPlan* p) {
   if (batch <= 0 || rows < 0 || heads <= 0 || max_rows < 0 || max_seq_len < 0 || rows * heads >= (1l << 31) - 256) return false;
   const long cols = (long)max_rows * heads;
-  p->cb = cols <= 32 ? 1 : 2;
+  p->cb = cols <= 32 ? 1 : cols <= 64 ? 2 : 4;
   p->items = rows * heads / (32 * p->cb) + batch;
   if (p->items * 32 * p->cb >= kMaxThreads / 256) return false;
-  p->workgroups = c->latent_dim == 512 ? 256 : 512;
+  p->workgroups = 256;
   return true;
 }
 static size_t latent_bytes(const dq_latent_cache* c, const LatentPlan& p) {
@@ -333,13 +338,14 @@ static size_t latent_bytes(const dq_latent_cache* c, const LatentPlan& p) {
 
 template <typename T, int R, int CB>
 static void launch_latent(const LatentArgs& a, const LatentPlan& p, hipStream_t st) {
-  hipLaunchKernelGGL((latent_attn_kernel<T, R, CB>), dim3((unsigned)p.workgroups), dim3(256), 0, st, a);
+  hipLaunchKernelGGL((latent_attn_kernel<T, R, CB>), dim3((unsigned)p.workgroups), dim3(64 * LatentShape<T, R, CB>::WAVES), 0, st, a);
   hipLaunchKernelGGL((latent_join_kernel<T, R, CB>), dim3((unsigned)(p.items * (32 * CB / kJoinColumns))), dim3(256), 0, st, a);
 }
 template <typename T, int R>
 static void launch_latent_cols(const LatentArgs& a, const LatentPlan& p, hipStream_t st) {
   if (p.cb == 1) launch_latent<T, R, 1>(a, p, st);
-  else launch_latent<T, R, 2>(a, p, st);
+  else if (p.cb == 2) launch_latent<T, R, 2>(a, p, st);
+  else launch_latent<T, R, 4>(a, p, st);
 }
 
 }  // namespace dq
@@ -350,9 +356,7 @@ extern "C" size_t dq_latent_workspace_bytes(const dq_latent_cache* cache, int32_
                                             int32_t max_seq_len) {
   LatentPlan p;
   if (!latent_cache_ok(cache) || !latent_plan(cache, batch, rows, q_heads, max_rows, max_seq_len, &p)) return 0;
-  p.cb = 2;                                               // (smaller calls with the same heads may take fewer columns, never more)
-  p.workgroups = 512;
-  return latent_bytes(cache, p);
+  return latent_bytes(cache, p);                          // (smaller calls with the same heads have no more columns)
 }
 
 extern "C" int32_t dq_latent_attention(const dq_latent_cache* cache, const dq_paged_batch* batch, const dq_heads* q, const dq_heads* out,
