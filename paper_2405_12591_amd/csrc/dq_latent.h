@@ -46,6 +46,18 @@ template <typename V> __device__ __forceinline__ V turned_rows(LdsBytes a, LdsBy
   return __builtin_bit_cast(V, both);
 }
 
+// sum + the eight values of v, in fp32, two at a time.
+__device__ __forceinline__ float add_eight(float sum, f16x8 v) {
+#pragma unroll
+  for (int i = 0; i < 8; i += 2) sum = __builtin_amdgcn_fdot2(f16x2{v[i], v[i + 1]}, f16x2{(_Float16)1.f, (_Float16)1.f}, sum, false);
+  return sum;
+}
+__device__ __forceinline__ float add_eight(float sum, bf16x8 v) {
+#pragma unroll
+  for (int i = 0; i < 8; i += 2) sum = __builtin_amdgcn_fdot2_f32_bf16(bf16x2{v[i], v[i + 1]}, bf16x2{(__bf16)1.f, (__bf16)1.f}, sum, false);
+  return sum;
+}
+
 // What a token that is not there has (zeros: nothing sees it, and 0 * NaN of what lies there would not be 0), and the key channels of
 // a page that does not exist (NaN for those who see its tokens).
 __device__ const u32x4 g_blank[2] = {{0, 0, 0, 0}, {0x7FFF7FFFu, 0x7FFF7FFFu, 0x7FFF7FFFu, 0x7FFF7FFFu}};

@@ -45,7 +45,7 @@ __device__ __forceinline__ uint32_t bits_from(uint64_t bits, int at) {
 // alone on its SIMD, 16 sequences of 14 thousand tokens with 128 heads took 178 us.)  Key rows are taken in the order that leaves a lane
 // the probabilities of 8 neighbouring tokens twice, the right operand of the second product.
 template <typename T, int R, int CB>
-__global__ __launch_bounds__((64 * LatentShape<T, R, CB>::WAVES), (LatentShape<T, R, CB>::WAVES / 4)) void latent_attn_kernel(LatentArgs a) {
+__global__ __launch_bounds__((64 * LatentShape<T, R, CB>::WAVES), 2) void latent_attn_kernel(LatentArgs a) {
   typedef LatentShape<T, R, CB> Shape;
   constexpr int ROT = Shape::ROT, W = Shape::W, CH = Shape::CH, M = Shape::M, NB = Shape::BUFFERS, WAVES = Shape::WAVES;
   constexpr int TT = kLatentTile, NK = R / 16 / CH, NR = ROT / 16 >= CH ? ROT / 16 / CH : 1, NCT = R / 32 / CH;   // a wave's steps and channel tiles
@@ -68,13 +68,22 @@ __global__ __launch_bounds__((64 * LatentShape<T, R, CB>::WAVES), (LatentShape<T
   // rows (keys), and those that read four pieces of four (values), touch all banks.
   auto swap_of = [](int token) { return (token & 3) << 2 | (token >> 2 & 3); };
   auto rot_swap_of = [](int token) { return ROT == 64 ? token >> 1 & 7 : token >> 2 & 3; };
-  const int k_token = (r32 & ~12) | (r32 & 4) << 1 | (r32 & 8) >> 1;
-  const int k_at = k_token * R * 2 + ((hl ^ swap_of(k_token)) << 4);            // ^ 32 (k % 8), + 256 (k / 8)
-  const int rot_at = k_token * ROT * 2 + ((hl ^ rot_swap_of(k_token)) << 4);    // ^ 32 k
-  const int i16 = lane & 15, side = lane >> 4 & 1;
-  const int v_token = 8 * hl + (i16 >> 2);                                       // + 4 j + 16 s
-  auto v_at = [&](int j) { return (v_token + 4 * j) * R * 2 + ((2 * side + ((i16 & 3) >> 1) ^ swap_of(v_token + 4 * j)) << 4) + (i16 & 1) * 8; };   // ^ 64 (c % 4), + 256 (c / 4)
-  const int v_at0 = v_at(0), v_at1 = v_at(1);
+  // A lane's places are formed with every tile: held over the loop they, and what comes of them, would not fit beside queries and results.
+  auto this_lane = []() __attribute__((always_inline)) {
+    int l = __builtin_amdgcn_mbcnt_hi(~0u, __builtin_amdgcn_mbcnt_lo(~0u, 0u));
+    asm volatile("" : "+v"(l));
+    return l;
+  };
+  struct KeyPlace { int c, rot; };                        // ^ 32 (k % 8), + 256 (k / 8); ^ 32 k
+  auto key_place = [&]() __attribute__((always_inline)) {
+    const int l = this_lane(), token = (l & 19) | (l & 4) << 1 | (l & 8) >> 1, half = l >> 5;
+    return KeyPlace{token * R * 2 + ((half ^ swap_of(token)) << 4), token * ROT * 2 + ((half ^ rot_swap_of(token)) << 4)};
+  };
+  struct ValuePlace { int a, b; };                        // tokens 8 half + (lane % 16) / 4, and 4 more; ^ 64 (c % 4), + 256 (c / 4)
+  auto value_place = [&]() __attribute__((always_inline)) {
+    const int l = this_lane(), token = (l >> 5 << 3) + (l >> 2 & 3), piece = (l >> 4 & 1) << 1 | (l >> 1 & 1);
+    return ValuePlace{token * R * 2 + ((piece ^ swap_of(token)) << 4) + (l & 1) * 8, (token + 4) * R * 2 + ((piece ^ swap_of(token + 4)) << 4) + (l & 1) * 8};
+  };
 
   for (; at < end;) {
     const Sequence s = sequence_of_wave(a.bt, P, b);
@@ -116,7 +125,7 @@ __global__ __launch_bounds__((64 * LatentShape<T, R, CB>::WAVES), (LatentShape<T
     int pages = 0, pages_from = t0;                       // of 64 tiles from pages_from on, one a lane
     auto load_pages = [&](int from) __attribute__((always_inline)) {
       pages_from = from;
-      const int t = from + lane;
+      const int t = from + this_lane();
       const int page = t < tiles && (long)t * TT < len ? a.bt.page_table[(long)b * a.bt.table_stride + t * TT / P] : -1;
       pages = page >= 0 && page < a.c.pages ? page : -1;
     };
@@ -133,60 +142,62 @@ __global__ __launch_bounds__((64 * LatentShape<T, R, CB>::WAVES), (LatentShape<T
       copy_to = lds_of(s_c[t % NB]) + 1024 * wave;
       copy_rot_to = lds_of(s_r[t % NB]) + ROWS * wave * ROT * 2;
     };
-    const int copy_row = R == 512 ? 0 : lane >> 5, rot_row = lane / (ROT / 8);
-    const uint32_t copy_piece = ((R == 512 ? lane : lane & 31) ^ swap_of(EACH * wave + copy_row)) << 4;
-    const uint32_t rot_offset = rot_row * W * 2 + ((lane % (ROT / 8) ^ rot_swap_of(ROWS * wave + rot_row)) << 4);
-    auto copy = [&](int i) __attribute__((always_inline)) {
-      if (i < LOADS - 1) copy_to_lds(copy_from + EACH * (wave + WAVES * i) * W, copy_row * W * 2 + (copy_piece ^ swap_of(WAVES * EACH * i) << 4), copy_to + 1024 * WAVES * i);
-      else if (rot_row < ROWS) copy_to_lds(copy_from + ROWS * wave * W + R, rot_offset, copy_rot_to);
-    };
     auto load_tile = [&](int t) __attribute__((always_inline)) {
       begin_tile(t);
+      const int l = this_lane(), row = R == 512 ? 0 : l >> 5, rot_row = l / (ROT / 8);
+      const uint32_t piece = ((R == 512 ? l : l & 31) ^ swap_of(EACH * wave + row)) << 4;
 #pragma unroll
-      for (int i = 0; i < LOADS; ++i) copy(i);
+      for (int i = 0; i < LOADS - 1; ++i)
+        copy_to_lds(copy_from + EACH * (wave + WAVES * i) * W, row * W * 2 + (piece ^ swap_of(WAVES * EACH * i) << 4), copy_to + 1024 * WAVES * i);
+      if (rot_row < ROWS)
+        copy_to_lds(copy_from + ROWS * wave * W + R, rot_row * W * 2 + ((l % (ROT / 8) ^ rot_swap_of(ROWS * wave + rot_row)) << 4), copy_rot_to);
     };
     // Behind the wave's copies of tile t, ahead of the barrier: values behind the last token become zeros (0 * NaN is not 0), a page that does not
     // exist rows of zeros with keys of NaN.
     auto mend_tile = [&](int t) __attribute__((always_inline)) {
       const int left = missing >> t % NB & 1 ? 0 : len - t * TT;
       if (left >= TT) return;
+      const int l = this_lane(), copy_row = R == 512 ? 0 : l >> 5, rot_row = l / (ROT / 8);
 #pragma unroll 1
       for (int i = 0; i < LOADS - 1; ++i)
-        if (EACH * (wave + WAVES * i) + copy_row >= left) *reinterpret_cast<u32x4*>(s_c[t % NB] + 1024 * (wave + WAVES * i) + 16 * lane) = u32x4{0, 0, 0, 0};
-      if ((missing >> t % NB & 1) && rot_row < ROWS) *reinterpret_cast<u32x4*>(s_r[t % NB] + ROWS * wave * ROT * 2 + 16 * lane) = g_blank[1];
+        if (EACH * (wave + WAVES * i) + copy_row >= left) *reinterpret_cast<u32x4*>(s_c[t % NB] + 1024 * (wave + WAVES * i) + 16 * l) = u32x4{0, 0, 0, 0};
+      if ((missing >> t % NB & 1) && rot_row < ROWS) *reinterpret_cast<u32x4*>(s_r[t % NB] + ROWS * wave * ROT * 2 + 16 * l) = g_blank[1];
       asm volatile("s_waitcnt lgkmcnt(0)" ::: "memory");
     };
 
     // ---- tile by tile ----
-    constexpr int KS = NK + NR, AHEAD = 4, V_AHEAD = 2;     // LDS reads on their way ahead of the products that take them
-    int k_here = k_at, rot_here = rot_at, v0_here = v_at0, v1_here = v_at1;
+    constexpr int KS = NK + NR, AHEAD = CB == 4 ? 4 : KS < 8 ? KS : 8, V_AHEAD = CB == 4 ? 2 : 4;   // LDS reads on their way ahead of the products that take them
+    KeyPlace kp;
+    ValuePlace vp;
     auto key = [&](int t, int k) __attribute__((always_inline)) {
       if (k < NK) {
         const int step = chs * NK + k;
-        return __builtin_bit_cast(tx8, *(LdsPieces)((LdsBytes)s_c[t % NB] + (k_here ^ 32 * (step % 8)) + 256 * (step / 8)));
+        return __builtin_bit_cast(tx8, *(LdsPieces)((LdsBytes)s_c[t % NB] + (kp.c ^ 32 * (step % 8)) + 256 * (step / 8)));
       }
-      return __builtin_bit_cast(tx8, *(LdsPieces)((LdsBytes)s_r[t % NB] + (rot_here ^ 32 * (turns ? chs * NR + k - NK : 0))));
+      return __builtin_bit_cast(tx8, *(LdsPieces)((LdsBytes)s_r[t % NB] + (kp.rot ^ 32 * (turns ? chs * NR + k - NK : 0))));
     };
     auto value = [&](int t, int i) __attribute__((always_inline)) {
       const int c = chs * NCT + i % NCT;
       const LdsBytes from = (LdsBytes)s_c[t % NB] + 16 * (i / NCT) * R * 2 + 256 * (c / 4);
-      return turned_rows<tx8>(from + (v0_here ^ 64 * (c % 4)), from + (v1_here ^ 64 * (c % 4)));
+      return turned_rows<tx8>(from + (vp.a ^ 64 * (c % 4)), from + (vp.b ^ 64 * (c % 4)));
     };
     load_pages(t0);
     __syncthreads();                                      // buffers have been read
+    // Tile t is there, and all are done with the ones before it, and with their sums.  Two tiles are on their way at all times.
+    auto arrive = [&](int t) __attribute__((always_inline)) {
+      if (t + 1 < t_end) wait_copies<LOADS>();
+      else wait_copies<0>();
+      mend_tile(t);
+      barrier();
+    };
     if (t0 < t_end) {
       load_tile(t0);
-      if (t0 + 1 < t_end) {
-        load_tile(t0 + 1);
-        wait_copies<LOADS>();
-      } else {
-        wait_copies<0>();
-      }
-      mend_tile(t0);
-      barrier();
+      if (t0 + 1 < t_end) load_tile(t0 + 1);
+      arrive(t0);
+      if (t0 + 2 < t_end) load_tile(t0 + 2);
     }
     for (int t = t0; t < t_end; ++t) {
-      asm volatile("" : "+v"(k_here), "+v"(rot_here), "+v"(v0_here), "+v"(v1_here));   // (else 18 places formed from them are held)
+      kp = key_place();
       f32x16 u;
 #pragma unroll
       for (int e = 0; e < 16; ++e) u[e] = 0.f;
@@ -199,19 +210,16 @@ __global__ __launch_bounds__((64 * LatentShape<T, R, CB>::WAVES), (LatentShape<T
         if (k + AHEAD < KS) kf[k % AHEAD] = key(t, k + AHEAD);
         __builtin_amdgcn_sched_barrier(0);
       }
-      barrier();                                          // the last tile's sums have been read
+      const int l_sums = this_lane();
 #pragma unroll
-      for (int i = 0; i < 4; ++i) s_sums[wave][i][lane] = f32x4{u[4 * i], u[4 * i + 1], u[4 * i + 2], u[4 * i + 3]};
-      wait_copies<0>();
-      if (t + 1 < t_end) mend_tile(t + 1);
+      for (int i = 0; i < 4; ++i) s_sums[wave][i][l_sums] = f32x4{u[4 * i], u[4 * i + 1], u[4 * i + 2], u[4 * i + 3]};
       asm volatile("s_waitcnt lgkmcnt(0)" ::: "memory");
-      barrier();                                          // sums and the next tile are there, and all are done with the last one
-      if (t + 2 < t_end) load_tile(t + 2);
+      barrier();
       // in an order that gives all of them the same bits: the waves must agree on maxima
       auto others = [&](int w, f32x16& to, bool add) __attribute__((always_inline)) {
 #pragma unroll
         for (int i = 0; i < 4; ++i) {
-          const f32x4 x = s_sums[cb * CH + (chs ^ w)][i][lane];
+          const f32x4 x = s_sums[cb * CH + (chs ^ w)][i][l_sums];
 #pragma unroll
           for (int e = 0; e < 4; ++e) to[4 * i + e] = add ? to[4 * i + e] + x[e] : x[e];
         }
@@ -224,8 +232,7 @@ __global__ __launch_bounds__((64 * LatentShape<T, R, CB>::WAVES), (LatentShape<T
         u += pair;
       }
       if (t * TT + TT > all_hi) {
-        int from = t * TT + 8 * hl;
-        asm volatile("" : "+v"(from)::"memory");          // (a branch, and nothing of it ahead of the loop)
+        const int from = t * TT + 8 * (this_lane() >> 5);   // (a branch, and nothing of it ahead of the loop)
         const uint32_t seen = low_bits(see_hi - from) | (bits_from(bits, from - before) & low_bits(len - from));
 #pragma unroll
         for (int e = 0; e < 16; ++e) u[e] = seen >> (16 * (e >> 3) + (e & 7)) & 1 ? u[e] : -INFINITY;
@@ -242,17 +249,13 @@ __global__ __launch_bounds__((64 * LatentShape<T, R, CB>::WAVES), (LatentShape<T
 #pragma unroll
         for (int ct = 0; ct < NCT; ++ct) o[ct] *= alpha;
       }
-      // probabilities in the rows' type, which their product with c needs (the sum keeps fp32)
+      // probabilities in the rows' type, which their product with c needs; the sum, in fp32, is of what they were rounded to
       const float base = m == -INFINITY ? 0.f : -m;
       tx8 p[2];
-      float sum = 0.f;
 #pragma unroll
-      for (int e = 0; e < 16; ++e) {
-        const float x = __builtin_amdgcn_exp2f(__builtin_fmaf(u[e], a.scale_log2, base));
-        sum += x;
-        p[e >> 3][e & 7] = to_element<tx8>(x);
-      }
-      l += sum;
+      for (int e = 0; e < 16; ++e) p[e >> 3][e & 7] = to_element<tx8>(__builtin_amdgcn_exp2f(__builtin_fmaf(u[e], a.scale_log2, base)));
+      l = add_eight(add_eight(l, p[0]), p[1]);
+      vp = value_place();
       tx8 vf[V_AHEAD];
 #pragma unroll
       for (int i = 0; i < V_AHEAD; ++i) vf[i] = value(t, i);
@@ -262,31 +265,35 @@ __global__ __launch_bounds__((64 * LatentShape<T, R, CB>::WAVES), (LatentShape<T
         if (i + V_AHEAD < 2 * NCT) vf[i % V_AHEAD] = value(t, i + V_AHEAD);
         __builtin_amdgcn_sched_barrier(0);
       }
+      if (t + 1 < t_end) {
+        arrive(t + 1);
+        if (t + 3 < t_end) load_tile(t + 3);
+      }
     }
 
-    // ---- the result, or a piece of it ----
+    // ---- the result, or a piece of it (places formed anew: held over the loop they would take registers) ----
     l += __shfl_xor(l, 32);
-    const int col = cb * 32 + r32;
-    const bool whole = t0 == 0 && t1 == tiles;
+    const int here = this_lane(), col = cb * 32 + (here & 31), half = here >> 5;
     if (first + col < pairs) {
-      if (whole) {
+      if (t0 == 0 && t1 == tiles) {
         const float inv = l == 0.f ? 0.f : 1.f / l;
-        uint16_t* const dst = a.out.data + (long)(s.row0 + my_row) * a.out.token_stride + (long)(my_pair % H) * a.out.head_stride + chs * NCT * 32;
+        const int row = (first + col) / H;
+        uint16_t* const dst = a.out.data + (long)(s.row0 + row) * a.out.token_stride + (long)(first + col - row * H) * a.out.head_stride + chs * NCT * 32 + 4 * half;
 #pragma unroll
         for (int ct = 0; ct < NCT; ++ct)
 #pragma unroll
           for (int e = 0; e < 4; ++e)
-            *reinterpret_cast<u32x2*>(dst + 32 * ct + 8 * e + 4 * hl) = u32x2{pack2<T>(o[ct][4 * e] * inv, o[ct][4 * e + 1] * inv),
-                                                                             pack2<T>(o[ct][4 * e + 2] * inv, o[ct][4 * e + 3] * inv)};
+            *reinterpret_cast<u32x2*>(dst + 32 * ct + 8 * e) = u32x2{pack2<T>(o[ct][4 * e] * inv, o[ct][4 * e + 1] * inv),
+                                                                    pack2<T>(o[ct][4 * e + 2] * inv, o[ct][4 * e + 3] * inv)};
       } else {
         const long slot = 2l * blockIdx.x + (t0 == 0);
-        float* const dst = a.o + (slot * M + col) * R + chs * NCT * 32;
+        float* const dst = a.o + (slot * M + col) * R + chs * NCT * 32 + 4 * half;
 #pragma unroll
         for (int ct = 0; ct < NCT; ++ct)
 #pragma unroll
           for (int e = 0; e < 4; ++e)
-            *reinterpret_cast<f32x4*>(dst + 32 * ct + 8 * e + 4 * hl) = f32x4{o[ct][4 * e], o[ct][4 * e + 1], o[ct][4 * e + 2], o[ct][4 * e + 3]};
-        if (hl == 0 && chs == 0) *reinterpret_cast<f32x2*>(a.ml + 2 * (slot * M + col)) = f32x2{m, l};
+            *reinterpret_cast<f32x4*>(dst + 32 * ct + 8 * e) = f32x4{o[ct][4 * e], o[ct][4 * e + 1], o[ct][4 * e + 2], o[ct][4 * e + 3]};
+        if (half == 0 && chs == 0) *reinterpret_cast<f32x2*>(a.ml + 2 * (slot * M + col)) = f32x2{m, l};
       }
     }
     at += t1 - t0;
