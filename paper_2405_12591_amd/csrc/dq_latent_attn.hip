@@ -305,9 +305,210 @@ __global__ __launch_bounds__((64 * LatentShape<T, R, CB>::WAVES), 2) void latent
   }
 }
 
-template <typename T, int R, int CB>
+// Up to 16 columns, which a wave takes with all their channels (queries 72, results 128 registers): every wave of a workgroup copies and works
+// tiles of 32 tokens by itself, nothing is shared and no wave waits for another before the end.  A wave's one tile of LDS is loaded again
+// when it has been read; three of four waves wait for memory at any time, which is what keeps it busy.  Products of 16 x 16: a lane gets the
+// scores of 8 neighbouring tokens of its column, the right operand of the second product.
+template <typename T, int R>
+__global__ __launch_bounds__(256, 1) void latent_narrow_kernel(LatentArgs a) {
+  constexpr int ROT = R == 512 ? 64 : 32, W = R + ROT, M = 16, WAVES = 4, TT = kLatentTile, NK = R / 32, NR = ROT / 32, NCT = R / 16;
+  constexpr int EACH = 1024 / (R * 2), COPIES = TT / EACH, ROT_EACH = 512 / ROT, ROT_COPIES = TT / ROT_EACH;   // rows of a copy, copies
+  typedef typename Vec8<T>::type tx8;
+  struct Tile { char c[TT * R * 2], r[TT * ROT * 2]; };
+  union Space {
+    Tile tile[WAVES];
+    float o[WAVES][M][R + 1];
+  };
+  __shared__ __align__(1024) Space s_space;
+  __shared__ float s_m[WAVES][M], s_l[WAVES][M];
+  const int tid = threadIdx.x, lane = tid & 63, wave = __builtin_amdgcn_readfirstlane(tid >> 6), col = lane & 15, G = lane >> 4;
+  const int H = a.q.heads, P = a.c.page_tokens;
+  const auto weight_of = [&](int b) { return latent_weight<M>(a, b); };
+  const long total = line_total(a.bt.batch, weight_of), quota = line_quota(a.line, total);
+  long at = (long)blockIdx.x * quota;
+  const long end = min(at + quota, total);
+  if (at >= end) return;
+  long begin;
+  int b = line_owner(a.bt.batch, at, weight_of, begin);
+
+  // Pieces of a row are exchanged by bits of the token, so that 16 lanes that read one piece of 16 rows (keys: tokens 8 i + 0..3), and 32 that
+  // read two pieces of eight (values), touch all banks.
+  auto swap_of = [](int t) { return (t & 3) << 2 | (t >> 3 & 1) << 1 | (t >> 4 & 1); };
+  auto rot_swap_of = [](int t) { return ROT == 64 ? (t >> 1 & 1) | (t >> 3 & 3) << 1 : t >> 3 & 3; };
+  const int k_token = 8 * (col >> 2) + (col & 3);         // + 4: the second product's
+  const int k_at = k_token * R * 2 + ((G ^ swap_of(k_token)) << 4), rot_at = k_token * ROT * 2 + ((G ^ rot_swap_of(k_token)) << 4);   // ^ 64 k (% 4), ^ 64 k
+  const int v_token = 8 * G + (col >> 2);                 // + 4: the second half
+  const int v_at = v_token * R * 2 + (((col & 3) >> 1 ^ swap_of(v_token)) << 4) + (col & 1) * 8;   // ^ 32 (c % 8), + 256 (c / 8)
+  char* const s_c = s_space.tile[wave].c;
+  char* const s_r = s_space.tile[wave].r;
+  const uint32_t c_to = lds_of(s_c), r_to = lds_of(s_r);
+
+  for (; at < end;) {
+    const Sequence s = sequence_of_wave(a.bt, P, b);
+    const Weight wt = weight_of(b);
+    const int n = min(s.n, a.max_rows), len = s.len, before = s.old;
+    const int unit = __builtin_amdgcn_readfirstlane((int)((at - begin) / wt.tiles)), tiles = __builtin_amdgcn_readfirstlane(wt.tiles);
+    const int t0 = __builtin_amdgcn_readfirstlane((int)(at - begin - (long)unit * tiles)), t1 = (int)min((long)tiles, t0 + (end - at));
+    const int pairs = n * H, first = unit * M;
+    const int my_pair = min(first + col, pairs - 1), my_row = my_pair / H;
+    const uint16_t* const q_row = a.q.data + (long)(s.row0 + my_row) * a.q.token_stride + (long)(my_pair % H) * a.q.head_stride + 8 * G;
+    tx8 q[NK + NR];
+#pragma unroll
+    for (int k = 0; k < NK + NR; ++k) q[k] = __builtin_bit_cast(tx8, *reinterpret_cast<const u32x4*>(q_row + 32 * k));
+    const int rows_lo = first / H;
+    uint64_t bits = 0;
+    int see_hi = a.causal ? min(before + my_row + 1, len) : len, all_hi = a.causal ? min(before + rows_lo + 1, len) : len;
+    if (a.seen) {
+      bits = a.seen[s.row0 + my_row];
+      if (s.n < 64) bits &= (1ull << s.n) - 1;
+      see_hi = all_hi = min(before, len);
+    }
+    const int t_end = min(t1, (len + TT - 1) / TT);
+    f32x4 o[NCT];
+#pragma unroll
+    for (int ct = 0; ct < NCT; ++ct) o[ct] = f32x4{0.f, 0.f, 0.f, 0.f};
+    float m = -INFINITY, l = 0.f;
+
+    int pages = -1, pages_from = t0 + wave;               // of 64 of this wave's tiles from pages_from on, one a lane
+    auto load_pages = [&](int from) __attribute__((always_inline)) {
+      pages_from = from;
+      const int t = from + lane * WAVES;
+      const int page = t < t_end ? a.bt.page_table[(long)b * a.bt.table_stride + t * TT / P] : -1;
+      pages = page >= 0 && page < a.c.pages ? page : -1;
+    };
+    int page = -1;                                        // of the tile on its way
+    auto load_tile = [&](int t) __attribute__((always_inline)) {
+      if (t - pages_from >= 64 * WAVES) load_pages(t);
+      page = __builtin_amdgcn_readlane(pages, (t - pages_from) / WAVES);
+      const uint16_t* const from = a.c.rows + ((long)max(page, 0) * P + t * TT % P) * W;
+      int here = lane;
+      asm volatile("" : "+v"(here));                      // (else the copies' offsets are held over the loop)
+      const int row = here / (64 / EACH), slot = here % (64 / EACH), rot_row = here / (ROT / 8), rot_slot = here % (ROT / 8);
+#pragma unroll
+      for (int i = 0; i < COPIES; ++i) copy_to_lds<true>(from + i * EACH * W, row * W * 2 + ((slot ^ swap_of(i * EACH + row)) << 4), c_to + 1024 * i);
+#pragma unroll
+      for (int i = 0; i < ROT_COPIES; ++i)
+        copy_to_lds<true>(from + i * ROT_EACH * W + R, rot_row * W * 2 + ((rot_slot ^ rot_swap_of(i * ROT_EACH + rot_row)) << 4), r_to + 1024 * i);
+    };
+
+    load_pages(t0 + wave);
+    __syncthreads();                                      // the last unit's results have been read
+    if (t0 + wave < t_end) load_tile(t0 + wave);
+    for (int t = t0 + wave; t < t_end; t += WAVES) {
+      wait_copies<0>();
+      const int left = page < 0 ? 0 : len - t * TT;
+      if (left < TT) {                                    // zeros behind the last token, keys of NaN on a page that does not exist
+        for (int i = 0; i < COPIES; ++i)
+          if (i * EACH + lane / (64 / EACH) >= left) *reinterpret_cast<u32x4*>(s_c + 1024 * i + 16 * lane) = u32x4{0, 0, 0, 0};
+        if (page < 0)
+          for (int i = 0; i < ROT_COPIES; ++i) *reinterpret_cast<u32x4*>(s_r + 1024 * i + 16 * lane) = g_blank[1];
+      }
+      f32x4 u[2];
+      u[0] = u[1] = f32x4{0.f, 0.f, 0.f, 0.f};
+      constexpr int KS = 2 * (NK + NR), AHEAD = 12, V_AHEAD = 8;   // LDS reads on their way ahead of the products that take them
+      auto key = [&](int i) __attribute__((always_inline)) {
+        const int k = i / 2, h = i % 2;
+        if (k < NK) return __builtin_bit_cast(tx8, *(LdsPieces)((LdsBytes)s_c + 4 * h * R * 2 + (k_at ^ 64 * (k % 4)) + 256 * (k / 4)));
+        return __builtin_bit_cast(tx8, *(LdsPieces)((LdsBytes)s_r + 4 * h * ROT * 2 + (rot_at ^ 64 * (k - NK))));
+      };
+      auto value = [&](int c) __attribute__((always_inline)) {
+        const LdsBytes from = (LdsBytes)s_c + (v_at ^ 32 * (c % 8)) + 256 * (c / 8);
+        return turned_rows<tx8>(from, from + 4 * R * 2);
+      };
+      tx8 kf[AHEAD], vf[V_AHEAD];
+#pragma unroll
+      for (int i = 0; i < AHEAD; ++i) kf[i] = key(i);
+#pragma unroll
+      for (int i = 0; i < KS; ++i) {
+        u[i % 2] = mma16(kf[i % AHEAD], q[i / 2], u[i % 2]);
+        if (i + AHEAD < KS) kf[i % AHEAD] = key(i + AHEAD);
+        if (i >= KS - V_AHEAD) vf[i - (KS - V_AHEAD)] = value(i - (KS - V_AHEAD));
+        __builtin_amdgcn_sched_barrier(0);
+      }
+      if (t * TT + TT > all_hi) {
+        const int from = t * TT + 8 * G;
+        const uint32_t seen = low_bits(see_hi - from) | (bits_from(bits, from - before) & low_bits(len - from));
+#pragma unroll
+        for (int e = 0; e < 8; ++e) u[e >> 2][e & 3] = seen >> e & 1 ? u[e >> 2][e & 3] : -INFINITY;
+      }
+      float top = u[0][0];
+#pragma unroll
+      for (int e = 1; e < 8; ++e) top = fmaxf(top, u[e >> 2][e & 3]);
+      top *= a.scale_log2;
+      if (__any(top > m + kLazy)) {
+        top = fmaxf(top, __shfl_xor(top, 16));
+        top = fmaxf(top, __shfl_xor(top, 32));
+        const float m_new = fmaxf(m, top), alpha = m_new == -INFINITY ? 1.f : __builtin_amdgcn_exp2f(m - m_new);
+        m = m_new;
+        l *= alpha;
+#pragma unroll
+        for (int ct = 0; ct < NCT; ++ct) o[ct] *= alpha;
+      }
+      const float base = m == -INFINITY ? 0.f : -m;
+      tx8 p;                                              // in the rows' type; the sum, in fp32, is of what they were rounded to
+#pragma unroll
+      for (int e = 0; e < 8; ++e) p[e] = to_element<tx8>(__builtin_amdgcn_exp2f(__builtin_fmaf(u[e >> 2][e & 3], a.scale_log2, base)));
+      l = add_eight(l, p);
+#pragma unroll
+      for (int c = 0; c < NCT; ++c) {
+        o[c] = mma16(vf[c % V_AHEAD], p, o[c]);
+        if (c + V_AHEAD < NCT) vf[c % V_AHEAD] = value(c + V_AHEAD);
+        __builtin_amdgcn_sched_barrier(0);
+      }
+      if (t + WAVES < t_end) {
+        asm volatile("s_waitcnt lgkmcnt(0)" ::: "memory");   // the tile has been read
+        load_tile(t + WAVES);
+      }
+    }
+
+    // ---- waves joined, then the result or a piece of it ----
+    l += __shfl_xor(l, 16);
+    l += __shfl_xor(l, 32);
+    __syncthreads();                                      // all tiles have been read
+#pragma unroll
+    for (int ct = 0; ct < NCT; ++ct)
+#pragma unroll
+      for (int e = 0; e < 4; ++e) s_space.o[wave][col][16 * ct + 4 * G + e] = o[ct][e];
+    if (G == 0) { s_m[wave][col] = m; s_l[wave][col] = l; }
+    __syncthreads();
+    const bool whole = t0 == 0 && t1 == tiles;
+    const long slot = 2l * blockIdx.x + (t0 == 0);
+    const int cols = min(pairs - first, M);
+    for (int idx = 2 * tid; idx < cols * R; idx += 512) {
+      const int c = idx / R, ch = idx % R;
+      float top = s_m[0][c];
+#pragma unroll
+      for (int w = 1; w < WAVES; ++w) top = fmaxf(top, s_m[w][c]);
+      const float base = top == -INFINITY ? 0.f : top;
+      float x = 0.f, y = 0.f, ll = 0.f;
+#pragma unroll
+      for (int w = 0; w < WAVES; ++w) {
+        const float f = __builtin_amdgcn_exp2f(s_m[w][c] - base);
+        x = __builtin_fmaf(s_space.o[w][c][ch], f, x);
+        y = __builtin_fmaf(s_space.o[w][c][ch + 1], f, y);
+        ll = __builtin_fmaf(s_l[w][c], f, ll);
+      }
+      if (whole) {
+        const float inv = ll == 0.f ? 0.f : 1.f / ll;
+        const int row = (first + c) / H;
+        uint16_t* const dst = a.out.data + (long)(s.row0 + row) * a.out.token_stride + (long)(first + c - row * H) * a.out.head_stride;
+        *reinterpret_cast<uint32_t*>(dst + ch) = pack2<T>(x * inv, y * inv);
+      } else {
+        *reinterpret_cast<f32x2*>(a.o + (slot * M + c) * R + ch) = f32x2{x, y};
+        if (ch == 0) *reinterpret_cast<f32x2*>(a.ml + 2 * (slot * M + c)) = f32x2{top, ll};
+      }
+    }
+    at += t1 - t0;
+    if (t1 == tiles && unit == __builtin_amdgcn_readfirstlane(wt.units) - 1) {   // the next sequence that has rows
+      begin = at;
+      do ++b;
+      while (at < end && weight_of(b).units == 0);
+    }
+  }
+}
+
+template <typename T, int R, int M>
 __global__ __launch_bounds__(256) void latent_join_kernel(LatentArgs a) {
-  constexpr int M = LatentShape<T, R, CB>::M;
   constexpr int GROUPS = M / kJoinColumns;
   const int H = a.q.heads, item = (int)(blockIdx.x / GROUPS), col = (int)(blockIdx.x % GROUPS) * kJoinColumns;
   const int b = item_owner(a.bt.starts, a.bt.rows, a.bt.batch, item, H, M, 1);
@@ -326,33 +527,50 @@ __global__ __launch_bounds__(256) void latent_join_kernel(LatentArgs a) {
 }
 
 struct LatentPlan {
-  int cb;
+  int cols;                // of a workgroup
   long items, workgroups;
 };
 
-static bool latent_plan(const dq_latent_cache* c, int batch, long rows, int heads, int max_rows, int max_seq_len, LatentPlan* p) {
+static bool latent_plan(int batch, long rows, int heads, int max_rows, int max_seq_len, LatentPlan* p) {
   if (batch <= 0 || rows < 0 || heads <= 0 || max_rows < 0 || max_seq_len < 0 || rows * heads >= (1l << 31) - 256) return false;
   const long cols = (long)max_rows * heads;
-  p->cb = cols <= 32 ? 1 : cols <= 64 ? 2 : 4;
-  p->items = rows * heads / (32 * p->cb) + batch;
-  if (p->items * 32 * p->cb >= kMaxThreads / 256) return false;
-  p->workgroups = 256;
+  p->cols = cols <= 16 ? 16 : cols <= 32 ? 32 : cols <= 64 ? 64 : 128;
+  p->items = rows * heads / p->cols + batch;
+  if (p->items * (p->cols / kJoinColumns) >= kMaxThreads / 256) return false;
+  p->workgroups = 256;                                    // a compute unit's LDS holds one
   return true;
 }
 static size_t latent_bytes(const dq_latent_cache* c, const LatentPlan& p) {
-  return (size_t)(2 * p.workgroups * 32 * p.cb) * (c->latent_dim + 2) * sizeof(float);
+  return (size_t)(2 * p.workgroups * p.cols) * (c->latent_dim + 2) * sizeof(float);
 }
 
 template <typename T, int R, int CB>
-static void launch_latent(const LatentArgs& a, const LatentPlan& p, hipStream_t st) {
+static void launch_latent_blocks(const LatentArgs& a, const LatentPlan& p, hipStream_t st) {
   hipLaunchKernelGGL((latent_attn_kernel<T, R, CB>), dim3((unsigned)p.workgroups), dim3(64 * LatentShape<T, R, CB>::WAVES), 0, st, a);
-  hipLaunchKernelGGL((latent_join_kernel<T, R, CB>), dim3((unsigned)(p.items * (32 * CB / kJoinColumns))), dim3(256), 0, st, a);
+}
+template <typename T, int R, int M>
+static void launch_latent_join(const LatentArgs& a, const LatentPlan& p, hipStream_t st) {
+  hipLaunchKernelGGL((latent_join_kernel<T, R, M>), dim3((unsigned)(p.items * (M / kJoinColumns))), dim3(256), 0, st, a);
 }
 template <typename T, int R>
-static void launch_latent_cols(const LatentArgs& a, const LatentPlan& p, hipStream_t st) {
-  if (p.cb == 1) launch_latent<T, R, 1>(a, p, st);
-  else if (p.cb == 2) launch_latent<T, R, 2>(a, p, st);
-  else launch_latent<T, R, 4>(a, p, st);
+static void launch_latent(const LatentArgs& a, const LatentPlan& p, hipStream_t st) {
+  switch (p.cols) {
+    case 16:
+      hipLaunchKernelGGL((latent_narrow_kernel<T, R>), dim3((unsigned)p.workgroups), dim3(256), 0, st, a);
+      launch_latent_join<T, R, 16>(a, p, st);
+      break;
+    case 32:
+      launch_latent_blocks<T, R, 1>(a, p, st);
+      launch_latent_join<T, R, 32>(a, p, st);
+      break;
+    case 64:
+      launch_latent_blocks<T, R, 2>(a, p, st);
+      launch_latent_join<T, R, 64>(a, p, st);
+      break;
+    default:
+      launch_latent_blocks<T, R, 4>(a, p, st);
+      launch_latent_join<T, R, 128>(a, p, st);
+  }
 }
 
 }  // namespace dq
@@ -362,7 +580,7 @@ using namespace dq;
 extern "C" size_t dq_latent_workspace_bytes(const dq_latent_cache* cache, int32_t batch, int32_t rows, int32_t q_heads, int32_t max_rows,
                                             int32_t max_seq_len) {
   LatentPlan p;
-  if (!latent_cache_ok(cache) || !latent_plan(cache, batch, rows, q_heads, max_rows, max_seq_len, &p)) return 0;
+  if (!latent_cache_ok(cache) || !latent_plan(batch, rows, q_heads, max_rows, max_seq_len, &p)) return 0;
   return latent_bytes(cache, p);                          // (smaller calls with the same heads have no more columns)
 }
 
@@ -373,7 +591,7 @@ extern "C" int32_t dq_latent_attention(const dq_latent_cache* cache, const dq_pa
   if (q->heads != out->heads || !workspace || ((uintptr_t)workspace & 15) || (flags & ~DQ_PAGED_CAUSAL) || !(softmax_scale > 0.f)) return DQ_EINVAL;
   if (seen && (((uintptr_t)seen & 7) || !(flags & DQ_PAGED_CAUSAL) || max_rows > 64)) return DQ_EINVAL;
   LatentPlan p;
-  if (!latent_plan(cache, batch->batch, batch->rows, q->heads, max_rows, max_seq_len, &p)) return DQ_EINVAL;
+  if (!latent_plan(batch->batch, batch->rows, q->heads, max_rows, max_seq_len, &p)) return DQ_EINVAL;
   if (workspace_bytes < latent_bytes(cache, p)) return DQ_ENOSPACE;
   if (batch->rows == 0 || max_rows == 0) return DQ_OK;
   LatentArgs a = {};
@@ -384,10 +602,10 @@ extern "C" int32_t dq_latent_attention(const dq_latent_cache* cache, const dq_pa
   a.scale_log2 = fmaxf(softmax_scale * 1.44269504088896340736f, 1e-37f);
   a.line = {(int)p.workgroups, 4};
   a.o = reinterpret_cast<float*>(workspace);
-  a.ml = a.o + 2 * p.workgroups * 32 * p.cb * cache->latent_dim;
+  a.ml = a.o + 2 * p.workgroups * p.cols * cache->latent_dim;
   hipStream_t st = (hipStream_t)hip_stream;
-  if (cache->dtype == DQ_BF16) { if (cache->latent_dim == 512) launch_latent_cols<__bf16, 512>(a, p, st); else launch_latent_cols<__bf16, 256>(a, p, st); }
-  else { if (cache->latent_dim == 512) launch_latent_cols<_Float16, 512>(a, p, st); else launch_latent_cols<_Float16, 256>(a, p, st); }
+  if (cache->dtype == DQ_BF16) { if (cache->latent_dim == 512) launch_latent<__bf16, 512>(a, p, st); else launch_latent<__bf16, 256>(a, p, st); }
+  else { if (cache->latent_dim == 512) launch_latent<_Float16, 512>(a, p, st); else launch_latent<_Float16, 256>(a, p, st); }
   DQ_HIP_CHECK(hipGetLastError());
   return DQ_OK;
 }
