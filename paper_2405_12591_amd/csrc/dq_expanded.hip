@@ -126,7 +126,7 @@ __global__ __launch_bounds__(256, 2) void expanded_attn_kernel(ExpandedArgs a) {
         const uint64_t lanes = __ballot(bad);
         if (lanes == 0 || !(lanes >> (lane / PD * PD) & ((1ull << PD) - 1))) continue;
         *v = u32x4{0, 0, 0, 0};
-        reinterpret_cast<u32x4*>(s_k[t & 1])[64 * (wave + 4 * i) + lane] = g_blank[1];
+        reinterpret_cast<u32x4*>(s_k[t & 1])[64 * (wave + 4 * i) + lane] = kNanPiece;
       }
       asm volatile("s_waitcnt lgkmcnt(0)" ::: "memory");
     }

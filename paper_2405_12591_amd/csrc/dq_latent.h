@@ -63,9 +63,10 @@ __device__ __forceinline__ float add_eight(float sum, bf16x8 v) {
   return sum;
 }
 
-// What a token that is not there has (zeros: nothing sees it, and 0 * NaN of what lies there would not be 0), and the key channels of
-// a page that does not exist (NaN for those who see its tokens).
-__device__ const u32x4 g_blank[2] = {{0, 0, 0, 0}, {0x7FFF7FFFu, 0x7FFF7FFFu, 0x7FFF7FFFu, 0x7FFF7FFFu}};
+// What a token that is not there has: zeros (nothing sees it, but 0 * NaN of what lies there would not be 0).
+__device__ const u32x4 g_blank[1] = {{0, 0, 0, 0}};
+
+constexpr u32x4 kNanPiece = {0x7FFF7FFFu, 0x7FFF7FFFu, 0x7FFF7FFFu, 0x7FFF7FFFu};   // eight NaN of either type
 
 // A ragged batch's tiles in one line: sequence after sequence, in a sequence unit after unit (a tile of query columns, a kv head), in a
 // unit from its first token tile on.  Workgroup w takes tiles [w quota, (w + 1) quota) of the line, whatever units they belong

@@ -103,16 +103,8 @@ __global__ __launch_bounds__((64 * LatentShape<T, R, CB>::WAVES), 2) void latent
     const bool turns = ROT / 16 >= CH || chs < ROT / 16;    // (four waves, two steps of shared channels)
 #pragma unroll
     for (int k = 0; k < NR; ++k) q[NK + k] = __builtin_bit_cast(tx8, turns ? *reinterpret_cast<const u32x4*>(q_row + R + 16 * (chs * NR + k)) : u32x4{0, 0, 0, 0});
-    const int place = before + my_row;
-    uint64_t bits = 0;                                    // of the sequence's own rows
-    int see_hi = a.causal ? min(place + 1, len) : len, all_hi = a.causal ? min(before + rows_lo + 1, len) : len;
-    int any_hi = a.causal ? min(before + rows_hi + 1, len) : len;
-    if (a.seen) {
-      bits = a.seen[s.row0 + my_row];
-      if (s.n < 64) bits &= (1ull << s.n) - 1;
-      see_hi = all_hi = min(before, len);
-      any_hi = len;
-    }
+    const int all_hi = a.seen ? min(before, len) : a.causal ? min(before + rows_lo + 1, len) : len;   // what every column, any column sees
+    const int any_hi = !a.seen && a.causal ? min(before + rows_hi + 1, len) : len;
     const int t_end = min(t1, (max(any_hi, 0) + TT - 1) / TT);
 
     f32x16 o[NCT];
@@ -161,12 +153,12 @@ __global__ __launch_bounds__((64 * LatentShape<T, R, CB>::WAVES), 2) void latent
 #pragma unroll 1
       for (int i = 0; i < LOADS - 1; ++i)
         if (EACH * (wave + WAVES * i) + copy_row >= left) *reinterpret_cast<u32x4*>(s_c[t % NB] + 1024 * (wave + WAVES * i) + 16 * l) = u32x4{0, 0, 0, 0};
-      if ((missing >> t % NB & 1) && rot_row < ROWS) *reinterpret_cast<u32x4*>(s_r[t % NB] + ROWS * wave * ROT * 2 + 16 * l) = g_blank[1];
+      if ((missing >> t % NB & 1) && rot_row < ROWS) *reinterpret_cast<u32x4*>(s_r[t % NB] + ROWS * wave * ROT * 2 + 16 * l) = kNanPiece;
       asm volatile("s_waitcnt lgkmcnt(0)" ::: "memory");
     };
 
     // ---- tile by tile ----
-    constexpr int KS = NK + NR, AHEAD = CB == 4 ? 4 : KS < 8 ? KS : 8, V_AHEAD = CB == 4 ? 2 : 4;   // LDS reads on their way ahead of the products that take them
+    constexpr int KS = NK + NR, AHEAD = CB == 4 ? 3 : KS < 8 ? KS : 8, V_AHEAD = CB == 4 ? 2 : 4;   // LDS reads on their way ahead of the products that take them
     KeyPlace kp;
     ValuePlace vp;
     auto key = [&](int t, int k) __attribute__((always_inline)) {
@@ -183,20 +175,8 @@ __global__ __launch_bounds__((64 * LatentShape<T, R, CB>::WAVES), 2) void latent
     };
     load_pages(t0);
     __syncthreads();                                      // buffers have been read
-    // Tile t is there, and all are done with the ones before it, and with their sums.  Two tiles are on their way at all times.
-    auto arrive = [&](int t) __attribute__((always_inline)) {
-      if (t + 1 < t_end) wait_copies<LOADS>();
-      else wait_copies<0>();
-      mend_tile(t);
-      barrier();
-    };
-    if (t0 < t_end) {
-      load_tile(t0);
-      if (t0 + 1 < t_end) load_tile(t0 + 1);
-      arrive(t0);
-      if (t0 + 2 < t_end) load_tile(t0 + 2);
-    }
-    for (int t = t0; t < t_end; ++t) {
+    // A tile's two halves: the wave's sums, handed over; then, behind a barrier, the whole scores, their softmax and the product with the values.
+    auto hand_over = [&](int t) __attribute__((always_inline)) {
       kp = key_place();
       f32x16 u;
 #pragma unroll
@@ -214,26 +194,36 @@ __global__ __launch_bounds__((64 * LatentShape<T, R, CB>::WAVES), 2) void latent
 #pragma unroll
       for (int i = 0; i < 4; ++i) s_sums[wave][i][l_sums] = f32x4{u[4 * i], u[4 * i + 1], u[4 * i + 2], u[4 * i + 3]};
       asm volatile("s_waitcnt lgkmcnt(0)" ::: "memory");
-      barrier();
+    };
+    auto finish = [&](int t) __attribute__((always_inline)) {
       // in an order that gives all of them the same bits: the waves must agree on maxima
-      auto others = [&](int w, f32x16& to, bool add) __attribute__((always_inline)) {
+      f32x16 u;
+      const int l_sums = this_lane();
+      auto sums_of = [&](int w, f32x16& to, bool add) __attribute__((always_inline)) {
 #pragma unroll
         for (int i = 0; i < 4; ++i) {
-          const f32x4 x = s_sums[cb * CH + (chs ^ w)][i][l_sums];
+          const f32x4 x = s_sums[cb * CH + w][i][l_sums];
 #pragma unroll
           for (int e = 0; e < 4; ++e) to[4 * i + e] = add ? to[4 * i + e] + x[e] : x[e];
+          if (CB == 4 && add && i % 2) __builtin_amdgcn_sched_barrier(0);
         }
       };
-      others(1, u, true);
-      if constexpr (CH == 4) {
-        f32x16 pair;
-        others(2, pair, false);
-        others(3, pair, true);
-        u += pair;
+      sums_of(0, u, false);
+#pragma unroll
+      for (int w = 1; w < CH; ++w) {
+        __builtin_amdgcn_sched_barrier(0);
+        sums_of(w, u, true);
       }
       if (t * TT + TT > all_hi) {
-        const int from = t * TT + 8 * (this_lane() >> 5);   // (a branch, and nothing of it ahead of the loop)
-        const uint32_t seen = low_bits(see_hi - from) | (bits_from(bits, from - before) & low_bits(len - from));
+        // what a column sees is looked up here, in the few tiles that ask for it: held over the loop it would take registers
+        const int lane_now = this_lane(), from = t * TT + 8 * (lane_now >> 5);
+        const int row = min(first + cb * 32 + (lane_now & 31), pairs - 1) / H;
+        uint32_t seen = low_bits((a.seen ? all_hi : a.causal ? min(before + row + 1, len) : len) - from);
+        if (a.seen) {
+          uint64_t bits = a.seen[s.row0 + row];
+          if (s.n < 64) bits &= (1ull << s.n) - 1;
+          seen |= bits_from(bits, from - before) & low_bits(len - from);
+        }
 #pragma unroll
         for (int e = 0; e < 16; ++e) u[e] = seen >> (16 * (e >> 3) + (e & 7)) & 1 ? u[e] : -INFINITY;
       }
@@ -265,10 +255,39 @@ __global__ __launch_bounds__((64 * LatentShape<T, R, CB>::WAVES), 2) void latent
         if (i + V_AHEAD < 2 * NCT) vf[i % V_AHEAD] = value(t, i + V_AHEAD);
         __builtin_amdgcn_sched_barrier(0);
       }
-      if (t + 1 < t_end) {
-        arrive(t + 1);
-        if (t + 3 < t_end) load_tile(t + 3);
+    };
+    auto arrived = [&](int t) __attribute__((always_inline)) {   // the wave's copies of tile t; the next one's are on their way
+      if (t + 1 < t_end) wait_copies<LOADS>();
+      else wait_copies<0>();
+      mend_tile(t);
+    };
+    if (t0 < t_end) {
+      load_tile(t0);
+      if (t0 + 1 < t_end) load_tile(t0 + 1);
+      arrived(t0);
+      barrier();
+    }
+    // Two barriers a tile.  Of each SIMD's two waves one finishes a tile while the other forms sums: the second four waves are half a tile
+    // behind, so that softmax and matrix instructions go together (118 us with all in step, 16 x 14 thousand tokens, 128 columns).
+    if (WAVES == 4 || wave < 4) {
+      for (int t = t0; t < t_end; ++t) {
+        hand_over(t);
+        barrier();
+        if (t + 2 < t_end) load_tile(t + 2);              // all are done with tile t - 1
+        finish(t);
+        if (t + 1 < t_end) arrived(t + 1);
+        barrier();
       }
+    } else {
+      for (int t = t0; t < t_end; ++t) {
+        if (t > t0) finish(t - 1);
+        barrier();
+        if (t + 2 < t_end) load_tile(t + 2);
+        hand_over(t);
+        if (t + 1 < t_end) arrived(t + 1);
+        barrier();
+      }
+      if (t0 < t_end) finish(t_end - 1);
     }
 
     // ---- the result, or a piece of it (places formed anew: held over the loop they would take registers) ----
@@ -401,7 +420,7 @@ __global__ __launch_bounds__(256, 1) void latent_narrow_kernel(LatentArgs a) {
         for (int i = 0; i < COPIES; ++i)
           if (i * EACH + lane / (64 / EACH) >= left) *reinterpret_cast<u32x4*>(s_c + 1024 * i + 16 * lane) = u32x4{0, 0, 0, 0};
         if (page < 0)
-          for (int i = 0; i < ROT_COPIES; ++i) *reinterpret_cast<u32x4*>(s_r + 1024 * i + 16 * lane) = g_blank[1];
+          for (int i = 0; i < ROT_COPIES; ++i) *reinterpret_cast<u32x4*>(s_r + 1024 * i + 16 * lane) = kNanPiece;
       }
       f32x4 u[2];
       u[0] = u[1] = f32x4{0.f, 0.f, 0.f, 0.f};
