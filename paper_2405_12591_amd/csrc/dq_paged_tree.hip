@@ -48,7 +48,9 @@ template <typename T, int D, bool FP8, int CB>
 __global__ __launch_bounds__(256, 2) void tree_attn_kernel(TreeArgs a) {
   constexpr int M = 32 * CB, TG = 4 / CB, NC = D / 32, PD = D / 8;
   typedef typename Vec8<T>::type tx8;
+  constexpr int NB = CB, PIECES = D / 16, COPIES = D / 8 / CB;   // tiles in LDS of a group of waves; 16-byte pieces of a key row; a wave's copies of a tile
   union Space {
+    char codes[TG][NB][2][kPagedTile * D];                // keys, values as the cache holds them
     char v[kTreeRows * D * 2];                            // drafted values, row by row
     float o[TG > 1 ? 4 : 1][32][D + 1];
   };
@@ -161,10 +163,14 @@ __global__ __launch_bounds__(256, 2) void tree_attn_kernel(TreeArgs a) {
     };
 
     // ---- full pages ----
-    const int code_tiles = len / P * runs, stride = TG;
-    const int last_code = min(s.first_tile + t1, code_tiles);
-    for (int batch0 = s.first_tile + t0 + tg; batch0 < last_code; batch0 += 64 * stride) {
-      const int t_l = batch0 + lane * stride;             // the next 64 tiles' blocks and scales, one per lane
+    // A tile's codes lie in one piece; they are copied to LDS past the registers, by the waves that read them (as 16-byte loads of rows they came in
+    // quarters of lines, and once for every wave).  Pieces are exchanged by bits of the row so that 16 lanes touch all banks.
+    auto key_swap = [](int t) { return PIECES == 8 ? (t >> 1 & 3) | (t >> 4 & 1) << 2 : (t >> 2 & 1) | (t >> 4 & 1) << 1; };
+    const int code_tiles = len / P * runs;
+    const int code_first = s.first_tile + t0, last_code = min(s.first_tile + t1, code_tiles);
+    __syncthreads();                                      // what the last unit left in LDS has been read
+    for (int batch0 = code_first; batch0 < last_code; batch0 += 64 * TG) {
+      const int t_l = batch0 + lane * TG + tg;            // the next 64 tiles' blocks and scales, one per lane
       int blk = -1;
       float sk = 0.f, lsv = 0.f, isv = 0.f;
       if (t_l < last_code) {
@@ -178,57 +184,86 @@ __global__ __launch_bounds__(256, 2) void tree_attn_kernel(TreeArgs a) {
         isv = 1.f / sv;
       }
       place_zero_blocks<D, FP8>(a.c.v_codes, blk, blk >= 0, lsv, isv);
-      const int count = min(64, (last_code - batch0 + stride - 1) / stride);
-      u32x4 kb[2][NC], vb[NC][2];
-      auto load_k = [&](int i) __attribute__((always_inline)) {
-        const GlobalBytes p = codes_of(a.c.k_codes, __builtin_amdgcn_readlane(blk, i), kPagedTile * D) + k_row * D + 16 * hl;
+      // (every group of waves goes through the barriers of the one with most tiles)
+      const int most = min(64, (last_code - batch0 + TG - 1) / TG), count = min(64, max(last_code - batch0 - tg + TG - 1, 0) / TG);
+      auto copy_tile = [&](int i) __attribute__((always_inline)) {
+        const int block = __builtin_amdgcn_readlane(blk, i);
+        int l = lane;
+        asm volatile("" : "+v"(l));                       // (else the offsets are held over the loop)
+        const int row = l / PIECES, key = row * D + ((l % PIECES ^ key_swap(row)) << 4), value = l / 4 * 64 + ((l % 4 ^ (l >> 4 & 3)) << 4);
+        const uint8_t* const ks = block < 0 ? reinterpret_cast<const uint8_t*>(g_no_codes) : a.c.k_codes + (long)block * (kPagedTile * D);
+        const uint8_t* const vs = block < 0 ? reinterpret_cast<const uint8_t*>(g_no_codes) : a.c.v_codes + (long)block * (kPagedTile * D);
+        const uint32_t to = lds_of(s_space.codes[tg][i % NB][0]);
 #pragma unroll
-        for (int tt = 0; tt < 2; ++tt)
-#pragma unroll
-          for (int c = 0; c < NC; ++c) kb[tt][c] = *(GlobalPieces)(p + 32 * tt * D + 32 * c);
+        for (int j = 0; j < COPIES; ++j) {
+          const int c = j * CB + cb, part = c % PIECES;   // keys' pieces first
+          const int turn = PIECES == 8 ? (part >> 1 & 1) << 2 : (part & 1) << 1;
+          copy_to_lds<CB < 4>(reinterpret_cast<const uint16_t*>((c < PIECES ? ks : vs) + 1024 * part), c < PIECES ? key ^ turn << 4 : value, to + 1024 * c);
+        }
       };
-      auto load_v = [&](int i) __attribute__((always_inline)) {
-        const GlobalBytes p = codes_of(a.c.v_codes, __builtin_amdgcn_readlane(blk, i), kPagedTile * D) + r32 * kPagedTile + 16 * hl;
-#pragma unroll
-        for (int ct = 0; ct < NC; ++ct)
-#pragma unroll
-          for (int tt = 0; tt < 2; ++tt) vb[ct][tt] = *(GlobalPieces)(p + ct * 32 * kPagedTile + 32 * tt);
+      u32x4 kb[CB == 1 ? 2 : 1][CB == 1 ? NC : 1], vb[CB == 1 ? NC : 1][CB == 1 ? 2 : 1];   // a wave alone: the tile in registers, the next one on its way
+      auto key_codes = [&](int i, int c, int tt) __attribute__((always_inline)) {
+        return *(LdsPieces)((LdsBytes)s_space.codes[tg][i % NB][0] + (32 * tt + k_row) * D + ((2 * c + hl ^ key_swap(k_row)) << 4));
       };
-      load_k(0);
-      load_v(0);
-      for (int i = 0; i < count; ++i) {
+      auto value_codes = [&](int i, int ct, int tt) __attribute__((always_inline)) {
+        return *(LdsPieces)((LdsBytes)s_space.codes[tg][i % NB][1] + (32 * ct + r32) * 64 + ((2 * tt + hl ^ (r32 >> 2 & 3)) << 4));
+      };
+      if (batch0 > code_first && CB > 1) __syncthreads();
+#pragma unroll
+      for (int i = 0; i < (NB > 1 ? NB - 1 : 1); ++i)
+        if (i < count) copy_tile(i);
+      for (int i = 0; i < most; ++i) {
+        if constexpr (CB == 1) {
+          wait_copies<0>();
+          if (i >= count) break;
+#pragma unroll
+          for (int tt = 0; tt < 2; ++tt)
+#pragma unroll
+            for (int c = 0; c < NC; ++c) {
+              kb[tt][c] = key_codes(i, c, tt);
+              vb[c][tt] = value_codes(i, c, tt);
+            }
+          asm volatile("s_waitcnt lgkmcnt(0)" ::: "memory");
+          if (i + 1 < count) copy_tile(i + 1);
+        } else {
+          if (NB > 2 && i + NB - 2 < count) wait_copies<(NB - 2) * COPIES>();
+          else wait_copies<0>();
+          barrier();                                      // the tile is there, and all are done with the one before it
+          if (i + NB - 1 < count) copy_tile(i + NB - 1);
+          if (i >= count) continue;
+        }
         float f = __builtin_bit_cast(float, __builtin_amdgcn_readlane(__builtin_bit_cast(int, sk), i));
         const float add = __builtin_bit_cast(float, __builtin_amdgcn_readlane(__builtin_bit_cast(int, lsv), i));
         const float inv_sv = __builtin_bit_cast(float, __builtin_amdgcn_readlane(__builtin_bit_cast(int, isv), i));
         f32x16 u[2];
 #pragma unroll
-        for (int tt = 0; tt < 2; ++tt) {
+        for (int e = 0; e < 32; ++e) u[e >> 4][e & 15] = 0.f;
 #pragma unroll
-          for (int e = 0; e < 16; ++e) u[tt][e] = 0.f;
+        for (int c = 0; c < NC; ++c)
 #pragma unroll
-          for (int c = 0; c < NC; ++c) {
-            u[tt] = mma32(codes_f16<FP8>(kb[tt][c].x, kb[tt][c].y), q[c][0], u[tt]);
-            u[tt] = mma32(codes_f16<FP8>(kb[tt][c].z, kb[tt][c].w), q[c][1], u[tt]);
-          }
-        }
-        if (i + 1 < count) load_k(i + 1);
+          for (int hf = 0; hf < 2; ++hf)
+#pragma unroll
+            for (int tt = 0; tt < 2; ++tt) {
+              const u32x4 w = CB == 1 ? kb[CB == 1 ? tt : 0][CB == 1 ? c : 0] : key_codes(i, c, tt);
+              u[tt] = mma32(hf ? codes_f16<FP8>(w.z, w.w) : codes_f16<FP8>(w.x, w.y), q[c][hf], u[tt]);
+            }
         f = keep_sign(f * sc);
-        const int from = (batch0 + i * stride) * kPagedTile;
+        const int from = (batch0 + i * TG + tg) * kPagedTile;
         if (from < all_lo) hide(u, f, from, see_lo, INT32_MAX);
         softmax(u, f, add, inv_sv);
         // 11 bits, as the codes' products want them (the sum keeps fp32)
 #pragma unroll
-        for (int tt = 0; tt < 2; ++tt)
+        for (int tt = 0; tt < 2; ++tt) {
+          f16x8 p[2];
 #pragma unroll
-          for (int hf = 0; hf < 2; ++hf) {
-            f16x8 p;
+          for (int e = 0; e < 16; ++e) p[e >> 3][e & 7] = (_Float16)u[tt][e];
 #pragma unroll
-            for (int e = 0; e < 8; ++e) p[e] = (_Float16)u[tt][8 * hf + e];
-#pragma unroll
-            for (int ct = 0; ct < NC; ++ct)
-              o[ct] = mma32(hf ? codes_f16<FP8>(vb[ct][tt].z, vb[ct][tt].w) : codes_f16<FP8>(vb[ct][tt].x, vb[ct][tt].y), p, o[ct]);
+          for (int ct = 0; ct < NC; ++ct) {
+            const u32x4 w = CB == 1 ? vb[CB == 1 ? ct : 0][CB == 1 ? tt : 0] : value_codes(i, ct, tt);
+            o[ct] = mma32(codes_f16<FP8>(w.x, w.y), p[0], o[ct]);
+            o[ct] = mma32(codes_f16<FP8>(w.z, w.w), p[1], o[ct]);
           }
-        if (i + 1 < count) load_v(i + 1);
+        }
       }
     }
 
@@ -297,7 +332,7 @@ __global__ __launch_bounds__(256, 2) void tree_attn_kernel(TreeArgs a) {
 
     // ---- the drafted rows: values through LDS, for their transposed reads ----
     if (t1 == tiles) {
-      __syncthreads();                                    // what the last unit left there has been read
+      __syncthreads();                                    // the codes have been read
       if (tid == 0) s_bad = 0;
       __syncthreads();
       auto swap_of = [](int t) { return PD == 16 ? (t & 3) << 2 | (t >> 2 & 3) : (t >> 1 & 1) << 2 | (t >> 2 & 3); };
