@@ -201,7 +201,6 @@ __global__ __launch_bounds__(256, 2) void tree_attn_kernel(TreeArgs a) {
           copy_to_lds<CB < 4>(reinterpret_cast<const uint16_t*>((c < PIECES ? ks : vs) + 1024 * part), c < PIECES ? key ^ turn << 4 : value, to + 1024 * c);
         }
       };
-      u32x4 kb[CB == 1 ? 2 : 1][CB == 1 ? NC : 1], vb[CB == 1 ? NC : 1][CB == 1 ? 2 : 1];   // a wave alone: the tile in registers, the next one on its way
       auto key_codes = [&](int i, int c, int tt) __attribute__((always_inline)) {
         return *(LdsPieces)((LdsBytes)s_space.codes[tg][i % NB][0] + (32 * tt + k_row) * D + ((2 * c + hl ^ key_swap(k_row)) << 4));
       };
@@ -214,17 +213,8 @@ __global__ __launch_bounds__(256, 2) void tree_attn_kernel(TreeArgs a) {
         if (i < count) copy_tile(i);
       for (int i = 0; i < most; ++i) {
         if constexpr (CB == 1) {
-          wait_copies<0>();
+          wait_copies<0>();                               // (a wave's own tile: the other waves compute meanwhile)
           if (i >= count) break;
-#pragma unroll
-          for (int tt = 0; tt < 2; ++tt)
-#pragma unroll
-            for (int c = 0; c < NC; ++c) {
-              kb[tt][c] = key_codes(i, c, tt);
-              vb[c][tt] = value_codes(i, c, tt);
-            }
-          asm volatile("s_waitcnt lgkmcnt(0)" ::: "memory");
-          if (i + 1 < count) copy_tile(i + 1);
         } else {
           if (NB > 2 && i + NB - 2 < count) wait_copies<(NB - 2) * COPIES>();
           else wait_copies<0>();
@@ -244,7 +234,7 @@ __global__ __launch_bounds__(256, 2) void tree_attn_kernel(TreeArgs a) {
           for (int hf = 0; hf < 2; ++hf)
 #pragma unroll
             for (int tt = 0; tt < 2; ++tt) {
-              const u32x4 w = CB == 1 ? kb[CB == 1 ? tt : 0][CB == 1 ? c : 0] : key_codes(i, c, tt);
+              const u32x4 w = key_codes(i, c, tt);
               u[tt] = mma32(hf ? codes_f16<FP8>(w.z, w.w) : codes_f16<FP8>(w.x, w.y), q[c][hf], u[tt]);
             }
         f = keep_sign(f * sc);
@@ -259,28 +249,41 @@ __global__ __launch_bounds__(256, 2) void tree_attn_kernel(TreeArgs a) {
           for (int e = 0; e < 16; ++e) p[e >> 3][e & 7] = (_Float16)u[tt][e];
 #pragma unroll
           for (int ct = 0; ct < NC; ++ct) {
-            const u32x4 w = CB == 1 ? vb[CB == 1 ? ct : 0][CB == 1 ? tt : 0] : value_codes(i, ct, tt);
+            const u32x4 w = value_codes(i, ct, tt);
             o[ct] = mma32(codes_f16<FP8>(w.x, w.y), p[0], o[ct]);
             o[ct] = mma32(codes_f16<FP8>(w.z, w.w), p[1], o[ct]);
           }
+        }
+        if (CB == 1 && i + 1 < count) {
+          asm volatile("s_waitcnt lgkmcnt(0)" ::: "memory");   // the tile has been read
+          copy_tile(i + 1);
         }
       }
     }
 
     // Products of 16-bit rows, keys `key(tt, channel)` and values `value(ct, tt, half)`, in their own type.
     auto row_tile = [&](auto key, auto value, float f, int from, int lo, int hi, uint64_t hidden, uint64_t bad) __attribute__((always_inline)) {
+      // (a half's pieces are asked for together, and the queries' once more, in their own type)
       f32x16 u[2];
+      tx8 rows_q[NC][2];
+#pragma unroll
+      for (int c = 0; c < NC; ++c)
+#pragma unroll
+        for (int hf = 0; hf < 2; ++hf) rows_q[c][hf] = __builtin_bit_cast(tx8, *reinterpret_cast<const u32x4*>(q_row + 32 * c + 8 * hf));
 #pragma unroll
       for (int tt = 0; tt < 2; ++tt) {
+        u32x4 keys[NC][2];
+#pragma unroll
+        for (int c = 0; c < NC; ++c)
+#pragma unroll
+          for (int hf = 0; hf < 2; ++hf) keys[c][hf] = key(tt, 32 * c + 8 * hf);
 #pragma unroll
         for (int e = 0; e < 16; ++e) u[tt][e] = 0.f;
 #pragma unroll
-        for (int c = 0; c < NC; ++c) {
-          if (tt || c) __builtin_amdgcn_sched_barrier(0);   // (all loads ahead of the first product would take 128 registers)
+        for (int c = 0; c < NC; ++c)
 #pragma unroll
-          for (int hf = 0; hf < 2; ++hf)
-            u[tt] = mma32(__builtin_bit_cast(tx8, key(tt, 32 * c + 8 * hf)), __builtin_bit_cast(tx8, *reinterpret_cast<const u32x4*>(q_row + 32 * c + 8 * hf)), u[tt]);
-        }
+          for (int hf = 0; hf < 2; ++hf) u[tt] = mma32(__builtin_bit_cast(tx8, keys[c][hf]), rows_q[c][hf], u[tt]);
+        __builtin_amdgcn_sched_barrier(0);
       }
       hide(u, f, from, lo, hi);
       int shift = 16 * hl;
@@ -294,7 +297,12 @@ __global__ __launch_bounds__(256, 2) void tree_attn_kernel(TreeArgs a) {
       }
       softmax(u, f, 0.f, 1.f);
 #pragma unroll
-      for (int tt = 0; tt < 2; ++tt)
+      for (int tt = 0; tt < 2; ++tt) {
+        tx8 values[NC][2];
+#pragma unroll
+        for (int ct = 0; ct < NC; ++ct)
+#pragma unroll
+          for (int hf = 0; hf < 2; ++hf) values[ct][hf] = value(ct, tt, hf);
 #pragma unroll
         for (int hf = 0; hf < 2; ++hf) {
           // in the rows' type, which their products need: 8 bits with bf16 rows, one more such rounding for each of these tokens
@@ -302,9 +310,10 @@ __global__ __launch_bounds__(256, 2) void tree_attn_kernel(TreeArgs a) {
 #pragma unroll
           for (int e = 0; e < 4; ++e) p[e] = pack2<T>(u[tt][8 * hf + 2 * e], u[tt][8 * hf + 2 * e + 1]);
 #pragma unroll
-          for (int ct = 0; ct < NC; ++ct) o[ct] = mma32(value(ct, tt, hf), __builtin_bit_cast(tx8, p), o[ct]);
-          __builtin_amdgcn_sched_barrier(0);
+          for (int ct = 0; ct < NC; ++ct) o[ct] = mma32(values[ct][hf], __builtin_bit_cast(tx8, p), o[ct]);
         }
+        __builtin_amdgcn_sched_barrier(0);
+      }
     };
 
     // ---- the page being filled ----
@@ -337,7 +346,7 @@ __global__ __launch_bounds__(256, 2) void tree_attn_kernel(TreeArgs a) {
       __syncthreads();
       auto swap_of = [](int t) { return PD == 16 ? (t & 3) << 2 | (t >> 2 & 3) : (t >> 1 & 1) << 2 | (t >> 2 & 3); };
       constexpr uint32_t kExp = __is_same(T, __bf16) ? 0x7F80u : 0x7C00u;
-#pragma unroll 1
+#pragma unroll
       for (int i = tid; i < kTreeRows * PD; i += 256) {   // (whole waves)
         const int row = i / PD, piece = i % PD;
         u32x4 w = {}, kw = {};
