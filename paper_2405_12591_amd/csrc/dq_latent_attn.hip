@@ -619,7 +619,7 @@ extern "C" int32_t dq_latent_attention(const dq_latent_cache* cache, const dq_pa
   a.max_rows = max_rows;
   a.causal = (flags & DQ_PAGED_CAUSAL) ? 1 : 0;
   a.scale_log2 = fmaxf(softmax_scale * 1.44269504088896340736f, 1e-37f);
-  a.line = {(int)p.workgroups, 4};
+  a.line = {(int)p.workgroups, p.cols == 16 ? 4 : 2};   // four waves with a tile each; all waves with one
   a.o = reinterpret_cast<float*>(workspace);
   a.ml = a.o + 2 * p.workgroups * p.cols * cache->latent_dim;
   hipStream_t st = (hipStream_t)hip_stream;

@@ -17,13 +17,16 @@ struct TreeArgs {
 };
 
 constexpr int kTreeRows = 64;
+// Tiles of the line that a unit's drafted rows count for: they are a chain of their own (values to LDS, keys, masks) and would otherwise make
+// the workgroups that have them the last ones (8 sequences of 2 to 9 thousand tokens, window 4096, 64 units: 30 us counted as one tile).
+constexpr int kDraftedTiles = 6;
 
 struct TreeSequence {
   int row0, n;             // its drafted rows
   int place0;              // place of a row that sees itself alone
   int len;                 // cached tokens
   int first_tile;          // of the cached tokens that any row sees
-  Weight w;                // units: kv head after kv head, a head's column tiles; tiles: of 64 cached tokens, and the drafted rows' one
+  Weight w;                // units: kv head after kv head, a head's column tiles; tiles: of 64 cached tokens, and the drafted rows'
 };
 template <int M>
 __device__ __forceinline__ TreeSequence tree_sequence(const TreeArgs& a, int b) {
@@ -36,7 +39,7 @@ __device__ __forceinline__ TreeSequence tree_sequence(const TreeArgs& a, int b) 
   t.first_tile = a.window ? max(t.place0 - a.window, 0) / kPagedTile : 0;   // (a row that sees none has the place before)
   const int code_tiles = (s.len + kPagedTile - 1) / kPagedTile;
   t.w.units = t.n ? a.c.kv_heads * ((t.n * a.group + M - 1) / M) : 0;
-  t.w.tiles = max(code_tiles - t.first_tile, 0) + 1;
+  t.w.tiles = max(code_tiles - t.first_tile, 0) + kDraftedTiles;
   return t;
 }
 
@@ -317,7 +320,7 @@ __global__ __launch_bounds__(256, 2) void tree_attn_kernel(TreeArgs a) {
     };
 
     // ---- the page being filled ----
-    for (int tile = max(code_tiles, s.first_tile + t0); tile < s.first_tile + min(t1, tiles - 1); ++tile) {
+    for (int tile = max(code_tiles, s.first_tile + t0); tile < s.first_tile + min(t1, tiles - kDraftedTiles); ++tile) {
       if ((tile - s.first_tile - t0) % TG != tg) continue;
       const int slot = a.bt.tail_slots ? a.bt.tail_slots[b] : b;
       const bool ok = slot >= 0 && slot < a.c.slots;
@@ -536,7 +539,7 @@ extern "C" int32_t dq_paged_tree_attention(const dq_paged_cache* cache, const dq
   a.max_rows = max_rows;
   a.window = window;
   a.scale_log2 = (softmax_scale > 0.f ? softmax_scale : 1.0f / sqrtf((float)cache->head_dim)) * 1.44269504088896340736f;
-  a.line = {(int)p.workgroups, 8};
+  a.line = {(int)p.workgroups, 1};
   a.o = reinterpret_cast<float*>(workspace);
   a.ml = a.o + 2 * p.workgroups * 32 * p.cb * cache->head_dim;
   hipStream_t st = (hipStream_t)hip_stream;
