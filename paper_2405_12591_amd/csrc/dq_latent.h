@@ -150,10 +150,10 @@ struct Pieces {
 __device__ __forceinline__ Pieces pieces_of(long begin, int tiles, long quota) { return {begin / quota, (begin + tiles - 1) / quota}; }
 __device__ __forceinline__ long slot_of(const Pieces& p, long w) { return w == p.first ? 2 * w + 1 : 2 * w; }
 
-// Joins the pieces of kJoinColumns columns (those below `valid`): a wave a column where there are few pieces, four waves a column, which take
+// Joins the pieces of kJoinColumns<D> columns (those below `valid`): a wave a column where there are few pieces, four waves a column, which take
 // every fourth piece, where there are many.  o: [slot, column, D] floats, ml: [slot, column, 2]; eight pieces are asked for at once.
 // (A workgroup a column spent most of its time on finding its unit: 39 us where this takes 8, 64 columns of 128 units in 4 or 5 pieces.)
-constexpr int kJoinColumns = 4;
+template <int D> constexpr int kJoinColumns = D >= 256 ? 4 : 16;   // (512 channels: 16 us, 21 with sixteen; 64 channels 16, 20 with four)
 template <typename T, int D, typename Slot, typename Out>
 __device__ __forceinline__ void join_columns(int count, Slot slot_of_piece, const float* o, const float* ml, int columns, int column0, int valid, Out out_of) {
   constexpr int PER = D / 64, AHEAD = 8;
@@ -201,12 +201,13 @@ __device__ __forceinline__ void join_columns(int count, Slot slot_of_piece, cons
     }
   };
   if (count <= 4 * AHEAD) {
-    if (column0 + wave >= valid) return;
-    const Sum r = add(column0 + wave, 0, 1);
-    store(out_of(column0 + wave), r.x, r.l);
+    for (int c = column0 + wave; c < min(column0 + kJoinColumns<D>, valid); c += 4) {
+      const Sum r = add(c, 0, 1);
+      store(out_of(c), r.x, r.l);
+    }
     return;
   }
-  for (int c = column0; c < min(column0 + kJoinColumns, valid); ++c) {
+  for (int c = column0; c < min(column0 + kJoinColumns<D>, valid); ++c) {
     const Sum r = add(c, wave, 4);
     __syncthreads();                                      // the last column's results have been read
 #pragma unroll

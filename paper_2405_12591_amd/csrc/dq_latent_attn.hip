@@ -45,7 +45,7 @@ __device__ __forceinline__ uint32_t bits_from(uint64_t bits, int at) {
 // alone on its SIMD, 16 sequences of 14 thousand tokens with 128 heads took 178 us.)  Key rows are taken in the order that leaves a lane
 // the probabilities of 8 neighbouring tokens twice, the right operand of the second product.
 template <typename T, int R, int CB>
-__global__ __launch_bounds__((64 * LatentShape<T, R, CB>::WAVES), 2) void latent_attn_kernel(LatentArgs a) {
+__global__ __launch_bounds__((64 * LatentShape<T, R, CB>::WAVES), (LatentShape<T, R, CB>::WAVES / 4)) void latent_attn_kernel(LatentArgs a) {
   typedef LatentShape<T, R, CB> Shape;
   constexpr int ROT = Shape::ROT, W = Shape::W, CH = Shape::CH, M = Shape::M, NB = Shape::BUFFERS, WAVES = Shape::WAVES;
   constexpr int TT = kLatentTile, NK = R / 16 / CH, NR = ROT / 16 >= CH ? ROT / 16 / CH : 1, NCT = R / 32 / CH;   // a wave's steps and channel tiles
@@ -528,8 +528,8 @@ __global__ __launch_bounds__(256, 1) void latent_narrow_kernel(LatentArgs a) {
 
 template <typename T, int R, int M>
 __global__ __launch_bounds__(256) void latent_join_kernel(LatentArgs a) {
-  constexpr int GROUPS = M / kJoinColumns;
-  const int H = a.q.heads, item = (int)(blockIdx.x / GROUPS), col = (int)(blockIdx.x % GROUPS) * kJoinColumns;
+  constexpr int GROUPS = M / kJoinColumns<R>;
+  const int H = a.q.heads, item = (int)(blockIdx.x / GROUPS), col = (int)(blockIdx.x % GROUPS) * kJoinColumns<R>;
   const int b = item_owner(a.bt.starts, a.bt.rows, a.bt.batch, item, H, M, 1);
   const Sequence s = sequence_of_wave(a.bt, a.c.page_tokens, b);
   const int pairs = min(s.n, a.max_rows) * H, first = (item - item_first(a.bt.starts, a.bt.rows, b, H, M, 1)) * M;
@@ -555,7 +555,7 @@ static bool latent_plan(int batch, long rows, int heads, int max_rows, int max_s
   const long cols = (long)max_rows * heads;
   p->cols = cols <= 16 ? 16 : cols <= 32 ? 32 : cols <= 64 ? 64 : 128;
   p->items = rows * heads / p->cols + batch;
-  if (p->items * (p->cols / kJoinColumns) >= kMaxThreads / 256) return false;
+  if (p->items * (p->cols / kJoinColumns<512>) >= kMaxThreads / 256) return false;
   p->workgroups = 256;                                    // a compute unit's LDS holds one
   return true;
 }
@@ -569,7 +569,7 @@ static void launch_latent_blocks(const LatentArgs& a, const LatentPlan& p, hipSt
 }
 template <typename T, int R, int M>
 static void launch_latent_join(const LatentArgs& a, const LatentPlan& p, hipStream_t st) {
-  hipLaunchKernelGGL((latent_join_kernel<T, R, M>), dim3((unsigned)(p.items * (M / kJoinColumns))), dim3(256), 0, st, a);
+  hipLaunchKernelGGL((latent_join_kernel<T, R, M>), dim3((unsigned)(p.items * (M / kJoinColumns<R>))), dim3(256), 0, st, a);
 }
 template <typename T, int R>
 static void launch_latent(const LatentArgs& a, const LatentPlan& p, hipStream_t st) {

@@ -459,8 +459,8 @@ __global__ __launch_bounds__(256, 2) void tree_attn_kernel(TreeArgs a) {
 template <typename T, int D, int CB>
 __global__ __launch_bounds__(256) void tree_join_kernel(TreeArgs a) {
   constexpr int M = 32 * CB;
-  constexpr unsigned GROUPS = M / kJoinColumns;
-  const int H = a.c.kv_heads, col = (int)(blockIdx.x % GROUPS) * kJoinColumns, h = (int)(blockIdx.x / GROUPS % (unsigned)H);
+  constexpr unsigned GROUPS = M / kJoinColumns<D>;
+  const int H = a.c.kv_heads, col = (int)(blockIdx.x % GROUPS) * kJoinColumns<D>, h = (int)(blockIdx.x / GROUPS % (unsigned)H);
   const int item = (int)(blockIdx.x / GROUPS / (unsigned)H);
   const int b = item_owner(a.bt.starts, a.bt.rows, a.bt.batch, item, a.group, M, 1);
   const TreeSequence s = tree_sequence<M>(a, b);
@@ -499,7 +499,7 @@ static void launch_tree(const TreeArgs& a, const TreePlan& p, hipStream_t st) {
   const dim3 grid((unsigned)p.workgroups);
   if (a.c.codes == DQ_CODES_E4M3) hipLaunchKernelGGL((tree_attn_kernel<T, D, true, CB>), grid, dim3(256), 0, st, a);
   else hipLaunchKernelGGL((tree_attn_kernel<T, D, false, CB>), grid, dim3(256), 0, st, a);
-  hipLaunchKernelGGL((tree_join_kernel<T, D, CB>), dim3((unsigned)(p.items * a.c.kv_heads * (32 * CB / kJoinColumns))), dim3(256), 0, st, a);
+  hipLaunchKernelGGL((tree_join_kernel<T, D, CB>), dim3((unsigned)(p.items * a.c.kv_heads * (32 * CB / kJoinColumns<D>))), dim3(256), 0, st, a);
 }
 template <typename T, int D>
 static void launch_tree_cols(const TreeArgs& a, const TreePlan& p, hipStream_t st) {
