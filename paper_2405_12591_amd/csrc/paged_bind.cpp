@@ -301,7 +301,7 @@ PyObject* paged_append(PyObject*, PyObject* const* a, Py_ssize_t n) {
 
 PyObject* paged_read(PyObject*, PyObject* const* a, Py_ssize_t n) {
   // cache, index, first, seq_lens, out_starts, page_table, tail_slots, k_out, v_out, stream
-  return guarded(n, 11, [&]() -> PyObject* {
+  return guarded(n, 10, [&]() -> PyObject* {
     const dq_paged_cache* const cache = static_cast<const dq_paged_cache*>(address(a[0]));
     const int64_t index = integer(a[1]);
     const Heads k = packed_rows(cache, index, "k_out", a[7], cache->kv_heads, -1, true);
