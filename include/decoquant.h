@@ -594,7 +594,7 @@ int32_t dq_latent_append(const dq_latent_cache* cache, const dq_paged_batch* bat
                          int64_t latent_stride, const uint16_t* k_rot, int64_t k_rot_stride, const uint16_t* weight,
                          float eps, const dq_heads* q, const dq_heads* q_out, const dq_rotary* rot, void* hip_stream);
 
-/* Rows first[b] <= t < seq_lens[b] (first NULL: from 0) into out [batch->rows, latent_dim + rot_dim], row out_starts[b] + t -
+/* Rows first[b] <= t < seq_lens[b] (first NULL: from 0) into out [batch->rows, latent_dim + rot_dim] (rows that do not overlap), row out_starts[b] + t -
  * first[b]; tokens past row out_starts[b+1] - 1 are left out, rows of a page that does not exist are zeros with k_rot of NaN.
  * batch->starts is not used. */
 int32_t dq_latent_read(const dq_latent_cache* cache, const dq_paged_batch* batch, const int32_t* first,
@@ -611,7 +611,7 @@ size_t dq_latent_workspace_bytes(const dq_latent_cache* cache, int32_t batch, in
  *   q         [rows, q_heads, latent_dim + rot_dim];  out [rows, q_heads, latent_dim], not overlapping q
  *   seen      NULL, or u64 [rows] (with DQ_PAGED_CAUSAL, max_rows <= 64): of the sequence's own rows, row i sees
  *             the j-th where bit j is set (a tree of drafted tokens), of the tokens before them all
- *   softmax_scale  must be positive (1/sqrt of a head's expanded channels)
+ *   softmax_scale  must be positive and finite (1/sqrt of a head's expanded channels)
  *   max_rows  host bound on the rows of any sequence; further rows of that sequence may be left out (not written)
  *   max_seq_len    host bound on seq_lens (a guess does: it sizes the launch only, which orders the sums)
  * fp32 accumulation, one rounding of the result, probabilities in the rows' type for their product with c.  A row that sees no

@@ -286,7 +286,7 @@ extern "C" int32_t dq_expanded_attention(const dq_expanded* x, int32_t max_rows,
   if (!heads_ok(&x->q, false) || !heads_ok(&x->k, false) || !heads_ok(&x->v, false) || !heads_ok(&x->out, false)) return DQ_EINVAL;
   if (x->q.heads != x->k.heads || x->q.heads != x->v.heads || x->q.heads != x->out.heads) return DQ_EINVAL;
   if (!x->k_rot || ((uintptr_t)x->k_rot & 15) || x->k_rot_stride < 0 || (x->k_rot_stride & 7)) return DQ_EINVAL;
-  if (!workspace || ((uintptr_t)workspace & 15) || (flags & ~DQ_PAGED_CAUSAL) || softmax_scale != softmax_scale) return DQ_EINVAL;
+  if (!workspace || ((uintptr_t)workspace & 15) || (flags & ~DQ_PAGED_CAUSAL) || !scale_ok(softmax_scale)) return DQ_EINVAL;
   if (x->tokens >= kMostTokens || x->rows >= kMostTokens) return DQ_EINVAL;
   ExpandedPlan p;
   if (!expanded_plan(x->batch, x->rows, x->q.heads, x->head_dim, max_rows, max_seq_len, &p)) return DQ_EINVAL;

@@ -18,11 +18,18 @@ inline bool latent_batch_ok(const dq_paged_batch* b, const dq_latent_cache* c, b
   return !uses_starts || b->starts || b->rows == b->batch;
 }
 
+inline bool scale_ok(float scale) { return scale * 1.44269504088896340736f < INFINITY; }
+
 // ---- memory to LDS, past the registers ----
 typedef __attribute__((address_space(3))) char* LdsBytes;
 typedef __attribute__((address_space(3))) const u32x4* LdsPieces;
 typedef short s16x4 __attribute__((ext_vector_type(4)));
 typedef __attribute__((address_space(3))) s16x4* LdsQuads;
+
+// An address that all lanes have in common, in scalar registers (an asm operand's "s" is no more than a wish without it).
+__device__ __forceinline__ uint64_t in_scalars(const void* p) {
+  return (uint64_t)(uint32_t)__builtin_amdgcn_readfirstlane((int)((uint64_t)p >> 32)) << 32 | (uint32_t)__builtin_amdgcn_readfirstlane((int)(uint64_t)p);
+}
 
 // 64 pieces of 16 bytes, one behind the other from `lds` on: a lane's piece is at base + offset, or at `from`.  As instructions of
 // their own: the compiler waits for all such copies ahead of every LDS read, the ones for later tiles too.  Kernels count
@@ -30,10 +37,10 @@ typedef __attribute__((address_space(3))) s16x4* LdsQuads;
 // once: past the caches' order (rows that one workgroup reads: a cache of 378 MB in 80 us, 89 without).
 template <bool once = false> __device__ __forceinline__ void copy_to_lds(const uint16_t* base, uint32_t offset, uint32_t lds) {
   if constexpr (once) {
-    asm volatile("s_mov_b32 m0, %0\n\ts_nop 0\n\tglobal_load_lds_dwordx4 %1, %2 nt" ::"s"(__builtin_amdgcn_readfirstlane(lds)), "v"(offset), "s"(base) : "memory");
+    asm volatile("s_mov_b32 m0, %0\n\ts_nop 0\n\tglobal_load_lds_dwordx4 %1, %2 nt" ::"s"(__builtin_amdgcn_readfirstlane(lds)), "v"(offset), "s"(in_scalars(base)) : "memory");
     return;
   }
-  asm volatile("s_mov_b32 m0, %0\n\ts_nop 0\n\tglobal_load_lds_dwordx4 %1, %2" ::"s"(__builtin_amdgcn_readfirstlane(lds)), "v"(offset), "s"(base) : "memory");
+  asm volatile("s_mov_b32 m0, %0\n\ts_nop 0\n\tglobal_load_lds_dwordx4 %1, %2" ::"s"(__builtin_amdgcn_readfirstlane(lds)), "v"(offset), "s"(in_scalars(base)) : "memory");
 }
 __device__ __forceinline__ void copy_to_lds(const uint16_t* from, uint32_t lds) {
   asm volatile("s_mov_b32 m0, %0\n\ts_nop 0\n\tglobal_load_lds_dwordx4 %1, off" ::"s"(__builtin_amdgcn_readfirstlane(lds)), "v"(from) : "memory");

@@ -226,7 +226,9 @@ extern "C" int32_t dq_latent_append(const dq_latent_cache* cache, const dq_paged
 
 extern "C" int32_t dq_latent_read(const dq_latent_cache* cache, const dq_paged_batch* batch, const int32_t* first, const int32_t* out_starts,
                                   uint16_t* out, int64_t out_stride, void* hip_stream) {
-  if (!latent_cache_ok(cache) || !latent_batch_ok(batch, cache, false) || !out_starts || !rows_ok(out, out_stride)) return DQ_EINVAL;
+  if (!latent_cache_ok(cache) || !latent_batch_ok(batch, cache, false) || !out_starts || !rows_ok(out, out_stride) ||
+      out_stride < cache->latent_dim + cache->rot_dim)
+    return DQ_EINVAL;
   if (batch->rows == 0) return DQ_OK;
   const LatentReadArgs a = {*cache, *batch, first, out_starts, out, out_stride};
   const dim3 grid((unsigned)((batch->rows + 31l) / 32));

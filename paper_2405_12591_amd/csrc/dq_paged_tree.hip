@@ -526,7 +526,7 @@ extern "C" int32_t dq_paged_tree_attention(const dq_paged_cache* cache, const dq
   if (!paged_cache_ok(cache) || !paged_batch_ok(batch, cache, true)) return DQ_EINVAL;
   if (!heads_ok(q, false) || !heads_ok(k, false) || !heads_ok(v, false) || !heads_ok(out, false)) return DQ_EINVAL;
   if (q->heads != out->heads || k->heads != cache->kv_heads || v->heads != cache->kv_heads) return DQ_EINVAL;
-  if (!seen || ((uintptr_t)seen & 7) || !workspace || ((uintptr_t)workspace & 15) || flags || softmax_scale != softmax_scale) return DQ_EINVAL;
+  if (!seen || ((uintptr_t)seen & 7) || !workspace || ((uintptr_t)workspace & 15) || flags || !scale_ok(softmax_scale)) return DQ_EINVAL;
   if (window != 0 && window < kTreeRows) return DQ_EINVAL;
   TreePlan p;
   if (!tree_plan(cache, batch->batch, batch->rows, q->heads, max_rows, max_seq_len, &p)) return DQ_EINVAL;
