@@ -4,12 +4,12 @@ in csrc/paged_bind.cpp.  These operators serve: tensors that require gradients a
 from __future__ import annotations
 
 import ctypes as C
-from typing import Optional
+from typing import Optional, Sequence
 
 import torch
 
 from .binding import DQError, lib
-from .paged import _DTYPES, Rotary, _call, _module
+from .paged import _DTYPES, Rotary, _Workspace, _call, _module
 
 
 class _CLatent(C.Structure):
@@ -106,7 +106,7 @@ def _workspace_bytes(cache: LatentCache, batch: int, rows: int, q_heads: int, ma
 
 
 def latent_workspace(cache: LatentCache, batch: int, rows: int, q_heads: int, max_rows: int, max_seq_len: int) -> torch.Tensor:
-    """Workspace of latent_attention for these sizes."""
+    """Workspace of latent_attention for these sizes and all smaller ones with the same heads."""
     return torch.empty(_workspace_bytes(cache, batch, rows, q_heads, max_rows, max_seq_len), dtype=torch.uint8, device=cache.device)
 
 
@@ -147,3 +147,73 @@ def expanded_attention(q: torch.Tensor, k: torch.Tensor, k_rot: torch.Tensor, v:
     index = q.get_device()
     _call(_module.expanded_attention, index, index, q, k, k_rot, v, out, starts, kv_starts, max_rows, max_seq_len, softmax_scale, causal, workspace)
     return out
+
+
+class LatentKVLayer:
+    """One layer's latents, as PagedKVLayer is for keys and values of their own: `batch` sequences of up to max_tokens tokens, each with its own
+    pages, the lengths on the device.  Rows come packed, sequence by sequence (`starts`, int32 [batch + 1]; None: one row each);
+    the host tracks only a bound, which sizes the launches.  Replays of a captured step count on the device only: add their rows to
+    tokens_upper.  (Loops with a page allocator of their own call latent_append and latent_attention.)"""
+
+    def __init__(self, batch: int, heads: int, max_tokens: int, latent_dim: int = 512, rot_dim: int = 64, page_tokens: int = 64,
+                 dtype=torch.bfloat16, device="cuda:0"):
+        if min(batch, heads, max_tokens) < 1 or page_tokens not in (64, 128):
+            raise DQError("a layer has sequences, heads, room for tokens and pages of 64 or 128 tokens")
+        self.batch, self.heads, self.max_tokens = batch, heads, max_tokens
+        width = -(-max_tokens // page_tokens)
+        self.cache = alloc_latent_cache(batch * width, latent_dim, rot_dim, page_tokens, dtype, device)
+        self.page_table = torch.arange(batch * width, dtype=torch.int32, device=device).view(batch, width)
+        self.seq_lens = torch.zeros(batch, dtype=torch.int32, device=device)
+        self.tokens_upper = 0               # no sequence holds more tokens than this (host-side bound)
+        self._ws = _Workspace(device)
+
+    def append(self, latent: torch.Tensor, k_rot: torch.Tensor, starts: Optional[torch.Tensor] = None, max_rows: int = 1,
+               q: Optional[torch.Tensor] = None, q_out: Optional[torch.Tensor] = None, rotary: Optional[Rotary] = None,
+               positions: Optional[torch.Tensor] = None, weight: Optional[torch.Tensor] = None, eps: float = 1e-6):
+        """Append rows, no sequence more than max_rows; norm, rotation and the queries' channels as latent_append takes them.  Returns
+        q_out (None without q)."""
+        if starts is None and max_rows != 1:
+            raise DQError("several rows per sequence need starts")
+        if self.tokens_upper + max_rows > self.max_tokens:
+            # the bound may be ahead of the lengths (ragged rows); only then is it worth a look at them
+            self.tokens_upper = int(self.seq_lens.max())
+            if self.tokens_upper + max_rows > self.max_tokens:
+                raise DQError("the rows exceed the layer's %d tokens per sequence" % self.max_tokens)
+        new = 1 if starts is None else starts.diff()
+        self.seq_lens += new
+        try:
+            q = latent_append(self.cache, latent, k_rot, starts, self.seq_lens, self.page_table, q=q, q_out=q_out, rotary=rotary,
+                              positions=positions, weight=weight, eps=eps)
+        except Exception:                   # whatever it was, nothing was launched
+            self.seq_lens -= new
+            raise
+        self.tokens_upper += max_rows
+        return q
+
+    def attend(self, q: torch.Tensor, softmax_scale: float, starts: Optional[torch.Tensor] = None, max_rows: int = 1,
+               out: Optional[torch.Tensor] = None, causal: bool = True, seen: Optional[torch.Tensor] = None) -> torch.Tensor:
+        """Absorbed attention of the rows just appended, q [rows, heads, latent_dim + rot_dim] (latent_attention)."""
+        bound = min(self.tokens_upper, self.max_tokens)
+        ws = self._ws.of(_workspace_bytes(self.cache, self.batch, q.shape[0], self.heads, max_rows, bound))
+        return latent_attention(self.cache, q, starts, self.seq_lens, self.page_table, max_rows, bound, softmax_scale, ws, out=out, causal=causal,
+                                seen=seen)
+
+    def shorten(self, lengths: Sequence[int]) -> None:
+        """Drop tokens from the ends: sequence b keeps its first lengths[b] (host integers).  Rows stay where they are until others
+        take their places; a drafted path is kept by appending its rows again behind the shortened lengths.  Looks at the device's
+        lengths, so not for captures."""
+        have = [min(n, self.page_table.shape[1] * self.cache.page_tokens) for n in self.seq_lens.tolist()]
+        if len(lengths) != self.batch or any(not 0 <= n <= h for n, h in zip(lengths, have)):
+            raise DQError("shorten needs a length for every sequence, at most its tokens")
+        self.seq_lens.copy_(torch.tensor(list(lengths), dtype=torch.int32))
+        self.tokens_upper = max(lengths)
+
+    def read(self, lengths: Sequence[int]):
+        """The first lengths[b] rows (host integers) of every sequence b, packed, [sum, latent_dim + rot_dim], and their int32 starts: what a
+        prompt's keys and values are expanded from (expanded_attention's kv_starts)."""
+        if len(lengths) != self.batch or min(lengths) < 0:
+            raise DQError("read needs a length for every sequence, none negative")
+        c = self.cache
+        starts = torch.tensor([sum(lengths[:b]) for b in range(self.batch + 1)], dtype=torch.int32, device=c.device)
+        out = torch.zeros((sum(lengths), c.latent_dim + c.rot_dim), dtype=c.dtype, device=c.device)
+        return latent_read(c, None, self.seq_lens, starts, self.page_table, out), starts

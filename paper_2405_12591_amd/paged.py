@@ -269,12 +269,16 @@ def paged_attention(cache: PagedCache, q: torch.Tensor, starts: Optional[torch.T
     return out
 
 
-def paged_tree_workspace(cache: PagedCache, batch: int, rows: int, q_heads: int, max_rows: int, max_seq_len: int) -> torch.Tensor:
-    """Workspace of paged_tree_attention for these sizes and all smaller ones with the same heads."""
+def _tree_workspace_bytes(cache: PagedCache, batch: int, rows: int, q_heads: int, max_rows: int, max_seq_len: int) -> int:
     n = lib.dq_paged_tree_workspace_bytes(C.byref(cache.c), batch, rows, q_heads, max_rows, max_seq_len)
     if n == 0:
         raise DQError("dq_paged_tree_workspace_bytes rejected the arguments")
-    return torch.empty(n, dtype=torch.uint8, device=cache.device)
+    return n
+
+
+def paged_tree_workspace(cache: PagedCache, batch: int, rows: int, q_heads: int, max_rows: int, max_seq_len: int) -> torch.Tensor:
+    """Workspace of paged_tree_attention for these sizes and all smaller ones with the same heads."""
+    return torch.empty(_tree_workspace_bytes(cache, batch, rows, q_heads, max_rows, max_seq_len), dtype=torch.uint8, device=cache.device)
 
 
 def paged_tree_attention(cache: PagedCache, q: torch.Tensor, k: torch.Tensor, v: torch.Tensor, seen: torch.Tensor, starts: Optional[torch.Tensor],
@@ -293,6 +297,25 @@ def paged_tree_attention(cache: PagedCache, q: torch.Tensor, k: torch.Tensor, v:
     _call(_module.paged_tree_attention, index, cache._at, index, q, k, v, out, seen, starts, seq_lens, page_table, tail_slots, max_rows, max_seq_len,
           softmax_scale, window, workspace)
     return out
+
+
+class _Workspace:
+    """A layer's workspace for calls whose kernels need no zeros in it: grows with the calls, and stays where graphs were captured with it."""
+
+    def __init__(self, device):
+        self.device, self.ws, self.outgrown = device, None, []
+
+    def of(self, need: int) -> torch.Tensor:
+        if self.ws is not None and need <= self.ws.numel():
+            return self.ws
+        if torch.cuda.is_available() and torch.cuda.is_current_stream_capturing():
+            self.outgrown.append(torch.empty(need, dtype=torch.uint8, device=self.device))   # the captured call's own: its memory is the graph's
+            return self.outgrown[-1]
+        if self.ws is not None:
+            self.outgrown.append(self.ws)            # a captured graph may still work in it
+            need = max(need, 2 * self.ws.numel())    # (all that were outgrown together are smaller than the next one)
+        self.ws = torch.empty(need, dtype=torch.uint8, device=self.device)
+        return self.ws
 
 
 class PagedKVLayer:
@@ -314,6 +337,7 @@ class PagedKVLayer:
         self.seq_lens = torch.zeros(batch, dtype=torch.int32, device=device)
         self.tokens_upper = 0               # no sequence holds more tokens than this (host-side bound)
         self._ws, self._outgrown = None, []
+        self._tree_ws = _Workspace(device)
 
     def append(self, k: torch.Tensor, v: torch.Tensor, starts: Optional[torch.Tensor] = None, max_rows: int = 1,
                q: Optional[torch.Tensor] = None, rotary: Optional[Rotary] = None, positions: Optional[torch.Tensor] = None,
@@ -364,6 +388,16 @@ class PagedKVLayer:
             ws = self._make_room(max(q.shape[0], self._fits[0]), max(max_rows, self._fits[1]))
         return paged_attention(self.cache, q, starts, self.seq_lens, self.page_table, max_rows, bound, ws, out=out,
                                softmax_scale=softmax_scale, causal=causal, window=window)
+
+    def attend_tree(self, q: torch.Tensor, k: torch.Tensor, v: torch.Tensor, seen: torch.Tensor, starts: torch.Tensor, max_rows: int,
+                    out: Optional[torch.Tensor] = None, softmax_scale: float = 0.0, window: int = 0) -> torch.Tensor:
+        """Attention of drafted rows q [rows, q_heads, d] with keys and values k, v [rows, kv_heads, d] that are not appended: over the layer's
+        tokens and the drafted rows that `seen` names (paged_tree_attention).  The rows of the accepted path are appended
+        afterwards (k[path], v[path]); refused ones leave nothing to take back."""
+        bound = min(self.tokens_upper, self.max_tokens)
+        need = _tree_workspace_bytes(self.cache, self.batch, q.shape[0], self.q_heads, max_rows, bound)
+        return paged_tree_attention(self.cache, q, k, v, seen, starts, self.seq_lens, self.page_table, max_rows, bound, self._tree_ws.of(need),
+                                    out=out, softmax_scale=softmax_scale, window=window)
 
     def shorten(self, lengths: Sequence[int]) -> None:
         """Drop tokens from the ends: sequence b keeps its first lengths[b] (host integers; 0 empties it), after drafted tokens
