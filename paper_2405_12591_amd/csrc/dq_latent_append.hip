@@ -11,7 +11,7 @@ struct LatentAppendArgs {
   float eps;
   dq_heads q, q_out;               // heads == 0: none
   dq_rotary rot;                   // rot_dim == 0: none
-  int heads_per_group, head_groups;   // of the queries; 0 groups: none
+  int head_groups;                 // of the queries; 0: none
 };
 
 // Which sequence each of a workgroup's packed rows belongs to: every thread looks at its sequences, all at once, and names the rows
@@ -30,19 +30,25 @@ __device__ __forceinline__ void place_rows(const int32_t* starts, int rows, int 
   __syncthreads();
 }
 
-// A workgroup takes 256 / (ROT / 16) rows: their latents and shared key channels, or a group of their queries' heads.  A wave norms a row
-// of 512 channels at a time (two of 256), its rows asked for together; a thread then keeps 16 of the rotated channels of one row, whose
-// angles it forms once for all heads of its group.
+// Of 256 / (ROT / 16) rows a workgroup takes a quarter's latents and shared key channels, or the queries' heads of a group.  A wave norms four
+// rows of 512 channels (eight of 256), all asked for together (all the rows' latents in one workgroup, four times as many after one another: 11.7 us
+// for 128 rows of 128 heads where this takes 6.1, 10.5 and 5.9 for 16 rows).  A thread keeps 16 of the rotated channels of one row, whose angles it
+// forms once for all heads of its group.
+constexpr int kLatentParts = 4;
+constexpr int kTurnedHeads = 8;   // of a group (28 thousand rows of 16 heads in prompts: 47 us, 51 with four, 52 with sixteen; 16 rows: 5.9, 5.5 with four)
 template <typename T, int R, bool INTERLEAVED>
 __global__ __launch_bounds__(256) void latent_append_kernel(LatentAppendArgs a) {
   constexpr int ROT = R == 512 ? 64 : 32, W = R + ROT, LANES = ROT / 16, ROWS = 256 / LANES;
-  constexpr int AT_ONCE = 512 / R, PASSES = ROWS / (4 * AT_ONCE), GROUP = 8;   // rows of a wave and pass, passes, those asked for together
+  constexpr int AT_ONCE = 512 / R, PASSES = ROWS / kLatentParts / (4 * AT_ONCE);   // rows of a wave and pass, passes
   __shared__ RowPlace s_place[ROWS];
   __shared__ int s_token[ROWS];
   __shared__ long s_row[ROWS];     // of the cache, or -1
   __shared__ bool s_bad[ROWS];
   const int tid = threadIdx.x, lane = tid & 63, wave = tid >> 6, P = a.c.page_tokens;
-  const int group = (int)(blockIdx.x % (unsigned)(a.head_groups + 1)), first = (int)(blockIdx.x / (unsigned)(a.head_groups + 1)) * ROWS;
+  const int groups = a.head_groups + kLatentParts, group = (int)(blockIdx.x % (unsigned)groups), first = (int)(blockIdx.x / (unsigned)groups) * ROWS;
+  const bool latents = group < kLatentParts;
+  const int row0 = group * (ROWS / kLatentParts);         // (latents) the first of its rows here
+  if (latents && first + row0 >= a.bt.rows) return;
   place_rows(a.bt.starts, a.bt.rows, a.bt.batch, first, s_place);
   if (tid < ROWS) {
     const RowPlace at = s_place[tid];
@@ -51,7 +57,7 @@ __global__ __launch_bounds__(256) void latent_append_kernel(LatentAppendArgs a) 
     if (at.b >= 0) {
       const Sequence s = sequence_of(a.bt, P, at.b);
       token = s.old + at.i;
-      if (group == 0 && token >= 0 && token < s.len) {
+      if (latents && token >= 0 && token < s.len) {
         const int page = a.bt.page_table[(long)at.b * a.bt.table_stride + token / P];
         if (page >= 0 && page < a.c.pages) row = (long)page * P + token % P;
       }
@@ -62,63 +68,62 @@ __global__ __launch_bounds__(256) void latent_append_kernel(LatentAppendArgs a) 
   }
   __syncthreads();
 
-  if (group == 0) {
+  if (latents) {
     const int piece = lane % (R / 8);                     // 8 channels
     u32x4 w = {};
     if (a.weight) w = *reinterpret_cast<const u32x4*>(a.weight + 8 * piece);
-    for (int g = 0; g < PASSES; g += GROUP) {
-      u32x4 v[GROUP];
+    u32x4 v[PASSES];
 #pragma unroll
-      for (int i = 0; i < GROUP; ++i) {
-        const int r = ((g + i) * 4 + wave) * AT_ONCE + lane / (R / 8);
-        v[i] = s_row[r] >= 0 ? *reinterpret_cast<const u32x4*>(a.latent + (long)(first + r) * a.latent_stride + 8 * piece) : u32x4{0, 0, 0, 0};
+    for (int i = 0; i < PASSES; ++i) {
+      const int r = row0 + (i * 4 + wave) * AT_ONCE + lane / (R / 8);
+      v[i] = s_row[r] >= 0 ? *reinterpret_cast<const u32x4*>(a.latent + (long)(first + r) * a.latent_stride + 8 * piece) : u32x4{0, 0, 0, 0};
+    }
+#pragma unroll
+    for (int i = 0; i < PASSES; ++i) {
+      const int r = row0 + (i * 4 + wave) * AT_ONCE + lane / (R / 8);
+      if (a.weight) {
+        float x[8], y[8], sum = 0.f;
+        unpack8<T>(v[i], x);
+        unpack8<T>(w, y);
+#pragma unroll
+        for (int e = 0; e < 8; ++e) sum = __builtin_fmaf(x[e], x[e], sum);
+        sum = row_reduce<16>(sum, [](float p, float q) { return p + q; });
+        sum += __shfl_xor(sum, 16);
+        if constexpr (R == 512) sum += __shfl_xor(sum, 32);
+        const float f = 1.0f / sqrtf(sum * (1.0f / R) + a.eps);
+#pragma unroll
+        for (int e = 0; e < 8; ++e) x[e] = x[e] * f * y[e];
+        v[i] = pack8<T>(x);
       }
+      constexpr uint32_t kExp = __is_same(T, __bf16) ? 0x7F80u : 0x7C00u;
+      bool bad = false;
 #pragma unroll
-      for (int i = 0; i < GROUP; ++i) {
-        const int r = ((g + i) * 4 + wave) * AT_ONCE + lane / (R / 8);
-        if (a.weight) {
-          float x[8], y[8], sum = 0.f;
-          unpack8<T>(v[i], x);
-          unpack8<T>(w, y);
-#pragma unroll
-          for (int e = 0; e < 8; ++e) sum = __builtin_fmaf(x[e], x[e], sum);
-          sum = row_reduce<16>(sum, [](float p, float q) { return p + q; });
-          sum += __shfl_xor(sum, 16);
-          if constexpr (R == 512) sum += __shfl_xor(sum, 32);
-          const float f = 1.0f / sqrtf(sum * (1.0f / R) + a.eps);
-#pragma unroll
-          for (int e = 0; e < 8; ++e) x[e] = x[e] * f * y[e];
-          v[i] = pack8<T>(x);
-        }
-        constexpr uint32_t kExp = __is_same(T, __bf16) ? 0x7F80u : 0x7C00u;
-        bool bad = false;
-#pragma unroll
-        for (int e = 0; e < 4; ++e) bad |= (v[i][e] & kExp) == kExp || (v[i][e] >> 16 & kExp) == kExp;
-        const uint64_t any = __ballot(bad) >> (R == 512 ? 0 : lane & 32) & (R == 512 ? ~0ull : 0xFFFFFFFFull);
-        if (any) v[i] = u32x4{0, 0, 0, 0};
-        const long row = s_row[r];
-        if (row < 0) continue;
-        *reinterpret_cast<u32x4*>(a.c.rows + row * W + 8 * piece) = v[i];
-        if (any && piece == 0) s_bad[r] = true;
-      }
+      for (int e = 0; e < 4; ++e) bad |= (v[i][e] & kExp) == kExp || (v[i][e] >> 16 & kExp) == kExp;
+      const uint64_t any = __ballot(bad) >> (R == 512 ? 0 : lane & 32) & (R == 512 ? ~0ull : 0xFFFFFFFFull);
+      if (any) v[i] = u32x4{0, 0, 0, 0};
+      const long row = s_row[r];
+      if (row < 0) continue;
+      *reinterpret_cast<u32x4*>(a.c.rows + row * W + 8 * piece) = v[i];
+      if (any && piece == 0) s_bad[r] = true;
     }
     __syncthreads();
   }
 
   const int unit = tid % LANES, r = tid / LANES;
-  const bool live = s_place[r].b >= 0 && (group > 0 || s_row[r] >= 0);
+  const bool live = latents ? r >= row0 && r < row0 + ROWS / kLatentParts && s_row[r] >= 0 : s_place[r].b >= 0;
+  if (!__any(live)) return;
   RowLayout l = row_layout(unit, a.rot.rot_dim, INTERLEAVED);
   if (!live) l.pair0 = -1;
   UnitTurns ut;
   load_turns(a.rot, l, first + r, s_token[r], ut);
   u32x4 v[2] = {};
-  const int h0 = (group - 1) * a.heads_per_group, h1 = min(h0 + a.heads_per_group, a.q.heads);
+  const int h0 = (group - kLatentParts) * kTurnedHeads, h1 = min(h0 + kTurnedHeads, a.q.heads);
   const uint16_t* const q = a.q.data + (long)(first + r) * a.q.token_stride;
   const uint16_t* const k = a.k_rot + (long)(first + r) * a.k_rot_stride;
-  if (live) load_unit(v, group ? q + h0 * a.q.head_stride : k, l);
+  if (live) load_unit(v, latents ? k : q + h0 * a.q.head_stride, l);
   float cs[8], sn[8];
   make_turns(l, ut, cs, sn);
-  if (group) {
+  if (!latents) {
     rotate_row<T, LANES, INTERLEAVED>(v, q, a.q_out.data + (long)(first + r) * a.q_out.token_stride, a.q.head_stride, a.q_out.head_stride, h0, h1, live,
                                       l, nullptr, 0.f, 0.f, cs, sn);
   } else if (live) {
@@ -209,14 +214,10 @@ extern "C" int32_t dq_latent_append(const dq_latent_cache* cache, const dq_paged
   if (rot) a.rot = *rot;
   const int rows_per_block = 256 / (cache->rot_dim / 16);
   const long blocks = (batch->rows + (long)rows_per_block - 1) / rows_per_block;
-  // Heads that share a row's angles: eight where the rows alone fill the chip, fewer where they do not.
-  int per = 8;
-  while (q && per > 1 && blocks * ((q->heads + (long)per - 1) / per) < 1024) per /= 2;
-  const long groups = q ? (q->heads + (long)per - 1) / per : 0;
-  if (blocks * (groups + 1) >= kMaxThreads / 256) return DQ_EINVAL;
-  a.heads_per_group = per;
+  const long groups = q ? (q->heads + kTurnedHeads - 1l) / kTurnedHeads : 0, workgroups = blocks * (groups + kLatentParts);
+  if (workgroups >= kMaxThreads / 256) return DQ_EINVAL;
   a.head_groups = (int)groups;
-  const dim3 grid((unsigned)(blocks * (groups + 1)));
+  const dim3 grid((unsigned)workgroups);
   hipStream_t st = (hipStream_t)hip_stream;
   if (cache->dtype == DQ_BF16) { if (cache->latent_dim == 512) launch_latent_append<__bf16, 512>(a, grid, st); else launch_latent_append<__bf16, 256>(a, grid, st); }
   else { if (cache->latent_dim == 512) launch_latent_append<_Float16, 512>(a, grid, st); else launch_latent_append<_Float16, 256>(a, grid, st); }
