@@ -106,7 +106,9 @@ template <typename F> __device__ __forceinline__ long line_total(int batch, F we
   }
   return wave_uniform(wave_sum(mine));
 }
-__device__ __forceinline__ long line_quota(const Line& l, long total) { return max((total + l.workgroups - 1) / l.workgroups, (long)l.min_quota); }
+// a / b, neither negative: in 32 bits where they do (b positive).
+__device__ __forceinline__ long over(long a, long b) { return (a | b) >> 32 ? a / b : (long)((uint32_t)a / (uint32_t)b); }
+__device__ __forceinline__ long line_quota(const Line& l, long total) { return max(over(total + l.workgroups - 1, l.workgroups), (long)l.min_quota); }
 
 // The sequence that holds place `at` of the line (at < total), and the place at which it begins.
 template <typename F> __device__ __forceinline__ int line_owner(int batch, long at, F weight_of, long& begin) {
@@ -135,11 +137,52 @@ template <typename F> __device__ __forceinline__ int line_owner(int batch, long 
   return batch;
 }
 
+// A sequence a lane and 31 bits of places, as nearly always: each one's places and their running sum, looked at once.  false: the line is longer.
+template <typename F> __device__ __forceinline__ bool short_line(int batch, F weight_of, int& mine, int& upto) {
+  if (batch > 64) return false;
+  const int lane = threadIdx.x & 63;
+  const Weight w = lane < batch ? weight_of(lane) : Weight{0, 0};
+  const long places = (long)w.units * w.tiles;
+  if (__any(places >= 1l << 24)) return false;
+  mine = upto = (int)places;
+  for (int o = 1; o < 64; o *= 2) {
+    const int x = __shfl_up(upto, o);
+    if (lane >= o) upto += x;
+  }
+  return true;
+}
+
+// A workgroup's places of the line, [at, end), and the sequence that holds the first of them, which begins at place `begin`; false: it has none.
+struct LineStart {
+  long at, end, begin;
+  int b;
+};
+template <typename F> __device__ __forceinline__ bool line_start(const Line& l, int batch, F weight_of, LineStart& s) {
+  int mine, upto;
+  if (short_line(batch, weight_of, mine, upto)) {
+    const uint32_t total = (uint32_t)__builtin_amdgcn_readlane(upto, 63), quota = (uint32_t)line_quota(l, total), at = blockIdx.x * quota;
+    if (at >= total) return false;
+    s.at = at;
+    s.end = min(at + quota, total);
+    s.b = __builtin_ctzll(__ballot((uint32_t)upto > at));
+    s.begin = (uint32_t)__builtin_amdgcn_readlane(upto - mine, s.b);
+    return true;
+  }
+  const long total = line_total(batch, weight_of), quota = line_quota(l, total);
+  s.at = (long)blockIdx.x * quota;
+  s.end = min(s.at + quota, total);
+  if (s.at >= s.end) return false;
+  s.b = line_owner(batch, s.at, weight_of, s.begin);
+  return true;
+}
+
 // The line's length, and its places before sequence b.
 struct LineSums {
   long total, before;
 };
 template <typename F> __device__ __forceinline__ LineSums line_sums(int batch, int b, F weight_of) {
+  int mine, upto;
+  if (short_line(batch, weight_of, mine, upto)) return {__builtin_amdgcn_readlane(upto, 63), __builtin_amdgcn_readlane(upto - mine, __builtin_amdgcn_readfirstlane(b))};
   long all = 0, lower = 0;
   for (int i = threadIdx.x & 63; i < batch; i += 64) {
     const Weight w = weight_of(i);
@@ -154,7 +197,7 @@ template <typename F> __device__ __forceinline__ LineSums line_sums(int batch, i
 struct Pieces {
   long first, last;
 };
-__device__ __forceinline__ Pieces pieces_of(long begin, int tiles, long quota) { return {begin / quota, (begin + tiles - 1) / quota}; }
+__device__ __forceinline__ Pieces pieces_of(long begin, int tiles, long quota) { return {over(begin, quota), over(begin + tiles - 1, quota)}; }
 __device__ __forceinline__ long slot_of(const Pieces& p, long w) { return w == p.first ? 2 * w + 1 : 2 * w; }
 
 // Joins the pieces of kJoinColumns<D> columns (those below `valid`): a wave a column where there are few pieces, four waves a column, which take

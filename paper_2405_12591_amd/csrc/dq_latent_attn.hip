@@ -15,12 +15,16 @@ struct LatentArgs {
 };
 
 constexpr int kLatentTile = 32;   // tokens
+// Tiles that are a place of the line: one, which all waves work on, or, where each wave works on tiles of its own, one for each (pieces cut
+// between them leave waves idle, twice in a workgroup: 64 sequences of 5056 tokens, 16 columns, 90 us where this takes 81).
+template <int M> constexpr int kLatentRound = M == 16 ? 4 : 1;
 
 template <int M>
 __device__ __forceinline__ Weight latent_weight(const LatentArgs& a, int b) {
   const Sequence s = sequence_of(a.bt, a.c.page_tokens, b);
   const int n = min(s.n, a.max_rows);
-  return {n ? (int)(((long)n * a.q.heads + M - 1) / M) : 0, max((s.len + kLatentTile - 1) / kLatentTile, 1)};
+  constexpr int PLACE = kLatentTile * kLatentRound<M>;
+  return {n ? (int)(((long)n * a.q.heads + M - 1) / M) : 0, max((int)((s.len + (long)PLACE - 1) / PLACE), 1)};
 }
 
 template <typename T, int R, int CB>
@@ -56,12 +60,11 @@ __global__ __launch_bounds__((64 * LatentShape<T, R, CB>::WAVES), (LatentShape<T
   const int tid = threadIdx.x, lane = tid & 63, wave = __builtin_amdgcn_readfirstlane(tid >> 6), r32 = lane & 31, hl = lane >> 5;
   const int cb = wave / CH, chs = wave % CH, H = a.q.heads, P = a.c.page_tokens;
   const auto weight_of = [&](int b) { return latent_weight<M>(a, b); };
-  const long total = line_total(a.bt.batch, weight_of), quota = line_quota(a.line, total);
-  long at = (long)blockIdx.x * quota;
-  const long end = min(at + quota, total);
-  if (at >= end) return;
-  long begin;
-  int b = line_owner(a.bt.batch, at, weight_of, begin);
+  LineStart here;
+  if (!line_start(a.line, a.bt.batch, weight_of, here)) return;
+  const long end = here.end;
+  long at = here.at, begin = here.begin;
+  int b = here.b;
 
   // ---- places in LDS ----
   // A row's 16-byte pieces are exchanged within runs of 16 by bits of the token, so that the 16 lanes that read one piece of 16 tokens'
@@ -89,7 +92,7 @@ __global__ __launch_bounds__((64 * LatentShape<T, R, CB>::WAVES), (LatentShape<T
     const Sequence s = sequence_of_wave(a.bt, P, b);
     const Weight wt = weight_of(b);
     const int n = min(s.n, a.max_rows), len = s.len, before = s.old;
-    const int unit = __builtin_amdgcn_readfirstlane((int)((at - begin) / wt.tiles)), tiles = __builtin_amdgcn_readfirstlane(wt.tiles);
+    const int unit = __builtin_amdgcn_readfirstlane((int)over(at - begin, wt.tiles)), tiles = __builtin_amdgcn_readfirstlane(wt.tiles);
     const int t0 = __builtin_amdgcn_readfirstlane((int)(at - begin - (long)unit * tiles)), t1 = (int)min((long)tiles, t0 + (end - at));
     const int pairs = n * H, first = unit * M;
     const int rows_lo = first / H, rows_hi = min(first + M - 1, pairs - 1) / H;
@@ -336,19 +339,18 @@ __global__ __launch_bounds__(256, 1) void latent_narrow_kernel(LatentArgs a) {
   struct Tile { char c[TT * R * 2], r[TT * ROT * 2]; };
   union Space {
     Tile tile[WAVES];
-    float o[WAVES][M][R + 1];
+    float o[WAVES][M][R + 4];
   };
   __shared__ __align__(1024) Space s_space;
   __shared__ float s_m[WAVES][M], s_l[WAVES][M];
   const int tid = threadIdx.x, lane = tid & 63, wave = __builtin_amdgcn_readfirstlane(tid >> 6), col = lane & 15, G = lane >> 4;
   const int H = a.q.heads, P = a.c.page_tokens;
   const auto weight_of = [&](int b) { return latent_weight<M>(a, b); };
-  const long total = line_total(a.bt.batch, weight_of), quota = line_quota(a.line, total);
-  long at = (long)blockIdx.x * quota;
-  const long end = min(at + quota, total);
-  if (at >= end) return;
-  long begin;
-  int b = line_owner(a.bt.batch, at, weight_of, begin);
+  LineStart here;
+  if (!line_start(a.line, a.bt.batch, weight_of, here)) return;
+  const long end = here.end;
+  long at = here.at, begin = here.begin;
+  int b = here.b;
 
   // Pieces of a row are exchanged by bits of the token, so that 16 lanes that read one piece of 16 rows (keys: tokens 8 i + 0..3), and 32 that
   // read two pieces of eight (values), touch all banks.
@@ -366,8 +368,8 @@ __global__ __launch_bounds__(256, 1) void latent_narrow_kernel(LatentArgs a) {
     const Sequence s = sequence_of_wave(a.bt, P, b);
     const Weight wt = weight_of(b);
     const int n = min(s.n, a.max_rows), len = s.len, before = s.old;
-    const int unit = __builtin_amdgcn_readfirstlane((int)((at - begin) / wt.tiles)), tiles = __builtin_amdgcn_readfirstlane(wt.tiles);
-    const int t0 = __builtin_amdgcn_readfirstlane((int)(at - begin - (long)unit * tiles)), t1 = (int)min((long)tiles, t0 + (end - at));
+    const int unit = __builtin_amdgcn_readfirstlane((int)over(at - begin, wt.tiles)), tiles = __builtin_amdgcn_readfirstlane(wt.tiles);
+    const int p0 = __builtin_amdgcn_readfirstlane((int)(at - begin - (long)unit * tiles)), p1 = (int)min((long)tiles, p0 + (end - at));
     const int pairs = n * H, first = unit * M;
     const int my_pair = min(first + col, pairs - 1), my_row = my_pair / H;
     const uint16_t* const q_row = a.q.data + (long)(s.row0 + my_row) * a.q.token_stride + (long)(my_pair % H) * a.q.head_stride + 8 * G;
@@ -382,7 +384,7 @@ __global__ __launch_bounds__(256, 1) void latent_narrow_kernel(LatentArgs a) {
       if (s.n < 64) bits &= (1ull << s.n) - 1;
       see_hi = all_hi = min(before, len);
     }
-    const int t_end = min(t1, (len + TT - 1) / TT);
+    const int t0 = WAVES * p0, t_end = (int)min((long)WAVES * p1, (long)(len + TT - 1) / TT);
     f32x4 o[NCT];
 #pragma unroll
     for (int ct = 0; ct < NCT; ++ct) o[ct] = f32x4{0.f, 0.f, 0.f, 0.f};
@@ -485,40 +487,43 @@ __global__ __launch_bounds__(256, 1) void latent_narrow_kernel(LatentArgs a) {
     l += __shfl_xor(l, 32);
     __syncthreads();                                      // all tiles have been read
 #pragma unroll
-    for (int ct = 0; ct < NCT; ++ct)
-#pragma unroll
-      for (int e = 0; e < 4; ++e) s_space.o[wave][col][16 * ct + 4 * G + e] = o[ct][e];
+    for (int ct = 0; ct < NCT; ++ct) *reinterpret_cast<f32x4*>(&s_space.o[wave][col][16 * ct + 4 * G]) = o[ct];
     if (G == 0) { s_m[wave][col] = m; s_l[wave][col] = l; }
     __syncthreads();
-    const bool whole = t0 == 0 && t1 == tiles;
-    const long slot = 2l * blockIdx.x + (t0 == 0);
+    const bool whole = p0 == 0 && p1 == tiles;
+    const long slot = 2l * blockIdx.x + (p0 == 0);
     const int cols = min(pairs - first, M);
-    for (int idx = 2 * tid; idx < cols * R; idx += 512) {
-      const int c = idx / R, ch = idx % R;
-      float top = s_m[0][c];
+#pragma unroll
+    for (int i = 0; i < M / WAVES; ++i) {
+      const int c = i * WAVES + wave;
+      if (c >= cols) break;
+      float top = s_m[0][c], f[WAVES], ll = 0.f;
 #pragma unroll
       for (int w = 1; w < WAVES; ++w) top = fmaxf(top, s_m[w][c]);
-      const float base = top == -INFINITY ? 0.f : top;
-      float x = 0.f, y = 0.f, ll = 0.f;
 #pragma unroll
       for (int w = 0; w < WAVES; ++w) {
-        const float f = __builtin_amdgcn_exp2f(s_m[w][c] - base);
-        x = __builtin_fmaf(s_space.o[w][c][ch], f, x);
-        y = __builtin_fmaf(s_space.o[w][c][ch + 1], f, y);
-        ll = __builtin_fmaf(s_l[w][c], f, ll);
+        f[w] = __builtin_amdgcn_exp2f(s_m[w][c] - (top == -INFINITY ? 0.f : top));
+        ll = __builtin_fmaf(s_l[w][c], f[w], ll);
       }
-      if (whole) {
-        const float inv = ll == 0.f ? 0.f : 1.f / ll;
-        const int row = (first + c) / H;
-        uint16_t* const dst = a.out.data + (long)(s.row0 + row) * a.out.token_stride + (long)(first + c - row * H) * a.out.head_stride;
-        *reinterpret_cast<uint32_t*>(dst + ch) = pack2<T>(x * inv, y * inv);
-      } else {
-        *reinterpret_cast<f32x2*>(a.o + (slot * M + c) * R + ch) = f32x2{x, y};
-        if (ch == 0) *reinterpret_cast<f32x2*>(a.ml + 2 * (slot * M + c)) = f32x2{top, ll};
+      const int row = (first + c) / H;
+      uint16_t* const dst = a.out.data + (long)(s.row0 + row) * a.out.token_stride + (long)(first + c - row * H) * a.out.head_stride;
+      const float inv = ll == 0.f ? 0.f : 1.f / ll;
+#pragma unroll
+      for (int ch = 4 * lane; ch < R; ch += 256) {
+        f32x4 x = {0.f, 0.f, 0.f, 0.f};
+#pragma unroll
+        for (int w = 0; w < WAVES; ++w) {
+          const f32x4 y = *reinterpret_cast<const f32x4*>(&s_space.o[w][c][ch]);
+#pragma unroll
+          for (int e = 0; e < 4; ++e) x[e] = __builtin_fmaf(y[e], f[w], x[e]);
+        }
+        if (whole) *reinterpret_cast<u32x2*>(dst + ch) = u32x2{pack2<T>(x[0] * inv, x[1] * inv), pack2<T>(x[2] * inv, x[3] * inv)};
+        else *reinterpret_cast<f32x4*>(a.o + (slot * M + c) * R + ch) = x;
       }
+      if (!whole && lane == 0) *reinterpret_cast<f32x2*>(a.ml + 2 * (slot * M + c)) = f32x2{top, ll};
     }
-    at += t1 - t0;
-    if (t1 == tiles && unit == __builtin_amdgcn_readfirstlane(wt.units) - 1) {   // the next sequence that has rows
+    at += p1 - p0;
+    if (p1 == tiles && unit == __builtin_amdgcn_readfirstlane(wt.units) - 1) {   // the next sequence that has rows
       begin = at;
       do ++b;
       while (at < end && weight_of(b).units == 0);
@@ -619,7 +624,7 @@ extern "C" int32_t dq_latent_attention(const dq_latent_cache* cache, const dq_pa
   a.max_rows = max_rows;
   a.causal = (flags & DQ_PAGED_CAUSAL) ? 1 : 0;
   a.scale_log2 = fmaxf(softmax_scale * 1.44269504088896340736f, 1e-37f);
-  a.line = {(int)p.workgroups, p.cols == 16 ? 4 : 2};   // four waves with a tile each; all waves with one
+  a.line = {(int)p.workgroups, p.cols == 16 ? 1 : 2};
   a.o = reinterpret_cast<float*>(workspace);
   a.ml = a.o + 2 * p.workgroups * p.cols * cache->latent_dim;
   hipStream_t st = (hipStream_t)hip_stream;

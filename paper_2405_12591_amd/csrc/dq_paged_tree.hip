@@ -63,12 +63,11 @@ __global__ __launch_bounds__(256, 2) void tree_attn_kernel(TreeArgs a) {
   const int tid = threadIdx.x, lane = tid & 63, wave = __builtin_amdgcn_readfirstlane(tid >> 6), r32 = lane & 31, hl = lane >> 5;
   const int cb = wave % CB, tg = wave / CB, H = a.c.kv_heads, P = a.c.page_tokens, runs = P / kPagedTile;
   const auto weight_of = [&](int b) { return tree_sequence<M>(a, b).w; };
-  const long total = line_total(a.bt.batch, weight_of), quota = line_quota(a.line, total);
-  long at = (long)blockIdx.x * quota;
-  const long end = min(at + quota, total);
-  if (at >= end) return;
-  long begin;
-  int b = line_owner(a.bt.batch, at, weight_of, begin);
+  LineStart here;
+  if (!line_start(a.line, a.bt.batch, weight_of, here)) return;
+  const long end = here.end;
+  long at = here.at, begin = here.begin;
+  int b = here.b;
   const int k_row = (r32 & 3) | (r32 >> 3) << 2 | (r32 >> 2 & 1) << 4;   // + 32 tt: the token of this lane's row
 
   while (at < end) {
@@ -76,7 +75,7 @@ __global__ __launch_bounds__(256, 2) void tree_attn_kernel(TreeArgs a) {
     auto uniform = [](int v) { return __builtin_amdgcn_readfirstlane(v); };
     s.row0 = uniform(s.row0); s.n = uniform(s.n); s.place0 = uniform(s.place0); s.len = uniform(s.len); s.first_tile = uniform(s.first_tile);
     const int n = s.n, len = s.len, tiles = uniform(s.w.tiles), units = uniform(s.w.units), col_tiles = units / H;
-    const int unit = uniform((int)((at - begin) / tiles)), h = unit / col_tiles, first = unit % col_tiles * M;
+    const int unit = uniform((int)over(at - begin, tiles)), h = unit / col_tiles, first = unit % col_tiles * M;
     const int t0 = uniform((int)(at - begin - (long)unit * tiles)), t1 = (int)min((long)tiles, t0 + (end - at));
     const int pairs = n * a.group;
     const int my_pair = min(first + cb * 32 + r32, pairs - 1), my_row = my_pair / a.group;

@@ -3,7 +3,7 @@ import pytest
 import torch
 
 import paper_2405_12591_amd as dq
-from latent_util import FORMS, Latents, check, normal, starts_of
+from latent_util import FORMS, Latents, attend64, check, normal, starts_of, tolerance
 from paged_util import DEV, HALF, heads64, ints, rotate_tolerance
 
 pytestmark = pytest.mark.gpu
@@ -77,6 +77,25 @@ def test_long_caches_and_many_sequences(latent):
         want = x.want(q, counts, 0.05)
         for max_len in (max(lens), 1, 100000):                      # the bound sizes the launch only
             check(x.attend(q.to(DEV), counts, 0.05, max_len=max_len), *want, "bound %d" % max_len)
+
+
+def test_a_line_of_more_than_24_bits():
+    """2^24 tiles and units in one sequence: 8 million tokens over 64 pages that the table names again and again, 8192 columns."""
+    gen = torch.Generator().manual_seed(10)
+    x = Latents([4096], 256, torch.float16, 64, gen)
+    n, rows, heads = 1 << 23, 64, 128
+    table = x.table[:, :64].repeat_interleave(2048, 1)
+    x.lens = [n]
+    q = normal((rows, heads, 288), torch.float16, gen)
+    got = x.attend(q.to(DEV), [rows], 0.05, causal=False, table=table).double().cpu()
+    some = slice(0, 64, 21)
+    see = torch.ones(4, 4096, dtype=torch.bool)
+    o, size, ds = attend64(q[some], x.rows[0], x.rows[0][:, :256], see, 0.05)
+    # on top of what shorter caches may be off by: a workgroup's 2^16 tiles are 2^17 additions to a result, four roundings each, and 2^19
+    # to a lane's sum of probabilities, at half a step each
+    v_max = float(x.rows[0][:, :256].double().abs().max())
+    tol = tolerance(o, size, ds, v_max, 4096, torch.float16) + size * (2.0 ** -5 + 2.0 ** -5)
+    assert bool(((got[some] - o).abs() <= tol).all())
 
 
 def test_rows_past_the_bound_are_left():
