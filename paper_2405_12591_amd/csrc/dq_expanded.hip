@@ -30,7 +30,8 @@ __device__ __forceinline__ ExpandedSequence expanded_sequence(const dq_expanded&
 
 // One workgroup of four waves per (tile of 128 rows, head, split), 32 rows a wave.  Tiles of 64 tokens are copied to LDS past the registers, a
 // tile ahead; scores are formed transposed, as in the kernel over latents, and the values' operand comes from rows as they lie by
-// transposing LDS reads.
+// transposing LDS reads.  Four prompts of 3500 to 4096 with 32 heads of 128 + 64, 606 GFLOP: 640 us, 947 TFLOP/s, 70 % of a large product's rate;
+// between the products every wave has its exponentials to form.
 template <typename T, int D>
 __global__ __launch_bounds__(256, 2) void expanded_attn_kernel(ExpandedArgs a) {
   constexpr int ROT = D / 2, W = D + ROT, TT = kExpandedTile, M = kExpandedRows, NK = D / 16, NR = ROT / 16, NCT = D / 32;

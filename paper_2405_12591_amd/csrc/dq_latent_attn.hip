@@ -46,8 +46,9 @@ __device__ __forceinline__ uint32_t bits_from(uint64_t bits, int at) {
 // both.  CH waves share a block of 32 columns: each multiplies its part of the channels, S^T = [c | k_rot] q^T, hands its sums to the
 // others through LDS, and then holds its part of O^T += c^T P^T, whose left operand comes from the same rows by transposing reads.  (So a
 // wave's queries and results fit 256 registers and two waves a SIMD hide each other's latencies: with all channels' queries in one wave,
-// alone on its SIMD, 16 sequences of 14 thousand tokens with 128 heads took 178 us.)  Key rows are taken in the order that leaves a lane
-// the probabilities of 8 neighbouring tokens twice, the right operand of the second product.
+// alone on its SIMD, 16 sequences of 14 thousand tokens with 128 heads took 178 us where this takes 104.)  Key rows are taken in the order that
+// leaves a lane the probabilities of 8 neighbouring tokens twice, the right operand of the second product.  Bound by matrix instructions: those
+// 64 GFLOP are 47 us at the rate of a large product; 16 us go into the pieces' writing (67 MB), 16 more into their join.
 template <typename T, int R, int CB>
 __global__ __launch_bounds__((64 * LatentShape<T, R, CB>::WAVES), (LatentShape<T, R, CB>::WAVES / 4)) void latent_attn_kernel(LatentArgs a) {
   typedef LatentShape<T, R, CB> Shape;
@@ -271,7 +272,7 @@ __global__ __launch_bounds__((64 * LatentShape<T, R, CB>::WAVES), (LatentShape<T
       barrier();
     }
     // Two barriers a tile.  Of each SIMD's two waves one finishes a tile while the other forms sums: the second four waves are half a tile
-    // behind, so that softmax and matrix instructions go together (118 us with all in step, 16 x 14 thousand tokens, 128 columns).
+    // behind, so that softmax and matrix instructions go together (16 x 14 thousand tokens, 128 columns: 104 us, 118 with all in step).
     if (WAVES == 4 || wave < 4) {
       for (int t = t0; t < t_end; ++t) {
         hand_over(t);
@@ -330,7 +331,8 @@ __global__ __launch_bounds__((64 * LatentShape<T, R, CB>::WAVES), (LatentShape<T
 // Up to 16 columns, which a wave takes with all their channels (queries 72, results 128 registers): every wave of a workgroup copies and works
 // tiles of 32 tokens by itself, nothing is shared and no wave waits for another before the end.  A wave's one tile of LDS is loaded again
 // when it has been read; three of four waves wait for memory at any time, which is what keeps it busy.  Products of 16 x 16: a lane gets the
-// scores of 8 neighbouring tokens of its column, the right operand of the second product.
+// scores of 8 neighbouring tokens of its column, the right operand of the second product.  Bound by memory, at 6.8 TB/s, behind 15 us that do
+// not shrink with the cache (finding the work, first tiles, joining waves): 64 sequences of 2000 to 8192 tokens, 16 heads, 378 MB in 77 us.
 template <typename T, int R>
 __global__ __launch_bounds__(256, 1) void latent_narrow_kernel(LatentArgs a) {
   constexpr int ROT = R == 512 ? 64 : 32, W = R + ROT, M = 16, WAVES = 4, TT = kLatentTile, NK = R / 32, NR = ROT / 32, NCT = R / 16;
@@ -550,6 +552,9 @@ __global__ __launch_bounds__(256) void latent_join_kernel(LatentArgs a) {
   });
 }
 
+// Columns of a workgroup: the fewest that hold a sequence's (row, head) pairs, 128 where there are more, since every tile of columns reads the
+// tokens again: 16 sequences of 14 thousand tokens with 128 heads 120 us in 128, 156 in 64, 231 in 32; 24 drafted rows of 32 heads behind 8 x 7
+// thousand 152, 221, 337; 64 sequences with 16 heads 85 us in the narrow kernel's 16, 91 in 32.
 struct LatentPlan {
   int cols;                // of a workgroup
   long items, workgroups;

@@ -18,7 +18,7 @@ struct TreeArgs {
 
 constexpr int kTreeRows = 64;
 // Tiles of the line that a unit's drafted rows count for: they are a chain of their own (values to LDS, keys, masks) and would otherwise make
-// the workgroups that have them the last ones (8 sequences of 2 to 9 thousand tokens, window 4096, 64 units: 30 us counted as one tile).
+// the workgroups that have them the last ones (8 sequences of 2 to 9 thousand tokens, window 4096, 64 units: 27 us, 30 counted as one tile).
 constexpr int kDraftedTiles = 6;
 
 struct TreeSequence {
@@ -44,9 +44,11 @@ __device__ __forceinline__ TreeSequence tree_sequence(const TreeArgs& a, int b) 
 }
 
 // A workgroup of four waves takes M = 32 CB (row, query head) columns of a kv head; CB blocks of 32 columns, and 4 / CB groups of waves that
-// share the tiles of 64 tokens and are joined through LDS.  As in the decode kernel every wave goes from codes in registers to f16 and
-// scores are formed transposed, here in products of 32 x 32: row r of a product stands for token (r & 3) + 4 (r >> 3) + 16 (r >> 2 & 1), so a
-// lane ends up with the scores of 16 neighbouring tokens of its column, twice, and takes the value codes of those in 16-byte loads.
+// share the tiles of 64 tokens and are joined through LDS.  Codes come to LDS as they lie in memory, and go to f16 on their way into the
+// products.  Scores are formed transposed, in products of 32 x 32: row r of a product stands for token (r & 3) + 4 (r >> 3) + 16 (r >> 2 & 1), so a
+// lane ends up with the scores of 16 neighbouring tokens of its column, twice, and takes the value codes of those in 16-byte pieces.  16 sequences
+// of 32768 tokens, 8 kv heads of 128, 64 columns, 1.08 GB: 203 us (166 are the reading), matrix instructions busy for a third of it and vector
+// instructions, two thirds of them from codes to f16 and exponentials, for 55 %.
 template <typename T, int D, bool FP8, int CB>
 __global__ __launch_bounds__(256, 2) void tree_attn_kernel(TreeArgs a) {
   constexpr int M = 32 * CB, TG = 4 / CB, NC = D / 32, PD = D / 8;
@@ -166,7 +168,7 @@ __global__ __launch_bounds__(256, 2) void tree_attn_kernel(TreeArgs a) {
 
     // ---- full pages ----
     // A tile's codes lie in one piece; they are copied to LDS past the registers, by the waves that read them (as 16-byte loads of rows they came in
-    // quarters of lines, and once for every wave).  Pieces are exchanged by bits of the row so that 16 lanes touch all banks.
+    // quarters of lines, and once for every wave: 273 us for what now takes 203).  Pieces are exchanged by bits of the row so that 16 lanes touch all banks.
     auto key_swap = [](int t) { return PIECES == 8 ? (t >> 1 & 3) | (t >> 4 & 1) << 2 : (t >> 2 & 1) | (t >> 4 & 1) << 1; };
     const int code_tiles = len / P * runs;
     const int code_first = s.first_tile + t0, last_code = min(s.first_tile + t1, code_tiles);
@@ -475,6 +477,9 @@ __global__ __launch_bounds__(256) void tree_join_kernel(TreeArgs a) {
   });
 }
 
+// Columns of a workgroup: the fewest of 32, 64 and 128 that hold a kv head's (row, query head) pairs, since every tile of columns reads the codes
+// again: 64 columns over 16 x 32768 tokens 204 us, 337 as twice 32 and 309 in a half empty 128; 30 to 64 over 4 x 8 to 16 thousand 131, 189, 196;
+// 104 over 8 x 2 to 4 thousand 27 in 128, 32 as twice 64.
 struct TreePlan {
   int cb;
   long items, workgroups;
