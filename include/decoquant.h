@@ -608,7 +608,7 @@ size_t dq_latent_workspace_bytes(const dq_latent_cache* cache, int32_t batch, in
 /*
  * Absorbed form: out[row, h] = softmax_t(q[row, h] . [c_t | k_rot_t] * scale) c_t over the cached tokens of the
  * row's sequence, the batch's rows being its last tokens (append first, then attend).
- *   q         [rows, q_heads, latent_dim + rot_dim];  out [rows, q_heads, latent_dim], not overlapping q
+ *   q         [rows, q_heads, latent_dim + rot_dim];  out [rows, q_heads, latent_dim], which shares no channel with q
  *   seen      NULL, or u64 [rows] (with DQ_PAGED_CAUSAL, max_rows <= 64): of the sequence's own rows, row i sees
  *             the j-th where bit j is set (a tree of drafted tokens), of the tokens before them all
  *   softmax_scale  must be positive and finite (1/sqrt of a head's expanded channels)
@@ -627,7 +627,7 @@ int32_t dq_latent_attention(const dq_latent_cache* cache, const dq_paged_batch* 
  * nothing paged: sequence b has rows starts[b] .. starts[b+1] - 1 of q and out and tokens kv_starts[b] ..
  * kv_starts[b+1] - 1 of k, k_rot and v, and its rows are its last tokens (earlier ones were read back and expanded).
  *   q [rows, heads, head_dim + rot_dim], k and v [tokens, heads, head_dim], k_rot [tokens, rot_dim],
- *   out [rows, heads, head_dim]; head_dim and rot_dim are 128 and 64, or 64 and 32
+ *   out [rows, heads, head_dim], which shares no channel with the others; head_dim and rot_dim are 128 and 64, or 64 and 32
  */
 typedef struct dq_expanded {
   dq_heads q, k, v, out;

@@ -286,6 +286,10 @@ extern "C" int32_t dq_expanded_attention(const dq_expanded* x, int32_t max_rows,
   if (x->dtype != DQ_F16 && x->dtype != DQ_BF16) return DQ_EINVAL;
   if (!heads_ok(&x->q, false) || !heads_ok(&x->k, false) || !heads_ok(&x->v, false) || !heads_ok(&x->out, false)) return DQ_EINVAL;
   if (x->q.heads != x->k.heads || x->q.heads != x->v.heads || x->q.heads != x->out.heads) return DQ_EINVAL;
+  const dq_heads rot = {const_cast<uint16_t*>(x->k_rot), 0, x->k_rot_stride, 0, 1};
+  if (heads_meet(&x->q, x->rows, x->head_dim + x->rot_dim, &x->out, x->rows, x->head_dim) || heads_meet(&x->k, x->tokens, x->head_dim, &x->out, x->rows, x->head_dim) ||
+      heads_meet(&x->v, x->tokens, x->head_dim, &x->out, x->rows, x->head_dim) || heads_meet(&rot, x->tokens, x->rot_dim, &x->out, x->rows, x->head_dim))
+    return DQ_EINVAL;
   if (!x->k_rot || ((uintptr_t)x->k_rot & 15) || x->k_rot_stride < 0 || (x->k_rot_stride & 7)) return DQ_EINVAL;
   if (!workspace || ((uintptr_t)workspace & 15) || (flags & ~DQ_PAGED_CAUSAL) || !scale_ok(softmax_scale)) return DQ_EINVAL;
   if (x->tokens >= kMostTokens || x->rows >= kMostTokens) return DQ_EINVAL;

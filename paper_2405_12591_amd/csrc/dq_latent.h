@@ -20,6 +20,24 @@ inline bool latent_batch_ok(const dq_paged_batch* b, const dq_latent_cache* c, b
 
 inline bool scale_ok(float scale) { return scale * 1.44269504088896340736f < INFINITY; }
 
+// Whether rows of heads that are read and rows of heads that are written may have channels in common.  Slices of one buffer do not: other columns
+// of its rows, or other channels of its heads.
+inline bool heads_meet(const dq_heads* a, long a_rows, int a_dim, const dq_heads* b, long b_rows, int b_dim) {
+  auto reach = [](const dq_heads* h, long rows, int dim, bool row) {   // elements from the first channel to behind the last one, of all rows or of one
+    return (__int128)(row ? 0 : rows - 1) * h->token_stride + (__int128)(h->heads - 1) * h->head_stride + dim;
+  };
+  if (a_rows <= 0 || b_rows <= 0) return false;
+  const __int128 apart = ((__int128)(intptr_t)b->data - (__int128)(intptr_t)a->data) / 2;
+  if (apart >= reach(a, a_rows, a_dim, false) || -apart >= reach(b, b_rows, b_dim, false)) return false;
+  auto interleaved = [&](__int128 period, __int128 a_in, __int128 b_in) {
+    const __int128 in = period > 0 ? (apart % period + period) % period : 0;
+    return period > 0 && in >= a_in && in + b_in <= period;
+  };
+  if (a->token_stride == b->token_stride && interleaved(a->token_stride, reach(a, 1, a_dim, true), reach(b, 1, b_dim, true))) return false;
+  return !(a->token_stride == b->token_stride && a->head_stride == b->head_stride && a->head_stride > 0 && a->token_stride % a->head_stride == 0 &&
+           interleaved(a->head_stride, a_dim, b_dim));
+}
+
 // ---- memory to LDS, past the registers ----
 typedef __attribute__((address_space(3))) char* LdsBytes;
 typedef __attribute__((address_space(3))) const u32x4* LdsPieces;
@@ -46,9 +64,9 @@ __device__ __forceinline__ void copy_to_lds(const uint16_t* from, uint32_t lds) 
   asm volatile("s_mov_b32 m0, %0\n\ts_nop 0\n\tglobal_load_lds_dwordx4 %1, off" ::"s"(__builtin_amdgcn_readfirstlane(lds)), "v"(from) : "memory");
 }
 // Waits for all of the wave's copies but the newest N; for the workgroup's other waves.  As instructions that no LDS read passes (the
-// compiler moves reads across the barrier builtin).
+// compiler moves reads across the barrier builtin), its result no less: what was read may be copied over from then on.
 template <int N> __device__ __forceinline__ void wait_copies() { asm volatile("s_waitcnt vmcnt(%0)" ::"i"(N) : "memory"); }
-__device__ __forceinline__ void barrier() { asm volatile("s_barrier" ::: "memory"); }
+__device__ __forceinline__ void barrier() { asm volatile("s_waitcnt lgkmcnt(0)\n\ts_barrier" ::: "memory"); }
 __device__ __forceinline__ uint32_t lds_of(const void* p) { return (uint32_t)(uintptr_t)(LdsBytes)p; }
 
 // Eight 16-bit values: the left operand of a product with rows as they lie (token by token) as channels.  Of each 16 lanes, four read

@@ -214,7 +214,7 @@ extern "C" int32_t dq_latent_append(const dq_latent_cache* cache, const dq_paged
   if (rot) a.rot = *rot;
   const int rows_per_block = 256 / (cache->rot_dim / 16);
   const long blocks = (batch->rows + (long)rows_per_block - 1) / rows_per_block;
-  const long groups = q ? (q->heads + kTurnedHeads - 1l) / kTurnedHeads : 0, workgroups = blocks * (groups + kLatentParts);
+  const long groups = q ? (q->heads + (kTurnedHeads - 1l)) / kTurnedHeads : 0, workgroups = blocks * (groups + kLatentParts);
   if (workgroups >= kMaxThreads / 256) return DQ_EINVAL;
   a.head_groups = (int)groups;
   const dim3 grid((unsigned)workgroups);

@@ -618,6 +618,7 @@ extern "C" int32_t dq_latent_attention(const dq_latent_cache* cache, const dq_pa
                                        size_t workspace_bytes, uint32_t flags, void* hip_stream) {
   if (!latent_cache_ok(cache) || !latent_batch_ok(batch, cache, true) || !heads_ok(q, false) || !heads_ok(out, false)) return DQ_EINVAL;
   if (q->heads != out->heads || !workspace || ((uintptr_t)workspace & 15) || (flags & ~DQ_PAGED_CAUSAL) || !(softmax_scale > 0.f) || !scale_ok(softmax_scale)) return DQ_EINVAL;
+  if (heads_meet(q, batch->rows, cache->latent_dim + cache->rot_dim, out, batch->rows, cache->latent_dim)) return DQ_EINVAL;
   if (seen && (((uintptr_t)seen & 7) || !(flags & DQ_PAGED_CAUSAL) || max_rows > 64)) return DQ_EINVAL;
   LatentPlan p;
   if (!latent_plan(batch->batch, batch->rows, q->heads, max_rows, max_seq_len, &p)) return DQ_EINVAL;

@@ -27,7 +27,7 @@ static dq_heads heads_of(int32_t n) {
 }
 
 int main(void) {
-  dq_heads h = heads_of(8), q = heads_of(32), many = heads_of(INT_MAX);
+  dq_heads h = heads_of(8), q = heads_of(32), many = heads_of(INT_MAX), out = heads_of(32), many_out = heads_of(INT_MAX);
   dq_paged_cache c = {(uint8_t*)fake, (float*)fake, (uint8_t*)fake, (float*)fake, (uint16_t*)fake, (uint16_t*)fake, 10, 8, 128, 64, 4, DQ_F16, DQ_CODES_INT8};
   dq_latent_cache l = {(uint16_t*)fake, 10, 64, 512, 64, DQ_BF16};
   dq_paged_batch b = {(const int32_t*)fake, (const int32_t*)fake, (const int32_t*)fake, (const int32_t*)fake, 4, 4, 5, 5}, none = b, y;
@@ -38,6 +38,8 @@ int main(void) {
   uint16_t* rows = (uint16_t*)fake;
   int i, j, k, m;
   none.rows = 0;
+  out.data = many_out.data = (uint16_t*)(uintptr_t)(1ull << 60);   /* far from all inputs */
+  e.out = out;
 
   /* sizes of all magnitudes: a size or a refusal, never an overflow, and never less than a smaller call's */
   for (i = 0; i < N; ++i)
@@ -64,7 +66,7 @@ int main(void) {
           y.batch = big[i];
           y.rows = big[j];
           if (y.rows) {
-            int32_t s = dq_latent_attention(&l, &y, &q, &q, NULL, big[k], big[m], 0.1f, fake, 0, DQ_PAGED_CAUSAL, NULL);
+            int32_t s = dq_latent_attention(&l, &y, &q, &out, NULL, big[k], big[m], 0.1f, fake, 0, DQ_PAGED_CAUSAL, NULL);
             CHECK(s == DQ_EINVAL || s == DQ_ENOSPACE);
             CHECK(s == DQ_EINVAL || dq_latent_workspace_bytes(&l, big[i], big[j], 32, big[k], big[m]) > 0);
             s = dq_paged_tree_attention(&c, &y, &q, &h, &h, &q, seen, big[k], big[m], 0.f, 0, fake, 0, 0, NULL);
@@ -82,25 +84,27 @@ int main(void) {
   y = b;
   y.batch = 1;
   y.rows = INT_MAX;
-  CHECK(dq_latent_attention(&l, &y, &many, &many, NULL, INT_MAX, INT_MAX, 1.f, fake, SIZE_MAX, DQ_PAGED_CAUSAL, NULL) == DQ_EINVAL);
+  CHECK(dq_latent_attention(&l, &y, &many, &many_out, NULL, INT_MAX, INT_MAX, 1.f, fake, SIZE_MAX, DQ_PAGED_CAUSAL, NULL) == DQ_EINVAL);
   CHECK(dq_paged_tree_attention(&c, &y, &many, &h, &h, &many, seen, 64, 1000, 0.f, 0, fake, SIZE_MAX, 0, NULL) == DQ_EINVAL);
-  e.q = e.k = e.v = e.out = many;
+  e.q = e.k = e.v = many;
+  e.out = many_out;
   e.rows = INT_MAX;
   CHECK(dq_expanded_attention(&e, INT_MAX, INT_MAX, 0.f, fake, SIZE_MAX, DQ_PAGED_CAUSAL, NULL) == DQ_EINVAL);
   CHECK(dq_latent_append(&l, &y, rows, 576, rows, 576, NULL, 0.f, &many, &many, &rot, NULL) == DQ_EINVAL);
-  e.q = e.k = e.v = e.out = q;
+  e.q = e.k = e.v = q;
+  e.out = out;
   e.rows = 4;
 
   /* no rows: nothing is launched, whatever the rest holds */
   CHECK(dq_latent_append(&l, &none, rows, 576, rows, 576, rows, 1e-6f, &q, &q, &rot, NULL) == DQ_OK);
   CHECK(dq_latent_read(&l, &none, NULL, w, rows, 576, NULL) == DQ_OK);
-  CHECK(dq_latent_attention(&l, &none, &q, &q, seen, 64, 0, 1.f, fake, dq_latent_workspace_bytes(&l, 4, 0, 32, 64, 0), DQ_PAGED_CAUSAL, NULL) == DQ_OK);
+  CHECK(dq_latent_attention(&l, &none, &q, &out, seen, 64, 0, 1.f, fake, dq_latent_workspace_bytes(&l, 4, 0, 32, 64, 0), DQ_PAGED_CAUSAL, NULL) == DQ_OK);
   CHECK(dq_paged_tree_attention(&c, &none, &q, &h, &h, &q, seen, 64, 0, 0.f, 64, fake, dq_paged_tree_workspace_bytes(&c, 4, 0, 32, 64, 0), 0, NULL) == DQ_OK);
   e.rows = 0;
   CHECK(dq_expanded_attention(&e, 64, 300, 0.f, fake, dq_expanded_workspace_bytes(4, 0, 32, 128, 64, 300), 0, NULL) == DQ_OK);
   e.rows = 4;
   /* rows, but none that the bound counts */
-  CHECK(dq_latent_attention(&l, &b, &q, &q, NULL, 0, 300, 1.f, fake, SIZE_MAX, 0, NULL) == DQ_OK);
+  CHECK(dq_latent_attention(&l, &b, &q, &out, NULL, 0, 300, 1.f, fake, SIZE_MAX, 0, NULL) == DQ_OK);
   CHECK(dq_paged_tree_attention(&c, &b, &q, &h, &h, &q, seen, 0, 300, 0.f, 0, fake, SIZE_MAX, 0, NULL) == DQ_OK);
   CHECK(dq_expanded_attention(&e, 0, 300, 0.f, fake, SIZE_MAX, 0, NULL) == DQ_OK);
 
@@ -111,9 +115,9 @@ int main(void) {
   CHECK(dq_latent_append(&l, &b, rows, INT64_MIN, rows, 576, NULL, 0.f, NULL, NULL, NULL, NULL) == DQ_EINVAL);
   CHECK(dq_latent_read(NULL, &b, NULL, w, rows, 576, NULL) == DQ_EINVAL);
   CHECK(dq_latent_read(&l, NULL, NULL, w, rows, 576, NULL) == DQ_EINVAL);
-  CHECK(dq_latent_attention(NULL, &b, &q, &q, NULL, 1, 300, 1.f, fake, SIZE_MAX, 0, NULL) == DQ_EINVAL);
-  CHECK(dq_latent_attention(&l, NULL, &q, &q, NULL, 1, 300, 1.f, fake, SIZE_MAX, 0, NULL) == DQ_EINVAL);
-  CHECK(dq_latent_attention(&l, &b, &q, &q, NULL, 1, 300, FLT_MAX, fake, SIZE_MAX, 0, NULL) == DQ_EINVAL);
+  CHECK(dq_latent_attention(NULL, &b, &q, &out, NULL, 1, 300, 1.f, fake, SIZE_MAX, 0, NULL) == DQ_EINVAL);
+  CHECK(dq_latent_attention(&l, NULL, &q, &out, NULL, 1, 300, 1.f, fake, SIZE_MAX, 0, NULL) == DQ_EINVAL);
+  CHECK(dq_latent_attention(&l, &b, &q, &out, NULL, 1, 300, FLT_MAX, fake, SIZE_MAX, 0, NULL) == DQ_EINVAL);
   CHECK(dq_paged_tree_attention(NULL, &b, &q, &h, &h, &q, seen, 1, 300, 0.f, 0, fake, SIZE_MAX, 0, NULL) == DQ_EINVAL);
   CHECK(dq_paged_tree_attention(&c, NULL, &q, &h, &h, &q, seen, 1, 300, 0.f, 0, fake, SIZE_MAX, 0, NULL) == DQ_EINVAL);
   CHECK(dq_paged_tree_attention(&c, &b, &q, &h, &h, &q, seen, 1, 300, NAN, 0, fake, SIZE_MAX, 0, NULL) == DQ_EINVAL);

@@ -162,6 +162,37 @@ def test_expanded_attention_refuses():
     assert call(rows=4, size=need(4, 4, 16, 128, 4, 300) - 1) == -2
 
 
+def test_outputs_that_share_channels_with_inputs_are_refused():
+    """What is refused for its places gives -1, what is not goes on to the size of the workspace (-2)."""
+    dq, latent, _ = _lib()
+
+    def absorbed(q, out, rows=4):
+        return dq.lib.dq_latent_attention(_latent(latent), _batch(rows=rows, batch=rows), q, out, None, 4, 300, 0.1, PTR, 0, 1, None)
+
+    q = _heads(data=FAR, heads=16, strides=(0, 9216, 576))      # (below PTR there would be no address left for the outputs)
+    end = FAR + 2 * 4 * 9216
+    for data, strides, status in ((FAR, (0, 9216, 576), -1), (FAR + 128, (0, 9216, 576), -1), (end, (0, 8192, 512), -2), (end - 16, (0, 8192, 512), -1),
+                                  (FAR - 2 * 4 * 8192, (0, 8192, 512), -2), (FAR - 2 * 4 * 8192 + 16, (0, 8192, 512), -1), (FAR + 64, (0, 8192, 512), -1)):
+        assert absorbed(q, _heads(data=data, heads=16, strides=strides)) == status, (data - FAR, strides)
+    # slices of one buffer: [rows, heads, 576 + 512], [rows, 16 heads of 576 and then 16 of 512], [heads, rows, ..]
+    assert absorbed(_heads(heads=16, strides=(0, 16 * 1088, 1088)), _heads(data=PTR + 2 * 576, heads=16, strides=(0, 16 * 1088, 1088))) == -2
+    assert absorbed(_heads(heads=16, strides=(0, 16 * 1088, 1088)), _heads(data=PTR + 2 * 568, heads=16, strides=(0, 16 * 1088, 1088))) == -1
+    assert absorbed(_heads(heads=16, strides=(0, 16 * 1088, 576)), _heads(data=PTR + 2 * 9216, heads=16, strides=(0, 16 * 1088, 512))) == -2
+    assert absorbed(_heads(heads=16, strides=(0, 16 * 1088, 576)), _heads(data=PTR + 2 * 9208, heads=16, strides=(0, 16 * 1088, 512))) == -1
+    assert absorbed(_heads(heads=16, strides=(0, 576, 4 * 576)), _heads(data=PTR + 2 * 16 * 4 * 576, heads=16, strides=(0, 512, 4 * 512))) == -2
+    assert absorbed(_heads(heads=16, strides=(0, 1 << 62, 1 << 60)), _heads(data=PTR + 2 * 576, heads=16, strides=(0, 1 << 62, 1 << 60))) == -2
+
+    def expanded(**out):
+        heads = [dict(heads=16, strides=(0, 6144, 384)), dict(data=PTR + 2 * 192, heads=16, strides=(0, 6144, 384)), dict(data=PTR + 2 * 256, heads=16, strides=(0, 6144, 384))]
+        packed = b"".join(_heads(**h) for h in heads + [dict(heads=16, strides=(0, 2048, 128), **out)])
+        tail = dict(k_rot=FAR, k_rot_stride=64, starts=PTR, kv_starts=PTR, batch=4, rows=4, tokens=4, head_dim=128, rot_dim=64, dtype=1)
+        return dq.lib.dq_expanded_attention(packed + _pack_expanded(*tail.values()), 4, 300, 0.1, PTR, 0, 1, None)
+
+    for data, status in ((PTR, -1), (PTR + 2 * 192, -1), (PTR + 2 * 256, -1), (PTR + 2 * 4 * 6144, -2), (FAR, -1), (FAR + 16, -1), (FAR + 2 * 4 * 64, -2),
+                         (FAR - 2 * 4 * 2048, -2)):
+        assert expanded(data=data) == status, data
+
+
 def test_the_binding_refuses_before_it_looks_for_a_gpu():
     dq, latent, paged = _lib()
     ok = torch.zeros(3, 64, 576, dtype=torch.bfloat16)
