@@ -211,7 +211,8 @@ __global__ __launch_bounds__(256, 2) void tree_attn_kernel(TreeArgs a) {
       auto value_codes = [&](int i, int ct, int tt) __attribute__((always_inline)) {
         return *(LdsPieces)((LdsBytes)s_space.codes[tg][i % NB][1] + (32 * ct + r32) * 64 + ((2 * tt + hl ^ (r32 >> 2 & 3)) << 4));
       };
-      if (batch0 > code_first && CB > 1) __syncthreads();
+      if (batch0 > code_first && CB > 1) __syncthreads();   // the last 64 tiles have been read
+      else asm volatile("s_waitcnt lgkmcnt(0)" ::: "memory");
 #pragma unroll
       for (int i = 0; i < (NB > 1 ? NB - 1 : 1); ++i)
         if (i < count) copy_tile(i);
