@@ -98,6 +98,25 @@ def test_a_line_of_more_than_24_bits():
     assert bool(((got[some] - o).abs() <= tol).all())
 
 
+@pytest.mark.parametrize("heads", [16, 24, 128])
+def test_pages_whose_offsets_take_more_than_32_bits(heads):
+    gen = torch.Generator().manual_seed(11)
+    x, off = Latents([300, 65], 512, torch.bfloat16, 64, gen), 60000
+    far = torch.empty((off + x.pool, 64, 576), dtype=torch.bfloat16, device=DEV)
+    far[off:] = x.cache.rows
+    x.cache = dq.LatentCache(far, 512)
+    x.table = torch.where(x.table >= 0, x.table + off, x.table)
+    q = normal((4, heads, 576), torch.bfloat16, gen)
+    check(x.attend(q[:2].to(DEV), [1, 1], 0.05), *x.want(q[:2], [1, 1], 0.05))
+    check(x.attend(q.to(DEV), [2, 2], 0.05), *x.want(q, [2, 2], 0.05))
+    new = normal((2, 576), torch.bfloat16, gen).to(DEV)
+    dq.latent_append(x.cache, new[:, :512], new[:, 512:], None, ints([300, 65]), x.table.to(DEV))     # the last tokens again
+    out = torch.zeros((365, 576), dtype=torch.bfloat16, device=DEV)
+    dq.latent_read(x.cache, None, ints([300, 65]), ints([0, 300, 365]), x.table.to(DEV), out)
+    want = torch.cat([x.rows[0][:299], new[:1].cpu(), x.rows[1][:64], new[1:].cpu()])
+    assert torch.equal(out.cpu(), want)
+
+
 def test_rows_past_the_bound_are_left():
     gen = torch.Generator().manual_seed(10)
     x = Latents([90, 40], 512, torch.float16, 64, gen)

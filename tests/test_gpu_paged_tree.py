@@ -98,6 +98,18 @@ def test_long_caches_and_many_sequences():
             check(x.run(max_len=max_len), *want, "bound %d" % max_len)
 
 
+@pytest.mark.parametrize("count", [9, 20, 40])
+def test_pages_whose_offsets_take_more_than_32_bits(count):
+    x, off = Trees([200, 129], [count, 3], 4, 2, 128, BF, E4, 64, 6), 300000
+    near, pages = x.cache, x.cache.pages
+    t = {n: torch.empty((off + pages,) + near.t[n].shape[1:], dtype=torch.uint8 if "codes" in n else torch.float32, device=DEV).view(near.t[n].dtype)
+         for n in ("k_codes", "k_scales", "v_codes", "v_scales")}
+    for n, far in t.items():
+        (far[off:].view(torch.uint8) if "codes" in n else far[off:]).copy_(near.t[n].view(torch.uint8) if "codes" in n else near.t[n])
+    x.cache = dq.PagedCache({**near.t, **t})
+    check(x.run(table=x.table + off), *x.want())
+
+
 def test_a_row_that_sees_nothing_is_zero_and_the_output_may_be_the_queries():
     x = Trees([0, 70], [6, 2], 3, 3, 64, F16, I8, 64, 5)
     x.seen[:6] = torch.tensor([1, 0, 5, 1 << 40, 0, 63])
