@@ -218,20 +218,25 @@ struct Pieces {
 __device__ __forceinline__ Pieces pieces_of(long begin, int tiles, long quota) { return {over(begin, quota), over(begin + tiles - 1, quota)}; }
 __device__ __forceinline__ long slot_of(const Pieces& p, long w) { return w == p.first ? 2 * w + 1 : 2 * w; }
 
-// Joins the pieces of kJoinColumns<D> columns (those below `valid`): a wave a column where there are few pieces, four waves a column, which take
-// every fourth piece, where there are many.  o: [slot, column, D] floats, ml: [slot, column, 2]; eight pieces are asked for at once.
-// (A workgroup a column spent most of its time on finding its unit: 39 us where this takes 8, 64 columns of 128 units in 4 or 5 pieces.)
+// Joins the pieces of kJoinColumns<D> columns (those below `valid`): a wave a column, or as many as 16-byte loads of a piece let it, where there are few
+// pieces, four waves, which take every fourth piece, where there are many.  o: [slot, column, D] floats, ml: [slot, column, 2]; eight
+// pieces are asked for at once.  (A workgroup a column spent most of its time on finding its unit: 39 us where this takes 8, 64 columns of 128
+// units in 4 or 5 pieces.)
 template <int D> constexpr int kJoinColumns = D >= 256 ? 4 : 16;   // (512 channels: 16 us, 21 with sixteen; 64 channels 16, 20 with four)
 template <typename T, int D, typename Slot, typename Out>
 __device__ __forceinline__ void join_columns(int count, Slot slot_of_piece, const float* o, const float* ml, int columns, int column0, int valid, Out out_of) {
-  constexpr int PER = D / 64, AHEAD = 8;
-  __shared__ float s_o[4][D], s_m[4], s_l[4];
-  const int tid = threadIdx.x, lane = tid & 63, wave = __builtin_amdgcn_readfirstlane(tid >> 6);
-  struct Sum { float m, l, x[PER]; };
-  auto add = [&](int column, int from, int step) {
+  constexpr int PER = D >= 256 ? D / 64 : 4, LANES = D / PER, AT_ONCE = 64 / LANES, AHEAD = 8;   // channels of a lane, lanes of a column, columns of a wave
+  __shared__ __align__(16) float s_o[4][64 * PER];
+  __shared__ float s_m[4][AT_ONCE], s_l[4][AT_ONCE];
+  const int tid = threadIdx.x, lane = tid & 63, wave = __builtin_amdgcn_readfirstlane(tid >> 6), in = lane % LANES, sub = lane / LANES;
+  const int end = min(column0 + kJoinColumns<D>, valid);
+  struct Sum { float m, l; f32x4 x[PER / 4]; };
+  auto add = [&](int c, int from, int step) {
+    const int column = min(c, end - 1);
     Sum r = {-INFINITY, 0.f, {}};
     for (int i0 = from; i0 < count; i0 += step * AHEAD) {
-      float y[AHEAD][PER], pm[AHEAD], pl[AHEAD];
+      f32x4 y[AHEAD][PER / 4];
+      float pm[AHEAD], pl[AHEAD];
 #pragma unroll
       for (int k = 0; k < AHEAD; ++k) {                   // (behind the last piece: that one again, with no weight)
         const long at = slot_of_piece(min(i0 + step * k, count - 1)) * columns + column;
@@ -239,7 +244,7 @@ __device__ __forceinline__ void join_columns(int count, Slot slot_of_piece, cons
         pm[k] = i0 + step * k < count ? v.x : -INFINITY;
         pl[k] = v.y;
 #pragma unroll
-        for (int e = 0; e < PER; ++e) y[k][e] = o[at * D + PER * lane + e];
+        for (int e = 0; e < PER / 4; ++e) y[k][e] = *reinterpret_cast<const f32x4*>(o + at * D + PER * in + 4 * e);
       }
       float top = r.m;
 #pragma unroll
@@ -248,51 +253,52 @@ __device__ __forceinline__ void join_columns(int count, Slot slot_of_piece, cons
       r.m = top;
       r.l *= back;
 #pragma unroll
-      for (int e = 0; e < PER; ++e) r.x[e] *= back;
+      for (int e = 0; e < PER / 4; ++e) r.x[e] *= back;
 #pragma unroll
       for (int k = 0; k < AHEAD; ++k) {
         const float w = __builtin_amdgcn_exp2f(pm[k] - at);
         r.l = __builtin_fmaf(pl[k], w, r.l);
 #pragma unroll
-        for (int e = 0; e < PER; ++e) r.x[e] = __builtin_fmaf(y[k][e], w, r.x[e]);
+        for (int e = 0; e < PER; ++e) r.x[e / 4][e % 4] = __builtin_fmaf(y[k][e / 4][e % 4], w, r.x[e / 4][e % 4]);
       }
     }
     return r;
   };
-  auto store = [&](uint16_t* out, const float* x, float l) {   // PER neighbouring channels a lane
+  auto store = [&](int c, const f32x4 (&x)[PER / 4], float l) {
+    if (c >= end) return;
     const float inv = l == 0.f ? 0.f : 1.f / l;
-    if constexpr (PER == 1) {
-      out[lane] = (uint16_t)pack2<T>(x[0] * inv, 0.f);
-    } else {
+    uint16_t* const out = out_of(c) + PER * in;
 #pragma unroll
-      for (int e = 0; e < PER; e += 2) reinterpret_cast<uint32_t*>(out + PER * lane)[e / 2] = pack2<T>(x[e] * inv, x[e + 1] * inv);
-    }
+    for (int e = 0; e < PER / 4; ++e)
+      *reinterpret_cast<u32x2*>(out + 4 * e) = u32x2{pack2<T>(x[e][0] * inv, x[e][1] * inv), pack2<T>(x[e][2] * inv, x[e][3] * inv)};
   };
   if (count <= 4 * AHEAD) {
-    for (int c = column0 + wave; c < min(column0 + kJoinColumns<D>, valid); c += 4) {
-      const Sum r = add(c, 0, 1);
-      store(out_of(c), r.x, r.l);
+    for (int c = column0 + wave * AT_ONCE; c < end; c += 4 * AT_ONCE) {
+      const Sum r = add(c + sub, 0, 1);
+      store(c + sub, r.x, r.l);
     }
     return;
   }
-  for (int c = column0; c < min(column0 + kJoinColumns<D>, valid); ++c) {
-    const Sum r = add(c, wave, 4);
-    __syncthreads();                                      // the last column's results have been read
+  int turn = 0;
+  for (int c = column0; c < end; c += AT_ONCE, ++turn) {
+    const Sum r = add(c + sub, wave, 4);
+    __syncthreads();                                      // the last columns' results have been read
 #pragma unroll
-    for (int e = 0; e < PER; ++e) s_o[wave][PER * lane + e] = r.x[e];
-    if (lane == 0) { s_m[wave] = r.m; s_l[wave] = r.l; }
+    for (int e = 0; e < PER / 4; ++e) *reinterpret_cast<f32x4*>(&s_o[wave][PER * lane + 4 * e]) = r.x[e];
+    if (in == 0) { s_m[wave][sub] = r.m; s_l[wave][sub] = r.l; }
     __syncthreads();
-    if (wave != (c & 3)) continue;
-    const float top = fmaxf(fmaxf(s_m[0], s_m[1]), fmaxf(s_m[2], s_m[3])), at = top == -INFINITY ? 0.f : top;
-    float x[PER] = {}, l = 0.f;
+    if (wave != (turn & 3)) continue;
+    const float top = fmaxf(fmaxf(s_m[0][sub], s_m[1][sub]), fmaxf(s_m[2][sub], s_m[3][sub])), at = top == -INFINITY ? 0.f : top;
+    f32x4 x[PER / 4] = {};
+    float l = 0.f;
 #pragma unroll
     for (int w = 0; w < 4; ++w) {
-      const float f = __builtin_amdgcn_exp2f(s_m[w] - at);
-      l = __builtin_fmaf(s_l[w], f, l);
+      const float f = __builtin_amdgcn_exp2f(s_m[w][sub] - at);
+      l = __builtin_fmaf(s_l[w][sub], f, l);
 #pragma unroll
-      for (int e = 0; e < PER; ++e) x[e] = __builtin_fmaf(s_o[w][PER * lane + e], f, x[e]);
+      for (int e = 0; e < PER; ++e) x[e / 4][e % 4] = __builtin_fmaf(s_o[w][PER * lane + e], f, x[e / 4][e % 4]);
     }
-    store(out_of(c), x, l);
+    store(c + sub, x, l);
   }
 }
 
