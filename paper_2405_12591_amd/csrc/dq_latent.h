@@ -220,9 +220,9 @@ __device__ __forceinline__ long slot_of(const Pieces& p, long w) { return w == p
 
 // Joins the pieces of kJoinColumns<D> columns (those below `valid`): a wave a column, or as many as 16-byte loads of a piece let it, where there are few
 // pieces, four waves, which take every fourth piece, where there are many.  o: [slot, column, D] floats, ml: [slot, column, 2]; eight
-// pieces are asked for at once.  (A workgroup a column spent most of its time on finding its unit: 39 us where this takes 8, 64 columns of 128
+// pieces are asked for at once.  (A workgroup a column spent most of its time on finding its unit: 39 us where this takes 9, 64 columns of 128
 // units in 4 or 5 pieces.)
-template <int D> constexpr int kJoinColumns = D >= 256 ? 4 : 16;   // (512 channels: 16 us, 21 with sixteen; 64 channels 16, 20 with four)
+template <int D> constexpr int kJoinColumns = D >= 256 ? 4 : 16;   // (512 channels: 16 us, 21 with sixteen; 128 channels 9.4, 10.0 with eight, 9.7 with 32; 64 channels 6.8, 8.1 with 32)
 template <typename T, int D, typename Slot, typename Out>
 __device__ __forceinline__ void join_columns(int count, Slot slot_of_piece, const float* o, const float* ml, int columns, int column0, int valid, Out out_of) {
   constexpr int PER = D >= 256 ? D / 64 : 4, LANES = D / PER, AT_ONCE = 64 / LANES, AHEAD = 8;   // channels of a lane, lanes of a column, columns of a wave
