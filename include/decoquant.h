@@ -594,9 +594,9 @@ int32_t dq_latent_append(const dq_latent_cache* cache, const dq_paged_batch* bat
                          int64_t latent_stride, const uint16_t* k_rot, int64_t k_rot_stride, const uint16_t* weight,
                          float eps, const dq_heads* q, const dq_heads* q_out, const dq_rotary* rot, void* hip_stream);
 
-/* Rows first[b] <= t < seq_lens[b] (first NULL: from 0) into out [batch->rows, latent_dim + rot_dim] (rows that do not overlap), row out_starts[b] + t -
- * first[b]; tokens past row out_starts[b+1] - 1 are left out, rows of a page that does not exist are zeros with k_rot of NaN.
- * batch->starts is not used. */
+/* Rows first[b] <= t < seq_lens[b] (first NULL: from 0) into out [batch->rows, latent_dim + rot_dim] (rows that do not overlap; the stride of
+ * one row alone is not looked at), row out_starts[b] + t - first[b]; tokens past row out_starts[b+1] - 1 are left out, rows of a page that
+ * does not exist are zeros with k_rot of NaN.  batch->starts is not used. */
 int32_t dq_latent_read(const dq_latent_cache* cache, const dq_paged_batch* batch, const int32_t* first,
                        const int32_t* out_starts, uint16_t* out, int64_t out_stride, void* hip_stream);
 

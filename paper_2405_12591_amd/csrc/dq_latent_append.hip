@@ -228,7 +228,7 @@ extern "C" int32_t dq_latent_append(const dq_latent_cache* cache, const dq_paged
 extern "C" int32_t dq_latent_read(const dq_latent_cache* cache, const dq_paged_batch* batch, const int32_t* first, const int32_t* out_starts,
                                   uint16_t* out, int64_t out_stride, void* hip_stream) {
   if (!latent_cache_ok(cache) || !latent_batch_ok(batch, cache, false) || !out_starts || !rows_ok(out, out_stride) ||
-      out_stride < cache->latent_dim + cache->rot_dim)
+      (batch->rows != 1 && out_stride < cache->latent_dim + cache->rot_dim))   // (a stride over one row says nothing)
     return DQ_EINVAL;
   if (batch->rows == 0) return DQ_OK;
   const LatentReadArgs a = {*cache, *batch, first, out_starts, out, out_stride};
