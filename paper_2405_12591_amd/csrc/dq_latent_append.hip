@@ -30,6 +30,15 @@ __device__ __forceinline__ void place_rows(const int32_t* starts, int rows, int 
   __syncthreads();
 }
 
+// Whether any of a piece's eight values is infinite or NaN.
+template <typename T> __device__ __forceinline__ bool not_finite(const u32x4& v) {
+  constexpr uint32_t kExp = __is_same(T, __bf16) ? 0x7F80u : 0x7C00u;
+  bool bad = false;
+#pragma unroll
+  for (int e = 0; e < 4; ++e) bad |= (v[e] & kExp) == kExp || (v[e] >> 16 & kExp) == kExp;
+  return bad;
+}
+
 // Of 256 / (ROT / 16) rows a workgroup takes a quarter's latents and shared key channels, or the queries' heads of a group.  A wave norms four
 // rows of 512 channels (eight of 256), all asked for together (all the rows' latents in one workgroup, four times as many after one another: 11.7 us
 // for 128 rows of 128 heads where this takes 6.1, 10.5 and 5.9 for 16 rows).  A thread keeps 16 of the rotated channels of one row, whose angles it
@@ -95,11 +104,7 @@ __global__ __launch_bounds__(256) void latent_append_kernel(LatentAppendArgs a) 
         for (int e = 0; e < 8; ++e) x[e] = x[e] * f * y[e];
         v[i] = pack8<T>(x);
       }
-      constexpr uint32_t kExp = __is_same(T, __bf16) ? 0x7F80u : 0x7C00u;
-      bool bad = false;
-#pragma unroll
-      for (int e = 0; e < 4; ++e) bad |= (v[i][e] & kExp) == kExp || (v[i][e] >> 16 & kExp) == kExp;
-      const uint64_t any = __ballot(bad) >> (R == 512 ? 0 : lane & 32) & (R == 512 ? ~0ull : 0xFFFFFFFFull);
+      const uint64_t any = __ballot(not_finite<T>(v[i])) >> (R == 512 ? 0 : lane & 32) & (R == 512 ? ~0ull : 0xFFFFFFFFull);
       if (any) v[i] = u32x4{0, 0, 0, 0};
       const long row = s_row[r];
       if (row < 0) continue;
@@ -129,12 +134,15 @@ __global__ __launch_bounds__(256) void latent_append_kernel(LatentAppendArgs a) 
   } else if (live) {
     u32x4 none[2] = {};
     ready_unit<T, LANES, INTERLEAVED>(v, none, false, l.pair0 >= 0, 0.f, 0.f, cs, sn);
-    if (s_bad[r])
-#pragma unroll
-      for (int e = 0; e < 4; ++e) v[0][e] = v[1][e] = 0x7FFF7FFFu;
-    uint16_t* const to = a.c.rows + s_row[r] * W + R;
-    *reinterpret_cast<u32x4*>(to + l.at0) = v[0];
-    *reinterpret_cast<u32x4*>(to + l.at1) = v[1];
+    // Key channels that came or were turned out of the type's range count as the latent's do: an infinite score would
+    // hide the token from half of the queries.  (A row's lanes are here together.)
+    const bool any = (__ballot(not_finite<T>(v[0]) || not_finite<T>(v[1])) >> (lane / LANES * LANES) & ((1u << LANES) - 1)) != 0;
+    uint16_t* const to = a.c.rows + s_row[r] * W;
+    if (any)
+      for (int e = 8 * unit; e < R; e += 8 * LANES) *reinterpret_cast<u32x4*>(to + e) = u32x4{0, 0, 0, 0};   // (behind the latent's own store: the barrier)
+    if (any || s_bad[r]) v[0] = v[1] = kNanPiece;
+    *reinterpret_cast<u32x4*>(to + R + l.at0) = v[0];
+    *reinterpret_cast<u32x4*>(to + R + l.at1) = v[1];
   }
 }
 
