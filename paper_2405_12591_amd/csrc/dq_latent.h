@@ -21,21 +21,37 @@ inline bool latent_batch_ok(const dq_paged_batch* b, const dq_latent_cache* c, b
 inline bool scale_ok(float scale) { return scale * 1.44269504088896340736f < INFINITY; }
 
 // Whether rows of heads that are read and rows of heads that are written may have channels in common.  Slices of one buffer do not: other columns
-// of its rows, or other channels of its heads.
+// of its rows, or other channels of its heads.  Exact where both have the same strides (a stride over one entry says nothing), on the safe side elsewhere.
 inline bool heads_meet(const dq_heads* a, long a_rows, int a_dim, const dq_heads* b, long b_rows, int b_dim) {
-  auto reach = [](const dq_heads* h, long rows, int dim, bool row) {   // elements from the first channel to behind the last one, of all rows or of one
-    return (__int128)(row ? 0 : rows - 1) * h->token_stride + (__int128)(h->heads - 1) * h->head_stride + dim;
-  };
+  typedef __int128 wide;
   if (a_rows <= 0 || b_rows <= 0) return false;
-  const __int128 apart = ((__int128)(intptr_t)b->data - (__int128)(intptr_t)a->data) / 2;
-  if (apart >= reach(a, a_rows, a_dim, false) || -apart >= reach(b, b_rows, b_dim, false)) return false;
-  auto interleaved = [&](__int128 period, __int128 a_in, __int128 b_in) {
-    const __int128 in = period > 0 ? (apart % period + period) % period : 0;
-    return period > 0 && in >= a_in && in + b_in <= period;
+  auto reach = [](const dq_heads* h, long rows, int dim) {   // elements from the first channel to behind the last one
+    return (wide)(rows - 1) * h->token_stride + (wide)(h->heads - 1) * h->head_stride + dim;
   };
-  if (a->token_stride == b->token_stride && interleaved(a->token_stride, reach(a, 1, a_dim, true), reach(b, 1, b_dim, true))) return false;
-  return !(a->token_stride == b->token_stride && a->head_stride == b->head_stride && a->head_stride > 0 && a->token_stride % a->head_stride == 0 &&
-           interleaved(a->head_stride, a_dim, b_dim));
+  const wide apart = ((wide)(intptr_t)b->data - (wide)(intptr_t)a->data) / 2;
+  if (apart >= reach(a, a_rows, a_dim) || -apart >= reach(b, b_rows, b_dim)) return false;
+  auto common = [](bool any_a, int64_t x, bool any_b, int64_t y) -> int64_t { return !any_a ? y : !any_b || x == y ? x : -1; };
+  const int64_t token = common(a_rows > 1, a->token_stride, b_rows > 1, b->token_stride), head = common(a->heads > 1, a->head_stride, b->heads > 1, b->head_stride);
+  if (token > 0) {                                        // the rows' columns, none of them past the next row
+    const wide in = (apart % token + token) % token;
+    if (in >= reach(a, 1, a_dim) && in + reach(b, 1, b_dim) <= token) return false;
+  }
+  if (token < 0 || head < 0) return true;
+  // A row D further on and a head E further on lie at x = apart + D token + E head: they meet if -b_dim < x < a_dim.
+  struct Steps { wide stride, from, to; } far = {token, 1 - a_rows, b_rows - 1}, near = {head, 1 - a->heads, b->heads - 1};
+  if (far.stride < near.stride) { const Steps x = far; far = near; near = x; }
+  auto up = [](wide n, wide d) { return n >= 0 ? (n + d - 1) / d : -(-n / d); };   // n / d, rounded up
+  auto near_meets = [&](wide x) {                         // with near's steps from x
+    wide n = near.stride ? up(1 - b_dim - x, near.stride) : 0;
+    n = n < near.from ? near.from : n;
+    return n <= near.to && x + n * near.stride > -b_dim && x + n * near.stride < a_dim;
+  };
+  if (far.stride == 0) return near_meets(apart);
+  wide n = up(1 - b_dim - near.to * near.stride - apart, far.stride);
+  n = n < far.from ? far.from : n;
+  for (int tries = 0; n <= far.to && apart + n * far.stride < a_dim - near.from * near.stride; ++n)
+    if (++tries > 8 || near_meets(apart + n * far.stride)) return true;   // (three at the most where rows and heads do not cross)
+  return false;
 }
 
 // ---- memory to LDS, past the registers ----

@@ -36,3 +36,58 @@ def test_a_row_read_alone_needs_no_stride():
         assert read(2, stride) == (accepted if stride == 576 else -1), stride
     for stride in (-8, 4, 580):
         assert read(1, stride) == -1 and read(2, stride) == -1, stride
+
+
+_pack_heads = struct.Struct("@Pqqqi4x").pack
+FAR = 1 << 40
+
+
+def _meeting(a, b):
+    """Whether two sets of runs of channels (first element, length) have an element in common."""
+    runs = sorted([(x, x + n, 0) for x, n in a] + [(x, x + n, 1) for x, n in b])
+    end = [-1 << 60, -1 << 60]
+    for x, y, side in runs:
+        if x < end[1 - side]:
+            return True
+        end[side] = max(end[side], y)
+    return False
+
+
+def _absorbed(q_heads, q_token, q_head, out_at, out_token, out_head, rows):
+    import paper_2405_12591_amd as dq
+    q = _pack_heads(FAR, 0, q_token, q_head, q_heads)
+    out = _pack_heads(FAR + 2 * out_at, 0, out_token, out_head, q_heads)
+    status = dq.lib.dq_latent_attention(_latent(), _batch(rows, rows), q, out, None, 1, 300, 0.1, PTR, 0, 1, None)
+    assert status in (-1, -2)                                       # refused for its places, or for the workspace, which is looked at next
+    cells = [(r, h) for r in range(rows) for h in range(q_heads)]
+    return status == -1, _meeting([(r * q_token + h * q_head, 576) for r, h in cells], [(out_at + r * out_token + h * out_head, 512) for r, h in cells])
+
+
+def test_outputs_beside_inputs_in_one_buffer_are_taken():
+    """Slices of [rows, heads * (576 + 512) + 8]: no channel in common, whatever multiple a row is of a head."""
+    for rows in (1, 2, 5):
+        for heads in (1, 2, 16):
+            for pad in (0, 8, 24, 1088):
+                row = heads * 1088 + pad
+                assert _absorbed(heads, row, 1088, 576, row, 1088, rows) == (False, False), (rows, heads, pad)
+                assert _absorbed(heads, row, 1088, 568, row, 1088, rows) == (True, True), (rows, heads, pad)
+                assert _absorbed(heads, 1088, 1088 * rows + pad, 576, 1088, 1088 * rows + pad, rows) == (False, False), (rows, heads, pad)
+
+
+def test_what_meets_is_refused_and_the_same_strides_exactly_that():
+    import random
+    rng = random.Random(0)
+    met = apart = 0
+    for i in range(6000):
+        rows, heads = rng.randint(1, 4), rng.randint(1, 4)
+        strides = [8 * rng.choice([0, 8, 64, 72, 73, 136, 137, 200, 272, 300, 545, 600, rng.randint(0, 700)]) for _ in range(4)]
+        if i % 2:
+            strides[2:] = strides[:2]
+        q_token, q_head, out_token, out_head = strides
+        refused, meet = _absorbed(heads, q_token, q_head, 8 * rng.randint(-800, 800), out_token, out_head, rows)
+        assert refused or not meet, (rows, heads, strides)
+        nested = max(strides[0], strides[1]) >= 1088 + (max(rows, heads) - 1) * min(strides[0], strides[1])
+        if i % 2 and nested:
+            assert refused == meet, (rows, heads, strides)
+            met, apart = met + meet, apart + (not meet)
+    assert met > 100 and apart > 100
