@@ -544,7 +544,7 @@ int32_t dq_paged_attention(const dq_paged_cache* cache, const dq_paged_batch* ba
  * so that refused rows leave nothing behind: accepted ones are appended afterwards (dq_paged_append), and no
  * page is quantized with a row that goes.  Sequence b owns rows starts[b] .. starts[b+1] - 1; seq_lens are the
  * CACHED tokens.  A row's place is seq_lens[b] + the number of rows it sees - 1.
- *   q, out    [rows, q_heads, d]; out may be q
+ *   q, out    [rows, q_heads, d]; out may be q itself (same data and strides), and shares no channel with the others
  *   k, v      [rows, kv_heads, d], keys ready (rotated by their places)
  *   seen      u64 [rows]: bit j: the row sees the j-th row of its sequence; bits of rows that are not there
  *             count neither here nor for the place

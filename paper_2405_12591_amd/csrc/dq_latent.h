@@ -54,6 +54,12 @@ inline bool heads_meet(const dq_heads* a, long a_rows, int a_dim, const dq_heads
   return false;
 }
 
+// Whether b may be written while a is read, each head by the threads that read it: the same rows of heads, or none that meet.
+inline bool heads_in_place(const dq_heads* a, const dq_heads* b, long rows, int dim) {
+  return (a->data == b->data && (rows <= 1 || a->token_stride == b->token_stride) && (a->heads <= 1 || a->head_stride == b->head_stride)) ||
+         !heads_meet(a, rows, dim, b, rows, dim);
+}
+
 // ---- memory to LDS, past the registers ----
 typedef __attribute__((address_space(3))) char* LdsBytes;
 typedef __attribute__((address_space(3))) const u32x4* LdsPieces;

@@ -537,6 +537,10 @@ extern "C" int32_t dq_paged_tree_attention(const dq_paged_cache* cache, const dq
   if (!tree_plan(cache, batch->batch, batch->rows, q->heads, max_rows, max_seq_len, &p)) return DQ_EINVAL;
   if (workspace_bytes < tree_bytes(p.workgroups, p.cb, cache->head_dim)) return DQ_ENOSPACE;
   if (batch->rows == 0 || max_rows == 0) return DQ_OK;
+  // every column tile of a kv head reads its drafted rows, and one that is done writes
+  if (heads_meet(k, batch->rows, cache->head_dim, out, batch->rows, cache->head_dim) || heads_meet(v, batch->rows, cache->head_dim, out, batch->rows, cache->head_dim) ||
+      !heads_in_place(q, out, batch->rows, cache->head_dim))
+    return DQ_EINVAL;
   TreeArgs a = {};
   a.c = *cache; a.bt = *batch; a.q = *q; a.k = *k; a.v = *v; a.out = *out;
   a.seen = seen;

@@ -290,7 +290,7 @@ def paged_tree_attention(cache: PagedCache, q: torch.Tensor, k: torch.Tensor, v:
     each row, bit j its sequence's j-th row (the row itself and its ancestors).  A sequence has at most 64 rows, max_rows at most;
     further ones are not seen and not written.  window > 0 (64 at least): of the cached tokens only those less than `window` before a row's
     place, which is seq_lens plus the rows it sees, less one.  Accepted rows are appended afterwards, refused ones leave nothing.  out
-    may be q.  No gradients."""
+    may be q itself, and shares no memory with the others.  No gradients."""
     if out is None:
         out = torch.empty(q.shape, dtype=q.dtype, device=q.device)
     index = cache.index

@@ -91,3 +91,30 @@ def test_what_meets_is_refused_and_the_same_strides_exactly_that():
             assert refused == meet, (rows, heads, strides)
             met, apart = met + meet, apart + (not meet)
     assert met > 100 and apart > 100
+
+
+
+def _tree(rows, q, k, v, out, q_heads=32, kv_heads=8):
+    """Status of a call over heads (first element from FAR, token stride, head stride): -1 refused, -3 a launch that finds no GPU."""
+    import paper_2405_12591_amd as dq
+    from paper_2405_12591_amd import paged
+    cache = C.byref(paged._CPaged(PTR, PTR, PTR, PTR, PTR, PTR, 10, kv_heads, 128, 64, 8, 0, 0))
+    heads = [_pack_heads(FAR + 2 * at, 0, token, head, n) for (at, token, head), n in zip((q, k, v, out), (q_heads, kv_heads, kv_heads, q_heads))]
+    return dq.lib.dq_paged_tree_attention(cache, _batch(rows, rows), *heads, PTR, 4, 300, 0.0, 0, PTR, 1 << 40, 0, None)
+
+
+@pytest.mark.skipif(torch.cuda.is_available(), reason="its accepted calls would be launched")
+@pytest.mark.parametrize("rows", [1, 2, 5])
+def test_a_trees_output_is_the_queries_or_apart(rows):
+    w = 48 * 128                                                    # a fused projection's row: 32 query heads, 8 of keys, 8 of values
+    q, k, v, far = (0, w, 128), (4096, w, 128), (5120, w, 128), 1 << 30
+    assert _tree(rows, q, k, v, (far, 4096, 128)) == -3 and _tree(rows, q, k, v, q) == -3
+    # over keys or values, wholly or in part, and over other queries than its own
+    for out in (k, v, (4096 - 8, w, 128), (4096 + 1024 + 1016, w, 128), (128, w, 128), (8, w, 128), (-8, w, 128), (0, w + 8, 128) if rows > 1 else k, (0, w, 136)):
+        assert _tree(rows, q, k, v, out) == -1, out
+    # queries elsewhere, the output in the place of the queries that were projected beside the keys; keys of every second head's place
+    assert _tree(rows, (far, 4096, 128), k, v, q) == -3
+    assert _tree(rows, (0, 16384, 512), (128, 16384, 512), (256, 16384, 512), (384, 16384, 512), q_heads=8) == -3
+    assert _tree(rows, (0, 16384, 512), (128, 16384, 512), (256, 16384, 512), (376, 16384, 512), q_heads=8) == -1
+    # one head, one row: their strides say nothing
+    assert _tree(1, (0, 8, 0), (far, 16, 0), (2 * far, 8, 0), (0, 0, 64), q_heads=1, kv_heads=1) == -3
