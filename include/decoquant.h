@@ -586,7 +586,8 @@ typedef struct dq_latent_cache {
  * aligned, strides multiples of 8), as they lie in a fused projection.  c = latent * weight / sqrt(mean(latent^2) + eps)
  * (weight NULL: latent as it is), k_rot turned by its position (rot NULL: as it is; rot->rot_dim is the cache's, positions NULL: a
  * token's place in its sequence); both in fp32 and rounded once.  q (NULL: none), heads [rows, q_heads, rot_dim], the
- * queries' channels that meet k_rot, takes the same rotation in the same launch, into q_out (q itself will do).
+ * queries' channels that meet k_rot, takes the same rotation in the same launch, into q_out (q itself, with the same
+ * strides, will do; it shares no channel with the others).
  * A row with a value that is not finite after that is kept as zeros with k_rot of NaN: a query that sees the token yields
  * NaN, the others are untouched.  Rows of a page that does not exist are dropped.  Lengths may go back at will.
  */

@@ -213,6 +213,11 @@ extern "C" int32_t dq_latent_append(const dq_latent_cache* cache, const dq_paged
   if (q && (!heads_ok(q, false) || !heads_ok(q_out, false) || q->heads != q_out->heads)) return DQ_EINVAL;
   if (!rotary_ok(rot, cache->rot_dim, batch->rows, false) || (rot && rot->rot_dim != cache->rot_dim)) return DQ_EINVAL;
   if (batch->rows == 0) return DQ_OK;
+  // queries are turned by other workgroups than take the rows in
+  const dq_heads c = {const_cast<uint16_t*>(latent), 0, latent_stride, 0, 1}, r = {const_cast<uint16_t*>(k_rot), 0, k_rot_stride, 0, 1};
+  if (q && (heads_meet(&c, batch->rows, cache->latent_dim, q_out, batch->rows, cache->rot_dim) ||
+            heads_meet(&r, batch->rows, cache->rot_dim, q_out, batch->rows, cache->rot_dim) || !heads_in_place(q, q_out, batch->rows, cache->rot_dim)))
+    return DQ_EINVAL;
   LatentAppendArgs a = {};
   a.c = *cache; a.bt = *batch;
   a.latent = latent; a.latent_stride = latent_stride;

@@ -74,10 +74,11 @@ def latent_append(cache: LatentCache, latent: torch.Tensor, k_rot: torch.Tensor,
                   eps: float = 1e-6):
     """Append the rows of a ragged batch (dq_latent_append): latent [rows, latent_dim], normed where a weight is given, and k_rot [rows,
     rot_dim], rotated where a rotation is; q [rows, heads, rot_dim], the queries' channels that meet k_rot, takes the same rotation
-    on the way.  Rows are views of a fused projection as they lie there.  starts: int32 [batch + 1], rows starts[b] ..
-    starts[b+1] - 1 are sequence b's last tokens (None: one row each); seq_lens: int32, the new rows included; page_table: int32
-    [batch, pages].  positions None: a token's place in its sequence.  Returns q_out (None without q).  Rows of no sequence stay
-    as they are.  seq_lens may go back at will: rows behind a sequence's end are never read."""
+    on the way, into q_out, which may be q itself and shares no memory with the others.  Rows are views of a fused projection as
+    they lie there.  starts: int32 [batch + 1], rows starts[b] .. starts[b+1] - 1 are sequence b's last tokens (None: one row each);
+    seq_lens: int32, the new rows included; page_table: int32 [batch, pages].  positions None: a token's place in its sequence.
+    Returns q_out (None without q).  Rows of no sequence stay as they are.  seq_lens may go back at will: rows behind a sequence's
+    end are never read."""
     if q is None:
         if q_out is not None:
             raise DQError("q_out without q")

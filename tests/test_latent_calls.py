@@ -118,3 +118,26 @@ def test_a_trees_output_is_the_queries_or_apart(rows):
     assert _tree(rows, (0, 16384, 512), (128, 16384, 512), (256, 16384, 512), (376, 16384, 512), q_heads=8) == -1
     # one head, one row: their strides say nothing
     assert _tree(1, (0, 8, 0), (far, 16, 0), (2 * far, 8, 0), (0, 0, 64), q_heads=1, kv_heads=1) == -3
+
+
+def _append(rows, c, k, q, q_out, q_heads=32):
+    """Status of a call over rows (first element from FAR, stride) and heads (.., token stride, head stride): -1 refused, -3 a launch that finds no GPU."""
+    import paper_2405_12591_amd as dq
+    rot = struct.Struct("@PPPqiii4x").pack(PTR, 0, 0, rows, 1, 64, 0)
+    heads = [_pack_heads(FAR + 2 * at, 0, token, head, q_heads) for at, token, head in (q, q_out)]
+    return dq.lib.dq_latent_append(_latent(), _batch(rows, rows), FAR + 2 * c[0], c[1], FAR + 2 * k[0], k[1], 0, 0.0, *heads, rot, None)
+
+
+@pytest.mark.skipif(torch.cuda.is_available(), reason="its accepted calls would be launched")
+@pytest.mark.parametrize("rows", [1, 2, 300])
+def test_turned_queries_are_their_own_output_or_apart(rows):
+    w = 576 + 32 * 192                                              # a fused projection's row: [c | k_rot | 32 heads of 128 + 64]
+    c, k, q, far = (0, w), (512, w), (576 + 128, w, 192), 1 << 30
+    assert _append(rows, c, k, q, q) == -3 and _append(rows, c, k, q, (far, 32 * 64, 64)) == -3
+    assert _append(rows, c, k, (far, 32 * 64, 64), q) == -3 and _append(rows, c, k, q, (576, w, 192)) == -3 and _append(rows, c, k, q, (576 + 64, w, 192)) == -3
+    for out in ((0, w, 192), (512, w, 192), (448, w, 64), (568, w, 192), (576 + 120, w, 192), (576 + 136, w, 192), (576 + 128 + 192, w, 192)):
+        assert _append(rows, c, k, q, out) == -1, out
+    # one head, one row: their strides say nothing; rows that are all the same one
+    assert _append(1, (0, 0), (512, 0), (far, 0, 0), (far, 8, 16), q_heads=1) == -3
+    assert _append(rows, (0, 0), (512, 0), (far, 64, 64), (576, 64, 64), q_heads=1) == -3
+    assert _append(rows, (0, 0), (512, 0), (far, 64, 64), (568, 64, 64), q_heads=1) == -1
