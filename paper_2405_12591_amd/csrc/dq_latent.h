@@ -77,13 +77,13 @@ __device__ __forceinline__ uint64_t in_scalars(const void* p) {
 // once: past the caches' order (rows that one workgroup reads: a cache of 378 MB in 80 us, 89 without).
 template <bool once = false> __device__ __forceinline__ void copy_to_lds(const uint16_t* base, uint32_t offset, uint32_t lds) {
   if constexpr (once) {
-    asm volatile("s_mov_b32 m0, %0\n\ts_nop 0\n\tglobal_load_lds_dwordx4 %1, %2 nt" ::"s"(__builtin_amdgcn_readfirstlane(lds)), "v"(offset), "s"(in_scalars(base)) : "memory");
+    asm volatile("s_mov_b32 m0, %0\n\ts_nop 0\n\tglobal_load_lds_dwordx4 %1, %2 nt" ::"s"(__builtin_amdgcn_readfirstlane(lds)), "v"(offset), "s"(in_scalars(base)) : "m0", "memory");
     return;
   }
-  asm volatile("s_mov_b32 m0, %0\n\ts_nop 0\n\tglobal_load_lds_dwordx4 %1, %2" ::"s"(__builtin_amdgcn_readfirstlane(lds)), "v"(offset), "s"(in_scalars(base)) : "memory");
+  asm volatile("s_mov_b32 m0, %0\n\ts_nop 0\n\tglobal_load_lds_dwordx4 %1, %2" ::"s"(__builtin_amdgcn_readfirstlane(lds)), "v"(offset), "s"(in_scalars(base)) : "m0", "memory");
 }
 __device__ __forceinline__ void copy_to_lds(const uint16_t* from, uint32_t lds) {
-  asm volatile("s_mov_b32 m0, %0\n\ts_nop 0\n\tglobal_load_lds_dwordx4 %1, off" ::"s"(__builtin_amdgcn_readfirstlane(lds)), "v"(from) : "memory");
+  asm volatile("s_mov_b32 m0, %0\n\ts_nop 0\n\tglobal_load_lds_dwordx4 %1, off" ::"s"(__builtin_amdgcn_readfirstlane(lds)), "v"(from) : "m0", "memory");
 }
 // Waits for all of the wave's copies but the newest N; for the workgroup's other waves.  As instructions that no LDS read passes (the
 // compiler moves reads across the barrier builtin), its result no less: what was read may be copied over from then on.
