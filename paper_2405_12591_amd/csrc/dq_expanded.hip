@@ -280,9 +280,13 @@ extern "C" size_t dq_expanded_workspace_bytes(int32_t batch, int32_t rows, int32
   return expanded_bytes(most, 2, head_dim);
 }
 
-extern "C" int32_t dq_expanded_attention(const dq_expanded* x, int32_t max_rows, int32_t max_seq_len, float softmax_scale, void* workspace,
+extern "C" int32_t dq_expanded_attention(const dq_expanded* call, int32_t max_rows, int32_t max_seq_len, float softmax_scale, void* workspace,
                                          size_t workspace_bytes, uint32_t flags, void* hip_stream) {
-  if (!x || !x->starts || !x->kv_starts || x->batch <= 0 || x->rows < 0 || x->tokens < 0 || !expanded_dims_ok(x->head_dim, x->rot_dim)) return DQ_EINVAL;
+  if (!call) return DQ_EINVAL;
+  dq_expanded one = *call;
+  const dq_expanded* const x = &one;
+  if (one.tokens == 0) one.k.data = one.v.data = const_cast<uint16_t*>(one.k_rot = one.out.data);   // tensors of no tokens have no address, and are not read
+  if (!x->starts || !x->kv_starts || x->batch <= 0 || x->rows < 0 || x->tokens < 0 || !expanded_dims_ok(x->head_dim, x->rot_dim)) return DQ_EINVAL;
   if (x->dtype != DQ_F16 && x->dtype != DQ_BF16) return DQ_EINVAL;
   if (!heads_ok(&x->q, false) || !heads_ok(&x->k, false) || !heads_ok(&x->v, false) || !heads_ok(&x->out, false)) return DQ_EINVAL;
   if (x->q.heads != x->k.heads || x->q.heads != x->v.heads || x->q.heads != x->out.heads) return DQ_EINVAL;
