@@ -647,7 +647,8 @@ size_t dq_expanded_workspace_bytes(int32_t batch, int32_t rows, int32_t heads, i
  *   softmax_scale           <= 0 selects 1/sqrt(head_dim + rot_dim)
  *   flags                   DQ_PAGED_CAUSAL: row i sees tokens up to its own place; without it all of its sequence
  * A row that sees no token yields zeros.  A row that sees no key or value that is not finite is untouched by those; one that
- * does has values that are not finite.
+ * sees such a value, or whose score with such a key is NaN or +inf, has values that are not finite.  A score of -inf is a weight of
+ * 0, as the formula has it (a row that has no other scores yields zeros).
  */
 int32_t dq_expanded_attention(const dq_expanded* x, int32_t max_rows, int32_t max_seq_len, float softmax_scale,
                               void* workspace, size_t workspace_bytes, uint32_t flags, void* hip_stream);
