@@ -3,7 +3,7 @@ import pytest
 import torch
 
 import paper_2405_12591_amd as dq
-from latent_util import attend64, tolerance
+from latent_util import attend64, check, tolerance
 from paged_util import DEV, ints
 from test_gpu_expanded import Prompt
 
@@ -54,3 +54,20 @@ def test_scores_that_are_all_minus_infinity_are_no_weight():
     k[0, 0, 3] = -float("inf")
     out = dq.expanded_attention(q, k, torch.ones(3, 32, dtype=torch.float16, device=DEV), v, ints([0, 3]), ints([0, 3]), 3, 3, dq.expanded_workspace(1, 3, 1, 64, 3, 3))
     assert not out[0].any() and bool((out[1:] == 1).all())
+
+
+@pytest.mark.parametrize("far", ["k", "k_rot", "v"])
+def test_whole_tiles_of_strides_that_pass_32_bits(far):
+    """64 tokens are a whole tile, whose rows are found by 32-bit offsets where those do: 15 rows of 9 * 2^24 elements are 2^32 bytes and 5 * 2^28 more."""
+    d, n, stride, gen = 64, 64, 9 << 24, torch.Generator().manual_seed(21)
+    assert 15 * stride * 2 > 1 << 32
+    try:
+        room = torch.zeros((n - 1) * stride + 64, dtype=torch.float16, device=DEV)
+    except torch.cuda.OutOfMemoryError:
+        pytest.skip("no room")
+    x = Prompt([n], [n], 1, d, torch.float16, gen)
+    near = {"k": x.kv[:n, 0, :d], "k_rot": x.kr[:n, 4 * d:], "v": x.kv[:n, 0, d:2 * d]}
+    t = {name: (torch.as_strided(room, rows.shape, (stride, 1)).copy_(rows) if name == far else rows.contiguous().to(DEV)) for name, rows in near.items()}
+    out = torch.full((x.q.shape[0], 1, d), 7.0, dtype=torch.float16, device=DEV)
+    dq.expanded_attention(x.q.to(DEV), t["k"][:, None], t["k_rot"], t["v"][:, None], ints([0, n]), ints([0, n]), n, n, dq.expanded_workspace(1, n, 1, d, n, n), out=out)
+    check(out, *x.want())
