@@ -550,9 +550,11 @@ int32_t dq_paged_attention(const dq_paged_cache* cache, const dq_paged_batch* ba
  *             count neither here nor for the place
  *   max_rows  host bound on the rows of any sequence, 1..64 (or 0); further rows of that sequence are not seen and not written
  *   window    > 0 (64 at least): of the cached tokens a row sees the ones less than `window` before its place only
+ *   max_seq_len    not negative, and not looked at: launch, workspace and results are the same whatever it is
  * The rest is as for dq_paged_attention, but the workspace: it needs no zeros (dq_paged_tree_workspace_bytes, for these sizes
- * and all smaller ones with the same heads; calls that share it must be ordered).  A drafted key or value row with a value
- * that is not finite yields NaN for the rows that see it and does nothing to the others.
+ * and all smaller ones with the same heads; calls that share it must be ordered), and holds 1024 pieces of 32, 64 or 128 columns
+ * (max_rows * q_heads / kv_heads) of d + 2 floats, however few sequences there are: 17 to 68 MB with 128 channels.  A drafted key
+ * or value row with a value that is not finite yields NaN for the rows that see it and does nothing to the others.
  */
 size_t dq_paged_tree_workspace_bytes(const dq_paged_cache* cache, int32_t batch, int32_t rows, int32_t q_heads,
                                      int32_t max_rows, int32_t max_seq_len);
@@ -602,7 +604,8 @@ int32_t dq_latent_read(const dq_latent_cache* cache, const dq_paged_batch* batch
                        const int32_t* out_starts, uint16_t* out, int64_t out_stride, void* hip_stream);
 
 /* Bytes dq_latent_attention needs for these sizes and all smaller ones with the same heads (0 on invalid arguments); no zeros needed,
- * calls that share it must be ordered. */
+ * calls that share it must be ordered.  512 pieces of 16, 32, 64 or 128 columns (max_rows * q_heads) of latent_dim + 2 floats, however few
+ * sequences there are: 17 to 135 MB with 512 channels.  A model's layers, whose calls are ordered anyway, do with one. */
 size_t dq_latent_workspace_bytes(const dq_latent_cache* cache, int32_t batch, int32_t rows, int32_t q_heads,
                                  int32_t max_rows, int32_t max_seq_len);
 
@@ -614,7 +617,7 @@ size_t dq_latent_workspace_bytes(const dq_latent_cache* cache, int32_t batch, in
  *             the j-th where bit j is set (a tree of drafted tokens), of the tokens before them all
  *   softmax_scale  must be positive and finite (1/sqrt of a head's expanded channels)
  *   max_rows  host bound on the rows of any sequence; further rows of that sequence may be left out (not written)
- *   max_seq_len    host bound on seq_lens (a guess does: it sizes the launch only, which orders the sums)
+ *   max_seq_len    not negative, and not looked at: launch, workspace and results are the same whatever it is
  * fp32 accumulation, one rounding of the result, probabilities in the rows' type for their product with c.  A row that sees no
  * token yields zeros; tokens of a page that does not exist yield NaN for those who see them.  flags: DQ_PAGED_CAUSAL.
  */

@@ -107,7 +107,8 @@ def _workspace_bytes(cache: LatentCache, batch: int, rows: int, q_heads: int, ma
 
 
 def latent_workspace(cache: LatentCache, batch: int, rows: int, q_heads: int, max_rows: int, max_seq_len: int) -> torch.Tensor:
-    """Workspace of latent_attention for these sizes and all smaller ones with the same heads."""
+    """Workspace of latent_attention for these sizes and all smaller ones with the same heads: 17 to 135 MB for 512 channels, by the columns max_rows *
+    q_heads alone.  Calls that share it must be ordered; a model's layers are."""
     return torch.empty(_workspace_bytes(cache, batch, rows, q_heads, max_rows, max_seq_len), dtype=torch.uint8, device=cache.device)
 
 
@@ -116,7 +117,7 @@ def latent_attention(cache: LatentCache, q: torch.Tensor, starts: Optional[torch
                      causal: bool = True, seen: Optional[torch.Tensor] = None) -> torch.Tensor:
     """softmax(q . [c | k_rot] * softmax_scale) c of the batch's rows q [rows, heads, latent_dim + rot_dim] over the cached tokens of their
     sequences, [rows, heads, latent_dim] (dq_latent_attention); rows are the last tokens of their sequence (append them first).
-    max_rows: host bound on the rows of any sequence; max_seq_len: on its tokens (a guess does).  seen: int64, a mask for each row: bit j
+    max_rows: host bound on the rows of any sequence; max_seq_len: on its tokens (any will do: it is not looked at).  seen: int64, a mask for each row: bit j
     names the j-th row of the sequence (a tree of drafted tokens; at most 64 rows); None: every row up to its own place.
     Rows of no sequence and a sequence's rows past max_rows are not written.  No gradients."""
     if out is None:

@@ -3,7 +3,7 @@ import pytest
 import torch
 
 import paper_2405_12591_amd as dq
-from latent_util import FORMS, Latents, normal, starts_of
+from latent_util import FORMS, Latents, attend64, check, normal, starts_of, tolerance
 from paged_util import DEV, ints
 
 pytestmark = pytest.mark.gpu
@@ -67,3 +67,47 @@ def test_key_channels_that_are_not_finite_are_nan_for_those_who_see_them_only(dt
     rest = [i for i in range(14) if i not in see]
     assert got[see].isnan().all()
     assert bool(((got.double().cpu() - want).abs() <= tol)[rest].all())
+
+
+@pytest.mark.parametrize("dtype", DTYPES)
+@pytest.mark.parametrize("latent,page", [(512, 64), (512, 128), (256, 64), (256, 128)])
+@pytest.mark.parametrize("heads,counts", [(1, [16, 3, 9]), (2, [8, 8, 1]), (3, [5, 4, 5]), (4, [4, 0, 3]), (16, [1, 1, 1])])
+def test_masks_of_up_to_16_columns(dtype, latent, page, heads, counts):
+    """The kernel that takes them, whose waves each form a tile's mask from bits that begin anywhere in it."""
+    gen = torch.Generator().manual_seed(heads + page)
+    x = Latents([165, 33, 64 + 9], latent, dtype, page, gen)
+    q = normal((sum(counts) + 2, heads, latent + FORMS[latent]), dtype, gen)
+    seen = torch.randint(-1 << 62, 1 << 62, (sum(counts) + 2,), generator=gen, dtype=torch.int64)   # any rows, and bits of rows that are not there
+    seen[0], seen[sum(counts) - 1] = 0, -1
+    check(x.attend(q.to(DEV), counts, 0.07, seen=seen), *x.want(q, counts, 0.07, seen=seen))
+
+
+@pytest.mark.parametrize("latent", [512, 256])
+@pytest.mark.parametrize("heads", [3, 6, 12, 30])                   # of four rows: 16, 32, 64 and 128 columns
+def test_the_bound_on_lengths_is_not_looked_at(latent, heads):
+    gen = torch.Generator().manual_seed(heads)
+    x = Latents([2100, 40, 700], latent, torch.bfloat16, 64, gen)
+    q = normal((9, heads, latent + FORMS[latent]), torch.bfloat16, gen).to(DEV)
+    assert len({dq.latent_workspace(x.cache, 3, 9, heads, 4, n).numel() for n in (0, 700, 2100, 1 << 30)}) == 1
+    first = x.attend(q, [4, 3, 2], 0.07)
+    for n in (0, 1, 64, 700, 1 << 30):
+        assert torch.equal(x.attend(q, [4, 3, 2], 0.07, max_len=n), first), n
+
+
+@pytest.mark.parametrize("latent", [512, 256])
+@pytest.mark.parametrize("heads", [16, 32, 64, 128])
+def test_sums_over_a_million_tokens(latent, heads):
+    """2^20 tokens over 32 pages that the table names again and again: what 2^11 tokens give."""
+    gen = torch.Generator().manual_seed(heads)
+    x = Latents([2048], latent, torch.float16, 64, gen)
+    table = x.table[:, :32].repeat(1, 512)
+    x.lens = [1 << 20]
+    q = normal((1, heads, latent + FORMS[latent]), torch.float16, gen)
+    got = x.attend(q.to(DEV), [1], 0.05, table=table).double().cpu()
+    o, size, ds = attend64(q, x.rows[0], x.rows[0][:, :latent], torch.ones(1, 2048, dtype=torch.bool), 0.05)
+    # on top of what 2^11 tokens may be off by: a workgroup has 128 tiles of 32 tokens (2^20 / 32 / 256), two matrix instructions each to a result, of
+    # four roundings each, 2^10 2^-24 of the terms' sizes, and eight instructions of two roundings each to a sum of probabilities, 2^11 2^-24.  (f16's smallest
+    # step counts 512 times as often against a sum that is 512 times as large.)
+    v_max = float(x.rows[0][:, :latent].double().abs().max())
+    tol = tolerance(o, size, ds, v_max, 2048, torch.float16) + size * 3 * 2.0 ** -14
+    assert bool(((got - o).abs() <= tol).all())
