@@ -155,10 +155,11 @@ class LatentKVLayer:
     """One layer's latents, as PagedKVLayer is for keys and values of their own: `batch` sequences of up to max_tokens tokens, each with its own
     pages, the lengths on the device.  Rows come packed, sequence by sequence (`starts`, int32 [batch + 1]; None: one row each);
     the host tracks only a bound, which sizes the launches.  Replays of a captured step count on the device only: add their rows to
-    tokens_upper.  (Loops with a page allocator of their own call latent_append and latent_attention.)"""
+    tokens_upper.  workspace_of: another layer, in whose workspace (17 to 135 MB, by the columns) this one works too, where their calls are
+    ordered, as a model's layers' are.  (Loops with a page allocator of their own call latent_append and latent_attention.)"""
 
     def __init__(self, batch: int, heads: int, max_tokens: int, latent_dim: int = 512, rot_dim: int = 64, page_tokens: int = 64,
-                 dtype=torch.bfloat16, device="cuda:0"):
+                 dtype=torch.bfloat16, device="cuda:0", workspace_of: Optional["LatentKVLayer"] = None):
         if min(batch, heads, max_tokens) < 1 or page_tokens not in (64, 128):
             raise DQError("a layer has sequences, heads, room for tokens and pages of 64 or 128 tokens")
         self.batch, self.heads, self.max_tokens = batch, heads, max_tokens
@@ -167,7 +168,7 @@ class LatentKVLayer:
         self.page_table = torch.arange(batch * width, dtype=torch.int32, device=device).view(batch, width)
         self.seq_lens = torch.zeros(batch, dtype=torch.int32, device=device)
         self.tokens_upper = 0               # no sequence holds more tokens than this (host-side bound)
-        self._ws = _Workspace(device)
+        self._ws = _Workspace.made_or_shared(self.cache.device, workspace_of, LatentKVLayer, "_ws")
 
     def append(self, latent: torch.Tensor, k_rot: torch.Tensor, starts: Optional[torch.Tensor] = None, max_rows: int = 1,
                q: Optional[torch.Tensor] = None, q_out: Optional[torch.Tensor] = None, rotary: Optional[Rotary] = None,

@@ -289,9 +289,9 @@ def paged_tree_attention(cache: PagedCache, q: torch.Tensor, k: torch.Tensor, v:
     """Attention of drafted rows that are not in the cache (dq_paged_tree_attention): q [rows, q_heads, d] over the seq_lens cached tokens of
     their sequences and over those drafted rows k, v [rows, kv_heads, d] (rotated by their places) that `seen` names: int64, a mask for
     each row, bit j its sequence's j-th row (the row itself and its ancestors).  A sequence has at most 64 rows, max_rows at most;
-    further ones are not seen and not written.  max_seq_len is not looked at.  window > 0 (64 at least): of the cached tokens only those less than `window` before a row's
-    place, which is seq_lens plus the rows it sees, less one.  Accepted rows are appended afterwards, refused ones leave nothing.  out
-    may be q itself, and shares no memory with the others.  No gradients."""
+    further ones are not seen and not written.  max_seq_len is not looked at.  window > 0 (64 at least): of the cached tokens only those
+    less than `window` before a row's place, which is seq_lens plus the rows it sees, less one.  Accepted rows are appended afterwards,
+    refused ones leave nothing.  out may be q itself, and shares no memory with the others.  No gradients."""
     if out is None:
         out = torch.empty(q.shape, dtype=q.dtype, device=q.device)
     index = cache.index
@@ -301,10 +301,23 @@ def paged_tree_attention(cache: PagedCache, q: torch.Tensor, k: torch.Tensor, v:
 
 
 class _Workspace:
-    """A layer's workspace for calls whose kernels need no zeros in it: grows with the calls, and stays where graphs were captured with it."""
+    """A layer's workspace, or that of several, for calls whose kernels need no zeros in it: grows with the calls, and stays where graphs were captured
+    with it."""
 
     def __init__(self, device):
         self.device, self.ws, self.outgrown = device, None, []
+
+    @classmethod
+    def made_or_shared(cls, device, layer, kind, name: str) -> "_Workspace":
+        """A new one, or the one that `layer` has as `name`."""
+        if layer is None:
+            return cls(device)
+        if not isinstance(layer, kind):
+            raise DQError("workspace_of must be another %s" % kind.__name__)
+        shared = getattr(layer, name)
+        if shared.device != device:
+            raise DQError("a layer on %s cannot work in the workspace of one on %s" % (device, shared.device))
+        return shared
 
     def of(self, need: int) -> torch.Tensor:
         if self.ws is not None and need <= self.ws.numel():
@@ -324,11 +337,12 @@ class PagedKVLayer:
     max_tokens tokens, each with its own pages and tail, the lengths on the device.  Rows come packed, sequence by
     sequence (`starts`, int32 [batch + 1]; None: one row each); the host tracks only bounds, which size the launches.
     Replays of a captured step count on the device only: add their rows to tokens_upper (which refuses what is too much;
-    rows of replays past max_tokens' pages are left out).
+    rows of replays past max_tokens' pages are left out).  workspace_of: another layer, in whose workspace of attend_tree (17 to 68 MB, by the
+    columns) this one works too, where their calls are ordered, as a model's layers' are.
     (Loops with a page allocator of their own call paged_append and paged_attention.)"""
 
     def __init__(self, batch: int, q_heads: int, kv_heads: int, head_dim: int, max_tokens: int, page_tokens: int = 64,
-                 dtype=torch.float16, codes=torch.int8, device="cuda:0"):
+                 dtype=torch.float16, codes=torch.int8, device="cuda:0", workspace_of: Optional["PagedKVLayer"] = None):
         if min(batch, max_tokens, q_heads, kv_heads) < 1 or q_heads % kv_heads or page_tokens not in (64, 128):
             raise DQError("a layer has sequences, room for tokens, q_heads a multiple of kv_heads and pages of 64 or 128 tokens")
         self.batch, self.q_heads, self.max_tokens = batch, q_heads, max_tokens
@@ -338,7 +352,7 @@ class PagedKVLayer:
         self.seq_lens = torch.zeros(batch, dtype=torch.int32, device=device)
         self.tokens_upper = 0               # no sequence holds more tokens than this (host-side bound)
         self._ws, self._outgrown = None, []
-        self._tree_ws = _Workspace(device)
+        self._tree_ws = _Workspace.made_or_shared(self.cache.device, workspace_of, PagedKVLayer, "_tree_ws")
 
     def append(self, k: torch.Tensor, v: torch.Tensor, starts: Optional[torch.Tensor] = None, max_rows: int = 1,
                q: Optional[torch.Tensor] = None, rotary: Optional[Rotary] = None, positions: Optional[torch.Tensor] = None,

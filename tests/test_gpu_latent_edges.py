@@ -111,3 +111,49 @@ def test_sums_over_a_million_tokens(latent, heads):
     v_max = float(x.rows[0][:, :latent].double().abs().max())
     tol = tolerance(o, size, ds, v_max, 2048, torch.float16) + size * 3 * 2.0 ** -14
     assert bool(((got - o).abs() <= tol).all())
+
+
+def test_layers_that_share_a_workspace():
+    """A model's layers one after the other, eagerly and in a captured step, while a larger call of one outgrows what they share: as layers with
+    workspaces of their own."""
+    gen = torch.Generator().manual_seed(40)
+    heads, n = 16, 3
+    first = dq.LatentKVLayer(2, heads, 300)
+    shared, alone = [first] + [dq.LatentKVLayer(2, heads, 300, workspace_of=first) for _ in range(n - 1)], [dq.LatentKVLayer(2, heads, 300) for _ in range(n)]
+    rows, q = normal((n, 2, 576), torch.bfloat16, gen).to(DEV), normal((n, 2, heads, 576), torch.bfloat16, gen).to(DEV)
+    out, want = (torch.zeros((n, 2, heads, 512), dtype=torch.bfloat16, device=DEV) for _ in range(2))
+
+    def step(layers, out):
+        for i, layer in enumerate(layers):
+            layer.append(rows[i, :, :512], rows[i, :, 512:])
+            layer.attend(q[i], 0.07, out=out[i])
+
+    side = torch.cuda.Stream()
+    side.wait_stream(torch.cuda.current_stream())
+    with torch.cuda.stream(side):
+        step(shared, out)
+    torch.cuda.current_stream().wait_stream(side)
+    step(alone, want)
+    assert torch.equal(out, want) and len({layer._ws.ws.data_ptr() for layer in shared}) == 1
+    graph = torch.cuda.CUDAGraph()
+    with torch.cuda.graph(graph):
+        step(shared, out)
+    for layer in shared:
+        layer.tokens_upper -= 1                                     # (the capture itself appended nothing)
+    big, big_q, starts = normal((80, 576), torch.bfloat16, gen).to(DEV), normal((80, heads, 576), torch.bfloat16, gen).to(DEV), ints([0, 40, 80])
+    for layers in (shared, alone):
+        layers[1].append(big[:, :512], big[:, 512:], starts, 40)
+    assert torch.equal(shared[1].attend(big_q, 0.07, starts, 40), alone[1].attend(big_q, 0.07, starts, 40))
+    for i in range(4):
+        rows.copy_(normal(rows.shape, torch.bfloat16, gen))
+        graph.replay()
+        step(alone, want)
+        torch.cuda.synchronize()
+        assert torch.equal(out, want), i
+        for layer in shared:
+            layer.tokens_upper += 1
+    step(shared, out)
+    step(alone, want)
+    assert torch.equal(out, want)
+    with pytest.raises(dq.DQError, match="workspace_of"):
+        dq.LatentKVLayer(2, heads, 300, workspace_of=dq.PagedKVLayer(1, 4, 4, 64, 100))

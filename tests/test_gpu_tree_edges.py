@@ -53,3 +53,19 @@ def test_the_bound_on_lengths_is_not_looked_at(most):
     first = x.run()
     for n in (0, 1, 64, 700, 1 << 30):
         assert torch.equal(x.run(max_len=n), first), n
+
+
+def test_layers_that_share_a_workspace():
+    gen = torch.Generator().manual_seed(41)
+    first = dq.PagedKVLayer(2, 4, 2, 64, 300, dtype=BF)
+    layers = [first, dq.PagedKVLayer(2, 4, 2, 64, 300, dtype=BF, workspace_of=first), dq.PagedKVLayer(2, 4, 2, 64, 300, dtype=BF)]
+    for most in (3, 30):                                            # the second call outgrows the first one's
+        q, k, v = (torch.randn((2 * most, n, 64), generator=gen).to(BF).to(DEV) for n in (4, 2, 2))
+        starts, seen = ints([0, most, 2 * most]), torch.tensor([(1 << i + 1) - 1 for i in range(most)] * 2, device=DEV)
+        outs = []
+        for layer in layers:
+            layer.append(k, v, starts, most)
+            outs.append(layer.attend_tree(q, k, v, seen, starts, most))
+        assert torch.equal(outs[0], outs[1]) and torch.equal(outs[0], outs[2])
+        ws = [layer._tree_ws.ws.data_ptr() for layer in layers]
+        assert ws[0] == ws[1] != ws[2]

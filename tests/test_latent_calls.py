@@ -156,3 +156,24 @@ def test_keys_of_no_tokens_have_no_address():
     for none in (dict(k=0), dict(v=0), dict(k_rot=0)):
         assert call(100, **none) == -1 and call(0, **none) == -3
     assert call(0, out=0) == -1 and call(100, out=0) == -1
+
+
+def test_a_workspace_is_shared_by_layers_of_a_kind_on_a_device():
+    import paper_2405_12591_amd as dq
+    from paper_2405_12591_amd.paged import _Workspace
+
+    class Layer:
+        _ws = _Workspace(torch.device("cpu"))
+
+    class Other:
+        _ws = _Workspace(torch.device("cpu"))
+
+    make = _Workspace.made_or_shared
+    assert make(torch.device("cpu"), Layer(), Layer, "_ws") is Layer._ws
+    alone = make(torch.device("cpu"), None, Layer, "_ws")
+    assert alone is not Layer._ws and alone.ws is None
+    for device, layer in (("cpu", Other()), ("cpu", "a layer"), ("meta", Layer())):
+        with pytest.raises(dq.DQError, match="workspace"):
+            make(torch.device(device), layer, Layer, "_ws")
+    small = Layer._ws.of(100)
+    assert Layer._ws.of(50) is small and Layer._ws.of(101).numel() >= 200 and Layer._ws.outgrown == [small]
