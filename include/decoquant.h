@@ -590,8 +590,8 @@ typedef struct dq_latent_cache {
  * token's place in its sequence); both in fp32 and rounded once.  q (NULL: none), heads [rows, q_heads, rot_dim], the
  * queries' channels that meet k_rot, takes the same rotation in the same launch, into q_out (q itself, with the same
  * strides, will do; it shares no channel with the others).
- * A row with a value that is not finite after that is kept as zeros with k_rot of NaN: a query that sees the token yields
- * NaN, the others are untouched.  Rows of a page that does not exist are dropped.  Lengths may go back at will.
+ * A row with a value that is not finite after that is kept with k_rot of NaN, and with c of zeros where c is not finite: a query that sees
+ * the token yields NaN, the others are untouched.  (Programs that write rows of their own into the pages keep to that.)  Rows of a page that does not exist are dropped.  Lengths may go back at will.
  */
 int32_t dq_latent_append(const dq_latent_cache* cache, const dq_paged_batch* batch, const uint16_t* latent,
                          int64_t latent_stride, const uint16_t* k_rot, int64_t k_rot_stride, const uint16_t* weight,

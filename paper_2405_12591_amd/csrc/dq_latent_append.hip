@@ -134,15 +134,14 @@ __global__ __launch_bounds__(256) void latent_append_kernel(LatentAppendArgs a) 
   } else if (live) {
     u32x4 none[2] = {};
     ready_unit<T, LANES, INTERLEAVED>(v, none, false, l.pair0 >= 0, 0.f, 0.f, cs, sn);
-    // Key channels that came or were turned out of the type's range count as the latent's do: an infinite score would
-    // hide the token from half of the queries.  (A row's lanes are here together.)
-    const bool any = (__ballot(not_finite<T>(v[0]) || not_finite<T>(v[1])) >> (lane / LANES * LANES) & ((1u << LANES) - 1)) != 0;
-    uint16_t* const to = a.c.rows + s_row[r] * W;
-    if (any)
-      for (int e = 8 * unit; e < R; e += 8 * LANES) *reinterpret_cast<u32x4*>(to + e) = u32x4{0, 0, 0, 0};   // (behind the latent's own store: the barrier)
-    if (any || s_bad[r]) v[0] = v[1] = kNanPiece;
-    *reinterpret_cast<u32x4*>(to + R + l.at0) = v[0];
-    *reinterpret_cast<u32x4*>(to + R + l.at1) = v[1];
+    // Key channels that came or were turned out of the type's range count as the latent's do: an infinite score would hide the token from
+    // half of the queries.  (A row's lanes are here together.  Its latent is finite, and stays: zeros over it, whose stores no row
+    // comes to, took 1.1 us of 62 for 28 thousand rows.)
+    const uint64_t lanes = __ballot(not_finite<T>(v[0]) || not_finite<T>(v[1]));
+    if (s_bad[r] || (lanes >> (lane / LANES * LANES) & ((1u << LANES) - 1))) v[0] = v[1] = kNanPiece;
+    uint16_t* const to = a.c.rows + s_row[r] * W + R;
+    *reinterpret_cast<u32x4*>(to + l.at0) = v[0];
+    *reinterpret_cast<u32x4*>(to + l.at1) = v[1];
   }
 }
 

@@ -55,8 +55,8 @@ def test_key_channels_that_are_not_finite_are_nan_for_those_who_see_them_only(dt
     read = torch.zeros((14, latent + rot), dtype=dtype, device=DEV)
     dq.latent_read(x.cache, ints([60, 60]), ints(lens), ints(starts_of(counts)), x.table.to(DEV), read)
     others = [i for i in range(14) if i not in (5, 11)]
-    assert torch.equal(read[others, :latent], new[others, :latent]) and bool(read[others].isfinite().all())
-    assert not read[[5, 11], :latent].any() and bool(read[[5, 11], latent:].isnan().all())
+    assert torch.equal(read[:, :latent], new[:, :latent]) and bool(read[others].isfinite().all())
+    assert bool(read[[5, 11], latent:].isnan().all())
     read = read.cpu()
     read[[5, 11]] = 1.0
     x.rows[0][60:], x.rows[1][60:] = read[:10], read[10:]
