@@ -75,6 +75,9 @@ __device__ __forceinline__ uint64_t in_scalars(const void* p) {
 // their own: the compiler waits for all such copies ahead of every LDS read, the ones for later tiles too.  Kernels count
 // them themselves (no register is written; a wait that counts too many of them waits longer).
 // once: past the caches' order (rows that one workgroup reads: a cache of 378 MB in 80 us, 89 without).
+// (m0 is declared as written, so that the compiler carries no setting of its own across.  Its warning, that m0 is not preserved, is meant so.)
+#pragma clang diagnostic push
+#pragma clang diagnostic ignored "-Winline-asm"
 template <bool once = false> __device__ __forceinline__ void copy_to_lds(const uint16_t* base, uint32_t offset, uint32_t lds) {
   if constexpr (once) {
     asm volatile("s_mov_b32 m0, %0\n\ts_nop 0\n\tglobal_load_lds_dwordx4 %1, %2 nt" ::"s"(__builtin_amdgcn_readfirstlane(lds)), "v"(offset), "s"(in_scalars(base)) : "m0", "memory");
@@ -85,6 +88,7 @@ template <bool once = false> __device__ __forceinline__ void copy_to_lds(const u
 __device__ __forceinline__ void copy_to_lds(const uint16_t* from, uint32_t lds) {
   asm volatile("s_mov_b32 m0, %0\n\ts_nop 0\n\tglobal_load_lds_dwordx4 %1, off" ::"s"(__builtin_amdgcn_readfirstlane(lds)), "v"(from) : "m0", "memory");
 }
+#pragma clang diagnostic pop
 // Waits for all of the wave's copies but the newest N; for the workgroup's other waves.  As instructions that no LDS read passes (the
 // compiler moves reads across the barrier builtin), its result no less: what was read may be copied over from then on.
 template <int N> __device__ __forceinline__ void wait_copies() { asm volatile("s_waitcnt vmcnt(%0)" ::"i"(N) : "memory"); }
