@@ -407,7 +407,8 @@ typedef struct dq_rotary {
   const double* inv_freq;      /* f64 [rot_dim / 2], radians per position; angles stay below 2^50     */
   const int32_t* positions;    /* i32 [axes, position_stride]; a token's column is its place among all
                                   rows of the call (sequence by sequence); any value.
-                                  NULL (dq_paged_append only, one axis): a token's place in its sequence */
+                                  NULL (dq_paged_append, dq_latent_append, one axis): a token's place in
+                                  its sequence */
   const uint8_t* axis_of_pair; /* u8 [rot_dim / 2]: the axis whose position turns pair i (time, height,
                                   width, ...); NULL with one axis; values >= axes count as the last    */
   int64_t position_stride;     /* >= the rows of the call where axes > 1                              */

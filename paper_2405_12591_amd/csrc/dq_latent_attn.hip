@@ -554,7 +554,8 @@ __global__ __launch_bounds__(256) void latent_join_kernel(LatentArgs a) {
 
 // Columns of a workgroup: the fewest that hold a sequence's (row, head) pairs, 128 where there are more, since every tile of columns reads the
 // tokens again: 16 sequences of 14 thousand tokens with 128 heads 120 us in 128, 156 in 64, 231 in 32; 24 drafted rows of 32 heads behind 8 x 7
-// thousand 152, 221, 337; 64 sequences with 16 heads 85 us in the narrow kernel's 16, 91 in 32.
+// thousand 152, 221, 337; 64 sequences with 16 heads 85 us in the narrow kernel's 16, 91 in 32.  What each takes of its own: 64 sequences of 2000 to
+// 8192 tokens with 16, 32 and 64 heads 84, 102 and 131 us.
 struct LatentPlan {
   int cols;                // of a workgroup
   long items, workgroups;
@@ -566,7 +567,7 @@ static bool latent_plan(int batch, long rows, int heads, int max_rows, int max_s
   p->cols = cols <= 16 ? 16 : cols <= 32 ? 32 : cols <= 64 ? 64 : 128;
   p->items = rows * heads / p->cols + batch;
   if (p->items * (p->cols / kJoinColumns<512>) >= kMaxThreads / 256) return false;
-  p->workgroups = 256;                                    // a compute unit's LDS holds one
+  p->workgroups = 256;   // a compute unit's LDS holds one (two of 256 channels and up to 32 columns, which are launched as one all the same)
   return true;
 }
 static size_t latent_bytes(const dq_latent_cache* c, const LatentPlan& p) {
